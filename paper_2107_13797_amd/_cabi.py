@@ -86,6 +86,27 @@ PEAK_PROTOTYPES = {
     "haflo_peak_limbs": (c_int, [c_int, C.POINTER(c_u32), C.POINTER(c_u32)]),
     "haflo_peak_montmul_chain": (c_int, [c_int, c_void_p, c_void_p, c_void_p, c_u64, c_int, c_void_p, c_size_t, c_void_p]),
 }
+# include/haflo_local.h (libhaflo.so)
+c_double = C.c_double
+LOCAL_PROTOTYPES = {
+    "haflo_dropout": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_size_t, c_size_t, c_size_t,
+                              c_double, c_u64, c_u64, c_void_p]),
+    "haflo_adapter_workspace_bytes": (c_size_t, [c_int, c_int, c_size_t, c_size_t, c_size_t, c_size_t, c_size_t]),
+    "haflo_adapter_forward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_size_t, c_size_t, c_size_t, c_size_t, c_size_t, c_double, c_u64, c_u64, c_void_p,
+                                      c_size_t, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "haflo_adapter_backward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_size_t, c_size_t, c_size_t, c_size_t, c_size_t,
+                                       c_double, c_u64, c_u64, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_size_t, c_void_p]),
+    "haflo_label_workspace_bytes": (c_size_t, [c_int, c_size_t, c_size_t, c_size_t]),
+    "haflo_label_logprobs": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_size_t, c_size_t, c_void_p, c_void_p,
+                                     c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "haflo_label_logprobs_backward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                              c_void_p, c_void_p, c_size_t, c_size_t, c_size_t, c_void_p, c_size_t,
+                                              c_void_p]),
+}
+TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
 LIMBS_29_MAD64, LIMBS_29_MAD64_SQUARE, LIMBS_24_MUL24, LIMBS_23_FMA64 = 0, 1, 2, 3
 PEAK_MAD_U64_U32, PEAK_MUL_LO_HI, PEAK_MUL_U24, PEAK_FMA_F64, PEAK_ADD_U32 = 0, 1, 2, 3, 4
 PEAK_FILL, PEAK_COPY, PEAK_READ = 0, 1, 2

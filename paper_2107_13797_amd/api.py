@@ -1,4 +1,4 @@
-"""Thin binding over the C boundary of libhaflo (include/haflo.h).
+"""Thin binding over the C boundary of libhaflo (include/haflo.h, include/haflo_local.h).
 
 Same names as the C entry points, argument marshalling only: tensors are
 allocated with torch on the current CUDA(HIP) device, their data pointers and
@@ -30,7 +30,7 @@ def lib():
             raise HafloError(
                 "libhaflo.so is missing: build it with `python -m paper_2107_13797_amd.build` "
                 "(there is no CPU fallback)")
-        _lib = _cabi.bind(C.CDLL(_LIB_PATH))
+        _lib = _cabi.bind(_cabi.bind(C.CDLL(_LIB_PATH)), prototypes=_cabi.LOCAL_PROTOTYPES)
     return _lib
 
 
@@ -323,6 +323,148 @@ def haflo_cipher_sum_segments(ctx, c, offsets, status=None):
     ws = _workspace(ctx, _cabi.OP_SUM_SEGMENTS, count, nseg)
     _check(lib().haflo_cipher_sum_segments(ctx.handle, _ptr(c) if count else None, count, _ptr(offsets), nseg,
                                            _ptr(out) if nseg else None, _ptr(status), _ptr(ws), ws.numel(), _stream()))
+    return out
+
+
+# The operators of a party's local step (include/haflo_local.h) work on ordinary float32, float16 and bfloat16 tensors and
+# need no Context; their workspaces come from torch's allocator call by call, in the current stream's order.
+_TYPES = {torch.float32: _cabi.TYPE_F32, torch.float16: _cabi.TYPE_F16, torch.bfloat16: _cabi.TYPE_BF16}
+
+
+def _type(t):
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise HafloError("expected float32, float16 or bfloat16, got %s" % t.dtype) from None
+
+
+def _matrix(t, like=None, rows=None, cols=None):
+    """Distance between the rows of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or (like is not None and t.dtype != like.dtype):
+        raise HafloError("expected a CUDA matrix" + (" of %s" % like.dtype if like is not None else ""))
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise HafloError("expected a matrix of %s x %s, got %s" % (rows, cols, tuple(t.shape)))
+    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise HafloError("expected rows of contiguous elements that do not overlap")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _dense(t, dtype, *shape):
+    """Address of a contiguous tensor of that type and shape."""
+    if t.dtype != dtype or t.shape != shape:
+        raise HafloError("expected %s of shape %s, got %s of %s" % (dtype, shape, t.dtype, tuple(t.shape)))
+    return _ptr(t)
+
+
+def _optional(t, dtype, *shape):
+    return None if t is None else _dense(t, dtype, *shape)
+
+
+def _scratch(nbytes):
+    if nbytes == 2 ** 64 - 1:
+        raise HafloError("sizes out of range")
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
+    """x / (1 - p) where the generator keeps an element, 0 elsewhere, plus `residual`. The gradient by x is the same call on the
+    gradient of the result, without a residual. A vector counts as one row; `out` may be x or the residual."""
+    if x.dim() == 1:
+        y = haflo_dropout(x[None], p, seed, offset, None if residual is None else residual[None], None if out is None else out[None])
+        return y[0] if out is None else out
+    kind, ldx = _type(x), _matrix(x)
+    rows, cols = x.shape
+    ldr = 0 if residual is None else _matrix(residual, x, rows, cols)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    _check(lib().haflo_dropout(kind, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, out.data_ptr(),
+                               _matrix(out, x, rows, cols), rows, cols, p, seed, offset, _stream()))
+    return out
+
+
+def haflo_adapter_forward(x, w, a, b, scale, index, p=0.0, seed=0, offset=0, status=None):
+    """y = x w^T + h b[index]^T, h = scale[index] drop(x) a[index]^T, row by row: the projection that all parties share with each
+    row's own adapter (index int32, -1: none). x [rows, inner], w [outer, inner], a [parties, rank, inner],
+    b [parties, outer, rank], scale float32 [parties]. Returns y and, for the backward pass, h (float32 [rows, rank])."""
+    kind, ldx = _type(x), _matrix(x)
+    rows, inner = x.shape
+    if a.dim() != 3:
+        raise HafloError("a: parties x rank x inner")
+    parties, rank = a.shape[0], a.shape[1]
+    ldw = _matrix(w, x, None, inner)
+    outer = w.shape[0]
+    pa, pb = _dense(a, x.dtype, parties, rank, inner), _dense(b, x.dtype, parties, outer, rank)
+    ps, pi = _dense(scale, torch.float32, parties), _dense(index, torch.int32, rows)
+    y = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
+    h = torch.empty((rows, rank), dtype=torch.float32, device=x.device)
+    nbytes = lib().haflo_adapter_workspace_bytes(kind, 0, rows, inner, outer, parties, rank)
+    ws = _scratch(nbytes)
+    _check(lib().haflo_adapter_forward(kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, rows, inner, outer, parties, rank,
+                                       p, seed, offset, y.data_ptr(), outer, h.data_ptr(), _ptr(status),
+                                       None if ws is None else ws.data_ptr(), nbytes, _stream()))
+    return y, h
+
+
+def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offset=0, need_dx=True, status=None):
+    """Gradients of haflo_adapter_forward by x (None without need_dx) and, float32 as haflo_encode_f32 takes them, by a and b; for the
+    forward call's arguments and its h."""
+    kind, ldx = _type(x), _matrix(x)
+    rows, inner = x.shape
+    if a.dim() != 3:
+        raise HafloError("a: parties x rank x inner")
+    parties, rank = a.shape[0], a.shape[1]
+    ldw = _matrix(w, x, None, inner)
+    outer = w.shape[0]
+    lddy = _matrix(dy, x, rows, outer)
+    pa, pb = _dense(a, x.dtype, parties, rank, inner), _dense(b, x.dtype, parties, outer, rank)
+    ps, pi, ph = _dense(scale, torch.float32, parties), _dense(index, torch.int32, rows), _dense(h, torch.float32, rows, rank)
+    dx = torch.empty((rows, inner), dtype=x.dtype, device=x.device) if need_dx else None
+    da = torch.empty((parties, rank, inner), dtype=torch.float32, device=x.device)
+    db = torch.empty((parties, outer, rank), dtype=torch.float32, device=x.device)
+    nbytes = lib().haflo_adapter_workspace_bytes(kind, 1, rows, inner, outer, parties, rank)
+    ws = _scratch(nbytes)
+    _check(lib().haflo_adapter_backward(kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, ph, rows,
+                                        inner, outer, parties, rank, p, seed, offset, dx.data_ptr() if need_dx else None, inner,
+                                        da.data_ptr(), db.data_ptr(), _ptr(status), ws.data_ptr(), nbytes, _stream()))
+    return dx, da, db
+
+
+def haflo_label_logprobs(logits, label, top=0, status=None):
+    """Row by row under softmax(logits): the label's log-probability (int32 label, -1: none, gives 0), the entropy, the logarithm of the
+    exponentials' sum, and the `top` greatest logits' log-probabilities and columns (None for top = 0), ties to the lowest."""
+    kind, ld = _type(logits), _matrix(logits)
+    rows, cols = logits.shape
+    pl = _dense(label, torch.int32, rows)
+    logp, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=logits.device).unbind()
+    top_logp = top_index = None
+    nbytes = lib().haflo_label_workspace_bytes(kind, rows, cols, top)
+    ws = _scratch(nbytes)
+    if top:
+        top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
+        top_index = torch.empty((rows, top), dtype=torch.int32, device=logits.device)
+    _check(lib().haflo_label_logprobs(kind, logits.data_ptr(), ld, pl, rows, cols, top, logp.data_ptr(), entropy.data_ptr(),
+                                      lse.data_ptr(), _ptr(top_logp), _ptr(top_index), _ptr(status),
+                                      None if ws is None else ws.data_ptr(), nbytes, _stream()))
+    return logp, entropy, lse, top_logp, top_index
+
+
+def haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dentropy=None, top_index=None, dtop=None, out=None):
+    """Gradient by the logits from the forward call's results and the gradients of its logp, entropy and top_logp. `out` may be
+    the logits."""
+    kind, ld = _type(logits), _matrix(logits)
+    rows, cols = logits.shape
+    top = 0 if dtop is None else dtop.shape[-1]
+    f32 = torch.float32
+    args = [_dense(label, torch.int32, rows), _dense(lse, f32, rows), _dense(entropy, f32, rows), _dense(dlogp, f32, rows),
+            _optional(dentropy, f32, rows), None, None]
+    if dtop is not None:
+        if top_index is None:
+            raise HafloError("dtop needs top_index")
+        args[5:] = _dense(top_index, torch.int32, rows, top), _dense(dtop, f32, rows, top)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
+    _check(lib().haflo_label_logprobs_backward(kind, logits.data_ptr(), ld, *args, rows, cols, top, out.data_ptr(),
+                                               _matrix(out, logits, rows, cols), _stream()))
     return out
 
 

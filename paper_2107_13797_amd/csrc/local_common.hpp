@@ -1,0 +1,150 @@
+// Helpers shared by the operators of a party's local step: element types, the dropout generator, wavefront
+// reductions, matrix instructions.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/haflo_local.h"
+
+namespace haflo {
+namespace local {
+
+using u16 = uint16_t;
+using u32 = uint32_t;
+using u64 = uint64_t;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWave = 64;
+constexpr size_t kMostCount = 0x7FFFFFFF;
+
+// Eight consecutive elements, the unit of loads, stores and of a dropout call.
+template <class T>
+struct Vec8 {
+  T v[8];
+};
+template <class T>
+constexpr int vec_words() {
+  return (int)sizeof(T) * 2;  // 32-bit words of eight elements
+}
+
+// Whether eight elements at a multiple of eight from `p`, rows `ld` apart, can be moved 16 bytes at a time.
+template <class T>
+inline bool wide_rows(const void* p, size_t ld) {
+  return ((uintptr_t)p & 15) == 0 && (ld * sizeof(T)) % 16 == 0;
+}
+
+template <class T>
+__device__ __forceinline__ Vec8<T> load_wide(const T* p) {  // 16-byte aligned
+  Vec8<T> r;
+  __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), sizeof(r));
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store_wide(T* p, const Vec8<T>& v) {
+  __builtin_memcpy(__builtin_assume_aligned(p, 16), &v, sizeof(v));
+}
+// The first `n` of eight elements; the others are zero.
+template <class T>
+__device__ __forceinline__ Vec8<T> load_some(const T* p, int n) {
+  Vec8<T> r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (T)0.0f;
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store_some(T* p, const Vec8<T>& v, int n) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < n) p[j] = v.v[j];
+}
+
+// The dropout of one call: what a kernel needs of (p, seed, offset).
+struct Drop {
+  u32 threshold;  // draws below it drop their element; 0: no dropout
+  float scale;
+  u32 k0, k1, o0, o1;
+};
+inline Drop make_drop(double p, u64 seed, u64 offset) {
+  Drop d;
+  d.threshold = (u32)__builtin_rint(p * 65536.0);
+  d.scale = d.threshold >= 65536u ? 0.0f : (float)(65536.0 / (65536.0 - (double)d.threshold));
+  d.k0 = (u32)seed;
+  d.k1 = (u32)(seed >> 32);
+  d.o0 = (u32)offset;
+  d.o1 = (u32)(offset >> 32);
+  return d;
+}
+// Philox4x32-10: ten rounds of two 32 x 32 -> 64-bit products.
+__device__ __forceinline__ u32x4 philox(const Drop& d, u32 group, u32 row) {
+  u32 c0 = group, c1 = row, c2 = d.o0, c3 = d.o1, k0 = d.k0, k1 = d.k1;
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const u64 x = (u64)c0 * 0xD2511F53u, y = (u64)c2 * 0xCD9E8D57u;
+    c0 = (u32)(y >> 32) ^ c1 ^ k0;
+    c1 = (u32)y;
+    c2 = (u32)(x >> 32) ^ c3 ^ k1;
+    c3 = (u32)x;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  u32x4 r = {c0, c1, c2, c3};
+  return r;
+}
+__device__ __forceinline__ bool kept(const Drop& d, const u32x4& draws, int j) {
+  return ((draws[j >> 1] >> (16 * (j & 1))) & 0xFFFFu) >= d.threshold;
+}
+
+__device__ __forceinline__ u32 lane_id() { return threadIdx.x & (kWave - 1); }
+__device__ __forceinline__ u32 lane_read(u32 v, int lane) {
+  return (u32)__builtin_amdgcn_ds_bpermute(lane << 2, (int)v);
+}
+__device__ __forceinline__ float lane_read(float v, int lane) {
+  return __builtin_bit_cast(float, lane_read(__builtin_bit_cast(u32, v), lane));
+}
+__device__ __forceinline__ u64 lane_read(u64 v, int lane) {
+  const u32 lo = lane_read((u32)v, lane), hi = lane_read((u32)(v >> 32), lane);
+  return (u64)hi << 32 | lo;
+}
+
+// acc += a b on 16 x 16 by 32: lane l holds rows l % 16 of both operands at elements 8 (l / 16) .. + 7, and in
+// acc[r] row 4 (l / 16) + r of the first operand against row l % 16 of the second.
+__device__ __forceinline__ f32x4 mma32(const Vec8<__bf16>& a, const Vec8<__bf16>& b, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma32(const Vec8<_Float16>& a, const Vec8<_Float16>& b, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+// the same in 32 bits: each instruction takes one element of every lane, so that element j of lane group g stands for
+// the reduction's place 8 g + j in both operands alike
+__device__ __forceinline__ f32x4 mma32(const Vec8<float>& a, const Vec8<float>& b, f32x4 acc) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], acc, 0, 0, 0);
+  return acc;
+}
+
+inline bool valid_type(int type) { return type == HAFLO_F32 || type == HAFLO_F16 || type == HAFLO_BF16; }
+inline size_t type_size(int type) { return type == HAFLO_F32 ? 4 : 2; }
+inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
+inline int launched() { return hipGetLastError() == hipSuccess ? HAFLO_OK : HAFLO_EHIP; }
+
+}  // namespace local
+}  // namespace haflo
+
+// Calls BODY with T as the element type that `type` names.
+#define HAFLO_LOCAL_TYPES(type, ...)         \
+  do {                                       \
+    if ((type) == HAFLO_F32) {               \
+      using T = float;                       \
+      __VA_ARGS__;                           \
+    } else if ((type) == HAFLO_F16) {        \
+      using T = _Float16;                    \
+      __VA_ARGS__;                           \
+    } else {                                 \
+      using T = __bf16;                      \
+      __VA_ARGS__;                           \
+    }                                        \
+  } while (0)

@@ -1,0 +1,440 @@
+// Log-probabilities of labels with entropy and top alternatives, and their gradient by the logits.
+//
+// One pass over a row keeps, per lane, the running maximum m, s = sum e^(x - m) and t = sum e^(x - m) (x - m); then
+// lse = m + ln s and the entropy is ln s - t / s. Two such states join by rescaling the one with the smaller maximum.
+// The greatest elements are kept as one descending list per wavefront, entry j in lane j; an element is the 64-bit key
+// (value in an order-preserving form, complement of its column), so that the larger key is the greater value or, of equal
+// ones, the lower column, and the list does not depend on the order in which elements come.
+#include "local_common.hpp"
+
+using namespace haflo::local;
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr size_t kSmallCols = 32;    // up to here a lane takes a row by itself
+constexpr size_t kWaveCols = 2048;   // up to here a wavefront does
+constexpr size_t kSplitCols = 2048;  // columns of one part of a row, at least
+constexpr size_t kSplitBlocks = 1024;
+constexpr int kAhead = 4;            // vectors on their way at a time
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+struct Soft {
+  float m, s, t;
+};
+__device__ __forceinline__ float shift_of(float m) { return m == neg_inf() ? 0.0f : m; }  // what exponents are taken relative to
+__device__ __forceinline__ void raise_to(Soft& a, float m) {                              // m >= a.m
+  const float by = a.m - shift_of(m), c = __builtin_amdgcn_exp2f(by * kLog2e);
+  if (a.s != 0.0f) {
+    a.t = c == 0.0f ? 0.0f : c * (a.t + by * a.s);
+    a.s *= c;
+  }
+  a.m = m;
+}
+__device__ __forceinline__ void join(Soft& a, Soft b) {
+  const float m = __builtin_fmaxf(a.m, b.m);
+  if (a.m < m) raise_to(a, m);
+  if (b.m < m) raise_to(b, m);
+  a.s += b.s;
+  a.t += b.t;
+}
+__device__ __forceinline__ Soft wave_join(Soft a) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int from = (int)(lane_id() ^ d);
+    Soft b;
+    b.m = lane_read(a.m, from);
+    b.s = lane_read(a.s, from);
+    b.t = lane_read(a.t, from);
+    // both lanes of a pair join in the same order, so that they hold the same bits
+    if (lane_id() & d) {
+      join(b, a);
+      a = b;
+    } else {
+      join(a, b);
+    }
+  }
+  return a;
+}
+
+__device__ __forceinline__ u64 key_of(float x, u32 col) {
+  u32 b = __builtin_bit_cast(u32, x);
+  if (x == 0.0f) b = 0;  // zeros of both signs are equal
+  u32 k = b & 0x80000000u ? ~b : b | 0x80000000u;
+  if (x != x) k = 0xFFFFFFFFu;
+  return (u64)k << 32 | (u32)~col;
+}
+__device__ __forceinline__ float value_of(u64 key) {
+  const u32 k = (u32)(key >> 32);
+  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+struct TopList {
+  u64 mine;  // this lane's entry, 0: none
+  u64 last;  // entry top - 1, the same in all lanes
+};
+// key_lane's `key` into the list, which it belongs into
+__device__ __forceinline__ void top_insert(TopList& l, u64 key, int key_lane, int top) {
+  const u32 lo = (u32)__builtin_amdgcn_readlane((int)(u32)key, key_lane);
+  const u32 hi = (u32)__builtin_amdgcn_readlane((int)(u32)(key >> 32), key_lane);
+  const u64 k = (u64)hi << 32 | lo;
+  const int place = __builtin_popcountll(__builtin_amdgcn_ballot_w64(l.mine > k));
+  // every lane's entry to the next lane
+  const u32 plo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)l.mine, 0x138, 0xF, 0xF, false);
+  const u32 phi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(l.mine >> 32), 0x138, 0xF, 0xF, false);
+  const int lane = (int)lane_id();
+  if (lane > place) l.mine = (u64)phi << 32 | plo;
+  if (lane == place) l.mine = k;
+  l.last = (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(l.mine >> 32), top - 1) << 32 |
+           (u32)__builtin_amdgcn_readlane((int)(u32)l.mine, top - 1);
+}
+// Two descending lists to the 64 greatest of both: the larger of each entry and the other list's mirrored one is a
+// bitonic sequence, which six exchanges sort.
+__device__ __forceinline__ u64 top_merge(u64 mine, u64 mirrored) {
+  u64 v = mine > mirrored ? mine : mirrored;
+#pragma unroll
+  for (int d = kWave / 2; d >= 1; d >>= 1) {
+    const u64 o = lane_read(v, (int)(lane_id() ^ d));
+    const bool upper = (lane_id() & d) != 0;
+    v = (o > v) != upper ? o : v;
+  }
+  return v;
+}
+
+// Rows need not begin at a 16-byte boundary: vector v of a row holds columns 8 v - skew .. + 7 with `skew` the elements
+// between the boundary below the row and the row, so that all vectors but the outer ones are loaded whole.
+template <class T>
+__device__ __forceinline__ u32 skew_of(const T* row) {
+  return (u32)((uintptr_t)row & 15) / (u32)sizeof(T);
+}
+
+template <class T>
+__device__ __forceinline__ void take(Soft& a, const Vec8<T>& v) {
+  float x[8], most = neg_inf();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    x[j] = (float)v.v[j];
+    most = __builtin_fmaxf(most, x[j]);
+  }
+  if (most > a.m) raise_to(a, most);
+  const float m = shift_of(a.m);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+    a.s += e;
+    a.t += e == 0.0f ? 0.0f : e * d;
+  }
+}
+
+// the elements of `v` that belong into the list; all lanes of a wavefront call this together
+template <class T>
+__device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, int col, u32 cols, bool live, int top) {
+  u64 k[8], most = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    k[j] = live && (u32)(col + j) < cols ? key_of((float)v.v[j], (u32)(col + j)) : 0;
+    most = k[j] > most ? k[j] : most;
+  }
+  if (__builtin_amdgcn_ballot_w64(most > l.last) == 0) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    u64 who = __builtin_amdgcn_ballot_w64(k[j] > l.last);
+    while (who) {
+      const int lane = __builtin_ctzll(who);
+      top_insert(l, k[j], lane, top);
+      who &= who - 1;
+      who &= __builtin_amdgcn_ballot_w64(k[j] > l.last);
+    }
+  }
+}
+
+// vector at column `col` (negative before the row) of a row; -inf outside
+template <class T>
+__device__ __forceinline__ Vec8<T> load_row(const T* row, int col, u32 cols) {
+  if (col >= 0 && (u32)col + 8 <= cols) return load_wide(row + col);
+  Vec8<T> r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r.v[j] = (u32)(col + j) < cols ? row[col + j] : (T)neg_inf();
+  return r;
+}
+
+struct LabelOut {
+  const int* label;
+  float *logp, *entropy, *lse, *top_logp;
+  int* top_index;
+  u32* status;
+};
+// what a row's state and list say, written by one wavefront
+template <class T>
+__device__ __forceinline__ void finish_row(const LabelOut& o, const T* row, u32 r, u32 cols, Soft a, u64 mine, int top) {
+  const float m = shift_of(a.m), log_s = logf(a.s);
+  const bool empty = a.s == 0.0f;
+  const u32 lane = lane_id();
+  if (lane == 0) {
+    const int label = o.label[r];
+    const bool has = (u32)label < cols;
+    if (!has && label != -1 && o.status) atomicOr(o.status, HAFLO_ST_RANGE);
+    const float x = has ? (float)row[label] : 0.0f;
+    o.logp[r] = !has ? 0.0f : empty ? neg_inf() : x - m - log_s;
+    o.entropy[r] = empty ? 0.0f : log_s - a.t / a.s;
+    o.lse[r] = empty ? neg_inf() : m + log_s;
+  }
+  if ((int)lane < top) {
+    o.top_logp[(size_t)r * top + lane] = empty ? neg_inf() : value_of(mine) - m - log_s;
+    o.top_index[(size_t)r * top + lane] = (int)~(u32)mine;
+  }
+}
+
+struct Part {  // of a row, joined by k_label_join
+  float m, s, t, unused;
+};
+
+// W wavefronts to a row or, with `parts` > 1, to one of its parts
+template <class T, int W, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_labels(const T* x, size_t ld, u32 rows, u32 cols, int top, u32 parts, LabelOut o,
+                                                     Part* part, u64* lists) {
+  __shared__ Soft soft[kWaves];
+  __shared__ u64 list[TOP ? kWaves : 1][kWave];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const u32 unit = W == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
+  const u32 r = unit / parts, p = unit % parts;
+  if (W == 1 && r >= rows) return;
+  const T* row = x + (size_t)r * ld;
+  const u32 skew = skew_of(row), vectors = (cols + skew + 7) / 8;
+  const u32 first = (u32)((u64)vectors * p / parts), end = (u32)((u64)vectors * (p + 1) / parts);
+  constexpr u32 kStep = W * kWave;
+  Soft a = {neg_inf(), 0.0f, 0.0f};
+  TopList l = {0, 0};
+  for (u32 base = first; base < end; base += kStep * kAhead) {
+    Vec8<T> v[kAhead];
+    const u32 at = base + threadIdx.x % kStep;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (at + i * kStep < end) v[i] = load_row(row, (int)((at + i * kStep) * 8 - skew), cols);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const bool live = at + i * kStep < end;
+      const int col = (int)((at + i * kStep) * 8 - skew);
+      if (live) take(a, v[i]);
+      if (TOP && base + i * kStep < end) take_top(l, v[i], col, cols, live, top);
+    }
+  }
+  a = wave_join(a);
+  u64 mine = l.mine;
+  if (W > 1) {
+    if (lane_id() == 0) soft[wave] = a;
+    if (TOP) list[wave][lane_id()] = mine;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < W; ++w) {
+      join(a, soft[w]);
+      if (TOP) mine = top_merge(mine, list[w][kWave - 1 - lane_id()]);
+    }
+  }
+  if (parts == 1) {
+    finish_row(o, row, r, cols, a, mine, top);
+  } else {
+    if (lane_id() == 0) part[unit] = Part{a.m, a.s, a.t, 0.0f};
+    if (TOP && (int)lane_id() < top) lists[(size_t)unit * top + lane_id()] = mine;
+  }
+}
+
+// a wavefront to a row: joins its parts, in their order
+template <class T, bool TOP>
+__global__ __launch_bounds__(kWave) void k_label_join(const T* x, size_t ld, u32 cols, int top, u32 parts, LabelOut o,
+                                                      const Part* part, const u64* lists) {
+  const u32 r = blockIdx.x, lane = lane_id();
+  Soft a = {neg_inf(), 0.0f, 0.0f};
+  for (u32 p = lane; p < parts; p += kWave) {
+    const Part q = part[(size_t)r * parts + p];
+    join(a, Soft{q.m, q.s, q.t});
+  }
+  a = wave_join(a);
+  u64 mine = 0;
+  if (TOP) {
+    for (u32 p = 0; p < parts; ++p) {
+      const int at = kWave - 1 - (int)lane;
+      mine = top_merge(mine, at < top ? lists[((size_t)r * parts + p) * top + at] : 0);
+    }
+  }
+  finish_row(o, x + (size_t)r * ld, r, cols, a, mine, top);
+}
+
+// a lane to a row of few columns
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_labels_small(const T* x, size_t ld, u32 rows, u32 cols, int top, LabelOut o) {
+  const u32 r = blockIdx.x * kThreads + threadIdx.x;
+  if (r >= rows) return;
+  const T* row = x + (size_t)r * ld;
+  float most = neg_inf();
+  for (u32 j = 0; j < cols; ++j) most = __builtin_fmaxf(most, (float)row[j]);
+  const float m = shift_of(most);
+  float s = 0.0f, t = 0.0f;
+  for (u32 j = 0; j < cols; ++j) {
+    const float d = (float)row[j] - m, e = __builtin_amdgcn_exp2f(d * kLog2e);
+    s += e;
+    t += e == 0.0f ? 0.0f : e * d;
+  }
+  const float log_s = logf(s);
+  const bool empty = s == 0.0f;
+  const int label = o.label[r];
+  const bool has = (u32)label < cols;
+  if (!has && label != -1 && o.status) atomicOr(o.status, HAFLO_ST_RANGE);
+  o.logp[r] = !has ? 0.0f : empty ? neg_inf() : (float)row[label] - m - log_s;
+  o.entropy[r] = empty ? 0.0f : log_s - t / s;
+  o.lse[r] = empty ? neg_inf() : m + log_s;
+  u64 last = ~0ull;
+  for (int k = 0; k < top; ++k) {
+    u64 best = 0;
+    for (u32 j = 0; j < cols; ++j) {
+      const u64 key = key_of((float)row[j], j);
+      if (key < last && key > best) best = key;
+    }
+    o.top_logp[(size_t)r * top + k] = empty ? neg_inf() : value_of(best) - m - log_s;
+    o.top_index[(size_t)r * top + k] = (int)~(u32)best;
+    last = best;
+  }
+}
+
+struct GradIn {
+  const int* label;
+  const float *lse, *entropy, *dlogp, *dentropy;
+  const int* top_index;
+  const float* dtop;
+};
+// a lane to eight columns of a row
+template <class T, bool SAME>
+__global__ __launch_bounds__(kThreads) void k_labels_grad(const T* x, size_t ld, u32 rows, u32 cols, int top, GradIn g, T* dx,
+                                                          size_t lddx) {
+  constexpr u32 kMostSkew = 16 / sizeof(T) - 1;
+  const u32 groups = (cols + kMostSkew + 7) / 8;
+  const u64 total = (u64)rows * groups, step = (u64)gridDim.x * kThreads;
+  for (u64 at = (u64)blockIdx.x * kThreads + threadIdx.x; at < total; at += step) {
+    const u32 r = (u32)(at / groups), v = (u32)(at - (u64)r * groups);
+    const T* row = x + (size_t)r * ld;
+    T* out = dx + (size_t)r * lddx;
+    const int col = (int)(v * 8 - skew_of(row));
+    if (col >= (int)cols) continue;
+    const Vec8<T> in = load_row(row, col, cols);
+    const float lse = g.lse[r], entropy = g.entropy[r], dh = g.dentropy ? g.dentropy[r] : 0.0f;
+    const int label = g.label[r];
+    const float dlogp = (u32)label < cols ? g.dlogp[r] : 0.0f;
+    float given = dlogp, extra[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) extra[j] = label == col + j ? dlogp : 0.0f;
+    if (g.dtop) {
+      for (int k = 0; k < top; ++k) {
+        const int i = g.top_index[(size_t)r * top + k];
+        const float d = (u32)i < cols ? g.dtop[(size_t)r * top + k] : 0.0f;
+        given += d;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) extra[j] += i == col + j ? d : 0.0f;
+      }
+    }
+    Vec8<T> res;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float lp = (float)in.v[j] - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
+      const float d = (p == 0.0f ? 0.0f : p * (-given - dh * (lp + entropy))) + extra[j];
+      res.v[j] = (T)(lse == neg_inf() ? 0.0f : d);
+    }
+    if (SAME && col >= 0 && (u32)col + 8 <= cols) {
+      store_wide(out + col, res);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((u32)(col + j) < cols) out[col + j] = res.v[j];
+    }
+  }
+}
+
+u32 label_parts(size_t rows, size_t cols) {
+  if (cols <= kWaveCols || rows == 0 || rows >= kSplitBlocks) return 1;
+  const size_t want = kSplitBlocks / rows, most = ceil_div(cols, kSplitCols);
+  return (u32)(want < most ? (want ? want : 1) : most);
+}
+
+bool label_sizes(int type, size_t rows, size_t cols, size_t top) {
+  return valid_type(type) && rows <= kMostCount && cols >= 1 && cols <= kMostCount - 16 && top <= HAFLO_LABEL_MAX_TOP && top <= cols;
+}
+
+size_t label_bytes(size_t rows, size_t cols, size_t top) {
+  const size_t parts = label_parts(rows, cols);
+  return parts == 1 ? 0 : align256(rows * parts * sizeof(Part)) + rows * parts * top * 8;
+}
+
+template <class T>
+int label_forward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, const LabelOut& o, void* ws, hipStream_t st) {
+  const u32 parts = label_parts(rows, cols);
+  Part* part = (Part*)ws;
+  u64* lists = (u64*)((char*)ws + align256(rows * parts * sizeof(Part)));
+  const dim3 block(kThreads);
+  if (cols <= kSmallCols) {
+    hipLaunchKernelGGL((k_labels_small<T>), dim3((unsigned)ceil_div(rows, kThreads)), block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, o);
+    return launched();
+  }
+#define HAFLO_LOCAL_RUN(W, TOP, UNITS) \
+  hipLaunchKernelGGL((k_labels<T, W, TOP>), dim3((unsigned)(UNITS)), block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, parts, o, part, lists)
+  if (cols <= kWaveCols) {
+    if (top) HAFLO_LOCAL_RUN(1, true, ceil_div(rows, kWaves));
+    else HAFLO_LOCAL_RUN(1, false, ceil_div(rows, kWaves));
+  } else {
+    if (top) HAFLO_LOCAL_RUN(kWaves, true, rows * parts);
+    else HAFLO_LOCAL_RUN(kWaves, false, rows * parts);
+  }
+#undef HAFLO_LOCAL_RUN
+  if (parts > 1) {
+    if (top)
+      hipLaunchKernelGGL((k_label_join<T, true>), dim3((unsigned)rows), dim3(kWave), 0, st, x, ld, (u32)cols, (int)top, parts, o, part, lists);
+    else
+      hipLaunchKernelGGL((k_label_join<T, false>), dim3((unsigned)rows), dim3(kWave), 0, st, x, ld, (u32)cols, (int)top, parts, o, part, lists);
+  }
+  return launched();
+}
+
+template <class T>
+int label_backward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, const GradIn& g, T* dx, size_t lddx, hipStream_t st) {
+  const size_t need = ceil_div(rows * ((cols + 16 / sizeof(T) + 6) / 8), kThreads);
+  const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(kThreads);
+  // every row of dx lies as its row of x does
+  const bool same = ((uintptr_t)x & 15) == ((uintptr_t)dx & 15) && (ld * sizeof(T)) % 16 == (lddx * sizeof(T)) % 16;
+  if (same) hipLaunchKernelGGL((k_labels_grad<T, true>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx, lddx);
+  else hipLaunchKernelGGL((k_labels_grad<T, false>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx, lddx);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t haflo_label_workspace_bytes(int type, size_t rows, size_t cols, size_t top) {
+  return label_sizes(type, rows, cols, top) ? label_bytes(rows, cols, top) : (size_t)-1;
+}
+
+int haflo_label_logprobs(int type, const void* d_logits, size_t ld, const int32_t* d_label, size_t rows, size_t cols,
+                         size_t top, float* d_logp, float* d_entropy, float* d_lse, float* d_top_logp,
+                         int32_t* d_top_index, uint32_t* d_status, void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (!label_sizes(type, rows, cols, top)) return HAFLO_EINVAL;
+  if (rows == 0) return HAFLO_OK;
+  if (!d_logits || ld < cols || !d_label || !d_logp || !d_entropy || !d_lse || (top && (!d_top_logp || !d_top_index))) return HAFLO_EINVAL;
+  const size_t bytes = label_bytes(rows, cols, top);
+  if (bytes && (!d_workspace || workspace_bytes < bytes)) return HAFLO_EINVAL;
+  const LabelOut o = {d_label, d_logp, d_entropy, d_lse, d_top_logp, d_top_index, d_status};
+  HAFLO_LOCAL_TYPES(type, return label_forward<T>((const T*)d_logits, ld, rows, cols, top, o, d_workspace, (hipStream_t)stream));
+}
+
+int haflo_label_logprobs_backward(int type, const void* d_logits, size_t ld, const int32_t* d_label, const float* d_lse,
+                                  const float* d_entropy, const float* d_dlogp, const float* d_dentropy,
+                                  const int32_t* d_top_index, const float* d_dtop, size_t rows, size_t cols, size_t top,
+                                  void* d_dx, size_t lddx, void* stream) {
+  if (!label_sizes(type, rows, cols, top)) return HAFLO_EINVAL;
+  if (rows == 0) return HAFLO_OK;
+  if (!d_logits || ld < cols || !d_label || !d_lse || !d_entropy || !d_dlogp || (d_dtop && top && !d_top_index) || !d_dx || lddx < cols)
+    return HAFLO_EINVAL;
+  const GradIn g = {d_label, d_lse, d_entropy, d_dlogp, d_dentropy, d_top_index, top ? d_dtop : nullptr};
+  HAFLO_LOCAL_TYPES(type, return label_backward<T>((const T*)d_logits, ld, rows, cols, top, g, (T*)d_dx, lddx, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,53 @@
+// CPU stand-in for <hip/hip_runtime.h> for the operators of a party's local step: the one of the ciphertext operators
+// with the matrix instructions on floating-point types and the few other builtins that those kernels use. Compiled by
+// clang, which knows the half types.
+#pragma once
+#include "../../include/hip/hip_runtime.h"
+
+namespace hipemu_local {
+// what each lane of a wavefront brought to its current exchange; two sets, as a lane may be one exchange ahead
+struct Slots {
+  float a[64][8], b[64][8];
+};
+inline Slots& slots(int parity) {
+  static Slots s[2][32];  // by wavefront of the block
+  return s[parity][threadIdx.x / 64];
+}
+inline int& parity() {
+  static int p[2048];  // by lane of the block
+  return p[threadIdx.x];
+}
+// one 16 x 16 product of `k` elements a lane; lane l's stand for the reduction's places k (l / 16) ..
+template <class C>
+inline C mfma(const float* a, const float* b, C c, int k) {
+  const int lane = (int)(threadIdx.x % 64), at = parity() ^= 1;
+  Slots& s = slots(at);
+  for (int j = 0; j < k; ++j) {
+    s.a[lane][j] = a[j];
+    s.b[lane][j] = b[j];
+  }
+  hipemu::ballot(true);
+  for (int r = 0; r < 4; ++r) {
+    float sum = c[r];
+    for (int g = 0; g < 4; ++g)
+      for (int j = 0; j < k; ++j) sum += s.a[16 * g + 4 * (lane / 16) + r][j] * s.b[16 * g + lane % 16][j];
+    c[r] = sum;
+  }
+  return c;
+}
+template <class V, class C>
+inline C mfma8(V a, V b, C c) {
+  float x[8], y[8];
+  for (int j = 0; j < 8; ++j) {
+    x[j] = (float)a[j];
+    y[j] = (float)b[j];
+  }
+  return mfma(x, y, c, 8);
+}
+}  // namespace hipemu_local
+
+#define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
+#define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
+#define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) hipemu_local::mfma(&(const float&)(a), &(const float&)(b), (c), 1)
+static inline float __builtin_amdgcn_exp2f(float x) { return exp2f(x); }
+static inline void __builtin_amdgcn_s_setprio(int) {}

@@ -1,0 +1,252 @@
+"""A party's local operators on the GPU, through the binding, against the definitions in 64 bits."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import local_cases as cases  # noqa: E402
+
+
+def dev(t):
+    """On the GPU with the host tensor's strides and its distance from an aligned address."""
+    if t is None:
+        return None
+    whole = torch.as_strided(t, (t.untyped_storage().nbytes() // t.element_size(),), (1,), 0).cuda()
+    return torch.as_strided(whole, t.shape, t.stride(), t.storage_offset())
+
+
+def back(*ts):
+    return tuple(t if t is None else t.cpu() for t in ts)
+
+
+class Gpu:
+    """The binding's functions on host tensors."""
+
+    def __init__(self, api):
+        self.api = api
+
+    def status(self):
+        return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def dropout(self, x, p, seed, offset, residual=None):
+        return self.api.haflo_dropout(dev(x), p, seed, offset, residual=dev(residual)).cpu()
+
+    def adapter_forward(self, x, w, a, b, scale, index, p, seed, offset):
+        st = self.status()
+        return back(*self.api.haflo_adapter_forward(*map(dev, (x, w, a, b, scale, index)), p, seed, offset, status=st)) + (int(st),)
+
+    def adapter_backward(self, dy, x, w, a, b, scale, index, h, p, seed, offset):
+        st = self.status()
+        return back(*self.api.haflo_adapter_backward(*map(dev, (dy, x, w, a, b, scale, index, h)), p, seed, offset, status=st)) + (int(st),)
+
+    def label_logprobs(self, x, label, top):
+        st = self.status()
+        return back(*self.api.haflo_label_logprobs(dev(x), dev(label), top, status=st)) + (int(st),)
+
+    def label_logprobs_backward(self, x, label, lse, entropy, dlogp, dentropy, top_index, dtop):
+        return self.api.haflo_label_logprobs_backward(*map(dev, (x, label, lse, entropy, dlogp, dentropy, top_index, dtop))).cpu()
+
+
+@pytest.fixture(scope="module")
+def api():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2107_13797_amd import api
+    api.lib()
+    return api
+
+
+@pytest.fixture(scope="module")
+def run(api):
+    return Gpu(api)
+
+
+@pytest.mark.parametrize("case", cases.DROPOUT, ids=str)
+def test_dropout(run, case):
+    cases.check_dropout(run, *case)
+
+
+def test_dropout_special(run):
+    cases.check_dropout_special(run)
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS + cases.ADAPTERS_LARGE, ids=str)
+def test_adapters(run, case):
+    cases.check_adapters(run, *case)
+
+
+def test_adapters_other_parties_infinities(run):
+    cases.check_adapters_other_parties_infinities(run)
+
+
+@pytest.mark.parametrize("case", cases.LABELS + cases.LABELS_LARGE, ids=str)
+def test_labels(run, case):
+    cases.check_labels(run, *case)
+
+
+def test_labels_nan(run):
+    cases.check_labels_nan(run)
+
+
+def test_in_place_and_vectors(api):
+    x = torch.randn(1000, device="cuda").to(torch.bfloat16)
+    want = api.haflo_dropout(x, 0.5, 3)
+    again = x.clone()
+    assert api.haflo_dropout(again, 0.5, 3, out=again) is again and torch.equal(again, want) and want.shape == x.shape
+    res = torch.randn(40, 24, device="cuda")
+    m = torch.randn(40, 24, device="cuda")
+    want = api.haflo_dropout(m, 0.1, 4, residual=res)
+    assert torch.equal(api.haflo_dropout(m, 0.1, 4, residual=res, out=res), want)
+    logits, label = torch.randn(9, 3001, device="cuda").half(), torch.arange(9, dtype=torch.int32, device="cuda")
+    logp, entropy, lse, _, _ = api.haflo_label_logprobs(logits, label)
+    ones = torch.ones(9, device="cuda")
+    want = api.haflo_label_logprobs_backward(logits, label, lse, entropy, ones)
+    assert torch.equal(api.haflo_label_logprobs_backward(logits, label, lse, entropy, ones, out=logits), want)
+
+
+def test_gradients_against_differences(api):
+    """Backward calls against differences of forward calls along random directions, in float32. With step t the quotient is off by
+    the third derivative's t^2 and the forward results' roundings over t; both directions' terms are bounded by `room`."""
+    gen = torch.Generator().manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, generator=gen).cuda()  # noqa: E731
+    rows, cols, t = 6, 40, 2.0 ** -7
+    x, label = rnd(rows, cols), torch.tensor([0, 3, -1, 39, 7, 7], dtype=torch.int32, device="cuda")
+    cl, ch, ct, dirn = rnd(rows), rnd(rows), rnd(rows, 3), rnd(rows, cols)
+
+    def value(v):
+        logp, entropy, _, top, _ = api.haflo_label_logprobs(v, label, 3)
+        return float((cl * logp).double().sum() + (ch * entropy).double().sum() + (ct * top).double().sum())
+
+    _, entropy, lse, _, index = api.haflo_label_logprobs(x, label, 3)
+    dx = api.haflo_label_logprobs_backward(x, label, lse, entropy, cl, ch, index, ct)
+    got, want = float((dx * dirn).double().sum()), (value(x + t * dirn) - value(x - t * dirn)) / (2 * t)
+    # third derivatives of these are below 8 |direction|^3 in each row, values below 64
+    room = t * t * 8 * float(dirn.abs().amax(1).pow(3).sum()) * float(cl.abs().max() + ch.abs().max() + ct.abs().sum(1).max()) + 64 * rows * 2.0 ** -22 / t
+    assert abs(got - want) <= room
+
+    # the adapters' result is linear in each of x, a and b: the quotient is exact but for roundings
+    n, r, inner, outer = 3, 4, 24, 20
+    x, w, a, b, scale = rnd(rows, inner), rnd(outer, inner), rnd(n, r, inner), rnd(n, outer, r), rnd(n).abs() + 0.5
+    ids, dy = torch.tensor([0, 2, -1, 0, 1, 2], dtype=torch.int32, device="cuda"), rnd(rows, outer)
+    fwd = lambda x, a, b: api.haflo_adapter_forward(x, w, a, b, scale, ids, 0.25, 11, 3)  # noqa: E731
+    y, h = fwd(x, a, b)
+    grads = api.haflo_adapter_backward(dy, x, w, a, b, scale, ids, h, 0.25, 11, 3)
+    for i, arg in enumerate((x, a, b)):
+        d = rnd(*arg.shape)
+        plus, minus = ([v + s * d if j == i else v for j, v in enumerate((x, a, b))] for s in (1.0, -1.0))
+        want = float(((fwd(*plus)[0].double() - fwd(*minus)[0].double()) * dy).sum()) / 2
+        size = float((y.abs().max() + fwd(*plus)[0].abs().max()) * dy.abs().sum())
+        assert abs(float((grads[i].double() * d).sum()) - want) <= size * (inner + r + 8) * 2.0 ** -20
+
+
+def test_same_bits_again(api):
+    """No result depends on timing."""
+    gen = torch.Generator().manual_seed(6)
+    x, w, a, b, scale, index, dy = map(dev, cases.adapter_inputs("bf16", 700, 520, 264, 16, 5, "mixed", 0))
+    y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.1, 1)
+    first = [y, h, *api.haflo_adapter_backward(dy, x, w, a, b, scale, index, h, 0.1, 1)]
+    logits, label = torch.randn(3, 70001, generator=gen).bfloat16().cuda(), torch.tensor([5, -1, 70000], dtype=torch.int32, device="cuda")
+    seen = api.haflo_label_logprobs(logits, label, 20)
+    for _ in range(3):
+        y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.1, 1)
+        assert all(torch.equal(p, q) for p, q in zip(first, [y, h, *api.haflo_adapter_backward(dy, x, w, a, b, scale, index, h, 0.1, 1)]))
+        assert all(torch.equal(p, q) for p, q in zip(seen, api.haflo_label_logprobs(logits, label, 20)))
+
+
+def test_side_stream_and_graph(api):
+    """A step captured on a side stream and replayed on new contents of the same buffers gives what the eager calls give."""
+    x, w, a, b, scale, index, dy = map(dev, cases.adapter_inputs("bf16", 200, 136, 136, 8, 3, "mixed", 0))
+    label = torch.arange(200, dtype=torch.int32, device="cuda") % 136
+    minus = torch.full((200,), -1.0 / 200, device="cuda")
+
+    def step():
+        y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.2, 9, 1)
+        logp, entropy, lse, top, at = api.haflo_label_logprobs(y, label, 2)
+        dlogits = api.haflo_label_logprobs_backward(y, label, lse, entropy, minus)
+        dx, da, db = api.haflo_adapter_backward(dlogits, x, w, a, b, scale, index, h, 0.2, 9, 1)
+        return y, logp, entropy, top, at, api.haflo_dropout(dx, 0.5, 2, residual=x), da, db
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    for k in range(3):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(k)).to(x.dtype))
+        torch.cuda.synchronize()
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+def test_long_rows_and_far_offsets(api):
+    """Elements past 2^31 in one array: dropout of the last rows of a wide matrix, labels in the last of many rows."""
+    rows, cols = 70001, 32768
+    x = torch.empty((rows, cols), dtype=torch.float16, device="cuda").fill_(1.0)
+    y = api.haflo_dropout(x, 0.5, 123, 7)
+    last = y[-2:].double().cpu()
+    f = torch.zeros(2, cols, dtype=torch.float64)
+    for r in range(2):
+        for g in range(0, cols // 8, 97):
+            words = cases.philox(g, rows - 2 + r, 123, 7)
+            for j in range(8):
+                f[r, 8 * g + j] = 2.0 * ((words[j // 2] >> (16 * (j % 2)) & 0xFFFF) >= 32768)
+                assert last[r, 8 * g + j] == f[r, 8 * g + j]
+    x[-1, 77] = 12.0
+    label = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    label[-1] = 77
+    logp, entropy, lse, top, at = api.haflo_label_logprobs(x, label, 1)
+    s = math.exp(1.0 - 12.0) * (cols - 1) + 1.0
+    assert int(at[-1, 0]) == 77 and abs(float(logp[-1]) + math.log(s)) < 1e-5 and float(logp[:-1].abs().max()) == 0.0
+    dx = api.haflo_label_logprobs_backward(x, label, lse, entropy, torch.ones(rows, device="cuda"), out=x)
+    assert abs(float(dx[-1, 77]) - (1.0 - 1.0 / s)) < 1e-3 and not bool(dx[:-1].any())
+
+
+def test_refusals(api):
+    f32, i32 = torch.float32, torch.int32
+    x = torch.zeros(4, 8, device="cuda")
+    bad = [
+        lambda: api.haflo_dropout(x.double(), 0.5, 1), lambda: api.haflo_dropout(x, 1.5, 1), lambda: api.haflo_dropout(x, -0.1, 1),
+        lambda: api.haflo_dropout(x, math.nan, 1), lambda: api.haflo_dropout(x.cpu(), 0.5, 1), lambda: api.haflo_dropout(x.t(), 0.5, 1),
+        lambda: api.haflo_dropout(x, 0.5, 1, residual=x[:3]), lambda: api.haflo_dropout(x, 0.5, 1, out=x.half()),
+        lambda: api.haflo_dropout(x[:1].expand(4, 8), 0.5, 1),
+    ]
+    w, a, b = torch.zeros(6, 8, device="cuda"), torch.zeros(2, 3, 8, device="cuda"), torch.zeros(2, 6, 3, device="cuda")
+    s, i = torch.zeros(2, device="cuda"), torch.zeros(4, dtype=i32, device="cuda")
+    big = torch.zeros(2, 129, 8, device="cuda")
+    fwd = api.haflo_adapter_forward
+    bad += [
+        lambda: fwd(x, w[:, :7], a, b, s, i), lambda: fwd(x, w, a.half(), b, s, i), lambda: fwd(x, w, a, b[:, :5], s, i),
+        lambda: fwd(x, w, a, b, s[:1], i), lambda: fwd(x, w, a, b, s, i.long()), lambda: fwd(x, w, a, b, s, i[:3]), lambda: fwd(x, w, a[0], b, s, i),
+        lambda: fwd(x, w, big, torch.zeros(2, 6, 129, device="cuda"), s, i), lambda: fwd(x, w, a, b, s, i, 2.0), lambda: fwd(x[0], w, a, b, s, i),
+        lambda: fwd(x, w, a[:0], b[:0], s[:0], i), lambda: fwd(x, w, a.transpose(1, 2).contiguous().transpose(1, 2), b, s, i),
+    ]
+    y, h = fwd(x, w, a, b, s, i)
+    bad += [lambda: api.haflo_adapter_backward(y[:3], x, w, a, b, s, i, h), lambda: api.haflo_adapter_backward(y, x, w, a, b, s, i, h[:, :2]),
+            lambda: api.haflo_adapter_backward(y.half(), x, w, a, b, s, i, h), lambda: api.haflo_adapter_backward(y, x, w, a, b, s, i, h, 1.1)]
+    one = torch.zeros(4, device="cuda")
+    lab = api.haflo_label_logprobs
+    bad += [
+        lambda: lab(x, i.long()), lambda: lab(x, i[:2]), lambda: lab(x, i, 9), lambda: lab(torch.zeros(4, 100, device="cuda"), i, 65),
+        lambda: lab(x[:, :0], i), lambda: lab(x.to(i32), i), lambda: lab(x, i, -1),
+        lambda: api.haflo_label_logprobs_backward(x, i, one, one, one[:3]), lambda: api.haflo_label_logprobs_backward(x, i, one, one, one.half()),
+        lambda: api.haflo_label_logprobs_backward(x, i, one, one, one, None, None, torch.zeros(4, 2, device="cuda")),
+    ]
+    for n, call in enumerate(bad):
+        with pytest.raises(api.HafloError):
+            call()
+            pytest.fail("call %d was not refused" % n)
+    # nothing to do is no error
+    assert api.haflo_dropout(x[:0], 0.5, 1).shape == (0, 8)
+    assert lab(x[:0], i[:0], 2)[4].shape == (0, 2)
+    y, h = fwd(x[:0], w, a, b, s, i[:0])
+    dx, da, db = api.haflo_adapter_backward(y, x[:0], w, a, b, s, i[:0], h)
+    assert y.shape == (0, 6) and dx.shape == (0, 8) and da.dtype == f32 and not da.any() and not db.any()
