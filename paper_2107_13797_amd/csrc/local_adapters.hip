@@ -4,9 +4,12 @@
 //   backward  g[t] = scale B[a]^T dy[t],         dx[t] = W^T dy[t] + drop'(A[a]^T g[t])
 //             dA[a] = sum_t g[t] drop(x[t])^T,   dB[a] = sum_t dy[t] h[t]^T
 //
-// h and g, the rows' short vectors ("z" where a kernel serves both directions), come from k_shrink; k_project forms the
-// large product with the adapters' part as its first summand; k_grad sums over the rows of one adapter, which k_group
-// lists. W^T and B^T for the backward pass are laid out by k_transpose, so that every product reduces along rows.
+// h and g, the rows' short vectors ("z" where a kernel serves both directions), come from k_shrink. k_project forms
+// the large product and adds the adapters' part, k_project_few does for few rows. k_group lists the rows by
+// adapter: a tile's rows are taken from that list, so that they share one adapter as a rule, whatever the order the
+// caller has them in, and k_grad sums over the rows of one adapter. Operands whose rows do not begin at 16-byte
+// boundaries are laid out anew by k_pad, and what reduces along columns (W, A and B of the backward pass) by k_transpose: so
+// every product reduces along rows in 16-byte loads.
 #include "local_common.hpp"
 
 using namespace haflo::local;
@@ -15,10 +18,10 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// An adapter matrix of every party, element (party, out, r) at party * party_step + out * out_step + r * r_step.
-struct Low {
-  size_t party_step, out_step, r_step;
-};
+template <class T>
+constexpr int step_elems() {  // of the reduction in one step of k_project: 128 bytes of a row
+  return 128 / (int)sizeof(T);
+}
 
 __device__ __forceinline__ int party_of(const int* index, u32 t, u32 parties) {
   const int a = index[t];
@@ -26,12 +29,11 @@ __device__ __forceinline__ int party_of(const int* index, u32 t, u32 parties) {
 }
 
 // eight elements at (row, k) of a matrix, zeros past its edges
-template <class T, bool WIDE>
+template <class T>
 __device__ __forceinline__ Vec8<T> load_tile(const T* m, size_t ld, u32 row, u32 rows, u32 k, u32 cols) {
   if (row >= rows || k >= cols) return Vec8<T>{};
   const T* p = m + (size_t)row * ld + k;
-  if (WIDE && k + 8 <= cols) return load_wide(p);
-  return load_some(p, cols - k < 8 ? (int)(cols - k) : 8);
+  return k + 8 <= cols ? load_wide(p) : load_some(p, (int)(cols - k));
 }
 template <class T>
 __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u32 k) {
@@ -41,42 +43,52 @@ __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u
     if (!kept(d, draws, j)) v.v[j] = (T)0.0f;
 }
 
-// z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows of length `inner`. A block takes 16 rows and one part of
-// the reduction, its wavefronts a quarter of that each; once for every party among the rows.
-template <class T, bool WIDE, int RT>
-__global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, const T* f, const float* scale, const int* index, u32 rows,
-                                                     u32 inner, u32 rank, u32 parties, Drop d, u32 parts, float* z, u32* status) {
-  __shared__ float sum[kThreads / kWave][RT][16][16];
+// z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without. A block takes ROWS rows (of `order`, or one
+// row as it lies) and one part of the reduction, its wavefronts a quarter of that each; once for every party among the rows.
+template <class T, int ROWS, int RT>
+__global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
+                                                     const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
+                                                     u32 z_ld, float* z, float* h, u32* status) {
+  constexpr int kAhead = RT == 1 ? 4 : 2;  // steps whose operands are on their way together
+  __shared__ float sum[kThreads / kWave][RT][16][17];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 t0 = blockIdx.x / parts * 16, part = blockIdx.x % parts;
-  const u32 mine = t0 + lane % 16;
+  const u32 at0 = blockIdx.x / parts * ROWS, part = blockIdx.x % parts;
+  const auto row_at = [&](u32 i) { return at0 + i >= rows ? rows : order ? order[at0 + i] : at0 + i; };
+  const u32 mine = row_at(ROWS == 1 ? 0 : lane % 16);
   const int raw = mine < rows ? index[mine] : -1;
   const int a = (u32)raw < parties ? raw : -1;
   if (status && part == 0 && threadIdx.x < 16 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
   // this wavefront's share of the reduction, in steps of 32
   const u32 steps = (inner + 31) / 32, units = parts * (kThreads / kWave), unit = part * (kThreads / kWave) + wave;
   const u32 first = (u32)((u64)steps * unit / units), end = (u32)((u64)steps * (unit + 1) / units);
-  float own[RT];  // of element (row lane / 16 * 4 + wave, r = lane % 16)
+  float own[RT];  // of row out_i, r = lane % 16
 #pragma unroll
   for (int i = 0; i < RT; ++i) own[i] = 0.0f;
-  const u32 out_t = t0 + lane / 16 * 4 + wave;
+  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave;
+  const u32 out_t = row_at(out_i);
   const int out_a = out_t < rows ? party_of(index, out_t, parties) : -1;
   u64 left = __builtin_amdgcn_ballot_w64(a >= 0) & 0xFFFF;
   while (left) {
     const int who = __builtin_amdgcn_readlane(a, __builtin_ctzll(left));
     left &= ~__builtin_amdgcn_ballot_w64(a == who);
-    const T* fa = f + (size_t)who * rank * inner;
+    const T* fa = f + (size_t)who * rank * f_ld;
     f32x4 acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (u32 s = first; s < end; ++s) {
-      const u32 k = s * 32 + lane / 16 * 8;
-      Vec8<T> xv = load_tile<T, WIDE>(x, ldx, mine, rows, k, inner);
-      if (d.threshold) apply_drop(xv, d, mine, k);
+    for (u32 s0 = first; s0 < end; s0 += kAhead) {
+      Vec8<T> xv[kAhead], fv[kAhead][RT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const Vec8<T> fv = load_tile<T, WIDE>(fa, inner, i * 16 + lane % 16, rank, k, inner);
-        acc[i] = mma32(fv, xv, acc[i]);
+      for (int u = 0; u < kAhead; ++u) {
+        const u32 k = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
+        xv[u] = load_tile(x, ldx, mine, rows, k, inner);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) fv[u][i] = load_tile(fa, f_ld, i * 16 + lane % 16, rank, k, inner);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (d.threshold) apply_drop(xv[u], d, mine, (s0 + u) * 32 + lane / 16 * 8);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[i] = mma32(fv[u][i], xv[u], acc[i]);
       }
     }
 #pragma unroll
@@ -87,213 +99,464 @@ __global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, con
     if (out_a == who) {
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        const u32 t = lane / 16 * 4 + wave, r = lane % 16;
-        own[i] = (sum[0][i][t][r] + sum[1][i][t][r]) + (sum[2][i][t][r] + sum[3][i][t][r]);
+        const u32 r = lane % 16;
+        own[i] = (sum[0][i][out_i][r] + sum[1][i][out_i][r]) + (sum[2][i][out_i][r] + sum[3][i][out_i][r]);
       }
     }
     __syncthreads();
   }
-  if (out_t < rows) {
+  if (out_t < rows && (ROWS != 1 || threadIdx.x < 16)) {
     const float by = out_a < 0 ? 0.0f : scale[out_a] * (d.threshold ? d.scale : 1.0f);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
-      if (i * 16 + lane % 16 < rank) z[((size_t)part * rows + out_t) * rank + i * 16 + lane % 16] = own[i] * by;
+    {
+      const u32 r = i * 16 + lane % 16;
+      if (r < z_ld) z[((size_t)part * rows + out_t) * z_ld + r] = r < rank ? own[i] * by : 0.0f;
+      if (h && r < rank) h[(size_t)out_t * rank + r] = own[i] * by;
+    }
   }
 }
 
-// z[i] = sum over parts
-__global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, size_t count, float* z) {
+// z[i] = sum over parts, and without the places behind the rank to h
+__global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, size_t count, u32 z_ld, u32 rank, float* z, float* h) {
   const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
   if (i >= count) return;
   float s = 0.0f;
   for (u32 p = 0; p < parts; ++p) s += in[p * count + i];
-  z[i] = s;
+  if (z) z[i] = s;
+  const u32 r = (u32)(i % z_ld);
+  if (h && r < rank) h[i / z_ld * rank + r] = s;
 }
 
-// out[c, r] = in[r, c], `count` matrices of rows x cols one behind the other
+// Rows of `cols` elements to rows of `out_ld`, a multiple of eight, with zeros behind them.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_transpose(const T* in, size_t ld, size_t in_step, u32 rows, u32 cols, T* out, size_t out_step) {
+__global__ __launch_bounds__(kThreads) void k_pad(const T* in, size_t ld, u32 rows, u32 cols, T* out, u32 out_ld) {
+  const u32 groups = out_ld / 8;
+  const u64 at = (u64)blockIdx.x * kThreads + threadIdx.x;
+  if (at >= (u64)rows * groups) return;
+  const u32 r = (u32)(at / groups), c = (u32)(at - (u64)r * groups) * 8;
+  store_wide(out + (size_t)r * out_ld + c, load_some(in + (size_t)r * ld + c, c >= cols ? 0 : (int)(cols - c)));
+}
+
+// out[c, r] = in[r, c], rows of out out_ld apart with zeros behind them; matrices one behind the other
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_transpose(const T* in, size_t ld, size_t in_step, u32 rows, u32 cols, T* out, u32 out_ld,
+                                                        size_t out_step) {
   __shared__ T tile[64][66];
-  const u32 tiles_c = (cols + 63) / 64, tiles = tiles_c * ((rows + 63) / 64);
+  const u32 tiles_c = (cols + 63) / 64, tiles = tiles_c * ((out_ld + 63) / 64);
   const u32 which = blockIdx.x / tiles, at = blockIdx.x % tiles, r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
   in += which * in_step;
   out += which * out_step;
   for (u32 i = threadIdx.x; i < 64 * 64; i += kThreads) {
     const u32 r = r0 + i / 64, c = c0 + i % 64;
-    if (r < rows && c < cols) tile[i / 64][i % 64] = in[(size_t)r * ld + c];
+    tile[i / 64][i % 64] = r < rows && c < cols ? in[(size_t)r * ld + c] : (T)0.0f;
   }
   __syncthreads();
   for (u32 i = threadIdx.x; i < 64 * 64; i += kThreads) {
     const u32 c = c0 + i / 64, r = r0 + i % 64;
-    if (r < rows && c < cols) out[(size_t)c * rows + r] = tile[i % 64][i / 64];
+    if (r < out_ld && c < cols) out[(size_t)c * out_ld + r] = tile[i % 64][i / 64];
   }
 }
 
-// y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k]. A block of four wavefronts takes 128 rows by 128
-// outputs, a wavefront 64 x 64 as 4 x 4 products of 16 x 16; 128 bytes of the reduction at a time go through LDS.
-template <class T, bool WIDE, bool DROP>
-__global__ __launch_bounds__(kThreads) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, Low low, const float* z,
-                                                      const int* index, u32 rows, u32 inner, u32 outer, u32 parties, u32 rank, Drop d,
-                                                      T* y, size_t ldy) {
-  constexpr int KE = 128 / sizeof(T), kPitch = KE + 16 / sizeof(T), kVecs = KE / 8;  // elements of a step, of a row in LDS
-  constexpr int kLoads = 128 * kVecs / kThreads;
-  __shared__ __align__(16) T lx[128 * kPitch];
-  __shared__ __align__(16) T lw[128 * kPitch];
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 tiles_o = (outer + 127) / 128;
-  const u32 t0 = blockIdx.x / tiles_o * 128, o0 = blockIdx.x % tiles_o * 128;
-  const u32 wt = t0 + (wave & 1) * 64, wo = o0 + (wave >> 1) * 64;  // this wavefront's corner
-  f32x4 acc[4][4];  // [outputs / 16][rows / 16]
+// ---------------------------------------------------------------------------------------------------
+// The adapters' part of k_project on matrix instructions. z is float32: on 16-bit types it enters as two bfloat16 pieces, the
+// value cut to eight bits and what is left rounded to eight, 2^-17 of it off at most, which a result of 16 bits does not
+// show; a float16 adapter element is two bfloat16 pieces exactly. Pieces of one rank stand at different places of the
+// reduction.
+__device__ __forceinline__ __bf16 piece(float v, bool rest) {
+  const u32 b = __builtin_bit_cast(u32, v);
+  const float cut = __builtin_bit_cast(float, b & 0xFFFF0000u);
+  if ((b & 0x7F800000u) == 0x7F800000u) return rest ? (__bf16)0.0f : (__bf16)v;  // infinities and NaN
+  return (__bf16)(rest ? v - cut : cut);
+}
+// z and the adapters' rows are `ranks` long, a multiple of sixteen, with zeros behind the rank.
+constexpr u32 kRanks = 16;
+template <class T>
+struct LowPart;
+template <>
+struct LowPart<__bf16> {
+  static constexpr u32 kStep = 16;  // ranks of one product
+  using Frag = Vec8<__bf16>;
+  static __device__ __forceinline__ Frag of_z(const float* z) {
+    const u32 g = lane_id() / 16;
+    const Vec8<float> v = load_wide(z + (g & 1) * 8);
+    Frag f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  // the adapters' part, in 32 bits: once for every party among the 64 rows
-  int a[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const u32 t = wt + j * 16 + lane % 16;
-    a[j] = t < rows ? party_of(index, t, parties) : -1;
+    for (int e = 0; e < 8; ++e) f.v[e] = piece(v.v[e], g >= 2);
+    return f;
   }
-  const int a_of_lane = wt + lane < rows ? party_of(index, wt + lane, parties) : -1;
-  u64 left = __builtin_amdgcn_ballot_w64(a_of_lane >= 0);
-  while (left) {
-    const int who = __builtin_amdgcn_readlane(a_of_lane, __builtin_ctzll(left));
-    left &= ~__builtin_amdgcn_ballot_w64(a_of_lane == who);
-    const T* fa = f + (size_t)who * low.party_step;
-    // rows of other parties are left as they are, not added to with zeros: an adapter may hold infinities
+  static __device__ __forceinline__ Frag of_f(const __bf16* w) { return load_wide(w + (lane_id() / 16 & 1) * 8); }
+  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) { return mma32(f, z, acc); }
+};
+template <>
+struct LowPart<_Float16> {
+  static constexpr u32 kStep = 8;
+  using Frag = Vec8<__bf16>;
+  static __device__ __forceinline__ Frag of_z(const float* z) {
+    const Vec8<float> v = load_wide(z);
+    Frag f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f32x4 own[4];
+    for (int e = 0; e < 8; ++e) f.v[e] = piece(v.v[e], lane_id() / 16 & 1);
+    return f;
+  }
+  static __device__ __forceinline__ Frag of_f(const _Float16* w) {
+    const Vec8<_Float16> v = load_wide(w);
+    Frag f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) own[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      const u32 o = wo + i * 16 + lane % 16;
-      for (u32 r0 = 0; r0 < rank; r0 += 16) {
-        const u32 r = r0 + lane / 16 * 4;
-        float zv[4][4], fv[4];
+    for (int e = 0; e < 8; ++e) f.v[e] = piece((float)v.v[e], lane_id() / 16 >= 2);
+    return f;
+  }
+  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) { return mma32(f, z, acc); }
+};
+template <>
+struct LowPart<float> {
+  static constexpr u32 kStep = 16;
+  using Frag = f32x4;
+  static __device__ __forceinline__ Frag of_z(const float* z) {
+    Frag f;
+    __builtin_memcpy(&f, __builtin_assume_aligned(z + lane_id() / 16 * 4, 16), 16);
+    return f;
+  }
+  static __device__ __forceinline__ Frag of_f(const float* w) { return of_z(w); }
+  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], z[e], acc, 0, 0, 0);
+    return acc;
+  }
+};
+
+// Sixteen bytes a lane from memory to LDS, lane l's to `to` + 16 l.
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// A tile's row in LDS is 128 bytes, eight pieces of 16; piece c of row r lies at place c ^ (r / 2) % 8, which spreads the
+// sixteen rows that lanes read at once over all banks.
+__device__ __forceinline__ u32 place_of(u32 row, u32 piece) { return piece ^ (row >> 1 & 7); }
+template <class T>
+__device__ __forceinline__ Vec8<T> load_frag(const T* tile, u32 row, u32 k) {  // eight elements from the k-th of a row
+  constexpr u32 kPer = 16 / sizeof(T);
+  Vec8<T> v;
+#pragma unroll
+  for (u32 i = 0; i < 8 / kPer; ++i)
+    __builtin_memcpy(&v.v[i * kPer], __builtin_assume_aligned(tile + row * step_elems<T>() + place_of(row, k / kPer + i) * kPer, 16), 16);
+  return v;
+}
+
+// Four sums with the draws that two words hold.
+__device__ __forceinline__ void drop_four(f32x4& v, const Drop& d, u32 lo, u32 hi) {
+  v[0] = (lo & 0xFFFFu) >= d.threshold ? v[0] * d.scale : 0.0f;
+  v[1] = (lo >> 16) >= d.threshold ? v[1] * d.scale : 0.0f;
+  v[2] = (hi & 0xFFFFu) >= d.threshold ? v[2] * d.scale : 0.0f;
+  v[3] = (hi >> 16) >= d.threshold ? v[3] * d.scale : 0.0f;
+}
+
+// One step of the reduction: the next step's tiles are asked for, this one's multiplied.
+template <class T, int TM, int TN, int WAVES, int RT, int OT>
+__device__ __forceinline__ void project_step(const T* __restrict__ x, const size_t (&at_x)[TM / 8 / WAVES], const T* __restrict__ w,
+                                             const size_t (&at_w)[TN / 8 / WAVES], u32 k_next, bool more, u32 wave, u32 row0, u32 out0, const T* __restrict__ cx, const T* __restrict__ cw,
+                                             T* __restrict__ nx, T* __restrict__ nw, f32x4 (&acc)[OT][RT]) {
+  constexpr int KE = step_elems<T>();
+  if (more) {
+#pragma unroll
+    for (int i = 0; i < TM / 8 / WAVES; ++i) load_to_lds(x + at_x[i] + k_next, nx + (i * WAVES + wave) * 8 * KE);
+#pragma unroll
+    for (int i = 0; i < TN / 8 / WAVES; ++i) load_to_lds(w + at_w[i] + k_next, nw + (i * WAVES + wave) * 8 * KE);
+  }
+  const u32 lane = lane_id();
+#pragma unroll
+  for (int s = 0; s < KE / 32; ++s) {
+    Vec8<T> xv[RT], wv[OT];
+    const u32 k = s * 32 + lane / 16 * 8;
+#pragma unroll
+    for (int i = 0; i < OT; ++i) wv[i] = load_frag(cw, out0 + i * 16 + lane % 16, k);
+#pragma unroll
+    for (int j = 0; j < RT; ++j) xv[j] = load_frag(cx, row0 + j * 16 + lane % 16, k);
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int i = 0; i < OT; ++i) acc[i][j] = mma32(wv[i], xv[j], acc[i][j]);
+  }
+}
+
+// y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k], inner a multiple of a step. A block takes TM rows (of
+// `order`) by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
+// is filled while the other is read.
+template <class T, int TM, int TN, int WM, int WN, bool DROP>
+__global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
+                                                             const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
+                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, bool wide_y) {
+  constexpr int KE = step_elems<T>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
+  constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
+  __shared__ __align__(16) T lx0[TM * KE];
+  __shared__ __align__(16) T lw0[TN * KE];
+  __shared__ __align__(16) T lx1[TM * KE];
+  __shared__ __align__(16) T lw1[TN * KE];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  // Blocks are dealt to the eight dies in turn: each gets neighbouring tiles, four tiles of rows by all outputs at a time,
+  // whose operands its cache holds.
+  const u32 tiles_m = (rows + TM - 1) / TM, tiles_n = (outer + TN - 1) / TN, tiles = tiles_m * tiles_n;
+  const u32 die = blockIdx.x % 8, per = tiles / 8, over = tiles % 8;
+  const u32 tile = die * per + (die < over ? die : over) + blockIdx.x / 8;
+  const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
+  const u32 t0 = (band * 4 + in_band % high) * TM, o0 = in_band / high * TN;
+  const u32 row0 = wave / WN * (TM / WM), out0 = wave % WN * (TN / WN);  // this wavefront's corner
+
+  size_t at_x[LX], at_w[LW];  // of this lane's pieces
+#pragma unroll
+  for (int i = 0; i < LX; ++i) {
+    const u32 r = (i * WAVES + wave) * 8 + lane / 8, at = t0 + r < rows ? t0 + r : rows - 1;
+    at_x[i] = (size_t)order[at] * ldx + place_of(r, lane % 8) * (16 / sizeof(T));
+  }
+#pragma unroll
+  for (int i = 0; i < LW; ++i) {
+    const u32 r = (i * WAVES + wave) * 8 + lane / 8, o = o0 + r < outer ? o0 + r : outer - 1;
+    at_w[i] = (size_t)o * ldw + place_of(r, lane % 8) * (16 / sizeof(T));
+  }
+#pragma unroll
+  for (int i = 0; i < LX; ++i) load_to_lds(x + at_x[i], lx0 + (i * WAVES + wave) * 8 * KE);
+#pragma unroll
+  for (int i = 0; i < LW; ++i) load_to_lds(w + at_w[i], lw0 + (i * WAVES + wave) * 8 * KE);
+
+  f32x4 acc[OT][RT];
+  u32 t[RT];  // this lane's rows, `rows`: none
+#pragma unroll
+  for (int j = 0; j < RT; ++j) {
+    const u32 at = t0 + row0 + j * 16 + lane % 16;
+    t[j] = at < rows ? order[at] : rows;
+#pragma unroll
+    for (int i = 0; i < OT; ++i) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  for (u32 k = 0; k < inner; k += 2 * KE) {
+    __syncthreads();
+    project_step<T, TM, TN, WAVES, RT, OT>(x, at_x, w, at_w, k + KE, k + KE < inner, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
+    __syncthreads();
+    if (k + KE < inner)
+      project_step<T, TM, TN, WAVES, RT, OT>(x, at_x, w, at_w, k + 2 * KE, k + 2 * KE < inner, wave, row0, out0, lx1, lw1, lx0, lw0, acc);
+  }
+  // the adapters' part, party by party along the list
+  using Low = LowPart<T>;
+  const u32 wave_at = t0 + row0, listed = begin[parties], wave_end = wave_at + TM / WM < rows ? wave_at + TM / WM : rows;
+  for (u32 at = wave_at; at < wave_end && at < listed;) {
+    const int who = index[order[at]];
+    const u32 next = begin[who + 1];
+#pragma unroll
+    for (int j = 0; j < RT; j += 2) {
+      const u32 p = wave_at + j * 16 + lane % 16;
+      const bool mine0 = p >= at && p < next, mine1 = p + 16 >= at && p + 16 < next;
+      if (__builtin_amdgcn_ballot_w64(mine0 || mine1) == 0) continue;
+      f32x4 low0[OT], low1[OT];
+#pragma unroll
+      for (int i = 0; i < OT; ++i) low0[i] = low1[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (u32 r0 = 0; r0 < ranks; r0 += Low::kStep) {
+        const typename Low::Frag z0 = Low::of_z(z + (size_t)(t[j] < rows ? t[j] : 0) * ranks + r0);
+        const typename Low::Frag z1 = Low::of_z(z + (size_t)(t[j + 1] < rows ? t[j + 1] : 0) * ranks + r0);
+#pragma unroll
+        for (int i = 0; i < OT; ++i) {
+          const u32 o = o0 + out0 + i * 16 + lane % 16;
+          const typename Low::Frag fv = Low::of_f(f + ((size_t)who * outer + (o < outer ? o : outer - 1)) * ranks + r0);
+          low0[i] = Low::mma(fv, z0, low0[i]);
+          low1[i] = Low::mma(fv, z1, low1[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < OT; ++i) {
+        if (DROP) {
+          // A lane's four outputs are half of a generator's call, the other half is the lane's beside it: of two rows' calls
+          // each makes one, and they exchange halves.
+          const bool odd = (lane & 16) != 0;
+          const u32x4 draws = philox(d, (o0 + out0 + i * 16 + lane / 16 * 4) >> 3, t[j] ^ ((t[j] ^ t[j + 1]) & (0u - (u32)odd)));
+          const u32 give0 = odd ? draws[0] : draws[2], give1 = odd ? draws[1] : draws[3];
+          const u32 keep0 = odd ? draws[2] : draws[0], keep1 = odd ? draws[3] : draws[1];
+          const u32 got0 = lane_read(give0, (int)(lane ^ 16)), got1 = lane_read(give1, (int)(lane ^ 16));
+          drop_four(low0[i], d, odd ? got0 : keep0, odd ? got1 : keep1);
+          drop_four(low1[i], d, odd ? keep0 : got0, odd ? keep1 : got1);
+        }
+        // nothing is added to other parties' rows, not even zeros' products: an adapter may hold infinities
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          fv[e] = o < outer && r + e < rank ? (float)fa[o * low.out_step + (r + e) * low.r_step] : 0.0f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) zv[j][e] = a[j] == who && r + e < rank ? z[(size_t)(wt + j * 16 + lane % 16) * rank + r + e] : 0.0f;
+          acc[i][j][e] += mine0 ? low0[i][e] : 0.0f;
+          acc[i][j + 1][e] += mine1 ? low1[i][e] : 0.0f;
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) own[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fv[e], zv[j][e], own[j], 0, 0, 0);
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (a[j] == who) acc[i][j] = own[j];
     }
-  }
-  if (DROP) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32 o = wo + i * 16 + lane / 16 * 4;
-        const u32x4 draws = philox(d, o >> 3, wt + j * 16 + lane % 16);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = kept(d, draws, (o & 4) + e) ? acc[i][j][e] * d.scale : 0.0f;
-      }
+    at = next;
   }
 
-  Vec8<T> gx[kLoads], gw[kLoads];
-  const auto fetch = [&](u32 k0) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const u32 c = threadIdx.x + i * kThreads, r = c / kVecs, k = k0 + c % kVecs * 8;
-      gx[i] = load_tile<T, WIDE>(x, ldx, t0 + r, rows, k, inner);
-      gw[i] = load_tile<T, WIDE>(w, ldw, o0 + r, outer, k, inner);
-    }
-  };
-  fetch(0);
-  for (u32 k0 = 0; k0 < inner; k0 += KE) {
-    __syncthreads();
+  for (int j = 0; j < RT; ++j) {
+    if (t[j] >= rows) continue;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const u32 c = threadIdx.x + i * kThreads, r = c / kVecs, k = c % kVecs * 8;
-      store_wide(lx + r * kPitch + k, gx[i]);
-      store_wide(lw + r * kPitch + k, gw[i]);
-    }
-    __syncthreads();
-    if (k0 + KE < inner) fetch(k0 + KE);
+    for (int i = 0; i < OT; ++i) {
+      const u32 o = o0 + out0 + i * 16 + lane / 16 * 4;
+      T* const to = y + (size_t)t[j] * ldy + o;
+      T v[4];
 #pragma unroll
-    for (int s = 0; s < KE / 32; ++s) {
-      Vec8<T> xv[4], wv[4];
-      const u32 k = s * 32 + lane / 16 * 8;
+      for (int e = 0; e < 4; ++e) v[e] = (T)acc[i][j][e];
+      if (wide_y && o + 4 <= outer) {
+        __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(T)), v, sizeof(v));
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) xv[j] = load_wide(lx + (wt - t0 + j * 16 + lane % 16) * kPitch + k);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) wv[i] = load_wide(lw + (wo - o0 + i * 16 + lane % 16) * kPitch + k);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mma32(wv[i], xv[j], acc[i][j]);
+        for (int e = 0; e < 4; ++e)
+          if (o + e < outer) to[e] = v[e];
+      }
     }
   }
+}
+
+// The same for few rows: W's rows are read once, by as many blocks as it has sixteens of them. A block's eight wavefronts
+// share the reduction, 64 elements each in turn; the adapters' part is added where they are joined. Parts of z are summed here, and
+// h, where it is wanted, is written by the first block.
+constexpr int kFewWaves = 8;
+template <class T, int RT, bool DROP>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld,
+                                                                   const float* z, u32 z_ld, u32 parts, const int* index, u32 rows, u32 inner, u32 outer, u32 parties,
+                                                                   u32 rank, Drop d, T* y, size_t ldy, float* h) {
+  constexpr int kThreadsFew = kFewWaves * kWave, kAhead = RT >= 4 ? 2 : 4;  // steps of 32
+  __shared__ float sum[kFewWaves][RT * 16][17];
+  __shared__ float zl[RT * 16 * 16];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  const u32 tiles_n = (outer + 15) / 16, t0 = blockIdx.x / tiles_n * (RT * 16), o0 = blockIdx.x % tiles_n * 16;
+  f32x4 acc[RT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int j = 0; j < RT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const u32 o = o0 + lane % 16;
+  for (u32 k0 = wave * 64; k0 < inner; k0 += kFewWaves * 64 * (kAhead / 2)) {
+    Vec8<T> wv[kAhead], xv[kAhead][RT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const u32 t = wt + j * 16 + lane % 16, o = wo + i * 16 + lane / 16 * 4;
-      if (t >= rows) continue;
+    for (int u = 0; u < kAhead; ++u) {
+      const u32 k = k0 + u / 2 * (kFewWaves * 64) + u % 2 * 32 + lane / 16 * 8;
+      wv[u] = load_tile(w, ldw, o, outer, k, inner);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (o + e < outer) y[(size_t)t * ldy + o + e] = (T)acc[i][j][e];
+      for (int j = 0; j < RT; ++j) xv[u][j] = load_tile(x, ldx, t0 + j * 16 + lane % 16, rows, k, inner);
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) acc[j] = mma32(wv[u], xv[u][j], acc[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < RT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[wave][j * 16 + lane % 16][lane / 16 * 4 + e] = acc[j][e];
+  constexpr int kOwn = RT * 256 / kThreadsFew > 0 ? RT * 256 / kThreadsFew : 1;
+  float low[kOwn];
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q) low[q] = 0.0f;
+  for (u32 r0 = 0; r0 < rank; r0 += 16) {
+    for (u32 i = threadIdx.x; i < RT * 256; i += kThreadsFew) {
+      const u32 t = t0 + i / 16, r = r0 + i % 16;
+      float s = 0.0f;
+      if (t < rows && r < rank) {
+        for (u32 p = 0; p < parts; ++p) s += z[((size_t)p * rows + t) * z_ld + r];
+        if (h && o0 == 0) h[(size_t)t * rank + r] = s;
+      }
+      zl[i] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+      const u32 i = threadIdx.x + q * kThreadsFew, t = t0 + i / 16, oo = o0 + i % 16;
+      const int a = i < RT * 256 && t < rows && oo < outer ? party_of(index, t, parties) : -1;
+      if (a >= 0) {
+        const T* const fr = f + ((size_t)a * outer + oo) * f_ld + r0;
+        const u32 n = rank - r0 < 16 ? rank - r0 : 16;
+        for (u32 r = 0; r < n; ++r) low[q] += zl[i / 16 * 16 + r] * (float)fr[r];
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q) {
+    const u32 i = threadIdx.x + q * kThreadsFew, t = t0 + i / 16, oo = o0 + i % 16;
+    if (i >= RT * 256 || t >= rows || oo >= outer) continue;
+    float s = low[q];
+    if (DROP) {
+      const u32x4 draws = philox(d, oo >> 3, t);
+      s = (draws[oo >> 1 & 3] >> (16 * (oo & 1)) & 0xFFFFu) >= d.threshold ? s * d.scale : 0.0f;
+    }
+    float m = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kFewWaves; ++v) m += sum[v][i / 16][i % 16];
+    y[(size_t)t * ldy + oo] = (T)(m + s);
+  }
 }
 
 constexpr u32 kGradRows = 128;  // rows of one chunk of a party's list
 constexpr u32 kGroupCounts = 16384;
-inline u32 group_waves(size_t parties) { return parties <= 1024 ? 16 : 4; }  // whose counts fit LDS
+inline u32 group_waves(size_t parties) { return parties < 1024 ? 16 : 3; }  // whose counts fit LDS
 
-// Groups the rows by adapter: `list` holds the rows of party 0 in ascending order, then those of party 1, ...;
-// begin[p] where p's start; chunk_begin[p] the first of p's chunks of kGradRows rows; chunk[c] = p. One block; its
-// wavefronts take a range of rows each, count them, and list them from where their counts say.
-__global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 parties, u32* begin, u32* chunk_begin, u32* chunk, u32* list,
+// Groups the rows by adapter: `order` holds the rows of party 0 in ascending order, then those of party 1, ..., at last
+// those without; begin[p] is where p's start, begin[parties] where the last begin; chunk_begin[p] the first of p's chunks of
+// kGradRows rows; chunk[c] = p. One block; its wavefronts take a range of rows each, count them, and list them from where their
+// counts say.
+__global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 parties, u32* begin, u32* chunk_begin, u32* chunk, u32* order,
                                                 u32* status) {
+  constexpr int kAhead = 8;
   __shared__ u32 counts[kGroupCounts];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), waves = blockDim.x / kWave;
-  const u32 per = (rows + waves - 1) / waves, first = wave * per < rows ? wave * per : rows, end = rows - first < per ? rows : first + per;
-  for (u32 i = threadIdx.x; i < waves * parties; i += blockDim.x) counts[i] = 0;
+  const u32 bins = parties + 1;
+  const u32 per = ((rows + waves - 1) / waves + kWave - 1) / kWave * kWave;
+  const u32 first = (u64)wave * per < rows ? wave * per : rows, end = rows - first < per ? rows : first + per;
+  for (u32 i = threadIdx.x; i < waves * bins; i += blockDim.x) counts[i] = 0;
   __syncthreads();
   for (int pass = 0; pass < 2; ++pass) {
-    for (u32 t0 = first; t0 < end; t0 += kWave) {
-      const u32 t = t0 + lane;
-      const int raw = t < end ? index[t] : -1;
-      const int a = (u32)raw < parties ? raw : -1;
-      if (pass == 0 && raw != a && raw != -1 && status) atomicOr(status, HAFLO_ST_RANGE);
-      u64 left = __builtin_amdgcn_ballot_w64(a >= 0);
-      while (left) {
-        const int leader = __builtin_ctzll(left), who = __builtin_amdgcn_readlane(a, leader);
-        const u64 same = __builtin_amdgcn_ballot_w64(a == who);
-        left &= ~same;
-        u32 at = 0;
-        if ((int)lane == leader) at = atomicAdd(&counts[wave * parties + who], (u32)__builtin_popcountll(same));
-        at = (u32)__builtin_amdgcn_readlane((int)at, leader);
-        if (pass == 1 && a == who) list[at + (u32)__builtin_popcountll(same & ((1ull << lane) - 1))] = t;
+    for (u32 base = first; base < end; base += kAhead * kWave) {
+      int raw[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32 t = base + i * kWave + lane;
+        raw[i] = t < end ? index[t] : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32 t = base + i * kWave + lane;
+        const u32 a = (u32)raw[i] < parties ? (u32)raw[i] : parties;
+        if (pass == 0 && a == parties && raw[i] != -1 && status) atomicOr(status, HAFLO_ST_RANGE);
+        u64 left = __builtin_amdgcn_ballot_w64(t < end);
+        while (left) {
+          const int leader = __builtin_ctzll(left);
+          const u32 who = (u32)__builtin_amdgcn_readlane((int)a, leader);
+          const u64 same = __builtin_amdgcn_ballot_w64(a == who) & left;
+          left &= ~same;
+          u32 at = 0;
+          if ((int)lane == leader) at = atomicAdd(&counts[wave * bins + who], (u32)__builtin_popcountll(same));
+          at = (u32)__builtin_amdgcn_readlane((int)at, leader);
+          if (pass == 1 && (same >> lane & 1)) order[at + (u32)__builtin_popcountll(same & ((1ull << lane) - 1))] = t;
+        }
       }
     }
     __syncthreads();
-    if (pass == 0 && threadIdx.x == 0) {  // counts to places
+    if (pass == 0 && wave == 0) {  // counts to places, 64 parties at a time
       u32 at = 0, chunks = 0;
-      for (u32 p = 0; p < parties; ++p) {
-        begin[p] = at;
-        chunk_begin[p] = chunks;
+      for (u32 p0 = 0; p0 < bins; p0 += kWave) {
+        const u32 p = p0 + lane;
         u32 n = 0;
-        for (u32 w = 0; w < waves; ++w) {
-          const u32 c = counts[w * parties + p];
-          counts[w * parties + p] = at + n;
-          n += c;
+        for (u32 w = 0; w < waves; ++w) n += p < bins ? counts[w * bins + p] : 0;
+        u32 to = n, c = p < parties ? (n + kGradRows - 1) / kGradRows : 0, c_to = c;
+#pragma unroll
+        for (int s = 1; s < kWave; s <<= 1) {  // sums up to each lane
+          const u32 below = lane_read(to, (int)lane - s), c_below = lane_read(c_to, (int)lane - s);
+          if ((int)lane >= s) {
+            to += below;
+            c_to += c_below;
+          }
         }
-        at += n;
-        for (u32 i = 0; i < n; i += kGradRows) chunk[chunks++] = p;
+        u32 place = at + to - n;
+        if (p < bins) {
+          begin[p] = place;
+          chunk_begin[p] = chunks + c_to - c;
+          for (u32 i = 0; i < c; ++i) chunk[chunks + c_to - c + i] = p;
+          for (u32 w = 0; w < waves; ++w) {
+            const u32 m = counts[w * bins + p];
+            counts[w * bins + p] = place;
+            place += m;
+          }
+        }
+        at += (u32)__builtin_amdgcn_readlane((int)to, kWave - 1);
+        chunks += (u32)__builtin_amdgcn_readlane((int)c_to, kWave - 1);
       }
-      begin[parties] = at;
-      chunk_begin[parties] = chunks;
     }
     __syncthreads();
   }
@@ -301,8 +564,8 @@ __global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 
 
 // out[chunk][r][col] = sum over the chunk's rows t of z[t, r] drop(m[t, col]): a block takes 512 columns and sixteen r,
 // its wavefronts a quarter of the rows each, a lane eight columns.
-template <class T, bool WIDE>
-__global__ __launch_bounds__(kThreads) void k_grad(const T* m, size_t ld, u32 cols, const float* z, u32 rank, u32 parties, const u32* begin,
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_grad(const T* m, size_t ld, u32 cols, const float* z, u32 z_ld, u32 rank, u32 parties, const u32* begin,
                                                    const u32* chunk_begin, const u32* chunk, const u32* list, Drop d, float* out) {
   constexpr int kR = 16;
   __shared__ float sum[kR / 2][kWave * 8];
@@ -320,14 +583,14 @@ __global__ __launch_bounds__(kThreads) void k_grad(const T* m, size_t ld, u32 co
     for (int j = 0; j < 8; ++j) acc[r][j] = 0.0f;
   for (u32 i = first + wave; i < end; i += kThreads / kWave) {
     const u32 t = (u32)__builtin_amdgcn_readfirstlane((int)list[i]);
-    Vec8<T> v = load_tile<T, WIDE>(m + (size_t)t * ld, ld, 0, 1, col, cols);
+    Vec8<T> v = load_tile(m + (size_t)t * ld, ld, 0, 1, col, cols);
     if (d.threshold) apply_drop(v, d, t, col);
     float f[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = (float)v.v[j];
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
-      const float zr = r0 + r < rank ? z[(size_t)t * rank + r0 + r] : 0.0f;
+      const float zr = r0 + r < rank ? z[(size_t)t * z_ld + r0 + r] : 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[r][j] += zr * f[j];
     }
@@ -377,14 +640,17 @@ bool adapter_sizes(int type, const Sizes& s) {
          s.outer <= kMostCount - 512 && s.parties >= 1 && s.parties <= HAFLO_ADAPTER_MAX_PARTIES && s.rank >= 1 &&
          s.rank <= HAFLO_ADAPTER_MAX_RANK;
 }
+constexpr size_t kFewRows = 64;  // up to here k_project_few
 // parts of k_shrink's reduction: enough blocks to fill the chip, at least 512 columns each
 u32 shrink_parts(size_t rows, size_t k) {
   if (rows == 0) return 1;
-  const size_t tiles = ceil_div(rows, 16), want = tiles < 512 ? ceil_div(512, tiles) : 1, most = ceil_div(k, 512);
+  const size_t tiles = rows <= kFewRows ? rows : ceil_div(rows, 16), want = tiles < 512 ? ceil_div(512, tiles) : 1, most = ceil_div(k, 512);
   return (u32)(want < most ? want : most);
 }
+size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * (128 / type_size(type)); }
+size_t whole_ranks(size_t rank) { return ceil_div(rank, kRanks) * kRanks; }
 struct Plan {
-  size_t z_parts, z, w_t, b_t, begin, chunk_begin, chunk, list, sums, total;
+  size_t z_parts, z, x, dy, w, low, f, begin, chunk_begin, chunk, order, sums, total;
   size_t chunks;  // at most
 };
 Plan adapter_plan(int type, bool backward, const Sizes& s) {
@@ -395,87 +661,152 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
     b += align256(bytes);
     return at;
   };
-  const size_t e = type_size(type), k = backward ? s.outer : s.inner, parts = shrink_parts(s.rows, k);
-  p.z_parts = take(parts > 1 ? parts * s.rows * s.rank * 4 : 0);
+  const size_t e = type_size(type), ranks = whole_ranks(s.rank);
+  const size_t k = backward ? s.outer : s.inner, n = backward ? s.inner : s.outer, kp = padded(type, k);  // the product's sizes
+  p.z_parts = take(shrink_parts(s.rows, k) * s.rows * ranks * 4);
+  p.z = take(s.rows * ranks * 4);
+  p.x = take(s.rows * padded(type, s.inner) * e);
+  p.w = take(n * kp * e);
+  p.low = take(s.parties * s.rank * kp * e);
+  p.f = take(s.parties * n * ranks * e);
+  p.chunks = s.rows / kGradRows + s.parties;
+  p.begin = take((s.parties + 1) * 4);
+  p.chunk_begin = take((s.parties + 1) * 4);
+  p.chunk = take(p.chunks * 4);
+  p.order = take(s.rows * 4);
   if (backward) {
-    p.z = take(s.rows * s.rank * 4);
-    p.w_t = take(s.inner * s.outer * e);
-    p.b_t = take(s.parties * s.outer * s.rank * e);
-    p.chunks = s.rows / kGradRows + s.parties;
-    p.begin = take((s.parties + 1) * 4);
-    p.chunk_begin = take((s.parties + 1) * 4);
-    p.chunk = take(p.chunks * 4);
-    p.list = take(s.rows * 4);
+    p.dy = take(s.rows * kp * e);
     p.sums = take(p.chunks * s.rank * (s.inner > s.outer ? s.inner : s.outer) * 4);
   }
   p.total = b;
   return p;
 }
 
+// A matrix with rows at 16-byte boundaries and of a multiple of `step` elements, zeros behind what they hold: itself, or its
+// copy at `room`.
 template <class T>
-void shrink(const T* x, size_t ldx, const T* f, const float* scale, const int* index, size_t rows, size_t inner, size_t rank,
-            size_t parties, const Drop& d, float* z_parts, float* z, u32* status, hipStream_t st) {
-  const u32 parts = shrink_parts(rows, inner);
-  const dim3 grid((unsigned)(ceil_div(rows, 16) * parts)), block(kThreads);
-  const bool wide = wide_rows<T>(x, ldx) && wide_rows<T>(f, inner);
-  float* const to = parts > 1 ? z_parts : z;
-#define HAFLO_LOCAL_RUN(WIDE, RT)                                                                                                     \
-  hipLaunchKernelGGL((k_shrink<T, WIDE, RT>), grid, block, 0, st, x, ldx, f, scale, index, (u32)rows, (u32)inner, (u32)rank, (u32)parties, d, \
-                     parts, to, status)
-#define HAFLO_LOCAL_RANK(WIDE)                  \
-  do {                                          \
-    if (rank <= 16) HAFLO_LOCAL_RUN(WIDE, 1);   \
-    else if (rank <= 64) HAFLO_LOCAL_RUN(WIDE, 4); \
-    else HAFLO_LOCAL_RUN(WIDE, 8);              \
+struct Rows {
+  const T* p;
+  size_t ld;
+};
+template <class T>
+Rows<T> lay_out(const void* m, size_t ld, size_t rows, size_t cols, size_t step, char* room, hipStream_t st) {
+  if (wide_rows<T>(m, ld) && cols % step == 0) return {(const T*)m, ld};
+  const size_t to = ceil_div(cols, step < 8 ? 8 : step) * (step < 8 ? 8 : step);
+  hipLaunchKernelGGL((k_pad<T>), dim3((unsigned)ceil_div(rows * (to / 8), kThreads)), dim3(kThreads), 0, st, (const T*)m, ld, (u32)rows, (u32)cols,
+                     (T*)room, (u32)to);
+  return {(const T*)room, to};
+}
+
+template <class T>
+Rows<T> transpose(const void* in, size_t ld, size_t in_step, size_t rows, size_t cols, size_t count, char* out, size_t out_ld, hipStream_t st) {
+  const size_t tiles = ceil_div(out_ld, 64) * ceil_div(cols, 64);
+  hipLaunchKernelGGL((k_transpose<T>), dim3((unsigned)(tiles * count)), dim3(kThreads), 0, st, (const T*)in, ld, in_step, (u32)rows, (u32)cols,
+                     (T*)out, (u32)out_ld, cols * out_ld);
+  return {(const T*)out, out_ld};
+}
+
+// What both directions do: z from x and the low-rank rows `low`, then x against `w` with `f` (outer x rank of every party).
+template <class T>
+struct Product {
+  Rows<T> x, w, low, f;
+  const float* scale;
+  const int* index;
+  Sizes s;  // `inner` is the reduction's length, `outer` the result's
+  Drop before, after;
+  char* ws;
+  Plan plan;
+  u32* status;
+  hipStream_t st;
+
+  bool few() const { return s.rows <= kFewRows; }
+  u32 ranks() const { return (u32)whole_ranks(s.rank); }
+  size_t padded_inner() const { return ceil_div(s.inner, step_elems<T>()) * step_elems<T>(); }
+  const u32* order() const { return few() ? nullptr : (const u32*)(ws + plan.order); }
+  float* z_parts() const { return (float*)(ws + plan.z_parts); }
+  float* z() const { return (float*)(ws + plan.z); }
+
+  // z, or with few rows its parts; dense as `h` too unless that is null
+  void shrink(float* h) const {
+    const u32 parts = shrink_parts(s.rows, s.inner);
+    const dim3 grid((unsigned)((few() ? s.rows : ceil_div(s.rows, 16)) * parts)), block(kThreads);
+    float* const to = few() || parts > 1 ? z_parts() : z();
+    float* const h_now = parts > 1 ? nullptr : h;
+#define HAFLO_LOCAL_RUN(ROWS, RT)                                                                                                            \
+  hipLaunchKernelGGL((k_shrink<T, ROWS, RT>), grid, block, 0, st, x.p, x.ld, low.p, low.ld, scale, index, order(), (u32)s.rows, (u32)s.inner, \
+                     (u32)s.rank, (u32)s.parties, before, parts, ranks(), to, h_now, status)
+#define HAFLO_LOCAL_RANK(ROWS)                        \
+  do {                                                \
+    if (s.rank <= 16) HAFLO_LOCAL_RUN(ROWS, 1);       \
+    else if (s.rank <= 64) HAFLO_LOCAL_RUN(ROWS, 4);  \
+    else HAFLO_LOCAL_RUN(ROWS, 8);                    \
   } while (0)
-  if (wide) HAFLO_LOCAL_RANK(true);
-  else HAFLO_LOCAL_RANK(false);
+    if (few()) HAFLO_LOCAL_RANK(1);
+    else HAFLO_LOCAL_RANK(16);
 #undef HAFLO_LOCAL_RANK
 #undef HAFLO_LOCAL_RUN
-  if (parts > 1)
-    hipLaunchKernelGGL(k_join, dim3((unsigned)ceil_div(rows * rank, kThreads)), block, 0, st, z_parts, parts, rows * rank, z);
-}
-
-template <class T>
-void project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const Low& low, const float* z, const int* index, size_t rows,
-             size_t inner, size_t outer, size_t parties, size_t rank, const Drop& d, T* y, size_t ldy, hipStream_t st) {
-  const dim3 grid((unsigned)(ceil_div(rows, 128) * ceil_div(outer, 128))), block(kThreads);
-  const bool wide = wide_rows<T>(x, ldx) && wide_rows<T>(w, ldw);
-#define HAFLO_LOCAL_RUN(WIDE, DROP)                                                                                                       \
-  hipLaunchKernelGGL((k_project<T, WIDE, DROP>), grid, block, 0, st, x, ldx, w, ldw, f, low, z, index, (u32)rows, (u32)inner, (u32)outer, \
-                     (u32)parties, (u32)rank, d, y, ldy)
-  if (d.threshold) {
-    if (wide) HAFLO_LOCAL_RUN(true, true);
-    else HAFLO_LOCAL_RUN(false, true);
-  } else {
-    if (wide) HAFLO_LOCAL_RUN(true, false);
-    else HAFLO_LOCAL_RUN(false, false);
+    if (!few() && parts > 1) join(h);
   }
+  void join(float* h) const {
+    const size_t count = s.rows * ranks();
+    hipLaunchKernelGGL(k_join, dim3((unsigned)ceil_div(count, kThreads)), dim3(kThreads), 0, st, (const float*)z_parts(),
+                       shrink_parts(s.rows, s.inner), count, ranks(), (u32)s.rank, z(), h);
+  }
+
+  // `h`: where few rows' z goes that has been in parts, or null
+  void project(float* h, T* y, size_t ldy) const {
+    if (few()) {
+      const u32 parts = shrink_parts(s.rows, s.inner);
+#define HAFLO_LOCAL_RUN(RT, DROP)                                                                                                        \
+  hipLaunchKernelGGL((k_project_few<T, RT, DROP>), dim3((unsigned)(ceil_div(s.rows, RT * 16) * ceil_div(s.outer, 16))),                  \
+                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, (const float*)z_parts(), ranks(), parts, index, \
+                     (u32)s.rows, (u32)s.inner, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, y, ldy, parts > 1 ? h : nullptr)
+#define HAFLO_LOCAL_FEW(DROP)                        \
+  do {                                               \
+    if (s.rows <= 16) HAFLO_LOCAL_RUN(1, DROP);      \
+    else if (s.rows <= 32) HAFLO_LOCAL_RUN(2, DROP); \
+    else HAFLO_LOCAL_RUN(4, DROP);                   \
+  } while (0)
+      if (after.threshold) HAFLO_LOCAL_FEW(true);
+      else HAFLO_LOCAL_FEW(false);
+#undef HAFLO_LOCAL_FEW
 #undef HAFLO_LOCAL_RUN
+      return;
+    }
+    const bool wide_y = (uintptr_t)y % (4 * sizeof(T)) == 0 && ldy % 4 == 0;
+#define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP)                                                                                             \
+  hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP>), dim3((unsigned)(ceil_div(s.rows, TM) * ceil_div(s.outer, TN))),                \
+                     dim3(WM * WN * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (const float*)z(), index, order(),                          \
+                     (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(), after, y, ldy, wide_y)
+#define HAFLO_LOCAL_TILE(DROP)                                                                                \
+  do {                                                                                                        \
+    if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP);         \
+    else if (ceil_div(s.rows, 128) * ceil_div(s.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, DROP);    \
+    else HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP);                                                                 \
+  } while (0)
+    if (after.threshold) HAFLO_LOCAL_TILE(true);
+    else HAFLO_LOCAL_TILE(false);
+#undef HAFLO_LOCAL_TILE
+#undef HAFLO_LOCAL_RUN
+  }
+};
+
+void group(const Sizes& s, const int* index, char* ws, const Plan& p, u32* status, hipStream_t st) {
+  hipLaunchKernelGGL(k_group, dim3(1), dim3(group_waves(s.parties) * kWave), 0, st, index, (u32)s.rows, (u32)s.parties, (u32*)(ws + p.begin),
+                     (u32*)(ws + p.chunk_begin), (u32*)(ws + p.chunk), (u32*)(ws + p.order), status);
 }
 
 template <class T>
-void grad(const T* m, size_t ld, size_t cols, const float* z, const Sizes& s, const Plan& p, char* ws, const Drop& d, size_t r_step,
+void grad(const Rows<T>& m, size_t cols, const float* z, size_t z_ld, const Sizes& s, const Plan& p, char* ws, const Drop& d, size_t r_step,
           size_t col_step, float* out, hipStream_t st) {
   const dim3 block(kThreads);
-  const dim3 grid((unsigned)(p.chunks * ceil_div(cols, 512) * ceil_div(s.rank, 16)));
-  const u32* begin = (const u32*)(ws + p.begin);
   const u32* chunk_begin = (const u32*)(ws + p.chunk_begin);
   float* const sums = (float*)(ws + p.sums);
-#define HAFLO_LOCAL_RUN(WIDE)                                                                                                          \
-  hipLaunchKernelGGL((k_grad<T, WIDE>), grid, block, 0, st, m, ld, (u32)cols, z, (u32)s.rank, (u32)s.parties, begin, chunk_begin,      \
-                     (const u32*)(ws + p.chunk), (const u32*)(ws + p.list), d, sums)
-  if (wide_rows<T>(m, ld)) HAFLO_LOCAL_RUN(true);
-  else HAFLO_LOCAL_RUN(false);
-#undef HAFLO_LOCAL_RUN
+  hipLaunchKernelGGL((k_grad<T>), dim3((unsigned)(p.chunks * ceil_div(cols, 512) * ceil_div(s.rank, 16))), block, 0, st, m.p, m.ld, (u32)cols, z,
+                     (u32)z_ld, (u32)s.rank, (u32)s.parties, (const u32*)(ws + p.begin), chunk_begin, (const u32*)(ws + p.chunk),
+                     (const u32*)(ws + p.order), d, sums);
   hipLaunchKernelGGL(k_grad_join, dim3((unsigned)(s.parties * ceil_div(s.rank * cols, kThreads))), block, 0, st, (const float*)sums, chunk_begin,
                      (u32)s.rank, (u32)cols, r_step, col_step, out);
-}
-
-template <class T>
-void transpose(const T* in, size_t ld, size_t in_step, size_t rows, size_t cols, size_t count, T* out, size_t out_step, hipStream_t st) {
-  const size_t tiles = ceil_div(rows, 64) * ceil_div(cols, 64);
-  hipLaunchKernelGGL((k_transpose<T>), dim3((unsigned)(tiles * count)), dim3(kThreads), 0, st, in, ld, in_step, (u32)rows, (u32)cols, out, out_step);
 }
 
 }  // namespace
@@ -496,16 +827,22 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
   if (rows == 0) return HAFLO_OK;
   if (!d_x || ldx < inner || !d_w || ldw < inner || !d_a || !d_b || !d_scale || !d_index || !d_y || ldy < outer || !d_h) return HAFLO_EINVAL;
   const Plan plan = adapter_plan(type, false, s);
-  if (plan.total && (!d_workspace || workspace_bytes < plan.total)) return HAFLO_EINVAL;
+  if (!d_workspace || workspace_bytes < plan.total) return HAFLO_EINVAL;
   char* const ws = (char*)d_workspace;
   const hipStream_t st = (hipStream_t)stream;
   const Drop d = make_drop(p, seed, offset);
   Drop none = d;
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
-    shrink<T>((const T*)d_x, ldx, (const T*)d_a, d_scale, d_index, rows, inner, rank, parties, d, (float*)(ws + plan.z_parts), d_h, d_status, st);
-    const Low low = {outer * rank, rank, 1};
-    project<T>((const T*)d_x, ldx, (const T*)d_w, ldw, (const T*)d_b, low, d_h, d_index, rows, inner, outer, parties, rank, none, (T*)d_y, ldy, st);
+    const bool many = rows > kFewRows;
+    const size_t step = many ? step_elems<T>() : 1;
+    if (many) group(s, d_index, ws, plan, d_status, st);
+    Product<T> f = {lay_out<T>(d_x, ldx, rows, inner, step, ws + plan.x, st), lay_out<T>(d_w, ldw, outer, inner, step, ws + plan.w, st),
+                    lay_out<T>(d_a, inner, parties * rank, inner, 1, ws + plan.low, st), {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
+                    plan, many ? nullptr : d_status, st};
+    if (many) f.f = lay_out<T>(d_b, rank, parties * outer, rank, kRanks, ws + plan.f, st);
+    f.shrink(d_h);
+    f.project(d_h, (T*)d_y, ldy);
   });
   return launched();
 }
@@ -527,22 +864,30 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
   Drop none = d;
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
-    float* const g = (float*)(ws + plan.z);
-    hipLaunchKernelGGL(k_group, dim3(1), dim3(group_waves(parties) * kWave), 0, st, d_index, (u32)rows, (u32)parties, (u32*)(ws + plan.begin),
-                       (u32*)(ws + plan.chunk_begin), (u32*)(ws + plan.chunk), (u32*)(ws + plan.list), d_status);
+    const bool many = rows > kFewRows;
+    const size_t step = many ? step_elems<T>() : 1;
+    const size_t ranks = whole_ranks(rank);
+    group(s, d_index, ws, plan, d_status, st);
+    Rows<T> x = {};
+    Rows<T> dy = {};
     if (rows) {
-      T* const b_t = (T*)(ws + plan.b_t);
-      transpose<T>((const T*)d_b, rank, outer * rank, outer, rank, parties, b_t, outer * rank, st);
-      shrink<T>((const T*)d_dy, lddy, b_t, d_scale, d_index, rows, outer, rank, parties, none, (float*)(ws + plan.z_parts), g, nullptr, st);
+      const size_t kp = padded(type, outer);
+      const Sizes back = {rows, outer, inner, parties, rank};
+      x = lay_out<T>(d_x, ldx, rows, inner, 1, ws + plan.x, st);
+      dy = lay_out<T>(d_dy, lddy, rows, outer, step, ws + plan.dy, st);
+      // B^T, W^T and A^T: what is reduced along columns here
+      Product<T> f = {dy, {}, transpose<T>(d_b, rank, outer * rank, outer, rank, parties, ws + plan.low, kp, st), {}, d_scale, d_index, back, none, d,
+                      ws, plan, nullptr, st};
+      f.shrink(nullptr);
+      if (!many) f.join(nullptr);  // k_grad reads it whole
       if (d_dx) {
-        T* const w_t = (T*)(ws + plan.w_t);
-        transpose<T>((const T*)d_w, ldw, 0, outer, inner, 1, w_t, 0, st);
-        const Low low = {rank * inner, 1, inner};
-        project<T>((const T*)d_dy, lddy, w_t, outer, (const T*)d_a, low, g, d_index, rows, outer, inner, parties, rank, d, (T*)d_dx, lddx, st);
+        f.w = transpose<T>(d_w, ldw, 0, outer, inner, 1, ws + plan.w, kp, st);
+        f.f = transpose<T>(d_a, inner, rank * inner, rank, inner, parties, ws + plan.f, ranks, st);
+        f.project(nullptr, (T*)d_dx, lddx);
       }
     }
-    grad<T>((const T*)d_x, ldx, inner, g, s, plan, ws, d, inner, 1, d_da, st);
-    grad<T>((const T*)d_dy, lddy, outer, d_h, s, plan, ws, none, 1, rank, d_db, st);
+    grad<T>(x, inner, (const float*)(ws + plan.z), ranks, s, plan, ws, d, inner, 1, d_da, st);
+    grad<T>(dy, outer, d_h, rank, s, plan, ws, none, 1, rank, d_db, st);
   });
   return launched();
 }

@@ -35,6 +35,10 @@ inline C mfma(const float* a, const float* b, C c, int k) {
   }
   return c;
 }
+template <class C>
+inline C mfma1(float a, float b, C c) {
+  return mfma(&a, &b, c, 1);
+}
 template <class V, class C>
 inline C mfma8(V a, V b, C c) {
   float x[8], y[8];
@@ -48,6 +52,9 @@ inline C mfma8(V a, V b, C c) {
 
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
 #define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
-#define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) hipemu_local::mfma(&(const float&)(a), &(const float&)(b), (c), 1)
+#define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) hipemu_local::mfma1((a), (b), (c))
+// each lane's sixteen bytes to its place behind the wavefront's address; there when the call returns
+#define __builtin_amdgcn_global_load_lds(from, to, size, offset, aux) \
+  memcpy((char*)(void*)(to) + (threadIdx.x % 64) * (size), (const char*)(const void*)(from), (size))
 static inline float __builtin_amdgcn_exp2f(float x) { return exp2f(x); }
 static inline void __builtin_amdgcn_s_setprio(int) {}
