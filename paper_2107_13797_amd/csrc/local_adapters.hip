@@ -225,9 +225,39 @@ struct LowPart<float> {
   }
 };
 
-// Sixteen bytes a lane from memory to LDS, lane l's to `to` + 16 l.
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// Where the rows of a tile are loaded from, sixteen bytes a lane straight into LDS, lane l's to `to` + 16 l. Matrices below
+// 4 GiB are read as buffers, whose offsets are 32-bit words and whose loads the compiler counts one by one; FAR ones are not.
+template <class T, bool FAR>
+struct Source;
+template <class T>
+struct Source<T, false> {
+  using At = u32;
+  __amdgpu_buffer_rsrc_t buffer;
+  __device__ __forceinline__ Source(const T* p, u32 bytes) : buffer(__builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000)) {}
+  static __device__ __forceinline__ At at(u32 row, size_t ld, u32 k) { return (row * (u32)ld + k) * (u32)sizeof(T); }
+  __device__ __forceinline__ void load(At at, u32 k, void* to) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void*)to, 16, (int)at, (int)(k * (u32)sizeof(T)), 0, 0);
+  }
+};
+template <class T>
+struct Source<T, true> {
+  using At = size_t;
+  const T* p;
+  __device__ __forceinline__ Source(const T* p_, u32) : p(p_) {}
+  static __device__ __forceinline__ At at(u32 row, size_t ld, u32 k) { return row * ld + k; }
+  __device__ __forceinline__ void load(At at, u32 k, void* to) const {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + at + k), (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  }
+};
+// Until this wavefront's loads but the latest LATER have arrived and its reads of LDS are done, and all other
+// wavefronts of the block are there too.
+template <int LATER>
+__device__ __forceinline__ void wait_for_tiles() {
+  asm volatile("" ::: "memory");
+  static_assert(LATER < 16, "");
+  __builtin_amdgcn_s_waitcnt(0x70 + LATER);  // vmcnt(LATER) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // A tile's row in LDS is 128 bytes, eight pieces of 16; piece c of row r lies at place c ^ (r / 2) % 8, which spreads the
@@ -251,47 +281,126 @@ __device__ __forceinline__ void drop_four(f32x4& v, const Drop& d, u32 lo, u32 h
   v[3] = (hi >> 16) >= d.threshold ? v[3] * d.scale : 0.0f;
 }
 
-// One step of the reduction: the next step's tiles are asked for, this one's multiplied.
-template <class T, int TM, int TN, int WAVES, int RT, int OT>
-__device__ __forceinline__ void project_step(const T* __restrict__ x, const size_t (&at_x)[TM / 8 / WAVES], const T* __restrict__ w,
-                                             const size_t (&at_w)[TN / 8 / WAVES], u32 k_next, bool more, u32 wave, u32 row0, u32 out0, const T* __restrict__ cx, const T* __restrict__ cw,
-                                             T* __restrict__ nx, T* __restrict__ nw, f32x4 (&acc)[OT][RT]) {
-  constexpr int KE = step_elems<T>();
-  if (more) {
+// The operands that a wavefront multiplies next: its outputs by XN sixteens of its rows.
+template <class T, int OT, int XN>
+struct Frags {
+  Vec8<T> w[OT], x[XN];
+};
+template <class T, int OT, int XN>
+__device__ __forceinline__ void load_w(Frags<T, OT, XN>& f, const T* tile, u32 out0, u32 s) {
 #pragma unroll
-    for (int i = 0; i < TM / 8 / WAVES; ++i) load_to_lds(x + at_x[i] + k_next, nx + (i * WAVES + wave) * 8 * KE);
+  for (int i = 0; i < OT; ++i) f.w[i] = load_frag(tile, out0 + i * 16 + lane_id() % 16, s * 32 + lane_id() / 16 * 8);
+}
+template <class T, int OT, int XN>
+__device__ __forceinline__ void load_x(Frags<T, OT, XN>& f, const T* tile, u32 row0, u32 s, u32 part) {
 #pragma unroll
-    for (int i = 0; i < TN / 8 / WAVES; ++i) load_to_lds(w + at_w[i] + k_next, nw + (i * WAVES + wave) * 8 * KE);
+  for (int j = 0; j < XN; ++j) f.x[j] = load_frag(tile, row0 + (part * XN + j) * 16 + lane_id() % 16, s * 32 + lane_id() / 16 * 8);
+}
+
+// Half (0: the first, 1: the second) of this wavefront's loads of both tiles at `k`, in LDS rows of whole steps.
+template <class T, int TM, int TN, int WAVES, class From>
+__device__ __forceinline__ void ask_tiles(int half, const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
+                                          const typename From::At (&at_w)[TN / 8 / WAVES], u32 k, u32 wave, T* lx, T* lw) {
+  constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
+#pragma unroll
+  for (int i = half * LX / 2; i < (half + 1) * LX / 2; ++i) x.load(at_x[i], k, lx + (i * WAVES + wave) * 8 * step_elems<T>());
+#pragma unroll
+  for (int i = half * LW / 2; i < (half + 1) * LW / 2; ++i) w.load(at_w[i], k, lw + (i * WAVES + wave) * 8 * step_elems<T>());
+}
+
+// One step of the reduction, with the first operands in `f`. Operands are read from LDS under the products before theirs, a
+// read between every few of them. Before the last products the next step's tiles are waited for; the tiles after those are then asked for
+// in place of this step's, one half under the last products and the other under the next step's first, so that the loads
+// neither hold the products up at one place nor are waited for before three quarters of a step are over.
+template <class T, int TM, int TN, int WAVES, class From, int XN, int RT, int OT>
+__device__ __forceinline__ void project_step(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
+                                             const typename From::At (&at_w)[TN / 8 / WAVES], u32 k_next, u32 k_after, u32 wave, u32 row0,
+                                             u32 out0, T* cx, T* cw, T* nx, T* nw,
+                                             Frags<T, OT, XN>& f, f32x4 (&acc)[OT][RT]) {
+  constexpr int KE = step_elems<T>(), kSub = KE / 32, kParts = RT / XN, kAll = kSub * kParts;
+  constexpr int kAsks = (TM + TN) / 8 / WAVES / 2, kReads = sizeof(T) / 2, kProducts = XN * OT * (sizeof(T) == 2 ? 1 : 8);
+#pragma unroll
+  for (int q = 0; q < kAll; ++q) {
+    const int s = q / kParts, part = q % kParts;
+    const bool last = q + 1 == kAll, new_w = last || (q + 1) / kParts != s;
+    Frags<T, OT, XN> next;
+    if (q == 0 && kAll > 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k_next, wave, nx, nw);
+    if (last) {
+      wait_for_tiles<0>();
+      ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k_after, wave, cx, cw);
+      if (kAll == 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k_after, wave, cx, cw);
+    }
+    load_x(next, last ? nx : cx, row0, last ? 0 : (q + 1) / kParts, last ? 0 : (q + 1) % kParts);
+    if (new_w) {
+      load_w(next, last ? nw : cw, out0, last ? 0 : s + 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < OT; ++i) next.w[i] = f.w[i];
+    }
+#pragma unroll
+    for (int j = 0; j < XN; ++j)
+#pragma unroll
+      for (int i = 0; i < OT; ++i) acc[i][part * XN + j] = mma32(f.w[i], f.x[j], acc[i][part * XN + j]);
+    // a load, where there are any, and one or more reads of LDS with products between them
+    constexpr int kSlots = kAsks < 4 ? kAsks : 4;
+#pragma unroll
+    for (int n = 0; n < kSlots; ++n) {
+      if (last || q == 0) __builtin_amdgcn_sched_group_barrier(0x010, kAsks / kSlots, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kProducts / kSlots / 4, 0);
+      if (new_w) __builtin_amdgcn_sched_group_barrier(0x100, (XN + OT) * kReads / kSlots, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x100, XN * kReads / kSlots, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kProducts / kSlots / 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    f = next;
   }
-  const u32 lane = lane_id();
-#pragma unroll
-  for (int s = 0; s < KE / 32; ++s) {
-    Vec8<T> xv[RT], wv[OT];
-    const u32 k = s * 32 + lane / 16 * 8;
-#pragma unroll
-    for (int i = 0; i < OT; ++i) wv[i] = load_frag(cw, out0 + i * 16 + lane % 16, k);
-#pragma unroll
-    for (int j = 0; j < RT; ++j) xv[j] = load_frag(cx, row0 + j * 16 + lane % 16, k);
-#pragma unroll
-    for (int j = 0; j < RT; ++j)
-#pragma unroll
-      for (int i = 0; i < OT; ++i) acc[i][j] = mma32(wv[i], xv[j], acc[i][j]);
+}
+
+// The whole reduction of a tile. That the four tiles in LDS are told apart here, and only here, is what lets the compiler see which reads
+// need not wait for the loads on their way.
+template <class T, int TM, int TN, int WAVES, class From, int RT, int OT>
+__device__ __forceinline__ void reduce(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
+                                       const typename From::At (&at_w)[TN / 8 / WAVES], u32 steps, u32 wave, u32 row0, u32 out0,
+                                       T* __restrict__ lx0, T* __restrict__ lw0, T* __restrict__ lx1, T* __restrict__ lw1, f32x4 (&acc)[OT][RT]) {
+  constexpr int KE = step_elems<T>(), XN = RT < 4 ? RT : 4;
+  const u32 inner = steps * KE;
+  const auto after = [&](u32 at) { return at + KE < inner ? at + KE : 0; };
+  u32 k = after(0);
+  ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, 0, wave, lx0, lw0);
+  ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, 0, wave, lx0, lw0);
+  ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k, wave, lx1, lw1);
+  if (KE / 32 * (RT / XN) == 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k, wave, lx1, lw1);
+  Frags<T, OT, XN> frags;
+  wait_for_tiles<(TM + TN) / 8 / WAVES / 2>();
+  load_x(frags, lx0, row0, 0, 0);
+  load_w(frags, lw0, out0, 0);
+  // the loads go round past the last step, rather than that the loop has other forms for its end
+  for (u32 i = 0;; i += 2) {
+    const u32 k2 = after(k), k3 = after(k2);
+    project_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, k2, wave, row0, out0, lx0, lw0, lx1, lw1, frags, acc);
+    if (i + 1 >= steps) break;
+    project_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k2, k3, wave, row0, out0, lx1, lw1, lx0, lw0, frags, acc);
+    if (i + 2 >= steps) break;
+    k = k3;
   }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): none of them arrives after the block's end
 }
 
 // y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k], inner a multiple of a step. A block takes TM rows (of
 // `order`) by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
 // is filled while the other is read.
-template <class T, int TM, int TN, int WM, int WN, bool DROP>
+template <class T, int TM, int TN, int WM, int WN, bool DROP, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
                                                              const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
-                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, bool wide_y) {
+                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, bool wide_y,
+                                                             u32 x_bytes, u32 w_bytes) {
   constexpr int KE = step_elems<T>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
   constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
-  __shared__ __align__(16) T lx0[TM * KE];
-  __shared__ __align__(16) T lw0[TN * KE];
-  __shared__ __align__(16) T lx1[TM * KE];
-  __shared__ __align__(16) T lw1[TN * KE];
+  __shared__ __align__(16) T lds[2 * (TM + TN) * KE];
+  T* const lx0 = lds;
+  T* const lw0 = lx0 + TM * KE;
+  T* const lx1 = lw0 + TN * KE;
+  T* const lw1 = lx1 + TM * KE;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   // Blocks are dealt to the eight dies in turn: each gets neighbouring tiles, four tiles of rows by all outputs at a time,
   // whose operands its cache holds.
@@ -302,22 +411,19 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   const u32 t0 = (band * 4 + in_band % high) * TM, o0 = in_band / high * TN;
   const u32 row0 = wave / WN * (TM / WM), out0 = wave % WN * (TN / WN);  // this wavefront's corner
 
-  size_t at_x[LX], at_w[LW];  // of this lane's pieces
+  using From = Source<T, FAR>;
+  const From from_x(x, x_bytes), from_w(w, w_bytes);
+  typename From::At at_x[LX], at_w[LW];  // this lane's pieces
 #pragma unroll
   for (int i = 0; i < LX; ++i) {
     const u32 r = (i * WAVES + wave) * 8 + lane / 8, at = t0 + r < rows ? t0 + r : rows - 1;
-    at_x[i] = (size_t)order[at] * ldx + place_of(r, lane % 8) * (16 / sizeof(T));
+    at_x[i] = From::at(order[at], ldx, place_of(r, lane % 8) * (16 / sizeof(T)));
   }
 #pragma unroll
   for (int i = 0; i < LW; ++i) {
     const u32 r = (i * WAVES + wave) * 8 + lane / 8, o = o0 + r < outer ? o0 + r : outer - 1;
-    at_w[i] = (size_t)o * ldw + place_of(r, lane % 8) * (16 / sizeof(T));
+    at_w[i] = From::at(o, ldw, place_of(r, lane % 8) * (16 / sizeof(T)));
   }
-#pragma unroll
-  for (int i = 0; i < LX; ++i) load_to_lds(x + at_x[i], lx0 + (i * WAVES + wave) * 8 * KE);
-#pragma unroll
-  for (int i = 0; i < LW; ++i) load_to_lds(w + at_w[i], lw0 + (i * WAVES + wave) * 8 * KE);
-
   f32x4 acc[OT][RT];
   u32 t[RT];  // this lane's rows, `rows`: none
 #pragma unroll
@@ -328,13 +434,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
     for (int i = 0; i < OT; ++i) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  for (u32 k = 0; k < inner; k += 2 * KE) {
-    __syncthreads();
-    project_step<T, TM, TN, WAVES, RT, OT>(x, at_x, w, at_w, k + KE, k + KE < inner, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
-    __syncthreads();
-    if (k + KE < inner)
-      project_step<T, TM, TN, WAVES, RT, OT>(x, at_x, w, at_w, k + 2 * KE, k + 2 * KE < inner, wave, row0, out0, lx1, lw1, lx0, lw0, acc);
-  }
+  reduce<T, TM, TN, WAVES>(from_x, at_x, from_w, at_w, inner / KE, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
+
   // the adapters' part, party by party along the list
   using Low = LowPart<T>;
   const u32 wave_at = t0 + row0, listed = begin[parties], wave_end = wave_at + TM / WM < rows ? wave_at + TM / WM : rows;
@@ -350,14 +451,14 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 #pragma unroll
       for (int i = 0; i < OT; ++i) low0[i] = low1[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       for (u32 r0 = 0; r0 < ranks; r0 += Low::kStep) {
-        const typename Low::Frag z0 = Low::of_z(z + (size_t)(t[j] < rows ? t[j] : 0) * ranks + r0);
-        const typename Low::Frag z1 = Low::of_z(z + (size_t)(t[j + 1] < rows ? t[j + 1] : 0) * ranks + r0);
+        const typename Low::Frag v0 = Low::of_z(z + (size_t)(t[j] < rows ? t[j] : 0) * ranks + r0);
+        const typename Low::Frag v1 = Low::of_z(z + (size_t)(t[j + 1] < rows ? t[j + 1] : 0) * ranks + r0);
 #pragma unroll
         for (int i = 0; i < OT; ++i) {
           const u32 o = o0 + out0 + i * 16 + lane % 16;
           const typename Low::Frag fv = Low::of_f(f + ((size_t)who * outer + (o < outer ? o : outer - 1)) * ranks + r0);
-          low0[i] = Low::mma(fv, z0, low0[i]);
-          low1[i] = Low::mma(fv, z1, low1[i]);
+          low0[i] = Low::mma(fv, v0, low0[i]);
+          low1[i] = Low::mma(fv, v1, low1[i]);
         }
       }
 #pragma unroll
@@ -380,10 +481,42 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
           acc[i][j + 1][e] += mine1 ? low1[i][e] : 0.0f;
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // one pair of rows at a time: the sums hold half of the registers
     }
     at = next;
   }
 
+  // A lane holds four outputs of each of its rows: results of 16 bits go through the tiles' place in LDS, a wavefront's through its
+  // own part of it, and leave in 16-byte pieces, a whole line or half a line of a row at a time.
+  constexpr u32 kPieces = OT * 16 * sizeof(T) / 16, kShift = kPieces == 8 ? 1 : 2;
+  if (sizeof(T) == 2 && wide_y) {
+    __syncthreads();  // other wavefronts have read the last tiles
+    T* const own = lds + wave * (RT * 16 * OT * 16);
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int i = 0; i < OT; ++i) {
+        T v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (T)acc[i][j][e];
+        const u32 r = j * 16 + lane % 16, piece = i * 2 + lane / 32;
+        __builtin_memcpy(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8 + (lane / 16 & 1) * 4, v, sizeof(v));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    __builtin_amdgcn_wave_barrier();
+    constexpr u32 kRows = kWave / kPieces;  // of one store
+#pragma unroll
+    for (u32 n = 0; n < RT * 16 / kRows; ++n) {
+      const u32 r = n * kRows + lane / kPieces, piece = lane % kPieces;
+      const Vec8<T> v = load_wide(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8);
+      const u32 row = lane_read(t[n * kRows / 16], (int)(r % 16)), o = o0 + out0 + piece * 8;
+      if (row >= rows || o >= outer) continue;
+      T* const to = y + (size_t)row * ldy + o;
+      if (o + 8 <= outer) store_wide(to, v);
+      else store_some(to, v, (int)(outer - o));
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < RT; ++j) {
     if (t[j] >= rows) continue;
@@ -394,8 +527,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
       T v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = (T)acc[i][j][e];
-      if (wide_y && o + 4 <= outer) {
-        __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(T)), v, sizeof(v));
+      if (sizeof(T) == 4 && wide_y && o + 4 <= outer) {
+        __builtin_memcpy(__builtin_assume_aligned(to, 16), v, sizeof(v));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -773,16 +906,20 @@ struct Product {
 #undef HAFLO_LOCAL_RUN
       return;
     }
-    const bool wide_y = (uintptr_t)y % (4 * sizeof(T)) == 0 && ldy % 4 == 0;
-#define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP)                                                                                             \
-  hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP>), dim3((unsigned)(ceil_div(s.rows, TM) * ceil_div(s.outer, TN))),                \
+    const bool wide_y = wide_rows<T>(y, ldy);
+    const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
+    const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
+#define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP, FAR)                                                                                        \
+  hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP, FAR>), dim3((unsigned)(ceil_div(s.rows, TM) * ceil_div(s.outer, TN))),           \
                      dim3(WM * WN * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (const float*)z(), index, order(),                          \
-                     (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(), after, y, ldy, wide_y)
-#define HAFLO_LOCAL_TILE(DROP)                                                                                \
-  do {                                                                                                        \
-    if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP);         \
-    else if (ceil_div(s.rows, 128) * ceil_div(s.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, DROP);    \
-    else HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP);                                                                 \
+                     (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(), after, y, ldy, \
+                     wide_y, (u32)x_bytes, (u32)w_bytes)
+#define HAFLO_LOCAL_TILE(DROP)                                                                                    \
+  do {                                                                                                            \
+    if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, true);                                                         \
+    else if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, false); \
+    else if (ceil_div(s.rows, 128) * ceil_div(s.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, DROP, false); \
+    else HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP, false);                                                              \
   } while (0)
     if (after.threshold) HAFLO_LOCAL_TILE(true);
     else HAFLO_LOCAL_TILE(false);

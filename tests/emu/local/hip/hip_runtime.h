@@ -56,5 +56,22 @@ inline C mfma8(V a, V b, C c) {
 // each lane's sixteen bytes to its place behind the wavefront's address; there when the call returns
 #define __builtin_amdgcn_global_load_lds(from, to, size, offset, aux) \
   memcpy((char*)(void*)(to) + (threadIdx.x % 64) * (size), (const char*)(const void*)(from), (size))
+struct hipemu_buffer {
+  const char* p;
+  uint32_t bytes;
+};
+#define __amdgpu_buffer_rsrc_t hipemu_buffer
+#define __builtin_amdgcn_make_buffer_rsrc(p, stride, bytes, flags) (hipemu_buffer{(const char*)(p), (uint32_t)(bytes)})
+// past the buffer's end a load gives zeros
+static inline void hipemu_buffer_to_lds(hipemu_buffer b, void* to, uint32_t size, uint32_t at) {
+  char* const mine = (char*)to + threadIdx.x % 64 * size;
+  if ((uint64_t)at + size <= b.bytes) memcpy(mine, b.p + at, size);
+  else memset(mine, 0, size);
+}
+#define __builtin_amdgcn_raw_ptr_buffer_load_lds(b, to, size, at, more, offset, aux) \
+  hipemu_buffer_to_lds((b), (void*)(to), (size), (uint32_t)(at) + (uint32_t)(more))
 static inline float __builtin_amdgcn_exp2f(float x) { return exp2f(x); }
 static inline void __builtin_amdgcn_s_setprio(int) {}
+static inline void __builtin_amdgcn_s_waitcnt(int) {}
+static inline void __builtin_amdgcn_wave_barrier() { hipemu::ballot(true); }
+static inline void __builtin_amdgcn_s_barrier() { hipemu::barrier(); }
