@@ -17,6 +17,7 @@ using namespace haflo::local;
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kShrinkWaves = 8;
 
 template <class T>
 constexpr int step_elems() {  // of the reduction in one step of k_project: 128 bytes of a row
@@ -44,13 +45,13 @@ __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u
 }
 
 // z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without. A block takes ROWS rows (of `order`, or one
-// row as it lies) and one part of the reduction, its wavefronts a quarter of that each; once for every party among the rows.
+// row as it lies) and one part of the reduction, its wavefronts an eighth of that each; once for every party among the rows.
 template <class T, int ROWS, int RT>
-__global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
+__global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
                                                      const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
                                                      u32 z_ld, float* z, float* h, u32* status) {
   constexpr int kAhead = RT == 1 ? 4 : 2;  // steps whose operands are on their way together
-  __shared__ float sum[kThreads / kWave][RT][16][17];
+  __shared__ float sum[kShrinkWaves][RT][16][17];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   const u32 at0 = blockIdx.x / parts * ROWS, part = blockIdx.x % parts;
   const auto row_at = [&](u32 i) { return at0 + i >= rows ? rows : order ? order[at0 + i] : at0 + i; };
@@ -59,12 +60,12 @@ __global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, con
   const int a = (u32)raw < parties ? raw : -1;
   if (status && part == 0 && threadIdx.x < 16 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
   // this wavefront's share of the reduction, in steps of 32
-  const u32 steps = (inner + 31) / 32, units = parts * (kThreads / kWave), unit = part * (kThreads / kWave) + wave;
+  const u32 steps = (inner + 31) / 32, units = parts * kShrinkWaves, unit = part * kShrinkWaves + wave;
   const u32 first = (u32)((u64)steps * unit / units), end = (u32)((u64)steps * (unit + 1) / units);
   float own[RT];  // of row out_i, r = lane % 16
 #pragma unroll
   for (int i = 0; i < RT; ++i) own[i] = 0.0f;
-  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave;
+  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave % 4;
   const u32 out_t = row_at(out_i);
   const int out_a = out_t < rows ? party_of(index, out_t, parties) : -1;
   u64 left = __builtin_amdgcn_ballot_w64(a >= 0) & 0xFFFF;
@@ -100,12 +101,15 @@ __global__ __launch_bounds__(kThreads) void k_shrink(const T* x, size_t ldx, con
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         const u32 r = lane % 16;
-        own[i] = (sum[0][i][out_i][r] + sum[1][i][out_i][r]) + (sum[2][i][out_i][r] + sum[3][i][out_i][r]);
+        float s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < kShrinkWaves; ++v) s += sum[v][i][out_i][r];
+        own[i] = s;
       }
     }
     __syncthreads();
   }
-  if (out_t < rows && (ROWS != 1 || threadIdx.x < 16)) {
+  if (out_t < rows && (ROWS == 1 ? threadIdx.x < 16 : wave < 4)) {
     const float by = out_a < 0 ? 0.0f : scale[out_a] * (d.threshold ? d.scale : 1.0f);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -126,36 +130,6 @@ __global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, s
   if (z) z[i] = s;
   const u32 r = (u32)(i % z_ld);
   if (h && r < rank) h[i / z_ld * rank + r] = s;
-}
-
-// Rows of `cols` elements to rows of `out_ld`, a multiple of eight, with zeros behind them.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_pad(const T* in, size_t ld, u32 rows, u32 cols, T* out, u32 out_ld) {
-  const u32 groups = out_ld / 8;
-  const u64 at = (u64)blockIdx.x * kThreads + threadIdx.x;
-  if (at >= (u64)rows * groups) return;
-  const u32 r = (u32)(at / groups), c = (u32)(at - (u64)r * groups) * 8;
-  store_wide(out + (size_t)r * out_ld + c, load_some(in + (size_t)r * ld + c, c >= cols ? 0 : (int)(cols - c)));
-}
-
-// out[c, r] = in[r, c], rows of out out_ld apart with zeros behind them; matrices one behind the other
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_transpose(const T* in, size_t ld, size_t in_step, u32 rows, u32 cols, T* out, u32 out_ld,
-                                                        size_t out_step) {
-  __shared__ T tile[64][66];
-  const u32 tiles_c = (cols + 63) / 64, tiles = tiles_c * ((out_ld + 63) / 64);
-  const u32 which = blockIdx.x / tiles, at = blockIdx.x % tiles, r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
-  in += which * in_step;
-  out += which * out_step;
-  for (u32 i = threadIdx.x; i < 64 * 64; i += kThreads) {
-    const u32 r = r0 + i / 64, c = c0 + i % 64;
-    tile[i / 64][i % 64] = r < rows && c < cols ? in[(size_t)r * ld + c] : (T)0.0f;
-  }
-  __syncthreads();
-  for (u32 i = threadIdx.x; i < 64 * 64; i += kThreads) {
-    const u32 c = c0 + i / 64, r = r0 + i % 64;
-    if (r < out_ld && c < cols) out[(size_t)c * out_ld + r] = tile[i % 64][i / 64];
-  }
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -616,37 +590,69 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, s
   }
 }
 
-constexpr u32 kGradRows = 128;  // rows of one chunk of a party's list
+// rows of one chunk of a party's list: as many as leave some 512 blocks of k_grad
+u32 chunk_rows(size_t rows, size_t cols, size_t rank) {
+  const size_t blocks = rows * ceil_div(cols, 128) * ceil_div(rank, 64) / 512;
+  u32 n = 16;
+  while (n < 256 && 2 * n <= blocks) n *= 2;
+  return n;
+}
+// What a call lays out before its products: matrices copied to rows of `out_ld` elements with zeros behind what they hold, or
+// transposed to such rows (`count` of them one behind the other), and the rows grouped by adapter by the first block.
+constexpr int kPrepareThreads = 1024;
 constexpr u32 kGroupCounts = 16384;
-inline u32 group_waves(size_t parties) { return parties < 1024 ? 16 : 3; }  // whose counts fit LDS
+__host__ __device__ inline u32 group_waves(u32 parties) { return parties < 1024 ? 16 : 3; }  // whose counts fit LDS
+template <class T>
+struct Layout {
+  const T* in;
+  T* out;
+  size_t ld, in_step, out_step;
+  u32 rows, cols, out_ld, first, transposed;  // `first`: of its blocks
+};
+struct Group {
+  const int* index;
+  u32 rows, parties, chunk_rows;
+  u32 *begin, *chunk_begin, *chunk, *order, *status;
+};
+constexpr int kLayouts = 5;
+template <class T>
+struct Prepare {
+  Layout<T> job[kLayouts];
+  int jobs;
+  bool grouped;
+  Group group;
+};
 
-// Groups the rows by adapter: `order` holds the rows of party 0 in ascending order, then those of party 1, ..., at last
-// those without; begin[p] is where p's start, begin[parties] where the last begin; chunk_begin[p] the first of p's chunks of
-// kGradRows rows; chunk[c] = p. One block; its wavefronts take a range of rows each, count them, and list them from where their
-// counts say.
-__global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 parties, u32* begin, u32* chunk_begin, u32* chunk, u32* order,
-                                                u32* status) {
+// `order` holds the rows of party 0 in ascending order, then those of party 1, ..., at last those without; begin[p] is where
+// p's start, begin[parties] where the last begin; chunk_begin[p] the first of p's chunks of chunk_rows rows; chunk[c] = p.
+// The block's wavefronts take a range of rows each, count them, and list them from where their counts say.
+__device__ void group_rows(const Group& g, u32* counts) {
   constexpr int kAhead = 8;
-  __shared__ u32 counts[kGroupCounts];
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), waves = blockDim.x / kWave;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), waves = group_waves(g.parties);
+  const u32 rows = g.rows, parties = g.parties;
+  const int* const index = g.index;
   const u32 bins = parties + 1;
   const u32 per = ((rows + waves - 1) / waves + kWave - 1) / kWave * kWave;
-  const u32 first = (u64)wave * per < rows ? wave * per : rows, end = rows - first < per ? rows : first + per;
-  for (u32 i = threadIdx.x; i < waves * bins; i += blockDim.x) counts[i] = 0;
+  const u32 first = wave < waves && (u64)wave * per < rows ? wave * per : rows, end = rows - first < per ? rows : first + per;
+  for (u32 i = threadIdx.x; i < waves * bins; i += kPrepareThreads) counts[i] = 0;
   __syncthreads();
+  int raw[kAhead];
+  u32 held = ~0u;  // where the rows that raw holds begin
   for (int pass = 0; pass < 2; ++pass) {
     for (u32 base = first; base < end; base += kAhead * kWave) {
-      int raw[kAhead];
+      if (base != held) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const u32 t = base + i * kWave + lane;
-        raw[i] = t < end ? index[t] : -1;
+        for (int i = 0; i < kAhead; ++i) {
+          const u32 t = base + i * kWave + lane;
+          raw[i] = t < end ? index[t] : -1;
+        }
+        held = base;
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const u32 t = base + i * kWave + lane;
         const u32 a = (u32)raw[i] < parties ? (u32)raw[i] : parties;
-        if (pass == 0 && a == parties && raw[i] != -1 && status) atomicOr(status, HAFLO_ST_RANGE);
+        if (pass == 0 && a == parties && raw[i] != -1 && g.status) atomicOr(g.status, HAFLO_ST_RANGE);
         u64 left = __builtin_amdgcn_ballot_w64(t < end);
         while (left) {
           const int leader = __builtin_ctzll(left);
@@ -656,7 +662,7 @@ __global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 
           u32 at = 0;
           if ((int)lane == leader) at = atomicAdd(&counts[wave * bins + who], (u32)__builtin_popcountll(same));
           at = (u32)__builtin_amdgcn_readlane((int)at, leader);
-          if (pass == 1 && (same >> lane & 1)) order[at + (u32)__builtin_popcountll(same & ((1ull << lane) - 1))] = t;
+          if (pass == 1 && (same >> lane & 1)) g.order[at + (u32)__builtin_popcountll(same & ((1ull << lane) - 1))] = t;
         }
       }
     }
@@ -667,7 +673,7 @@ __global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 
         const u32 p = p0 + lane;
         u32 n = 0;
         for (u32 w = 0; w < waves; ++w) n += p < bins ? counts[w * bins + p] : 0;
-        u32 to = n, c = p < parties ? (n + kGradRows - 1) / kGradRows : 0, c_to = c;
+        u32 to = n, c = p < parties ? (n + g.chunk_rows - 1) / g.chunk_rows : 0, c_to = c;
 #pragma unroll
         for (int s = 1; s < kWave; s <<= 1) {  // sums up to each lane
           const u32 below = lane_read(to, (int)lane - s), c_below = lane_read(c_to, (int)lane - s);
@@ -678,9 +684,9 @@ __global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 
         }
         u32 place = at + to - n;
         if (p < bins) {
-          begin[p] = place;
-          chunk_begin[p] = chunks + c_to - c;
-          for (u32 i = 0; i < c; ++i) chunk[chunks + c_to - c + i] = p;
+          g.begin[p] = place;
+          g.chunk_begin[p] = chunks + c_to - c;
+          for (u32 i = 0; i < c; ++i) g.chunk[chunks + c_to - c + i] = p;
           for (u32 w = 0; w < waves; ++w) {
             const u32 m = counts[w * bins + p];
             counts[w * bins + p] = place;
@@ -695,74 +701,177 @@ __global__ __launch_bounds__(1024) void k_group(const int* index, u32 rows, u32 
   }
 }
 
-// out[chunk][r][col] = sum over the chunk's rows t of z[t, r] drop(m[t, col]): a block takes 512 columns and sixteen r,
-// its wavefronts a quarter of the rows each, a lane eight columns.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_grad(const T* m, size_t ld, u32 cols, const float* z, u32 z_ld, u32 rank, u32 parties, const u32* begin,
-                                                   const u32* chunk_begin, const u32* chunk, const u32* list, Drop d, float* out) {
-  constexpr int kR = 16;
-  __shared__ float sum[kR / 2][kWave * 8];
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 tiles_c = (cols + 511) / 512, tiles_r = (rank + kR - 1) / kR;
-  const u32 c = blockIdx.x / (tiles_c * tiles_r), at = blockIdx.x % (tiles_c * tiles_r);
-  if (c >= chunk_begin[parties]) return;
-  const u32 col = at / tiles_r * 512 + lane * 8, r0 = at % tiles_r * kR;
-  const u32 p = chunk[c], first = begin[p] + (c - chunk_begin[p]) * kGradRows;
-  const u32 end = first + kGradRows < begin[p + 1] ? first + kGradRows : begin[p + 1];
-  float acc[kR][8];
-#pragma unroll
-  for (int r = 0; r < kR; ++r)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[r][j] = 0.0f;
-  for (u32 i = first + wave; i < end; i += kThreads / kWave) {
-    const u32 t = (u32)__builtin_amdgcn_readfirstlane((int)list[i]);
-    Vec8<T> v = load_tile(m + (size_t)t * ld, ld, 0, 1, col, cols);
-    if (d.threshold) apply_drop(v, d, t, col);
-    float f[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = (float)v.v[j];
-#pragma unroll
-    for (int r = 0; r < kR; ++r) {
-      const float zr = r0 + r < rank ? z[(size_t)t * z_ld + r0 + r] : 0.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[r][j] += zr * f[j];
+__global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p) {
+  __shared__ __align__(16) u32 lds[kGroupCounts];
+  u32 block = blockIdx.x;
+  if (p.grouped) {
+    if (block == 0) {
+      group_rows(p.group, lds);
+      return;
     }
+    --block;
   }
-  const float by = d.threshold ? d.scale : 1.0f;
-  // the wavefronts' sums one after the other, in their order, half of the r at a time
-  for (int half = 0; half < 2; ++half) {
-    for (u32 w = 0; w < (u32)(kThreads / kWave); ++w) {
-      if (wave == w) {
-#pragma unroll
-        for (int r = 0; r < kR; ++r)
-          if (r / (kR / 2) == half) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              float* const s = &sum[r % (kR / 2)][lane * 8 + j];
-              *s = w == 0 ? acc[r][j] : *s + acc[r][j];
-            }
-          }
-      }
-      __syncthreads();
-    }
-    for (u32 i = threadIdx.x; i < (u32)(kR / 2) * 512; i += kThreads) {
-      const u32 r = r0 + half * (kR / 2) + i / 512, cc = at / tiles_r * 512 + i % 512;
-      if (r < rank && cc < cols) out[((size_t)c * rank + r) * cols + cc] = sum[i / 512][i % 512] * by;
-    }
-    __syncthreads();
+  int j = 0;
+  while (j + 1 < p.jobs && block >= p.job[j + 1].first) ++j;
+  const Layout<T> job = p.job[j];
+  block -= job.first;
+  if (!job.transposed) {
+    const u32 groups = job.out_ld / 8;
+    const u64 at = (u64)block * kPrepareThreads + threadIdx.x;
+    if (at >= (u64)job.rows * groups) return;
+    const u32 r = (u32)(at / groups), c = (u32)(at - (u64)r * groups) * 8;
+    store_wide(job.out + (size_t)r * job.out_ld + c, load_some(job.in + (size_t)r * job.ld + c, c >= job.cols ? 0 : (int)(job.cols - c)));
+    return;
+  }
+  T(*const tile)[66] = (T(*)[66])lds;
+  const u32 tiles_c = (job.cols + 63) / 64, tiles = tiles_c * ((job.out_ld + 63) / 64);
+  const u32 which = block / tiles, at = block % tiles, r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
+  const T* const in = job.in + which * job.in_step;
+  T* const out = job.out + which * job.out_step;
+  for (u32 i = threadIdx.x; i < 64 * 64; i += kPrepareThreads) {
+    const u32 r = r0 + i / 64, c = c0 + i % 64;
+    tile[i / 64][i % 64] = r < job.rows && c < job.cols ? in[(size_t)r * job.ld + c] : (T)0.0f;
+  }
+  __syncthreads();
+  for (u32 i = threadIdx.x; i < 64 * 64; i += kPrepareThreads) {
+    const u32 c = c0 + i / 64, r = r0 + i % 64;
+    if (r < job.out_ld && c < job.cols) out[(size_t)c * job.out_ld + r] = tile[i % 64][i / 64];
   }
 }
 
-// grad[p] = sum of the party's chunks, in their order; laid out as r_step and col_step say
-__global__ __launch_bounds__(kThreads) void k_grad_join(const float* in, const u32* chunk_begin, u32 rank, u32 cols, size_t r_step,
-                                                        size_t col_step, float* grad) {
-  const size_t n = (size_t)rank * cols;
-  const u32 blocks = (u32)((n + kThreads - 1) / kThreads), p = blockIdx.x / blocks;
-  const size_t i = (size_t)(blockIdx.x % blocks) * kThreads + threadIdx.x;
+// out[chunk][r][col] = sum over the chunk's rows t of z[t, r] drop(m[t, col]) on matrix instructions in 32 bits, whose
+// operands are one element a lane: lane l holds eight columns from 8 (l % 16) on of row l / 16 out of four, and element j of
+// all lanes is one operand, for the columns 8 c + j. A block takes 128 columns and RT sixteens of z, its wavefronts every
+// fourth four rows each. The next rows are on their way while the present ones are multiplied.
+// Both gradients are formed by one launch.
+template <class T>
+struct GradOf {
+  const T* m;
+  size_t ld;
+  const float* z;
+  float *out, *grad;
+  size_t r_step, col_step;  // of the gradient
+  u32 cols, z_ld;
+  Drop d;
+};
+template <class T, int RT>
+__global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32 rank, u32 parties, const u32* __restrict__ begin,
+                                                   const u32* __restrict__ chunk_begin, const u32* __restrict__ chunk,
+                                                   const u32* __restrict__ list, u32 chunk_rows) {
+  constexpr int kAhead = 2, kWaves = kThreads / kWave;
+  __shared__ f32x4 sum[kWaves - 1][RT][8][kWave];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  const u32 tiles_r = (rank + RT * 16 - 1) / (RT * 16), of_a = (a.cols + 127) / 128 * tiles_r, of_b = (b.cols + 127) / 128 * tiles_r;
+  const u32 c = blockIdx.x / (of_a + of_b), both = blockIdx.x % (of_a + of_b), at = both < of_a ? both : both - of_a;
+  if (c >= chunk_begin[parties]) return;
+  const GradOf<T> g = both < of_a ? a : b;
+  const T* __restrict__ const m = g.m;
+  const float* __restrict__ const z = g.z;
+  float* __restrict__ const out = g.out;
+  const size_t ld = g.ld;
+  const u32 cols = g.cols, z_ld = g.z_ld;
+  const Drop d = g.d;
+  const u32 col = at / tiles_r * 128 + lane % 16 * 8, r0 = at % tiles_r * (RT * 16), r = r0 + lane % 16;
+  const u32 p = chunk[c], first = begin[p] + (c - chunk_begin[p]) * chunk_rows;
+  const u32 end = first + chunk_rows < begin[p + 1] ? first + chunk_rows : begin[p + 1];
+  const u32 mine = first + wave * 4 + lane / 16, turns = (end - first + kWaves * 4 - 1) / (kWaves * 4);
+  f32x4 acc[RT][8];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  struct Rows4 {
+    Vec8<T> v;
+    float z[RT];
+    u32 t;
+  } ahead[kAhead];
+  u32 listed[kAhead];  // the rows after those
+  const auto look = [&](u32 n) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const u32 i = mine + (n + u) * (kWaves * 4);
+      listed[u] = i < end ? list[i] : ~0u;
+    }
+  };
+  const auto fetch = [&](u32 n) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ahead[u].t = listed[u];
+    look(n + kAhead);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const bool some = ahead[u].t != ~0u;
+      ahead[u].v = some ? load_tile(m + (size_t)ahead[u].t * ld, ld, 0, 1, col, cols) : Vec8<T>{};
+#pragma unroll
+      for (int i = 0; i < RT; ++i) ahead[u].z[i] = some && r + i * 16 < rank ? z[(size_t)ahead[u].t * z_ld + r + i * 16] : 0.0f;
+    }
+  };
+  look(0);
+  fetch(0);
+  for (u32 n = 0; n < turns; n += kAhead) {
+    Rows4 now[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) now[u] = ahead[u];
+    if (n + kAhead < turns) fetch(n + kAhead);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (d.threshold) apply_drop(now[u].v, d, now[u].t, col);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float f = (float)now[u].v.v[j];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(now[u].z[i], f, acc[i][j], 0, 0, 0);
+      }
+    }
+  }
+  if (wave != 0) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[wave - 1][i][j][lane] = acc[i][j];
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const float by = d.threshold ? d.scale : 1.0f;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < kWaves - 1; ++w) acc[i][j] += sum[w][i][j][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const u32 rr = r0 + i * 16 + lane / 16 * 4 + e;
+      if (rr >= rank || col >= cols) continue;
+      float* const to = out + ((size_t)c * rank + rr) * cols + col;
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = acc[i][j][e] * by;
+      if (col + 8 <= cols) {
+        __builtin_memcpy(to, v, sizeof(v));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j < cols) to[j] = v[j];
+      }
+    }
+  }
+}
+
+// grad[p] = sum of the party's chunks, in their order
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_grad_join(GradOf<T> a, GradOf<T> b, const u32* __restrict__ chunk_begin, u32 rank) {
+  const size_t n_a = (size_t)rank * a.cols, n_b = (size_t)rank * b.cols;
+  const u32 of_a = (u32)((n_a + kThreads - 1) / kThreads), of_b = (u32)((n_b + kThreads - 1) / kThreads);
+  const u32 p = blockIdx.x / (of_a + of_b), both = blockIdx.x % (of_a + of_b);
+  const GradOf<T> g = both < of_a ? a : b;
+  const size_t n = both < of_a ? n_a : n_b, i = (size_t)(both < of_a ? both : both - of_a) * kThreads + threadIdx.x;
   if (i >= n) return;
+  const u32 end = chunk_begin[p + 1];
   float s = 0.0f;
-  for (u32 c = chunk_begin[p]; c < chunk_begin[p + 1]; ++c) s += in[c * n + i];
-  grad[p * n + i / cols * r_step + i % cols * col_step] = s;
+#pragma unroll 8
+  for (u32 c = chunk_begin[p]; c < end; ++c) s += g.out[c * n + i];
+  g.grad[p * n + i / g.cols * g.r_step + i % g.cols * g.col_step] = s;
 }
 
 struct Sizes {
@@ -782,8 +891,9 @@ u32 shrink_parts(size_t rows, size_t k) {
 }
 size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * (128 / type_size(type)); }
 size_t whole_ranks(size_t rank) { return ceil_div(rank, kRanks) * kRanks; }
+u32 grad_rows(const Sizes& s) { return chunk_rows(s.rows, s.inner + s.outer, s.rank); }
 struct Plan {
-  size_t z_parts, z, x, dy, w, low, f, begin, chunk_begin, chunk, order, sums, total;
+  size_t z_parts, z, x, dy, w, low, f, begin, chunk_begin, chunk, order, sums_a, sums_b, total;
   size_t chunks;  // at most
 };
 Plan adapter_plan(int type, bool backward, const Sizes& s) {
@@ -802,41 +912,56 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
   p.w = take(n * kp * e);
   p.low = take(s.parties * s.rank * kp * e);
   p.f = take(s.parties * n * ranks * e);
-  p.chunks = s.rows / kGradRows + s.parties;
+  p.chunks = s.rows / grad_rows(s) + s.parties;
   p.begin = take((s.parties + 1) * 4);
   p.chunk_begin = take((s.parties + 1) * 4);
   p.chunk = take(p.chunks * 4);
   p.order = take(s.rows * 4);
   if (backward) {
     p.dy = take(s.rows * kp * e);
-    p.sums = take(p.chunks * s.rank * (s.inner > s.outer ? s.inner : s.outer) * 4);
+    p.sums_a = take(p.chunks * s.rank * s.inner * 4);
+    p.sums_b = take(p.chunks * s.rank * s.outer * 4);
   }
   p.total = b;
   return p;
 }
 
-// A matrix with rows at 16-byte boundaries and of a multiple of `step` elements, zeros behind what they hold: itself, or its
-// copy at `room`.
 template <class T>
 struct Rows {
   const T* p;
   size_t ld;
 };
+// Collects what is to be laid out, and launches it.
 template <class T>
-Rows<T> lay_out(const void* m, size_t ld, size_t rows, size_t cols, size_t step, char* room, hipStream_t st) {
-  if (wide_rows<T>(m, ld) && cols % step == 0) return {(const T*)m, ld};
-  const size_t to = ceil_div(cols, step < 8 ? 8 : step) * (step < 8 ? 8 : step);
-  hipLaunchKernelGGL((k_pad<T>), dim3((unsigned)ceil_div(rows * (to / 8), kThreads)), dim3(kThreads), 0, st, (const T*)m, ld, (u32)rows, (u32)cols,
-                     (T*)room, (u32)to);
-  return {(const T*)room, to};
-}
+struct Layouts {
+  Prepare<T> p = {};
+  size_t blocks = 0;
 
+  Rows<T> add(const void* in, char* out, size_t ld, size_t in_step, size_t out_step, size_t rows, size_t cols, size_t out_ld, bool transposed, size_t need) {
+    p.job[p.jobs++] = {(const T*)in, (T*)out, ld, in_step, out_step, (u32)rows, (u32)cols, (u32)out_ld, (u32)blocks, transposed ? 1u : 0u};
+    blocks += need;
+    return {(const T*)out, out_ld};
+  }
+  // A matrix with rows at 16-byte boundaries and of a multiple of `step` elements, zeros behind what they hold: itself, or its
+  // copy at `room`.
+  Rows<T> wide(const void* m, size_t ld, size_t rows, size_t cols, size_t step, char* room) {
+    if (wide_rows<T>(m, ld) && cols % step == 0) return {(const T*)m, ld};
+    const size_t to = ceil_div(cols, step < 8 ? 8 : step) * (step < 8 ? 8 : step);
+    return add(m, room, ld, 0, 0, rows, cols, to, false, ceil_div(rows * (to / 8), kPrepareThreads));
+  }
+  Rows<T> transposed(const void* in, size_t ld, size_t in_step, size_t rows, size_t cols, size_t count, char* room, size_t out_ld) {
+    return add(in, room, ld, in_step, cols * out_ld, rows, cols, out_ld, true, ceil_div(out_ld, 64) * ceil_div(cols, 64) * count);
+  }
+  void launch(hipStream_t st) {
+    blocks += p.grouped ? 1 : 0;
+    if (blocks) hipLaunchKernelGGL((k_prepare<T>), dim3((unsigned)blocks), dim3(kPrepareThreads), 0, st, p);
+  }
+};
 template <class T>
-Rows<T> transpose(const void* in, size_t ld, size_t in_step, size_t rows, size_t cols, size_t count, char* out, size_t out_ld, hipStream_t st) {
-  const size_t tiles = ceil_div(out_ld, 64) * ceil_div(cols, 64);
-  hipLaunchKernelGGL((k_transpose<T>), dim3((unsigned)(tiles * count)), dim3(kThreads), 0, st, (const T*)in, ld, in_step, (u32)rows, (u32)cols,
-                     (T*)out, (u32)out_ld, cols * out_ld);
-  return {(const T*)out, out_ld};
+void add_group(Prepare<T>& to, const Sizes& s, const int* index, char* ws, const Plan& p, u32* status) {
+  to.grouped = true;
+  to.group = {index, (u32)s.rows, (u32)s.parties, grad_rows(s), (u32*)(ws + p.begin), (u32*)(ws + p.chunk_begin), (u32*)(ws + p.chunk),
+          (u32*)(ws + p.order), status};
 }
 
 // What both directions do: z from x and the low-rank rows `low`, then x against `w` with `f` (outer x rank of every party).
@@ -862,7 +987,7 @@ struct Product {
   // z, or with few rows its parts; dense as `h` too unless that is null
   void shrink(float* h) const {
     const u32 parts = shrink_parts(s.rows, s.inner);
-    const dim3 grid((unsigned)((few() ? s.rows : ceil_div(s.rows, 16)) * parts)), block(kThreads);
+    const dim3 grid((unsigned)((few() ? s.rows : ceil_div(s.rows, 16)) * parts)), block(kShrinkWaves * kWave);
     float* const to = few() || parts > 1 ? z_parts() : z();
     float* const h_now = parts > 1 ? nullptr : h;
 #define HAFLO_LOCAL_RUN(ROWS, RT)                                                                                                            \
@@ -928,22 +1053,20 @@ struct Product {
   }
 };
 
-void group(const Sizes& s, const int* index, char* ws, const Plan& p, u32* status, hipStream_t st) {
-  hipLaunchKernelGGL(k_group, dim3(1), dim3(group_waves(s.parties) * kWave), 0, st, index, (u32)s.rows, (u32)s.parties, (u32*)(ws + p.begin),
-                     (u32*)(ws + p.chunk_begin), (u32*)(ws + p.chunk), (u32*)(ws + p.order), status);
-}
-
 template <class T>
-void grad(const Rows<T>& m, size_t cols, const float* z, size_t z_ld, const Sizes& s, const Plan& p, char* ws, const Drop& d, size_t r_step,
-          size_t col_step, float* out, hipStream_t st) {
+void grads(const GradOf<T>& a, const GradOf<T>& b, const Sizes& s, const Plan& p, char* ws, hipStream_t st) {
   const dim3 block(kThreads);
   const u32* chunk_begin = (const u32*)(ws + p.chunk_begin);
-  float* const sums = (float*)(ws + p.sums);
-  hipLaunchKernelGGL((k_grad<T>), dim3((unsigned)(p.chunks * ceil_div(cols, 512) * ceil_div(s.rank, 16))), block, 0, st, m.p, m.ld, (u32)cols, z,
-                     (u32)z_ld, (u32)s.rank, (u32)s.parties, (const u32*)(ws + p.begin), chunk_begin, (const u32*)(ws + p.chunk),
-                     (const u32*)(ws + p.order), d, sums);
-  hipLaunchKernelGGL(k_grad_join, dim3((unsigned)(s.parties * ceil_div(s.rank * cols, kThreads))), block, 0, st, (const float*)sums, chunk_begin,
-                     (u32)s.rank, (u32)cols, r_step, col_step, out);
+#define HAFLO_LOCAL_RUN(RT)                                                                                                             \
+  hipLaunchKernelGGL((k_grad<T, RT>), dim3((unsigned)(p.chunks * (ceil_div(a.cols, 128) + ceil_div(b.cols, 128)) * ceil_div(s.rank, RT * 16))), \
+                     block, 0, st, a, b, (u32)s.rank, (u32)s.parties, (const u32*)(ws + p.begin), chunk_begin,                          \
+                     (const u32*)(ws + p.chunk), (const u32*)(ws + p.order), grad_rows(s))
+  if (s.rank <= 16) HAFLO_LOCAL_RUN(1);
+  else if (s.rank <= 32) HAFLO_LOCAL_RUN(2);
+  else HAFLO_LOCAL_RUN(4);
+#undef HAFLO_LOCAL_RUN
+  const size_t need = ceil_div(s.rank * a.cols, kThreads) + ceil_div(s.rank * b.cols, kThreads);
+  hipLaunchKernelGGL((k_grad_join<T>), dim3((unsigned)(s.parties * need)), block, 0, st, a, b, chunk_begin, (u32)s.rank);
 }
 
 }  // namespace
@@ -973,11 +1096,13 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
   HAFLO_LOCAL_TYPES(type, {
     const bool many = rows > kFewRows;
     const size_t step = many ? step_elems<T>() : 1;
-    if (many) group(s, d_index, ws, plan, d_status, st);
-    Product<T> f = {lay_out<T>(d_x, ldx, rows, inner, step, ws + plan.x, st), lay_out<T>(d_w, ldw, outer, inner, step, ws + plan.w, st),
-                    lay_out<T>(d_a, inner, parties * rank, inner, 1, ws + plan.low, st), {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
+    Layouts<T> lay;
+    if (many) add_group(lay.p, s, d_index, ws, plan, d_status);
+    Product<T> f = {lay.wide(d_x, ldx, rows, inner, step, ws + plan.x), lay.wide(d_w, ldw, outer, inner, step, ws + plan.w),
+                    lay.wide(d_a, inner, parties * rank, inner, 1, ws + plan.low), {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
                     plan, many ? nullptr : d_status, st};
-    if (many) f.f = lay_out<T>(d_b, rank, parties * outer, rank, kRanks, ws + plan.f, st);
+    if (many) f.f = lay.wide(d_b, rank, parties * outer, rank, kRanks, ws + plan.f);
+    lay.launch(st);
     f.shrink(d_h);
     f.project(d_h, (T*)d_y, ldy);
   });
@@ -1004,27 +1129,32 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
     const bool many = rows > kFewRows;
     const size_t step = many ? step_elems<T>() : 1;
     const size_t ranks = whole_ranks(rank);
-    group(s, d_index, ws, plan, d_status, st);
+    const size_t kp = padded(type, outer);
+    const Sizes back = {rows, outer, inner, parties, rank};
+    Layouts<T> lay;
+    add_group(lay.p, s, d_index, ws, plan, d_status);
     Rows<T> x = {};
     Rows<T> dy = {};
     if (rows) {
-      const size_t kp = padded(type, outer);
-      const Sizes back = {rows, outer, inner, parties, rank};
-      x = lay_out<T>(d_x, ldx, rows, inner, 1, ws + plan.x, st);
-      dy = lay_out<T>(d_dy, lddy, rows, outer, step, ws + plan.dy, st);
+      x = lay.wide(d_x, ldx, rows, inner, 1, ws + plan.x);
+      dy = lay.wide(d_dy, lddy, rows, outer, step, ws + plan.dy);
       // B^T, W^T and A^T: what is reduced along columns here
-      Product<T> f = {dy, {}, transpose<T>(d_b, rank, outer * rank, outer, rank, parties, ws + plan.low, kp, st), {}, d_scale, d_index, back, none, d,
+      Product<T> f = {dy, {}, lay.transposed(d_b, rank, outer * rank, outer, rank, parties, ws + plan.low, kp), {}, d_scale, d_index, back, none, d,
                       ws, plan, nullptr, st};
+      if (d_dx) {
+        f.w = lay.transposed(d_w, ldw, 0, outer, inner, 1, ws + plan.w, kp);
+        f.f = lay.transposed(d_a, inner, rank * inner, rank, inner, parties, ws + plan.f, ranks);
+      }
+      lay.launch(st);
       f.shrink(nullptr);
       if (!many) f.join(nullptr);  // k_grad reads it whole
-      if (d_dx) {
-        f.w = transpose<T>(d_w, ldw, 0, outer, inner, 1, ws + plan.w, kp, st);
-        f.f = transpose<T>(d_a, inner, rank * inner, rank, inner, parties, ws + plan.f, ranks, st);
-        f.project(nullptr, (T*)d_dx, lddx);
-      }
+      if (d_dx) f.project(nullptr, (T*)d_dx, lddx);
+    } else {
+      lay.launch(st);
     }
-    grad<T>(x, inner, (const float*)(ws + plan.z), ranks, s, plan, ws, d, inner, 1, d_da, st);
-    grad<T>(dy, outer, d_h, rank, s, plan, ws, none, 1, rank, d_db, st);
+    const GradOf<T> a = {x.p, x.ld, (const float*)(ws + plan.z), (float*)(ws + plan.sums_a), d_da, inner, 1, (u32)inner, (u32)ranks, d};
+    const GradOf<T> b = {dy.p, dy.ld, d_h, (float*)(ws + plan.sums_b), d_db, 1, rank, (u32)outer, (u32)rank, none};
+    grads<T>(a, b, s, plan, ws, st);
   });
   return launched();
 }
