@@ -327,43 +327,48 @@ def haflo_cipher_sum_segments(ctx, c, offsets, status=None):
 
 
 # The operators of a party's local step (include/haflo_local.h) work on ordinary float32, float16 and bfloat16 tensors and
-# need no Context; their workspaces come from torch's allocator call by call, in the current stream's order.
+# need no Context; their workspaces come from torch's allocator call by call, in the current stream's order. Small calls take
+# as long as the host needs for them, so checks look at each property once.
 _TYPES = {torch.float32: _cabi.TYPE_F32, torch.float16: _cabi.TYPE_F16, torch.bfloat16: _cabi.TYPE_BF16}
 
 
 def _type(t):
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise HafloError("expected float32, float16 or bfloat16, got %s" % t.dtype) from None
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise HafloError("expected float32, float16 or bfloat16, got %s" % t.dtype)
+    return kind
 
 
-def _matrix(t, like=None, rows=None, cols=None):
-    """Distance between the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or (like is not None and t.dtype != like.dtype):
-        raise HafloError("expected a CUDA matrix" + (" of %s" % like.dtype if like is not None else ""))
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise HafloError("expected a matrix of %s x %s, got %s" % (rows, cols, tuple(t.shape)))
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+def _matrix(t, dtype, rows=None, cols=None):
+    """(rows, columns, distance between rows) of a matrix whose rows are contiguous and do not overlap."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype is not dtype:
+        raise HafloError("expected a CUDA matrix of %s" % dtype)
+    r, c = t.shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise HafloError("expected a matrix of %s x %s, got %s x %s" % (rows, cols, r, c))
+    if t.is_contiguous():
+        return r, c, c
+    ld, step = t.stride()
+    if (step != 1 and c > 1) or (ld < c and r > 1):
         raise HafloError("expected rows of contiguous elements that do not overlap")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return r, c, max(ld, c)
 
 
 def _dense(t, dtype, *shape):
     """Address of a contiguous tensor of that type and shape."""
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise HafloError("expected %s of shape %s, got %s of %s" % (dtype, shape, t.dtype, tuple(t.shape)))
     return _ptr(t)
 
 
-def _optional(t, dtype, *shape):
-    return None if t is None else _dense(t, dtype, *shape)
-
-
-def _scratch(nbytes):
+def _scratch(nbytes, like):
+    """Address and owner of `nbytes` of workspace."""
+    if not nbytes:
+        return None, None
     if nbytes == 2 ** 64 - 1:
         raise HafloError("sizes out of range")
-    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+    ws = like.new_empty(nbytes, dtype=torch.uint8)
+    return ws.data_ptr(), ws
 
 
 def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
@@ -372,99 +377,94 @@ def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
     if x.dim() == 1:
         y = haflo_dropout(x[None], p, seed, offset, None if residual is None else residual[None], None if out is None else out[None])
         return y[0] if out is None else out
-    kind, ldx = _type(x), _matrix(x)
-    rows, cols = x.shape
-    ldr = 0 if residual is None else _matrix(residual, x, rows, cols)
+    dtype = x.dtype
+    kind, (rows, cols, ldx) = _type(x), _matrix(x, dtype)
+    pr = ldr = 0
+    if residual is not None:
+        pr, ldr = residual.data_ptr(), _matrix(residual, dtype, rows, cols)[2]
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    _check(lib().haflo_dropout(kind, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, out.data_ptr(),
-                               _matrix(out, x, rows, cols), rows, cols, p, seed, offset, _stream()))
+        out, ldy = x.new_empty((rows, cols)), cols
+    else:
+        ldy = _matrix(out, dtype, rows, cols)[2]
+    _check(lib().haflo_dropout(kind, x.data_ptr(), ldx, pr, ldr, out.data_ptr(), ldy, rows, cols, p, seed, offset, _stream()))
     return out
+
+
+def _adapter_sizes(x, w, a, b, scale, index):
+    dtype = x.dtype
+    kind, (rows, inner, ldx) = _type(x), _matrix(x, dtype)
+    outer, _, ldw = _matrix(w, dtype, None, inner)
+    if a.dim() != 3:
+        raise HafloError("a: parties x rank x inner")
+    parties, rank, _ = a.shape
+    return (kind, rows, inner, outer, parties, rank, ldx, ldw, _dense(a, dtype, parties, rank, inner), _dense(b, dtype, parties, outer, rank),
+            _dense(scale, torch.float32, parties), _dense(index, torch.int32, rows))
 
 
 def haflo_adapter_forward(x, w, a, b, scale, index, p=0.0, seed=0, offset=0, status=None):
     """y = x w^T + h b[index]^T, h = scale[index] drop(x) a[index]^T, row by row: the projection that all parties share with each
     row's own adapter (index int32, -1: none). x [rows, inner], w [outer, inner], a [parties, rank, inner],
     b [parties, outer, rank], scale float32 [parties]. Returns y and, for the backward pass, h (float32 [rows, rank])."""
-    kind, ldx = _type(x), _matrix(x)
-    rows, inner = x.shape
-    if a.dim() != 3:
-        raise HafloError("a: parties x rank x inner")
-    parties, rank = a.shape[0], a.shape[1]
-    ldw = _matrix(w, x, None, inner)
-    outer = w.shape[0]
-    pa, pb = _dense(a, x.dtype, parties, rank, inner), _dense(b, x.dtype, parties, outer, rank)
-    ps, pi = _dense(scale, torch.float32, parties), _dense(index, torch.int32, rows)
-    y = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
-    h = torch.empty((rows, rank), dtype=torch.float32, device=x.device)
+    kind, rows, inner, outer, parties, rank, ldx, ldw, pa, pb, ps, pi = _adapter_sizes(x, w, a, b, scale, index)
+    y, h = x.new_empty((rows, outer)), scale.new_empty((rows, rank))
     nbytes = lib().haflo_adapter_workspace_bytes(kind, 0, rows, inner, outer, parties, rank)
-    ws = _scratch(nbytes)
-    _check(lib().haflo_adapter_forward(kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, rows, inner, outer, parties, rank,
-                                       p, seed, offset, y.data_ptr(), outer, h.data_ptr(), _ptr(status),
-                                       None if ws is None else ws.data_ptr(), nbytes, _stream()))
+    pw, ws = _scratch(nbytes, scale)
+    _check(lib().haflo_adapter_forward(kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, rows, inner, outer, parties, rank, p, seed,
+                                       offset, y.data_ptr(), outer, h.data_ptr(), _ptr(status), pw, nbytes, _stream()))
     return y, h
 
 
 def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offset=0, need_dx=True, status=None):
     """Gradients of haflo_adapter_forward by x (None without need_dx) and, float32 as haflo_encode_f32 takes them, by a and b; for the
     forward call's arguments and its h."""
-    kind, ldx = _type(x), _matrix(x)
-    rows, inner = x.shape
-    if a.dim() != 3:
-        raise HafloError("a: parties x rank x inner")
-    parties, rank = a.shape[0], a.shape[1]
-    ldw = _matrix(w, x, None, inner)
-    outer = w.shape[0]
-    lddy = _matrix(dy, x, rows, outer)
-    pa, pb = _dense(a, x.dtype, parties, rank, inner), _dense(b, x.dtype, parties, outer, rank)
-    ps, pi, ph = _dense(scale, torch.float32, parties), _dense(index, torch.int32, rows), _dense(h, torch.float32, rows, rank)
-    dx = torch.empty((rows, inner), dtype=x.dtype, device=x.device) if need_dx else None
-    da = torch.empty((parties, rank, inner), dtype=torch.float32, device=x.device)
-    db = torch.empty((parties, outer, rank), dtype=torch.float32, device=x.device)
+    kind, rows, inner, outer, parties, rank, ldx, ldw, pa, pb, ps, pi = _adapter_sizes(x, w, a, b, scale, index)
+    lddy, ph = _matrix(dy, x.dtype, rows, outer)[2], _dense(h, torch.float32, rows, rank)
+    dx = x.new_empty((rows, inner)) if need_dx else None
+    da, db = scale.new_empty((parties, rank, inner)), scale.new_empty((parties, outer, rank))
     nbytes = lib().haflo_adapter_workspace_bytes(kind, 1, rows, inner, outer, parties, rank)
-    ws = _scratch(nbytes)
-    _check(lib().haflo_adapter_backward(kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, ph, rows,
-                                        inner, outer, parties, rank, p, seed, offset, dx.data_ptr() if need_dx else None, inner,
-                                        da.data_ptr(), db.data_ptr(), _ptr(status), ws.data_ptr(), nbytes, _stream()))
+    pw, ws = _scratch(nbytes, scale)
+    _check(lib().haflo_adapter_backward(kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, ph, rows, inner, outer,
+                                        parties, rank, p, seed, offset, dx.data_ptr() if need_dx else None, inner, da.data_ptr(),
+                                        db.data_ptr(), _ptr(status), pw, nbytes, _stream()))
     return dx, da, db
 
 
 def haflo_label_logprobs(logits, label, top=0, status=None):
     """Row by row under softmax(logits): the label's log-probability (int32 label, -1: none, gives 0), the entropy, the logarithm of the
     exponentials' sum, and the `top` greatest logits' log-probabilities and columns (None for top = 0), ties to the lowest."""
-    kind, ld = _type(logits), _matrix(logits)
-    rows, cols = logits.shape
-    pl = _dense(label, torch.int32, rows)
-    logp, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=logits.device).unbind()
-    top_logp = top_index = None
+    kind, (rows, cols, ld) = _type(logits), _matrix(logits, logits.dtype)
+    pl, f32 = _dense(label, torch.int32, rows), torch.float32
     nbytes = lib().haflo_label_workspace_bytes(kind, rows, cols, top)
-    ws = _scratch(nbytes)
+    pw, ws = _scratch(nbytes, logits)
+    sums = logits.new_empty((3, rows), dtype=f32)
+    at = sums.data_ptr()
+    top_logp = top_index = None
     if top:
-        top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
-        top_index = torch.empty((rows, top), dtype=torch.int32, device=logits.device)
-    _check(lib().haflo_label_logprobs(kind, logits.data_ptr(), ld, pl, rows, cols, top, logp.data_ptr(), entropy.data_ptr(),
-                                      lse.data_ptr(), _ptr(top_logp), _ptr(top_index), _ptr(status),
-                                      None if ws is None else ws.data_ptr(), nbytes, _stream()))
+        top_logp, top_index = logits.new_empty((rows, top), dtype=f32), logits.new_empty((rows, top), dtype=torch.int32)
+    _check(lib().haflo_label_logprobs(kind, logits.data_ptr(), ld, pl, rows, cols, top, at, at + 4 * rows, at + 8 * rows, _ptr(top_logp),
+                                      _ptr(top_index), _ptr(status), pw, nbytes, _stream()))
+    logp, entropy, lse = sums.unbind()
     return logp, entropy, lse, top_logp, top_index
 
 
 def haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dentropy=None, top_index=None, dtop=None, out=None):
     """Gradient by the logits from the forward call's results and the gradients of its logp, entropy and top_logp. `out` may be
     the logits."""
-    kind, ld = _type(logits), _matrix(logits)
-    rows, cols = logits.shape
-    top = 0 if dtop is None else dtop.shape[-1]
-    f32 = torch.float32
-    args = [_dense(label, torch.int32, rows), _dense(lse, f32, rows), _dense(entropy, f32, rows), _dense(dlogp, f32, rows),
-            _optional(dentropy, f32, rows), None, None]
+    dtype, f32, top, pt, pi = logits.dtype, torch.float32, 0, None, None
+    kind, (rows, cols, ld) = _type(logits), _matrix(logits, dtype)
     if dtop is not None:
-        if top_index is None:
-            raise HafloError("dtop needs top_index")
-        args[5:] = _dense(top_index, torch.int32, rows, top), _dense(dtop, f32, rows, top)
+        if top_index is None or dtop.dim() != 2:
+            raise HafloError("dtop: rows x top, with its top_index")
+        top = dtop.shape[1]
+        pi, pt = _dense(top_index, torch.int32, rows, top), _dense(dtop, f32, rows, top)
     if out is None:
-        out = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
-    _check(lib().haflo_label_logprobs_backward(kind, logits.data_ptr(), ld, *args, rows, cols, top, out.data_ptr(),
-                                               _matrix(out, logits, rows, cols), _stream()))
+        out, lddx = logits.new_empty((rows, cols)), cols
+    else:
+        lddx = _matrix(out, dtype, rows, cols)[2]
+    _check(lib().haflo_label_logprobs_backward(
+        kind, logits.data_ptr(), ld, _dense(label, torch.int32, rows), _dense(lse, f32, rows), _dense(entropy, f32, rows),
+        _dense(dlogp, f32, rows), None if dentropy is None else _dense(dentropy, f32, rows), pi, pt, rows, cols, top, out.data_ptr(), lddx,
+        _stream()))
     return out
 
 

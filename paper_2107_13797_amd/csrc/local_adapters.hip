@@ -17,7 +17,7 @@ using namespace haflo::local;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kShrinkWaves = 8;
+constexpr int kShrinkWaves = 4;
 
 template <class T>
 constexpr int step_elems() {  // of the reduction in one step of k_project: 128 bytes of a row
@@ -45,7 +45,8 @@ __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u
 }
 
 // z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without. A block takes ROWS rows (of `order`, or one
-// row as it lies) and one part of the reduction, its wavefronts an eighth of that each; once for every party among the rows.
+// row as it lies) and one part of the reduction, its wavefronts
+// 256 bytes of every row in turn; once for every party among the rows.
 template <class T, int ROWS, int RT>
 __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
                                                      const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
@@ -59,13 +60,12 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   const int raw = mine < rows ? index[mine] : -1;
   const int a = (u32)raw < parties ? raw : -1;
   if (status && part == 0 && threadIdx.x < 16 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
-  // this wavefront's share of the reduction, in steps of 32
-  const u32 steps = (inner + 31) / 32, units = parts * kShrinkWaves, unit = part * kShrinkWaves + wave;
-  const u32 first = (u32)((u64)steps * unit / units), end = (u32)((u64)steps * (unit + 1) / units);
+  // the part's share of the reduction, in steps of 32
+  const u32 steps = (inner + 31) / 32, first = (u32)((u64)steps * part / parts), end = (u32)((u64)steps * (part + 1) / parts);
   float own[RT];  // of row out_i, r = lane % 16
 #pragma unroll
   for (int i = 0; i < RT; ++i) own[i] = 0.0f;
-  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave % 4;
+  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave;
   const u32 out_t = row_at(out_i);
   const int out_a = out_t < rows ? party_of(index, out_t, parties) : -1;
   u64 left = __builtin_amdgcn_ballot_w64(a >= 0) & 0xFFFF;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
     f32x4 acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (u32 s0 = first; s0 < end; s0 += kAhead) {
+    for (u32 s0 = first + wave * kAhead; s0 < end; s0 += kShrinkWaves * kAhead) {
       Vec8<T> xv[kAhead], fv[kAhead][RT];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
     }
     __syncthreads();
   }
-  if (out_t < rows && (ROWS == 1 ? threadIdx.x < 16 : wave < 4)) {
+  if (out_t < rows && (ROWS != 1 || threadIdx.x < 16)) {
     const float by = out_a < 0 ? 0.0f : scale[out_a] * (d.threshold ? d.scale : 1.0f);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 // h, where it is wanted, is written by the first block.
 constexpr int kFewWaves = 8;
 template <class T, int RT, bool DROP>
-__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld,
+__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld, bool wide_f,
                                                                    const float* z, u32 z_ld, u32 parts, const int* index, u32 rows, u32 inner, u32 outer, u32 parties,
                                                                    u32 rank, Drop d, T* y, size_t ldy, float* h) {
   constexpr int kThreadsFew = kFewWaves * kWave, kAhead = RT >= 4 ? 2 : 4;  // steps of 32
@@ -569,7 +569,10 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, s
       if (a >= 0) {
         const T* const fr = f + ((size_t)a * outer + oo) * f_ld + r0;
         const u32 n = rank - r0 < 16 ? rank - r0 : 16;
-        for (u32 r = 0; r < n; ++r) low[q] += zl[i / 16 * 16 + r] * (float)fr[r];
+        const Vec8<T> f0 = wide_f ? load_wide(fr) : load_some(fr, (int)n), f1 = n <= 8 ? Vec8<T>{} : wide_f ? load_wide(fr + 8) : load_some(fr + 8, (int)n - 8);
+#pragma unroll
+        for (u32 r = 0; r < 16; ++r)
+          if (r < n) low[q] += zl[i / 16 * 16 + r] * (float)(r < 8 ? f0.v[r & 7] : f1.v[r & 7]);
       }
     }
     __syncthreads();
@@ -1017,7 +1020,7 @@ struct Product {
       const u32 parts = shrink_parts(s.rows, s.inner);
 #define HAFLO_LOCAL_RUN(RT, DROP)                                                                                                        \
   hipLaunchKernelGGL((k_project_few<T, RT, DROP>), dim3((unsigned)(ceil_div(s.rows, RT * 16) * ceil_div(s.outer, 16))),                  \
-                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, (const float*)z_parts(), ranks(), parts, index, \
+                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, s.rank % 8 == 0 && wide_rows<T>(f.p, f.ld), (const float*)z_parts(), ranks(), parts, index, \
                      (u32)s.rows, (u32)s.inner, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, y, ldy, parts > 1 ? h : nullptr)
 #define HAFLO_LOCAL_FEW(DROP)                        \
   do {                                               \
