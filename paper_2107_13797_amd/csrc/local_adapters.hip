@@ -5,11 +5,10 @@
 //             dA[a] = sum_t g[t] drop(x[t])^T,   dB[a] = sum_t dy[t] h[t]^T
 //
 // h and g, the rows' short vectors ("z" where a kernel serves both directions), come from k_shrink. k_project forms
-// the large product and adds the adapters' part, k_project_few does for few rows. k_group lists the rows by
+// the large product and adds the adapters' part, k_project_few does for few rows. k_prepare lists the rows by
 // adapter: a tile's rows are taken from that list, so that they share one adapter as a rule, whatever the order the
-// caller has them in, and k_grad sums over the rows of one adapter. Operands whose rows do not begin at 16-byte
-// boundaries are laid out anew by k_pad, and what reduces along columns (W, A and B of the backward pass) by k_transpose: so
-// every product reduces along rows in 16-byte loads.
+// caller has them in, and k_grad sums over the rows of one adapter. It also lays out anew what reduces along columns (W, A and B
+// of the backward pass) and, for k_project, operands whose rows do not begin at 16-byte boundaries.
 #include "local_common.hpp"
 
 using namespace haflo::local;
@@ -366,8 +365,7 @@ __device__ __forceinline__ void reduce(const From& x, const typename From::At (&
 template <class T, int TM, int TN, int WM, int WN, bool DROP, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
                                                              const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
-                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, bool wide_y,
-                                                             u32 x_bytes, u32 w_bytes) {
+                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, u32 x_bytes, u32 w_bytes) {
   constexpr int KE = step_elems<T>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
   constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
   __shared__ __align__(16) T lds[2 * (TM + TN) * KE];
@@ -463,7 +461,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   // A lane holds four outputs of each of its rows: results of 16 bits go through the tiles' place in LDS, a wavefront's through its
   // own part of it, and leave in 16-byte pieces, a whole line or half a line of a row at a time.
   constexpr u32 kPieces = OT * 16 * sizeof(T) / 16, kShift = kPieces == 8 ? 1 : 2;
-  if (sizeof(T) == 2 && wide_y) {
+  if (sizeof(T) == 2) {
     __syncthreads();  // other wavefronts have read the last tiles
     T* const own = lds + wave * (RT * 16 * OT * 16);
 #pragma unroll
@@ -482,7 +480,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 #pragma unroll
     for (u32 n = 0; n < RT * 16 / kRows; ++n) {
       const u32 r = n * kRows + lane / kPieces, piece = lane % kPieces;
-      const Vec8<T> v = load_wide(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8);
+      Vec8<T> v;
+      __builtin_memcpy(&v, __builtin_assume_aligned(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8, 16), 16);
       const u32 row = lane_read(t[n * kRows / 16], (int)(r % 16)), o = o0 + out0 + piece * 8;
       if (row >= rows || o >= outer) continue;
       T* const to = y + (size_t)row * ldy + o;
@@ -501,8 +500,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
       T v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = (T)acc[i][j][e];
-      if (sizeof(T) == 4 && wide_y && o + 4 <= outer) {
-        __builtin_memcpy(__builtin_assume_aligned(to, 16), v, sizeof(v));
+      if (o + 4 <= outer) {
+        __builtin_memcpy(to, v, sizeof(v));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -517,7 +516,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 // h, where it is wanted, is written by the first block.
 constexpr int kFewWaves = 8;
 template <class T, int RT, bool DROP>
-__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld, bool wide_f,
+__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld,
                                                                    const float* z, u32 z_ld, u32 parts, const int* index, u32 rows, u32 inner, u32 outer, u32 parties,
                                                                    u32 rank, Drop d, T* y, size_t ldy, float* h) {
   constexpr int kThreadsFew = kFewWaves * kWave, kAhead = RT >= 4 ? 2 : 4;  // steps of 32
@@ -569,7 +568,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, s
       if (a >= 0) {
         const T* const fr = f + ((size_t)a * outer + oo) * f_ld + r0;
         const u32 n = rank - r0 < 16 ? rank - r0 : 16;
-        const Vec8<T> f0 = wide_f ? load_wide(fr) : load_some(fr, (int)n), f1 = n <= 8 ? Vec8<T>{} : wide_f ? load_wide(fr + 8) : load_some(fr + 8, (int)n - 8);
+        const Vec8<T> f0 = n >= 8 ? load_wide(fr) : load_some(fr, (int)n), f1 = n <= 8 ? Vec8<T>{} : n == 16 ? load_wide(fr + 8) : load_some(fr + 8, (int)n - 8);
 #pragma unroll
         for (u32 r = 0; r < 16; ++r)
           if (r < n) low[q] += zl[i / 16 * 16 + r] * (float)(r < 8 ? f0.v[r & 7] : f1.v[r & 7]);
@@ -896,7 +895,7 @@ size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * 
 size_t whole_ranks(size_t rank) { return ceil_div(rank, kRanks) * kRanks; }
 u32 grad_rows(const Sizes& s) { return chunk_rows(s.rows, s.inner + s.outer, s.rank); }
 struct Plan {
-  size_t z_parts, z, x, dy, w, low, f, begin, chunk_begin, chunk, order, sums_a, sums_b, total;
+  size_t z_parts, z, x, w, low, f, begin, chunk_begin, chunk, order, sums_a, sums_b, total;
   size_t chunks;  // at most
 };
 Plan adapter_plan(int type, bool backward, const Sizes& s) {
@@ -911,9 +910,9 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
   const size_t k = backward ? s.outer : s.inner, n = backward ? s.inner : s.outer, kp = padded(type, k);  // the product's sizes
   p.z_parts = take(shrink_parts(s.rows, k) * s.rows * ranks * 4);
   p.z = take(s.rows * ranks * 4);
-  p.x = take(s.rows * padded(type, s.inner) * e);
+  p.x = take(s.rows * kp * e);
   p.w = take(n * kp * e);
-  p.low = take(s.parties * s.rank * kp * e);
+  if (backward) p.low = take(s.parties * s.rank * kp * e);
   p.f = take(s.parties * n * ranks * e);
   p.chunks = s.rows / grad_rows(s) + s.parties;
   p.begin = take((s.parties + 1) * 4);
@@ -921,7 +920,6 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
   p.chunk = take(p.chunks * 4);
   p.order = take(s.rows * 4);
   if (backward) {
-    p.dy = take(s.rows * kp * e);
     p.sums_a = take(p.chunks * s.rank * s.inner * 4);
     p.sums_b = take(p.chunks * s.rank * s.outer * 4);
   }
@@ -945,11 +943,11 @@ struct Layouts {
     blocks += need;
     return {(const T*)out, out_ld};
   }
-  // A matrix with rows at 16-byte boundaries and of a multiple of `step` elements, zeros behind what they hold: itself, or its
-  // copy at `room`.
+  // A matrix with rows at 16-byte boundaries and of a multiple of `step` elements, zeros behind what they hold, as k_project
+  // needs it: itself, or its copy at `room`.
   Rows<T> wide(const void* m, size_t ld, size_t rows, size_t cols, size_t step, char* room) {
-    if (wide_rows<T>(m, ld) && cols % step == 0) return {(const T*)m, ld};
-    const size_t to = ceil_div(cols, step < 8 ? 8 : step) * (step < 8 ? 8 : step);
+    if ((uintptr_t)m % 16 == 0 && ld * sizeof(T) % 16 == 0 && cols % step == 0) return {(const T*)m, ld};
+    const size_t to = ceil_div(cols, step) * step;
     return add(m, room, ld, 0, 0, rows, cols, to, false, ceil_div(rows * (to / 8), kPrepareThreads));
   }
   Rows<T> transposed(const void* in, size_t ld, size_t in_step, size_t rows, size_t cols, size_t count, char* room, size_t out_ld) {
@@ -1020,7 +1018,7 @@ struct Product {
       const u32 parts = shrink_parts(s.rows, s.inner);
 #define HAFLO_LOCAL_RUN(RT, DROP)                                                                                                        \
   hipLaunchKernelGGL((k_project_few<T, RT, DROP>), dim3((unsigned)(ceil_div(s.rows, RT * 16) * ceil_div(s.outer, 16))),                  \
-                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, s.rank % 8 == 0 && wide_rows<T>(f.p, f.ld), (const float*)z_parts(), ranks(), parts, index, \
+                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, (const float*)z_parts(), ranks(), parts, index, \
                      (u32)s.rows, (u32)s.inner, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, y, ldy, parts > 1 ? h : nullptr)
 #define HAFLO_LOCAL_FEW(DROP)                        \
   do {                                               \
@@ -1034,14 +1032,13 @@ struct Product {
 #undef HAFLO_LOCAL_RUN
       return;
     }
-    const bool wide_y = wide_rows<T>(y, ldy);
     const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
     const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
 #define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP, FAR)                                                                                        \
   hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP, FAR>), dim3((unsigned)(ceil_div(s.rows, TM) * ceil_div(s.outer, TN))),           \
                      dim3(WM * WN * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (const float*)z(), index, order(),                          \
                      (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(), after, y, ldy, \
-                     wide_y, (u32)x_bytes, (u32)w_bytes)
+                     (u32)x_bytes, (u32)w_bytes)
 #define HAFLO_LOCAL_TILE(DROP)                                                                                    \
   do {                                                                                                            \
     if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, true);                                                         \
@@ -1098,13 +1095,15 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
     const bool many = rows > kFewRows;
-    const size_t step = many ? step_elems<T>() : 1;
     Layouts<T> lay;
-    if (many) add_group(lay.p, s, d_index, ws, plan, d_status);
-    Product<T> f = {lay.wide(d_x, ldx, rows, inner, step, ws + plan.x), lay.wide(d_w, ldw, outer, inner, step, ws + plan.w),
-                    lay.wide(d_a, inner, parties * rank, inner, 1, ws + plan.low), {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
+    Product<T> f = {{(const T*)d_x, ldx}, {(const T*)d_w, ldw}, {(const T*)d_a, inner}, {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
                     plan, many ? nullptr : d_status, st};
-    if (many) f.f = lay.wide(d_b, rank, parties * outer, rank, kRanks, ws + plan.f);
+    if (many) {
+      add_group(lay.p, s, d_index, ws, plan, d_status);
+      f.x = lay.wide(d_x, ldx, rows, inner, step_elems<T>(), ws + plan.x);
+      f.w = lay.wide(d_w, ldw, outer, inner, step_elems<T>(), ws + plan.w);
+      f.f = lay.wide(d_b, rank, parties * outer, rank, kRanks, ws + plan.f);
+    }
     lay.launch(st);
     f.shrink(d_h);
     f.project(d_h, (T*)d_y, ldy);
@@ -1130,17 +1129,14 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
     const bool many = rows > kFewRows;
-    const size_t step = many ? step_elems<T>() : 1;
     const size_t ranks = whole_ranks(rank);
     const size_t kp = padded(type, outer);
     const Sizes back = {rows, outer, inner, parties, rank};
     Layouts<T> lay;
     add_group(lay.p, s, d_index, ws, plan, d_status);
-    Rows<T> x = {};
-    Rows<T> dy = {};
+    Rows<T> dy = {(const T*)d_dy, lddy};
     if (rows) {
-      x = lay.wide(d_x, ldx, rows, inner, 1, ws + plan.x);
-      dy = lay.wide(d_dy, lddy, rows, outer, step, ws + plan.dy);
+      if (many) dy = lay.wide(d_dy, lddy, rows, outer, step_elems<T>(), ws + plan.x);
       // B^T, W^T and A^T: what is reduced along columns here
       Product<T> f = {dy, {}, lay.transposed(d_b, rank, outer * rank, outer, rank, parties, ws + plan.low, kp), {}, d_scale, d_index, back, none, d,
                       ws, plan, nullptr, st};
@@ -1155,7 +1151,7 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
     } else {
       lay.launch(st);
     }
-    const GradOf<T> a = {x.p, x.ld, (const float*)(ws + plan.z), (float*)(ws + plan.sums_a), d_da, inner, 1, (u32)inner, (u32)ranks, d};
+    const GradOf<T> a = {(const T*)d_x, ldx, (const float*)(ws + plan.z), (float*)(ws + plan.sums_a), d_da, inner, 1, (u32)inner, (u32)ranks, d};
     const GradOf<T> b = {dy.p, dy.ld, d_h, (float*)(ws + plan.sums_b), d_db, 1, rank, (u32)outer, (u32)rank, none};
     grads<T>(a, b, s, plan, ws, st);
   });

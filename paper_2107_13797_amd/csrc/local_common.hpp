@@ -25,26 +25,31 @@ template <class T>
 struct Vec8 {
   T v[8];
 };
+// Vector accesses of memory need no more alignment than an element's.
+typedef u32x4 u32x4_of_2 __attribute__((aligned(2), may_alias));
+typedef u32x4 u32x4_of_4 __attribute__((aligned(4), may_alias));
 template <class T>
-constexpr int vec_words() {
-  return (int)sizeof(T) * 2;  // 32-bit words of eight elements
-}
-
-// Whether eight elements at a multiple of eight from `p`, rows `ld` apart, can be moved 16 bytes at a time.
-template <class T>
-inline bool wide_rows(const void* p, size_t ld) {
-  return ((uintptr_t)p & 15) == 0 && (ld * sizeof(T)) % 16 == 0;
-}
-
-template <class T>
-__device__ __forceinline__ Vec8<T> load_wide(const T* p) {  // 16-byte aligned
+__device__ __forceinline__ Vec8<T> load_wide(const T* p) {
   Vec8<T> r;
-  __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), sizeof(r));
+  if (sizeof(T) == 2) {
+    const u32x4 v = *(const u32x4_of_2*)p;
+    __builtin_memcpy(&r, &v, 16);
+  } else {
+    const u32x4 v[2] = {((const u32x4_of_4*)p)[0], ((const u32x4_of_4*)p)[1]};
+    __builtin_memcpy(&r, v, sizeof(r));
+  }
   return r;
 }
 template <class T>
-__device__ __forceinline__ void store_wide(T* p, const Vec8<T>& v) {
-  __builtin_memcpy(__builtin_assume_aligned(p, 16), &v, sizeof(v));
+__device__ __forceinline__ void store_wide(T* p, const Vec8<T>& r) {
+  u32x4 v[sizeof(r) / 16];
+  __builtin_memcpy(v, &r, sizeof(r));
+  if (sizeof(T) == 2) {
+    *(u32x4_of_2*)p = v[0];
+  } else {
+    ((u32x4_of_4*)p)[0] = v[0];
+    ((u32x4_of_4*)p)[1] = v[sizeof(r) / 16 - 1];
+  }
 }
 // The first `n` of eight elements; the others are zero.
 template <class T>

@@ -8,8 +8,8 @@ namespace {
 constexpr int kDropThreads = 256;
 constexpr int kDropBlocks = 4096;
 
-// A lane takes eight consecutive columns of a row: one generator call and, where rows allow it, 16-byte accesses.
-template <class T, bool WIDE, bool RESIDUAL>
+// A lane takes eight consecutive columns of a row: one generator call and 16-byte accesses.
+template <class T, bool RESIDUAL>
 __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, size_t ldx, const T* res, size_t ldr, T* y, size_t ldy,
                                                           u32 rows, u32 cols, Drop d) {
   const u32 groups = (cols + 7) / 8;
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, size_t ldx
     const T* px = x + row * ldx + col;
     const T* pr = RESIDUAL ? res + row * ldr + col : nullptr;
     T* py = y + row * ldy + col;
-    const bool wide = WIDE && n == 8;
+    const bool wide = n == 8;
     Vec8<T> v = wide ? load_wide(px) : load_some(px, n), r = {};
     if (RESIDUAL) r = wide ? load_wide(pr) : load_some(pr, n);
     const u32x4 draws = philox(d, g, row);
@@ -41,17 +41,10 @@ int dropout(const void* x, size_t ldx, const void* res, size_t ldr, void* y, siz
             const Drop& d, hipStream_t st) {
   const size_t need = ceil_div(rows * ceil_div(cols, 8), kDropThreads);
   const dim3 grid((unsigned)(need < kDropBlocks ? need : kDropBlocks)), block(kDropThreads);
-  const bool wide = wide_rows<T>(x, ldx) && wide_rows<T>(y, ldy) && (!res || wide_rows<T>(res, ldr));
-#define HAFLO_LOCAL_RUN(WIDE, RES) \
-  hipLaunchKernelGGL((k_dropout<T, WIDE, RES>), grid, block, 0, st, (const T*)x, ldx, (const T*)res, ldr, (T*)y, ldy, (u32)rows, (u32)cols, d)
-  if (res) {
-    if (wide) HAFLO_LOCAL_RUN(true, true);
-    else HAFLO_LOCAL_RUN(false, true);
-  } else {
-    if (wide) HAFLO_LOCAL_RUN(true, false);
-    else HAFLO_LOCAL_RUN(false, false);
-  }
-#undef HAFLO_LOCAL_RUN
+  if (res)
+    hipLaunchKernelGGL((k_dropout<T, true>), grid, block, 0, st, (const T*)x, ldx, (const T*)res, ldr, (T*)y, ldy, (u32)rows, (u32)cols, d);
+  else
+    hipLaunchKernelGGL((k_dropout<T, false>), grid, block, 0, st, (const T*)x, ldx, (const T*)res, ldr, (T*)y, ldy, (u32)rows, (u32)cols, d);
   return launched();
 }
 

@@ -72,8 +72,9 @@ __device__ __forceinline__ float value_of(u64 key) {
 }
 
 struct TopList {
-  u64 mine;  // this lane's entry, 0: none
-  u64 last;  // entry top - 1, the same in all lanes
+  u64 mine;   // this lane's entry, 0: none
+  u64 last;   // entry top - 1, the same in all lanes, or the floor where that is higher
+  u64 floor;  // no element up to it belongs into the list
 };
 // key_lane's `key` into the list, which it belongs into
 __device__ __forceinline__ void top_insert(TopList& l, u64 key, int key_lane, int top) {
@@ -87,8 +88,9 @@ __device__ __forceinline__ void top_insert(TopList& l, u64 key, int key_lane, in
   const int lane = (int)lane_id();
   if (lane > place) l.mine = (u64)phi << 32 | plo;
   if (lane == place) l.mine = k;
-  l.last = (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(l.mine >> 32), top - 1) << 32 |
-           (u32)__builtin_amdgcn_readlane((int)(u32)l.mine, top - 1);
+  const u64 last = (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(l.mine >> 32), top - 1) << 32 |
+                   (u32)__builtin_amdgcn_readlane((int)(u32)l.mine, top - 1);
+  l.last = last > l.floor ? last : l.floor;
 }
 // Two descending lists to the 64 greatest of both: the larger of each entry and the other list's mirrored one is a
 // bitonic sequence, which six exchanges sort.
@@ -101,13 +103,6 @@ __device__ __forceinline__ u64 top_merge(u64 mine, u64 mirrored) {
     v = (o > v) != upper ? o : v;
   }
   return v;
-}
-
-// Rows need not begin at a 16-byte boundary: vector v of a row holds columns 8 v - skew .. + 7 with `skew` the elements
-// between the boundary below the row and the row, so that all vectors but the outer ones are loaded whole.
-template <class T>
-__device__ __forceinline__ u32 skew_of(const T* row) {
-  return (u32)((uintptr_t)row & 15) / (u32)sizeof(T);
 }
 
 template <class T>
@@ -130,14 +125,24 @@ __device__ __forceinline__ void take(Soft& a, const Vec8<T>& v) {
 
 // the elements of `v` that belong into the list; all lanes of a wavefront call this together
 template <class T>
-__device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, int col, u32 cols, bool live, int top) {
+__device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, u32 col, u32 cols, bool live, int top) {
   u64 k[8], most = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    k[j] = live && (u32)(col + j) < cols ? key_of((float)v.v[j], (u32)(col + j)) : 0;
+    k[j] = live && col + j < cols ? key_of((float)v.v[j], col + j) : 0;
     most = k[j] > most ? k[j] : most;
   }
   if (__builtin_amdgcn_ballot_w64(most > l.last) == 0) return;
+  if (l.last == 0) {
+    // The first elements: `top` lanes have one that is no less than the top-th of the lanes' greatest, which is found bit by
+    // bit; what is less need not be inserted only to be pushed out again (20 of 512: 25 insertions instead of 85).
+    const u32 key = (u32)(most >> 32);
+    u32 least = 0;
+#pragma unroll 1
+    for (u32 bit = 0x80000000u; bit; bit >>= 1)
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= (least | bit))) >= top) least |= bit;
+    if (least) l.last = l.floor = ((u64)least << 32) - 1;
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     u64 who = __builtin_amdgcn_ballot_w64(k[j] > l.last);
@@ -150,13 +155,13 @@ __device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, int col, 
   }
 }
 
-// vector at column `col` (negative before the row) of a row; -inf outside
+// eight elements of a row from column `col` on; -inf past its end
 template <class T>
-__device__ __forceinline__ Vec8<T> load_row(const T* row, int col, u32 cols) {
-  if (col >= 0 && (u32)col + 8 <= cols) return load_wide(row + col);
+__device__ __forceinline__ Vec8<T> load_row(const T* row, u32 col, u32 cols) {
+  if (col + 8 <= cols) return load_wide(row + col);
   Vec8<T> r;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) r.v[j] = (u32)(col + j) < cols ? row[col + j] : (T)neg_inf();
+  for (int j = 0; j < 8; ++j) r.v[j] = col + j < cols ? row[col + j] : (T)neg_inf();
   return r;
 }
 
@@ -202,21 +207,21 @@ __global__ __launch_bounds__(kThreads) void k_labels(const T* x, size_t ld, u32 
   const u32 r = unit / parts, p = unit % parts;
   if (W == 1 && r >= rows) return;
   const T* row = x + (size_t)r * ld;
-  const u32 skew = skew_of(row), vectors = (cols + skew + 7) / 8;
+  const u32 vectors = (cols + 7) / 8;
   const u32 first = (u32)((u64)vectors * p / parts), end = (u32)((u64)vectors * (p + 1) / parts);
   constexpr u32 kStep = W * kWave;
   Soft a = {neg_inf(), 0.0f, 0.0f};
-  TopList l = {0, 0};
+  TopList l = {0, 0, 0};
   for (u32 base = first; base < end; base += kStep * kAhead) {
     Vec8<T> v[kAhead];
     const u32 at = base + threadIdx.x % kStep;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (at + i * kStep < end) v[i] = load_row(row, (int)((at + i * kStep) * 8 - skew), cols);
+      if (at + i * kStep < end) v[i] = load_row(row, (at + i * kStep) * 8, cols);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const bool live = at + i * kStep < end;
-      const int col = (int)((at + i * kStep) * 8 - skew);
+      const u32 col = (at + i * kStep) * 8;
       if (live) take(a, v[i]);
       if (TOP && base + i * kStep < end) take_top(l, v[i], col, cols, live, top);
     }
@@ -241,25 +246,39 @@ __global__ __launch_bounds__(kThreads) void k_labels(const T* x, size_t ld, u32 
   }
 }
 
-// a wavefront to a row: joins its parts, in their order
+// Joins the parts of a row: its first wavefront the sums, in their order; all of them every eighth list each, and what they
+// have then pair by pair.
+constexpr int kJoinWaves = 8;
 template <class T, bool TOP>
-__global__ __launch_bounds__(kWave) void k_label_join(const T* x, size_t ld, u32 cols, int top, u32 parts, LabelOut o,
-                                                      const Part* part, const u64* lists) {
-  const u32 r = blockIdx.x, lane = lane_id();
+__global__ __launch_bounds__((TOP ? kJoinWaves : 1) * kWave) void k_label_join(const T* x, size_t ld, u32 cols, int top, u32 parts, LabelOut o,
+                                                                              const Part* part, const u64* lists) {
+  __shared__ u64 list[TOP ? kJoinWaves / 2 : 1][kWave];
+  const u32 r = blockIdx.x, lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  u64 mine = 0;
+  if (TOP) {
+    const int at = kWave - 1 - (int)lane;  // mirrored
+    const u64* const mirrored = lists + (size_t)r * parts * top + at;
+    u64 next = wave < parts && at < top ? mirrored[(size_t)wave * top] : 0;
+    for (u32 p = wave; p < parts; p += kJoinWaves) {
+      const u64 now = next;
+      if (p + kJoinWaves < parts) next = at < top ? mirrored[(size_t)(p + kJoinWaves) * top] : 0;
+      mine = top_merge(mine, now);
+    }
+#pragma unroll
+    for (u32 half = kJoinWaves / 2; half >= 1; half >>= 1) {
+      if (wave >= half && wave < 2 * half) list[wave - half][lane] = mine;
+      __syncthreads();
+      if (wave < half) mine = top_merge(mine, list[wave][kWave - 1 - lane]);
+      __syncthreads();
+    }
+    if (wave != 0) return;
+  }
   Soft a = {neg_inf(), 0.0f, 0.0f};
   for (u32 p = lane; p < parts; p += kWave) {
     const Part q = part[(size_t)r * parts + p];
     join(a, Soft{q.m, q.s, q.t});
   }
-  a = wave_join(a);
-  u64 mine = 0;
-  if (TOP) {
-    for (u32 p = 0; p < parts; ++p) {
-      const int at = kWave - 1 - (int)lane;
-      mine = top_merge(mine, at < top ? lists[((size_t)r * parts + p) * top + at] : 0);
-    }
-  }
-  finish_row(o, x + (size_t)r * ld, r, cols, a, mine, top);
+  finish_row(o, x + (size_t)r * ld, r, cols, wave_join(a), mine, top);
 }
 
 // a lane to a row of few columns
@@ -305,32 +324,32 @@ struct GradIn {
   const float* dtop;
 };
 // a lane to eight columns of a row
-template <class T, bool SAME>
+template <class T>
 __global__ __launch_bounds__(kThreads) void k_labels_grad(const T* x, size_t ld, u32 rows, u32 cols, int top, GradIn g, T* dx,
                                                           size_t lddx) {
-  constexpr u32 kMostSkew = 16 / sizeof(T) - 1;
-  const u32 groups = (cols + kMostSkew + 7) / 8;
+  const u32 groups = (cols + 7) / 8;
   const u64 total = (u64)rows * groups, step = (u64)gridDim.x * kThreads;
   for (u64 at = (u64)blockIdx.x * kThreads + threadIdx.x; at < total; at += step) {
     const u32 r = (u32)(at / groups), v = (u32)(at - (u64)r * groups);
     const T* row = x + (size_t)r * ld;
     T* out = dx + (size_t)r * lddx;
-    const int col = (int)(v * 8 - skew_of(row));
-    if (col >= (int)cols) continue;
+    const u32 col = v * 8;
     const Vec8<T> in = load_row(row, col, cols);
     const float lse = g.lse[r], entropy = g.entropy[r], dh = g.dentropy ? g.dentropy[r] : 0.0f;
     const int label = g.label[r];
     const float dlogp = (u32)label < cols ? g.dlogp[r] : 0.0f;
     float given = dlogp, extra[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) extra[j] = label == col + j ? dlogp : 0.0f;
+    for (int j = 0; j < 8; ++j) extra[j] = (u32)label == col + j ? dlogp : 0.0f;
     if (g.dtop) {
       for (int k = 0; k < top; ++k) {
         const int i = g.top_index[(size_t)r * top + k];
         const float d = (u32)i < cols ? g.dtop[(size_t)r * top + k] : 0.0f;
         given += d;
+        if ((u32)i - col < 8u) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) extra[j] += i == col + j ? d : 0.0f;
+          for (int j = 0; j < 8; ++j) extra[j] += (u32)i == col + j ? d : 0.0f;
+        }
       }
     }
     Vec8<T> res;
@@ -340,13 +359,8 @@ __global__ __launch_bounds__(kThreads) void k_labels_grad(const T* x, size_t ld,
       const float d = (p == 0.0f ? 0.0f : p * (-given - dh * (lp + entropy))) + extra[j];
       res.v[j] = (T)(lse == neg_inf() ? 0.0f : d);
     }
-    if (SAME && col >= 0 && (u32)col + 8 <= cols) {
-      store_wide(out + col, res);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if ((u32)(col + j) < cols) out[col + j] = res.v[j];
-    }
+    if (col + 8 <= cols) store_wide(out + col, res);
+    else store_some(out + col, res, (int)(cols - col));
   }
 }
 
@@ -387,7 +401,7 @@ int label_forward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, c
 #undef HAFLO_LOCAL_RUN
   if (parts > 1) {
     if (top)
-      hipLaunchKernelGGL((k_label_join<T, true>), dim3((unsigned)rows), dim3(kWave), 0, st, x, ld, (u32)cols, (int)top, parts, o, part, lists);
+      hipLaunchKernelGGL((k_label_join<T, true>), dim3((unsigned)rows), dim3(kJoinWaves * kWave), 0, st, x, ld, (u32)cols, (int)top, parts, o, part, lists);
     else
       hipLaunchKernelGGL((k_label_join<T, false>), dim3((unsigned)rows), dim3(kWave), 0, st, x, ld, (u32)cols, (int)top, parts, o, part, lists);
   }
@@ -396,12 +410,9 @@ int label_forward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, c
 
 template <class T>
 int label_backward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, const GradIn& g, T* dx, size_t lddx, hipStream_t st) {
-  const size_t need = ceil_div(rows * ((cols + 16 / sizeof(T) + 6) / 8), kThreads);
-  const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(kThreads);
-  // every row of dx lies as its row of x does
-  const bool same = ((uintptr_t)x & 15) == ((uintptr_t)dx & 15) && (ld * sizeof(T)) % 16 == (lddx * sizeof(T)) % 16;
-  if (same) hipLaunchKernelGGL((k_labels_grad<T, true>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx, lddx);
-  else hipLaunchKernelGGL((k_labels_grad<T, false>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx, lddx);
+  const size_t need = ceil_div(rows * ceil_div(cols, 8), kThreads);
+  hipLaunchKernelGGL((k_labels_grad<T>), dim3((unsigned)(need < 8192 ? need : 8192)), dim3(kThreads), 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx,
+                     lddx);
   return launched();
 }
 
