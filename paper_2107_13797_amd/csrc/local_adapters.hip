@@ -5,7 +5,7 @@
 //             dA[a] = sum_t g[t] drop(x[t])^T,   dB[a] = sum_t dy[t] h[t]^T
 //
 // h and g, the rows' short vectors ("z" where a kernel serves both directions), come from k_shrink. k_project forms
-// the large product and adds the adapters' part, k_project_few does for few rows. k_prepare lists the rows by
+// the large product and adds the adapters' part, k_few does for few rows. k_prepare lists the rows by
 // adapter: a tile's rows are taken from that list, so that they share one adapter as a rule, whatever the order the
 // caller has them in, and k_grad sums over the rows of one adapter. It also lays out anew what reduces along columns (W, A and B
 // of the backward pass) and, for k_project, operands whose rows do not begin at 16-byte boundaries.
@@ -46,16 +46,16 @@ __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u
 // z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without. A block takes ROWS rows (of `order`, or one
 // row as it lies) and one part of the reduction, its wavefronts
 // 256 bytes of every row in turn; once for every party among the rows.
-template <class T, int ROWS, int RT>
+template <class T, int RT>
 __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
                                                      const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
                                                      u32 z_ld, float* z, float* h, u32* status) {
   constexpr int kAhead = RT == 1 ? 4 : 2;  // steps whose operands are on their way together
   __shared__ float sum[kShrinkWaves][RT][16][17];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 at0 = blockIdx.x / parts * ROWS, part = blockIdx.x % parts;
-  const auto row_at = [&](u32 i) { return at0 + i >= rows ? rows : order ? order[at0 + i] : at0 + i; };
-  const u32 mine = row_at(ROWS == 1 ? 0 : lane % 16);
+  const u32 at0 = blockIdx.x / parts * 16, part = blockIdx.x % parts;
+  const auto row_at = [&](u32 i) { return at0 + i >= rows ? rows : order[at0 + i]; };
+  const u32 mine = row_at(lane % 16);
   const int raw = mine < rows ? index[mine] : -1;
   const int a = (u32)raw < parties ? raw : -1;
   if (status && part == 0 && threadIdx.x < 16 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   float own[RT];  // of row out_i, r = lane % 16
 #pragma unroll
   for (int i = 0; i < RT; ++i) own[i] = 0.0f;
-  const u32 out_i = ROWS == 1 ? 0 : lane / 16 * 4 + wave;
+  const u32 out_i = lane / 16 * 4 + wave;
   const u32 out_t = row_at(out_i);
   const int out_a = out_t < rows ? party_of(index, out_t, parties) : -1;
   u64 left = __builtin_amdgcn_ballot_w64(a >= 0) & 0xFFFF;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
     }
     __syncthreads();
   }
-  if (out_t < rows && (ROWS != 1 || threadIdx.x < 16)) {
+  if (out_t < rows) {
     const float by = out_a < 0 ? 0.0f : scale[out_a] * (d.threshold ? d.scale : 1.0f);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -511,85 +511,176 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   }
 }
 
-// The same for few rows: W's rows are read once, by as many blocks as it has sixteens of them. A block's eight wavefronts
-// share the reduction, 64 elements each in turn; the adapters' part is added where they are joined. Parts of z are summed here, and
-// h, where it is wanted, is written by the first block.
+// The same for few rows, in two launches. k_few reads W once: a block takes 64 outputs and one part of the reduction, 1024 bytes of
+// every row at a time, its wavefronts four sixteens of outputs in two halves of that; further blocks form the parts of z = h or
+// g for one row each, as k_shrink does. k_few_join adds the parts, and the adapters' part to them. x goes through LDS: what a
+// matrix instruction takes of it is 64 bytes of each of sixteen rows, and such a load costs some 70 cycles of the unit that
+// addresses memory where 1024 bytes in a row cost 16 (64 rows: 25 us when every wavefront loaded its operands itself).
 constexpr int kFewWaves = 8;
-template <class T, int RT, bool DROP>
-__global__ __launch_bounds__(kFewWaves * kWave) void k_project_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, u32 f_ld,
-                                                                   const float* z, u32 z_ld, u32 parts, const int* index, u32 rows, u32 inner, u32 outer, u32 parties,
-                                                                   u32 rank, Drop d, T* y, size_t ldy, float* h) {
-  constexpr int kThreadsFew = kFewWaves * kWave, kAhead = RT >= 4 ? 2 : 4;  // steps of 32
-  __shared__ float sum[kFewWaves][RT * 16][17];
-  __shared__ float zl[RT * 16 * 16];
+constexpr int kFewBytes = 1024;
+// eight elements, the q-th of a row in LDS; pieces of 16 bytes of sixteen rows lie on different banks
+template <class T>
+__device__ __forceinline__ T* few_piece(T* tile, u32 row, u32 q, u32 e) {
+  constexpr u32 kPieces = sizeof(T) / 2;  // of eight elements
+  return tile + row * (kFewBytes / sizeof(T)) + ((q * kPieces + e) ^ (row & 15)) * (16 / sizeof(T));
+}
+template <class T, int RT>
+__device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, size_t ldw, u32 rows, u32 inner, u32 outer, u32 tile, u32 part,
+                                            u32 parts, float* sums, T* lx, f32x4* half) {
+  constexpr u32 kElems = kFewBytes / sizeof(T), kSteps = kElems / 32 / 2, kLanes = kElems / 8, kRows = kWave / kLanes;  // rows of a load
+  constexpr u32 kLoads = RT * 16 / (kFewWaves * kRows), kPieces = sizeof(T) / 2;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 tiles_n = (outer + 15) / 16, t0 = blockIdx.x / tiles_n * (RT * 16), o0 = blockIdx.x % tiles_n * 16;
+  const u32 o = tile * 64 + wave % 4 * 16 + lane % 16;
+  const u32 turns = (inner + kElems - 1) / kElems, first = (u32)((u64)turns * part / parts), end = (u32)((u64)turns * (part + 1) / parts);
   f32x4 acc[RT];
 #pragma unroll
   for (int j = 0; j < RT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const u32 o = o0 + lane % 16;
-  for (u32 k0 = wave * 64; k0 < inner; k0 += kFewWaves * 64 * (kAhead / 2)) {
-    Vec8<T> wv[kAhead], xv[kAhead][RT];
+  for (u32 n = first; n < end; ++n) {
+    Vec8<T> wv[kSteps], xv[kLoads];
+#pragma unroll
+    for (u32 i = 0; i < kLoads; ++i)
+      xv[i] = load_tile(x, ldx, (i * kFewWaves + wave) * kRows + lane / kLanes, rows, n * kElems + lane % kLanes * 8, inner);
+#pragma unroll
+    for (u32 s = 0; s < kSteps; ++s) wv[s] = load_tile(w, ldw, o, outer, n * kElems + (wave / 4 * kSteps + s) * 32 + lane / 16 * 8, inner);
+    if (n != first) __syncthreads();
+#pragma unroll
+    for (u32 i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (u32 e = 0; e < kPieces; ++e)
+        __builtin_memcpy(__builtin_assume_aligned(few_piece(lx, (i * kFewWaves + wave) * kRows + lane / kLanes, lane % kLanes, e), 16),
+                         &xv[i].v[e * (16 / sizeof(T))], 16);
+    __syncthreads();
+#pragma unroll
+    for (u32 s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        Vec8<T> f;
+#pragma unroll
+        for (u32 e = 0; e < kPieces; ++e)
+          __builtin_memcpy(&f.v[e * (16 / sizeof(T))],
+                           __builtin_assume_aligned(few_piece(lx, j * 16 + lane % 16, (wave / 4 * kSteps + s) * 4 + lane / 16, e), 16), 16);
+        acc[j] = mma32(wv[s], f, acc[j]);
+      }
+  }
+  __syncthreads();
+  if (wave >= 4) {
+#pragma unroll
+    for (int j = 0; j < RT; ++j) half[((wave - 4) * RT + j) * kWave + lane] = acc[j];
+  }
+  __syncthreads();
+  if (wave >= 4) return;
+  const u32 o4 = tile * 64 + wave * 16 + lane / 16 * 4;
+#pragma unroll
+  for (int j = 0; j < RT; ++j) {
+    const u32 t = j * 16 + lane % 16;
+    if (t >= rows) continue;
+    const f32x4 s = acc[j] + half[(wave * RT + j) * kWave + lane];
+    float* const to = sums + ((size_t)part * rows + t) * outer + o4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (o4 + e < outer) to[e] = s[e];
+  }
+}
+
+template <class T, int RT, int ZT>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, size_t f_ld,
+                                                           const float* scale, const int* index, u32 rows, u32 inner, u32 outer, u32 rank,
+                                                           u32 parties, Drop d, u32 parts, u32 z_parts, u32 z_ld, float* sums, float* z,
+                                                           u32* status) {
+  __shared__ __align__(16) char lds[RT * 16 * kFewBytes];  // tiles of x, then halves of sums; or parts of z
+  const u32 products = (outer + 63) / 64 * parts;
+  if (blockIdx.x < products) {
+    few_product<T, RT>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
+    return;
+  }
+  float(*const lz)[ZT * 16] = (float(*)[ZT * 16])lds;
+  constexpr int kAhead = ZT == 1 ? 4 : 2;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  const u32 t = (blockIdx.x - products) / z_parts, part = (blockIdx.x - products) % z_parts;
+  const int raw = index[t], a = party_of(index, t, parties);
+  if (status && part == 0 && threadIdx.x == 0 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
+  float* const to = z + ((size_t)part * rows + t) * z_ld;
+  if (a < 0) {
+    if (threadIdx.x < z_ld) to[threadIdx.x] = 0.0f;
+    return;
+  }
+  const T* const fa = f + (size_t)a * rank * f_ld;
+  const u32 steps = (inner + 31) / 32, first = (u32)((u64)steps * part / z_parts), end = (u32)((u64)steps * (part + 1) / z_parts);
+  f32x4 acc[ZT];
+#pragma unroll
+  for (int i = 0; i < ZT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (u32 s0 = first + wave * kAhead; s0 < end; s0 += kFewWaves * kAhead) {
+    Vec8<T> xv[kAhead], fv[kAhead][ZT];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const u32 k = k0 + u / 2 * (kFewWaves * 64) + u % 2 * 32 + lane / 16 * 8;
-      wv[u] = load_tile(w, ldw, o, outer, k, inner);
+      const u32 k = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
+      xv[u] = load_tile(x, ldx, t, rows, k, inner);
 #pragma unroll
-      for (int j = 0; j < RT; ++j) xv[u][j] = load_tile(x, ldx, t0 + j * 16 + lane % 16, rows, k, inner);
+      for (int i = 0; i < ZT; ++i) fv[u][i] = load_tile(fa, f_ld, i * 16 + lane % 16, rank, k, inner);
     }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
+    for (int u = 0; u < kAhead; ++u) {
+      if (d.threshold) apply_drop(xv[u], d, t, (s0 + u) * 32 + lane / 16 * 8);
 #pragma unroll
-      for (int j = 0; j < RT; ++j) acc[j] = mma32(wv[u], xv[u][j], acc[j]);
+      for (int i = 0; i < ZT; ++i) acc[i] = mma32(fv[u][i], xv[u], acc[i]);
+    }
   }
+  // all sixteen rows of the second operand were the same one: its first column has the sums
+  if (lane % 16 == 0) {
 #pragma unroll
-  for (int j = 0; j < RT; ++j)
+    for (int i = 0; i < ZT; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[wave][j * 16 + lane % 16][lane / 16 * 4 + e] = acc[j][e];
-  constexpr int kOwn = RT * 256 / kThreadsFew > 0 ? RT * 256 / kThreadsFew : 1;
-  float low[kOwn];
-#pragma unroll
-  for (int q = 0; q < kOwn; ++q) low[q] = 0.0f;
-  for (u32 r0 = 0; r0 < rank; r0 += 16) {
-    for (u32 i = threadIdx.x; i < RT * 256; i += kThreadsFew) {
-      const u32 t = t0 + i / 16, r = r0 + i % 16;
-      float s = 0.0f;
-      if (t < rows && r < rank) {
-        for (u32 p = 0; p < parts; ++p) s += z[((size_t)p * rows + t) * z_ld + r];
-        if (h && o0 == 0) h[(size_t)t * rank + r] = s;
-      }
-      zl[i] = s;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const u32 i = threadIdx.x + q * kThreadsFew, t = t0 + i / 16, oo = o0 + i % 16;
-      const int a = i < RT * 256 && t < rows && oo < outer ? party_of(index, t, parties) : -1;
-      if (a >= 0) {
-        const T* const fr = f + ((size_t)a * outer + oo) * f_ld + r0;
-        const u32 n = rank - r0 < 16 ? rank - r0 : 16;
-        const Vec8<T> f0 = n >= 8 ? load_wide(fr) : load_some(fr, (int)n), f1 = n <= 8 ? Vec8<T>{} : n == 16 ? load_wide(fr + 8) : load_some(fr + 8, (int)n - 8);
-#pragma unroll
-        for (u32 r = 0; r < 16; ++r)
-          if (r < n) low[q] += zl[i / 16 * 16 + r] * (float)(r < 8 ? f0.v[r & 7] : f1.v[r & 7]);
-      }
-    }
-    __syncthreads();
+      for (int e = 0; e < 4; ++e) lz[wave][i * 16 + lane / 16 * 4 + e] = acc[i][e];
   }
+  __syncthreads();
+  const u32 r = threadIdx.x;
+  if (r >= z_ld) return;
+  float s = 0.0f;
 #pragma unroll
-  for (int q = 0; q < kOwn; ++q) {
-    const u32 i = threadIdx.x + q * kThreadsFew, t = t0 + i / 16, oo = o0 + i % 16;
-    if (i >= RT * 256 || t >= rows || oo >= outer) continue;
-    float s = low[q];
+  for (int v = 0; v < kFewWaves; ++v) s += r < ZT * 16 ? lz[v][r] : 0.0f;
+  to[r] = r < rank ? s * scale[a] * (d.threshold ? d.scale : 1.0f) : 0.0f;
+}
+
+// A block takes 256 outputs of a row, a lane one. Its z is written to `z_out` (z_ld places) or `h` (rank) by the first of the row.
+template <class T, bool DROP>
+__global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const float* z, const T* f, u32 f_ld, const int* index, u32 rows, u32 outer,
+                                                       u32 parties, u32 rank, Drop d, u32 parts, u32 z_parts, u32 z_ld, T* y, size_t ldy,
+                                                       float* z_out, float* h) {
+  __shared__ float zl[HAFLO_ADAPTER_MAX_RANK];
+  const u32 blocks = (outer + kThreads - 1) / kThreads, t = blockIdx.x / blocks, o = blockIdx.x % blocks * kThreads + threadIdx.x;
+  float m = 0.0f;
+  if (o < outer && y)
+#pragma unroll 4
+    for (u32 p = 0; p < parts; ++p) m += sums[((size_t)p * rows + t) * outer + o];
+  if (threadIdx.x < z_ld) {
+    float s = 0.0f;
+    for (u32 p = 0; p < z_parts; ++p) s += z[((size_t)p * rows + t) * z_ld + threadIdx.x];
+    zl[threadIdx.x] = s;
+    if (blockIdx.x % blocks == 0) {
+      if (z_out) z_out[(size_t)t * z_ld + threadIdx.x] = s;
+      if (h && threadIdx.x < rank) h[(size_t)t * rank + threadIdx.x] = s;
+    }
+  }
+  __syncthreads();
+  if (o >= outer || !y) return;
+  const int a = party_of(index, t, parties);
+  if (a >= 0) {
+    const T* const fr = f + ((size_t)a * outer + o) * f_ld;
+    float low = 0.0f;
+    for (u32 r0 = 0; r0 < rank; r0 += 8) {
+      const Vec8<T> v = r0 + 8 <= rank ? load_wide(fr + r0) : load_some(fr + r0, (int)(rank - r0));
+#pragma unroll
+      for (u32 r = 0; r < 8; ++r)
+        if (r0 + r < rank) low += zl[r0 + r] * (float)v.v[r];
+    }
     if (DROP) {
-      const u32x4 draws = philox(d, oo >> 3, t);
-      s = (draws[oo >> 1 & 3] >> (16 * (oo & 1)) & 0xFFFFu) >= d.threshold ? s * d.scale : 0.0f;
+      const u32x4 draws = philox(d, o >> 3, t);
+      const u32 word = o & 4 ? (o & 2 ? draws[3] : draws[2]) : (o & 2 ? draws[1] : draws[0]);
+      low = (word >> (16 * (o & 1)) & 0xFFFFu) >= d.threshold ? low * d.scale : 0.0f;
     }
-    float m = 0.0f;
-#pragma unroll
-    for (int v = 0; v < kFewWaves; ++v) m += sum[v][i / 16][i % 16];
-    y[(size_t)t * ldy + oo] = (T)(m + s);
+    m += low;
   }
+  y[(size_t)t * ldy + o] = (T)m;
 }
 
 // rows of one chunk of a party's list: as many as leave some 512 blocks of k_grad
@@ -884,18 +975,23 @@ bool adapter_sizes(int type, const Sizes& s) {
          s.outer <= kMostCount - 512 && s.parties >= 1 && s.parties <= HAFLO_ADAPTER_MAX_PARTIES && s.rank >= 1 &&
          s.rank <= HAFLO_ADAPTER_MAX_RANK;
 }
-constexpr size_t kFewRows = 64;  // up to here k_project_few
+constexpr size_t kFewRows = 64;  // up to here k_few
 // parts of k_shrink's reduction: enough blocks to fill the chip, at least 512 columns each
 u32 shrink_parts(size_t rows, size_t k) {
   if (rows == 0) return 1;
   const size_t tiles = rows <= kFewRows ? rows : ceil_div(rows, 16), want = tiles < 512 ? ceil_div(512, tiles) : 1, most = ceil_div(k, 512);
   return (u32)(want < most ? want : most);
 }
+// parts of k_few's reduction: two blocks of it to a compute unit, at least 1024 bytes of a row each
+u32 few_parts(int type, size_t k, size_t n) {
+  const size_t want = ceil_div(512, ceil_div(n, 64)), most = ceil_div(k * type_size(type), kFewBytes);
+  return (u32)(want < most ? want : most);
+}
 size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * (128 / type_size(type)); }
 size_t whole_ranks(size_t rank) { return ceil_div(rank, kRanks) * kRanks; }
 u32 grad_rows(const Sizes& s) { return chunk_rows(s.rows, s.inner + s.outer, s.rank); }
 struct Plan {
-  size_t z_parts, z, x, w, low, f, begin, chunk_begin, chunk, order, sums_a, sums_b, total;
+  size_t z_parts, few_sums, z, x, w, low, f, begin, chunk_begin, chunk, order, sums_a, sums_b, total;
   size_t chunks;  // at most
 };
 Plan adapter_plan(int type, bool backward, const Sizes& s) {
@@ -909,6 +1005,7 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
   const size_t e = type_size(type), ranks = whole_ranks(s.rank);
   const size_t k = backward ? s.outer : s.inner, n = backward ? s.inner : s.outer, kp = padded(type, k);  // the product's sizes
   p.z_parts = take(shrink_parts(s.rows, k) * s.rows * ranks * 4);
+  if (s.rows <= kFewRows) p.few_sums = take(few_parts(type, k, n) * s.rows * n * 4);
   p.z = take(s.rows * ranks * 4);
   p.x = take(s.rows * kp * e);
   p.w = take(n * kp * e);
@@ -978,60 +1075,60 @@ struct Product {
   u32* status;
   hipStream_t st;
 
-  bool few() const { return s.rows <= kFewRows; }
   u32 ranks() const { return (u32)whole_ranks(s.rank); }
   size_t padded_inner() const { return ceil_div(s.inner, step_elems<T>()) * step_elems<T>(); }
-  const u32* order() const { return few() ? nullptr : (const u32*)(ws + plan.order); }
+  const u32* order() const { return (const u32*)(ws + plan.order); }
   float* z_parts() const { return (float*)(ws + plan.z_parts); }
   float* z() const { return (float*)(ws + plan.z); }
 
-  // z, or with few rows its parts; dense as `h` too unless that is null
+  // z, dense as `h` too unless that is null
   void shrink(float* h) const {
     const u32 parts = shrink_parts(s.rows, s.inner);
-    const dim3 grid((unsigned)((few() ? s.rows : ceil_div(s.rows, 16)) * parts)), block(kShrinkWaves * kWave);
-    float* const to = few() || parts > 1 ? z_parts() : z();
+    const dim3 grid((unsigned)(ceil_div(s.rows, 16) * parts)), block(kShrinkWaves * kWave);
+    float* const to = parts > 1 ? z_parts() : z();
     float* const h_now = parts > 1 ? nullptr : h;
-#define HAFLO_LOCAL_RUN(ROWS, RT)                                                                                                            \
-  hipLaunchKernelGGL((k_shrink<T, ROWS, RT>), grid, block, 0, st, x.p, x.ld, low.p, low.ld, scale, index, order(), (u32)s.rows, (u32)s.inner, \
+#define HAFLO_LOCAL_RUN(RT)                                                                                                           \
+  hipLaunchKernelGGL((k_shrink<T, RT>), grid, block, 0, st, x.p, x.ld, low.p, low.ld, scale, index, order(), (u32)s.rows, (u32)s.inner, \
                      (u32)s.rank, (u32)s.parties, before, parts, ranks(), to, h_now, status)
-#define HAFLO_LOCAL_RANK(ROWS)                        \
-  do {                                                \
-    if (s.rank <= 16) HAFLO_LOCAL_RUN(ROWS, 1);       \
-    else if (s.rank <= 64) HAFLO_LOCAL_RUN(ROWS, 4);  \
-    else HAFLO_LOCAL_RUN(ROWS, 8);                    \
-  } while (0)
-    if (few()) HAFLO_LOCAL_RANK(1);
-    else HAFLO_LOCAL_RANK(16);
-#undef HAFLO_LOCAL_RANK
+    if (s.rank <= 16) HAFLO_LOCAL_RUN(1);
+    else if (s.rank <= 64) HAFLO_LOCAL_RUN(4);
+    else HAFLO_LOCAL_RUN(8);
 #undef HAFLO_LOCAL_RUN
-    if (!few() && parts > 1) join(h);
-  }
-  void join(float* h) const {
     const size_t count = s.rows * ranks();
-    hipLaunchKernelGGL(k_join, dim3((unsigned)ceil_div(count, kThreads)), dim3(kThreads), 0, st, (const float*)z_parts(),
-                       shrink_parts(s.rows, s.inner), count, ranks(), (u32)s.rank, z(), h);
+    if (parts > 1)
+      hipLaunchKernelGGL(k_join, dim3((unsigned)ceil_div(count, kThreads)), dim3(kThreads), 0, st, (const float*)z_parts(), parts, count, ranks(),
+                         (u32)s.rank, z(), h);
   }
 
-  // `h`: where few rows' z goes that has been in parts, or null
-  void project(float* h, T* y, size_t ldy) const {
-    if (few()) {
-      const u32 parts = shrink_parts(s.rows, s.inner);
-#define HAFLO_LOCAL_RUN(RT, DROP)                                                                                                        \
-  hipLaunchKernelGGL((k_project_few<T, RT, DROP>), dim3((unsigned)(ceil_div(s.rows, RT * 16) * ceil_div(s.outer, 16))),                  \
-                     dim3(kFewWaves * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (u32)f.ld, (const float*)z_parts(), ranks(), parts, index, \
-                     (u32)s.rows, (u32)s.inner, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, y, ldy, parts > 1 ? h : nullptr)
-#define HAFLO_LOCAL_FEW(DROP)                        \
-  do {                                               \
-    if (s.rows <= 16) HAFLO_LOCAL_RUN(1, DROP);      \
-    else if (s.rows <= 32) HAFLO_LOCAL_RUN(2, DROP); \
-    else HAFLO_LOCAL_RUN(4, DROP);                   \
+  // Few rows: y, unless it is null, and z; dense as `h` too unless that is null.
+  void few_rows(float* h, T* y, size_t ldy) const {
+    const u32 zp = shrink_parts(s.rows, s.inner), parts = few_parts(sizeof(T) == 4 ? HAFLO_F32 : HAFLO_F16, s.inner, s.outer);
+    const dim3 grid((unsigned)(y ? ceil_div(s.outer, 64) * parts + s.rows * zp : s.rows * zp)), block(kFewWaves * kWave);
+    float* const sums = (float*)(ws + plan.few_sums);
+#define HAFLO_LOCAL_RUN(RT, ZT)                                                                                                            \
+  hipLaunchKernelGGL((k_few<T, RT, ZT>), grid, block, 0, st, x.p, x.ld, w.p, w.ld, low.p, low.ld, scale, index, (u32)s.rows, (u32)s.inner, \
+                     (u32)(y ? s.outer : 0), (u32)s.rank, (u32)s.parties, before, parts, zp, ranks(), sums, z_parts(), status)
+#define HAFLO_LOCAL_RANK(RT)                       \
+  do {                                             \
+    if (s.rank <= 16) HAFLO_LOCAL_RUN(RT, 1);      \
+    else if (s.rank <= 64) HAFLO_LOCAL_RUN(RT, 4); \
+    else HAFLO_LOCAL_RUN(RT, 8);                   \
   } while (0)
-      if (after.threshold) HAFLO_LOCAL_FEW(true);
-      else HAFLO_LOCAL_FEW(false);
-#undef HAFLO_LOCAL_FEW
+    if (s.rows <= 16) HAFLO_LOCAL_RANK(1);
+    else if (s.rows <= 32) HAFLO_LOCAL_RANK(2);
+    else HAFLO_LOCAL_RANK(4);
+#undef HAFLO_LOCAL_RANK
 #undef HAFLO_LOCAL_RUN
-      return;
-    }
+    const dim3 join((unsigned)(s.rows * ceil_div(s.outer, kThreads)));
+#define HAFLO_LOCAL_RUN(DROP)                                                                                                                \
+  hipLaunchKernelGGL((k_few_join<T, DROP>), join, dim3(kThreads), 0, st, (const float*)sums, (const float*)z_parts(), f.p, (u32)f.ld, index, \
+                     (u32)s.rows, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, parts, zp, ranks(), y, ldy, z(), h)
+    if (after.threshold) HAFLO_LOCAL_RUN(true);
+    else HAFLO_LOCAL_RUN(false);
+#undef HAFLO_LOCAL_RUN
+  }
+
+  void project(T* y, size_t ldy) const {
     const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
     const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
 #define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP, FAR)                                                                                        \
@@ -1105,8 +1202,12 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
       f.f = lay.wide(d_b, rank, parties * outer, rank, kRanks, ws + plan.f);
     }
     lay.launch(st);
-    f.shrink(d_h);
-    f.project(d_h, (T*)d_y, ldy);
+    if (many) {
+      f.shrink(d_h);
+      f.project((T*)d_y, ldy);
+    } else {
+      f.few_rows(d_h, (T*)d_y, ldy);
+    }
   });
   return launched();
 }
@@ -1145,9 +1246,12 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
         f.f = lay.transposed(d_a, inner, rank * inner, rank, inner, parties, ws + plan.f, ranks);
       }
       lay.launch(st);
-      f.shrink(nullptr);
-      if (!many) f.join(nullptr);  // k_grad reads it whole
-      if (d_dx) f.project(nullptr, (T*)d_dx, lddx);
+      if (many) {
+        f.shrink(nullptr);
+        if (d_dx) f.project((T*)d_dx, lddx);
+      } else {
+        f.few_rows(nullptr, (T*)d_dx, lddx);
+      }
     } else {
       lay.launch(st);
     }
