@@ -16,7 +16,6 @@ using namespace haflo::local;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kShrinkWaves = 4;
 
 template <class T>
 constexpr int step_elems() {  // of the reduction in one step of k_project: 128 bytes of a row
@@ -28,28 +27,71 @@ __device__ __forceinline__ int party_of(const int* index, u32 t, u32 parties) {
   return (u32)a < parties ? a : -1;
 }
 
-// eight elements at (row, k) of a matrix, zeros past its edges
+// a place below `count`, the last one for those behind it
+__device__ __forceinline__ u32 lowest(u32 i, u32 count) { return i < count ? i : count - 1; }
+
+// Eight elements at column k of a row of `cols`, in two steps: a load without a branch, as the compiler waits for a load at the
+// next branch around one, and where the elements pass the row's end, so the row's last eight were loaded, their moving to
+// their places, with zeros behind them. Rows of less than eight are loaded element by element.
 template <class T>
-__device__ __forceinline__ Vec8<T> load_tile(const T* m, size_t ld, u32 row, u32 rows, u32 k, u32 cols) {
-  if (row >= rows || k >= cols) return Vec8<T>{};
-  const T* p = m + (size_t)row * ld + k;
-  return k + 8 <= cols ? load_wide(p) : load_some(p, (int)(cols - k));
+__device__ __forceinline__ Vec8<T> load_row(const T* row, u32 k, u32 cols) {
+  return load_wide(row + (k + 8 <= cols ? k : cols - 8));
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> load_short(const T* row, u32 k, u32 cols) {
+  return load_some(row, k == 0 ? (int)cols : 0);
+}
+template <class T>
+__device__ __forceinline__ void settle(Vec8<T>& v, u32 k, u32 cols) {
+  if (k + 8 <= cols || cols < 8) return;
+  const u32 by = k + 8 - cols;
+  const Vec8<T> was = v;
+  v = Vec8<T>{};
+#pragma unroll
+  for (u32 n = 1; n < 8; ++n)
+    if (by == n) {
+#pragma unroll
+      for (u32 j = 0; j + n < 8; ++j) v.set(j, was.get(j + n));
+    }
 }
 template <class T>
 __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u32 k) {
   const u32x4 draws = philox(d, k >> 3, row);
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (!kept(d, draws, j)) v.v[j] = (T)0.0f;
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 4) v.w[j >> 2][j & 3] = kept(d, draws, j) ? v.w[j >> 2][j & 3] : 0u;
+    else v.w[0][j >> 1] &= kept(d, draws, j) ? 0xFFFFFFFFu : j & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+  }
+}
+// Rows that several wavefronts multiply go through LDS, 1024 bytes of each at a time.
+constexpr int kRowBytes = 1024;
+// eight elements, the q-th of a row in LDS; pieces of 16 bytes of sixteen rows lie on different banks
+template <class T>
+__device__ __forceinline__ T* row_piece(T* tile, u32 row, u32 q, u32 e) {
+  constexpr u32 kPieces = sizeof(T) / 2;  // of eight elements
+  return tile + row * (kRowBytes / sizeof(T)) + ((q * kPieces + e) ^ (row & 15)) * (16 / sizeof(T));
+}
+template <class T>
+__device__ __forceinline__ void put_row(T* tile, u32 row, u32 q, const Vec8<T>& v) {
+#pragma unroll
+  for (u32 e = 0; e < sizeof(T) / 2; ++e) *(u32x4*)row_piece(tile, row, q, e) = v.w[e];
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> get_row(T* tile, u32 row, u32 q) {
+  Vec8<T> v;
+#pragma unroll
+  for (u32 e = 0; e < sizeof(T) / 2; ++e) v.w[e] = *(const u32x4*)row_piece(tile, row, q, e);
+  return v;
 }
 
-// z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without. A block takes ROWS rows (of `order`, or one
-// row as it lies) and one part of the reduction, its wavefronts
-// 256 bytes of every row in turn; once for every party among the rows.
+// z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without.
+// A block takes sixteen rows of `order` and one part of the reduction, its wavefronts some steps in turn each; once for every
+// party among the rows. Rows behind the last, of x and of F, are the last one again: what they give is left aside.
+constexpr int kShrinkWaves = 4;
 template <class T, int RT>
 __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
-                                                     const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
-                                                     u32 z_ld, float* z, float* h, u32* status) {
+                                                                 const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
+                                                                 u32 z_ld, float* z, float* h, u32* status) {
   constexpr int kAhead = RT == 1 ? 4 : 2;  // steps whose operands are on their way together
   __shared__ float sum[kShrinkWaves][RT][16][17];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
@@ -67,6 +109,10 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   const u32 out_i = lane / 16 * 4 + wave;
   const u32 out_t = row_at(out_i);
   const int out_a = out_t < rows ? party_of(index, out_t, parties) : -1;
+  const T* const x_row = x + (size_t)lowest(mine, rows) * ldx;
+  size_t f_at[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) f_at[i] = (size_t)lowest(i * 16 + lane % 16, rank) * f_ld;
   u64 left = __builtin_amdgcn_ballot_w64(a >= 0) & 0xFFFF;
   while (left) {
     const int who = __builtin_amdgcn_readlane(a, __builtin_ctzll(left));
@@ -77,15 +123,29 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
     for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     for (u32 s0 = first + wave * kAhead; s0 < end; s0 += kShrinkWaves * kAhead) {
       Vec8<T> xv[kAhead], fv[kAhead][RT];
+      u32 k[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const u32 k = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
-        xv[u] = load_tile(x, ldx, mine, rows, k, inner);
+      for (int u = 0; u < kAhead; ++u) k[u] = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
+      if (inner >= 8) {
 #pragma unroll
-        for (int i = 0; i < RT; ++i) fv[u][i] = load_tile(fa, f_ld, i * 16 + lane % 16, rank, k, inner);
+        for (int u = 0; u < kAhead; ++u) {
+          xv[u] = load_row(x_row, k[u], inner);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) fv[u][i] = load_row(fa + f_at[i], k[u], inner);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          xv[u] = load_short(x_row, k[u], inner);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) fv[u][i] = load_short(fa + f_at[i], k[u], inner);
+        }
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
+        settle(xv[u], k[u], inner);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) settle(fv[u][i], k[u], inner);
         if (d.threshold) apply_drop(xv[u], d, mine, (s0 + u) * 32 + lane / 16 * 8);
 #pragma unroll
         for (int i = 0; i < RT; ++i) acc[i] = mma32(fv[u][i], xv[u], acc[i]);
@@ -111,8 +171,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   if (out_t < rows) {
     const float by = out_a < 0 ? 0.0f : scale[out_a] * (d.threshold ? d.scale : 1.0f);
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
-    {
+    for (int i = 0; i < RT; ++i) {
       const u32 r = i * 16 + lane % 16;
       if (r < z_ld) z[((size_t)part * rows + out_t) * z_ld + r] = r < rank ? own[i] * by : 0.0f;
       if (h && r < rank) h[(size_t)out_t * rank + r] = own[i] * by;
@@ -153,9 +212,9 @@ struct LowPart<__bf16> {
   static __device__ __forceinline__ Frag of_z(const float* z) {
     const u32 g = lane_id() / 16;
     const Vec8<float> v = load_wide(z + (g & 1) * 8);
-    Frag f;
+    Frag f = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = piece(v.v[e], g >= 2);
+    for (int e = 0; e < 8; ++e) f.set(e, piece(v.get(e), g >= 2));
     return f;
   }
   static __device__ __forceinline__ Frag of_f(const __bf16* w) { return load_wide(w + (lane_id() / 16 & 1) * 8); }
@@ -167,16 +226,16 @@ struct LowPart<_Float16> {
   using Frag = Vec8<__bf16>;
   static __device__ __forceinline__ Frag of_z(const float* z) {
     const Vec8<float> v = load_wide(z);
-    Frag f;
+    Frag f = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = piece(v.v[e], lane_id() / 16 & 1);
+    for (int e = 0; e < 8; ++e) f.set(e, piece(v.get(e), lane_id() / 16 & 1));
     return f;
   }
   static __device__ __forceinline__ Frag of_f(const _Float16* w) {
     const Vec8<_Float16> v = load_wide(w);
-    Frag f;
+    Frag f = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = piece((float)v.v[e], lane_id() / 16 >= 2);
+    for (int e = 0; e < 8; ++e) f.set(e, piece((float)v.get(e), lane_id() / 16 >= 2));
     return f;
   }
   static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) { return mma32(f, z, acc); }
@@ -242,7 +301,7 @@ __device__ __forceinline__ Vec8<T> load_frag(const T* tile, u32 row, u32 k) {  /
   Vec8<T> v;
 #pragma unroll
   for (u32 i = 0; i < 8 / kPer; ++i)
-    __builtin_memcpy(&v.v[i * kPer], __builtin_assume_aligned(tile + row * step_elems<T>() + place_of(row, k / kPer + i) * kPer, 16), 16);
+    v.w[i] = *(const u32x4*)(tile + row * step_elems<T>() + place_of(row, k / kPer + i) * kPer);
   return v;
 }
 
@@ -481,7 +540,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
     for (u32 n = 0; n < RT * 16 / kRows; ++n) {
       const u32 r = n * kRows + lane / kPieces, piece = lane % kPieces;
       Vec8<T> v;
-      __builtin_memcpy(&v, __builtin_assume_aligned(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8, 16), 16);
+      v.w[0] = *(const u32x4*)(own + r * (OT * 16) + (piece ^ (r >> kShift & (kPieces - 1))) * 8);
       const u32 row = lane_read(t[n * kRows / 16], (int)(r % 16)), o = o0 + out0 + piece * 8;
       if (row >= rows || o >= outer) continue;
       T* const to = y + (size_t)row * ldy + o;
@@ -513,54 +572,45 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 
 // The same for few rows, in two launches. k_few reads W once: a block takes 64 outputs and one part of the reduction, 1024 bytes of
 // every row at a time, its wavefronts four sixteens of outputs in two halves of that; further blocks form the parts of z = h or
-// g for one row each, as k_shrink does. k_few_join adds the parts, and the adapters' part to them. x goes through LDS: what a
-// matrix instruction takes of it is 64 bytes of each of sixteen rows, and such a load costs some 70 cycles of the unit that
-// addresses memory where 1024 bytes in a row cost 16 (64 rows: 25 us when every wavefront loaded its operands itself).
+// g for one row each, as k_shrink does. k_few_join adds the parts, and the adapters' part to them. What bounds it is the
+// reading of W: 64 rows of 4096 to 4096 in bfloat16 take 16 us and 6 for the joining, one row 8.6 and 4.4.
 constexpr int kFewWaves = 8;
-constexpr int kFewBytes = 1024;
-// eight elements, the q-th of a row in LDS; pieces of 16 bytes of sixteen rows lie on different banks
-template <class T>
-__device__ __forceinline__ T* few_piece(T* tile, u32 row, u32 q, u32 e) {
-  constexpr u32 kPieces = sizeof(T) / 2;  // of eight elements
-  return tile + row * (kFewBytes / sizeof(T)) + ((q * kPieces + e) ^ (row & 15)) * (16 / sizeof(T));
-}
-template <class T, int RT>
+template <class T, int RT, bool SHORT>
 __device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, size_t ldw, u32 rows, u32 inner, u32 outer, u32 tile, u32 part,
                                             u32 parts, float* sums, T* lx, f32x4* half) {
-  constexpr u32 kElems = kFewBytes / sizeof(T), kSteps = kElems / 32 / 2, kLanes = kElems / 8, kRows = kWave / kLanes;  // rows of a load
-  constexpr u32 kLoads = RT * 16 / (kFewWaves * kRows), kPieces = sizeof(T) / 2;
+  constexpr u32 kElems = kRowBytes / sizeof(T), kSteps = kElems / 32 / 2, kLanes = kElems / 8, kRows = kWave / kLanes;  // rows of a load
+  constexpr u32 kLoads = RT * 16 / (kFewWaves * kRows);
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   const u32 o = tile * 64 + wave % 4 * 16 + lane % 16;
   const u32 turns = (inner + kElems - 1) / kElems, first = (u32)((u64)turns * part / parts), end = (u32)((u64)turns * (part + 1) / parts);
+  size_t x_at[kLoads];
+#pragma unroll
+  for (u32 i = 0; i < kLoads; ++i) x_at[i] = (size_t)lowest((i * kFewWaves + wave) * kRows + lane / kLanes, rows) * ldx;
+  const T* const w_row = w + (size_t)lowest(o, outer) * ldw;
   f32x4 acc[RT];
 #pragma unroll
   for (int j = 0; j < RT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   for (u32 n = first; n < end; ++n) {
     Vec8<T> wv[kSteps], xv[kLoads];
+    const u32 kx = n * kElems + lane % kLanes * 8, kw = n * kElems + wave / 4 * kSteps * 32 + lane / 16 * 8;
+    const auto load = [&](const T* row, u32 k) { return SHORT ? load_short(row, k, inner) : load_row(row, k, inner); };
 #pragma unroll
-    for (u32 i = 0; i < kLoads; ++i)
-      xv[i] = load_tile(x, ldx, (i * kFewWaves + wave) * kRows + lane / kLanes, rows, n * kElems + lane % kLanes * 8, inner);
+    for (u32 i = 0; i < kLoads; ++i) xv[i] = load(x + x_at[i], kx);
 #pragma unroll
-    for (u32 s = 0; s < kSteps; ++s) wv[s] = load_tile(w, ldw, o, outer, n * kElems + (wave / 4 * kSteps + s) * 32 + lane / 16 * 8, inner);
+    for (u32 s = 0; s < kSteps; ++s) wv[s] = load(w_row, kw + s * 32);
     if (n != first) __syncthreads();
 #pragma unroll
-    for (u32 i = 0; i < kLoads; ++i)
-#pragma unroll
-      for (u32 e = 0; e < kPieces; ++e)
-        __builtin_memcpy(__builtin_assume_aligned(few_piece(lx, (i * kFewWaves + wave) * kRows + lane / kLanes, lane % kLanes, e), 16),
-                         &xv[i].v[e * (16 / sizeof(T))], 16);
+    for (u32 i = 0; i < kLoads; ++i) {
+      settle(xv[i], kx, inner);
+      put_row(lx, (i * kFewWaves + wave) * kRows + lane / kLanes, lane % kLanes, xv[i]);
+    }
     __syncthreads();
 #pragma unroll
-    for (u32 s = 0; s < kSteps; ++s)
+    for (u32 s = 0; s < kSteps; ++s) {
+      settle(wv[s], kw + s * 32, inner);
 #pragma unroll
-      for (int j = 0; j < RT; ++j) {
-        Vec8<T> f;
-#pragma unroll
-        for (u32 e = 0; e < kPieces; ++e)
-          __builtin_memcpy(&f.v[e * (16 / sizeof(T))],
-                           __builtin_assume_aligned(few_piece(lx, j * 16 + lane % 16, (wave / 4 * kSteps + s) * 4 + lane / 16, e), 16), 16);
-        acc[j] = mma32(wv[s], f, acc[j]);
-      }
+      for (int j = 0; j < RT; ++j) acc[j] = mma32(wv[s], get_row(lx, j * 16 + lane % 16, (wave / 4 * kSteps + s) * 4 + lane / 16), acc[j]);
+    }
   }
   __syncthreads();
   if (wave >= 4) {
@@ -587,10 +637,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
                                                            const float* scale, const int* index, u32 rows, u32 inner, u32 outer, u32 rank,
                                                            u32 parties, Drop d, u32 parts, u32 z_parts, u32 z_ld, float* sums, float* z,
                                                            u32* status) {
-  __shared__ __align__(16) char lds[RT * 16 * kFewBytes];  // tiles of x, then halves of sums; or parts of z
+  __shared__ __align__(16) char lds[RT * 16 * kRowBytes];  // tiles of x, then halves of sums; or parts of z
   const u32 products = (outer + 63) / 64 * parts;
   if (blockIdx.x < products) {
-    few_product<T, RT>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
+    if (inner < 8) few_product<T, RT, true>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
+    else few_product<T, RT, false>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
     return;
   }
   float(*const lz)[ZT * 16] = (float(*)[ZT * 16])lds;
@@ -606,20 +657,37 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
   }
   const T* const fa = f + (size_t)a * rank * f_ld;
   const u32 steps = (inner + 31) / 32, first = (u32)((u64)steps * part / z_parts), end = (u32)((u64)steps * (part + 1) / z_parts);
+  size_t f_at[ZT];
+#pragma unroll
+  for (int i = 0; i < ZT; ++i) f_at[i] = (size_t)lowest(i * 16 + lane % 16, rank) * f_ld;
   f32x4 acc[ZT];
 #pragma unroll
   for (int i = 0; i < ZT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   for (u32 s0 = first + wave * kAhead; s0 < end; s0 += kFewWaves * kAhead) {
     Vec8<T> xv[kAhead], fv[kAhead][ZT];
+    u32 k[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const u32 k = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
-      xv[u] = load_tile(x, ldx, t, rows, k, inner);
+    for (int u = 0; u < kAhead; ++u) k[u] = s0 + u < end ? (s0 + u) * 32 + lane / 16 * 8 : inner;
+    if (inner >= 8) {
 #pragma unroll
-      for (int i = 0; i < ZT; ++i) fv[u][i] = load_tile(fa, f_ld, i * 16 + lane % 16, rank, k, inner);
+      for (int u = 0; u < kAhead; ++u) {
+        xv[u] = load_row(x + (size_t)t * ldx, k[u], inner);
+#pragma unroll
+        for (int i = 0; i < ZT; ++i) fv[u][i] = load_row(fa + f_at[i], k[u], inner);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        xv[u] = load_short(x + (size_t)t * ldx, k[u], inner);
+#pragma unroll
+        for (int i = 0; i < ZT; ++i) fv[u][i] = load_short(fa + f_at[i], k[u], inner);
+      }
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
+      settle(xv[u], k[u], inner);
+#pragma unroll
+      for (int i = 0; i < ZT; ++i) settle(fv[u][i], k[u], inner);
       if (d.threshold) apply_drop(xv[u], d, t, (s0 + u) * 32 + lane / 16 * 8);
 #pragma unroll
       for (int i = 0; i < ZT; ++i) acc[i] = mma32(fv[u][i], xv[u], acc[i]);
@@ -671,7 +739,7 @@ __global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const 
       const Vec8<T> v = r0 + 8 <= rank ? load_wide(fr + r0) : load_some(fr + r0, (int)(rank - r0));
 #pragma unroll
       for (u32 r = 0; r < 8; ++r)
-        if (r0 + r < rank) low += zl[r0 + r] * (float)v.v[r];
+        if (r0 + r < rank) low += zl[r0 + r] * (float)v.get(r);
     }
     if (DROP) {
       const u32x4 draws = philox(d, o >> 3, t);
@@ -718,45 +786,49 @@ struct Prepare {
 
 // `order` holds the rows of party 0 in ascending order, then those of party 1, ..., at last those without; begin[p] is where
 // p's start, begin[parties] where the last begin; chunk_begin[p] the first of p's chunks of chunk_rows rows; chunk[c] = p.
-// The block's wavefronts take a range of rows each, count them, and list them from where their counts say.
+// The block's wavefronts take a range of rows each, count them, and list them from where their counts say. One compute unit's
+// vector instructions bound it (16384 rows: 18 us, 3001 rows of more parties: 10); more blocks would cost another launch.
 __device__ void group_rows(const Group& g, u32* counts) {
   constexpr int kAhead = 8;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), waves = group_waves(g.parties);
   const u32 rows = g.rows, parties = g.parties;
   const int* const index = g.index;
-  const u32 bins = parties + 1;
+  const u32 bins = parties + 1, bits = 32 - (u32)__builtin_clz(parties);
   const u32 per = ((rows + waves - 1) / waves + kWave - 1) / kWave * kWave;
   const u32 first = wave < waves && (u64)wave * per < rows ? wave * per : rows, end = rows - first < per ? rows : first + per;
   for (u32 i = threadIdx.x; i < waves * bins; i += kPrepareThreads) counts[i] = 0;
   __syncthreads();
   int raw[kAhead];
+  u32 at[kAhead], first_of[kAhead], below[kAhead];
   u32 held = ~0u;  // where the rows that raw holds begin
   for (int pass = 0; pass < 2; ++pass) {
     for (u32 base = first; base < end; base += kAhead * kWave) {
       if (base != held) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const u32 t = base + i * kWave + lane;
-          raw[i] = t < end ? index[t] : -1;
-        }
+        for (int i = 0; i < kAhead; ++i) raw[i] = index[lowest(base + i * kWave + lane, end)];
         held = base;
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const u32 t = base + i * kWave + lane;
         const u32 a = (u32)raw[i] < parties ? (u32)raw[i] : parties;
-        if (pass == 0 && a == parties && raw[i] != -1 && g.status) atomicOr(g.status, HAFLO_ST_RANGE);
-        u64 left = __builtin_amdgcn_ballot_w64(t < end);
-        while (left) {
-          const int leader = __builtin_ctzll(left);
-          const u32 who = (u32)__builtin_amdgcn_readlane((int)a, leader);
-          const u64 same = __builtin_amdgcn_ballot_w64(a == who) & left;
-          left &= ~same;
-          u32 at = 0;
-          if ((int)lane == leader) at = atomicAdd(&counts[wave * bins + who], (u32)__builtin_popcountll(same));
-          at = (u32)__builtin_amdgcn_readlane((int)at, leader);
-          if (pass == 1 && (same >> lane & 1)) g.order[at + (u32)__builtin_popcountll(same & ((1ull << lane) - 1))] = t;
+        if (pass == 0 && t < end && a == parties && raw[i] != -1 && g.status) atomicOr(g.status, HAFLO_ST_RANGE);
+        u64 same = __builtin_amdgcn_ballot_w64(t < end);  // the lanes whose row has this one's party, bit by bit
+        for (u32 b = 0; b < bits; ++b) {
+          const u64 ones = __builtin_amdgcn_ballot_w64(a >> b & 1);
+          same &= a >> b & 1 ? ones : ~ones;
         }
+        // the first of them counts them; a wavefront's additions take place in their order, none waits for the one before
+        at[i] = 0;
+        first_of[i] = same ? (u32)__builtin_ctzll(same) : lane;
+        below[i] = (u32)__builtin_popcountll(same & ((1ull << lane) - 1));
+        if (t < end && first_of[i] == lane) at[i] = atomicAdd(&counts[wave * bins + a], (u32)__builtin_popcountll(same));
+      }
+      if (pass == 0) continue;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const u32 t = base + i * kWave + lane, from = lane_read(at[i], (int)first_of[i]);
+        if (t < end) g.order[from + below[i]] = t;
       }
     }
     __syncthreads();
@@ -779,12 +851,20 @@ __device__ void group_rows(const Group& g, u32* counts) {
         if (p < bins) {
           g.begin[p] = place;
           g.chunk_begin[p] = chunks + c_to - c;
-          for (u32 i = 0; i < c; ++i) g.chunk[chunks + c_to - c + i] = p;
           for (u32 w = 0; w < waves; ++w) {
             const u32 m = counts[w * bins + p];
             counts[w * bins + p] = place;
             place += m;
           }
+        }
+        const u32 c_from = chunks + c_to - c;
+        u64 many = __builtin_amdgcn_ballot_w64(c > 4);
+        if (c <= 4)
+          for (u32 i = 0; i < c; ++i) g.chunk[c_from + i] = p;
+        for (; many; many &= many - 1) {  // all lanes for a party of many
+          const int of = __builtin_ctzll(many);
+          const u32 base = (u32)__builtin_amdgcn_readlane((int)c_from, of), n_of = (u32)__builtin_amdgcn_readlane((int)c, of);
+          for (u32 i = lane; i < n_of; i += kWave) g.chunk[base + i] = p0 + of;
         }
         at += (u32)__builtin_amdgcn_readlane((int)to, kWave - 1);
         chunks += (u32)__builtin_amdgcn_readlane((int)c_to, kWave - 1);
@@ -814,7 +894,10 @@ __global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p) {
     const u64 at = (u64)block * kPrepareThreads + threadIdx.x;
     if (at >= (u64)job.rows * groups) return;
     const u32 r = (u32)(at / groups), c = (u32)(at - (u64)r * groups) * 8;
-    store_wide(job.out + (size_t)r * job.out_ld + c, load_some(job.in + (size_t)r * job.ld + c, c >= job.cols ? 0 : (int)(job.cols - c)));
+    const T* const row = job.in + (size_t)r * job.ld;
+    Vec8<T> v = job.cols < 8 ? load_short(row, c, job.cols) : load_row(row, c, job.cols);
+    settle(v, c, job.cols);
+    store_wide(job.out + (size_t)r * job.out_ld + c, v);
     return;
   }
   T(*const tile)[66] = (T(*)[66])lds;
@@ -822,9 +905,17 @@ __global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p) {
   const u32 which = block / tiles, at = block % tiles, r0 = at / tiles_c * 64, c0 = at % tiles_c * 64;
   const T* const in = job.in + which * job.in_step;
   T* const out = job.out + which * job.out_step;
-  for (u32 i = threadIdx.x; i < 64 * 64; i += kPrepareThreads) {
-    const u32 r = r0 + i / 64, c = c0 + i % 64;
-    tile[i / 64][i % 64] = r < job.rows && c < job.cols ? in[(size_t)r * job.ld + c] : (T)0.0f;
+  constexpr u32 kLoads = 64 * 64 / kPrepareThreads;
+  T v[kLoads];
+#pragma unroll
+  for (u32 n = 0; n < kLoads; ++n) {
+    const u32 i = n * kPrepareThreads + threadIdx.x;
+    v[n] = in[(size_t)lowest(r0 + i / 64, job.rows) * job.ld + lowest(c0 + i % 64, job.cols)];
+  }
+#pragma unroll
+  for (u32 n = 0; n < kLoads; ++n) {
+    const u32 i = n * kPrepareThreads + threadIdx.x;
+    tile[i / 64][i % 64] = r0 + i / 64 < job.rows ? v[n] : (T)0.0f;
   }
   __syncthreads();
   for (u32 i = threadIdx.x; i < 64 * 64; i += kPrepareThreads) {
@@ -884,19 +975,24 @@ __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const u32 i = mine + (n + u) * (kWaves * 4);
-      listed[u] = i < end ? list[i] : ~0u;
+      listed[u] = list[lowest(i, end)];
     }
   };
   const auto fetch = [&](u32 n) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) ahead[u].t = listed[u];
     look(n + kAhead);
+    if (cols >= 8) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) ahead[u].v = load_row(m + (size_t)ahead[u].t * ld, col, cols);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) ahead[u].v = load_short(m + (size_t)ahead[u].t * ld, col, cols);
+    }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const bool some = ahead[u].t != ~0u;
-      ahead[u].v = some ? load_tile(m + (size_t)ahead[u].t * ld, ld, 0, 1, col, cols) : Vec8<T>{};
 #pragma unroll
-      for (int i = 0; i < RT; ++i) ahead[u].z[i] = some && r + i * 16 < rank ? z[(size_t)ahead[u].t * z_ld + r + i * 16] : 0.0f;
+      for (int i = 0; i < RT; ++i) ahead[u].z[i] = z[(size_t)ahead[u].t * z_ld + lowest(r + i * 16, rank)];
     }
   };
   look(0);
@@ -908,10 +1004,16 @@ __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32
     if (n + kAhead < turns) fetch(n + kAhead);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
+      settle(now[u].v, col, cols);
       if (d.threshold) apply_drop(now[u].v, d, now[u].t, col);
+      if (mine + (n + u) * (kWaves * 4) >= end) {  // the last row again
+        now[u].v = Vec8<T>{};
+#pragma unroll
+        for (int i = 0; i < RT; ++i) now[u].z[i] = 0.0f;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float f = (float)now[u].v.v[j];
+        const float f = (float)now[u].v.get(j);
 #pragma unroll
         for (int i = 0; i < RT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(now[u].z[i], f, acc[i][j], 0, 0, 0);
       }
@@ -984,7 +1086,7 @@ u32 shrink_parts(size_t rows, size_t k) {
 }
 // parts of k_few's reduction: two blocks of it to a compute unit, at least 1024 bytes of a row each
 u32 few_parts(int type, size_t k, size_t n) {
-  const size_t want = ceil_div(512, ceil_div(n, 64)), most = ceil_div(k * type_size(type), kFewBytes);
+  const size_t want = ceil_div(512, ceil_div(n, 64)), most = ceil_div(k * type_size(type), kRowBytes);
   return (u32)(want < most ? want : most);
 }
 size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * (128 / type_size(type)); }

@@ -13,57 +13,70 @@ using u16 = uint16_t;
 using u32 = uint32_t;
 using u64 = uint64_t;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef u32 u32x4 __attribute__((ext_vector_type(4), may_alias));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWave = 64;
 constexpr size_t kMostCount = 0x7FFFFFFF;
 
-// Eight consecutive elements, the unit of loads, stores and of a dropout call.
+// Eight consecutive elements, the unit of loads, stores and of a dropout call. It is held in whole words, and elements are
+// taken out where they are used: as eight elements it would be taken apart right behind its load, which would so be waited for.
 template <class T>
 struct Vec8 {
-  T v[8];
+  u32x4 w[sizeof(T) / 2];
+  __device__ __forceinline__ T get(int j) const {
+    if constexpr (sizeof(T) == 4) {
+      const u32 word = w[j >> 2][j & 3];  // (a copy: the cast of an element itself takes the vector's first)
+      return __builtin_bit_cast(T, word);
+    } else {
+      return __builtin_bit_cast(T, (u16)(w[0][j >> 1] >> (16 * (j & 1))));
+    }
+  }
+  __device__ __forceinline__ void set(int j, T v) {
+    if constexpr (sizeof(T) == 4) {
+      w[j >> 2][j & 3] = __builtin_bit_cast(u32, v);
+    } else {
+      const u32 b = __builtin_bit_cast(u16, v);
+      w[0][j >> 1] = j & 1 ? (w[0][j >> 1] & 0xFFFFu) | b << 16 : (w[0][j >> 1] & 0xFFFF0000u) | b;
+    }
+  }
 };
+
 // Vector accesses of memory need no more alignment than an element's.
 typedef u32x4 u32x4_of_2 __attribute__((aligned(2), may_alias));
 typedef u32x4 u32x4_of_4 __attribute__((aligned(4), may_alias));
 template <class T>
 __device__ __forceinline__ Vec8<T> load_wide(const T* p) {
   Vec8<T> r;
-  if (sizeof(T) == 2) {
-    const u32x4 v = *(const u32x4_of_2*)p;
-    __builtin_memcpy(&r, &v, 16);
-  } else {
-    const u32x4 v[2] = {((const u32x4_of_4*)p)[0], ((const u32x4_of_4*)p)[1]};
-    __builtin_memcpy(&r, v, sizeof(r));
+#pragma unroll
+  for (u32 i = 0; i < sizeof(T) / 2; ++i) {
+    if constexpr (sizeof(T) == 2) r.w[i] = ((const u32x4_of_2*)p)[i];
+    else r.w[i] = ((const u32x4_of_4*)p)[i];
   }
   return r;
 }
 template <class T>
 __device__ __forceinline__ void store_wide(T* p, const Vec8<T>& r) {
-  u32x4 v[sizeof(r) / 16];
-  __builtin_memcpy(v, &r, sizeof(r));
-  if (sizeof(T) == 2) {
-    *(u32x4_of_2*)p = v[0];
-  } else {
-    ((u32x4_of_4*)p)[0] = v[0];
-    ((u32x4_of_4*)p)[1] = v[sizeof(r) / 16 - 1];
+#pragma unroll
+  for (u32 i = 0; i < sizeof(T) / 2; ++i) {
+    if constexpr (sizeof(T) == 2) ((u32x4_of_2*)p)[i] = r.w[i];
+    else ((u32x4_of_4*)p)[i] = r.w[i];
   }
 }
-// The first `n` of eight elements; the others are zero.
+// The first `n` of eight elements; the others are `other`.
 template <class T>
-__device__ __forceinline__ Vec8<T> load_some(const T* p, int n) {
-  Vec8<T> r;
+__device__ __forceinline__ Vec8<T> load_some(const T* p, int n, T other = (T)0.0f) {
+  Vec8<T> r = {};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (T)0.0f;
+  for (int j = 0; j < 8; ++j) r.set(j, j < n ? p[j] : other);
   return r;
 }
 template <class T>
 __device__ __forceinline__ void store_some(T* p, const Vec8<T>& v, int n) {
 #pragma unroll
   for (int j = 0; j < 8; ++j)
-    if (j < n) p[j] = v.v[j];
+    if (j < n) p[j] = v.get(j);
 }
 
 // The dropout of one call: what a kernel needs of (p, seed, offset).
@@ -126,7 +139,7 @@ __device__ __forceinline__ f32x4 mma32(const Vec8<_Float16>& a, const Vec8<_Floa
 // the reduction's place 8 g + j in both operands alike
 __device__ __forceinline__ f32x4 mma32(const Vec8<float>& a, const Vec8<float>& b, f32x4 acc) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], acc, 0, 0, 0);
+  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.get(j), b.get(j), acc, 0, 0, 0);
   return acc;
 }
 

@@ -27,9 +27,9 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, size_t ldx
     const u32x4 draws = philox(d, g, row);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float f = kept(d, draws, j) ? (float)v.v[j] * d.scale : 0.0f;
-      if (RESIDUAL) f += (float)r.v[j];
-      v.v[j] = (T)f;
+      float f = kept(d, draws, j) ? (float)v.get(j) * d.scale : 0.0f;
+      if (RESIDUAL) f += (float)r.get(j);
+      v.set(j, (T)f);
     }
     if (wide) store_wide(py, v);
     else store_some(py, v, n);

@@ -110,7 +110,7 @@ __device__ __forceinline__ void take(Soft& a, const Vec8<T>& v) {
   float x[8], most = neg_inf();
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    x[j] = (float)v.v[j];
+    x[j] = (float)v.get(j);
     most = __builtin_fmaxf(most, x[j]);
   }
   if (most > a.m) raise_to(a, most);
@@ -129,7 +129,7 @@ __device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, u32 col, 
   u64 k[8], most = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    k[j] = live && col + j < cols ? key_of((float)v.v[j], col + j) : 0;
+    k[j] = live && col + j < cols ? key_of((float)v.get(j), col + j) : 0;
     most = k[j] > most ? k[j] : most;
   }
   if (__builtin_amdgcn_ballot_w64(most > l.last) == 0) return;
@@ -158,11 +158,7 @@ __device__ __forceinline__ void take_top(TopList& l, const Vec8<T>& v, u32 col, 
 // eight elements of a row from column `col` on; -inf past its end
 template <class T>
 __device__ __forceinline__ Vec8<T> load_row(const T* row, u32 col, u32 cols) {
-  if (col + 8 <= cols) return load_wide(row + col);
-  Vec8<T> r;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) r.v[j] = col + j < cols ? row[col + j] : (T)neg_inf();
-  return r;
+  return col + 8 <= cols ? load_wide(row + col) : load_some(row + col, (int)(cols - col), (T)neg_inf());
 }
 
 struct LabelOut {
@@ -352,12 +348,12 @@ __global__ __launch_bounds__(kThreads) void k_labels_grad(const T* x, size_t ld,
         }
       }
     }
-    Vec8<T> res;
+    Vec8<T> res = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float lp = (float)in.v[j] - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
+      const float lp = (float)in.get(j) - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
       const float d = (p == 0.0f ? 0.0f : p * (-given - dh * (lp + entropy))) + extra[j];
-      res.v[j] = (T)(lse == neg_inf() ? 0.0f : d);
+      res.set(j, (T)(lse == neg_inf() ? 0.0f : d));
     }
     if (col + 8 <= cols) store_wide(out + col, res);
     else store_some(out + col, res, (int)(cols - col));
