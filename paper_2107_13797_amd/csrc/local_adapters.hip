@@ -787,7 +787,8 @@ struct Prepare {
 // `order` holds the rows of party 0 in ascending order, then those of party 1, ..., at last those without; begin[p] is where
 // p's start, begin[parties] where the last begin; chunk_begin[p] the first of p's chunks of chunk_rows rows; chunk[c] = p.
 // The block's wavefronts take a range of rows each, count them, and list them from where their counts say. One compute unit's
-// vector instructions bound it (16384 rows: 18 us, 3001 rows of more parties: 10); more blocks would cost another launch.
+// vector instructions bound it (16384 rows: 13 us party by party, 18 when every 64 rows were taken as mixed; 3001 mixed rows:
+// 11); more blocks would cost another launch.
 __device__ void group_rows(const Group& g, u32* counts) {
   constexpr int kAhead = 8;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), waves = group_waves(g.parties);
@@ -814,7 +815,9 @@ __device__ void group_rows(const Group& g, u32* counts) {
         const u32 a = (u32)raw[i] < parties ? (u32)raw[i] : parties;
         if (pass == 0 && t < end && a == parties && raw[i] != -1 && g.status) atomicOr(g.status, HAFLO_ST_RANGE);
         u64 same = __builtin_amdgcn_ballot_w64(t < end);  // the lanes whose row has this one's party, bit by bit
-        for (u32 b = 0; b < bits; ++b) {
+        const u32 one = (u32)__builtin_amdgcn_readfirstlane((int)a);
+        const bool mixed = __builtin_amdgcn_ballot_w64(t < end && a != one) != 0;  // (rows often come party by party)
+        for (u32 b = 0; mixed && b < bits; ++b) {
           const u64 ones = __builtin_amdgcn_ballot_w64(a >> b & 1);
           same &= a >> b & 1 ? ones : ~ones;
         }
