@@ -250,3 +250,61 @@ def test_refusals(api):
     y, h = fwd(x[:0], w, a, b, s, i[:0])
     dx, da, db = api.haflo_adapter_backward(y, x[:0], w, a, b, s, i[:0], h)
     assert y.shape == (0, 6) and dx.shape == (0, 8) and da.dtype == f32 and not da.any() and not db.any()
+
+
+def test_adapters_without_dx(api):
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for rows in (7, 300):
+        x, w = torch.randn(rows, 40, generator=g, device="cuda"), torch.randn(24, 40, generator=g, device="cuda")
+        a, b = torch.randn(3, 5, 40, generator=g, device="cuda"), torch.randn(3, 24, 5, generator=g, device="cuda")
+        scale, index = torch.ones(3, device="cuda"), (torch.arange(rows, device="cuda") % 4 - 1).to(torch.int32)
+        y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.25, 9, 1)
+        _, da, db = api.haflo_adapter_backward(y, x, w, a, b, scale, index, h, 0.25, 9, 1)
+        none, da2, db2 = api.haflo_adapter_backward(y, x, w, a, b, scale, index, h, 0.25, 9, 1, need_dx=False)
+        assert none is None and torch.equal(da, da2) and torch.equal(db, db2)
+
+
+def test_adapters_past_32_bits(api):
+    """x and dx of more than 4 GiB. Small integers: every sum is exact in 32 bits, so is each result before its rounding."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rows, inner, outer, rank = 70000, 32768, 16, 2
+    bf16 = torch.bfloat16
+
+    def ints(*shape):
+        return torch.randint(-1, 2, shape, generator=g, device="cuda", dtype=torch.int8).to(bf16)
+
+    x, w, a, b = ints(rows, inner), ints(outer, inner), ints(2, rank, inner), ints(2, outer, rank)
+    scale, index = torch.tensor([1.0, 2.0], device="cuda"), torch.randint(-1, 2, (rows,), generator=g, device="cuda").to(torch.int32)
+    dy = ints(rows, outer)
+    y, h = api.haflo_adapter_forward(x, w, a, b, scale, index)
+    dx, da, db = api.haflo_adapter_backward(dy, x, w, a, b, scale, index, h)
+    some = torch.cat([torch.arange(40), torch.arange(rows - 40, rows)]).cuda()
+    xs, dys, of = x[some].double(), dy[some].double(), index[some].long()
+    by = torch.where(of < 0, 0.0, scale.double()[of])
+    hs = by[:, None] * (a.double()[of] @ xs[:, :, None])[..., 0]
+    assert torch.equal(h[some].double(), hs)
+    assert torch.equal(y[some], (xs @ w.double().t() + (b.double()[of] @ hs[:, :, None])[..., 0]).to(bf16))
+    gs = by[:, None] * (dys[:, None, :] @ b.double()[of])[:, 0]
+    assert torch.equal(dx[some], (dys @ w.double() + (gs[:, None, :] @ a.double()[of])[:, 0]).to(bf16))
+    cols = torch.cat([torch.arange(9), torch.arange(inner - 9, inner)]).cuda()
+    for p in range(2):
+        mine = (index == p).nonzero()[:, 0]
+        gp = scale[p].double() * (dy[mine].double() @ b[p].double())
+        assert torch.equal(da[p][:, cols].double(), gp.t() @ x[mine][:, cols].double())
+        assert torch.equal(db[p].double(), dy[mine].double().t() @ h[mine].double())
+
+
+def test_homo_adapters_round_end_to_end(api):
+    """Local steps of several parties, the encrypted average of their adapters, an answer under it: the decoded sum is the exact
+    integer sum of the quantised weights, the parties' losses have fallen, and the answer's labels stand in order."""
+    from paper_2107_13797_amd.examples import homo_adapters
+    p, q = api.haflo_keygen(1024, 11)
+    own, pub = api.haflo_ctx_create_private(p, q, 1024), api.haflo_ctx_create_public(p * q, 1024)
+    res = homo_adapters.run_round(api, pub, own, parties=3, rows=150, width=72, labels=10, rank=4, steps=6, seed=3)
+    own.close()
+    pub.close()
+    assert res["weights"] == 4 * (72 + 72 + 72 + 10)
+    assert res["sum_q"] == res["want_sum_q"]
+    assert res["loss"]["local"] < res["loss"]["before"]
+    logps = [v for _, v in res["answer"]]
+    assert len(set(i for i, _ in res["answer"])) == 5 and logps == sorted(logps, reverse=True) and max(logps) < 0
