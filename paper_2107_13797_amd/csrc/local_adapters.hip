@@ -570,14 +570,14 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   }
 }
 
-// The same for few rows, in two launches. k_few reads W once: a block takes 64 outputs and one part of the reduction, 1024 bytes of
+// The same for few rows, in two launches. k_few reads W once for 64 rows: a block takes them, 64 outputs and one part of the reduction, 1024 bytes of
 // every row at a time, its wavefronts four sixteens of outputs in two halves of that; further blocks form the parts of z = h or
 // g for one row each, as k_shrink does. k_few_join adds the parts, and the adapters' part to them. What bounds it is the
 // reading of W: 64 rows of 4096 to 4096 in bfloat16 take 16 us and 6 for the joining, one row 8.6 and 4.4.
 constexpr int kFewWaves = 8;
 template <class T, int RT, bool SHORT>
 __device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, size_t ldw, u32 rows, u32 inner, u32 outer, u32 tile, u32 part,
-                                            u32 parts, float* sums, T* lx, f32x4* half) {
+                                            u32 parts, size_t part_step, float* sums, T* lx, f32x4* half) {
   constexpr u32 kElems = kRowBytes / sizeof(T), kSteps = kElems / 32 / 2, kLanes = kElems / 8, kRows = kWave / kLanes;  // rows of a load
   constexpr u32 kLoads = RT * 16 / (kFewWaves * kRows);
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
@@ -625,7 +625,7 @@ __device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, 
     const u32 t = j * 16 + lane % 16;
     if (t >= rows) continue;
     const f32x4 s = acc[j] + half[(wave * RT + j) * kWave + lane];
-    float* const to = sums + ((size_t)part * rows + t) * outer + o4;
+    float* const to = sums + part * part_step + (size_t)t * outer + o4;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (o4 + e < outer) to[e] = s[e];
@@ -638,10 +638,15 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
                                                            u32 parties, Drop d, u32 parts, u32 z_parts, u32 z_ld, float* sums, float* z,
                                                            u32* status) {
   __shared__ __align__(16) char lds[RT * 16 * kRowBytes];  // tiles of x, then halves of sums; or parts of z
-  const u32 products = (outer + 63) / 64 * parts;
+  constexpr u32 kGroup = RT * 16;
+  const u32 tiles = (outer + 63) / 64 * parts, products = (rows + kGroup - 1) / kGroup * tiles;
   if (blockIdx.x < products) {
-    if (inner < 8) few_product<T, RT, true>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
-    else few_product<T, RT, false>(x, ldx, w, ldw, rows, inner, outer, blockIdx.x / parts, blockIdx.x % parts, parts, sums, (T*)lds, (f32x4*)lds);
+    const u32 t0 = blockIdx.x / tiles * kGroup, at = blockIdx.x % tiles, count = rows - t0 < kGroup ? rows - t0 : kGroup;
+    const T* const x0 = x + (size_t)t0 * ldx;
+    float* const to = sums + (size_t)t0 * outer;
+    const size_t step = (size_t)rows * outer;
+    if (inner < 8) few_product<T, RT, true>(x0, ldx, w, ldw, count, inner, outer, at / parts, at % parts, parts, step, to, (T*)lds, (f32x4*)lds);
+    else few_product<T, RT, false>(x0, ldx, w, ldw, count, inner, outer, at / parts, at % parts, parts, step, to, (T*)lds, (f32x4*)lds);
     return;
   }
   float(*const lz)[ZT * 16] = (float(*)[ZT * 16])lds;
@@ -1080,16 +1085,23 @@ bool adapter_sizes(int type, const Sizes& s) {
          s.outer <= kMostCount - 512 && s.parties >= 1 && s.parties <= HAFLO_ADAPTER_MAX_PARTIES && s.rank >= 1 &&
          s.rank <= HAFLO_ADAPTER_MAX_RANK;
 }
-constexpr size_t kFewRows = 64;  // up to here k_few
+// Whether k_few takes a product: up to 256 rows, where k_project's tiles would leave most of the chip idle; float32, whose matrix
+// instructions bound it sooner, up to 2^31 products of elements. Forward, us by k_few and by k_project: bfloat16 4096 to 4096
+// 128 rows 27 and 48, 256 rows 41 and 47, 4096 to 256 128 rows 15 and 33; float32 4096 to 4096 128 rows 61 and 89, 192 rows 98 and
+// 92, 4096 to 256 256 rows 24 and 87.
+bool few(int type, const Sizes& s) {
+  return s.rows <= 256 && (type != HAFLO_F32 || s.rows * s.inner <= ((size_t)1 << 31) / s.outer);
+}
 // parts of k_shrink's reduction: enough blocks to fill the chip, at least 512 columns each
-u32 shrink_parts(size_t rows, size_t k) {
+u32 shrink_parts(bool by_row, size_t rows, size_t k) {
   if (rows == 0) return 1;
-  const size_t tiles = rows <= kFewRows ? rows : ceil_div(rows, 16), want = tiles < 512 ? ceil_div(512, tiles) : 1, most = ceil_div(k, 512);
+  const size_t tiles = by_row ? rows : ceil_div(rows, 16), want = tiles < 512 ? ceil_div(512, tiles) : 1, most = ceil_div(k, 512);
   return (u32)(want < most ? want : most);
 }
 // parts of k_few's reduction: two blocks of it to a compute unit, at least 1024 bytes of a row each
-u32 few_parts(int type, size_t k, size_t n) {
-  const size_t want = ceil_div(512, ceil_div(n, 64)), most = ceil_div(k * type_size(type), kRowBytes);
+u32 few_parts(int type, size_t rows, size_t k, size_t n) {
+  if (rows == 0) return 1;
+  const size_t want = ceil_div(512, ceil_div(rows, 64) * ceil_div(n, 64)), most = ceil_div(k * type_size(type), kRowBytes);
   return (u32)(want < most ? want : most);
 }
 size_t padded(int type, size_t k) { return ceil_div(k, 128 / type_size(type)) * (128 / type_size(type)); }
@@ -1109,8 +1121,8 @@ Plan adapter_plan(int type, bool backward, const Sizes& s) {
   };
   const size_t e = type_size(type), ranks = whole_ranks(s.rank);
   const size_t k = backward ? s.outer : s.inner, n = backward ? s.inner : s.outer, kp = padded(type, k);  // the product's sizes
-  p.z_parts = take(shrink_parts(s.rows, k) * s.rows * ranks * 4);
-  if (s.rows <= kFewRows) p.few_sums = take(few_parts(type, k, n) * s.rows * n * 4);
+  p.z_parts = take(shrink_parts(few(type, s), s.rows, k) * s.rows * ranks * 4);
+  if (few(type, s)) p.few_sums = take(few_parts(type, s.rows, k, n) * s.rows * n * 4);
   p.z = take(s.rows * ranks * 4);
   p.x = take(s.rows * kp * e);
   p.w = take(n * kp * e);
@@ -1188,7 +1200,7 @@ struct Product {
 
   // z, dense as `h` too unless that is null
   void shrink(float* h) const {
-    const u32 parts = shrink_parts(s.rows, s.inner);
+    const u32 parts = shrink_parts(false, s.rows, s.inner);
     const dim3 grid((unsigned)(ceil_div(s.rows, 16) * parts)), block(kShrinkWaves * kWave);
     float* const to = parts > 1 ? z_parts() : z();
     float* const h_now = parts > 1 ? nullptr : h;
@@ -1207,8 +1219,8 @@ struct Product {
 
   // Few rows: y, unless it is null, and z; dense as `h` too unless that is null.
   void few_rows(float* h, T* y, size_t ldy) const {
-    const u32 zp = shrink_parts(s.rows, s.inner), parts = few_parts(sizeof(T) == 4 ? HAFLO_F32 : HAFLO_F16, s.inner, s.outer);
-    const dim3 grid((unsigned)(y ? ceil_div(s.outer, 64) * parts + s.rows * zp : s.rows * zp)), block(kFewWaves * kWave);
+    const u32 zp = shrink_parts(true, s.rows, s.inner), parts = few_parts(sizeof(T) == 4 ? HAFLO_F32 : HAFLO_F16, s.rows, s.inner, s.outer);
+    const dim3 grid((unsigned)(y ? ceil_div(s.rows, 64) * ceil_div(s.outer, 64) * parts + s.rows * zp : s.rows * zp)), block(kFewWaves * kWave);
     float* const sums = (float*)(ws + plan.few_sums);
 #define HAFLO_LOCAL_RUN(RT, ZT)                                                                                                            \
   hipLaunchKernelGGL((k_few<T, RT, ZT>), grid, block, 0, st, x.p, x.ld, w.p, w.ld, low.p, low.ld, scale, index, (u32)s.rows, (u32)s.inner, \
@@ -1296,7 +1308,7 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
   Drop none = d;
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
-    const bool many = rows > kFewRows;
+    const bool many = !few(type, s);
     Layouts<T> lay;
     Product<T> f = {{(const T*)d_x, ldx}, {(const T*)d_w, ldw}, {(const T*)d_a, inner}, {(const T*)d_b, rank}, d_scale, d_index, s, d, none, ws,
                     plan, many ? nullptr : d_status, st};
@@ -1334,7 +1346,7 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
   Drop none = d;
   none.threshold = 0;
   HAFLO_LOCAL_TYPES(type, {
-    const bool many = rows > kFewRows;
+    const bool many = !few(type, s);
     const size_t ranks = whole_ranks(rank);
     const size_t kp = padded(type, outer);
     const Sizes back = {rows, outer, inner, parties, rank};

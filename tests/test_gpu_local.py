@@ -308,3 +308,11 @@ def test_homo_adapters_round_end_to_end(api):
     assert res["loss"]["local"] < res["loss"]["before"]
     logps = [v for _, v in res["answer"]]
     assert len(set(i for i, _ in res["answer"])) == 5 and logps == sorted(logps, reverse=True) and max(logps) < 0
+
+
+@pytest.mark.parametrize("case", [
+    ("bf16", 65, 1033, 130, 16, 5, 0.1, "mixed", 1), ("f16", 130, 7, 65, 5, 3, 0.2, "mixed", 0), ("f32", 193, 300, 41, 33, 9, 0.0, "sorted", 3),
+    ("bf16", 256, 520, 1001, 70, 2, 0.05, "mixed", 0), ("f32", 257, 65, 520, 4, 4, 0.1, "mixed", 0)], ids=str)
+def test_adapters_some_rows(run, case):
+    """Between one and four groups of 64 rows, and one row more."""
+    cases.check_adapters(run, *case)
