@@ -87,6 +87,8 @@ __device__ __forceinline__ Vec8<T> get_row(T* tile, u32 row, u32 q) {
 // z[t, r] = scale[a] s sum_k drop(x[t, k]) F[a][r, k], F rows f_ld apart; z rows z_ld long with zeros behind the rank, h without.
 // A block takes sixteen rows of `order` and one part of the reduction, its wavefronts some steps in turn each; once for every
 // party among the rows. Rows behind the last, of x and of F, are the last one again: what they give is left aside.
+// Reading x bounds it: 8192 x 4096 bfloat16 with rank 16, 28 to 33 us, 2.0 to 2.4 TB/s; with the rows brought to LDS by all
+// wavefronts first and multiplied from there 28 to 40.
 constexpr int kShrinkWaves = 4;
 template <class T, int RT>
 __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   }
 }
 
-// z[i] = sum over parts, and without the places behind the rank to h
+// A lane an element (3001 rows, 2 us: a launch): z[i] = sum over parts, and without the places behind the rank to h
 __global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, size_t count, u32 z_ld, u32 rank, float* z, float* h) {
   const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
   if (i >= count) return;
@@ -420,7 +422,9 @@ __device__ __forceinline__ void reduce(const From& x, const typename From::At (&
 
 // y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k], inner a multiple of a step. A block takes TM rows (of
 // `order`) by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
-// is filled while the other is read.
+// is filled while the other is read. Matrix instructions and the reads of LDS between them bound the large tiles (8192 x 4096
+// to 4096, bfloat16: 231 us, 1190 TFLOP/s; 336 us by tiles of 128 x 128), the wait for each step's loads the small ones
+// (float16 3001 x 1001 to 515: 19 us, 164 TFLOP/s).
 template <class T, int TM, int TN, int WM, int WN, bool DROP, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
                                                              const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
@@ -714,7 +718,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
   to[r] = r < rank ? s * scale[a] * (d.threshold ? d.scale : 1.0f) : 0.0f;
 }
 
-// A block takes 256 outputs of a row, a lane one. Its z is written to `z_out` (z_ld places) or `h` (rank) by the first of the row.
+// A block takes 256 outputs of a row, a lane one: the reading of the parts bounds it (64 rows of 4096, 8 parts: 5.8 us). Its z is written to `z_out` (z_ld places) or `h` (rank) by the first of the row.
 template <class T, bool DROP>
 __global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const float* z, const T* f, u32 f_ld, const int* index, u32 rows, u32 outer,
                                                        u32 parties, u32 rank, Drop d, u32 parts, u32 z_parts, u32 z_ld, T* y, size_t ldy,
@@ -765,6 +769,7 @@ u32 chunk_rows(size_t rows, size_t cols, size_t rank) {
 }
 // What a call lays out before its products: matrices copied to rows of `out_ld` elements with zeros behind what they hold, or
 // transposed to such rows (`count` of them one behind the other), and the rows grouped by adapter by the first block.
+// Memory bounds it: W of 4096 x 4096 in bfloat16 transposed in 26 us, 2.6 TB/s. One launch, as a short one costs 3 us and more.
 constexpr int kPrepareThreads = 1024;
 constexpr u32 kGroupCounts = 16384;
 __host__ __device__ inline u32 group_waves(u32 parties) { return parties < 1024 ? 16 : 3; }  // whose counts fit LDS
@@ -936,7 +941,8 @@ __global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p) {
 // operands are one element a lane: lane l holds eight columns from 8 (l % 16) on of row l / 16 out of four, and element j of
 // all lanes is one operand, for the columns 8 c + j. A block takes 128 columns and RT sixteens of z, its wavefronts every
 // fourth four rows each. The next rows are on their way while the present ones are multiplied.
-// Both gradients are formed by one launch.
+// Both gradients are formed by one launch. 8192 rows of 4096 and 4096 columns, rank 16, bfloat16: 54 us, 40 TFLOP/s and 2.5 TB/s, so
+// bound by neither alone but by a row's way from memory to its sixteen products; four rows ahead in place of two gain nothing.
 template <class T>
 struct GradOf {
   const T* m;
@@ -1061,7 +1067,8 @@ __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32
   }
 }
 
-// grad[p] = sum of the party's chunks, in their order
+// grad[p] = sum of the party's chunks, in their order. A lane takes an element; the chunks' reading bounds it (8192 rows, 8 parties,
+// 16 x 8192 weights: 9 us).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_grad_join(GradOf<T> a, GradOf<T> b, const u32* __restrict__ chunk_begin, u32 rank) {
   const size_t n_a = (size_t)rank * a.cols, n_b = (size_t)rank * b.cols;
@@ -1245,6 +1252,9 @@ struct Product {
 #undef HAFLO_LOCAL_RUN
   }
 
+  // The largest tiles that give every compute unit one: W and x are read once for a tile's side. Calls, us: bfloat16 4096 x 4096 to
+  // 2048 by 128 x 128 95, by 64 x 64 125; 4096 x 512 to 2048 33 and 37; too few tiles, float16 3001 x 1001 to 515, the product alone
+  // 30 and 19. float32 is bound by its matrix instructions: 4096 x 1024 to 1024 95 by 128 x 128 and 89 by 64 x 64, which it takes.
   void project(T* y, size_t ldy) const {
     const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
     const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
@@ -1257,6 +1267,7 @@ struct Product {
   do {                                                                                                            \
     if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, true);                                                         \
     else if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, false); \
+    else if constexpr (sizeof(T) == 4) HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP, false);                                \
     else if (ceil_div(s.rows, 128) * ceil_div(s.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, DROP, false); \
     else HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP, false);                                                              \
   } while (0)

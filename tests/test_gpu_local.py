@@ -316,3 +316,9 @@ def test_homo_adapters_round_end_to_end(api):
 def test_adapters_some_rows(run, case):
     """Between one and four groups of 64 rows, and one row more."""
     cases.check_adapters(run, *case)
+
+
+@pytest.mark.parametrize("case", [("bf16", 8200, 2051, 1, 0, 3, "ties"), ("f32", 8195, 2049, 0, 0, 0, "ties")], ids=str)
+def test_labels_many_rows(run, case):
+    """Rows that a wavefront takes for their number, longer than it takes otherwise."""
+    cases.check_labels(run, *case)
