@@ -193,71 +193,26 @@ __global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, s
 }
 
 // ---------------------------------------------------------------------------------------------------
-// The adapters' part of k_project on matrix instructions. z is float32: on 16-bit types it enters as two bfloat16 pieces, the
-// value cut to eight bits and what is left rounded to eight, 2^-17 of it off at most, which a result of 16 bits does not
-// show; a float16 adapter element is two bfloat16 pieces exactly. Pieces of one rank stand at different places of the
-// reduction.
-__device__ __forceinline__ __bf16 piece(float v, bool rest) {
-  const u32 b = __builtin_bit_cast(u32, v);
-  const float cut = __builtin_bit_cast(float, b & 0xFFFF0000u);
-  if ((b & 0x7F800000u) == 0x7F800000u) return rest ? (__bf16)0.0f : (__bf16)v;  // infinities and NaN
-  return (__bf16)(rest ? v - cut : cut);
-}
+// The adapters' part of k_project: matrix instructions in 32 bits, as z is float32 and may cancel against the large product, and an
+// infinity of z or of an adapter must meet the other's whole element. Lane l holds four ranks from 4 (l / 16) on of its row.
 // z and the adapters' rows are `ranks` long, a multiple of sixteen, with zeros behind the rank.
 constexpr u32 kRanks = 16;
+__device__ __forceinline__ f32x4 low_of_z(const float* z) {
+  f32x4 v;
+  __builtin_memcpy(&v, __builtin_assume_aligned(z + lane_id() / 16 * 4, 16), sizeof(v));
+  return v;
+}
 template <class T>
-struct LowPart;
-template <>
-struct LowPart<__bf16> {
-  static constexpr u32 kStep = 16;  // ranks of one product
-  using Frag = Vec8<__bf16>;
-  static __device__ __forceinline__ Frag of_z(const float* z) {
-    const u32 g = lane_id() / 16;
-    const Vec8<float> v = load_wide(z + (g & 1) * 8);
-    Frag f = {};
+__device__ __forceinline__ f32x4 low_of_f(const T* f) {
+  T t[4];
+  __builtin_memcpy(t, __builtin_assume_aligned(f + lane_id() / 16 * 4, 4 * sizeof(T)), sizeof(t));
+  return f32x4{(float)t[0], (float)t[1], (float)t[2], (float)t[3]};
+}
+__device__ __forceinline__ f32x4 low_mma(const f32x4& f, const f32x4& z, f32x4 acc) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.set(e, piece(v.get(e), g >= 2));
-    return f;
-  }
-  static __device__ __forceinline__ Frag of_f(const __bf16* w) { return load_wide(w + (lane_id() / 16 & 1) * 8); }
-  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) { return mma32(f, z, acc); }
-};
-template <>
-struct LowPart<_Float16> {
-  static constexpr u32 kStep = 8;
-  using Frag = Vec8<__bf16>;
-  static __device__ __forceinline__ Frag of_z(const float* z) {
-    const Vec8<float> v = load_wide(z);
-    Frag f = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.set(e, piece(v.get(e), lane_id() / 16 & 1));
-    return f;
-  }
-  static __device__ __forceinline__ Frag of_f(const _Float16* w) {
-    const Vec8<_Float16> v = load_wide(w);
-    Frag f = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.set(e, piece((float)v.get(e), lane_id() / 16 >= 2));
-    return f;
-  }
-  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) { return mma32(f, z, acc); }
-};
-template <>
-struct LowPart<float> {
-  static constexpr u32 kStep = 16;
-  using Frag = f32x4;
-  static __device__ __forceinline__ Frag of_z(const float* z) {
-    Frag f;
-    __builtin_memcpy(&f, __builtin_assume_aligned(z + lane_id() / 16 * 4, 16), 16);
-    return f;
-  }
-  static __device__ __forceinline__ Frag of_f(const float* w) { return of_z(w); }
-  static __device__ __forceinline__ f32x4 mma(const Frag& f, const Frag& z, f32x4 acc) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], z[e], acc, 0, 0, 0);
-    return acc;
-  }
-};
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], z[e], acc, 0, 0, 0);
+  return acc;
+}
 
 // Where the rows of a tile are loaded from, sixteen bytes a lane straight into LDS, lane l's to `to` + 16 l. Matrices below
 // 4 GiB are read as buffers, whose offsets are 32-bit words and whose loads the compiler counts one by one; FAR ones are not.
@@ -472,7 +427,6 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   reduce<T, TM, TN, WAVES>(from_x, at_x, from_w, at_w, inner / KE, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
 
   // the adapters' part, party by party along the list
-  using Low = LowPart<T>;
   const u32 wave_at = t0 + row0, listed = begin[parties], wave_end = wave_at + TM / WM < rows ? wave_at + TM / WM : rows;
   for (u32 at = wave_at; at < wave_end && at < listed;) {
     const int who = index[order[at]];
@@ -485,15 +439,15 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
       f32x4 low0[OT], low1[OT];
 #pragma unroll
       for (int i = 0; i < OT; ++i) low0[i] = low1[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      for (u32 r0 = 0; r0 < ranks; r0 += Low::kStep) {
-        const typename Low::Frag v0 = Low::of_z(z + (size_t)(t[j] < rows ? t[j] : 0) * ranks + r0);
-        const typename Low::Frag v1 = Low::of_z(z + (size_t)(t[j + 1] < rows ? t[j + 1] : 0) * ranks + r0);
+      for (u32 r0 = 0; r0 < ranks; r0 += kRanks) {
+        const f32x4 v0 = low_of_z(z + (size_t)(t[j] < rows ? t[j] : 0) * ranks + r0);
+        const f32x4 v1 = low_of_z(z + (size_t)(t[j + 1] < rows ? t[j + 1] : 0) * ranks + r0);
 #pragma unroll
         for (int i = 0; i < OT; ++i) {
           const u32 o = o0 + out0 + i * 16 + lane % 16;
-          const typename Low::Frag fv = Low::of_f(f + ((size_t)who * outer + (o < outer ? o : outer - 1)) * ranks + r0);
-          low0[i] = Low::mma(fv, v0, low0[i]);
-          low1[i] = Low::mma(fv, v1, low1[i]);
+          const f32x4 fv = low_of_f(f + ((size_t)who * outer + (o < outer ? o : outer - 1)) * ranks + r0);
+          low0[i] = low_mma(fv, v0, low0[i]);
+          low1[i] = low_mma(fv, v1, low1[i]);
         }
       }
 #pragma unroll

@@ -286,3 +286,53 @@ def check_labels_nan(run):
         assert got[4][1, :2].tolist() == [cols - 2, cols - 1] and got[4][2, 0] == 1
         dx = run.label_logprobs_backward(x, torch.zeros(4, dtype=torch.int32), got[2], got[1], torch.ones(4), None, None, None)
         assert bool(dx[1:3].isnan().all()) and not bool(dx[[0, 3]].isnan().any())
+
+
+# --------------------------------------------------------------------------------------------------- adapters, more than 256 rows
+
+ADAPTERS_SHORT_SUMS = [  # sums of few terms, which leave their own roundings little room
+    ("f16", 256, 1, 24, 1, 3, 0.0, "one", 0), ("f16", 300, 1, 24, 1, 3, 0.0, "one", 0), ("bf16", 500, 3, 70, 2, 300, 0.3, "mixed", 1),
+    ("f32", 300, 1, 24, 1, 3, 0.0, "one", 0),
+]
+
+
+def check_adapters_cancelling(run, kind, rows):
+    """W = -B A but for its rounding: what is left of y and dx shows how many bits of h and g the adapters' part takes."""
+    inner, outer, rank = 2, 3, 2
+    x, w, a, b, scale, index, dy = adapter_inputs(kind, rows, inner, outer, rank, 2, "one", 0)
+    scale[:] = 1.0
+    w.copy_((-(b[1].double() @ a[1].double())).to(w.dtype))
+    f = factor(rows, inner, 0.0, 1, 0)
+    want, most = (adapter_exact(x, w, a, b, scale, index, dy, f, absolute=m) for m in (False, True))
+    u, ulp = UNIT[x.dtype], 2.0 ** -23
+    y, h, _ = run.adapter_forward(x, w, a, b, scale, index, 0.0, 1, 0)
+    near(y, want[0], u * want[0].abs() + (inner + rank + 8) * ulp * most[0] + TINY[x.dtype])
+    dx, _, _, _ = run.adapter_backward(dy, x, w, a, b, scale, index, h, 0.0, 1, 0)
+    near(dx, want[2], u * want[2].abs() + (outer + rank + 8) * ulp * most[2] + TINY[x.dtype])
+
+
+def check_adapters_own_infinities(run, kind):
+    """An infinity that a row's own adapter or its h or g holds reaches the results that it is a term of, as infinity or, against a
+    zero, as NaN, however many rows come together. All else is small integers, whose sums are exact."""
+    few = None
+    for rows in (256, 257):
+        inner, outer, rank, parties = 8, 16, 3, 2
+        gen = torch.Generator().manual_seed(9)
+        ints = lambda *s: torch.randint(-2, 3, s, generator=gen).to(TYPES[kind])  # noqa: E731
+        w, a, b = ints(outer, inner), ints(parties, rank, inner), ints(parties, outer, rank)
+        x, dy, index = ints(257, inner)[:rows], ints(257, outer)[:rows], (torch.arange(rows) % 3 - 1).to(torch.int32)
+        b[1, 2, 0], b[1, 3, 1], a[1, 2, 4] = math.inf, -math.inf, math.inf  # a row's B, and its A, so its h
+        scale = torch.tensor([1.0, 2.0])
+        f = factor(rows, inner, 0.0, 1, 0)
+        want = adapter_exact(x, w, a, b, scale, index, dy, f)
+        y, h, _ = run.adapter_forward(x, w, a, b, scale, index, 0.0, 1, 0)
+        near(y, want[0], 0.0)
+        near(h, want[1], 0.0)
+        dx, _, _, _ = run.adapter_backward(dy, x, w, a, b, scale, index, h, 0.0, 1, 0)
+        near(dx, want[2], 0.0)
+        if rows == 256:
+            assert bool(y.isinf().any()) and bool(y.isnan().any()) and bool(dx.isinf().any() | dx.isnan().any())
+            few = y, dx
+        else:
+            for got, was in zip((y, dx), few):
+                assert torch.equal(got[:256].nan_to_num(7e3), was.nan_to_num(7e3))

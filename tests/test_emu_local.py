@@ -174,3 +174,19 @@ def test_no_rows(run):
     none = slice(0, 0)
     _, da, db, status = run.adapter_backward(dy[none], x[none], w, a, b, scale, index[none], torch.zeros(0, 3), 0.0, 0, 0)
     assert not da.any() and not db.any() and status == 0
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_SHORT_SUMS, ids=str)
+def test_adapters_short_sums(run, case):
+    cases.check_adapters(run, *case)
+
+
+@pytest.mark.parametrize("rows", [200, 300])
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_cancelling(run, kind, rows):
+    cases.check_adapters_cancelling(run, kind, rows)
+
+
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_own_infinities(run, kind):
+    cases.check_adapters_own_infinities(run, kind)

@@ -322,3 +322,19 @@ def test_adapters_some_rows(run, case):
 def test_labels_many_rows(run, case):
     """Rows that a wavefront takes for their number, longer than it takes otherwise."""
     cases.check_labels(run, *case)
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_SHORT_SUMS, ids=str)
+def test_adapters_short_sums(run, case):
+    cases.check_adapters(run, *case)
+
+
+@pytest.mark.parametrize("rows", [200, 300])
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_cancelling(run, kind, rows):
+    cases.check_adapters_cancelling(run, kind, rows)
+
+
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_own_infinities(run, kind):
+    cases.check_adapters_own_infinities(run, kind)
