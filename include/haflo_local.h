@@ -99,7 +99,9 @@ int haflo_label_logprobs(int type, const void* d_logits, size_t ld, const int32_
                          void* stream);
 /*
  * Gradient by the logits, from the forward call's lse, entropy and d_top_index:
- *   dx_j = p_j (-(dlogp + sum_k dtop_k) - dentropy (x_j - lse + entropy)) + [j = label] dlogp + sum_k [j = top_k] dtop_k
+ *   dx_j = p_j (-(dlogp + sum_k dtop_k) - dentropy (ln p_j + entropy)) + [j = label] dlogp + sum_k [j = top_k] dtop_k
+ * p_j = e^(x_j - lse) / sum_i e^(x_i - lse): the sum is formed again, so that nothing is lost where float32 holds lse coarsely, in
+ * rows far from zero and of the lowest value only.
  * d_dentropy and d_dtop (rows x top) may be NULL: zeros. dlogp of a row without label is
  * not used; a top index outside the row is left out. d_dx may be d_logits where the distances between rows are the same.
  */

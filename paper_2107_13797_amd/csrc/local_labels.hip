@@ -20,6 +20,7 @@ constexpr size_t kWaveCols = 2048, kManyWaveCols = 8192, kManyRows = 8192;
 constexpr size_t kSplitCols = 2048;  // columns of one part of a row, at least
 constexpr size_t kSplitBlocks = 1024;
 constexpr int kAhead = 4;            // vectors on their way at a time
+constexpr size_t kGradBlocks = 1 << 21;  // blocks of a launch at most, which loop over the rows
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -317,52 +318,128 @@ __global__ __launch_bounds__(kThreads) void k_labels_small(const T* x, size_t ld
   }
 }
 
+// a number below `count`, the last one for those behind it
+__device__ __forceinline__ u32 lowest(u32 i, u32 count) { return i < count ? i : count - 1; }
+
 struct GradIn {
   const int* label;
   const float *lse, *entropy, *dlogp, *dentropy;
   const int* top_index;
   const float* dtop;
 };
-// A lane to eight columns of a row: dx = -p (g + dentropy (x - lse + entropy)), p = e^(x - lse) and g the sum of what
-// label and alternatives are given, plus that at their columns.
-// Memory bounds it, one reading and one writing (8192 x 32768 bfloat16: 192 us, 5.6 TB/s).
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_labels_grad(const T* x, size_t ld, u32 rows, u32 cols, int top, GradIn g, T* dx,
-                                                          size_t lddx) {
-  const u32 groups = (cols + 7) / 8;
-  const u64 total = (u64)rows * groups, step = (u64)gridDim.x * kThreads;
-  for (u64 at = (u64)blockIdx.x * kThreads + threadIdx.x; at < total; at += step) {
-    const u32 r = (u32)(at / groups), v = (u32)(at - (u64)r * groups);
-    const T* row = x + (size_t)r * ld;
-    T* out = dx + (size_t)r * lddx;
-    const u32 col = v * 8;
-    const Vec8<T> in = load_row(row, col, cols);
-    const float lse = g.lse[r], entropy = g.entropy[r], dh = g.dentropy ? g.dentropy[r] : 0.0f;
+// dx = -p (g + dentropy (ln p + entropy)), p = e^(x - lse) / z and g the sum of what label and alternatives are given, plus that at
+// their columns. z, the row's sum of e^(x - lse), is formed here once more: float32 holds lse to 2^-24 of the logits' size, so that z is 1
+// for small ones only (a row of the type's lowest value has lse equal to it, and z is the row's length).
+// WAVES wavefronts take a row or, with WAVES = 0, a group of 2^shift lanes of one. A lane keeps its first HELD vectors of the row between
+// the sum and the results and reads what is behind them twice; it writes only columns that it alone reads, after the sum. Memory bounds
+// it, one reading and one writing (8192 x 32768 bfloat16: 212 us, 5.1 TB/s; 2048 x 131072, three quarters of it read twice: 237); of
+// a single row the one compute unit that it is on (131072 columns: 22 us).
+template <class T, int WAVES, int HELD, bool TOP>
+__global__ __launch_bounds__(WAVES > kWaves ? WAVES * kWave : kThreads, 4) void k_labels_grad(const T* x, size_t ld, u32 rows, u32 cols, int top, u32 shift,
+                                                                                         GradIn g, T* dx, size_t lddx) {
+  constexpr u32 kBlock = WAVES > kWaves ? WAVES * kWave : kThreads;
+  __shared__ float sums[WAVES > 1 ? WAVES : 1];
+  const u32 lanes = WAVES ? WAVES * kWave : 1u << shift, per = WAVES ? kBlock / (WAVES * kWave) : kBlock >> shift;
+  // whole vectors, and what is left behind them, the next lane's
+  const u32 q = threadIdx.x & (lanes - 1), vectors = cols / 8, rest = q == (vectors & (lanes - 1)) ? cols % 8 : 0;
+  for (u32 r0 = blockIdx.x * per; r0 < rows; r0 += gridDim.x * per) {
+    u32 mine = r0 + (WAVES ? threadIdx.x / (WAVES * kWave) : threadIdx.x >> shift);
+    if (WAVES) mine = (u32)__builtin_amdgcn_readfirstlane((int)mine);
+    const u32 r = mine < rows ? mine : rows - 1;
+    const T* const row = x + (size_t)r * ld;
+    T* const out = dx + (size_t)r * lddx;
+    const float lse = g.lse[r];
+    Vec8<T> held[HELD], tail = {};
+    const auto load = [&](u32 base) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (base + i * lanes < vectors) held[i] = load_wide(row + (base + i * lanes) * 8);
+    };
+    float z = 0.0f;
+    const auto add = [&](const Vec8<T>& v) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z += __builtin_amdgcn_exp2f(((float)v.get(j) - lse) * kLog2e);
+    };
+    if (rest) tail = load_some(row + vectors * 8, (int)rest, (T)neg_inf());
+    for (u32 base = q + HELD * lanes; base < vectors; base += HELD * lanes) {
+      load(base);
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (base + i * lanes < vectors) add(held[i]);
+    }
+    load(q);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (q + i * lanes < vectors) add(held[i]);
+    if (rest) add(tail);
+    for (u32 d = 1; d < (lanes < kWave ? lanes : kWave); d <<= 1) z += lane_read(z, (int)(lane_id() ^ d));
+    if (WAVES > 1) {
+      if (lane_id() == 0) sums[threadIdx.x / kWave] = z;
+      __syncthreads();
+      z = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) z += sums[w];
+      __syncthreads();
+    }
+    const float dh = g.dentropy ? g.dentropy[r] : 0.0f, by = 1.0f / z, log_p = g.entropy[r] - logf(z);
     const int label = g.label[r];
     const float dlogp = (u32)label < cols ? g.dlogp[r] : 0.0f;
-    float given = dlogp, extra[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) extra[j] = (u32)label == col + j ? dlogp : 0.0f;
-    if (g.dtop) {
-      for (int k = 0; k < top; ++k) {
-        const int i = g.top_index[(size_t)r * top + k];
-        const float d = (u32)i < cols ? g.dtop[(size_t)r * top + k] : 0.0f;
-        given += d;
-        if ((u32)i - col < 8u) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) extra[j] += (u32)i == col + j ? d : 0.0f;
-        }
+    const int* const top_index = g.top_index + (size_t)r * top;
+    const float* const dtop = g.dtop + (size_t)r * top;
+    float given = dlogp;
+    u32 hits = 0;  // which of this lane's vectors hold alternatives, bit by bit, the last bit for all from the 32nd on
+    const auto turn_of = [&](u32 vector) { return lowest(WAVES ? vector / (WAVES * kWave) : vector >> shift, 32); };
+    if (TOP) {
+#pragma unroll 4
+      for (int k = 0; k < top; ++k) {  // (without a branch: the loads of several are on their way together)
+        const u32 at = (u32)top_index[k];
+        const float d = dtop[k];
+        given += at < cols ? d : 0.0f;
+        hits |= (at / 8 & (lanes - 1)) == q ? 1u << turn_of(at / 8) : 0u;
       }
     }
-    Vec8<T> res = {};
+    const auto result = [&](Vec8<T> v, u32 col) {
+      // the words alone are kept, rather than the exponentials of all: registers are short
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float lp = (float)in.get(j) - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      const float d = (p == 0.0f ? 0.0f : p * (-given - dh * (lp + entropy))) + extra[j];
-      res.set(j, (T)(lse == neg_inf() ? 0.0f : d));
+      for (u32 n = 0; n < sizeof(T) / 2; ++n) asm volatile("" : "+v"(v.w[n]));
+      float d[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float far = (float)v.get(j) - lse, p = __builtin_amdgcn_exp2f(far * kLog2e) * by;
+        d[j] = p == 0.0f ? 0.0f : p * (-given - dh * (far + log_p));
+      }
+      const auto give = [&](u32 at, float more) {
+        const u32 place = at - col;
+        if (place < 8u && at < cols) {
+#pragma unroll
+          for (u32 j = 0; j < 8; ++j) d[j] += place == j ? more : 0.0f;
+        }
+      };
+      give((u32)label, dlogp);
+      if (TOP && (hits >> turn_of(col / 8) & 1))
+        for (int k = 0; k < top; ++k) {
+          const u32 at = (u32)top_index[k];
+          if (at - col < 8u) give(at, dtop[k]);
+        }
+      Vec8<T> res = {};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) res.set(j, (T)(lse == neg_inf() ? 0.0f : d[j]));
+      return res;
+    };
+    const auto put = [&](u32 base) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) {
+        if (base + i * lanes < vectors) store_wide(out + (base + i * lanes) * 8, result(held[i], (base + i * lanes) * 8));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (mine >= rows) continue;
+    put(q);
+    for (u32 base = q + HELD * lanes; base < vectors; base += HELD * lanes) {
+      load(base);
+      put(base);
     }
-    if (col + 8 <= cols) store_wide(out + col, res);
-    else store_some(out + col, res, (int)(cols - col));
+    if (rest) store_some(out + vectors * 8, result(tail, vectors * 8), (int)rest);
   }
 }
 
@@ -412,9 +489,30 @@ int label_forward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, c
 
 template <class T>
 int label_backward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, const GradIn& g, T* dx, size_t lddx, hipStream_t st) {
-  const size_t need = ceil_div(rows * ceil_div(cols, 8), kThreads);
-  hipLaunchKernelGGL((k_labels_grad<T>), dim3((unsigned)(need < 8192 ? need : 8192)), dim3(kThreads), 0, st, x, ld, (u32)rows, (u32)cols, (int)top, g, dx,
-                     lddx);
+  // Few rows to a wavefront where they fill its lanes, few wavefronts to a row where they hold it: barriers and idle lanes cost more than the
+  // registers. us by groups and by wavefronts: 16384 x 2000 bfloat16 26 and 28, x 1000 float32 24 and 26. By one wavefront and by four: 16384
+  // x 2500 bfloat16 37 and 53, x 4000 50 and 50, x 4100 54 and 62, x 5000 69 and 71; float32 x 2500 62 and 80, x 4000 101 and 93, x 5000 137 and
+  // 117. By four and by eight: 8192 x 12000 bfloat16 76 and 90, x 16500 106 and 129; float32 x 16500 211 and 203. By eight and by
+  // sixteen: 4096 x 32768 bfloat16 112 and 125, x 33000 120 and 133, 2048 x 131072 250 and 237; float32 x 131072 562 and 510. Rows of 16 bits
+  // are so taken on to a quarter more than is held.
+  constexpr int kHeld = sizeof(T) == 2 ? 4 : 2;  // vectors of a lane in a group: 64 bytes
+  u32 shift = 0;  // of a group's lanes
+  while ((size_t)(8 * kHeld) << shift < cols && shift < 6) ++shift;
+#define HAFLO_LOCAL_RUN(WAVES, HELD, PER, THREADS)                                                                                     \
+  do {                                                                                                                               \
+    const dim3 grid((unsigned)(ceil_div(rows, PER) < kGradBlocks ? ceil_div(rows, PER) : kGradBlocks)), block(THREADS);              \
+    if (g.dtop)                                                                                                                      \
+      hipLaunchKernelGGL((k_labels_grad<T, WAVES, HELD, true>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, shift, g, dx, lddx); \
+    else                                                                                                                             \
+      hipLaunchKernelGGL((k_labels_grad<T, WAVES, HELD, false>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, 0, shift, g, dx, lddx); \
+  } while (0)
+  constexpr size_t kFull = 8 * kWave * 8, kPast = sizeof(T) == 2 ? kFull * 5 / 4 : kFull;  // what a wavefront holds, and how far it goes
+  if (cols <= 8 * kWave * kHeld) HAFLO_LOCAL_RUN(0, kHeld, (size_t)kThreads >> shift, kThreads);
+  else if (cols <= kPast) HAFLO_LOCAL_RUN(1, 8, kWaves, kThreads);
+  else if (cols <= 4 * kPast) HAFLO_LOCAL_RUN(4, 8, 1, 4 * kWave);
+  else if (cols <= 8 * kPast) HAFLO_LOCAL_RUN(8, 8, 1, 8 * kWave);
+  else HAFLO_LOCAL_RUN(16, 4, 1, 16 * kWave);
+#undef HAFLO_LOCAL_RUN
   return launched();
 }
 

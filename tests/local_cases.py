@@ -336,3 +336,52 @@ def check_adapters_own_infinities(run, kind):
         else:
             for got, was in zip((y, dx), few):
                 assert torch.equal(got[:256].nan_to_num(7e3), was.nan_to_num(7e3))
+
+
+# --------------------------------------------------------------------------------------------------- labels, far from zero
+
+LABELS_FAR = [  # type, rows, cols, pad, first, top, shift of the logits, mask
+    ("f32", 70, 2, 0, 0, 1, 0.0, "low"), ("f32", 5, 7, 1, 0, 2, 1e5, ""), ("f32", 9, 33, 0, 1, 3, 1e4, "low"), ("bf16", 9, 8, 0, 0, 1, 0.0, "low"),
+    ("f16", 30, 100, 3, 0, 5, 3e4, "inf"), ("f32", 4, 512, 0, 0, 0, -1e5, ""), ("f32", 5, 515, 2, 0, 4, 1e6, "inf"), ("bf16", 3, 700, 0, 0, 0, 1e4, "low"),
+    ("f32", 3, 2100, 0, 0, 9, 1e5, "low"), ("bf16", 2, 9000, 0, 0, 3, 0.0, "low"), ("f32", 2, 9000, 1, 1, 0, -1e4, ""), ("f16", 2, 33001, 0, 0, 2, 0.0, "low"),
+    ("f32", 2, 40000, 0, 0, 0, 1e9, "low"), ("bf16", 1, 300001, 0, 0, 20, 0.0, ""),
+]
+
+
+def check_labels_far(run, kind, rows, cols, pad, first, top, shift, mask):
+    """The gradient's accuracy does not depend on where a row's logits lie, as lse's does. A probability is off by its exponential, whose
+    argument is rounded and multiplied, and by the sum of the row's; nothing grows with the maximum."""
+    x, label, gen = label_inputs(kind, rows, cols, pad, first, "")
+    x.copy_((x.float() + shift).to(x.dtype))
+    if mask:
+        value = -math.inf if mask == "inf" else torch.finfo(x.dtype).min
+        x[torch.rand(rows, cols, generator=gen) < 0.5] = value
+        x[-1] = value
+    _, _, _, _, index, _, _, has, some = label_exact(x, label, top)
+    away = torch.where(some[:, None], x.double() - torch.where(some, x.double().amax(1), 0.0)[:, None], -math.inf)  # (64 bits do not hold lse either)
+    lp = torch.where(some[:, None], away - torch.exp(away).sum(1, keepdim=True).log(), -math.inf)
+    prob = torch.exp(lp)
+    entropy = -torch.where(prob > 0, prob * lp, 0.0).sum(1)
+    got = run.label_logprobs(x, label, top)
+    near(got[1], entropy, 2.0 ** -23 * (40 + 2 * entropy + cols / 64) * (1 + entropy))
+    dlogp, dh = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen)
+    dtop = torch.randn(rows, top, generator=gen) if top else None
+    given = torch.where(has, dlogp, 0.0).double()
+    one = torch.zeros(rows, cols, dtype=torch.float64)
+    one[torch.arange(rows)[has], label[has].long()] += dlogp[has].double()
+    if top:
+        one.scatter_add_(1, index, dtop.double())
+        given = given + dtop.double().sum(1)
+    safe = torch.where(prob > 0, lp, 0.0)
+    mean = (prob * safe.abs()).sum(1, keepdim=True)
+    for d in (torch.zeros(rows), dh):
+        dx = run.label_logprobs_backward(x, label, got[2], got[1], dlogp, d if d is dh else None, index.to(torch.int32) if top else None, dtop)
+        d = d.double()
+        want = torch.where(some[:, None], prob * (-given[:, None] - d[:, None] * (safe + entropy[:, None])) + one, 0.0)
+        ulp = 2.0 ** -23
+        far = torch.where(prob > 0, (x.double() - got[2].double()[:, None]).abs(), 0.0)  # what the exponentials are taken of
+        of_p = ulp * (40 + 2 * far + 2 * (prob * far).sum(1, keepdim=True) + cols / 64 + top)
+        of_entropy = ulp * (40 + 2 * mean + cols / 64) * (1 + mean)
+        weight = prob * (given.abs()[:, None] + (dtop.abs().double().sum(1, keepdim=True) if top else 0.0) + d.abs()[:, None] * (safe.abs() + entropy[:, None] + 1))
+        room = UNIT[x.dtype] * want.abs() + weight * of_p + prob * d.abs()[:, None] * (of_p + of_entropy) + 2 * (top + 2) * ulp * one.abs() + TINY[x.dtype]
+        near(dx, want, torch.where(some[:, None], room, 0.0))

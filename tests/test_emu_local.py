@@ -190,3 +190,8 @@ def test_adapters_cancelling(run, kind, rows):
 @pytest.mark.parametrize("kind", cases.TYPES)
 def test_adapters_own_infinities(run, kind):
     cases.check_adapters_own_infinities(run, kind)
+
+
+@pytest.mark.parametrize("case", cases.LABELS_FAR, ids=str)
+def test_labels_far(run, case):
+    cases.check_labels_far(run, *case)

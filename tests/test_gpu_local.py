@@ -338,3 +338,22 @@ def test_adapters_cancelling(run, kind, rows):
 @pytest.mark.parametrize("kind", cases.TYPES)
 def test_adapters_own_infinities(run, kind):
     cases.check_adapters_own_infinities(run, kind)
+
+
+@pytest.mark.parametrize("case", cases.LABELS_FAR, ids=str)
+def test_labels_far(run, case):
+    cases.check_labels_far(run, *case)
+
+
+@pytest.mark.parametrize("cols", [2, 33, 700, 1500, 4000, 9000, 33001, 50000])
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_labels_gradient_in_place(api, kind, cols):
+    """Every form of the gradient reads a row before it writes it."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    logits = torch.randn(37, cols, generator=g, device="cuda").to(cases.TYPES[kind])
+    label = torch.randint(-1, cols, (37,), generator=g, device="cuda").to(torch.int32)
+    _, entropy, lse, _, index = api.haflo_label_logprobs(logits, label, 2)
+    dlogp, dh, dtop = (torch.randn(37, *s, generator=g, device="cuda") for s in ((), (), (2,)))
+    want = api.haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dh, index, dtop)
+    got = api.haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dh, index, dtop, out=logits)
+    assert got is logits and torch.equal(got, want)
