@@ -21,7 +21,7 @@ constexpr size_t kSplitCols = 2048;  // columns of one part of a row, at least
 constexpr size_t kSplitBlocks = 1024;
 constexpr int kAhead = 4;            // vectors on their way at a time
 constexpr size_t kGradBlocks = 1 << 21;  // blocks of a launch at most, which loop over the rows
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = (float)(1.44269504088896341 - (double)kLog2e), kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
@@ -405,8 +405,11 @@ __global__ __launch_bounds__(WAVES > kWaves ? WAVES * kWave : kThreads, 4) void 
       float d[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float far = (float)v.get(j) - lse, p = __builtin_amdgcn_exp2f(far * kLog2e) * by;
-        d[j] = p == 0.0f ? 0.0f : p * (-given - dh * (far + log_p));
+        const float far = (float)v.get(j) - lse, product = far * kLog2e;
+        float p = __builtin_amdgcn_exp2f(product) * by;
+        // what the product's rounding took from the exponent, 2^-24 of it, shows in 32-bit results alone
+        const float more = sizeof(T) == 4 ? (fmaf(far, kLog2e, -product) + far * kLog2eRest) * kLn2 : 0.0f;
+        d[j] = p == 0.0f ? 0.0f : fmaf(p, more, p) * (-given - dh * (far + log_p));
       }
       const auto give = [&](u32 at, float more) {
         const u32 place = at - col;

@@ -385,3 +385,22 @@ def check_labels_far(run, kind, rows, cols, pad, first, top, shift, mask):
         weight = prob * (given.abs()[:, None] + (dtop.abs().double().sum(1, keepdim=True) if top else 0.0) + d.abs()[:, None] * (safe.abs() + entropy[:, None] + 1))
         room = UNIT[x.dtype] * want.abs() + weight * of_p + prob * d.abs()[:, None] * (of_p + of_entropy) + 2 * (top + 2) * ulp * one.abs() + TINY[x.dtype]
         near(dx, want, torch.where(some[:, None], room, 0.0))
+
+
+def check_labels_far_columns(run):
+    """Columns far below the maximum in float32: their exponentials are as exact as the near ones'. The maximum is 0, and so is lse, whose sum
+    the others do not reach; x - lse is exact, and a column's gradient is off by one exponential and a few products."""
+    gen = torch.Generator().manual_seed(11)
+    x = -torch.rand(40, 100, generator=gen) * 55 - 25
+    x[:, 3] = 0.0
+    x[:, 70] = -math.inf
+    label, given = torch.full((40,), -1, dtype=torch.int32), torch.randn(40, 2, generator=gen)
+    label[::2] = 3
+    got = run.label_logprobs(x, label, 2)
+    assert not got[2].any() and bool((got[4][:, 0] == 3).all())
+    dx = run.label_logprobs_backward(x, label, got[2], got[1], given[:, 0].contiguous(), None, got[4], torch.stack((given[:, 1], torch.zeros(40)), 1))
+    want = -torch.exp(x.double()) * (torch.where(label >= 0, given[:, 0], 0.0) + given[:, 1])[:, None].double()
+    others = torch.arange(100) != 3
+    # 2 units of the exponential, its argument's rounding put back to 2^-24 of it, four products, the sum of what is given
+    size = torch.exp(x.double()) * given.double().abs().sum(1, keepdim=True)
+    near(dx[:, others], want[:, others], (8 * 2.0 ** -24 * size + 2.0 ** -149)[:, others])

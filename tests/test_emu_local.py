@@ -195,3 +195,7 @@ def test_adapters_own_infinities(run, kind):
 @pytest.mark.parametrize("case", cases.LABELS_FAR, ids=str)
 def test_labels_far(run, case):
     cases.check_labels_far(run, *case)
+
+
+def test_labels_far_columns(run):
+    cases.check_labels_far_columns(run)

@@ -357,3 +357,7 @@ def test_labels_gradient_in_place(api, kind, cols):
     want = api.haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dh, index, dtop)
     got = api.haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dh, index, dtop, out=logits)
     assert got is logits and torch.equal(got, want)
+
+
+def test_labels_far_columns(run):
+    cases.check_labels_far_columns(run)
