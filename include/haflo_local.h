@@ -40,7 +40,8 @@ enum haflo_type { HAFLO_F32 = 0, HAFLO_F16 = 1, HAFLO_BF16 = 2 };
  * numbers: as easy as 1, 2, 3", 2011): counter (col >> 3, row, low and high word of `offset`), key (low and high
  * word of `seed`); the call's four words give the draws of columns 8 (col >> 3) + 0 .. 7, the low
  * half of a word first. Dropped elements are 0 whatever x holds there. The gradient by x is the same call on
- * dy without a residual; the residual's is dy. d_y may be d_x or d_residual. 0 <= p <= 1.
+ * dy without a residual; the residual's is dy. d_y may be d_x or d_residual where the distances between rows are the same (else
+ * HAFLO_EINVAL). 0 <= p <= 1.
  */
 int haflo_dropout(int type, const void* d_x, size_t ldx, const void* d_residual, size_t ldr, void* d_y, size_t ldy,
                   size_t rows, size_t cols, double p, uint64_t seed, uint64_t offset, void* stream);
@@ -103,7 +104,7 @@ int haflo_label_logprobs(int type, const void* d_logits, size_t ld, const int32_
  * p_j = e^(x_j - lse) / sum_i e^(x_i - lse): the sum is formed again, so that nothing is lost where float32 holds lse coarsely, in
  * rows far from zero and of the lowest value only.
  * d_dentropy and d_dtop (rows x top) may be NULL: zeros. dlogp of a row without label is
- * not used; a top index outside the row is left out. d_dx may be d_logits where the distances between rows are the same.
+ * not used; a top index outside the row is left out. d_dx may be d_logits where the distances between rows are the same (else HAFLO_EINVAL).
  */
 int haflo_label_logprobs_backward(int type, const void* d_logits, size_t ld, const int32_t* d_label, const float* d_lse,
                                   const float* d_entropy, const float* d_dlogp, const float* d_dentropy,

@@ -147,6 +147,10 @@ inline bool valid_type(int type) { return type == HAFLO_F32 || type == HAFLO_F16
 inline size_t type_size(int type) { return type == HAFLO_F32 ? 4 : 2; }
 inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
+// Whether an output may lie where an input does: each element over its own, so with rows equally far apart.
+inline bool in_place(const void* in, size_t ld_in, const void* out, size_t ld_out, size_t rows) {
+  return in != out || ld_in == ld_out || rows <= 1;
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? HAFLO_OK : HAFLO_EHIP; }
 
 }  // namespace local

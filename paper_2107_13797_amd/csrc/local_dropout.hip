@@ -56,6 +56,7 @@ extern "C" int haflo_dropout(int type, const void* d_x, size_t ldx, const void* 
   if (!valid_type(type) || !(p >= 0.0 && p <= 1.0) || rows > kMostCount || cols > kMostCount) return HAFLO_EINVAL;
   if (rows == 0 || cols == 0) return HAFLO_OK;
   if (!d_x || !d_y || ldx < cols || ldy < cols || (d_residual && ldr < cols)) return HAFLO_EINVAL;
+  if (!in_place(d_x, ldx, d_y, ldy, rows) || !in_place(d_residual, ldr, d_y, ldy, rows)) return HAFLO_EINVAL;
   const Drop d = make_drop(p, seed, offset);
   HAFLO_LOCAL_TYPES(type, return dropout<T>(d_x, ldx, d_residual, ldr, d_y, ldy, rows, cols, d, (hipStream_t)stream));
 }

@@ -547,6 +547,7 @@ int haflo_label_logprobs_backward(int type, const void* d_logits, size_t ld, con
   if (rows == 0) return HAFLO_OK;
   if (!d_logits || ld < cols || !d_label || !d_lse || !d_entropy || !d_dlogp || (d_dtop && top && !d_top_index) || !d_dx || lddx < cols)
     return HAFLO_EINVAL;
+  if (!in_place(d_logits, ld, d_dx, lddx, rows)) return HAFLO_EINVAL;
   const GradIn g = {d_label, d_lse, d_entropy, d_dlogp, d_dentropy, d_top_index, top ? d_dtop : nullptr};
   HAFLO_LOCAL_TYPES(type, return label_backward<T>((const T*)d_logits, ld, rows, cols, top, g, (T*)d_dx, lddx, (hipStream_t)stream));
 }

@@ -199,3 +199,17 @@ def test_labels_far(run, case):
 
 def test_labels_far_columns(run):
     cases.check_labels_far_columns(run)
+
+
+def test_in_place_refusals(run):
+    """A result over an input whose rows lie at another distance would be written where other rows are still read."""
+    lib, one, two = run.lib, run.buf(torch.zeros(64)), run.buf(torch.zeros(64))
+    p, other = one.p, two.p
+    drop = lambda x, ldx, r, ldr, y, ldy, rows: lib.haflo_dropout(0, x, ldx, r, ldr, y, ldy, rows, 8, 0.5, 1, 0, None)  # noqa: E731
+    assert drop(p, 8, None, 0, p, 9, 3) == -1 and drop(p, 16, None, 0, p, 8, 3) == -1 and drop(other, 8, p, 12, p, 8, 3) == -1
+    assert drop(p, 9, None, 0, p, 9, 3) == 0 and drop(other, 8, p, 9, p, 9, 3) == 0 and drop(p, 8, p, 8, p, 8, 3) == 0
+    assert drop(p, 9, None, 0, p, 8, 1) == 0 and drop(p, 8, None, 0, other, 9, 3) == 0
+    row = run.buf(torch.zeros(8))
+    grad = lambda x, ld, dx, lddx, rows: lib.haflo_label_logprobs_backward(0, x, ld, row.p, row.p, row.p, row.p, None, None, None, rows, 8, 0, dx, lddx, None)  # noqa: E731
+    assert grad(p, 8, p, 9, 3) == -1 and grad(p, 9, p, 8, 3) == -1
+    assert grad(p, 9, p, 9, 3) == 0 and grad(p, 8, p, 9, 1) == 0

@@ -361,3 +361,15 @@ def test_labels_gradient_in_place(api, kind, cols):
 
 def test_labels_far_columns(run):
     cases.check_labels_far_columns(run)
+
+
+def test_in_place_refusals(api):
+    wide = torch.zeros(4, 16, device="cuda")
+    dense = torch.as_strided(wide, (4, 8), (8, 1))
+    zero, label = torch.zeros(4, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    for x, out in ((wide[:, :8], dense), (dense, wide[:, :8])):
+        for call in (lambda: api.haflo_dropout(x, 0.5, 1, out=out), lambda: api.haflo_dropout(x.clone(), 0.5, 1, residual=x, out=out),
+                     lambda: api.haflo_label_logprobs_backward(x, label, zero, zero, zero, out=out)):
+            with pytest.raises(api.HafloError):
+                call()
+    assert api.haflo_dropout(wide[:, :8], 0.5, 1, out=wide[:, :8]).shape == (4, 8)
