@@ -18,8 +18,8 @@
  * same device gives the same bits.
  *
  * Matrices are row-major; `ld*` is the distance between rows in elements, at
- * least the row's length. Elements need no more alignment than their type's. Outputs may not
- * overlap inputs except where it says so. Counts are below 2^31.
+ * least the row's length. Elements need no more alignment than their type's, a workspace that of 16 bytes (else HAFLO_EINVAL). Outputs
+ * may not overlap inputs except where it says so. Counts are below 2^31.
  */
 #ifndef HAFLO_LOCAL_H
 #define HAFLO_LOCAL_H

@@ -1266,7 +1266,7 @@ int haflo_adapter_forward(int type, const void* d_x, size_t ldx, const void* d_w
   if (rows == 0) return HAFLO_OK;
   if (!d_x || ldx < inner || !d_w || ldw < inner || !d_a || !d_b || !d_scale || !d_index || !d_y || ldy < outer || !d_h) return HAFLO_EINVAL;
   const Plan plan = adapter_plan(type, false, s);
-  if (!d_workspace || workspace_bytes < plan.total) return HAFLO_EINVAL;
+  if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;
   char* const ws = (char*)d_workspace;
   const hipStream_t st = (hipStream_t)stream;
   const Drop d = make_drop(p, seed, offset);
@@ -1304,7 +1304,7 @@ int haflo_adapter_backward(int type, const void* d_dy, size_t lddy, const void* 
   if (!d_w || ldw < inner || !d_a || !d_b || !d_scale || !d_da || !d_db) return HAFLO_EINVAL;
   if (rows && (!d_dy || lddy < outer || !d_x || ldx < inner || !d_index || !d_h || (d_dx && lddx < inner))) return HAFLO_EINVAL;
   const Plan plan = adapter_plan(type, true, s);
-  if (!d_workspace || workspace_bytes < plan.total) return HAFLO_EINVAL;
+  if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;
   char* const ws = (char*)d_workspace;
   const hipStream_t st = (hipStream_t)stream;
   const Drop d = make_drop(p, seed, offset);

@@ -151,6 +151,10 @@ inline size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
 inline bool in_place(const void* in, size_t ld_in, const void* out, size_t ld_out, size_t rows) {
   return in != out || ld_in == ld_out || rows <= 1;
 }
+// Whether a workspace does for a call that needs `bytes`: its parts are read sixteen bytes at a time.
+inline bool enough(const void* ws, size_t ws_bytes, size_t bytes) {
+  return bytes == 0 || (ws && (uintptr_t)ws % 16 == 0 && ws_bytes >= bytes);
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? HAFLO_OK : HAFLO_EHIP; }
 
 }  // namespace local

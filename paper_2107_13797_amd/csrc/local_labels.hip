@@ -534,7 +534,7 @@ int haflo_label_logprobs(int type, const void* d_logits, size_t ld, const int32_
   if (rows == 0) return HAFLO_OK;
   if (!d_logits || ld < cols || !d_label || !d_logp || !d_entropy || !d_lse || (top && (!d_top_logp || !d_top_index))) return HAFLO_EINVAL;
   const size_t bytes = label_bytes(rows, cols, top);
-  if (bytes && (!d_workspace || workspace_bytes < bytes)) return HAFLO_EINVAL;
+  if (!enough(d_workspace, workspace_bytes, bytes)) return HAFLO_EINVAL;
   const LabelOut o = {d_label, d_logp, d_entropy, d_lse, d_top_logp, d_top_index, d_status};
   HAFLO_LOCAL_TYPES(type, return label_forward<T>((const T*)d_logits, ld, rows, cols, top, o, d_workspace, (hipStream_t)stream));
 }

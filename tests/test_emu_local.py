@@ -213,3 +213,21 @@ def test_in_place_refusals(run):
     grad = lambda x, ld, dx, lddx, rows: lib.haflo_label_logprobs_backward(0, x, ld, row.p, row.p, row.p, row.p, None, None, None, rows, 8, 0, dx, lddx, None)  # noqa: E731
     assert grad(p, 8, p, 9, 3) == -1 and grad(p, 9, p, 8, 3) == -1
     assert grad(p, 9, p, 9, 3) == 0 and grad(p, 8, p, 9, 1) == 0
+
+
+def test_workspace_alignment(run):
+    """A workspace off a 16-byte boundary is refused, whatever it has room for."""
+    lib = run.lib
+    need = [lib.haflo_adapter_workspace_bytes(0, b, 300, 8, 8, 1, 4) for b in (0, 1)] + [lib.haflo_label_workspace_bytes(0, 1, 9000, 4)]
+    some, ws = run.buf(torch.zeros(300 * 8)), run.buf(torch.zeros(max(need) + 16, dtype=torch.uint8))
+    index, p = run.buf(torch.zeros(300, dtype=torch.int32)), some.p
+    out = [run.buf(torch.zeros(300 * 8)) for _ in range(4)]
+    for off in (0, 4, 8):
+        args = (ws.p + off, need[0], None)
+        got = [lib.haflo_adapter_forward(0, p, 8, p, 8, p, p, p, index.p, 300, 8, 8, 1, 4, 0.0, 0, 0, out[0].p, 8, out[1].p, None, *args)]
+        args = (ws.p + off, need[1], None)
+        got += [lib.haflo_adapter_backward(0, p, 8, p, 8, p, 8, p, p, p, index.p, p, 300, 8, 8, 1, 4, 0.0, 0, 0, out[0].p, 8, out[1].p, out[2].p, None, *args)]
+        args = (ws.p + off, need[2], None)
+        wide = run.buf(torch.zeros(9000))
+        got += [lib.haflo_label_logprobs(0, wide.p, 9000, index.p, 1, 9000, 4, out[0].p, out[1].p, out[2].p, out[3].p, index.p, None, *args)]
+        assert got == ([0, 0, 0] if off == 0 else [-1, -1, -1])
