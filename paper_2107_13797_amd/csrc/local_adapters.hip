@@ -93,11 +93,11 @@ constexpr int kShrinkWaves = 4;
 template <class T, int RT>
 __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, size_t ldx, const T* f, size_t f_ld, const float* scale, const int* index,
                                                                  const u32* order, u32 rows, u32 inner, u32 rank, u32 parties, Drop d, u32 parts,
-                                                                 u32 z_ld, float* z, float* h, u32* status) {
+                                                                 u32 z_ld, float* z, float* h, u32* status, u32 first_block) {
   constexpr int kAhead = RT == 1 ? 4 : 2;  // steps whose operands are on their way together
   __shared__ float sum[kShrinkWaves][RT][16][17];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 at0 = blockIdx.x / parts * 16, part = blockIdx.x % parts;
+  const u32 block = first_block + blockIdx.x, at0 = block / parts * 16, part = block % parts;
   const auto row_at = [&](u32 i) { return at0 + i >= rows ? rows : order[at0 + i]; };
   const u32 mine = row_at(lane % 16);
   const int raw = mine < rows ? index[mine] : -1;
@@ -383,7 +383,8 @@ __device__ __forceinline__ void reduce(const From& x, const typename From::At (&
 template <class T, int TM, int TN, int WM, int WN, bool DROP, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
                                                              const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
-                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, u32 x_bytes, u32 w_bytes) {
+                                                             u32 outer, u32 parties, u32 ranks, Drop d, T* y, size_t ldy, u32 x_bytes, u32 w_bytes,
+                                                             u32 first_block) {
   constexpr int KE = step_elems<T>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
   constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
   __shared__ __align__(16) T lds[2 * (TM + TN) * KE];
@@ -395,8 +396,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
   // Blocks are dealt to the eight dies in turn: each gets neighbouring tiles, four tiles of rows by all outputs at a time,
   // whose operands its cache holds.
   const u32 tiles_m = (rows + TM - 1) / TM, tiles_n = (outer + TN - 1) / TN, tiles = tiles_m * tiles_n;
-  const u32 die = blockIdx.x % 8, per = tiles / 8, over = tiles % 8;
-  const u32 tile = die * per + (die < over ? die : over) + blockIdx.x / 8;
+  const u32 block = first_block + blockIdx.x, die = block % 8, per = tiles / 8, over = tiles % 8;
+  const u32 tile = die * per + (die < over ? die : over) + block / 8;
   const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
   const u32 t0 = (band * 4 + in_band % high) * TM, o0 = in_band / high * TN;
   const u32 row0 = wave / WN * (TM / WM), out0 = wave % WN * (TN / WN);  // this wavefront's corner
@@ -594,12 +595,13 @@ template <class T, int RT, int ZT>
 __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, size_t f_ld,
                                                            const float* scale, const int* index, u32 rows, u32 inner, u32 outer, u32 rank,
                                                            u32 parties, Drop d, u32 parts, u32 z_parts, u32 z_ld, float* sums, float* z,
-                                                           u32* status) {
+                                                           u32* status, u32 first_block) {
   __shared__ __align__(16) char lds[RT * 16 * kRowBytes];  // tiles of x, then halves of sums; or parts of z
   constexpr u32 kGroup = RT * 16;
   const u32 tiles = (outer + 63) / 64 * parts, products = (rows + kGroup - 1) / kGroup * tiles;
-  if (blockIdx.x < products) {
-    const u32 t0 = blockIdx.x / tiles * kGroup, at = blockIdx.x % tiles, count = rows - t0 < kGroup ? rows - t0 : kGroup;
+  const u32 block = first_block + blockIdx.x;
+  if (block < products) {
+    const u32 t0 = block / tiles * kGroup, at = block % tiles, count = rows - t0 < kGroup ? rows - t0 : kGroup;
     const T* const x0 = x + (size_t)t0 * ldx;
     float* const to = sums + (size_t)t0 * outer;
     const size_t step = (size_t)rows * outer;
@@ -610,7 +612,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
   float(*const lz)[ZT * 16] = (float(*)[ZT * 16])lds;
   constexpr int kAhead = ZT == 1 ? 4 : 2;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const u32 t = (blockIdx.x - products) / z_parts, part = (blockIdx.x - products) % z_parts;
+  const u32 t = (block - products) / z_parts, part = (block - products) % z_parts;
   const int raw = index[t], a = party_of(index, t, parties);
   if (status && part == 0 && threadIdx.x == 0 && raw != a && raw != -1) atomicOr(status, HAFLO_ST_RANGE);
   float* const to = z + ((size_t)part * rows + t) * z_ld;
@@ -676,9 +678,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
 template <class T, bool DROP>
 __global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const float* z, const T* f, u32 f_ld, const int* index, u32 rows, u32 outer,
                                                        u32 parties, u32 rank, Drop d, u32 parts, u32 z_parts, u32 z_ld, T* y, size_t ldy,
-                                                       float* z_out, float* h) {
+                                                       float* z_out, float* h, u32 first_block) {
   __shared__ float zl[HAFLO_ADAPTER_MAX_RANK];
-  const u32 blocks = (outer + kThreads - 1) / kThreads, t = blockIdx.x / blocks, o = blockIdx.x % blocks * kThreads + threadIdx.x;
+  const u32 block = first_block + blockIdx.x, blocks = (outer + kThreads - 1) / kThreads, t = block / blocks, o = block % blocks * kThreads + threadIdx.x;
   float m = 0.0f;
   if (o < outer && y)
 #pragma unroll 4
@@ -687,7 +689,7 @@ __global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const 
     float s = 0.0f;
     for (u32 p = 0; p < z_parts; ++p) s += z[((size_t)p * rows + t) * z_ld + threadIdx.x];
     zl[threadIdx.x] = s;
-    if (blockIdx.x % blocks == 0) {
+    if (block % blocks == 0) {
       if (z_out) z_out[(size_t)t * z_ld + threadIdx.x] = s;
       if (h && threadIdx.x < rank) h[(size_t)t * rank + threadIdx.x] = s;
     }
@@ -842,9 +844,9 @@ __device__ void group_rows(const Group& g, u32* counts) {
 }
 
 template <class T>
-__global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p) {
+__global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p, u32 first_block) {
   __shared__ __align__(16) u32 lds[kGroupCounts];
-  u32 block = blockIdx.x;
+  u32 block = first_block + blockIdx.x;
   if (p.grouped) {
     if (block == 0) {
       group_rows(p.group, lds);
@@ -910,12 +912,12 @@ struct GradOf {
 template <class T, int RT>
 __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32 rank, u32 parties, const u32* __restrict__ begin,
                                                    const u32* __restrict__ chunk_begin, const u32* __restrict__ chunk,
-                                                   const u32* __restrict__ list, u32 chunk_rows) {
+                                                   const u32* __restrict__ list, u32 chunk_rows, u32 first_block) {
   constexpr int kAhead = 2, kWaves = kThreads / kWave;
   __shared__ f32x4 sum[kWaves - 1][RT][8][kWave];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   const u32 tiles_r = (rank + RT * 16 - 1) / (RT * 16), of_a = (a.cols + 127) / 128 * tiles_r, of_b = (b.cols + 127) / 128 * tiles_r;
-  const u32 c = blockIdx.x / (of_a + of_b), both = blockIdx.x % (of_a + of_b), at = both < of_a ? both : both - of_a;
+  const u32 block = first_block + blockIdx.x, c = block / (of_a + of_b), both = block % (of_a + of_b), at = both < of_a ? both : both - of_a;
   if (c >= chunk_begin[parties]) return;
   const GradOf<T> g = both < of_a ? a : b;
   const T* __restrict__ const m = g.m;
@@ -1024,10 +1026,11 @@ __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32
 // grad[p] = sum of the party's chunks, in their order. A lane takes an element; the chunks' reading bounds it (8192 rows, 8 parties,
 // 16 x 8192 weights: 9 us).
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_grad_join(GradOf<T> a, GradOf<T> b, const u32* __restrict__ chunk_begin, u32 rank) {
+__global__ __launch_bounds__(kThreads) void k_grad_join(GradOf<T> a, GradOf<T> b, const u32* __restrict__ chunk_begin, u32 rank,
+                                                     u32 first_block) {
   const size_t n_a = (size_t)rank * a.cols, n_b = (size_t)rank * b.cols;
   const u32 of_a = (u32)((n_a + kThreads - 1) / kThreads), of_b = (u32)((n_b + kThreads - 1) / kThreads);
-  const u32 p = blockIdx.x / (of_a + of_b), both = blockIdx.x % (of_a + of_b);
+  const u32 block = first_block + blockIdx.x, p = block / (of_a + of_b), both = block % (of_a + of_b);
   const GradOf<T> g = both < of_a ? a : b;
   const size_t n = both < of_a ? n_a : n_b, i = (size_t)(both < of_a ? both : both - of_a) * kThreads + threadIdx.x;
   if (i >= n) return;
@@ -1130,7 +1133,7 @@ struct Layouts {
   }
   void launch(hipStream_t st) {
     blocks += p.grouped ? 1 : 0;
-    if (blocks) hipLaunchKernelGGL((k_prepare<T>), dim3((unsigned)blocks), dim3(kPrepareThreads), 0, st, p);
+    in_turns(blocks, kPrepareThreads, [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL((k_prepare<T>), grid, block, 0, st, p, first); });
   }
 };
 template <class T>
@@ -1162,12 +1165,14 @@ struct Product {
   // z, dense as `h` too unless that is null
   void shrink(float* h) const {
     const u32 parts = shrink_parts(false, s.rows, s.inner);
-    const dim3 grid((unsigned)(ceil_div(s.rows, 16) * parts)), block(kShrinkWaves * kWave);
+    const size_t blocks = ceil_div(s.rows, 16) * parts;
     float* const to = parts > 1 ? z_parts() : z();
     float* const h_now = parts > 1 ? nullptr : h;
-#define HAFLO_LOCAL_RUN(RT)                                                                                                           \
-  hipLaunchKernelGGL((k_shrink<T, RT>), grid, block, 0, st, x.p, x.ld, low.p, low.ld, scale, index, order(), (u32)s.rows, (u32)s.inner, \
-                     (u32)s.rank, (u32)s.parties, before, parts, ranks(), to, h_now, status)
+#define HAFLO_LOCAL_RUN(RT)                                                                                                             \
+  in_turns(blocks, kShrinkWaves * kWave, [&](u32 first, dim3 grid, dim3 block) {                                                        \
+    hipLaunchKernelGGL((k_shrink<T, RT>), grid, block, 0, st, x.p, x.ld, low.p, low.ld, scale, index, order(), (u32)s.rows, (u32)s.inner, \
+                       (u32)s.rank, (u32)s.parties, before, parts, ranks(), to, h_now, status, first);                                  \
+  })
     if (s.rank <= 16) HAFLO_LOCAL_RUN(1);
     else if (s.rank <= 64) HAFLO_LOCAL_RUN(4);
     else HAFLO_LOCAL_RUN(8);
@@ -1181,11 +1186,13 @@ struct Product {
   // Few rows: y, unless it is null, and z; dense as `h` too unless that is null.
   void few_rows(float* h, T* y, size_t ldy) const {
     const u32 zp = shrink_parts(true, s.rows, s.inner), parts = few_parts(sizeof(T) == 4 ? HAFLO_F32 : HAFLO_F16, s.rows, s.inner, s.outer);
-    const dim3 grid((unsigned)(y ? ceil_div(s.rows, 64) * ceil_div(s.outer, 64) * parts + s.rows * zp : s.rows * zp)), block(kFewWaves * kWave);
+    const size_t blocks = (y ? ceil_div(s.rows, 64) * ceil_div(s.outer, 64) * parts : 0) + s.rows * zp;
     float* const sums = (float*)(ws + plan.few_sums);
-#define HAFLO_LOCAL_RUN(RT, ZT)                                                                                                            \
-  hipLaunchKernelGGL((k_few<T, RT, ZT>), grid, block, 0, st, x.p, x.ld, w.p, w.ld, low.p, low.ld, scale, index, (u32)s.rows, (u32)s.inner, \
-                     (u32)(y ? s.outer : 0), (u32)s.rank, (u32)s.parties, before, parts, zp, ranks(), sums, z_parts(), status)
+#define HAFLO_LOCAL_RUN(RT, ZT)                                                                                                              \
+  in_turns(blocks, kFewWaves * kWave, [&](u32 first, dim3 grid, dim3 block) {                                                                \
+    hipLaunchKernelGGL((k_few<T, RT, ZT>), grid, block, 0, st, x.p, x.ld, w.p, w.ld, low.p, low.ld, scale, index, (u32)s.rows, (u32)s.inner, \
+                       (u32)(y ? s.outer : 0), (u32)s.rank, (u32)s.parties, before, parts, zp, ranks(), sums, z_parts(), status, first);     \
+  })
 #define HAFLO_LOCAL_RANK(RT)                       \
   do {                                             \
     if (s.rank <= 16) HAFLO_LOCAL_RUN(RT, 1);      \
@@ -1197,10 +1204,11 @@ struct Product {
     else HAFLO_LOCAL_RANK(4);
 #undef HAFLO_LOCAL_RANK
 #undef HAFLO_LOCAL_RUN
-    const dim3 join((unsigned)(s.rows * ceil_div(s.outer, kThreads)));
-#define HAFLO_LOCAL_RUN(DROP)                                                                                                                \
-  hipLaunchKernelGGL((k_few_join<T, DROP>), join, dim3(kThreads), 0, st, (const float*)sums, (const float*)z_parts(), f.p, (u32)f.ld, index, \
-                     (u32)s.rows, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, parts, zp, ranks(), y, ldy, z(), h)
+#define HAFLO_LOCAL_RUN(DROP)                                                                                                               \
+  in_turns(s.rows * ceil_div(s.outer, kThreads), kThreads, [&](u32 first, dim3 grid, dim3 block) {                                          \
+    hipLaunchKernelGGL((k_few_join<T, DROP>), grid, block, 0, st, (const float*)sums, (const float*)z_parts(), f.p, (u32)f.ld, index,       \
+                       (u32)s.rows, (u32)s.outer, (u32)s.parties, (u32)s.rank, after, parts, zp, ranks(), y, ldy, z(), h, first);           \
+  })
     if (after.threshold) HAFLO_LOCAL_RUN(true);
     else HAFLO_LOCAL_RUN(false);
 #undef HAFLO_LOCAL_RUN
@@ -1213,10 +1221,11 @@ struct Product {
     const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
     const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
 #define HAFLO_LOCAL_RUN(TM, TN, WM, WN, DROP, FAR)                                                                                        \
-  hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP, FAR>), dim3((unsigned)(ceil_div(s.rows, TM) * ceil_div(s.outer, TN))),           \
-                     dim3(WM * WN * kWave), 0, st, x.p, x.ld, w.p, w.ld, f.p, (const float*)z(), index, order(),                          \
-                     (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(), after, y, ldy, \
-                     (u32)x_bytes, (u32)w_bytes)
+  in_turns(ceil_div(s.rows, TM) * ceil_div(s.outer, TN), WM * WN * kWave, [&](u32 first, dim3 grid, dim3 block) {                         \
+    hipLaunchKernelGGL((k_project<T, TM, TN, WM, WN, DROP, FAR>), grid, block, 0, st, x.p, x.ld, w.p, w.ld, f.p, (const float*)z(), index, \
+                       order(), (const u32*)(ws + plan.begin), (u32)s.rows, (u32)padded_inner(), (u32)s.outer, (u32)s.parties, ranks(),   \
+                       after, y, ldy, (u32)x_bytes, (u32)w_bytes, first);                                                                 \
+  })
 #define HAFLO_LOCAL_TILE(DROP)                                                                                    \
   do {                                                                                                            \
     if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, true);                                                         \
@@ -1234,18 +1243,21 @@ struct Product {
 
 template <class T>
 void grads(const GradOf<T>& a, const GradOf<T>& b, const Sizes& s, const Plan& p, char* ws, hipStream_t st) {
-  const dim3 block(kThreads);
   const u32* chunk_begin = (const u32*)(ws + p.chunk_begin);
+  const size_t columns = ceil_div(a.cols, 128) + ceil_div(b.cols, 128);
 #define HAFLO_LOCAL_RUN(RT)                                                                                                             \
-  hipLaunchKernelGGL((k_grad<T, RT>), dim3((unsigned)(p.chunks * (ceil_div(a.cols, 128) + ceil_div(b.cols, 128)) * ceil_div(s.rank, RT * 16))), \
-                     block, 0, st, a, b, (u32)s.rank, (u32)s.parties, (const u32*)(ws + p.begin), chunk_begin,                          \
-                     (const u32*)(ws + p.chunk), (const u32*)(ws + p.order), grad_rows(s))
+  in_turns(p.chunks * columns * ceil_div(s.rank, RT * 16), kThreads, [&](u32 first, dim3 grid, dim3 block) {                            \
+    hipLaunchKernelGGL((k_grad<T, RT>), grid, block, 0, st, a, b, (u32)s.rank, (u32)s.parties, (const u32*)(ws + p.begin), chunk_begin, \
+                       (const u32*)(ws + p.chunk), (const u32*)(ws + p.order), grad_rows(s), first);                                    \
+  })
   if (s.rank <= 16) HAFLO_LOCAL_RUN(1);
   else if (s.rank <= 32) HAFLO_LOCAL_RUN(2);
   else HAFLO_LOCAL_RUN(4);
 #undef HAFLO_LOCAL_RUN
   const size_t need = ceil_div(s.rank * a.cols, kThreads) + ceil_div(s.rank * b.cols, kThreads);
-  hipLaunchKernelGGL((k_grad_join<T>), dim3((unsigned)(s.parties * need)), block, 0, st, a, b, chunk_begin, (u32)s.rank);
+  in_turns(s.parties * need, kThreads, [&](u32 first, dim3 grid, dim3 block) {
+    hipLaunchKernelGGL((k_grad_join<T>), grid, block, 0, st, a, b, chunk_begin, (u32)s.rank, first);
+  });
 }
 
 }  // namespace

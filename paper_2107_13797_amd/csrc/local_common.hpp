@@ -155,6 +155,17 @@ inline bool in_place(const void* in, size_t ld_in, const void* out, size_t ld_ou
 inline bool enough(const void* ws, size_t ws_bytes, size_t bytes) {
   return bytes == 0 || (ws && (uintptr_t)ws % 16 == 0 && ws_bytes >= bytes);
 }
+// Lanes of one launch at most: the runtime counts them in 32 bits. What takes more is launched in turns, each from the block on that
+// the kernel's last argument names.
+#ifndef HAFLO_LOCAL_LANES
+#define HAFLO_LOCAL_LANES 0x80000000u
+#endif
+template <class F>
+inline void in_turns(size_t blocks, u32 threads, const F& launch) {
+  const size_t most = HAFLO_LOCAL_LANES / threads;
+  for (size_t first = 0; first < blocks; first += most)
+    launch((u32)first, dim3((unsigned)(blocks - first < most ? blocks - first : most)), dim3(threads));
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? HAFLO_OK : HAFLO_EHIP; }
 
 }  // namespace local

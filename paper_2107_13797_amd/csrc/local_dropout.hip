@@ -6,7 +6,7 @@ using namespace haflo::local;
 namespace {
 
 constexpr int kDropThreads = 256;
-constexpr int kDropBlocks = 4096;
+constexpr size_t kDropBlocks = HAFLO_LOCAL_LANES / kDropThreads < 4096 ? HAFLO_LOCAL_LANES / kDropThreads : 4096;
 
 // A lane takes eight consecutive columns of a row: one generator call and 16-byte accesses. Memory bounds it (16384 x 4096 bfloat16 with
 // a residual: 75 us, 5.4 TB/s).

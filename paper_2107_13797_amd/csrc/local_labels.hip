@@ -200,11 +200,11 @@ struct Part {  // of a row, joined by k_label_join
 // one long row the length of a part and its list (131072 columns, 20 greatest: 11 us).
 template <class T, int W, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_labels(const T* x, size_t ld, u32 rows, u32 cols, int top, u32 parts, LabelOut o,
-                                                     Part* part, u64* lists) {
+                                                     Part* part, u64* lists, u32 first_block) {
   __shared__ Soft soft[kWaves];
   __shared__ u64 list[TOP ? kWaves : 1][kWave];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-  const u32 unit = W == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
+  const u32 block = first_block + blockIdx.x, unit = W == 1 ? block * kWaves + wave : block;
   const u32 r = unit / parts, p = unit % parts;
   if (W == 1 && r >= rows) return;
   const T* row = x + (size_t)r * ld;
@@ -466,13 +466,14 @@ int label_forward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, c
   const u32 parts = label_parts(rows, cols);
   Part* part = (Part*)ws;
   u64* lists = (u64*)((char*)ws + align256(rows * parts * sizeof(Part)));
-  const dim3 block(kThreads);
   if (cols <= kSmallCols) {
-    hipLaunchKernelGGL((k_labels_small<T>), dim3((unsigned)ceil_div(rows, kThreads)), block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, o);
+    hipLaunchKernelGGL((k_labels_small<T>), dim3((unsigned)ceil_div(rows, kThreads)), dim3(kThreads), 0, st, x, ld, (u32)rows, (u32)cols, (int)top, o);
     return launched();
   }
-#define HAFLO_LOCAL_RUN(W, TOP, UNITS) \
-  hipLaunchKernelGGL((k_labels<T, W, TOP>), dim3((unsigned)(UNITS)), block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, parts, o, part, lists)
+#define HAFLO_LOCAL_RUN(W, TOP, BLOCKS)                                                                                                       \
+  in_turns(BLOCKS, kThreads, [&](u32 first, dim3 grid, dim3 block) {                                                                         \
+    hipLaunchKernelGGL((k_labels<T, W, TOP>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, parts, o, part, lists, first);       \
+  })
   if (cols <= kWaveCols || (cols <= kManyWaveCols && rows >= kManyRows)) {
     if (top) HAFLO_LOCAL_RUN(1, true, ceil_div(rows, kWaves));
     else HAFLO_LOCAL_RUN(1, false, ceil_div(rows, kWaves));
@@ -503,7 +504,8 @@ int label_backward(const T* x, size_t ld, size_t rows, size_t cols, size_t top, 
   while ((size_t)(8 * kHeld) << shift < cols && shift < 6) ++shift;
 #define HAFLO_LOCAL_RUN(WAVES, HELD, PER, THREADS)                                                                                     \
   do {                                                                                                                               \
-    const dim3 grid((unsigned)(ceil_div(rows, PER) < kGradBlocks ? ceil_div(rows, PER) : kGradBlocks)), block(THREADS);              \
+    const size_t most = HAFLO_LOCAL_LANES / (THREADS) < kGradBlocks ? HAFLO_LOCAL_LANES / (THREADS) : kGradBlocks;                   \
+    const dim3 grid((unsigned)(ceil_div(rows, PER) < most ? ceil_div(rows, PER) : most)), block(THREADS);                            \
     if (g.dtop)                                                                                                                      \
       hipLaunchKernelGGL((k_labels_grad<T, WAVES, HELD, true>), grid, block, 0, st, x, ld, (u32)rows, (u32)cols, (int)top, shift, g, dx, lddx); \
     else                                                                                                                             \

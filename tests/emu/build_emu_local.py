@@ -10,6 +10,7 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 CSRC = os.path.join(ROOT, "paper_2107_13797_amd", "csrc")
 OUT = os.path.join(HERE, "libhaflo_emu_local.so")
 OBJ = os.path.join(HERE, "_build", "local")
+NARROW = 1 << 16  # lanes of a launch at most in the library whose launches are in many turns
 CLANG = "/opt/rocm/llvm/bin/clang++"
 
 
@@ -19,25 +20,27 @@ def _run(cmd):
         raise RuntimeError("emulation build failed: %s\n%s" % (" ".join(cmd[-3:]), res.stderr[-4000:]))
 
 
-def _compile(src):
-    obj = os.path.join(OBJ, os.path.basename(src) + ".o")
+def _compile(src, flags=()):
+    obj = os.path.join(OBJ, os.path.basename(src) + (".narrow.o" if flags else ".o"))
     _run([CLANG, "-O2", "-std=c++17", "-fPIC", "-w", "-x", "c++", "-c", "-I", os.path.join(HERE, "local"), "-I", os.path.join(HERE, "include"),
-          src, "-o", obj])
+          *flags, src, "-o", obj])
     return obj
 
 
-def build():
+def build(narrow=False):
+    out = OUT.replace(".so", "_narrow.so") if narrow else OUT
+    flags = ["-DHAFLO_LOCAL_LANES=%d" % NARROW, "-DHIPEMU_LANES=%d" % NARROW] if narrow else []
     srcs = sorted(glob.glob(os.path.join(CSRC, "local_*.hip"))) + [os.path.join(HERE, "hipemu.cpp")]
     used = srcs + [os.path.join(CSRC, "local_common.hpp"), os.path.join(HERE, "include", "hip", "hip_runtime.h"),
                    os.path.join(HERE, "local", "hip", "hip_runtime.h"), os.path.join(ROOT, "include", "haflo_local.h"),
                    os.path.abspath(__file__)]
-    if os.path.exists(OUT) and os.path.getmtime(OUT) >= max(os.path.getmtime(p) for p in used):
-        return OUT
+    if os.path.exists(out) and os.path.getmtime(out) >= max(os.path.getmtime(p) for p in used):
+        return out
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=4) as pool:
-        objs = list(pool.map(_compile, srcs))
-    _run([CLANG, "-shared", "-fPIC"] + objs + ["-o", OUT])
-    return OUT
+        objs = list(pool.map(lambda src: _compile(src, flags), srcs))
+    _run([CLANG, "-shared", "-fPIC"] + objs + ["-o", out])
+    return out
 
 
 if __name__ == "__main__":

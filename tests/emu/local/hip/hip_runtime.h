@@ -4,6 +4,46 @@
 #pragma once
 #include "../../include/hip/hip_runtime.h"
 
+// A launch is limited in lanes, as on the card, and is noted by the kernel's name as the source has it.
+#include <string>
+#ifndef HIPEMU_LANES
+#define HIPEMU_LANES 0xFFFFFFFFu
+#endif
+namespace hipemu_local {
+inline std::string& launches() {
+  static std::string s;
+  return s;
+}
+inline bool& refused() {
+  static bool r = false;
+  return r;
+}
+inline bool may_launch(const char* kernel, dim3 grid, dim3 block) {
+  launches() += std::string(kernel) + "\n";
+  if ((uint64_t)grid.x * block.x <= HIPEMU_LANES) return true;
+  refused() = true;
+  return false;
+}
+inline hipError_t last_error() {
+  const bool r = refused();
+  refused() = false;
+  return r ? hipErrorInvalidValue : hipSuccess;
+}
+}  // namespace hipemu_local
+// the kernels launched since the last call
+extern "C" __attribute__((weak, used)) const char* hipemu_launches() {
+  static std::string s;
+  s.swap(hipemu_local::launches());
+  hipemu_local::launches().clear();
+  return s.c_str();
+}
+#undef hipLaunchKernelGGL
+#define hipLaunchKernelGGL(kernel, grid, block, shmem, stream, ...)                 \
+  ((void)(stream), hipemu_local::may_launch(#kernel, (grid), (block))               \
+                       ? hipemu::launch((grid), (block), [&]() { kernel(__VA_ARGS__); }) \
+                       : (void)0)
+#define hipGetLastError hipemu_local::last_error
+
 namespace hipemu_local {
 // what each lane of a wavefront brought to its current exchange; two sets, as a lane may be one exchange ahead
 struct Slots {

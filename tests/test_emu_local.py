@@ -231,3 +231,23 @@ def test_workspace_alignment(run):
         wide = run.buf(torch.zeros(9000))
         got += [lib.haflo_label_logprobs(0, wide.p, 9000, index.p, 1, 9000, 4, out[0].p, out[1].p, out[2].p, out[3].p, index.p, None, *args)]
         assert got == ([0, 0, 0] if off == 0 else [-1, -1, -1])
+
+
+@pytest.fixture(scope="module")
+def narrow():
+    """The same sources with few lanes to a launch, so that ordinary sizes take several where the card's limit would be passed."""
+    import build_emu_local
+    lib = _cabi.bind(C.CDLL(build_emu_local.build(narrow=True)), prototypes=_cabi.LOCAL_PROTOTYPES)
+    lib.hipemu_alloc.restype = C.c_void_p
+    lib.hipemu_alloc.argtypes = [C.c_size_t]
+    lib.hipemu_free.argtypes = [C.c_void_p]
+    return Emulated(lib)
+
+
+def test_launches_in_turns(run, narrow):
+    cases.check_adapters(narrow, "f32", 9000, 7, 70, 2, 300, 0.1, "mixed", 1)
+    cases.check_adapters(narrow, "bf16", 40, 16, 8200, 4, 2, 0.1, "mixed", 0)
+    cases.check_labels(narrow, "bf16", 1100, 40, 0, 0, 2, "inf")
+    cases.check_labels(narrow, "f32", 300, 2100, 0, 0, 0, "inf")
+    cases.check_labels(narrow, "f16", 300, 4110, 0, 0, 0, "")
+    cases.check_dropout(narrow, "f16", 300, 2200, 0, 0, 0.5, True)

@@ -373,3 +373,18 @@ def test_in_place_refusals(api):
             with pytest.raises(api.HafloError):
                 call()
     assert api.haflo_dropout(wide[:, :8], 0.5, 1, out=wide[:, :8]).shape == (4, 8)
+
+
+def test_labels_of_very_many_rows(api):
+    """More rows than wavefronts fit one launch, whose lanes are counted in 32 bits."""
+    rows, cols = 2 ** 26 + 5, 33
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    label = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    some = torch.tensor([0, 1, 2 ** 26 - 1, 2 ** 26, rows - 1], device="cuda")
+    x[some, 5] = torch.arange(1, 6, device="cuda").bfloat16()
+    label[some] = 5
+    logp, entropy, lse, _, _ = api.haflo_label_logprobs(x, label)
+    want = torch.full((rows,), math.log(cols), device="cuda")
+    want[some] = torch.log(cols - 1 + torch.exp(torch.arange(1, 6, device="cuda").double())).float()
+    assert float((lse - want).abs().max()) < 1e-5
+    assert float((logp[some] - (torch.arange(1, 6, device="cuda") - want[some])).abs().max()) < 1e-5 and float((logp - x[:, 5].float() + want).abs().max()) < 1e-5
