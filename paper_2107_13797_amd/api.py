@@ -327,8 +327,8 @@ def haflo_cipher_sum_segments(ctx, c, offsets, status=None):
 
 
 # The operators of a party's local step (include/haflo_local.h) work on ordinary float32, float16 and bfloat16 tensors and
-# need no Context; their workspaces come from torch's allocator call by call, in the current stream's order. Small calls take
-# as long as the host needs for them, so checks look at each property once.
+# need no Context; their workspaces come from torch's allocator call by call, in the current stream's order. Operands lie on the
+# current device, whose stream a call goes to. Small calls take as long as the host needs for them, so checks look at each property once.
 _TYPES = {torch.float32: _cabi.TYPE_F32, torch.float16: _cabi.TYPE_F16, torch.bfloat16: _cabi.TYPE_BF16}
 
 
@@ -339,10 +339,17 @@ def _type(t):
     return kind
 
 
+def _here(t):
+    device = t.get_device()  # below zero: the host
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise HafloError("expected a tensor of the current CUDA device, got one of %s" % t.device)
+
+
 def _matrix(t, dtype, rows=None, cols=None):
     """(rows, columns, distance between rows) of a matrix whose rows are contiguous and do not overlap."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype is not dtype:
-        raise HafloError("expected a CUDA matrix of %s" % dtype)
+    _here(t)
+    if t.dim() != 2 or t.dtype is not dtype:
+        raise HafloError("expected a matrix of %s" % dtype)
     r, c = t.shape
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise HafloError("expected a matrix of %s x %s, got %s x %s" % (rows, cols, r, c))
@@ -356,8 +363,19 @@ def _matrix(t, dtype, rows=None, cols=None):
 
 def _dense(t, dtype, *shape):
     """Address of a contiguous tensor of that type and shape."""
+    _here(t)
     if t.dtype is not dtype or t.shape != shape:
         raise HafloError("expected %s of shape %s, got %s of %s" % (dtype, shape, t.dtype, tuple(t.shape)))
+    if not t.is_contiguous():
+        raise HafloError("expected a contiguous tensor")
+    return t.data_ptr()
+
+
+def _status(t):
+    """Address of the word that a call's status is OR-ed into, or None."""
+    if t is None:
+        return None
+    _here(t)
     return _ptr(t)
 
 
@@ -410,7 +428,7 @@ def haflo_adapter_forward(x, w, a, b, scale, index, p=0.0, seed=0, offset=0, sta
     nbytes = lib().haflo_adapter_workspace_bytes(kind, 0, rows, inner, outer, parties, rank)
     pw, ws = _scratch(nbytes, scale)
     _check(lib().haflo_adapter_forward(kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, rows, inner, outer, parties, rank, p, seed,
-                                       offset, y.data_ptr(), outer, h.data_ptr(), _ptr(status), pw, nbytes, _stream()))
+                                       offset, y.data_ptr(), outer, h.data_ptr(), _status(status), pw, nbytes, _stream()))
     return y, h
 
 
@@ -425,7 +443,7 @@ def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offse
     pw, ws = _scratch(nbytes, scale)
     _check(lib().haflo_adapter_backward(kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, ph, rows, inner, outer,
                                         parties, rank, p, seed, offset, dx.data_ptr() if need_dx else None, inner, da.data_ptr(),
-                                        db.data_ptr(), _ptr(status), pw, nbytes, _stream()))
+                                        db.data_ptr(), _status(status), pw, nbytes, _stream()))
     return dx, da, db
 
 
@@ -442,7 +460,7 @@ def haflo_label_logprobs(logits, label, top=0, status=None):
     if top:
         top_logp, top_index = logits.new_empty((rows, top), dtype=f32), logits.new_empty((rows, top), dtype=torch.int32)
     _check(lib().haflo_label_logprobs(kind, logits.data_ptr(), ld, pl, rows, cols, top, at, at + 4 * rows, at + 8 * rows, _ptr(top_logp),
-                                      _ptr(top_index), _ptr(status), pw, nbytes, _stream()))
+                                      _ptr(top_index), _status(status), pw, nbytes, _stream()))
     logp, entropy, lse = sums.unbind()
     return logp, entropy, lse, top_logp, top_index
 
