@@ -376,7 +376,9 @@ def _status(t):
     if t is None:
         return None
     _here(t)
-    return _ptr(t)
+    if t.dtype not in (torch.int32, torch.uint32) or t.numel() < 1:
+        raise HafloError("status: expected an int32 or uint32 element, got %s of shape %s" % (t.dtype, tuple(t.shape)))
+    return t.data_ptr()
 
 
 def _scratch(nbytes, like):

@@ -83,3 +83,17 @@ def test_operands_on_one_device(monkeypatch):
                 call({n: OnDevice(t, 1 if odd in (n, None) else 0) for n, t in tensors.items()})
                 pytest.fail("call %d took %s of another device" % (number, odd or "all"))
             assert not [n for n in reached if not n.endswith("workspace_bytes")]
+
+
+def test_status_type(monkeypatch):
+    """Four bytes are written to the status: it has to be a 32-bit integer."""
+    from paper_2107_13797_amd import api
+    monkeypatch.setattr(api, "_lib", type("L", (), {"__getattr__": lambda s, n: lambda *a: 0})())
+    monkeypatch.setattr(api, "_stream", lambda: None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    for tensors, call in _calls(api):
+        if "status" not in tensors:
+            continue
+        for bad in (torch.zeros(1, dtype=torch.int8), torch.zeros(0, dtype=torch.int32), torch.zeros(1)):
+            with pytest.raises(api.HafloError):
+                call({n: OnDevice(t, 0) for n, t in dict(tensors, status=bad).items()})
