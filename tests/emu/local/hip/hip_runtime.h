@@ -18,8 +18,13 @@ inline bool& refused() {
   static bool r = false;
   return r;
 }
+inline bool& dry() {
+  static bool d = false;
+  return d;
+}
 inline bool may_launch(const char* kernel, dim3 grid, dim3 block) {
   launches() += std::string(kernel) + "\n";
+  if (dry()) return false;
   if ((uint64_t)grid.x * block.x <= HIPEMU_LANES) return true;
   refused() = true;
   return false;
@@ -37,6 +42,8 @@ extern "C" __attribute__((weak, used)) const char* hipemu_launches() {
   hipemu_local::launches().clear();
   return s.c_str();
 }
+// kernels are noted but not run
+extern "C" __attribute__((weak, used)) void hipemu_dry(int on) { hipemu_local::dry() = on != 0; }
 #undef hipLaunchKernelGGL
 #define hipLaunchKernelGGL(kernel, grid, block, shmem, stream, ...)                 \
   ((void)(stream), hipemu_local::may_launch(#kernel, (grid), (block))               \

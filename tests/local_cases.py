@@ -404,3 +404,97 @@ def check_labels_far_columns(run):
     # 2 units of the exponential, its argument's rounding put back to 2^-24 of it, four products, the sum of what is given
     size = torch.exp(x.double()) * given.double().abs().sum(1, keepdim=True)
     near(dx[:, others], want[:, others], (8 * 2.0 ** -24 * size + 2.0 ** -149)[:, others])
+
+
+# --------------------------------------------------------------------------------------------------- adapters, the forms for many rows
+
+ADAPTERS_MANY = [  # more rows than k_few takes, by tiles of 64 x 64
+    ("bf16", 300, 33, 19, 17, 3, 0.2, "mixed", 3), ("f16", 257, 70, 131, 1, 5, 0.1, "mixed", 1), ("f32", 333, 41, 70, 128, 2, 0.3, "mixed", 0),
+    ("bf16", 500, 130, 65, 128, 9, 0.5, "sorted", 8), ("f16", 300, 64, 64, 16, 4, 0.1, "none", 0), ("f32", 270, 7, 8, 17, 3, 0.5, "bad", 1),
+    ("bf16", 280, 5, 200, 16, 64, 0.1, "bad", 0), ("f16", 400, 600, 24, 17, 40, 0.05, "one", 0), ("f32", 300, 16, 24, 16, 2, 0.0, "mixed", 0),
+    ("bf16", 300, 40, 40, 8, 2, 1.0, "mixed", 0),
+]
+
+ADAPTERS_TILES = [  # for the GPU: the larger tiles, forward where the outputs are many, backward and with dropout where the inputs are
+    ("bf16", 2040, 70, 2040, 16, 5, 0.3, "mixed", 0), ("bf16", 2040, 2040, 70, 3, 5, 0.3, "mixed", 0), ("f16", 2040, 70, 2040, 33, 5, 0.3, "mixed", 1),
+    ("f16", 2040, 2040, 70, 16, 5, 0.3, "mixed", 0), ("f16", 2040, 2040, 70, 5, 2, 0.0, "sorted", 0), ("bf16", 4090, 70, 4081, 16, 7, 0.3, "mixed", 0),
+    ("bf16", 4090, 4081, 70, 24, 7, 0.3, "mixed", 0), ("bf16", 3900, 3841, 130, 16, 1, 0.0, "one", 0), ("f16", 4090, 70, 4081, 3, 300, 0.3, "mixed", 0),
+    ("f16", 4090, 4081, 70, 16, 7, 0.3, "sorted", 0), ("f32", 4090, 33, 4081, 16, 7, 0.3, "mixed", 0), ("f32", 4090, 4081, 33, 5, 7, 0.3, "mixed", 0),
+]
+
+
+def factor_of_many(rows, cols, p, seed, offset):
+    """As `factor`, with whole arrays of calls at a time."""
+    u, low, t = np.uint64, np.uint64(0xFFFFFFFF), round(65536 * p)
+    groups = (cols + 7) // 8
+    c = list(np.broadcast_arrays(np.arange(groups, dtype=u)[None], np.arange(rows, dtype=u)[:, None], u(offset & 0xFFFFFFFF), u(offset >> 32)))
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(10):
+        x, y = c[0] * u(0xD2511F53), c[2] * u(0xCD9E8D57)
+        c = [(y >> u(32)) ^ c[1] ^ u(k[0]), y & low, (x >> u(32)) ^ c[3] ^ u(k[1]), x & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    draws = np.stack([c[j // 2] >> u(16 * (j % 2)) & u(0xFFFF) for j in range(8)], -1).reshape(rows, groups * 8)[:, :cols]
+    return torch.from_numpy(np.where(draws >= t, 65536.0 / max(65536.0 - t, 1.0), 0.0))
+
+
+def adapter_exact_of_many(x, w, a, b, scale, index, dy, f, absolute=False):
+    """As `adapter_exact`, party by party."""
+    t64 = (lambda v: v.double().abs()) if absolute else (lambda v: v.double())
+    x, w, a, b, dy = (t64(v) for v in (x, w, a, b, dy))
+    xd = torch.where(f > 0, x * f, 0.0)
+    y, h, dx = x @ w.T, torch.zeros(x.shape[0], a.shape[1], dtype=torch.float64), dy @ w
+    da, db = torch.zeros_like(a), torch.zeros_like(b)
+    for p in range(a.shape[0]):
+        t = (index == p).nonzero()[:, 0]
+        h[t] = scale[p].double() * (xd[t] @ a[p].T)
+        y[t] += h[t] @ b[p].T
+        g = scale[p].double() * (dy[t] @ b[p])
+        dx[t] += f[t] * (g @ a[p])
+        da[p], db[p] = g.T @ xd[t], dy[t].T @ h[t]
+    return y, h, dx, da, db
+
+
+def check_adapters_of_many(run, kind, rows, inner, outer, rank, parties, p, order, pad, seed=2 ** 40 + 3, offset=5):
+    x, w, a, b, scale, index, dy = adapter_inputs(kind, rows, inner, outer, rank, parties, order, pad)
+    f = factor_of_many(rows, inner, p, seed, offset)
+    want, most = (adapter_exact_of_many(x, w, a, b, scale, index, dy, f, absolute=m) for m in (False, True))
+    y, h, status = run.adapter_forward(x, w, a, b, scale, index, p, seed, offset)
+    u, ulp = UNIT[x.dtype], 2.0 ** -23
+    assert status == (1 if order == "bad" else 0)
+    near(y, want[0], u * want[0].abs() + (inner + rank + 8) * ulp * most[0] + TINY[x.dtype])
+    near(h, want[1], (inner + 8) * ulp * most[1])
+    dx, da, db, status = run.adapter_backward(dy, x, w, a, b, scale, index, h, p, seed, offset)
+    assert status == (1 if order == "bad" else 0)
+    near(dx, want[2], u * want[2].abs() + (outer + rank + 8) * ulp * most[2] + TINY[x.dtype])
+    near(da, want[3], (outer + rows + 8) * ulp * most[3])
+    near(db, want[4], (inner + rows + 8) * ulp * most[4])
+
+
+def check_factor_of_many():
+    for rows, cols, p, seed, offset in ((7, 33, 0.3, 2 ** 63 + 5, 2 ** 40 + 9), (3, 8, 1.0, 1, 0), (2, 20, 0.0, 0, 3)):
+        assert torch.equal(factor(rows, cols, p, seed, offset), factor_of_many(rows, cols, p, seed, offset))
+
+
+def check_adapters_isolation(run, kind, rows):
+    """What another party's adapter or another row holds does not reach a row, and rows keep their bits."""
+    x, w, a, b, scale, index, dy = adapter_inputs(kind, rows, 24, 20, 4, 4, "mixed", 0)
+    index[:] = torch.arange(rows) % 3 - 1  # parties 2 and 3 have no row
+    clean = run.adapter_forward(x, w, a, b, scale, index, 0.25, 3, 0)
+    back = run.adapter_backward(dy, x, w, a, b, scale, index, clean[1], 0.25, 3, 0)
+    a[1], b[1], a[2], b[2], a[3], b[3] = math.inf, math.nan, math.nan, math.inf, -math.inf, -math.inf
+    x[2], dy[5] = math.nan, math.inf  # rows of party 1
+    dirty = run.adapter_forward(x, w, a, b, scale, index, 0.25, 3, 0)
+    dirty_back = run.adapter_backward(dy, x, w, a, b, scale, index, clean[1], 0.25, 3, 0)
+    mine = index < 1
+    assert all(torch.equal(d[mine], c[mine]) for d, c in zip(dirty[:2], clean[:2])) and torch.equal(dirty_back[0][mine], back[0][mine])
+    assert torch.equal(dirty_back[1][0], back[1][0]) and torch.equal(dirty_back[2][0], back[2][0])
+    assert not dirty_back[1][2:].any() and not dirty_back[2][2:].any()
+
+
+# what the sizes of the lists above leave of the kernels' forms, by type
+ADAPTERS_FORMS = [(kind, rows, 70 + rank, 60, rank, 3, 0.2, "mixed", 1) for kind in TYPES for rows in (9, 25, 70) for rank in (7, 40, 100)]
+ADAPTERS_FORMS += [("f16", 260, 90, 30, 100, 2, 0.1, "mixed", 0)]
+LABELS_FORMS = [  # as LABELS_FAR
+    ("f16", 3, 100, 0, 0, 0, 10.0, "inf"), ("f16", 2, 3000, 1, 0, 0, -10.0, "low"), ("f16", 2, 41001, 0, 1, 3, 0.0, ""), ("bf16", 2, 21000, 3, 0, 4, 0.0, "inf"),
+    ("f32", 3, 6001, 0, 0, 3, 100.0, ""), ("f32", 2, 17000, 0, 0, 2, -1000.0, "low"),
+]

@@ -251,3 +251,87 @@ def test_launches_in_turns(run, narrow):
     cases.check_labels(narrow, "f32", 300, 2100, 0, 0, 0, "inf")
     cases.check_labels(narrow, "f16", 300, 4110, 0, 0, 0, "")
     cases.check_dropout(narrow, "f16", 300, 2200, 0, 0, 0.5, True)
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_MANY, ids=str)
+def test_adapters_many(run, case):
+    cases.check_adapters_of_many(run, *case)
+
+
+@pytest.mark.parametrize("rows", [40, 300])
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_isolation(run, kind, rows):
+    cases.check_adapters_isolation(run, kind, rows)
+
+
+def test_factor_of_many():
+    cases.check_factor_of_many()
+
+
+class Forms:
+    """Which kernels calls of given sizes launch: entry points with addresses that nothing reads, as no kernel runs."""
+
+    def __init__(self, lib):
+        self.lib = lib
+        lib.hipemu_launches.restype = C.c_char_p
+        lib.hipemu_dry.argtypes = [C.c_int]
+
+    def of(self, call):
+        self.lib.hipemu_launches()
+        self.lib.hipemu_dry(1)
+        try:
+            assert call() == 0
+        finally:
+            self.lib.hipemu_dry(0)
+        return [n.strip("()") for n in self.lib.hipemu_launches().decode().split("\n") if n]
+
+    def adapters(self, kind, rows, inner, outer, rank, parties, p, order, pad):
+        t, a, big = NAMES[cases.TYPES[kind]], 2 ** 20, 2 ** 62
+        fwd = lambda: self.lib.haflo_adapter_forward(t, a, inner + pad, a, inner + pad, a, a, a, a, rows, inner, outer, parties, rank, p, 0, 0, a, outer, a, None, a, big, None)  # noqa: E731
+        bwd = lambda: self.lib.haflo_adapter_backward(t, a, outer + pad, a, inner + pad, a, inner + pad, a, a, a, a, a, rows, inner, outer, parties, rank, p, 0, 0, a, inner, a, a, None, a, big, None)  # noqa: E731
+        return {(kind,) + (n,) for n in self.of(fwd) + self.of(bwd)}
+
+    def labels(self, kind, rows, cols, top, backward):
+        t, a = NAMES[cases.TYPES[kind]], 2 ** 20
+        if backward:
+            call = lambda: self.lib.haflo_label_logprobs_backward(t, a, cols, a, a, a, a, a, a if top else None, a if top else None, rows, cols, top, a, cols, None)  # noqa: E731
+        else:
+            call = lambda: self.lib.haflo_label_logprobs(t, a, cols, a, rows, cols, top, a, a, a, a, a, None, a, 2 ** 62, None)  # noqa: E731
+        return {(kind, n) for n in self.of(call)}
+
+
+def test_every_form_is_tested(run):
+    """Each kernel form that some size selects is selected by a case that the GPU runs against the definition."""
+    import test_gpu_local as gpu
+    forms, listed = Forms(run.lib), lambda test: test.pytestmark[0].args[1]
+    every, tested = set(), set()
+    for kind in cases.TYPES:
+        for rank in (1, 16, 17, 32, 33, 64, 65, 128):
+            for p in (0.0, 0.1):
+                for rows, inner, outer in ((1, 8, 8), (20, 8, 8), (40, 8, 8), (300, 8, 8), (300, 600, 600), (300, 513, 8), (2100, 2100, 2100), (8192, 4096, 4096), (70000, 32768, 32768)):
+                    every |= forms.adapters(kind, rows, inner, outer, rank, 3, p, "", 0)
+        for cols in (2, 33, 700, 1100, 2049, 3000, 6000, 9000, 17000, 30000, 50000):
+            for rows in (1, 40, 2000, 9000):
+                for top in (0, 2):
+                    every |= forms.labels(kind, rows, cols, top, False) | forms.labels(kind, rows, cols, top, True)
+    for case in cases.ADAPTERS + cases.ADAPTERS_LARGE + cases.ADAPTERS_SHORT_SUMS + cases.ADAPTERS_MANY + cases.ADAPTERS_TILES + cases.ADAPTERS_FORMS + listed(gpu.test_adapters_some_rows):
+        tested |= forms.adapters(*case)
+    for kind, rows in gpu.FAR_FORWARD:
+        tested |= forms.adapters(kind, rows, 32768, 16, 2, 2, 0.0, "", 0)
+    for kind, rows in gpu.FAR_GRADIENT:
+        tested |= forms.adapters(kind, rows, 16, 32768, 2, 2, 0.5, "", 0)
+    for kind, rows, cols, _, _, top, *_ in cases.LABELS + cases.LABELS_LARGE + cases.LABELS_FAR + cases.LABELS_FORMS + listed(gpu.test_labels_many_rows):
+        tested |= forms.labels(kind, rows, cols, top, False) | forms.labels(kind, rows, cols, top, True) | forms.labels(kind, rows, cols, 0, True)
+    assert not every - tested, sorted(every - tested)
+    tiles = {(k, n) for k, n in every if n.startswith("k_project")}
+    assert len(tiles) == 2 * 8 + 6, sorted(tiles)
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_FORMS, ids=str)
+def test_adapters_forms(run, case):
+    cases.check_adapters_of_many(run, *case)
+
+
+@pytest.mark.parametrize("case", cases.LABELS_FORMS, ids=str)
+def test_labels_forms(run, case):
+    cases.check_labels_far(run, *case)

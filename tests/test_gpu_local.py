@@ -388,3 +388,102 @@ def test_labels_of_very_many_rows(api):
     want[some] = torch.log(cols - 1 + torch.exp(torch.arange(1, 6, device="cuda").double())).float()
     assert float((lse - want).abs().max()) < 1e-5
     assert float((logp[some] - (torch.arange(1, 6, device="cuda") - want[some])).abs().max()) < 1e-5 and float((logp - x[:, 5].float() + want).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_MANY + cases.ADAPTERS_TILES, ids=str)
+def test_adapters_many(run, case):
+    cases.check_adapters_of_many(run, *case)
+
+
+@pytest.mark.parametrize("rows", [40, 300])
+@pytest.mark.parametrize("kind", cases.TYPES)
+def test_adapters_isolation(run, kind, rows):
+    cases.check_adapters_isolation(run, kind, rows)
+
+
+def test_graph_of_many_rows(api):
+    """As test_side_stream_and_graph, with the kernels for more than 256 rows: their lists of rows, layouts and joined sums."""
+    x, w, a, b, scale, index, dy = map(dev, cases.adapter_inputs("f16", 700, 1033, 130, 8, 5, "mixed", 0))
+
+    def step():
+        y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.2, 9, 1)
+        return (y, h, *api.haflo_adapter_backward(dy, x, w, a, b, scale, index, h, 0.2, 9, 1))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    for k in range(3):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(k)).to(x.dtype))
+        index.copy_(torch.randint(-1, 5, index.shape, generator=torch.Generator().manual_seed(k)).to(torch.int32))
+        torch.cuda.synchronize()
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+FAR_GRADIENT = [("bf16", 70000), ("f16", 70000), ("f32", 36000)]
+
+
+@pytest.mark.parametrize("kind,rows", FAR_GRADIENT)
+def test_adapters_gradient_past_32_bits(api, kind, rows):
+    """dy of more than 4 GiB, with dropout. Small integers and a factor of two: every sum is exact in 32 bits."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    inner, outer, rank, dtype = 16, 32768, 2, cases.TYPES[kind]
+
+    def ints(*shape):
+        return torch.randint(-1, 2, shape, generator=g, device="cuda", dtype=torch.int8).to(dtype)
+
+    x, w, a, b, dy = ints(rows, inner), ints(outer, inner), ints(2, rank, inner), ints(2, outer, rank), ints(rows, outer)
+    scale, index = torch.tensor([1.0, 2.0], device="cuda"), torch.randint(-1, 2, (rows,), generator=g, device="cuda").to(torch.int32)
+    y, h = api.haflo_adapter_forward(x, w, a, b, scale, index, 0.5, 77)
+    dx, da, db = api.haflo_adapter_backward(dy, x, w, a, b, scale, index, h, 0.5, 77)
+    kept = api.haflo_dropout(torch.ones_like(x), 0.5, 77).double()
+    some = torch.cat([torch.arange(40), torch.arange(rows - 40, rows)]).cuda()
+    dys, of = dy[some].double(), index[some].long()
+    by = torch.where(of < 0, 0.0, scale.double()[of])
+    gs = by[:, None] * (dys[:, None, :] @ b.double()[of])[:, 0]
+    assert torch.equal(dx[some], (dys @ w.double() + kept[some] * (gs[:, None, :] @ a.double()[of])[:, 0]).to(dtype))
+    cols = torch.cat([torch.arange(9), torch.arange(outer - 9, outer)]).cuda()
+    for p in range(2):
+        mine = (index == p).nonzero()[:, 0]
+        assert torch.equal(db[p][cols].double(), dy[mine][:, cols].double().t() @ h[mine].double())
+
+
+FAR_FORWARD = [("f16", 70000), ("f32", 36000), ("bf16", 70000)]  # the last by test_adapters_past_32_bits
+
+
+@pytest.mark.parametrize("kind,rows", FAR_FORWARD[:2])
+def test_adapters_past_32_bits_of_other_types(api, kind, rows):
+    """x of more than 4 GiB in the other types, as test_adapters_past_32_bits."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    inner, outer, rank, dtype = 32768, 16, 2, cases.TYPES[kind]
+
+    def ints(*shape):
+        return torch.randint(-1, 2, shape, generator=g, device="cuda", dtype=torch.int8).to(dtype)
+
+    x, w, a, b = ints(rows, inner), ints(outer, inner), ints(2, rank, inner), ints(2, outer, rank)
+    scale, index = torch.tensor([1.0, 2.0], device="cuda"), torch.randint(-1, 2, (rows,), generator=g, device="cuda").to(torch.int32)
+    y, h = api.haflo_adapter_forward(x, w, a, b, scale, index)
+    some = torch.cat([torch.arange(40), torch.arange(rows - 40, rows)]).cuda()
+    xs, of = x[some].double(), index[some].long()
+    by = torch.where(of < 0, 0.0, scale.double()[of])
+    hs = by[:, None] * (a.double()[of] @ xs[:, :, None])[..., 0]
+    assert torch.equal(h[some].double(), hs)
+    assert torch.equal(y[some], (xs @ w.double().t() + (b.double()[of] @ hs[:, :, None])[..., 0]).to(dtype))
+
+
+@pytest.mark.parametrize("case", cases.ADAPTERS_FORMS, ids=str)
+def test_adapters_forms(run, case):
+    cases.check_adapters_of_many(run, *case)
+
+
+@pytest.mark.parametrize("case", cases.LABELS_FORMS, ids=str)
+def test_labels_forms(run, case):
+    cases.check_labels_far(run, *case)
