@@ -12,11 +12,15 @@ using namespace haflo::local;
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-// Up to here a lane takes a row by itself (262144 rows of bfloat16, us, and by wavefronts: 2 columns 9 and 120, 32 columns 35 and 122).
+// Up to here a lane takes a row by itself. 262144 rows, us, and by wavefronts: float32 24 columns 37 and 119, 33 columns 99 and 134, 48 columns 164
+// and 127; bfloat16 33 columns 39 and 136, 48 columns 70 and 129, 64 columns 123 and 133; with 16 alternatives 33 columns 342 and 445, 48 661 and
+// 488; 64 rows of 33 columns 9 and 10.
 constexpr size_t kSmallCols = 32;
 // Up to here a wavefront does (16384 rows, us, and by blocks: 1000 columns 16 and 35, 2000 columns 25 and 43), and of longer rows
-// where there are many (16384 rows: 4000 columns 34 and 52, 8000 columns 55 and 75).
-constexpr size_t kWaveCols = 2048, kManyWaveCols = 8192, kManyRows = 8192;
+// where there are many. By wavefronts and by blocks: 2048 rows of 2049 bfloat16 10 and 10, of 16384 23 and 21; 3000 rows 10 and 12, 28 and 27; 4096
+// rows of 2049 10 and 14, of 16384 33 and 33, of 32768 61 and 55; 16384 rows of 4000 34 and 52, of 16000 110 and 126. float32: 2048 rows of
+// 16384 28 and 27, 4096 rows of 2049 10 and 14, of 16384 48 and 47, of 65536 191 and 188. With alternatives the wavefronts gain more.
+constexpr size_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 3000;
 constexpr size_t kSplitCols = 2048;  // columns of one part of a row, at least
 constexpr size_t kSplitBlocks = 1024;
 constexpr int kAhead = 4;            // vectors on their way at a time
