@@ -56,7 +56,7 @@ int haflo_dropout(int type, const void* d_x, size_t ldx, const void* d_residual,
  * rows x inner matrix x (p = 0: none), on the adapter's side only.
  * d_h: float32, rows x rank, dense; the backward pass takes it. An index outside -1 .. parties - 1 counts as
  * -1 and HAFLO_ST_RANGE is OR-ed into d_status (one device uint32, or NULL).
- * 1 <= rank <= HAFLO_ADAPTER_MAX_RANK, 1 <= parties <= HAFLO_ADAPTER_MAX_PARTIES, inner, outer >= 1.
+ * 1 <= rank <= HAFLO_ADAPTER_MAX_RANK, 1 <= parties <= HAFLO_ADAPTER_MAX_PARTIES, inner, outer >= 1, matrices of at most 2^56 elements.
  */
 #define HAFLO_ADAPTER_MAX_RANK 128
 #define HAFLO_ADAPTER_MAX_PARTIES 4096

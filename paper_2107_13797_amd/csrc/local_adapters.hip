@@ -1044,10 +1044,12 @@ __global__ __launch_bounds__(kThreads) void k_grad_join(GradOf<T> a, GradOf<T> b
 struct Sizes {
   size_t rows, inner, outer, parties, rank;
 };
+constexpr size_t kMostElements = (size_t)1 << 56;  // of a matrix, so that sums of sizes stay within 64 bits
 bool adapter_sizes(int type, const Sizes& s) {
   return valid_type(type) && s.rows <= kMostCount && s.inner >= 1 && s.inner <= kMostCount - 512 && s.outer >= 1 &&
          s.outer <= kMostCount - 512 && s.parties >= 1 && s.parties <= HAFLO_ADAPTER_MAX_PARTIES && s.rank >= 1 &&
-         s.rank <= HAFLO_ADAPTER_MAX_RANK;
+         s.rank <= HAFLO_ADAPTER_MAX_RANK && s.rows * s.inner <= kMostElements && s.rows * s.outer <= kMostElements &&
+         s.inner * s.outer <= kMostElements;
 }
 // Whether k_few takes a product: up to 256 rows, where k_project's tiles would leave most of the chip idle; float32, whose matrix
 // instructions bound it sooner, up to 2^31 products of elements. Forward, us by k_few and by k_project: bfloat16 4096 to 4096

@@ -335,3 +335,15 @@ def test_adapters_forms(run, case):
 @pytest.mark.parametrize("case", cases.LABELS_FORMS, ids=str)
 def test_labels_forms(run, case):
     cases.check_labels_far(run, *case)
+
+
+def test_sizes_past_64_bits(run):
+    """Counts that each are in range, whose products a workspace's size does not hold, are refused rather than wrapped around."""
+    size, most = run.lib.haflo_adapter_workspace_bytes, 2 ** 31 - 600
+    for kind in (0, 1, 2):
+        for backward in (0, 1):
+            for rows, inner, outer in ((most, most, 64), (most, 64, most), (64, most, most), (2 ** 30, 2 ** 28, 2 ** 28)):
+                assert size(kind, backward, rows, inner, outer, 4096, 128) == 2 ** 64 - 1
+            for rows, inner, outer in ((most, 64, 64), (64, most, 64), (64, 64, most), (2 ** 20, 2 ** 20, 2 ** 20)):
+                need = size(kind, backward, rows, inner, outer, 4096, 128)
+                assert (2 * rows * inner if rows > 256 else 2 * outer * inner) <= need < 2 ** 63
