@@ -328,7 +328,8 @@ def haflo_cipher_sum_segments(ctx, c, offsets, status=None):
 
 # The operators of a party's local step (include/haflo_local.h) work on ordinary float32, float16 and bfloat16 tensors and
 # need no Context; their workspaces come from torch's allocator call by call, in the current stream's order. Operands lie on the
-# current device, whose stream a call goes to. Small calls take as long as the host needs for them, so checks look at each property once.
+# current device, whose stream a call goes to. They are not known to autograd: results require no gradient whatever their
+# inputs require, and a program calls the functions for gradients itself. Small calls take as long as the host needs for them, so checks look at each property once.
 _TYPES = {torch.float32: _cabi.TYPE_F32, torch.float16: _cabi.TYPE_F16, torch.bfloat16: _cabi.TYPE_BF16}
 
 
@@ -393,7 +394,7 @@ def _scratch(nbytes, like):
 
 def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
     """x / (1 - p) where the generator keeps an element, 0 elsewhere, plus `residual`. The gradient by x is the same call on the
-    gradient of the result, without a residual. A vector counts as one row; `out` may be x or the residual."""
+    gradient of the result, without a residual; autograd records nothing. A vector counts as one row; `out` may be x or the residual."""
     if x.dim() == 1:
         y = haflo_dropout(x[None], p, seed, offset, None if residual is None else residual[None], None if out is None else out[None])
         return y[0] if out is None else out
@@ -424,7 +425,8 @@ def _adapter_sizes(x, w, a, b, scale, index):
 def haflo_adapter_forward(x, w, a, b, scale, index, p=0.0, seed=0, offset=0, status=None):
     """y = x w^T + h b[index]^T, h = scale[index] drop(x) a[index]^T, row by row: the projection that all parties share with each
     row's own adapter (index int32, -1: none). x [rows, inner], w [outer, inner], a [parties, rank, inner],
-    b [parties, outer, rank], scale float32 [parties]. Returns y and, for the backward pass, h (float32 [rows, rank])."""
+    b [parties, outer, rank], scale float32 [parties]. Returns y and, for haflo_adapter_backward, h (float32 [rows, rank]); autograd
+    records nothing."""
     kind, rows, inner, outer, parties, rank, ldx, ldw, pa, pb, ps, pi = _adapter_sizes(x, w, a, b, scale, index)
     y, h = x.new_empty((rows, outer)), scale.new_empty((rows, rank))
     nbytes = lib().haflo_adapter_workspace_bytes(kind, 0, rows, inner, outer, parties, rank)
@@ -451,7 +453,8 @@ def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offse
 
 def haflo_label_logprobs(logits, label, top=0, status=None):
     """Row by row under softmax(logits): the label's log-probability (int32 label, -1: none, gives 0), the entropy, the logarithm of the
-    exponentials' sum, and the `top` greatest logits' log-probabilities and columns (None for top = 0), ties to the lowest."""
+    exponentials' sum, and the `top` greatest logits' log-probabilities and columns (None for top = 0), ties to the lowest. The gradient
+    is haflo_label_logprobs_backward; autograd records nothing."""
     kind, (rows, cols, ld) = _type(logits), _matrix(logits, logits.dtype)
     pl, f32 = _dense(label, torch.int32, rows), torch.float32
     nbytes = lib().haflo_label_workspace_bytes(kind, rows, cols, top)
