@@ -1216,9 +1216,11 @@ struct Product {
 #undef HAFLO_LOCAL_RUN
   }
 
-  // The largest tiles that give every compute unit one: W and x are read once for a tile's side. Calls, us: bfloat16 4096 x 4096 to
-  // 2048 by 128 x 128 95, by 64 x 64 125; 4096 x 512 to 2048 33 and 37; too few tiles, float16 3001 x 1001 to 515, the product alone
-  // 30 and 19. float32 is bound by its matrix instructions: 4096 x 1024 to 1024 95 by 128 x 128 and 89 by 64 x 64, which it takes.
+  // The largest tiles that give every compute unit one: W and x are read once for a tile's side. Calls, us: bfloat16 8192 x 4096 to 4096 by
+  // 256 x 256 238, by 128 x 128 301; 4096 x 1024 to 4096 55 and 69; 4096 x 4096 to 2048 by 128 x 128 97, by 64 x 64 123; 4096 x 512 to 2048
+  // 33 and 35; too few tiles, float16 3001 x 1001 to 515, 38 and 32. float32 is bound by its matrix instructions and takes the small tiles,
+  // which leave the fewest of them idle: 8192 x 4096 to 4096 by 256 x 256 2131, by 128 x 128 1970, by 64 x 64 1955; 4096 x 1024 to 1024 by
+  // 128 x 128 96, by 64 x 64 90; 16384 x 1024 to 1024 310, 308 and 314.
   void project(T* y, size_t ldy) const {
     const size_t x_bytes = ((s.rows - 1) * x.ld + padded_inner()) * sizeof(T), w_bytes = ((s.outer - 1) * w.ld + padded_inner()) * sizeof(T);
     const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
@@ -1231,8 +1233,8 @@ struct Product {
 #define HAFLO_LOCAL_TILE(DROP)                                                                                    \
   do {                                                                                                            \
     if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, true);                                                         \
-    else if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, false); \
     else if constexpr (sizeof(T) == 4) HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP, false);                                \
+    else if (ceil_div(s.rows, 256) * ceil_div(s.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, DROP, false); \
     else if (ceil_div(s.rows, 128) * ceil_div(s.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, DROP, false); \
     else HAFLO_LOCAL_RUN(64, 64, 2, 2, DROP, false);                                                              \
   } while (0)

@@ -324,7 +324,7 @@ def test_every_form_is_tested(run):
         tested |= forms.labels(kind, rows, cols, top, False) | forms.labels(kind, rows, cols, top, True) | forms.labels(kind, rows, cols, 0, True)
     assert not every - tested, sorted(every - tested)
     tiles = {(k, n) for k, n in every if n.startswith("k_project")}
-    assert len(tiles) == 2 * 8 + 6, sorted(tiles)
+    assert len(tiles) == 2 * 8 + 4, sorted(tiles)
 
 
 @pytest.mark.parametrize("case", cases.ADAPTERS_FORMS, ids=str)
