@@ -329,7 +329,8 @@ def haflo_cipher_sum_segments(ctx, c, offsets, status=None):
 # The operators of a party's local step (include/haflo_local.h) work on ordinary float32, float16 and bfloat16 tensors and
 # need no Context; their workspaces come from torch's allocator call by call, in the current stream's order. Operands lie on the
 # current device, whose stream a call goes to. They are not known to autograd: results require no gradient whatever their
-# inputs require, and a program calls the functions for gradients itself. Small calls take as long as the host needs for them, so checks look at each property once.
+# inputs require, and a program calls the functions for gradients itself. Small calls take as long as the host needs for them, so
+# checks look at each property once.
 _TYPES = {torch.float32: _cabi.TYPE_F32, torch.float16: _cabi.TYPE_F16, torch.bfloat16: _cabi.TYPE_BF16}
 
 
@@ -340,15 +341,17 @@ def _type(t):
     return kind
 
 
-def _here(t):
-    device = t.get_device()  # below zero: the host
-    if device < 0 or device != torch._C._cuda_getDevice():
-        raise HafloError("expected a tensor of the current CUDA device, got one of %s" % t.device)
+def _stream_of(*tensors):
+    """The current device's stream, on which all of the tensors (or None) have to lie."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:  # (below zero: the host)
+            raise HafloError("expected a tensor of the current CUDA device, got one of %s" % t.device)
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _matrix(t, dtype, rows=None, cols=None):
     """(rows, columns, distance between rows) of a matrix whose rows are contiguous and do not overlap."""
-    _here(t)
     if t.dim() != 2 or t.dtype is not dtype:
         raise HafloError("expected a matrix of %s" % dtype)
     r, c = t.shape
@@ -364,7 +367,6 @@ def _matrix(t, dtype, rows=None, cols=None):
 
 def _dense(t, dtype, *shape):
     """Address of a contiguous tensor of that type and shape."""
-    _here(t)
     if t.dtype is not dtype or t.shape != shape:
         raise HafloError("expected %s of shape %s, got %s of %s" % (dtype, shape, t.dtype, tuple(t.shape)))
     if not t.is_contiguous():
@@ -376,7 +378,6 @@ def _status(t):
     """Address of the word that a call's status is OR-ed into, or None."""
     if t is None:
         return None
-    _here(t)
     if t.dtype not in (torch.int32, torch.uint32) or t.numel() < 1:
         raise HafloError("status: expected an int32 or uint32 element, got %s of shape %s" % (t.dtype, tuple(t.shape)))
     return t.data_ptr()
@@ -398,7 +399,7 @@ def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
     if x.dim() == 1:
         y = haflo_dropout(x[None], p, seed, offset, None if residual is None else residual[None], None if out is None else out[None])
         return y[0] if out is None else out
-    dtype = x.dtype
+    dtype, stream = x.dtype, _stream_of(x, residual, out)
     kind, (rows, cols, ldx) = _type(x), _matrix(x, dtype)
     pr = ldr = 0
     if residual is not None:
@@ -407,7 +408,7 @@ def haflo_dropout(x, p, seed, offset=0, residual=None, out=None):
         out, ldy = x.new_empty((rows, cols)), cols
     else:
         ldy = _matrix(out, dtype, rows, cols)[2]
-    _check(lib().haflo_dropout(kind, x.data_ptr(), ldx, pr, ldr, out.data_ptr(), ldy, rows, cols, p, seed, offset, _stream()))
+    _check(lib().haflo_dropout(kind, x.data_ptr(), ldx, pr, ldr, out.data_ptr(), ldy, rows, cols, p, seed, offset, stream))
     return out
 
 
@@ -427,18 +428,20 @@ def haflo_adapter_forward(x, w, a, b, scale, index, p=0.0, seed=0, offset=0, sta
     row's own adapter (index int32, -1: none). x [rows, inner], w [outer, inner], a [parties, rank, inner],
     b [parties, outer, rank], scale float32 [parties]. Returns y and, for haflo_adapter_backward, h (float32 [rows, rank]); autograd
     records nothing."""
+    stream = _stream_of(x, w, a, b, scale, index, status)
     kind, rows, inner, outer, parties, rank, ldx, ldw, pa, pb, ps, pi = _adapter_sizes(x, w, a, b, scale, index)
     y, h = x.new_empty((rows, outer)), scale.new_empty((rows, rank))
     nbytes = lib().haflo_adapter_workspace_bytes(kind, 0, rows, inner, outer, parties, rank)
     pw, ws = _scratch(nbytes, scale)
     _check(lib().haflo_adapter_forward(kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, rows, inner, outer, parties, rank, p, seed,
-                                       offset, y.data_ptr(), outer, h.data_ptr(), _status(status), pw, nbytes, _stream()))
+                                       offset, y.data_ptr(), outer, h.data_ptr(), _status(status), pw, nbytes, stream))
     return y, h
 
 
 def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offset=0, need_dx=True, status=None):
     """Gradients of haflo_adapter_forward by x (None without need_dx) and, float32 as haflo_encode_f32 takes them, by a and b; for the
     forward call's arguments and its h."""
+    stream = _stream_of(dy, x, w, a, b, scale, index, h, status)
     kind, rows, inner, outer, parties, rank, ldx, ldw, pa, pb, ps, pi = _adapter_sizes(x, w, a, b, scale, index)
     lddy, ph = _matrix(dy, x.dtype, rows, outer)[2], _dense(h, torch.float32, rows, rank)
     dx = x.new_empty((rows, inner)) if need_dx else None
@@ -447,7 +450,7 @@ def haflo_adapter_backward(dy, x, w, a, b, scale, index, h, p=0.0, seed=0, offse
     pw, ws = _scratch(nbytes, scale)
     _check(lib().haflo_adapter_backward(kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, pa, pb, ps, pi, ph, rows, inner, outer,
                                         parties, rank, p, seed, offset, dx.data_ptr() if need_dx else None, inner, da.data_ptr(),
-                                        db.data_ptr(), _status(status), pw, nbytes, _stream()))
+                                        db.data_ptr(), _status(status), pw, nbytes, stream))
     return dx, da, db
 
 
@@ -455,6 +458,7 @@ def haflo_label_logprobs(logits, label, top=0, status=None):
     """Row by row under softmax(logits): the label's log-probability (int32 label, -1: none, gives 0), the entropy, the logarithm of the
     exponentials' sum, and the `top` greatest logits' log-probabilities and columns (None for top = 0), ties to the lowest. The gradient
     is haflo_label_logprobs_backward; autograd records nothing."""
+    stream = _stream_of(logits, label, status)
     kind, (rows, cols, ld) = _type(logits), _matrix(logits, logits.dtype)
     pl, f32 = _dense(label, torch.int32, rows), torch.float32
     nbytes = lib().haflo_label_workspace_bytes(kind, rows, cols, top)
@@ -465,7 +469,7 @@ def haflo_label_logprobs(logits, label, top=0, status=None):
     if top:
         top_logp, top_index = logits.new_empty((rows, top), dtype=f32), logits.new_empty((rows, top), dtype=torch.int32)
     _check(lib().haflo_label_logprobs(kind, logits.data_ptr(), ld, pl, rows, cols, top, at, at + 4 * rows, at + 8 * rows, _ptr(top_logp),
-                                      _ptr(top_index), _status(status), pw, nbytes, _stream()))
+                                      _ptr(top_index), _status(status), pw, nbytes, stream))
     logp, entropy, lse = sums.unbind()
     return logp, entropy, lse, top_logp, top_index
 
@@ -473,6 +477,7 @@ def haflo_label_logprobs(logits, label, top=0, status=None):
 def haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dentropy=None, top_index=None, dtop=None, out=None):
     """Gradient by the logits from the forward call's results and the gradients of its logp, entropy and top_logp. `out` may be
     the logits."""
+    stream = _stream_of(logits, label, lse, entropy, dlogp, dentropy, top_index, dtop, out)
     dtype, f32, top, pt, pi = logits.dtype, torch.float32, 0, None, None
     kind, (rows, cols, ld) = _type(logits), _matrix(logits, dtype)
     if dtop is not None:
@@ -487,7 +492,7 @@ def haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dentropy=N
     _check(lib().haflo_label_logprobs_backward(
         kind, logits.data_ptr(), ld, _dense(label, torch.int32, rows), _dense(lse, f32, rows), _dense(entropy, f32, rows),
         _dense(dlogp, f32, rows), None if dentropy is None else _dense(dentropy, f32, rows), pi, pt, rows, cols, top, out.data_ptr(), lddx,
-        _stream()))
+        stream))
     return out
 
 

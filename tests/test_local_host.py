@@ -72,8 +72,8 @@ def test_operands_on_one_device(monkeypatch):
             return lambda *args: reached.append(name) or 0
 
     monkeypatch.setattr(api, "_lib", Library())
-    monkeypatch.setattr(api, "_stream", lambda: None)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: None, raising=False)
     for number, (tensors, call) in enumerate(_calls(api)):
         call({n: OnDevice(t, 0) for n, t in tensors.items()})
         assert reached
@@ -89,8 +89,8 @@ def test_status_type(monkeypatch):
     """Four bytes are written to the status: it has to be a 32-bit integer."""
     from paper_2107_13797_amd import api
     monkeypatch.setattr(api, "_lib", type("L", (), {"__getattr__": lambda s, n: lambda *a: 0})())
-    monkeypatch.setattr(api, "_stream", lambda: None)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: None, raising=False)
     for tensors, call in _calls(api):
         if "status" not in tensors:
             continue
