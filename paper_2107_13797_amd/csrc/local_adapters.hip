@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
   }
 }
 
-// A lane an element (3001 rows, 2 us: a launch): z[i] = sum over parts, and without the places behind the rank to h
+// A lane an element (3001 rows, 3 us: a launch): z[i] = sum over parts, and without the places behind the rank to h
 __global__ __launch_bounds__(kThreads) void k_join(const float* in, u32 parts, size_t count, u32 z_ld, u32 rank, float* z, float* h) {
   const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
   if (i >= count) return;
@@ -378,8 +378,8 @@ __device__ __forceinline__ void reduce(const From& x, const typename From::At (&
 // y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k], inner a multiple of a step. A block takes TM rows (of
 // `order`) by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
 // is filled while the other is read. Matrix instructions and the reads of LDS between them bound the large tiles (8192 x 4096
-// to 4096, bfloat16: 231 us, 1190 TFLOP/s; 336 us by tiles of 128 x 128), the wait for each step's loads the small ones
-// (float16 3001 x 1001 to 515: 19 us, 164 TFLOP/s).
+// to 4096, bfloat16: 231 us, 1190 TFLOP/s; a call 301 instead of 238 by tiles of 128 x 128), the wait for each step's loads the small
+// ones (float16 3001 x 1001 to 515: 14 us, 221 TFLOP/s).
 template <class T, int TM, int TN, int WM, int WN, bool DROP, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t ldx, const T* w, size_t ldw, const T* f, const float* z,
                                                              const int* index, const u32* order, const u32* begin, u32 rows, u32 inner,
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_project(const T* x, size_t 
 // The same for few rows, in two launches. k_few reads W once for 64 rows: a block takes them, 64 outputs and one part of the reduction, 1024 bytes of
 // every row at a time, its wavefronts four sixteens of outputs in two halves of that; further blocks form the parts of z = h or
 // g for one row each, as k_shrink does. k_few_join adds the parts, and the adapters' part to them. What bounds it is the
-// reading of W: 64 rows of 4096 to 4096 in bfloat16 take 16 us and 6 for the joining, one row 8.6 and 4.4.
+// reading of W: 64 rows of 4096 to 4096 in bfloat16 take 16 us and 6 for the joining, one row 9.7 and 4.7.
 constexpr int kFewWaves = 8;
 template <class T, int RT, bool SHORT>
 __device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, size_t ldw, u32 rows, u32 inner, u32 outer, u32 tile, u32 part,
@@ -674,7 +674,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
   to[r] = r < rank ? s * scale[a] * (d.threshold ? d.scale : 1.0f) : 0.0f;
 }
 
-// A block takes 256 outputs of a row, a lane one: the reading of the parts bounds it (64 rows of 4096, 8 parts: 5.8 us). Its z is written to `z_out` (z_ld places) or `h` (rank) by the first of the row.
+// A block takes 256 outputs of a row, a lane one: the reading of the parts bounds it (64 rows of 4096, 8 parts: 6 us). Its z is written to `z_out` (z_ld places) or `h` (rank) by the first of the row.
 template <class T, bool DROP>
 __global__ __launch_bounds__(kThreads) void k_few_join(const float* sums, const float* z, const T* f, u32 f_ld, const int* index, u32 rows, u32 outer,
                                                        u32 parties, u32 rank, Drop d, u32 parts, u32 z_parts, u32 z_ld, T* y, size_t ldy,
@@ -897,7 +897,7 @@ __global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p, u32 f
 // operands are one element a lane: lane l holds eight columns from 8 (l % 16) on of row l / 16 out of four, and element j of
 // all lanes is one operand, for the columns 8 c + j. A block takes 128 columns and RT sixteens of z, its wavefronts every
 // fourth four rows each. The next rows are on their way while the present ones are multiplied.
-// Both gradients are formed by one launch. 8192 rows of 4096 and 4096 columns, rank 16, bfloat16: 54 us, 40 TFLOP/s and 2.5 TB/s, so
+// Both gradients are formed by one launch. 8192 rows of 4096 and 4096 columns, rank 16, bfloat16: 56 us, 38 TFLOP/s and 2.4 TB/s, so
 // bound by neither alone but by a row's way from memory to its sixteen products; four rows ahead in place of two gain nothing.
 template <class T>
 struct GradOf {
@@ -1053,8 +1053,8 @@ bool adapter_sizes(int type, const Sizes& s) {
 }
 // Whether k_few takes a product: up to 256 rows, where k_project's tiles would leave most of the chip idle; float32, whose matrix
 // instructions bound it sooner, up to 2^31 products of elements. Forward, us by k_few and by k_project: bfloat16 4096 to 4096
-// 128 rows 27 and 48, 256 rows 41 and 47, 4096 to 256 128 rows 15 and 33; float32 4096 to 4096 128 rows 61 and 89, 192 rows 98 and
-// 92, 4096 to 256 256 rows 24 and 87.
+// 128 rows 27 and 46, 256 rows 41 and 46, 4096 to 256 128 rows 17 and 33; float32 4096 to 4096 128 rows 61 and 89, 192 rows 98 and
+// 92, 4096 to 256 256 rows 25 and 87.
 bool few(int type, const Sizes& s) {
   return s.rows <= 256 && (type != HAFLO_F32 || s.rows * s.inner <= ((size_t)1 << 31) / s.outer);
 }
