@@ -10,7 +10,7 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 CSRC = os.path.join(ROOT, "paper_2107_13797_amd", "csrc")
 OUT = os.path.join(HERE, "libhaflo_emu_local.so")
 OBJ = os.path.join(HERE, "_build", "local")
-NARROW = 1 << 16  # lanes of a launch at most in the library whose launches are in many turns
+NARROW = 1 << 14  # lanes of a launch at most in the library whose launches are in many turns
 CLANG = "/opt/rocm/llvm/bin/clang++"
 
 

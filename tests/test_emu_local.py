@@ -245,12 +245,12 @@ def narrow():
 
 
 def test_launches_in_turns(run, narrow):
-    cases.check_adapters(narrow, "f32", 9000, 7, 70, 2, 300, 0.1, "mixed", 1)
-    cases.check_adapters(narrow, "bf16", 40, 16, 8200, 4, 2, 0.1, "mixed", 0)
-    cases.check_labels(narrow, "bf16", 1100, 40, 0, 0, 2, "inf")
-    cases.check_labels(narrow, "f32", 300, 2100, 0, 0, 0, "inf")
-    cases.check_labels(narrow, "f16", 300, 4110, 0, 0, 0, "")
-    cases.check_dropout(narrow, "f16", 300, 2200, 0, 0, 0.5, True)
+    cases.check_adapters(narrow, "f32", 2500, 7, 70, 2, 100, 0.1, "mixed", 1)
+    cases.check_adapters(narrow, "bf16", 40, 16, 2100, 4, 2, 0.1, "mixed", 0)
+    cases.check_labels(narrow, "bf16", 300, 40, 0, 0, 2, "inf")
+    cases.check_labels(narrow, "f32", 200, 2100, 0, 0, 0, "inf")
+    cases.check_labels(narrow, "f16", 100, 5130, 0, 0, 0, "")
+    cases.check_dropout(narrow, "f16", 100, 2200, 0, 0, 0.5, True)
 
 
 @pytest.mark.parametrize("case", cases.ADAPTERS_MANY, ids=str)
