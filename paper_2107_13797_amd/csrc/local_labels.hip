@@ -200,7 +200,7 @@ struct Part {  // of a row, joined by k_label_join
   float m, s, t, unused;
 };
 
-// W wavefronts to a row or, with `parts` > 1, to one of its parts. Reading the row bounds it (8192 x 32768 bfloat16: 156 us, 3.4 TB/s);
+// W wavefronts to a row or, with `parts` > 1, to one of its parts. Reading the row bounds it (8192 x 32768 bfloat16: 112 us call after call, 4.8 TB/s);
 // one long row the length of a part and its list (131072 columns, 20 greatest: 11 us).
 template <class T, int W, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_labels(const T* x, size_t ld, u32 rows, u32 cols, int top, u32 parts, LabelOut o,
@@ -336,8 +336,8 @@ struct GradIn {
 // for small ones only (a row of the type's lowest value has lse equal to it, and z is the row's length).
 // WAVES wavefronts take a row or, with WAVES = 0, a group of 2^shift lanes of one. A lane keeps its first HELD vectors of the row between
 // the sum and the results and reads what is behind them twice; it writes only columns that it alone reads, after the sum. Memory bounds
-// it, one reading and one writing (8192 x 32768 bfloat16: 228 us, 4.7 TB/s; calls 213 and, with lse taken for exact and without the sum,
-// 202; 2048 x 131072, three quarters of it read twice, 237 and 201); of a single row the one compute unit that it is on (131072 columns: 22).
+// it, one reading and one writing (8192 x 32768 bfloat16: 201 to 213 us call after call, 5.0 to 5.3 TB/s, and with lse taken for exact, without
+// the sum, 202; 2048 x 131072, three quarters of it read twice, 237 and 201); of a single row the one compute unit that it is on (131072 columns: 22).
 template <class T, int WAVES, int HELD, bool TOP>
 __global__ __launch_bounds__(WAVES > kWaves ? WAVES * kWave : kThreads, 4) void k_labels_grad(const T* x, size_t ld, u32 rows, u32 cols, int top, u32 shift,
                                                                                          GradIn g, T* dx, size_t lddx) {
