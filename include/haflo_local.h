@@ -111,6 +111,80 @@ int haflo_label_logprobs_backward(int type, const void* d_logits, size_t ld, con
                                   const int32_t* d_top_index, const float* d_dtop, size_t rows, size_t cols, size_t top,
                                   void* d_dx, size_t lddx, void* stream);
 
+/*
+ * The norms around a block of a model, with its gate and the residual stream, row by row:
+ *   p = f / sqrt(mean f^2 + eps) * post   (d_post NULL: p = f)
+ *   r = scale x + gate * p,   h = r / sqrt(mean r^2 + eps) * pre
+ * x: the stream before the block, f: what the block gave, r: the stream behind it (d_r), h: what the next block takes (d_h). The gate is
+ * d_gate (rows x cols), or d_gate_cols for all rows (float32[cols]), or 1 where both are NULL. d_pre NULL: no h. d_f
+ * NULL: only h, of r = x, and scale has to be 1; not both NULL.
+ * d_post, d_pre: float32[cols]. d_rstd: float32, 2 x rows, both roots' reciprocals (1 where there is no norm), which the
+ * backward pass takes. h is formed from r before its rounding; means of squares are held in 64 bits. d_r and d_h may each be one of the
+ * inputs where the distances between rows are the same (else HAFLO_EINVAL). cols >= 1, eps > 0, finite.
+ */
+int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, size_t ldf, const float* d_post,
+                        const void* d_gate, size_t ldg, const float* d_gate_cols, const float* d_pre, size_t rows,
+                        size_t cols, double scale, double eps, void* d_r, size_t ldr, void* d_h, size_t ldh,
+                        float* d_rstd, void* stream);
+/*
+ * Its gradients, for the forward call's arguments and its d_rstd, from dh (where there is h) and dr (NULL: zeros), the
+ * gradient that r has from elsewhere:
+ *   D = dr + gradient of h by r,   dx = scale D,   dgate = D * p (d_dgate, or summed over rows: d_dgate_cols),
+ *   df = gradient of p by f for gate * D,   dpost, dpre: sums over rows
+ * Each output may be NULL. dx, df, dgate: of `type`, each may be one of the inputs where the distances between rows are the same
+ * (else HAFLO_EINVAL); dpost, dgate_cols, dpre: float32[cols], zeros for no rows.
+ */
+size_t haflo_residual_norm_workspace_bytes(int type, size_t rows, size_t cols);
+int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const void* d_dr, size_t lddr, const void* d_x,
+                                 size_t ldx, const void* d_f, size_t ldf, const float* d_post, const void* d_gate,
+                                 size_t ldg, const float* d_gate_cols, const float* d_pre, const float* d_rstd,
+                                 size_t rows, size_t cols, double scale, void* d_dx, size_t lddx, void* d_df, size_t lddf,
+                                 void* d_dgate, size_t lddg, float* d_dgate_cols, float* d_dpost, float* d_dpre,
+                                 void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Newton-Schulz orthogonalisation of `parties` matrices of rows x cols, of which the shorter side is at most
+ * HAFLO_ADAPTER_MAX_RANK, as an adapter's gradient is:
+ *   X = G / (|G|_F + eps);  for each step (a, b, c): K = X X^T, X <- a X + (b K + c K^2) X;   out = keep base + scale X
+ * (of a matrix with more rows than columns K = X^T X, from the right). d_coefficients: host memory, steps x 3; five times
+ * (3.4445, -4.7750, 2.0315) brings singular values between about 0.7 and 1.2, (1.5, -0.5, 0) towards 1. d_base NULL: none.
+ * Matrices lie step_* elements apart. All products are held in 64 bits. A NaN or an infinity in a matrix makes its X NaN; one of
+ * zeros gives X = 0. d_out may be d_g or d_base where all distances are the same (else HAFLO_EINVAL).
+ * 1 <= steps <= HAFLO_UPDATE_MAX_STEPS, parties <= HAFLO_ADAPTER_MAX_PARTIES, parties times the longer side <= 2^38, ldo <= 2^32,
+ * eps > 0, all factors finite.
+ */
+#define HAFLO_UPDATE_MAX_STEPS 16
+size_t haflo_update_workspace_bytes(int type, size_t parties, size_t rows, size_t cols);
+int haflo_orthogonal_update(int type, const void* d_g, size_t ldg, size_t step_g, const void* d_base, size_t ldb,
+                            size_t step_b, size_t parties, size_t rows, size_t cols, const double* coefficients, int steps,
+                            double keep, double scale, double eps, void* d_out, size_t ldo, size_t step_o, void* d_workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of eight bits: scale = amax / 127 and q = rint(x (127 / amax)), -127 .. 127, of each row, the quotients and the product
+ * rounded to float32. d_q: rows of HAFLO_INT8_ROW * ceil(cols / HAFLO_INT8_ROW) bytes, dense, zeros behind the columns, at a 16-byte
+ * boundary. A row of zeros has scale 0; a row with a NaN or an infinity has scale NaN and q = 0.
+ * 1 <= cols <= HAFLO_INT8_MAX_COLS.
+ */
+#define HAFLO_INT8_ROW 128
+#define HAFLO_INT8_MAX_COLS 130944
+int haflo_quantize_rows(int type, const void* d_x, size_t ldx, size_t rows, size_t cols, int8_t* d_q, float* d_scale,
+                        void* stream);
+/*
+ * A projection with weights of eight bits, as the common model answers with:
+ *   y[t, o] = x_scale[t] w_scale[o] sum_k xq[t, k] wq[o, k] + bias[o] + residual[t, o]
+ * d_xq, d_wq (outer rows): as haflo_quantize_rows lays them out, of `inner` columns; sums are exact. rows * outer <= 2^42. d_bias: float32[outer] or NULL;
+ * d_residual (type, rows x outer) or NULL; d_y may be d_residual where the distances between rows are the same (else HAFLO_EINVAL).
+ */
+int haflo_int8_product(int type, const int8_t* d_xq, const float* d_x_scale, const int8_t* d_wq, const float* d_w_scale,
+                       const float* d_bias, const void* d_residual, size_t ldr, size_t rows, size_t inner, size_t outer,
+                       void* d_y, size_t ldy, void* stream);
+/* The same of x (type, rows x inner), which is brought to eight bits first, in the workspace. */
+size_t haflo_int8_workspace_bytes(int type, size_t rows, size_t inner, size_t outer);
+int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq, const float* d_w_scale,
+                       const float* d_bias, const void* d_residual, size_t ldr, size_t rows, size_t inner, size_t outer,
+                       void* d_y, size_t ldy, void* d_workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -105,6 +105,23 @@ LOCAL_PROTOTYPES = {
     "haflo_label_logprobs_backward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_void_p, c_size_t, c_size_t, c_size_t, c_void_p, c_size_t,
                                               c_void_p]),
+    "haflo_residual_norm": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p,
+                                    c_size_t, c_size_t, c_double, c_double, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p]),
+    "haflo_residual_norm_workspace_bytes": (c_size_t, [c_int, c_size_t, c_size_t]),
+    "haflo_residual_norm_backward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_size_t,
+                                             c_void_p, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_size_t, c_size_t, c_double,
+                                             c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_size_t, c_void_p]),
+    "haflo_update_workspace_bytes": (c_size_t, [c_int, c_size_t, c_size_t, c_size_t]),
+    "haflo_orthogonal_update": (c_int, [c_int, c_void_p, c_size_t, c_size_t, c_void_p, c_size_t, c_size_t, c_size_t, c_size_t, c_size_t,
+                                        C.POINTER(c_double), c_int, c_double, c_double, c_double, c_void_p, c_size_t, c_size_t, c_void_p,
+                                        c_size_t, c_void_p]),
+    "haflo_quantize_rows": (c_int, [c_int, c_void_p, c_size_t, c_size_t, c_size_t, c_void_p, c_void_p, c_void_p]),
+    "haflo_int8_product": (c_int, [c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_size_t, c_size_t,
+                                   c_size_t, c_void_p, c_size_t, c_void_p]),
+    "haflo_int8_workspace_bytes": (c_size_t, [c_int, c_size_t, c_size_t, c_size_t]),
+    "haflo_int8_forward": (c_int, [c_int, c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_size_t, c_size_t,
+                                   c_size_t, c_void_p, c_size_t, c_void_p, c_size_t, c_void_p]),
 }
 TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
 LIMBS_29_MAD64, LIMBS_29_MAD64_SQUARE, LIMBS_24_MUL24, LIMBS_23_FMA64 = 0, 1, 2, 3

@@ -496,6 +496,165 @@ def haflo_label_logprobs_backward(logits, label, lse, entropy, dlogp, dentropy=N
     return out
 
 
+def _vector(t, n):
+    """Address of float32 values for `n` columns, or None."""
+    return None if t is None else _dense(t, torch.float32, n)
+
+
+def _norm_operands(x, f, post, gate, pre):
+    dtype = x.dtype
+    kind, (rows, cols, ldx) = _type(x), _matrix(x, dtype)
+    ldf = cols if f is None else _matrix(f, dtype, rows, cols)[2]
+    pg = pc = None
+    ldg = cols
+    if gate is not None:
+        if gate.dim() == 1:
+            pc = _vector(gate, cols)
+        else:
+            ldg, pg = _matrix(gate, dtype, rows, cols)[2], gate.data_ptr()
+    return kind, rows, cols, (x.data_ptr(), ldx, None if f is None else f.data_ptr(), ldf, _vector(post, cols), pg, ldg, pc, _vector(pre, cols))
+
+
+def _result(like, rows, cols, out):
+    """A result of like's type and the distance between its rows: `out`, or a new one."""
+    if out is None:
+        return like.new_empty((rows, cols)), cols
+    return out, _matrix(out, like.dtype, rows, cols)[2]
+
+
+def haflo_residual_norm(x, f=None, post=None, gate=None, pre=None, scale=1.0, eps=1e-6, out=None, normed=None):
+    """The norms around a block with its gate and the residual stream, row by row: r = scale x + gate p, p = f / sqrt(mean f^2 + eps) post
+    (f itself without `post`), and h = r / sqrt(mean r^2 + eps) pre. x: the stream before the block, f: what the block gave (None: r
+    is x), gate: float32 [cols] for all rows, or a matrix of x's type, or None; post, pre: float32 [cols] or None. Returns r (None without f), h
+    (None without pre) and, for haflo_residual_norm_backward, both roots' reciprocals (float32 [2, rows]); autograd records nothing.
+    `out` and `normed`, what r and h are written to, may each be one of the inputs."""
+    stream = _stream_of(x, f, post, gate, pre, out, normed)
+    kind, rows, cols, operands = _norm_operands(x, f, post, gate, pre)
+    r, ldr = (None, cols) if f is None else _result(x, rows, cols, out)
+    h, ldh = (None, cols) if pre is None else _result(x, rows, cols, normed)
+    rstd = x.new_empty((2, rows), dtype=torch.float32)
+    _check(lib().haflo_residual_norm(kind, *operands, rows, cols, scale, eps, None if r is None else r.data_ptr(), ldr,
+                                     None if h is None else h.data_ptr(), ldh, rstd.data_ptr(), stream))
+    return r, h, rstd
+
+
+def haflo_residual_norm_backward(dh, dr, x, f, post, gate, pre, rstd, scale=1.0, need_dx=True):
+    """Gradients of haflo_residual_norm for its arguments and its rstd, from that of h (None without pre) and the one that r has from
+    elsewhere (None: zeros): by x (None without need_dx), f, post, gate and pre, each None where that is None; those of float32 [cols] are
+    sums over the rows."""
+    stream = _stream_of(dh, dr, x, f, post, gate, pre, rstd)
+    kind, rows, cols, operands = _norm_operands(x, f, post, gate, pre)
+    if (dh is None) != (pre is None):
+        raise HafloError("dh: the gradient of h, where there is one")
+    lddh = cols if dh is None else _matrix(dh, x.dtype, rows, cols)[2]
+    lddr = cols if dr is None else _matrix(dr, x.dtype, rows, cols)[2]
+    pr = _dense(rstd, torch.float32, 2, rows)
+    dx = x.new_empty((rows, cols)) if need_dx else None
+    df = None if f is None else x.new_empty((rows, cols))
+    by_cols = gate is not None and gate.dim() == 1
+    dgate = None if gate is None else gate.new_empty(gate.shape)
+    dpost, dpre = (None if t is None else t.new_empty(cols) for t in (post, pre))
+    nbytes = lib().haflo_residual_norm_workspace_bytes(kind, rows, cols)
+    pw, ws = _scratch(nbytes, x)
+    at = [None if t is None else t.data_ptr() for t in (dh, dr, dx, df, dgate, dpost, dpre)]
+    _check(lib().haflo_residual_norm_backward(kind, at[0], lddh, at[1], lddr, *operands, pr, rows, cols, scale, at[2], cols, at[3], cols,
+                                              None if by_cols else at[4], cols, at[4] if by_cols else None, at[5], at[6], pw, nbytes, stream))
+    return dx, df, dpost, dgate, dpre
+
+
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def _batch(t, dtype, shape):
+    """(address, distance between rows, distance between matrices) of matrices whose rows are contiguous."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise HafloError("expected %s of shape %s, got %s of %s" % (dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    _, rows, cols = shape
+    step, ld, one = t.stride()
+    if t.is_contiguous():
+        return t.data_ptr(), cols, rows * cols
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1) or step < 0:
+        raise HafloError("expected rows of contiguous elements that do not overlap")
+    return t.data_ptr(), max(ld, cols), step
+
+
+def haflo_orthogonal_update(g, base=None, keep=1.0, scale=1.0, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None):
+    """keep base + scale X, X from Newton-Schulz steps on each matrix of g [parties, rows, cols], the shorter side at most 128: X = g /
+    (|g| + eps), then for each (a, b, c) of `coefficients` X <- a X + (b K + c K^2) X, K = X X^T. base, and out, which may be g or base: of
+    g's type and shape; without base scale X alone. Products are held in 64 bits; autograd records nothing."""
+    stream = _stream_of(g, base, out)
+    dtype, shape = g.dtype, g.shape
+    kind = _type(g)
+    if g.dim() != 3:
+        raise HafloError("g: parties x rows x cols")
+    steps = len(coefficients)
+    if not 1 <= steps <= 16 or any(len(c) != 3 for c in coefficients):
+        raise HafloError("coefficients: three of each of 1 to 16 steps")
+    parties, rows, cols = shape
+    pg, pb = _batch(g, dtype, shape), (None, cols, 0) if base is None else _batch(base, dtype, shape)
+    if out is None:
+        out = g.new_empty(shape)
+    po = _batch(out, dtype, shape)
+    nbytes = lib().haflo_update_workspace_bytes(kind, parties, rows, cols)
+    pw, ws = _scratch(nbytes, g)
+    values = (C.c_double * (3 * steps))(*(v for c in coefficients for v in c))
+    _check(lib().haflo_orthogonal_update(kind, *pg, *pb, parties, rows, cols, values, steps, keep, scale, eps, *po, pw, nbytes, stream))
+    return out
+
+
+def _int8_width(cols):
+    return (cols + 127) // 128 * 128
+
+
+def haflo_quantize_rows(x):
+    """Rows of eight bits: q = rint(x (127 / amax)) as int8 with zeros up to a multiple of 128 columns, and each row's scale amax / 127
+    (float32; NaN, with q = 0, for a row that holds a NaN or an infinity)."""
+    stream = _stream_of(x)
+    kind, (rows, cols, ldx) = _type(x), _matrix(x, x.dtype)
+    q, scale = x.new_empty((rows, _int8_width(cols)), dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
+    _check(lib().haflo_quantize_rows(kind, x.data_ptr(), ldx, rows, cols, q.data_ptr(), scale.data_ptr(), stream))
+    return q, scale
+
+
+def _int8_weights(wq, w_scale, inner, bias):
+    if wq.dim() != 2:
+        raise HafloError("wq: outer x width, as haflo_quantize_rows gives it")
+    outer = wq.shape[0]
+    return outer, _dense(wq, torch.int8, outer, _int8_width(inner)), _dense(w_scale, torch.float32, outer), _vector(bias, outer)
+
+
+def haflo_int8_product(xq, x_scale, wq, w_scale, cols, dtype=torch.float32, bias=None, residual=None, out=None):
+    """x_scale w_scale (xq wq^T) + bias + residual of rows and weights that haflo_quantize_rows brought to eight bits, from `cols` columns
+    both; the whole numbers' sums are exact. bias float32 [outer]; residual, and out, which may be it: [rows, outer] of `dtype`."""
+    stream = _stream_of(xq, x_scale, wq, w_scale, bias, residual, out)
+    if xq.dim() != 2:
+        raise HafloError("xq: rows x width, as haflo_quantize_rows gives it")
+    rows, like = xq.shape[0], x_scale.new_empty(0, dtype=dtype)
+    kind, px, ps = _type(like), _dense(xq, torch.int8, rows, _int8_width(cols)), _dense(x_scale, torch.float32, rows)
+    outer, pw, pws, pb = _int8_weights(wq, w_scale, cols, bias)
+    ldr = outer if residual is None else _matrix(residual, dtype, rows, outer)[2]
+    y, ldy = _result(like, rows, outer, out)
+    _check(lib().haflo_int8_product(kind, px, ps, pw, pws, pb, None if residual is None else residual.data_ptr(), ldr, rows, cols, outer,
+                                    y.data_ptr(), ldy, stream))
+    return y
+
+
+def haflo_int8_forward(x, wq, w_scale, bias=None, residual=None, out=None):
+    """haflo_int8_product of x, whose rows are brought to eight bits within the call: the projection with weights of eight bits that the
+    common model answers with. It is not trained through. The result is of x's type."""
+    stream = _stream_of(x, wq, w_scale, bias, residual, out)
+    dtype = x.dtype
+    kind, (rows, inner, ldx) = _type(x), _matrix(x, dtype)
+    outer, pw, pws, pb = _int8_weights(wq, w_scale, inner, bias)
+    ldr = outer if residual is None else _matrix(residual, dtype, rows, outer)[2]
+    y, ldy = _result(x, rows, outer, out)
+    nbytes = lib().haflo_int8_workspace_bytes(kind, rows, inner, outer)
+    pws2, ws = _scratch(nbytes, x)
+    _check(lib().haflo_int8_forward(kind, x.data_ptr(), ldx, pw, pws, pb, None if residual is None else residual.data_ptr(), ldr, rows, inner, outer,
+                                    y.data_ptr(), ldy, pws2, nbytes, stream))
+    return y
+
+
 class Stager:
     """Owner of a haflo_stager: host numpy arrays in the interchange format <-> device arrays."""
 

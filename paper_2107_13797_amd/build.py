@@ -15,7 +15,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libhaflo.so")
 PEAK_LIB = os.path.join(HERE, "libhaflo_peak.so")  # the roofline microbenchmarks, a library of their own
 SOURCES = ["ctx.cpp", "staging.cpp", "store.cpp", "kernels_basic.hip", "kernels_modexp.hip", "kernels_rns.hip", "kernels_matvec.hip", "kernels_buckets.hip", "kernels_loss.hip",
-           "local_dropout.hip", "local_adapters.hip", "local_labels.hip"]
+           "local_dropout.hip", "local_adapters.hip", "local_labels.hip", "local_norm.hip", "local_update.hip", "local_int8.hip"]
 PEAK_SOURCES = ["peak_microbench.hip", "limb_variants.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -79,6 +79,17 @@ __device__ __forceinline__ void store_some(T* p, const Vec8<T>& v, int n) {
     if (j < n) p[j] = v.get(j);
 }
 
+// Eight elements of a row from column `col` on, zeros behind its end; no element of another vector is read.
+template <class T>
+__device__ __forceinline__ Vec8<T> load_cols(const T* row, u32 col, u32 cols) {
+  return col + 8 <= cols ? load_wide(row + col) : load_some(row + col, col < cols ? (int)(cols - col) : 0);
+}
+template <class T>
+__device__ __forceinline__ void store_cols(T* row, u32 col, u32 cols, const Vec8<T>& v) {
+  if (col + 8 <= cols) store_wide(row + col, v);
+  else store_some(row + col, v, col < cols ? (int)(cols - col) : 0);
+}
+
 // The dropout of one call: what a kernel needs of (p, seed, offset).
 struct Drop {
   u32 threshold;  // draws below it drop their element; 0: no dropout
@@ -125,6 +136,9 @@ __device__ __forceinline__ float lane_read(float v, int lane) {
 __device__ __forceinline__ u64 lane_read(u64 v, int lane) {
   const u32 lo = lane_read((u32)v, lane), hi = lane_read((u32)(v >> 32), lane);
   return (u64)hi << 32 | lo;
+}
+__device__ __forceinline__ double lane_read(double v, int lane) {
+  return __builtin_bit_cast(double, lane_read(__builtin_bit_cast(u64, v), lane));
 }
 
 // acc += a b on 16 x 16 by 32: lane l holds rows l % 16 of both operands at elements 8 (l / 16) .. + 7, and in

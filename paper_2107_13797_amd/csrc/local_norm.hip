@@ -1,0 +1,492 @@
+// The norms around a block of a model, with the gate and the residual stream between them, and their gradients.
+//
+//   forward   p = f q post (q = 1 / sqrt(mean f^2 + eps); p = f without a norm behind the block)
+//             r = scale x + gate p,   h = r t pre,   t = 1 / sqrt(mean r^2 + eps)
+//   backward  a = dh pre,  D = dr + t (a - r^ mean(a r^)),  r^ = r t          dx = scale D,  dpre = sum over rows of dh r^
+//             b = D gate post,  df = q (b - f^ mean(b f^)),  f^ = f q         dgate = D p,  dpost = sum over rows of D gate f^
+//
+// A lane holds eight columns of a row and a group of lanes the row, so that each matrix is read once. Means of squares are
+// taken in 64 bits: every float32 has a square there. The way back forms p and r again from x, f and both roots, which is
+// fewer bytes than reading them, and keeps its columns' sums over all rows that a block takes.
+#include "local_common.hpp"
+
+using namespace haflo::local;
+
+namespace {
+
+constexpr u32 kThreads = 256;
+constexpr u32 kMostLanes = 1024;                      // of one row
+constexpr size_t kRowCols = (size_t)kMostLanes * 8;   // columns of a row that lanes hold; longer rows are read again
+constexpr size_t kNormBlocks = 2048, kBackBlocks = 512;
+constexpr u32 kTileCols = kThreads * 8;               // of the long rows' way back
+
+enum Mode { kStream = 0, kGated = 1, kFullGate = 2 };  // r = x; a block's f with a gate by columns or none; a gate for every element
+
+template <class T>
+struct Norm {
+  const T *x, *f, *gate;
+  size_t ldx, ldf, ldg;
+  const float *gate_cols, *post, *pre;
+  u32 rows, cols;
+  float scale;
+  double eps, per_col;  // 1 / cols
+};
+
+struct Eight {
+  float v[8];
+};
+template <class T>
+__device__ __forceinline__ Eight floats(const Vec8<T>& a) {
+  Eight e;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e.v[j] = (float)a.get(j);
+  return e;
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> rounded(const Eight& e) {
+  Vec8<T> a = {};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) a.set(j, (T)e.v[j]);
+  return a;
+}
+__device__ __forceinline__ Eight gains(const float* g, u32 col, u32 cols) {  // ones without any
+  if (g) return floats(load_cols(g, col, cols));
+  Eight e;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e.v[j] = 1.0f;
+  return e;
+}
+__device__ __forceinline__ double squares(const Eight& e) {
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s += (double)e.v[j] * (double)e.v[j];
+  return s;
+}
+__device__ __forceinline__ float products(const Eight& a, const Eight& b) {
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s += a.v[j] * b.v[j];
+  return s;
+}
+
+// The sum over a row's group of `lanes` lanes, a power of two, the same bits in each. Groups of more than a wavefront are whole blocks, and
+// take turns at two places in LDS: a wavefront is at most one sum ahead.
+template <class S>
+struct GroupSum {
+  S (*parts)[kMostLanes / kWave];
+  u32 lanes, turn;
+  __device__ __forceinline__ S operator()(S v) {
+    for (u32 d = 1; d < lanes && d < kWave; d <<= 1) v += lane_read(v, (int)(lane_id() ^ d));
+    if (lanes > kWave) {
+      turn ^= 1;
+      if (lane_id() == 0) parts[turn][threadIdx.x / kWave] = v;
+      __syncthreads();
+      v = parts[turn][0];
+      for (u32 w = 1; w < lanes / kWave; ++w) v += parts[turn][w];
+    }
+    return v;
+  }
+};
+__device__ __forceinline__ float root(double sum, double per_col, double eps) { return (float)(1.0 / sqrt(sum * per_col + eps)); }
+
+// f^ and r of eight columns; f^ is f where q is 1
+template <int MODE>
+__device__ __forceinline__ void join_stream(const Eight& x, Eight& f, const Eight& post, const Eight& gate, float q, float scale, Eight& p, Eight& r) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    f.v[j] *= q;
+    p.v[j] = f.v[j] * post.v[j];
+    r.v[j] = MODE == kStream ? x.v[j] : scale * x.v[j] + gate.v[j] * p.v[j];
+  }
+}
+
+// Memory bounds it.
+template <class T, int MODE, int MOST>
+__global__ __launch_bounds__(MOST) void k_norm(Norm<T> n, u32 lanes, T* r_out, size_t ldr, T* h_out, size_t ldh, float* rstd) {
+  __shared__ double parts[2][kMostLanes / kWave];
+  GroupSum<double> sum = {parts, lanes, 0};
+  const u32 groups = blockDim.x / lanes, col = threadIdx.x % lanes * 8;
+  const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
+  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += (u64)gridDim.x * groups) {
+    const u64 mine = base + threadIdx.x / lanes;
+    const bool live = mine < n.rows;
+    const u64 row = live ? mine : n.rows - 1;
+    Vec8<T> xv = load_cols(n.x + row * n.ldx, col, n.cols), fv = {}, gv = {};
+    if (MODE != kStream) fv = load_cols(n.f + row * n.ldf, col, n.cols);
+    if (MODE == kFullGate) gv = load_cols(n.gate + row * n.ldg, col, n.cols);
+    Eight f = floats(fv), p, r;
+    float q = 1.0f, t = 1.0f;
+    if (MODE != kStream && n.post) q = root(sum(squares(f)), n.per_col, n.eps);
+    join_stream<MODE>(floats(xv), f, post, MODE == kFullGate ? floats(gv) : by_cols, q, n.scale, p, r);
+    if (n.pre) t = root(sum(squares(r)), n.per_col, n.eps);
+    if (!live) continue;
+    if (MODE != kStream) store_cols(r_out + row * ldr, col, n.cols, rounded<T>(r));
+    if (n.pre) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r.v[j] *= t * pre.v[j];
+      store_cols(h_out + row * ldh, col, n.cols, rounded<T>(r));
+    }
+    if (col == 0) {
+      rstd[row] = q;
+      rstd[n.rows + row] = t;
+    }
+  }
+}
+
+// The same for rows that the lanes do not hold: a block takes a row, and reads it once for each mean and once for the results.
+template <class T, int MODE>
+__global__ __launch_bounds__(kMostLanes) void k_norm_long(Norm<T> n, T* r_out, size_t ldr, T* h_out, size_t ldh, float* rstd) {
+  __shared__ double parts[2][kMostLanes / kWave];
+  GroupSum<double> sum = {parts, kMostLanes, 0};
+  for (u64 row = blockIdx.x; row < n.rows; row += gridDim.x) {
+    float q = 1.0f, t = 1.0f;
+    const auto stream = [&](u32 col) {
+      Eight f = {}, gate = {}, p, r;
+      if (MODE != kStream) f = floats(load_cols(n.f + row * n.ldf, col, n.cols));
+      if (MODE != kStream) gate = MODE == kFullGate ? floats(load_cols(n.gate + row * n.ldg, col, n.cols)) : gains(n.gate_cols, col, n.cols);
+      join_stream<MODE>(floats(load_cols(n.x + row * n.ldx, col, n.cols)), f, gains(n.post, col, n.cols), gate, q, n.scale, p, r);
+      return r;
+    };
+    if (MODE != kStream && n.post) {
+      double s = 0.0;
+      for (u32 col = threadIdx.x * 8; col < n.cols; col += kRowCols) s += squares(floats(load_cols(n.f + row * n.ldf, col, n.cols)));
+      q = root(sum(s), n.per_col, n.eps);
+    }
+    if (n.pre) {
+      double s = 0.0;
+      for (u32 col = threadIdx.x * 8; col < n.cols; col += kRowCols) s += squares(stream(col));
+      t = root(sum(s), n.per_col, n.eps);
+    }
+    for (u32 col = threadIdx.x * 8; col < n.cols; col += kRowCols) {
+      Eight r = stream(col);
+      if (MODE != kStream) store_cols(r_out + row * ldr, col, n.cols, rounded<T>(r));
+      if (n.pre) {
+        const Eight pre = gains(n.pre, col, n.cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.v[j] *= t * pre.v[j];
+        store_cols(h_out + row * ldh, col, n.cols, rounded<T>(r));
+      }
+    }
+    if (threadIdx.x == 0) {
+      rstd[row] = q;
+      rstd[n.rows + row] = t;
+    }
+  }
+}
+
+template <class T>
+struct Back {
+  const T *dh, *dr;
+  size_t lddh, lddr;
+  const float* rstd;
+  T *dx, *df, *dgate;
+  size_t lddx, lddf, lddg;
+  float* sums;   // of dpost, dgate by columns and dpre: blocks x width each
+  u32 width;     // of a row of them
+};
+// Eight columns of a row on the way back, up to the means.
+struct BackRow {
+  Eight x, f, gate, dh, dr;  // f: f^ from its root on
+  float q, t;
+};
+template <class T, int MODE>
+__device__ __forceinline__ BackRow back_load(const Norm<T>& n, const Back<T>& b, u64 row, u32 col, const Eight& by_cols) {
+  BackRow v;
+  Vec8<T> xv = load_cols(n.x + row * n.ldx, col, n.cols), fv = {}, gv = {}, hv = {}, rv = {};
+  if (MODE != kStream) fv = load_cols(n.f + row * n.ldf, col, n.cols);
+  if (MODE == kFullGate) gv = load_cols(n.gate + row * n.ldg, col, n.cols);
+  if (n.pre) hv = load_cols(b.dh + row * b.lddh, col, n.cols);
+  if (b.dr) rv = load_cols(b.dr + row * b.lddr, col, n.cols);
+  v.x = floats(xv);
+  v.f = floats(fv);
+  v.gate = MODE == kFullGate ? floats(gv) : by_cols;
+  v.dh = floats(hv);
+  v.dr = floats(rv);
+  v.q = b.rstd[row];
+  v.t = b.rstd[n.rows + row];
+  return v;
+}
+// from there to D: v.dr; r^ in `unit`
+__device__ __forceinline__ void stream_grad(BackRow& v, const Eight& unit, const Eight& pre, float mean) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v.dr.v[j] += v.t * (v.dh.v[j] * pre.v[j] - unit.v[j] * mean);
+}
+struct Sums {
+  Eight post, gate, pre;
+};
+template <class T, int MODE>
+__device__ __forceinline__ void back_store(const Norm<T>& n, const Back<T>& b, u64 row, u32 col, const BackRow& v, const Eight& p, const Eight& unit,
+                                           const Eight& post, float mean, Sums& s) {
+  Eight dx, df, dg;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    dx.v[j] = MODE == kStream ? v.dr.v[j] : n.scale * v.dr.v[j];
+    s.pre.v[j] += v.dh.v[j] * unit.v[j];
+    if (MODE != kStream) {
+      const float dp = v.dr.v[j] * v.gate.v[j];
+      df.v[j] = n.post ? v.q * (dp * post.v[j] - v.f.v[j] * mean) : dp;
+      s.post.v[j] += dp * v.f.v[j];
+      dg.v[j] = v.dr.v[j] * p.v[j];
+      s.gate.v[j] += dg.v[j];
+    }
+  }
+  if (b.dx) store_cols(b.dx + row * b.lddx, col, n.cols, rounded<T>(dx));
+  if (MODE != kStream && b.df) store_cols(b.df + row * b.lddf, col, n.cols, rounded<T>(df));
+  if (MODE == kFullGate && b.dgate) store_cols(b.dgate + row * b.lddg, col, n.cols, rounded<T>(dg));
+}
+
+// Memory bounds it.
+template <class T, int MODE, int MOST>
+__global__ __launch_bounds__(MOST) void k_norm_back(Norm<T> n, Back<T> b, u32 lanes) {
+  __shared__ float parts[2][kMostLanes / kWave];
+  __shared__ float joined[3][kThreads * 8];
+  GroupSum<float> sum = {parts, lanes, 0};
+  const u32 groups = blockDim.x / lanes, group = threadIdx.x / lanes, col = threadIdx.x % lanes * 8;
+  const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
+  Sums s = {};
+  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += (u64)gridDim.x * groups) {
+    const u64 mine = base + group;
+    const bool live = mine < n.rows;
+    const u64 row = live ? mine : n.rows - 1;
+    BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
+    Eight p, unit;
+    join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
+    if (n.pre) {
+      Eight a;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a.v[j] = v.dh.v[j] * pre.v[j];
+      stream_grad(v, unit, pre, sum(products(a, unit)) * (float)n.per_col);
+    }
+    float mean = 0.0f;
+    if (MODE != kStream && n.post) {
+      Eight a;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a.v[j] = v.dr.v[j] * v.gate.v[j] * post.v[j];
+      mean = sum(products(a, v.f)) * (float)n.per_col;
+    }
+    if (live) back_store<T, MODE>(n, b, row, col, v, p, unit, post, mean, s);
+  }
+  // the groups' sums of the same columns, in their order
+  Eight* const mine[3] = {&s.post, &s.gate, &s.pre};
+  if (groups > 1) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) joined[i][threadIdx.x * 8 + j] = mine[i]->v[j];
+    __syncthreads();
+    if (group != 0) return;
+    for (u32 g = 1; g < groups; ++g)
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mine[i]->v[j] += joined[i][(g * lanes + threadIdx.x) * 8 + j];
+  }
+  if (col < b.width)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) store_wide(b.sums + ((size_t)i * gridDim.x + blockIdx.x) * b.width + col, rounded<float>(*mine[i]));
+}
+
+// Long rows: both means of a row, by one block.
+template <class T, int MODE>
+__global__ __launch_bounds__(kMostLanes) void k_norm_means(Norm<T> n, Back<T> b, float* means) {
+  __shared__ float parts[2][kMostLanes / kWave];
+  GroupSum<float> sum = {parts, kMostLanes, 0};
+  for (u64 row = blockIdx.x; row < n.rows; row += gridDim.x) {
+    float first = 0.0f, second = 0.0f;
+    // `step` 0: a r^ of eight columns; 1: b f^, with the first mean
+    const auto terms = [&](u32 col, int step) {
+      const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
+      BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
+      Eight p, unit, a;
+      join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
+      if (step == 1 && n.pre) stream_grad(v, unit, pre, first);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a.v[j] = step == 0 ? v.dh.v[j] * pre.v[j] : v.dr.v[j] * v.gate.v[j] * post.v[j];
+      return products(a, step == 0 ? unit : v.f);
+    };
+    if (n.pre) {
+      float s = 0.0f;
+      for (u32 col = threadIdx.x * 8; col < n.cols; col += kRowCols) s += terms(col, 0);
+      first = sum(s) * (float)n.per_col;
+    }
+    if (MODE != kStream && n.post) {
+      float s = 0.0f;
+      for (u32 col = threadIdx.x * 8; col < n.cols; col += kRowCols) s += terms(col, 1);
+      second = sum(s) * (float)n.per_col;
+    }
+    if (threadIdx.x == 0) {
+      means[row] = first;
+      means[n.rows + row] = second;
+    }
+  }
+}
+// Long rows with their means: a block takes eight columns a lane of every `blocks`-th row.
+template <class T, int MODE>
+__global__ __launch_bounds__(kThreads) void k_norm_back_long(Norm<T> n, Back<T> b, const float* means, u32 blocks) {
+  const u32 part = blockIdx.x % blocks, col = blockIdx.x / blocks * kTileCols + threadIdx.x * 8;
+  if (col >= n.cols) return;
+  const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
+  Sums s = {};
+  for (u64 row = part; row < n.rows; row += blocks) {
+    BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
+    Eight p, unit;
+    join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
+    if (n.pre) stream_grad(v, unit, pre, means[row]);
+    back_store<T, MODE>(n, b, row, col, v, p, unit, post, means[n.rows + row], s);
+  }
+  const Eight* const mine[3] = {&s.post, &s.gate, &s.pre};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) store_wide(b.sums + ((size_t)i * blocks + part) * b.width + col, rounded<float>(*mine[i]));
+}
+
+// The blocks' sums of 64 columns: four wavefronts take a quarter of the blocks each.
+struct Joined {
+  float* out[3];
+};
+__global__ __launch_bounds__(kThreads) void k_norm_join(const float* sums, u32 blocks, u32 width, u32 cols, Joined to) {
+  __shared__ float parts[kThreads / kWave][kWave];
+  const u32 tiles = (cols + kWave - 1) / kWave, which = blockIdx.x / tiles, lane = lane_id(), wave = threadIdx.x / kWave;
+  const u32 col = blockIdx.x % tiles * kWave + lane;
+  float* const out = which == 0 ? to.out[0] : which == 1 ? to.out[1] : to.out[2];
+  if (!out) return;
+  float s = 0.0f;
+  const u32 first = (u32)((u64)blocks * wave / 4), end = (u32)((u64)blocks * (wave + 1) / 4);
+  if (col < cols)
+    for (u32 i = first; i < end; ++i) s += sums[((size_t)which * blocks + i) * width + col];
+  parts[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && col < cols) out[col] = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
+}
+
+u32 lanes_of(size_t cols) {
+  u32 lanes = 1;
+  while ((size_t)lanes * 8 < cols) lanes *= 2;
+  return lanes;
+}
+u32 threads_of(u32 lanes) { return lanes <= (u32)kWave ? kThreads : lanes; }
+size_t row_blocks(size_t rows, size_t cols, size_t most) {
+  const u32 lanes = lanes_of(cols);
+  const size_t need = ceil_div(rows, threads_of(lanes) / lanes);
+  return need < most ? need : most;
+}
+struct Plan {
+  size_t blocks, width, means, total;
+};
+Plan back_plan(size_t rows, size_t cols) {
+  Plan p;
+  p.width = ceil_div(cols, 8) * 8;
+  p.blocks = cols <= kRowCols ? row_blocks(rows, cols, kBackBlocks) : rows < 64 ? rows : 64;
+  p.means = align256(3 * p.blocks * p.width * 4);
+  p.total = p.means + (cols <= kRowCols ? 0 : align256(2 * rows * 4));
+  return p;
+}
+bool norm_sizes(int type, size_t rows, size_t cols) { return valid_type(type) && rows <= kMostCount && cols >= 1 && cols <= kMostCount; }
+
+template <class T, int MODE>
+void norm(const Norm<T>& n, T* r, size_t ldr, T* h, size_t ldh, float* rstd, hipStream_t st) {
+  if (n.cols > kRowCols) {
+    hipLaunchKernelGGL((k_norm_long<T, MODE>), dim3((unsigned)(n.rows < kNormBlocks ? n.rows : kNormBlocks)), dim3(kMostLanes), 0, st, n, r, ldr, h, ldh,
+                       rstd);
+    return;
+  }
+  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes);
+  const dim3 grid((unsigned)row_blocks(n.rows, n.cols, kNormBlocks)), block(threads);
+  if (threads > 512) hipLaunchKernelGGL((k_norm<T, MODE, kMostLanes>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
+  else hipLaunchKernelGGL((k_norm<T, MODE, 512>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
+}
+template <class T, int MODE>
+void norm_back(const Norm<T>& n, const Back<T>& b, const Plan& plan, char* ws, hipStream_t st) {
+  if (n.cols > kRowCols) {
+    float* const means = (float*)(ws + plan.means);
+    hipLaunchKernelGGL((k_norm_means<T, MODE>), dim3((unsigned)(n.rows < kNormBlocks ? n.rows : kNormBlocks)), dim3(kMostLanes), 0, st, n, b, means);
+    hipLaunchKernelGGL((k_norm_back_long<T, MODE>), dim3((unsigned)(plan.blocks * ceil_div(n.cols, kTileCols))), dim3(kThreads), 0, st, n, b,
+                       (const float*)means, (u32)plan.blocks);
+    return;
+  }
+  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes);
+  const dim3 grid((unsigned)plan.blocks), block(threads);
+  if (threads > 512) hipLaunchKernelGGL((k_norm_back<T, MODE, kMostLanes>), grid, block, 0, st, n, b, lanes);
+  else hipLaunchKernelGGL((k_norm_back<T, MODE, 512>), grid, block, 0, st, n, b, lanes);
+}
+
+}  // namespace
+
+extern "C" {
+
+int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, size_t ldf, const float* d_post, const void* d_gate, size_t ldg,
+                        const float* d_gate_cols, const float* d_pre, size_t rows, size_t cols, double scale, double eps, void* d_r, size_t ldr,
+                        void* d_h, size_t ldh, float* d_rstd, void* stream) {
+  if (!norm_sizes(type, rows, cols) || !(eps > 0.0 && eps < HUGE_VAL) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
+  if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
+  if (rows == 0) return HAFLO_OK;
+  if (!d_x || ldx < cols || (d_f && (ldf < cols || !d_r || ldr < cols)) || (d_gate && ldg < cols) || (d_pre && (!d_h || ldh < cols)) || !d_rstd)
+    return HAFLO_EINVAL;
+  const struct {
+    const void* p;
+    size_t ld;
+  } in[3] = {{d_x, ldx}, {d_f, ldf}, {d_gate, ldg}}, out[2] = {{d_f ? d_r : nullptr, ldr}, {d_pre ? d_h : nullptr, ldh}};
+  for (const auto& o : out)
+    for (const auto& i : in)
+      if (o.p && !in_place(i.p, i.ld, o.p, o.ld, rows)) return HAFLO_EINVAL;
+  if (out[0].p && out[0].p == out[1].p) return HAFLO_EINVAL;
+  const hipStream_t st = (hipStream_t)stream;
+  HAFLO_LOCAL_TYPES(type, {
+    const Norm<T> n = {(const T*)d_x, (const T*)d_f, (const T*)d_gate, ldx, ldf, ldg, d_gate_cols, d_post, d_pre, (u32)rows, (u32)cols, (float)scale,
+                       eps, 1.0 / (double)cols};
+    if (!d_f) norm<T, kStream>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
+    else if (d_gate) norm<T, kFullGate>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
+    else norm<T, kGated>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
+  });
+  return launched();
+}
+
+size_t haflo_residual_norm_workspace_bytes(int type, size_t rows, size_t cols) {
+  return norm_sizes(type, rows, cols) ? back_plan(rows, cols).total : (size_t)-1;
+}
+
+int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const void* d_dr, size_t lddr, const void* d_x, size_t ldx, const void* d_f,
+                                 size_t ldf, const float* d_post, const void* d_gate, size_t ldg, const float* d_gate_cols, const float* d_pre,
+                                 const float* d_rstd, size_t rows, size_t cols, double scale, void* d_dx, size_t lddx, void* d_df, size_t lddf,
+                                 void* d_dgate, size_t lddg, float* d_dgate_cols, float* d_dpost, float* d_dpre, void* d_workspace,
+                                 size_t workspace_bytes, void* stream) {
+  if (!norm_sizes(type, rows, cols) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
+  if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
+  // a gradient of what is not there
+  if ((d_dpost && !d_post) || (d_dpre && !d_pre) || (d_dgate_cols && !d_gate_cols) || (d_dgate && !d_gate) || (d_df && !d_f)) return HAFLO_EINVAL;
+  if (rows && (!d_x || ldx < cols || (d_f && ldf < cols) || (d_gate && ldg < cols) || (d_pre && (!d_dh || lddh < cols)) || (d_dr && lddr < cols) || !d_rstd ||
+               (d_dx && lddx < cols) || (d_df && lddf < cols) || (d_dgate && lddg < cols)))
+    return HAFLO_EINVAL;
+  const struct {
+    const void* p;
+    size_t ld;
+  } in[5] = {{d_x, ldx}, {d_f, ldf}, {d_gate, ldg}, {d_pre ? d_dh : nullptr, lddh}, {d_dr, lddr}}, out[3] = {{d_dx, lddx}, {d_df, lddf}, {d_dgate, lddg}};
+  for (int o = 0; o < 3; ++o) {
+    for (const auto& i : in)
+      if (out[o].p && !in_place(i.p, i.ld, out[o].p, out[o].ld, rows)) return HAFLO_EINVAL;
+    if (out[o].p && (out[o].p == out[(o + 1) % 3].p)) return HAFLO_EINVAL;
+  }
+  const Plan plan = back_plan(rows, cols);
+  if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;
+  char* const ws = (char*)d_workspace;
+  const hipStream_t st = (hipStream_t)stream;
+  if (rows) HAFLO_LOCAL_TYPES(type, {
+    const Norm<T> n = {(const T*)d_x, (const T*)d_f, (const T*)d_gate, ldx, ldf, ldg, d_gate_cols, d_post, d_pre, (u32)rows, (u32)cols, (float)scale,
+                       0.0, 1.0 / (double)cols};
+    const Back<T> b = {(const T*)d_dh, (const T*)d_dr, lddh, lddr, d_rstd, (T*)d_dx, (T*)d_df, (T*)d_dgate, lddx, lddf, lddg, (float*)ws, (u32)plan.width};
+    if (!d_f) norm_back<T, kStream>(n, b, plan, ws, st);
+    else if (d_gate) norm_back<T, kFullGate>(n, b, plan, ws, st);
+    else norm_back<T, kGated>(n, b, plan, ws, st);
+  });
+  if (d_dpost || d_dgate_cols || d_dpre)
+    hipLaunchKernelGGL(k_norm_join, dim3((unsigned)(3 * ceil_div(cols, kWave))), dim3(kThreads), 0, st, (const float*)ws, (u32)plan.blocks, (u32)plan.width,
+                       (u32)cols, Joined{{d_dpost, d_dgate_cols, d_dpre}});
+  return launched();
+}
+
+}  // extern "C"

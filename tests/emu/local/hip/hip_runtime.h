@@ -97,6 +97,23 @@ inline C mfma8(V a, V b, C c) {
 }
 }  // namespace hipemu_local
 
+// one 16 x 16 product by 4 in 64 bits: lane l's row of the result is 4 r + l / 16
+typedef double hipemu_f64x4 __attribute__((ext_vector_type(4)));
+static inline hipemu_f64x4 __builtin_amdgcn_mfma_f64_16x16x4f64(double a, double b, hipemu_f64x4 c, int, int, int) {
+  struct Wave {
+    double a[64], b[64];
+  };
+  static Wave waves[2][32];  // as Slots
+  const int lane = (int)(threadIdx.x % 64), at = hipemu_local::parity() ^= 1;
+  Wave& s = waves[at][threadIdx.x / 64];
+  s.a[lane] = a;
+  s.b[lane] = b;
+  hipemu::ballot(true);
+  for (int r = 0; r < 4; ++r)
+    for (int g = 0; g < 4; ++g) c[r] += s.a[16 * g + 4 * r + lane / 16] * s.b[16 * g + lane % 16];
+  return c;
+}
+
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
 #define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) hipemu_local::mfma8((a), (b), (c))
 #define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) hipemu_local::mfma1((a), (b), (c))
