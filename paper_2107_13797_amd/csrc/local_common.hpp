@@ -141,6 +141,33 @@ __device__ __forceinline__ double lane_read(double v, int lane) {
   return __builtin_bit_cast(double, lane_read(__builtin_bit_cast(u64, v), lane));
 }
 
+// What a lane of the same sixteen holds, by a move that the vector unit makes on the way (quad_perm, row_half_mirror, row_mirror)
+template <int CTRL>
+__device__ __forceinline__ u32 lane_swap(u32 v) {
+  return (u32)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL>
+__device__ __forceinline__ float lane_swap(float v) {
+  return __builtin_bit_cast(float, lane_swap<CTRL>(__builtin_bit_cast(u32, v)));
+}
+template <int CTRL>
+__device__ __forceinline__ double lane_swap(double v) {
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(double, (u64)lane_swap<CTRL>((u32)(b >> 32)) << 32 | lane_swap<CTRL>((u32)b));
+}
+// `with` over a wavefront's groups of `lanes` lanes, a power of two: pairs, then pairs of what they hold, so that with a commutative `with` all
+// lanes of a group hold the same bits.
+template <class S, class F>
+__device__ __forceinline__ S lanes_join(S v, u32 lanes, const F& with) {
+  if (lanes >= 2) v = with(v, lane_swap<0xB1>(v));
+  if (lanes >= 4) v = with(v, lane_swap<0x4E>(v));
+  if (lanes >= 8) v = with(v, lane_swap<0x141>(v));
+  if (lanes >= 16) v = with(v, lane_swap<0x140>(v));
+  if (lanes >= 32) v = with(v, lane_read(v, (int)(lane_id() ^ 16)));
+  if (lanes >= 64) v = with(v, lane_read(v, (int)(lane_id() ^ 32)));
+  return v;
+}
+
 // acc += a b on 16 x 16 by 32: lane l holds rows l % 16 of both operands at elements 8 (l / 16) .. + 7, and in
 // acc[r] row 4 (l / 16) + r of the first operand against row l % 16 of the second.
 __device__ __forceinline__ f32x4 mma32(const Vec8<__bf16>& a, const Vec8<__bf16>& b, f32x4 acc) {

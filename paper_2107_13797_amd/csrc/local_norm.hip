@@ -15,9 +15,10 @@ using namespace haflo::local;
 namespace {
 
 constexpr u32 kThreads = 256;
+constexpr u32 kBlockLanes = 512;                      // of a block, of rows that take no more
 constexpr u32 kMostLanes = 1024;                      // of one row
 constexpr size_t kRowCols = (size_t)kMostLanes * 8;   // columns of a row that lanes hold; longer rows are read again
-constexpr size_t kNormBlocks = 2048, kBackBlocks = 512;
+constexpr size_t kNormBlocks = 1024, kBackBlocks = 512;
 constexpr u32 kTileCols = kThreads * 8;               // of the long rows' way back
 
 enum Mode { kStream = 0, kGated = 1, kFullGate = 2 };  // r = x; a block's f with a gate by columns or none; a gate for every element
@@ -62,27 +63,21 @@ __device__ __forceinline__ double squares(const Eight& e) {
   for (int j = 0; j < 8; ++j) s += (double)e.v[j] * (double)e.v[j];
   return s;
 }
-__device__ __forceinline__ float products(const Eight& a, const Eight& b) {
-  float s = 0.0f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s += a.v[j] * b.v[j];
-  return s;
-}
-
-// The sum over a row's group of `lanes` lanes, a power of two, the same bits in each. Groups of more than a wavefront are whole blocks, and
-// take turns at two places in LDS: a wavefront is at most one sum ahead.
+// The sum over a row's group of `lanes` lanes, a power of two, the same bits in each. Groups of more than a wavefront take turns at two
+// places in LDS: a wavefront is at most one sum ahead. All of a block's groups call it together.
 template <class S>
 struct GroupSum {
   S (*parts)[kMostLanes / kWave];
   u32 lanes, turn;
   __device__ __forceinline__ S operator()(S v) {
-    for (u32 d = 1; d < lanes && d < kWave; d <<= 1) v += lane_read(v, (int)(lane_id() ^ d));
+    v = lanes_join(v, lanes, [](S a, S b) { return a + b; });
     if (lanes > kWave) {
       turn ^= 1;
-      if (lane_id() == 0) parts[turn][threadIdx.x / kWave] = v;
+      const u32 wave = threadIdx.x / kWave, waves = lanes / kWave, first = wave & ~(waves - 1);
+      if (lane_id() == 0) parts[turn][wave] = v;
       __syncthreads();
-      v = parts[turn][0];
-      for (u32 w = 1; w < lanes / kWave; ++w) v += parts[turn][w];
+      v = parts[turn][first];
+      for (u32 w = 1; w < waves; ++w) v += parts[turn][first + w];
     }
     return v;
   }
@@ -107,13 +102,21 @@ __global__ __launch_bounds__(MOST) void k_norm(Norm<T> n, u32 lanes, T* r_out, s
   GroupSum<double> sum = {parts, lanes, 0};
   const u32 groups = blockDim.x / lanes, col = threadIdx.x % lanes * 8;
   const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
-  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += (u64)gridDim.x * groups) {
-    const u64 mine = base + threadIdx.x / lanes;
+  const u64 step = (u64)gridDim.x * groups;
+  u64 mine = (u64)blockIdx.x * groups + threadIdx.x / lanes;
+  Vec8<T> xn, fn, gn;
+  const auto ask = [&](u64 row) {
+    row = row < n.rows ? row : n.rows - 1;
+    xn = load_cols(n.x + row * n.ldx, col, n.cols);
+    if (MODE != kStream) fn = load_cols(n.f + row * n.ldf, col, n.cols);
+    if (MODE == kFullGate) gn = load_cols(n.gate + row * n.ldg, col, n.cols);
+  };
+  ask(mine);
+  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += step, mine += step) {
     const bool live = mine < n.rows;
-    const u64 row = live ? mine : n.rows - 1;
-    Vec8<T> xv = load_cols(n.x + row * n.ldx, col, n.cols), fv = {}, gv = {};
-    if (MODE != kStream) fv = load_cols(n.f + row * n.ldf, col, n.cols);
-    if (MODE == kFullGate) gv = load_cols(n.gate + row * n.ldg, col, n.cols);
+    const u64 row = mine;
+    const Vec8<T> xv = xn, fv = fn, gv = gn;
+    if (base + step < n.rows) ask(mine + step);
     Eight f = floats(fv), p, r;
     float q = 1.0f, t = 1.0f;
     if (MODE != kStream && n.post) q = root(sum(squares(f)), n.per_col, n.eps);
@@ -181,111 +184,143 @@ struct Back {
   const float* rstd;
   T *dx, *df, *dgate;
   size_t lddx, lddf, lddg;
-  float* sums;   // of dpost, dgate by columns and dpre: blocks x width each
+  float* sums;   // of the block's gains and of dpre: blocks x width each
   u32 width;     // of a row of them
 };
-// Eight columns of a row on the way back, up to the means.
+// Eight columns of a row on the way back: as they are loaded, and up to the means.
+template <class T, int MODE>
+struct BackIn {
+  Vec8<T> x, f, gate, dh, dr;
+  float q, t;
+  __device__ __forceinline__ void load(const Norm<T>& n, const Back<T>& b, u64 row, u32 col) {
+    row = row < n.rows ? row : n.rows - 1;
+    x = load_cols(n.x + row * n.ldx, col, n.cols);
+    if (MODE != kStream) f = load_cols(n.f + row * n.ldf, col, n.cols);
+    if (MODE == kFullGate) gate = load_cols(n.gate + row * n.ldg, col, n.cols);
+    dh = dr = Vec8<T>{};
+    if (n.pre) dh = load_cols(b.dh + row * b.lddh, col, n.cols);
+    if (b.dr) dr = load_cols(b.dr + row * b.lddr, col, n.cols);
+    q = b.rstd[row];
+    t = b.rstd[n.rows + row];
+  }
+};
 struct BackRow {
-  Eight x, f, gate, dh, dr;  // f: f^ from its root on
+  Eight f, unit, gate, dh, dr;  // f^ (f without a norm), r^
   float q, t;
 };
-template <class T, int MODE>
-__device__ __forceinline__ BackRow back_load(const Norm<T>& n, const Back<T>& b, u64 row, u32 col, const Eight& by_cols) {
+template <int MODE, class T>
+__device__ __forceinline__ BackRow back_row(const BackIn<T, MODE>& in, const Eight& post, const Eight& by_cols, float scale) {
   BackRow v;
-  Vec8<T> xv = load_cols(n.x + row * n.ldx, col, n.cols), fv = {}, gv = {}, hv = {}, rv = {};
-  if (MODE != kStream) fv = load_cols(n.f + row * n.ldf, col, n.cols);
-  if (MODE == kFullGate) gv = load_cols(n.gate + row * n.ldg, col, n.cols);
-  if (n.pre) hv = load_cols(b.dh + row * b.lddh, col, n.cols);
-  if (b.dr) rv = load_cols(b.dr + row * b.lddr, col, n.cols);
-  v.x = floats(xv);
-  v.f = floats(fv);
-  v.gate = MODE == kFullGate ? floats(gv) : by_cols;
-  v.dh = floats(hv);
-  v.dr = floats(rv);
-  v.q = b.rstd[row];
-  v.t = b.rstd[n.rows + row];
+  v.f = MODE == kStream ? Eight{} : floats(in.f);
+  v.gate = MODE == kFullGate ? floats(in.gate) : by_cols;
+  v.q = in.q;
+  v.t = in.t;
+  Eight p;
+  join_stream<MODE>(floats(in.x), v.f, post, v.gate, v.q, scale, p, v.unit);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v.unit.v[j] *= v.t;
+  v.dh = floats(in.dh);
+  v.dr = floats(in.dr);
   return v;
 }
-// from there to D: v.dr; r^ in `unit`
-__device__ __forceinline__ void stream_grad(BackRow& v, const Eight& unit, const Eight& pre, float mean) {
+// the first mean's terms, and from it to D: v.dr
+__device__ __forceinline__ float stream_terms(const BackRow& v, const Eight& pre) {
+  float s = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v.dr.v[j] += v.t * (v.dh.v[j] * pre.v[j] - unit.v[j] * mean);
+  for (int j = 0; j < 8; ++j) s += v.dh.v[j] * pre.v[j] * v.unit.v[j];
+  return s;
 }
+__device__ __forceinline__ void stream_grad(BackRow& v, const Eight& pre, float mean) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v.dr.v[j] += v.t * (v.dh.v[j] * pre.v[j] - v.unit.v[j] * mean);
+}
+// the second mean's terms
+__device__ __forceinline__ float block_terms(const BackRow& v, const Eight& post) {
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s += v.dr.v[j] * v.gate.v[j] * post.v[j] * v.f.v[j];
+  return s;
+}
+// Sums over rows: of D f^, or of D gate f^ with a gate for every element, and of dh r^. A gate by columns and the gain behind the block
+// are the same for all rows, so that both their gradients are the first sum's.
 struct Sums {
-  Eight post, gate, pre;
+  Eight block, pre;
 };
 template <class T, int MODE>
-__device__ __forceinline__ void back_store(const Norm<T>& n, const Back<T>& b, u64 row, u32 col, const BackRow& v, const Eight& p, const Eight& unit,
-                                           const Eight& post, float mean, Sums& s) {
-  Eight dx, df, dg;
+__device__ __forceinline__ void back_store(const Norm<T>& n, const Back<T>& b, u64 row, u32 col, const BackRow& v, const Eight& post, float mean, Sums& s) {
+  Eight e;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    dx.v[j] = MODE == kStream ? v.dr.v[j] : n.scale * v.dr.v[j];
-    s.pre.v[j] += v.dh.v[j] * unit.v[j];
-    if (MODE != kStream) {
-      const float dp = v.dr.v[j] * v.gate.v[j];
-      df.v[j] = n.post ? v.q * (dp * post.v[j] - v.f.v[j] * mean) : dp;
-      s.post.v[j] += dp * v.f.v[j];
-      dg.v[j] = v.dr.v[j] * p.v[j];
-      s.gate.v[j] += dg.v[j];
-    }
+    s.pre.v[j] += v.dh.v[j] * v.unit.v[j];
+    if (MODE != kStream) s.block.v[j] += (MODE == kFullGate ? v.dr.v[j] * v.gate.v[j] : v.dr.v[j]) * v.f.v[j];
+    e.v[j] = MODE == kStream ? v.dr.v[j] : n.scale * v.dr.v[j];
   }
-  if (b.dx) store_cols(b.dx + row * b.lddx, col, n.cols, rounded<T>(dx));
-  if (MODE != kStream && b.df) store_cols(b.df + row * b.lddf, col, n.cols, rounded<T>(df));
-  if (MODE == kFullGate && b.dgate) store_cols(b.dgate + row * b.lddg, col, n.cols, rounded<T>(dg));
+  if (b.dx) store_cols(b.dx + row * b.lddx, col, n.cols, rounded<T>(e));
+  if (MODE != kStream && b.df) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float dp = v.dr.v[j] * v.gate.v[j];
+      e.v[j] = n.post ? v.q * (dp * post.v[j] - v.f.v[j] * mean) : dp;
+    }
+    store_cols(b.df + row * b.lddf, col, n.cols, rounded<T>(e));
+  }
+  if (MODE == kFullGate && b.dgate) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e.v[j] = v.dr.v[j] * (v.f.v[j] * post.v[j]);
+    store_cols(b.dgate + row * b.lddg, col, n.cols, rounded<T>(e));
+  }
 }
 
-// Memory bounds it.
+// The gains lie in LDS, as registers are for the row and for the next one, which is asked for before the means are formed. Memory bounds it.
 template <class T, int MODE, int MOST>
-__global__ __launch_bounds__(MOST) void k_norm_back(Norm<T> n, Back<T> b, u32 lanes) {
+__global__ __launch_bounds__(MOST, 4) void k_norm_back(Norm<T> n, Back<T> b, u32 lanes) {
   __shared__ float parts[2][kMostLanes / kWave];
-  __shared__ float joined[3][kThreads * 8];
+  __shared__ __align__(16) float held[3][MOST * 8];
   GroupSum<float> sum = {parts, lanes, 0};
   const u32 groups = blockDim.x / lanes, group = threadIdx.x / lanes, col = threadIdx.x % lanes * 8;
-  const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
+  if (group == 0) {
+    store_wide(held[0] + col, rounded<float>(gains(n.post, col, n.cols)));
+    store_wide(held[1] + col, rounded<float>(gains(n.pre, col, n.cols)));
+    store_wide(held[2] + col, rounded<float>(gains(n.gate_cols, col, n.cols)));
+  }
+  const auto gain = [&](int which) { return floats(*(const Vec8<float>*)(held[which] + col)); };
+  const u64 step = (u64)gridDim.x * groups;
+  u64 mine = (u64)blockIdx.x * groups + group;
   Sums s = {};
-  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += (u64)gridDim.x * groups) {
-    const u64 mine = base + group;
-    const bool live = mine < n.rows;
-    const u64 row = live ? mine : n.rows - 1;
-    BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
-    Eight p, unit;
-    join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
+  constexpr bool kEarly = sizeof(T) == 2 && MODE != kFullGate;  // (where the next row's registers are there)
+  BackIn<T, MODE> next;
+  if (kEarly) next.load(n, b, mine, col);
+  __syncthreads();
+  for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += step, mine += step) {
+    if (!kEarly) next.load(n, b, mine, col);
+    BackRow v = back_row(next, gain(0), MODE == kFullGate ? Eight{} : gain(2), n.scale);
+    if (kEarly && base + step < n.rows) next.load(n, b, mine + step, col);
     if (n.pre) {
-      Eight a;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) a.v[j] = v.dh.v[j] * pre.v[j];
-      stream_grad(v, unit, pre, sum(products(a, unit)) * (float)n.per_col);
+      const float mean = sum(stream_terms(v, gain(1))) * (float)n.per_col;
+      stream_grad(v, gain(1), mean);
     }
-    float mean = 0.0f;
-    if (MODE != kStream && n.post) {
-      Eight a;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) a.v[j] = v.dr.v[j] * v.gate.v[j] * post.v[j];
-      mean = sum(products(a, v.f)) * (float)n.per_col;
-    }
-    if (live) back_store<T, MODE>(n, b, row, col, v, p, unit, post, mean, s);
+    const float mean = MODE != kStream && n.post ? sum(block_terms(v, gain(0))) * (float)n.per_col : 0.0f;
+    if (mine < n.rows) back_store<T, MODE>(n, b, mine, col, v, gain(0), mean, s);
   }
   // the groups' sums of the same columns, in their order
-  Eight* const mine[3] = {&s.post, &s.gate, &s.pre};
+  Eight* const mine_of[2] = {&s.block, &s.pre};
   if (groups > 1) {
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) joined[i][threadIdx.x * 8 + j] = mine[i]->v[j];
+    for (int i = 0; i < 2; ++i) store_wide(held[i] + threadIdx.x * 8, rounded<float>(*mine_of[i]));
     __syncthreads();
     if (group != 0) return;
     for (u32 g = 1; g < groups; ++g)
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
+      for (int i = 0; i < 2; ++i) {
+        const Eight other = floats(*(const Vec8<float>*)(held[i] + (g * lanes + threadIdx.x) * 8));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) mine[i]->v[j] += joined[i][(g * lanes + threadIdx.x) * 8 + j];
+        for (int j = 0; j < 8; ++j) mine_of[i]->v[j] += other.v[j];
+      }
   }
   if (col < b.width)
 #pragma unroll
-    for (int i = 0; i < 3; ++i) store_wide(b.sums + ((size_t)i * gridDim.x + blockIdx.x) * b.width + col, rounded<float>(*mine[i]));
+    for (int i = 0; i < 2; ++i) store_wide(b.sums + ((size_t)i * gridDim.x + blockIdx.x) * b.width + col, rounded<float>(*mine_of[i]));
 }
 
 // Long rows: both means of a row, by one block.
@@ -295,18 +330,15 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_means(Norm<T> n, Back<T> b,
   GroupSum<float> sum = {parts, kMostLanes, 0};
   for (u64 row = blockIdx.x; row < n.rows; row += gridDim.x) {
     float first = 0.0f, second = 0.0f;
-    // `step` 0: a r^ of eight columns; 1: b f^, with the first mean
+    // `step` 0: the first mean's terms of eight columns; 1: the second's, with the first mean
     const auto terms = [&](u32 col, int step) {
-      const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
-      BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
-      Eight p, unit, a;
-      join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
-      if (step == 1 && n.pre) stream_grad(v, unit, pre, first);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) a.v[j] = step == 0 ? v.dh.v[j] * pre.v[j] : v.dr.v[j] * v.gate.v[j] * post.v[j];
-      return products(a, step == 0 ? unit : v.f);
+      const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols);
+      BackIn<T, MODE> in;
+      in.load(n, b, row, col);
+      BackRow v = back_row(in, post, gains(n.gate_cols, col, n.cols), n.scale);
+      if (step == 0) return stream_terms(v, pre);
+      if (n.pre) stream_grad(v, pre, first);
+      return block_terms(v, post);
     };
     if (n.pre) {
       float s = 0.0f;
@@ -332,36 +364,51 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_long(Norm<T> n, Back<T> 
   const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
   Sums s = {};
   for (u64 row = part; row < n.rows; row += blocks) {
-    BackRow v = back_load<T, MODE>(n, b, row, col, by_cols);
-    Eight p, unit;
-    join_stream<MODE>(v.x, v.f, post, v.gate, v.q, n.scale, p, unit);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) unit.v[j] *= v.t;
-    if (n.pre) stream_grad(v, unit, pre, means[row]);
-    back_store<T, MODE>(n, b, row, col, v, p, unit, post, means[n.rows + row], s);
+    BackIn<T, MODE> in;
+    in.load(n, b, row, col);
+    BackRow v = back_row(in, post, by_cols, n.scale);
+    if (n.pre) stream_grad(v, pre, means[row]);
+    back_store<T, MODE>(n, b, row, col, v, post, means[n.rows + row], s);
   }
-  const Eight* const mine[3] = {&s.post, &s.gate, &s.pre};
+  const Eight* const held[2] = {&s.block, &s.pre};
 #pragma unroll
-  for (int i = 0; i < 3; ++i) store_wide(b.sums + ((size_t)i * blocks + part) * b.width + col, rounded<float>(*mine[i]));
+  for (int i = 0; i < 2; ++i) store_wide(b.sums + ((size_t)i * blocks + part) * b.width + col, rounded<float>(*held[i]));
 }
 
-// The blocks' sums of 64 columns: four wavefronts take a quarter of the blocks each.
+// The blocks' sums of 64 columns: sixteen wavefronts take a part of the blocks each, eight loads on their way at a time.
+constexpr u32 kJoinWaves = 16;
 struct Joined {
-  float* out[3];
+  float *post, *gate, *pre;
+  const float *of_post, *of_gate;  // what the first sum is multiplied by for them, or NULL
 };
-__global__ __launch_bounds__(kThreads) void k_norm_join(const float* sums, u32 blocks, u32 width, u32 cols, Joined to) {
-  __shared__ float parts[kThreads / kWave][kWave];
+__global__ __launch_bounds__(kJoinWaves * kWave) void k_norm_join(const float* sums, u32 blocks, u32 width, u32 cols, Joined to) {
+  __shared__ float parts[kJoinWaves][kWave];
   const u32 tiles = (cols + kWave - 1) / kWave, which = blockIdx.x / tiles, lane = lane_id(), wave = threadIdx.x / kWave;
   const u32 col = blockIdx.x % tiles * kWave + lane;
-  float* const out = which == 0 ? to.out[0] : which == 1 ? to.out[1] : to.out[2];
-  if (!out) return;
+  if (which == 0 ? !to.post && !to.gate : !to.pre) return;
+  const u32 first = (u32)((u64)blocks * wave / kJoinWaves), end = (u32)((u64)blocks * (wave + 1) / kJoinWaves);
+  const float* const from = sums + (size_t)which * blocks * width + (col < cols ? col : cols - 1);
   float s = 0.0f;
-  const u32 first = (u32)((u64)blocks * wave / 4), end = (u32)((u64)blocks * (wave + 1) / 4);
-  if (col < cols)
-    for (u32 i = first; i < end; ++i) s += sums[((size_t)which * blocks + i) * width + col];
+  u32 i = first;
+  for (; i + 8 <= end; i += 8) {
+    float v[8];
+#pragma unroll
+    for (u32 j = 0; j < 8; ++j) v[j] = from[(size_t)(i + j) * width];
+    s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  }
+  for (; i < end; ++i) s += from[(size_t)i * width];
   parts[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < cols) out[col] = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
+  if (wave != 0 || col >= cols) return;
+  s = 0.0f;
+#pragma unroll
+  for (u32 w = 0; w < kJoinWaves; ++w) s += parts[w][lane];
+  if (which == 1) {
+    to.pre[col] = s;
+  } else {
+    if (to.post) to.post[col] = to.of_post ? s * to.of_post[col] : s;
+    if (to.gate) to.gate[col] = to.of_gate ? s * to.of_gate[col] : s;
+  }
 }
 
 u32 lanes_of(size_t cols) {
@@ -369,10 +416,15 @@ u32 lanes_of(size_t cols) {
   while ((size_t)lanes * 8 < cols) lanes *= 2;
   return lanes;
 }
-u32 threads_of(u32 lanes) { return lanes <= (u32)kWave ? kThreads : lanes; }
+// Several rows to a block where there are many: their columns' sums are joined in LDS, and a compute unit holds few blocks.
+u32 threads_of(u32 lanes, size_t rows) {
+  u32 threads = lanes < (u32)kWave ? (u32)kWave : lanes;
+  while (threads < kBlockLanes && ceil_div(rows, threads / lanes) > kBackBlocks) threads *= 2;
+  return threads;
+}
 size_t row_blocks(size_t rows, size_t cols, size_t most) {
   const u32 lanes = lanes_of(cols);
-  const size_t need = ceil_div(rows, threads_of(lanes) / lanes);
+  const size_t need = ceil_div(rows, threads_of(lanes, rows) / lanes);
   return need < most ? need : most;
 }
 struct Plan {
@@ -382,7 +434,7 @@ Plan back_plan(size_t rows, size_t cols) {
   Plan p;
   p.width = ceil_div(cols, 8) * 8;
   p.blocks = cols <= kRowCols ? row_blocks(rows, cols, kBackBlocks) : rows < 64 ? rows : 64;
-  p.means = align256(3 * p.blocks * p.width * 4);
+  p.means = align256(2 * p.blocks * p.width * 4);
   p.total = p.means + (cols <= kRowCols ? 0 : align256(2 * rows * 4));
   return p;
 }
@@ -395,10 +447,10 @@ void norm(const Norm<T>& n, T* r, size_t ldr, T* h, size_t ldh, float* rstd, hip
                        rstd);
     return;
   }
-  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes);
+  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes, n.rows);
   const dim3 grid((unsigned)row_blocks(n.rows, n.cols, kNormBlocks)), block(threads);
-  if (threads > 512) hipLaunchKernelGGL((k_norm<T, MODE, kMostLanes>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
-  else hipLaunchKernelGGL((k_norm<T, MODE, 512>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
+  if (threads > kBlockLanes) hipLaunchKernelGGL((k_norm<T, MODE, kMostLanes>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
+  else hipLaunchKernelGGL((k_norm<T, MODE, kBlockLanes>), grid, block, 0, st, n, lanes, r, ldr, h, ldh, rstd);
 }
 template <class T, int MODE>
 void norm_back(const Norm<T>& n, const Back<T>& b, const Plan& plan, char* ws, hipStream_t st) {
@@ -409,10 +461,10 @@ void norm_back(const Norm<T>& n, const Back<T>& b, const Plan& plan, char* ws, h
                        (const float*)means, (u32)plan.blocks);
     return;
   }
-  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes);
+  const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes, n.rows);
   const dim3 grid((unsigned)plan.blocks), block(threads);
-  if (threads > 512) hipLaunchKernelGGL((k_norm_back<T, MODE, kMostLanes>), grid, block, 0, st, n, b, lanes);
-  else hipLaunchKernelGGL((k_norm_back<T, MODE, 512>), grid, block, 0, st, n, b, lanes);
+  if (threads > kBlockLanes) hipLaunchKernelGGL((k_norm_back<T, MODE, kMostLanes>), grid, block, 0, st, n, b, lanes);
+  else hipLaunchKernelGGL((k_norm_back<T, MODE, kBlockLanes>), grid, block, 0, st, n, b, lanes);
 }
 
 }  // namespace
@@ -484,8 +536,8 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
     else norm_back<T, kGated>(n, b, plan, ws, st);
   });
   if (d_dpost || d_dgate_cols || d_dpre)
-    hipLaunchKernelGGL(k_norm_join, dim3((unsigned)(3 * ceil_div(cols, kWave))), dim3(kThreads), 0, st, (const float*)ws, (u32)plan.blocks, (u32)plan.width,
-                       (u32)cols, Joined{{d_dpost, d_dgate_cols, d_dpre}});
+    hipLaunchKernelGGL(k_norm_join, dim3((unsigned)(2 * ceil_div(cols, kWave))), dim3(kJoinWaves * kWave), 0, st, (const float*)ws, (u32)plan.blocks, (u32)plan.width,
+                       (u32)cols, Joined{d_dpost, d_dgate_cols, d_dpre, d_gate_cols, d_post});
   return launched();
 }
 

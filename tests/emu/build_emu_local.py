@@ -31,7 +31,7 @@ def build(narrow=False):
     out = OUT.replace(".so", "_narrow.so") if narrow else OUT
     flags = ["-DHAFLO_LOCAL_LANES=%d" % NARROW, "-DHIPEMU_LANES=%d" % NARROW] if narrow else []
     srcs = sorted(glob.glob(os.path.join(CSRC, "local_*.hip"))) + [os.path.join(HERE, "hipemu.cpp")]
-    used = srcs + [os.path.join(CSRC, "local_common.hpp"), os.path.join(HERE, "include", "hip", "hip_runtime.h"),
+    used = srcs + glob.glob(os.path.join(CSRC, "local_*.hpp")) + [os.path.join(HERE, "include", "hip", "hip_runtime.h"),
                    os.path.join(HERE, "local", "hip", "hip_runtime.h"), os.path.join(ROOT, "include", "haflo_local.h"),
                    os.path.abspath(__file__)]
     if os.path.exists(out) and os.path.getmtime(out) >= max(os.path.getmtime(p) for p in used):

@@ -97,6 +97,10 @@ uint32_t dpp(uint32_t old, uint32_t src, int ctrl, int row_mask, int bank_mask, 
     if (lane + 1 < kWave) from = lane + 1;
   } else if (ctrl == 0x138) {  // wave_shr:1 - lane i reads lane i-1 of the wavefront
     if (lane >= 1) from = lane - 1;
+  } else if (ctrl == 0x140) {  // row_mirror
+    from = row + 15 - pos;
+  } else if (ctrl == 0x141) {  // row_half_mirror
+    from = row + (pos ^ 7);
   } else if (ctrl >= 0x150 && ctrl <= 0x15f) {  // row_newbcast:n - every lane of a row reads its lane n
     from = row + (ctrl - 0x150);
   } else if (ctrl >= 0 && ctrl <= 0xff) {  // quad_perm
