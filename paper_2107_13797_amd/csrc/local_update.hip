@@ -33,6 +33,11 @@ struct Batch {
   size_t ld, step;
 };
 
+template <bool V>
+struct Flag {
+  static constexpr bool value = V;
+};
+
 // The short side is covered by KT tiles of sixteen. Row `place` of tile i is the short side's 16 i + place where its rows are the
 // matrix's; where they are its columns, it is KT place + i, so that a lane's rows of all tiles lie beside each other in memory.
 template <int KT, bool TALL>
@@ -40,37 +45,56 @@ __device__ __forceinline__ u32 short_of(u32 tile, u32 place) {
   return TALL ? KT * place + tile : 16 * tile + place;
 }
 
-// KT elements from `s` on of a row of `k`, zeros behind it
-template <class T, int KT>
-__device__ __forceinline__ void load_few(const T* row, u32 s, u32 k, T (&out)[KT]) {
-  if (s + KT <= k) {
+// `N` elements from `s` on of a row of `k`, zeros behind it
+template <class T, int N>
+__device__ __forceinline__ void load_few(const T* row, u32 s, u32 k, T (&out)[N]) {
+  if (s + N <= k) {
     __builtin_memcpy(out, row + s, sizeof(out));
   } else {
 #pragma unroll
-    for (int i = 0; i < KT; ++i) out[i] = s + i < k ? row[s + i] : (T)0.0f;
+    for (int i = 0; i < N; ++i) out[i] = s + i < k ? row[s + i] : (T)0.0f;
   }
 }
 
-// What a lane holds of 32 places of the long side: row (lane % 16) of every tile at places at + 8 (lane / 16) .. + 7
+// What a lane holds of 32 places of the long side: row (lane % 16) of every tile at places at + 8 (lane / 16) .. + 7. Where rows are
+// the matrix's columns, each place is one load of KT elements; WHOLE: KT divides k, so that a lane's are all there or none is.
 template <class T, int KT, bool TALL>
-__device__ __forceinline__ void load_chunk(const T* m, size_t ld, u32 k, u32 length, u32 at, Vec8<T> (&v)[KT]) {
-  const u32 place = lane_id() % 16, l = at + lane_id() / 16 * 8;
-  if constexpr (TALL) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      T few[KT] = {};
-      if (l + e < length) load_few<T, KT>(m + (size_t)(l + e) * ld, KT * place, k, few);
-#pragma unroll
-      for (int i = 0; i < KT; ++i) v[i].set(e, few[i]);
-    }
-  } else {
+struct Chunk;
+template <class T, int KT>
+struct Chunk<T, KT, false> {
+  Vec8<T> v[KT];
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const T* m, size_t ld, u32 k, u32 length, u32 at) {
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      const u32 s = 16 * i + place;
-      v[i] = load_cols(m + (size_t)(s < k ? s : k - 1) * ld, l, length);
+      const u32 s = 16 * i + lane_id() % 16;
+      v[i] = load_cols(m + (size_t)(s < k ? s : k - 1) * ld, at + lane_id() / 16 * 8, length);
     }
   }
-}
+  __device__ __forceinline__ double get(int i, int e, u32, u32, u32) const { return (double)(float)v[i].get(e); }
+};
+template <class T, int KT>
+struct Chunk<T, KT, true> {
+  T v[8][KT];
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const T* m, size_t ld, u32 k, u32 length, u32 at) {
+    const u32 s = KT * (lane_id() % 16), l = at + lane_id() / 16 * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const T* const row = m + (size_t)(l + e < length ? l + e : length - 1) * ld;
+      if (WHOLE) {
+        __builtin_memcpy(v[e], row + (s < k ? s : 0), sizeof(v[e]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < KT; ++i) v[e][i] = row[s + i < k ? s + i : k - 1];
+      }
+    }
+  }
+  // (what lies past the matrix is another of its elements, and zero here)
+  __device__ __forceinline__ double get(int i, int e, u32 k, u32 length, u32 at) const {
+    return KT * (lane_id() % 16) + i < k && at + lane_id() / 16 * 8 + e < length ? (double)(float)v[e][i] : 0.0;
+  }
+};
 
 // Rows W and 7 - W of eight rows of tiles, on and under the diagonal: nine products whichever.
 template <int W>
@@ -96,28 +120,37 @@ __global__ __launch_bounds__(kThreads) void k_gram(Batch<const T> g, u32 k, u32 
   f64x4 acc[kPairs];
 #pragma unroll
   for (int n = 0; n < kPairs; ++n) acc[n] = f64x4{0.0, 0.0, 0.0, 0.0};
-  for (u32 c = kSplit ? first : first + wave; c < end; c += kSplit ? 1 : kWaves) {
-    Vec8<T> v[KT];
-    load_chunk<T, KT, TALL>(m, g.ld, k, length, c * kChunk, v);
+  const auto add = [&](auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    constexpr u32 kStride = kSplit ? 1 : kWaves;
+    Chunk<T, KT, TALL> now, next;
+    u32 c = kSplit ? first : first + wave;
+    if (c < end) next.template load<kWhole>(m, g.ld, k, length, c * kChunk);
+    for (; c < end; c += kStride) {
+      now = next;
+      if (c + kStride < end) next.template load<kWhole>(m, g.ld, k, length, (c + kStride) * kChunk);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      double d[KT];
+      for (int e = 0; e < 8; ++e) {
+        double d[KT];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) d[i] = (double)(float)v[i].get(e);
-      if constexpr (kSplit) {
-        if (wave == 0) two_rows<0>(d, acc);
-        else if (wave == 1) two_rows<1>(d, acc);
-        else if (wave == 2) two_rows<2>(d, acc);
-        else two_rows<3>(d, acc);
-      } else {
-        int n = 0;
+        for (int i = 0; i < KT; ++i) d[i] = now.get(i, e, k, length, c * kChunk);
+        if constexpr (kSplit) {
+          if (wave == 0) two_rows<0>(d, acc);
+          else if (wave == 1) two_rows<1>(d, acc);
+          else if (wave == 2) two_rows<2>(d, acc);
+          else two_rows<3>(d, acc);
+        } else {
+          int n = 0;
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
+          for (int i = 0; i < KT; ++i)
 #pragma unroll
-          for (int j = 0; j <= i; ++j, ++n) acc[n] = mma4(d[i], d[j], acc[n]);
+            for (int j = 0; j <= i; ++j, ++n) acc[n] = mma4(d[i], d[j], acc[n]);
+        }
       }
     }
-  }
+  };
+  if (k % KT == 0) add(Flag<true>());
+  else add(Flag<false>());
   double* const to = out + (size_t)block * N * N;
   const auto put = [&](u32 i, u32 j, u32 row, u32 col, double v) {  // both halves of the symmetric matrix, zeros past the short side
     const u32 s = short_of<KT, TALL>(i, row), t = short_of<KT, TALL>(j, col);
@@ -154,79 +187,129 @@ struct Steps {
   double c[HAFLO_UPDATE_MAX_STEPS][3];
   int count;
 };
-// The sum over a block's threads of a power of two.
+// The sum over a block's threads.
 template <u32 THREADS>
 __device__ __forceinline__ double block_sum(double v, double* room) {
-#pragma unroll
-  for (u32 d = 1; d < kWave; d <<= 1) v += lane_read(v, (int)(lane_id() ^ d));
+  v = lanes_join(v, kWave, [](double a, double b) { return a + b; });
   if (THREADS == kWave) return v;
   if (lane_id() == 0) room[threadIdx.x / kWave] = v;
   __syncthreads();
   v = 0.0;
 #pragma unroll
   for (u32 w = 0; w < THREADS / kWave; ++w) v += room[w];
-  __syncthreads();
   return v;
 }
-// G's factor 1 / (|G|_F + eps), from the parts' diagonals
-template <u32 THREADS>
-__device__ __forceinline__ double factor_of(const double* parts, u32 count, u32 n, double eps, double* room) {
-  double t = 0.0;
-  for (u32 i = threadIdx.x; i < count * n; i += THREADS) t += parts[(size_t)(i / n) * n * n + (size_t)(i % n) * (n + 1)];
-  return 1.0 / (sqrt(block_sum<THREADS>(t, room)) + eps);
+// element i of the parts' sum, eight loads on their way at a time
+__device__ __forceinline__ double sum_parts(const double* parts, u32 count, size_t each, u32 i) {
+  double s = 0.0;
+  u32 p = 0;
+  for (; p + 8 <= count; p += 8) {
+    double v[8];
+#pragma unroll
+    for (u32 j = 0; j < 8; ++j) v[j] = parts[(p + j) * each + i];
+    s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  }
+#pragma unroll 4
+  for (; p < count; ++p) s += parts[p * each + i];
+  return s;
+}
+__device__ __forceinline__ double factor_of(double squares, double eps) { return 1.0 / (sqrt(squares) + eps); }
+
+// One tile of x y, N elements each of rows i of x and j of y: lane l takes elements 8 t + 2 (l / 16) and the next of row l % 16 of both.
+template <u32 N>
+__device__ __forceinline__ f64x4 tile_product(const double* x, const double* y, u32 i, u32 j, u32 ld) {
+  const u32 at = lane_id() % 16 * ld + lane_id() / 16 * 2;
+  const double *const a = x + 16 * i * ld + at, *const b = y + 16 * j * ld + at;
+  double u[N / 8][2], v[N / 8][2];
+#pragma unroll
+  for (u32 t = 0; t < N / 8; ++t) {
+    __builtin_memcpy(u[t], __builtin_assume_aligned(a + 8 * t, 16), 16);
+    __builtin_memcpy(v[t], __builtin_assume_aligned(b + 8 * t, 16), 16);
+  }
+  f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (u32 t = 0; t < N / 8; ++t)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) acc = mma4(u[t][e], v[t][e], acc);
+  return acc;
+}
+// tile -> its row and column among those on and under the diagonal
+__device__ __forceinline__ u32 tile_row(u32 tile) {
+  u32 i = 0;
+  while ((i + 1) * (i + 2) / 2 <= tile) ++i;
+  return i;
 }
 
-// The polynomial of up to 64 rows, by one block in LDS: to = scale P / (|G|_F + eps). Products are of symmetric matrices that commute, so
-// the tiles on and under the diagonal are formed and mirrored, and the second operand's rows are read for its columns.
+// The polynomial of up to 64 rows, by one block in LDS: to = scale P / (|G|_F + eps). Products are of symmetric matrices that commute: the
+// tiles on and under the diagonal are formed and mirrored, and the second operand's rows are read for its columns. Results
+// stay in registers until all have read the operands, and then take an operand's place. The matrix instructions in turn bound it.
 template <int KT>
-__global__ __launch_bounds__(KT == 1 ? kWave : kThreads) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, double* to) {
-  constexpr u32 N = 16 * KT, S = N + 4, THREADS = KT == 1 ? kWave : kThreads, WAVES = THREADS / kWave;
-  __shared__ double lds[4][N * S], room[WAVES];
+constexpr u32 step_threads() {
+  return KT == 1 ? kWave : KT == 2 ? 4 * kWave : 8 * kWave;
+}
+template <int KT>
+__global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, double* to) {
+  constexpr u32 N = 16 * KT, S = N + 2, THREADS = step_threads<KT>(), WAVES = THREADS / kWave, TILES = KT * (KT + 1) / 2;
+  __shared__ __align__(16) double lds[3][N * S];
+  __shared__ double room[WAVES];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   parts += (size_t)blockIdx.x * count * N * N;
   to += (size_t)blockIdx.x * N * N;
-  const double by = factor_of<THREADS>(parts, count, N, eps, room);
-  double *K = lds[0], *Q = lds[1], *P = lds[2], *M = lds[3];
+  double *const K = lds[0], *const Q = lds[1], *const P = lds[2];
+  double squares = 0.0;
   for (u32 i = threadIdx.x; i < N * N; i += THREADS) {
-    double s = 0.0;
-    for (u32 p = 0; p < count; ++p) s += parts[(size_t)p * N * N + i];
-    K[i / N * S + i % N] = s * by * by;
+    const double s = sum_parts(parts, count, N * N, i);
+    K[i / N * S + i % N] = s;
+    if (i / N == i % N) squares += s;
   }
+  const double by = factor_of(block_sum<THREADS>(squares, room), eps);
+  for (u32 i = threadIdx.x; i < N * N; i += THREADS) K[i / N * S + i % N] *= by * by;  // (each thread its own)
   __syncthreads();
-  // out = one I + self x + both x y
-  const auto product = [&](double* out, const double* x, const double* y, double one, double self, double both) {
-    int n = 0;
+  // out = one I + self x + both x y, of x0 and, with two jobs, of x1
+  const auto products = [&](auto jobs, double* out0, double* out1, const double* x0, const double* x1, const double* y, double one, double self, double both) {
+    constexpr u32 TOTAL = decltype(jobs)::value ? 2 * TILES : TILES, PER = (TOTAL + WAVES - 1) / WAVES;
+    f64x4 acc[PER];
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+    for (u32 n = 0; n < PER; ++n) {
+      const u32 id = wave + n * WAVES, tile = id % TILES, i = tile_row(tile), j = tile - i * (i + 1) / 2;
+      if (id >= TOTAL) continue;
+      const double* const from = id < TILES ? x0 : x1;
+      acc[n] = tile_product<N>(from, y, i, j, S);
 #pragma unroll
-      for (int j = 0; j <= i; ++j, ++n) {
-        if ((u32)n % WAVES != wave) continue;
-        f64x4 acc = {0.0, 0.0, 0.0, 0.0};
-        const u32 a = (16 * i + lane % 16) * S + lane / 16, b = (16 * j + lane % 16) * S + lane / 16;
-#pragma unroll 8
-        for (u32 k = 0; k < N; k += 4) acc = mma4(x[a + k], y[b + k], acc);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const u32 row = 16 * i + 4 * r + lane / 16, col = 16 * j + lane % 16;
-          const double v = both * acc[r] + (self != 0.0 ? self * x[row * S + col] : 0.0) + (row == col ? one : 0.0);
-          out[row * S + col] = v;
-          if (i != j) out[col * S + row] = v;
-        }
+      for (int r = 0; r < 4; ++r) {
+        const u32 row = 16 * i + 4 * r + lane / 16, col = 16 * j + lane % 16;
+        acc[n][r] = both * acc[n][r] + (self != 0.0 ? self * from[row * S + col] : 0.0) + (row == col ? one : 0.0);
       }
+    }
+    __syncthreads();
+#pragma unroll
+    for (u32 n = 0; n < PER; ++n) {
+      const u32 id = wave + n * WAVES, tile = id % TILES, i = tile_row(tile), j = tile - i * (i + 1) / 2;
+      if (id >= TOTAL) continue;
+      double* const o = id < TILES ? out0 : out1;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const u32 row = 16 * i + 4 * r + lane / 16, col = 16 * j + lane % 16;
+        o[row * S + col] = acc[n][r];
+        if (i != j) o[col * S + row] = acc[n][r];
+      }
+    }
     __syncthreads();
   };
+  const Flag<false> one_job;
+  const Flag<true> two_jobs;
   for (int s = 0; s < steps.count; ++s) {
-    product(s == 0 ? P : Q, K, K, steps.c[s][0], steps.c[s][1], steps.c[s][2]);
-    const double* const q = s == 0 ? P : Q;
-    if (s + 1 < steps.count) {
-      product(M, K, q, 0.0, 0.0, 1.0);
-      product(K, M, q, 0.0, 0.0, 1.0);
-    }
-    if (s > 0) {
-      product(M, P, Q, 0.0, 0.0, 1.0);
-      double* const was = P;
-      P = M;
-      M = was;
+    const bool last = s + 1 == steps.count;
+    double* const first = s == 0 ? P : Q;
+    products(one_job, first, first, K, K, K, steps.c[s][0], steps.c[s][1], steps.c[s][2]);
+    if (s == 0 && !last) {
+      products(one_job, Q, Q, K, K, P, 0.0, 0.0, 1.0);  // (Q for what is between)
+      products(one_job, K, K, Q, Q, P, 0.0, 0.0, 1.0);
+    } else if (s > 0 && last) {
+      products(one_job, P, P, P, P, Q, 0.0, 0.0, 1.0);
+    } else if (s > 0) {
+      products(two_jobs, K, P, K, P, Q, 0.0, 0.0, 1.0);
+      products(one_job, K, K, K, K, Q, 0.0, 0.0, 1.0);
     }
   }
   for (u32 i = threadIdx.x; i < N * N; i += THREADS) to[i] = P[i / N * S + i % N] * (by * scale);
@@ -236,13 +319,18 @@ __global__ __launch_bounds__(KT == 1 ? kWave : kThreads) void k_steps(const doub
 constexpr u32 kLarge = 128;
 __global__ __launch_bounds__(1024) void k_gram_join(const double* parts, u32 count, double eps, double* K, double* factor) {
   __shared__ double room[16];
+  constexpr u32 kEach = kLarge * kLarge / 1024;
   parts += (size_t)blockIdx.x * count * kLarge * kLarge;
-  const double by = factor_of<1024>(parts, count, kLarge, eps, room);
-  for (u32 i = threadIdx.x; i < kLarge * kLarge; i += 1024) {
-    double s = 0.0;
-    for (u32 p = 0; p < count; ++p) s += parts[(size_t)p * kLarge * kLarge + i];
-    K[(size_t)blockIdx.x * kLarge * kLarge + i] = s * by * by;
+  double s[kEach], squares = 0.0;
+#pragma unroll
+  for (u32 n = 0; n < kEach; ++n) {
+    const u32 i = n * 1024 + threadIdx.x;
+    s[n] = sum_parts(parts, count, kLarge * kLarge, i);
+    if (i / kLarge == i % kLarge) squares += s[n];
   }
+  const double by = factor_of(block_sum<1024>(squares, room), eps);
+#pragma unroll
+  for (u32 n = 0; n < kEach; ++n) K[(size_t)blockIdx.x * kLarge * kLarge + n * 1024 + threadIdx.x] = s[n] * by * by;
   if (threadIdx.x == 0) factor[blockIdx.x] = by;
 }
 // out = one I + self x + both x y, times the party's factor where there is one
@@ -260,15 +348,10 @@ __global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 fi
   const u32 block = first_block + blockIdx.x, lane = lane_id(), tile = block % kLargeTiles, of = block / kLargeTiles;
   const Product q = p.job[of % jobs];
   const u32 party = of / jobs;
-  u32 i = 0;
-  while ((i + 1) * (i + 2) / 2 <= tile) ++i;
-  const u32 j = tile - i * (i + 1) / 2;
+  const u32 i = tile_row(tile), j = tile - i * (i + 1) / 2;
   const size_t at = (size_t)party * kLarge * kLarge;
-  const double *x = q.x + at, *y = q.y + at;
-  f64x4 acc = {0.0, 0.0, 0.0, 0.0};
-  const u32 a = (16 * i + lane % 16) * kLarge + lane / 16, b = (16 * j + lane % 16) * kLarge + lane / 16;
-#pragma unroll 8
-  for (u32 k = 0; k < kLarge; k += 4) acc = mma4(x[a + k], y[b + k], acc);
+  const double* const x = q.x + at;
+  const f64x4 acc = tile_product<kLarge>(x, q.y + at, i, j, kLarge);
   const double by = q.factor ? q.factor[party] : 1.0;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -279,64 +362,72 @@ __global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 fi
   }
 }
 
-// out = keep base + P G. P lies in LDS; a wavefront takes `kPlaces` places of the long side by the whole short side.
-template <class T, int KT, bool TALL>
+// out = keep base + P G. P lies in LDS; a wavefront takes `kPlaces` places of the long side by the whole short side at a time, and asks
+// for the next ones before it multiplies.
+template <int KT, bool TALL>
 struct Apply {
-  static constexpr int kVec = KT == 8 ? 2 : 4;                 // along the long side, of rows
-  static constexpr u32 kPlaces = TALL ? 32 : 16 * kVec;
-  static constexpr u32 N = 16 * KT, S = N + 4;
+  static constexpr int kVec = KT == 8 ? 2 : 4;  // along the long side, of rows
+  static constexpr u32 kPlaces = TALL ? 16 : 16 * kVec;
+  static constexpr u32 N = 16 * KT, S = N + 2;
 };
 template <class T, int KT, bool TALL>
 __global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<const T> base, Batch<T> out, const double* poly, u32 k, u32 length, double keep,
                                                     u32 blocks, u32 first_block) {
-  using A = Apply<T, KT, TALL>;
+  using A = Apply<KT, TALL>;
   constexpr u32 N = A::N, S = A::S;
   __shared__ __align__(16) double P[N * S];
   const u32 block = first_block + blockIdx.x, party = block / blocks;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), place = lane % 16, group = lane / 16;
   poly += (size_t)party * N * N;
-  for (u32 i = threadIdx.x; i < N * N; i += kThreads) P[i / N * S + i % N] = poly[i];
-  __syncthreads();
-  const u32 at = (block % blocks * kWaves + wave) * A::kPlaces;
-  if (at >= length) return;
   const T* const m = g.p + party * g.step;
   const T* const b = base.p ? base.p + party * base.step : nullptr;
   T* const o = out.p + party * out.step;
+  const u32 pieces = (length + A::kPlaces - 1) / A::kPlaces, stride = blocks * kWaves;
+  u32 piece = block % blocks * kWaves + wave;
   if constexpr (TALL) {
     // rows of the result are places of the long side; tile j holds the short side's KT (lane % 16) + j
-    f64x4 acc[2][KT];
+    T next[KT][4], x[KT][4];
+    const auto ask = [&](u32 at) {  // sixteen of the reduction, four to a lane, KT times
+      const u32 l = at + place;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (u32 t = 0; t < KT; ++t) load_few<T, 4>(m + (size_t)(l < length ? l : length - 1) * g.ld, 16 * t + 4 * group, k, next[t]);
+    };
+    if (piece < pieces) ask(piece * A::kPlaces);
+    for (u32 i = threadIdx.x; i < N * N; i += kThreads) P[i / N * S + i % N] = poly[i];
+    __syncthreads();
+    for (; piece < pieces; piece += stride) {
+      const u32 at = piece * A::kPlaces, s = KT * place;
+      __builtin_memcpy(x, next, sizeof(x));
+      T was[4][KT] = {};
+      if (b) {
 #pragma unroll
-      for (int j = 0; j < KT; ++j) acc[i][j] = f64x4{0.0, 0.0, 0.0, 0.0};
-#pragma unroll 2
-    for (u32 t = 0; t < KT; ++t) {  // sixteen of the reduction, four to a lane
-      T x[2][4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const u32 l = at + 16 * i + place;
-        load_few<T, 4>(m + (size_t)(l < length ? l : length - 1) * g.ld, 16 * t + 4 * group, k, x[i]);
+        for (int r = 0; r < 4; ++r) {
+          const u32 l = at + 4 * r + group;
+          load_few<T, KT>(b + (size_t)(l < length ? l : length - 1) * base.ld, s, k, was[r]);
+        }
       }
+      if (piece + stride < pieces) ask((piece + stride) * A::kPlaces);
+      f64x4 acc[KT];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        double d[KT];
-        __builtin_memcpy(d, &P[(16 * t + 4 * group + e) * S + KT * place], sizeof(d));
+      for (int j = 0; j < KT; ++j) acc[j] = f64x4{0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (u32 t = 0; t < KT; ++t)
 #pragma unroll
-          for (int j = 0; j < KT; ++j) acc[i][j] = mma4((double)(float)x[i][e], d[j], acc[i][j]);
-      }
-    }
+        for (int e = 0; e < 4; ++e) {
+          double d[KT];
+          __builtin_memcpy(d, &P[(16 * t + 4 * group + e) * S + s], sizeof(d));
+          const double v = (double)(float)x[t][e];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+          for (int j = 0; j < KT; ++j) acc[j] = mma4(v, d[j], acc[j]);
+          if (KT == 8) __builtin_amdgcn_sched_barrier(0);  // (P's elements not all at once: there are registers for two steps')
+        }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const u32 l = at + 16 * i + 4 * r + group, s = KT * place;
+        const u32 l = at + 4 * r + group;
         if (l >= length) continue;
-        T was[KT] = {}, now[KT];
-        if (b) load_few<T, KT>(b + (size_t)l * base.ld, s, k, was);
+        T now[KT];
 #pragma unroll
-        for (int j = 0; j < KT; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[j] + acc[i][j][r] : acc[i][j][r]);
+        for (int j = 0; j < KT; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[r][j] + acc[j][r] : acc[j][r]);
         T* const to = o + (size_t)l * out.ld + s;
         if (s + KT <= k) {
           __builtin_memcpy(to, now, sizeof(now));
@@ -346,60 +437,69 @@ __global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<cons
             if (s + j < k) to[j] = now[j];
         }
       }
+    }
   } else {
     // tile j of the result's columns holds places at + kVec (lane % 16) + j
     constexpr int V = A::kVec;
-    f64x4 acc[KT][V];
+    for (u32 i = threadIdx.x; i < N * N; i += kThreads) P[i / N * S + i % N] = poly[i];
+    __syncthreads();
+    for (; piece < pieces; piece += stride) {
+      f64x4 acc[KT][V];
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+      for (int i = 0; i < KT; ++i)
 #pragma unroll
-      for (int j = 0; j < V; ++j) acc[i][j] = f64x4{0.0, 0.0, 0.0, 0.0};
-    const u32 l = at + V * place;
-    const auto ask = [&](u32 s, T (&x)[V]) {
-      if (s < k) {
-        load_few<T, V>(m + (size_t)s * g.ld, l < length ? l : length, length, x);
-      } else {
+        for (int j = 0; j < V; ++j) acc[i][j] = f64x4{0.0, 0.0, 0.0, 0.0};
+      const u32 l = piece * A::kPlaces + V * place;
+      const auto ask = [&](u32 s, T (&x)[V]) { load_few<T, V>(m + (size_t)(s < k ? s : k - 1) * g.ld, l < length ? l : length, length, x); };
+      constexpr u32 kAhead = N / 4 < 8 ? N / 4 : 8;  // loads on their way together, of one row of each lane group
+      T x[kAhead][V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = (T)0.0f;
-      }
-    };
-#pragma unroll 4
-    for (u32 t = 0; t < N; t += 4) {
-      T x[V];
-      ask(t + group, x);
+      for (u32 n = 0; n < kAhead; ++n) ask(4 * n + group, x[n]);
+      for (u32 t0 = 0; t0 < N; t0 += 4 * kAhead) {
+        T now[kAhead][V];
+        __builtin_memcpy(now, x, sizeof(x));
+        if (t0 + 4 * kAhead < N) {
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        const double d = P[(16 * i + place) * S + t + group];
+          for (u32 n = 0; n < kAhead; ++n) ask(t0 + 4 * (kAhead + n) + group, x[n]);
+        }
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[i][j] = mma4(d, (double)(float)x[j], acc[i][j]);
-      }
-    }
+        for (u32 n = 0; n < kAhead; ++n) {
+          const u32 s = t0 + 4 * n + group;
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+          for (int i = 0; i < KT; ++i) {
+            const double d = P[(16 * i + place) * S + s];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const u32 s = 16 * i + 4 * r + group;
-        if (s >= k) continue;
-        T was[V] = {}, now[V];
-        if (b) load_few<T, V>(b + (size_t)s * base.ld, l < length ? l : length, length, was);
-#pragma unroll
-        for (int j = 0; j < V; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[j] + acc[i][j][r] : acc[i][j][r]);
-        T* const to = o + (size_t)s * out.ld + l;
-        if (l + V <= length) {
-          __builtin_memcpy(to, now, sizeof(now));
-        } else {
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (l + j < length) to[j] = now[j];
+            for (int j = 0; j < V; ++j) acc[i][j] = mma4(d, s < k ? (double)(float)now[n][j] : 0.0, acc[i][j]);
+          }
         }
       }
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const u32 s = 16 * i + 4 * r + group;
+          if (s >= k) continue;
+          T was[V] = {}, now[V];
+          if (b) load_few<T, V>(b + (size_t)s * base.ld, l < length ? l : length, length, was);
+#pragma unroll
+          for (int j = 0; j < V; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[j] + acc[i][j][r] : acc[i][j][r]);
+          T* const to = o + (size_t)s * out.ld + l;
+          if (l + V <= length) {
+            __builtin_memcpy(to, now, sizeof(now));
+          } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+              if (l + j < length) to[j] = now[j];
+          }
+        }
+    }
   }
 }
 
 struct Shape {
   size_t parties, k, length;
   bool tall;
-  u32 tiles() const { return k <= 16 ? 1 : k <= 32 ? 2 : k <= 64 ? 4 : 8; }
+  u32 tiles() const { return k <= 16 ? 1 : k <= 32 ? 2 : k <= 48 ? 3 : k <= 64 ? 4 : 8; }
   size_t side() const { return 16 * tiles(); }
 };
 struct Plan {
@@ -455,6 +555,12 @@ void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double sc
   }
 }
 
+// Blocks of one matrix in k_apply: each brings P to LDS once, and there are enough for all compute units.
+u32 apply_blocks(const Shape& s, u32 places) {
+  const size_t need = ceil_div(s.length, places), want = ceil_div((size_t)1024, s.parties);
+  return (u32)(need < want ? need : want);
+}
+
 template <class T, bool TALL>
 void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, const Shape& s, const Plan& plan, const Steps& steps, double keep,
             double scale, double eps, char* ws, hipStream_t st) {
@@ -465,11 +571,11 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
       hipLaunchKernelGGL((k_gram<T, KT, TALL>), grid, block, 0, st, g, (u32)s.k, (u32)s.length, (u32)plan.parts, (double*)(ws + plan.gram), first); \
     });                                                                                                                                         \
     if constexpr (KT <= 4)                                                                                                                      \
-      hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(KT == 1 ? kWave : kThreads), 0, st, (const double*)(ws + plan.gram),    \
+      hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)(ws + plan.gram),             \
                          (u32)plan.parts, steps, scale, eps, poly);                                                                             \
     else                                                                                                                                        \
       large_steps(s, plan, steps, scale, eps, ws, st);                                                                                          \
-    const u32 blocks = (u32)ceil_div(s.length, kWaves * Apply<T, KT, TALL>::kPlaces);                                                           \
+    const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);                                                                      \
     in_turns(s.parties * blocks, kThreads, [&](u32 first, dim3 grid, dim3 block) {                                                              \
       hipLaunchKernelGGL((k_apply<T, KT, TALL>), grid, block, 0, st, g, base, out, (const double*)poly, (u32)s.k, (u32)s.length, keep, blocks,  \
                          first);                                                                                                                \
@@ -478,6 +584,7 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
   switch (s.tiles()) {
     case 1: HAFLO_LOCAL_RUN(1); break;
     case 2: HAFLO_LOCAL_RUN(2); break;
+    case 3: HAFLO_LOCAL_RUN(3); break;
     case 4: HAFLO_LOCAL_RUN(4); break;
     default: HAFLO_LOCAL_RUN(8); break;
   }
