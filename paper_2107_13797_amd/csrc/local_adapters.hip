@@ -10,17 +10,13 @@
 // caller has them in, and k_grad sums over the rows of one adapter. It also lays out anew what reduces along columns (W, A and B
 // of the backward pass) and, for k_project, operands whose rows do not begin at 16-byte boundaries.
 #include "local_common.hpp"
+#include "local_tiles.hpp"
 
 using namespace haflo::local;
 
 namespace {
 
 constexpr int kThreads = 256;
-
-template <class T>
-constexpr int step_elems() {  // of the reduction in one step of k_project: 128 bytes of a row
-  return 128 / (int)sizeof(T);
-}
 
 __device__ __forceinline__ int party_of(const int* index, u32 t, u32 parties) {
   const int a = index[t];
@@ -214,165 +210,12 @@ __device__ __forceinline__ f32x4 low_mma(const f32x4& f, const f32x4& z, f32x4 a
   return acc;
 }
 
-// Where the rows of a tile are loaded from, sixteen bytes a lane straight into LDS, lane l's to `to` + 16 l. Matrices below
-// 4 GiB are read as buffers, whose offsets are 32-bit words and whose loads the compiler counts one by one; FAR ones are not.
-template <class T, bool FAR>
-struct Source;
-template <class T>
-struct Source<T, false> {
-  using At = u32;
-  __amdgpu_buffer_rsrc_t buffer;
-  __device__ __forceinline__ Source(const T* p, u32 bytes) : buffer(__builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000)) {}
-  static __device__ __forceinline__ At at(u32 row, size_t ld, u32 k) { return (row * (u32)ld + k) * (u32)sizeof(T); }
-  __device__ __forceinline__ void load(At at, u32 k, void* to) const {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void*)to, 16, (int)at, (int)(k * (u32)sizeof(T)), 0, 0);
-  }
-};
-template <class T>
-struct Source<T, true> {
-  using At = size_t;
-  const T* p;
-  __device__ __forceinline__ Source(const T* p_, u32) : p(p_) {}
-  static __device__ __forceinline__ At at(u32 row, size_t ld, u32 k) { return row * ld + k; }
-  __device__ __forceinline__ void load(At at, u32 k, void* to) const {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + at + k), (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-  }
-};
-// Until this wavefront's loads but the latest LATER have arrived and its reads of LDS are done, and all other
-// wavefronts of the block are there too.
-template <int LATER>
-__device__ __forceinline__ void wait_for_tiles() {
-  asm volatile("" ::: "memory");
-  static_assert(LATER < 16, "");
-  __builtin_amdgcn_s_waitcnt(0x70 + LATER);  // vmcnt(LATER) lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-// A tile's row in LDS is 128 bytes, eight pieces of 16; piece c of row r lies at place c ^ (r / 2) % 8, which spreads the
-// sixteen rows that lanes read at once over all banks.
-__device__ __forceinline__ u32 place_of(u32 row, u32 piece) { return piece ^ (row >> 1 & 7); }
-template <class T>
-__device__ __forceinline__ Vec8<T> load_frag(const T* tile, u32 row, u32 k) {  // eight elements from the k-th of a row
-  constexpr u32 kPer = 16 / sizeof(T);
-  Vec8<T> v;
-#pragma unroll
-  for (u32 i = 0; i < 8 / kPer; ++i)
-    v.w[i] = *(const u32x4*)(tile + row * step_elems<T>() + place_of(row, k / kPer + i) * kPer);
-  return v;
-}
-
 // Four sums with the draws that two words hold.
 __device__ __forceinline__ void drop_four(f32x4& v, const Drop& d, u32 lo, u32 hi) {
   v[0] = (lo & 0xFFFFu) >= d.threshold ? v[0] * d.scale : 0.0f;
   v[1] = (lo >> 16) >= d.threshold ? v[1] * d.scale : 0.0f;
   v[2] = (hi & 0xFFFFu) >= d.threshold ? v[2] * d.scale : 0.0f;
   v[3] = (hi >> 16) >= d.threshold ? v[3] * d.scale : 0.0f;
-}
-
-// The operands that a wavefront multiplies next: its outputs by XN sixteens of its rows.
-template <class T, int OT, int XN>
-struct Frags {
-  Vec8<T> w[OT], x[XN];
-};
-template <class T, int OT, int XN>
-__device__ __forceinline__ void load_w(Frags<T, OT, XN>& f, const T* tile, u32 out0, u32 s) {
-#pragma unroll
-  for (int i = 0; i < OT; ++i) f.w[i] = load_frag(tile, out0 + i * 16 + lane_id() % 16, s * 32 + lane_id() / 16 * 8);
-}
-template <class T, int OT, int XN>
-__device__ __forceinline__ void load_x(Frags<T, OT, XN>& f, const T* tile, u32 row0, u32 s, u32 part) {
-#pragma unroll
-  for (int j = 0; j < XN; ++j) f.x[j] = load_frag(tile, row0 + (part * XN + j) * 16 + lane_id() % 16, s * 32 + lane_id() / 16 * 8);
-}
-
-// Half (0: the first, 1: the second) of this wavefront's loads of both tiles at `k`, in LDS rows of whole steps.
-template <class T, int TM, int TN, int WAVES, class From>
-__device__ __forceinline__ void ask_tiles(int half, const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
-                                          const typename From::At (&at_w)[TN / 8 / WAVES], u32 k, u32 wave, T* lx, T* lw) {
-  constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
-#pragma unroll
-  for (int i = half * LX / 2; i < (half + 1) * LX / 2; ++i) x.load(at_x[i], k, lx + (i * WAVES + wave) * 8 * step_elems<T>());
-#pragma unroll
-  for (int i = half * LW / 2; i < (half + 1) * LW / 2; ++i) w.load(at_w[i], k, lw + (i * WAVES + wave) * 8 * step_elems<T>());
-}
-
-// One step of the reduction, with the first operands in `f`. Operands are read from LDS under the products before theirs, a
-// read between every few of them. Before the last products the next step's tiles are waited for; the tiles after those are then asked for
-// in place of this step's, one half under the last products and the other under the next step's first, so that the loads
-// neither hold the products up at one place nor are waited for before three quarters of a step are over.
-template <class T, int TM, int TN, int WAVES, class From, int XN, int RT, int OT>
-__device__ __forceinline__ void project_step(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
-                                             const typename From::At (&at_w)[TN / 8 / WAVES], u32 k_next, u32 k_after, u32 wave, u32 row0,
-                                             u32 out0, T* cx, T* cw, T* nx, T* nw,
-                                             Frags<T, OT, XN>& f, f32x4 (&acc)[OT][RT]) {
-  constexpr int KE = step_elems<T>(), kSub = KE / 32, kParts = RT / XN, kAll = kSub * kParts;
-  constexpr int kAsks = (TM + TN) / 8 / WAVES / 2, kReads = sizeof(T) / 2, kProducts = XN * OT * (sizeof(T) == 2 ? 1 : 8);
-#pragma unroll
-  for (int q = 0; q < kAll; ++q) {
-    const int s = q / kParts, part = q % kParts;
-    const bool last = q + 1 == kAll, new_w = last || (q + 1) / kParts != s;
-    Frags<T, OT, XN> next;
-    if (q == 0 && kAll > 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k_next, wave, nx, nw);
-    if (last) {
-      wait_for_tiles<0>();
-      ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k_after, wave, cx, cw);
-      if (kAll == 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k_after, wave, cx, cw);
-    }
-    load_x(next, last ? nx : cx, row0, last ? 0 : (q + 1) / kParts, last ? 0 : (q + 1) % kParts);
-    if (new_w) {
-      load_w(next, last ? nw : cw, out0, last ? 0 : s + 1);
-    } else {
-#pragma unroll
-      for (int i = 0; i < OT; ++i) next.w[i] = f.w[i];
-    }
-#pragma unroll
-    for (int j = 0; j < XN; ++j)
-#pragma unroll
-      for (int i = 0; i < OT; ++i) acc[i][part * XN + j] = mma32(f.w[i], f.x[j], acc[i][part * XN + j]);
-    // a load, where there are any, and one or more reads of LDS with products between them
-    constexpr int kSlots = kAsks < 4 ? kAsks : 4;
-#pragma unroll
-    for (int n = 0; n < kSlots; ++n) {
-      if (last || q == 0) __builtin_amdgcn_sched_group_barrier(0x010, kAsks / kSlots, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kProducts / kSlots / 4, 0);
-      if (new_w) __builtin_amdgcn_sched_group_barrier(0x100, (XN + OT) * kReads / kSlots, 0);
-      else __builtin_amdgcn_sched_group_barrier(0x100, XN * kReads / kSlots, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kProducts / kSlots / 2, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    f = next;
-  }
-}
-
-// The whole reduction of a tile. That the four tiles in LDS are told apart here, and only here, is what lets the compiler see which reads
-// need not wait for the loads on their way.
-template <class T, int TM, int TN, int WAVES, class From, int RT, int OT>
-__device__ __forceinline__ void reduce(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
-                                       const typename From::At (&at_w)[TN / 8 / WAVES], u32 steps, u32 wave, u32 row0, u32 out0,
-                                       T* __restrict__ lx0, T* __restrict__ lw0, T* __restrict__ lx1, T* __restrict__ lw1, f32x4 (&acc)[OT][RT]) {
-  constexpr int KE = step_elems<T>(), XN = RT < 4 ? RT : 4;
-  const u32 inner = steps * KE;
-  const auto after = [&](u32 at) { return at + KE < inner ? at + KE : 0; };
-  u32 k = after(0);
-  ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, 0, wave, lx0, lw0);
-  ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, 0, wave, lx0, lw0);
-  ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k, wave, lx1, lw1);
-  if (KE / 32 * (RT / XN) == 1) ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k, wave, lx1, lw1);
-  Frags<T, OT, XN> frags;
-  wait_for_tiles<(TM + TN) / 8 / WAVES / 2>();
-  load_x(frags, lx0, row0, 0, 0);
-  load_w(frags, lw0, out0, 0);
-  // the loads go round past the last step, rather than that the loop has other forms for its end
-  for (u32 i = 0;; i += 2) {
-    const u32 k2 = after(k), k3 = after(k2);
-    project_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, k2, wave, row0, out0, lx0, lw0, lx1, lw1, frags, acc);
-    if (i + 1 >= steps) break;
-    project_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k2, k3, wave, row0, out0, lx1, lw1, lx0, lw0, frags, acc);
-    if (i + 2 >= steps) break;
-    k = k3;
-  }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): none of them arrives after the block's end
 }
 
 // y[t, o] = drop'(sum_r z[t, r] F[a][o, r]) + sum_k x[t, k] W[o, k], inner a multiple of a step. A block takes TM rows (of

@@ -5,15 +5,15 @@
 // Sums are whole numbers of 32 bits and exact. Rows of eight bits are kept with zeros up to a multiple of 128 bytes, so that no
 // product has an end to look after.
 #include "local_common.hpp"
+#include "local_tiles.hpp"
 
 using namespace haflo::local;
 
 namespace {
 
-constexpr u32 kThreads = 256, kWaves = kThreads / kWave;
+constexpr u32 kThreads = 256;
 constexpr u32 kMostLanes = 1024;
 constexpr size_t kRow = HAFLO_INT8_ROW, kMostInner = HAFLO_INT8_MAX_COLS;
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr size_t kMostResults = (size_t)1 << 42;  // whose tiles 32 bits count
 
@@ -53,36 +53,42 @@ __device__ __forceinline__ u64 eight_bits(const Vec8<T>& v, const Scale& s) {
   return q;
 }
 
-// Rows to eight bits: a group of `lanes` lanes a row, eight columns to a lane, and of a longer row the others again. Memory bounds it.
-template <class T>
-__global__ __launch_bounds__(kMostLanes) void k_quantize(const T* x, size_t ldx, u32 rows, u32 cols, u32 width, u32 lanes, int8_t* q, float* scale,
-                                                         u32 first_block) {
-  __shared__ u32 most[kMostLanes / kWave];
-  const u32 groups = blockDim.x / lanes, at = threadIdx.x % lanes * 8;
-  const u64 mine = (u64)(first_block + blockIdx.x) * groups + threadIdx.x / lanes;
-  const u64 row = mine < rows ? mine : rows - 1;
-  const T* const from = x + row * ldx;
+// A row to eight bits by a group of `lanes` lanes, eight columns to a lane, and of a longer row the others again: `put` takes eight bytes at
+// each multiple of eight below `width`. All of a block's groups call it together. Returns the row's scale.
+template <class T, class Put>
+__device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width, u32 lanes, u32* room, const Put& put) {
+  const u32 at = threadIdx.x % lanes * 8;
   const Vec8<T> own = load_cols(from, at, cols);
   u32 m = most_of(own);
   for (u32 col = at + lanes * 8; col < cols; col += lanes * 8) {
     const u32 b = most_of(load_cols(from, col, cols));
     m = b > m ? b : m;
   }
-  for (u32 d = 1; d < lanes && d < kWave; d <<= 1) {
-    const u32 o = lane_read(m, (int)(lane_id() ^ d));
-    m = o > m ? o : m;
-  }
+  m = lanes_join(m, lanes, [](u32 a, u32 b) { return a > b ? a : b; });
   if (lanes > kWave) {
-    if (lane_id() == 0) most[threadIdx.x / kWave] = m;
+    const u32 wave = threadIdx.x / kWave, waves = lanes / kWave, first = wave & ~(waves - 1);
+    if (lane_id() == 0) room[wave] = m;
     __syncthreads();
-    for (u32 w = 0; w < lanes / kWave; ++w) m = most[w] > m ? most[w] : m;
+    for (u32 w = 0; w < waves; ++w) m = room[first + w] > m ? room[first + w] : m;
   }
-  if (mine >= rows) return;
   const Scale s = scale_of(m);
+  if (at < width) put(at, eight_bits(own, s));
+  for (u32 col = at + lanes * 8; col < width; col += lanes * 8) put(col, eight_bits(load_cols(from, col, cols), s));
+  return s.scale;
+}
+// Memory bounds it.
+template <class T>
+__global__ __launch_bounds__(kMostLanes) void k_quantize(const T* x, size_t ldx, u32 rows, u32 cols, u32 width, u32 lanes, int8_t* q, float* scale,
+                                                         u32 first_block) {
+  __shared__ u32 room[kMostLanes / kWave];
+  const u64 mine = (u64)(first_block + blockIdx.x) * (blockDim.x / lanes) + threadIdx.x / lanes;
+  const bool live = mine < rows;
+  const u64 row = live ? mine : rows - 1;
   u64* const to = (u64*)(q + row * width);
-  if (at < width) to[at / 8] = eight_bits(own, s);
-  for (u32 col = at + lanes * 8; col < width; col += lanes * 8) to[col / 8] = eight_bits(load_cols(from, col, cols), s);
-  if (at == 0) scale[row] = s.scale;
+  const float s = quantize_row(x + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
+    if (live) to[col / 8] = v;
+  });
+  if (live && threadIdx.x % lanes == 0) scale[row] = s;
 }
 
 template <class T>
@@ -94,59 +100,191 @@ struct Out {
   size_t ldy;
   u32 rows, outer;
 };
-// four outputs from `o` on of row t
+// four outputs from `o` on of row t, which there is
 template <class T>
-__device__ __forceinline__ void store_four(const Out<T>& to, u32 t, u32 o, const i32x4& acc) {
-  if (t >= to.rows) return;
-  const float by = to.x_scale[t];
+__device__ __forceinline__ void store_four(const Out<T>& to, u32 t, u32 o, const i32x4& acc, float x_scale) {
+  float v[4];
+  T* const y = to.y + t * to.ldy + o;
+  const T* const res = to.residual ? to.residual + t * to.ldr + o : nullptr;
+  if (o + 4 <= to.outer) {
+    float ws[4], bias[4] = {};
+    T was[4] = {}, now[4];
+    __builtin_memcpy(ws, to.w_scale + o, sizeof(ws));
+    if (to.bias) __builtin_memcpy(bias, to.bias + o, sizeof(bias));
+    if (res) __builtin_memcpy(was, res, sizeof(was));
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (o + r >= to.outer) return;
-    float v = (float)acc[r] * (by * to.w_scale[o + r]);
-    if (to.bias) v += to.bias[o + r];
-    if (to.residual) v += (float)to.residual[t * to.ldr + o + r];
-    to.y[t * to.ldy + o + r] = (T)v;
+    for (int r = 0; r < 4; ++r) now[r] = (T)((float)acc[r] * (x_scale * ws[r]) + bias[r] + (float)was[r]);
+    __builtin_memcpy(y, now, sizeof(now));
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (o + r < to.outer) y[r] = (T)((float)acc[r] * (x_scale * to.w_scale[o + r]) + (to.bias ? to.bias[o + r] : 0.0f) + (res ? (float)res[r] : 0.0f));
   }
 }
 
-// y of 16 outputs by 16 R rows, a wavefront each, its operands from memory as they are needed.
-template <class T, int R>
-__global__ __launch_bounds__(kThreads) void k_int8(const int8_t* x, const int8_t* w, u32 width, Out<T> to, u32 first_block) {
-  const u32 wave = threadIdx.x / kWave, lane = lane_id(), tiles = (to.outer + 63) / 64, block = first_block + blockIdx.x;
-  const u32 o0 = (block % tiles * kWaves + wave) * 16, t0 = block / tiles * 16 * R;
-  const auto row = [&](u32 i, u32 n) { return i < n ? i : n - 1; };
-  const int8_t* const wr = w + (size_t)row(o0 + lane % 16, to.outer) * width + lane / 16 * 16;
+// A block takes TM rows by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
+// is filled while the other is read.
+template <class T, int TM, int TN, int WM, int WN, bool FAR>
+__global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const int8_t* w, u32 width, Out<T> to, u32 x_bytes, u32 w_bytes, u32 first_block) {
+  constexpr int KE = step_elems<int8_t>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
+  constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
+  __shared__ __align__(16) int8_t lds[2 * (TM + TN) * KE];
+  int8_t* const lx0 = lds;
+  int8_t* const lw0 = lx0 + TM * KE;
+  int8_t* const lx1 = lw0 + TN * KE;
+  int8_t* const lw1 = lx1 + TM * KE;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  // Blocks are dealt to the eight dies in turn: each gets neighbouring tiles, four tiles of rows by all outputs at a time,
+  // whose operands its cache holds.
+  const u32 tiles_m = (to.rows + TM - 1) / TM, tiles_n = (to.outer + TN - 1) / TN, tiles = tiles_m * tiles_n;
+  const u32 block = first_block + blockIdx.x, die = block % 8, per = tiles / 8, over = tiles % 8;
+  const u32 tile = die * per + (die < over ? die : over) + block / 8;
+  const u32 band = tile / (4 * tiles_n), in_band = tile % (4 * tiles_n), high = tiles_m - band * 4 < 4 ? tiles_m - band * 4 : 4;
+  const u32 t0 = (band * 4 + in_band % high) * TM, o0 = in_band / high * TN;
+  const u32 row0 = wave / WN * (TM / WM), out0 = wave % WN * (TN / WN);  // this wavefront's corner
+
+  using From = Source<int8_t, FAR>;
+  const From from_x(x, x_bytes), from_w(w, w_bytes);
+  typename From::At at_x[LX], at_w[LW];  // this lane's pieces; rows behind the last are the last one again
+#pragma unroll
+  for (int i = 0; i < LX; ++i) {
+    const u32 r = (i * WAVES + wave) * 8 + lane / 8, t = t0 + r < to.rows ? t0 + r : to.rows - 1;
+    at_x[i] = From::at(t, width, place_of(r, lane % 8) * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < LW; ++i) {
+    const u32 r = (i * WAVES + wave) * 8 + lane / 8, o = o0 + r < to.outer ? o0 + r : to.outer - 1;
+    at_w[i] = From::at(o, width, place_of(r, lane % 8) * 16);
+  }
+  i32x4 acc[OT][RT];
+#pragma unroll
+  for (int j = 0; j < RT; ++j)
+#pragma unroll
+    for (int i = 0; i < OT; ++i) acc[i][j] = i32x4{0, 0, 0, 0};
+  reduce<int8_t, TM, TN, WAVES>(from_x, at_x, from_w, at_w, width / KE, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
+#pragma unroll
+  for (int j = 0; j < RT; ++j) {
+    const u32 t = t0 + row0 + j * 16 + lane % 16;
+    if (t >= to.rows) continue;
+    const float by = to.x_scale[t];
+#pragma unroll
+    for (int i = 0; i < OT; ++i) store_four(to, t, o0 + out0 + i * 16 + lane / 16 * 4, acc[i][j], by);
+  }
+}
+
+// Few rows: a block takes 16 outputs by 16 R rows, its wavefronts a part of the reduction each, so that W is on its way from all
+// of them at once; their sums are joined in LDS. With OWN the block brings the rows, at most four, to eight bits itself.
+constexpr u32 kFewWaves = 8, kFewThreads = kFewWaves * kWave, kOwnBytes = 32768;
+template <class T, int R, bool OWN>
+__global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ldx, u32 cols, const int8_t* xq, const int8_t* w, u32 width, Out<T> to,
+                                                          u32 first_block) {
+  constexpr u32 kAhead = R == 1 ? 4 : R == 2 ? 4 : 2;  // pieces of 128 bytes of each row that are on their way together
+  __shared__ __align__(16) int8_t own[OWN ? kOwnBytes : 16];
+  __shared__ float own_scale[4];
+  __shared__ u32 room[kFewWaves];
+  __shared__ int sums[kFewWaves][R][256];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  const u32 tiles = (to.outer + 15) / 16, block = first_block + blockIdx.x, o0 = block % tiles * 16, t0 = block / tiles * 16 * R;
+  const auto last = [](u32 i, u32 n) { return i < n ? i : n - 1; };
+  const u32 pieces = width / 128, first = pieces * wave / kFewWaves, end = pieces * (wave + 1) / kFewWaves;
+  const int8_t* const wr = w + (size_t)last(o0 + lane % 16, to.outer) * width + lane / 16 * 16;
+  i32x4 wv[kAhead][2];
+  const auto ask = [&](u32 p) {
+#pragma unroll
+    for (u32 u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (u32 h = 0; h < 2; ++h) wv[u][h] = *(const i32x4*)(wr + (size_t)last(p + u, end) * 128 + h * 64);
+  };
+  if (first < end) ask(first);
+  if (OWN) {
+    const u32 groups = to.rows == 1 ? 1 : to.rows == 2 ? 2 : 4, lanes = kFewThreads / groups, group = threadIdx.x / lanes, row = last(group, to.rows);
+    const float s = quantize_row(xf + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
+      if (group < to.rows) *(u64*)(own + group * width + col) = v;
+    });
+    if (threadIdx.x % lanes == 0) own_scale[group] = s;
+    __syncthreads();
+  }
   const int8_t* xr[R];
   i32x4 acc[R];
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    xr[j] = x + (size_t)row(t0 + 16 * j + lane % 16, to.rows) * width + lane / 16 * 16;
+    xr[j] = (OWN ? own : xq) + (size_t)last(t0 + 16 * j + lane % 16, to.rows) * width + lane / 16 * 16;
     acc[j] = i32x4{0, 0, 0, 0};
   }
-  for (u32 k = 0; k < width; k += 64) {
-    const i32x4 a = *(const i32x4*)(wr + k);
+  for (u32 p = first; p < end; p += kAhead) {
+    i32x4 wn[kAhead][2];
 #pragma unroll
-    for (int j = 0; j < R; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, *(const i32x4*)(xr[j] + k), acc[j], 0, 0, 0);
+    for (u32 u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (u32 h = 0; h < 2; ++h) wn[u][h] = wv[u][h];
+    if (p + kAhead < end) ask(p + kAhead);
+#pragma unroll
+    for (u32 u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (u32 h = 0; h < 2; ++h) {
+        if (p + u >= end) wn[u][h] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          const i32x4 xv = *(const i32x4*)(xr[j] + (size_t)last(p + u, end) * 128 + h * 64);
+          acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wn[u][h], xv, acc[j], 0, 0, 0);
+        }
+      }
   }
+  // row t of the tile at 16 t, its outputs beside each other
 #pragma unroll
-  for (int j = 0; j < R; ++j) store_four(to, t0 + 16 * j + lane % 16, o0 + lane / 16 * 4, acc[j]);
+  for (int j = 0; j < R; ++j) *(i32x4*)&sums[wave][j][lane % 16 * 16 + lane / 16 * 4] = acc[j];
+  __syncthreads();
+  for (u32 i = threadIdx.x; i < 256 * R; i += kFewThreads) {
+    const u32 t = t0 + i / 16, o = o0 + i % 16;
+    if (t >= to.rows || o >= to.outer) continue;
+    int s = 0;
+#pragma unroll
+    for (u32 v = 0; v < kFewWaves; ++v) s += sums[v][i / 256][i % 256];
+    float y = (float)s * ((OWN ? own_scale[t] : to.x_scale[t]) * to.w_scale[o]);
+    if (to.bias) y += to.bias[o];
+    if (to.residual) y += (float)to.residual[t * to.ldr + o];
+    to.y[t * to.ldy + o] = (T)y;
+  }
 }
 
+constexpr size_t kFewRows = 64, kOwnRows = 4;
+bool own_rows(size_t rows, size_t cols) { return rows <= kOwnRows && rows * row_bytes(cols) <= kOwnBytes; }
+template <class T>
+void few(const T* x, size_t ldx, size_t cols, const int8_t* xq, const int8_t* w, const Out<T>& to, hipStream_t st) {
+#define HAFLO_LOCAL_RUN(R, OWN)                                                                                                            \
+  in_turns(ceil_div(to.rows, 16 * R) * ceil_div(to.outer, 16), kFewThreads, [&](u32 first, dim3 grid, dim3 block) {                        \
+    hipLaunchKernelGGL((k_int8_few<T, R, OWN>), grid, block, 0, st, x, ldx, (u32)cols, xq, w, (u32)row_bytes(cols), to, first);            \
+  })
+  if (!xq) HAFLO_LOCAL_RUN(1, true);
+  else if (to.rows <= 16) HAFLO_LOCAL_RUN(1, false);
+  else if (to.rows <= 32) HAFLO_LOCAL_RUN(2, false);
+  else HAFLO_LOCAL_RUN(4, false);
+#undef HAFLO_LOCAL_RUN
+}
 template <class T>
 void quantize(const void* x, size_t ldx, size_t rows, size_t cols, int8_t* q, float* scale, hipStream_t st) {
   const size_t width = row_bytes(cols);
   u32 lanes = 16;
   while (lanes < kMostLanes && (size_t)lanes * 8 < width) lanes *= 2;
-  const u32 threads = lanes <= (u32)kWave ? kThreads : lanes;
+  const u32 threads = lanes < kThreads ? kThreads : lanes;
   in_turns(ceil_div(rows, threads / lanes), threads, [&](u32 first, dim3 grid, dim3 block) {
     hipLaunchKernelGGL((k_quantize<T>), grid, block, 0, st, (const T*)x, ldx, (u32)rows, (u32)cols, (u32)width, lanes, q, scale, first);
   });
 }
 template <class T>
 void product(const int8_t* x, const int8_t* w, size_t cols, const Out<T>& to, hipStream_t st) {
-  in_turns(ceil_div(to.rows, 64) * ceil_div(to.outer, 64), kThreads, [&](u32 first, dim3 grid, dim3 block) {
-    hipLaunchKernelGGL((k_int8<T, 4>), grid, block, 0, st, x, w, (u32)row_bytes(cols), to, first);
-  });
+  if (to.rows <= kFewRows) return few<T>(nullptr, 0, cols, x, w, to, st);
+  const size_t width = row_bytes(cols), x_bytes = to.rows * width, w_bytes = to.outer * width;
+  const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
+#define HAFLO_LOCAL_RUN(TM, TN, WM, WN, FAR)                                                                                        \
+  in_turns(ceil_div(to.rows, TM) * ceil_div(to.outer, TN), WM * WN * kWave, [&](u32 first, dim3 grid, dim3 block) {                 \
+    hipLaunchKernelGGL((k_int8<T, TM, TN, WM, WN, FAR>), grid, block, 0, st, x, w, (u32)width, to, (u32)x_bytes, (u32)w_bytes, first); \
+  })
+  if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, true);
+  else if (ceil_div(to.rows, 256) * ceil_div(to.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, false);
+  else if (ceil_div(to.rows, 128) * ceil_div(to.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, false);
+  else HAFLO_LOCAL_RUN(64, 64, 2, 2, false);
+#undef HAFLO_LOCAL_RUN
 }
 
 bool int8_sizes(int type, size_t rows, size_t inner, size_t outer) {
@@ -157,7 +295,8 @@ struct Plan {
   size_t scale, total;
 };
 Plan int8_plan(size_t rows, size_t inner) {
-  Plan p;
+  Plan p = {0, 0};
+  if (own_rows(rows, inner)) return p;
   p.scale = align256(rows * row_bytes(inner));
   p.total = p.scale + align256(rows * 4);
   return p;
@@ -204,6 +343,11 @@ int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq
   int8_t* const xq = (int8_t*)d_workspace;
   float* const x_scale = (float*)((char*)d_workspace + plan.scale);
   HAFLO_LOCAL_TYPES(type, {
+    if (plan.total == 0) {
+      few<T>((const T*)d_x, ldx, inner, nullptr, d_wq, {nullptr, d_w_scale, d_bias, (const T*)d_residual, ldr, (T*)d_y, ldy, (u32)rows, (u32)outer},
+             (hipStream_t)stream);
+      return launched();
+    }
     quantize<T>(d_x, ldx, rows, inner, xq, x_scale, (hipStream_t)stream);
     const Out<T> to = {x_scale, d_w_scale, d_bias, (const T*)d_residual, ldr, (T*)d_y, ldy, (u32)rows, (u32)outer};
     product<T>(xq, d_wq, inner, to, (hipStream_t)stream);
