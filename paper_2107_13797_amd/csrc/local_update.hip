@@ -33,9 +33,23 @@ struct Batch {
   size_t ld, step;
 };
 
-template <bool V>
-struct Flag {
-  static constexpr bool value = V;
+// Blocks are dealt to the eight dies in turn, and a matrix's blocks go to one of them, whose cache then holds what they all read: its
+// K, factors and P come from memory once in each launch (k_products of 64 matrices of 128 rows 14 us where each die reads them all).
+// `each` blocks a matrix; a block past the last matrix has none.
+constexpr u32 kDies = 8;
+struct Place {
+  u32 party, part;
+};
+__device__ __forceinline__ Place place_of_block(u32 block, u32 each, u32 parties) {
+  if (parties < kDies) return {block / each, block % each};
+  const u32 at = block / kDies;
+  return {at / each * kDies + block % kDies, at % each};
+}
+inline size_t blocks_of(size_t each, size_t parties) { return (parties < kDies ? parties : ceil_div(parties, kDies) * kDies) * each; }
+
+template <int V>
+struct Number {
+  static constexpr int value = V;
 };
 
 // The short side is covered by KT tiles of sixteen. Row `place` of tile i is the short side's 16 i + place where its rows are the
@@ -45,55 +59,64 @@ __device__ __forceinline__ u32 short_of(u32 tile, u32 place) {
   return TALL ? KT * place + tile : 16 * tile + place;
 }
 
-// `N` elements from `s` on of a row of `k`, zeros behind it
+// `N` elements from `s` on of a row of `k`; past its end any of the row's
 template <class T, int N>
 __device__ __forceinline__ void load_few(const T* row, u32 s, u32 k, T (&out)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = row[s + i < k ? s + i : k - 1];
+}
+// the same where N divides k and no element is taken by itself
+template <class T, int N>
+__device__ __forceinline__ void load_whole(const T* row, u32 s, u32 k, T (&out)[N]) {
+  __builtin_memcpy(out, row + (s < k ? s : 0), sizeof(out));
+}
+template <class T, int N>
+__device__ __forceinline__ void store_few(T* row, u32 s, u32 k, const T (&in)[N]) {
   if (s + N <= k) {
-    __builtin_memcpy(out, row + s, sizeof(out));
+    __builtin_memcpy(row + s, in, sizeof(in));
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) out[i] = s + i < k ? row[s + i] : (T)0.0f;
+    for (int i = 0; i < N; ++i)
+      if (s + i < k) row[s + i] = in[i];
   }
 }
 
-// What a lane holds of 32 places of the long side: row (lane % 16) of every tile at places at + 8 (lane / 16) .. + 7. Where rows are
-// the matrix's columns, each place is one load of KT elements; WHOLE: KT divides k, so that a lane's are all there or none is.
+// What a lane holds of 32 places of the long side: row (lane % 16) of every tile at places at + 8 (lane / 16) .. + 7, zeros past the long
+// side. Rows past the short side are other ones of the matrix: what they give is left aside. Loads stand in no branch that lanes
+// take apart, as they would be waited for at its end. WHOLE: KT divides k.
 template <class T, int KT, bool TALL>
-struct Chunk;
-template <class T, int KT>
-struct Chunk<T, KT, false> {
-  Vec8<T> v[KT];
+struct Chunk {
+  Vec8<T> v[KT];      // of rows
+  T t[TALL ? 8 : 1][KT];  // of columns: each place is one load of KT elements
   template <bool WHOLE>
   __device__ __forceinline__ void load(const T* m, size_t ld, u32 k, u32 length, u32 at) {
+    const u32 place = lane_id() % 16, l = at + lane_id() / 16 * 8;
+    if constexpr (TALL) {
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      const u32 s = 16 * i + lane_id() % 16;
-      v[i] = load_cols(m + (size_t)(s < k ? s : k - 1) * ld, at + lane_id() / 16 * 8, length);
-    }
-  }
-  __device__ __forceinline__ double get(int i, int e, u32, u32, u32) const { return (double)(float)v[i].get(e); }
-};
-template <class T, int KT>
-struct Chunk<T, KT, true> {
-  T v[8][KT];
-  template <bool WHOLE>
-  __device__ __forceinline__ void load(const T* m, size_t ld, u32 k, u32 length, u32 at) {
-    const u32 s = KT * (lane_id() % 16), l = at + lane_id() / 16 * 8;
+      for (int e = 0; e < 8; ++e) {
+        const T* const row = m + (size_t)(l + e < length ? l + e : length - 1) * ld;
+        if (WHOLE) load_whole<T, KT>(row, KT * place, k, t[e]);
+        else load_few<T, KT>(row, KT * place, k, t[e]);
+      }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const T* const row = m + (size_t)(l + e < length ? l + e : length - 1) * ld;
-      if (WHOLE) {
-        __builtin_memcpy(v[e], row + (s < k ? s : 0), sizeof(v[e]));
-      } else {
-#pragma unroll
-        for (int i = 0; i < KT; ++i) v[e][i] = row[s + i < k ? s + i : k - 1];
+      for (int i = 0; i < KT; ++i) {
+        const u32 s = 16 * i + place;
+        const T* const row = m + (size_t)(s < k ? s : k - 1) * ld;
+        if (at + kChunk <= length) v[i] = load_wide(row + l);
+        else v[i] = load_cols(row, l, length);
       }
     }
   }
-  // (what lies past the matrix is another of its elements, and zero here)
-  __device__ __forceinline__ double get(int i, int e, u32 k, u32 length, u32 at) const {
-    return KT * (lane_id() % 16) + i < k && at + lane_id() / 16 * 8 + e < length ? (double)(float)v[e][i] : 0.0;
+  __device__ __forceinline__ void end(u32 length, u32 at) {  // (rows' ends are zeros already)
+    if (!TALL || at + kChunk <= length) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
+        if (at + lane_id() / 16 * 8 + e >= length) t[TALL ? e : 0][i] = (T)0.0f;
   }
+  __device__ __forceinline__ double get(int i, int e) const { return TALL ? (double)(float)t[TALL ? e : 0][i] : (double)(float)v[i].get(e); }
 };
 
 // Rows W and 7 - W of eight rows of tiles, on and under the diagonal: nine products whichever.
@@ -105,40 +128,32 @@ __device__ __forceinline__ void two_rows(const double (&d)[8], f64x4 (&acc)[9]) 
   for (int j = 0; j <= 7 - W; ++j) acc[W + 1 + j] = mma4(d[7 - W], d[j], acc[W + 1 + j]);
 }
 
-// One part of K_0, unscaled: a block takes `parts`-th pieces of the long side. Up to four tiles each wavefront forms all products of tiles,
-// of its own chunks; of eight a wavefront forms two rows of tiles, of all chunks.
+// The products of tiles of chunks first, first + stride .. below end. Up to four tiles a wavefront forms all products, of eight two
+// rows' (`wave` 0 .. 3).
+template <int KT>
+constexpr int pairs_of() {
+  return KT == 8 ? 9 : KT * (KT + 1) / 2;
+}
 template <class T, int KT, bool TALL>
-__global__ __launch_bounds__(kThreads) void k_gram(Batch<const T> g, u32 k, u32 length, u32 parts, double* out, u32 first_block) {
-  constexpr u32 N = 16 * KT;
-  constexpr bool kSplit = KT == 8;
-  constexpr int kPairs = kSplit ? 9 : KT * (KT + 1) / 2;
-  __shared__ double sum[kSplit ? 1 : kWaves][256];
-  const u32 block = first_block + blockIdx.x, party = block / parts, part = block % parts;
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  const T* const m = g.p + party * g.step;
-  const u32 chunks = (length + kChunk - 1) / kChunk, first = (u32)((u64)chunks * part / parts), end = (u32)((u64)chunks * (part + 1) / parts);
-  f64x4 acc[kPairs];
+__device__ __forceinline__ void gram(const T* m, size_t ld, u32 k, u32 length, u32 first, u32 end, u32 stride, u32 wave, f64x4 (&acc)[pairs_of<KT>()]) {
 #pragma unroll
-  for (int n = 0; n < kPairs; ++n) acc[n] = f64x4{0.0, 0.0, 0.0, 0.0};
-  const auto add = [&](auto whole) {
+  for (int n = 0; n < pairs_of<KT>(); ++n) acc[n] = f64x4{0.0, 0.0, 0.0, 0.0};
+  const auto add = [&](auto whole, auto rows) {
     constexpr bool kWhole = decltype(whole)::value;
-    constexpr u32 kStride = kSplit ? 1 : kWaves;
     Chunk<T, KT, TALL> now, next;
-    u32 c = kSplit ? first : first + wave;
-    if (c < end) next.template load<kWhole>(m, g.ld, k, length, c * kChunk);
-    for (; c < end; c += kStride) {
+    u32 c = first;
+    if (c < end) next.template load<kWhole>(m, ld, k, length, c * kChunk);
+    for (; c < end; c += stride) {
       now = next;
-      if (c + kStride < end) next.template load<kWhole>(m, g.ld, k, length, (c + kStride) * kChunk);
+      if (c + stride < end) next.template load<kWhole>(m, ld, k, length, (c + stride) * kChunk);
+      now.end(length, c * kChunk);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         double d[KT];
 #pragma unroll
-        for (int i = 0; i < KT; ++i) d[i] = now.get(i, e, k, length, c * kChunk);
-        if constexpr (kSplit) {
-          if (wave == 0) two_rows<0>(d, acc);
-          else if (wave == 1) two_rows<1>(d, acc);
-          else if (wave == 2) two_rows<2>(d, acc);
-          else two_rows<3>(d, acc);
+        for (int i = 0; i < KT; ++i) d[i] = now.get(i, e);
+        if constexpr (KT == 8) {
+          two_rows<decltype(rows)::value>(d, acc);
         } else {
           int n = 0;
 #pragma unroll
@@ -149,37 +164,79 @@ __global__ __launch_bounds__(kThreads) void k_gram(Batch<const T> g, u32 k, u32 
       }
     }
   };
-  if (k % KT == 0) add(Flag<true>());
-  else add(Flag<false>());
-  double* const to = out + (size_t)block * N * N;
-  const auto put = [&](u32 i, u32 j, u32 row, u32 col, double v) {  // both halves of the symmetric matrix, zeros past the short side
-    const u32 s = short_of<KT, TALL>(i, row), t = short_of<KT, TALL>(j, col);
-    const double w = s < k && t < k ? v : 0.0;
-    to[s * N + t] = w;
-    if (i != j) to[t * N + s] = w;
+  const auto by_rows = [&](auto whole) {
+    if (KT < 8 || wave == 0) add(whole, Number<0>());
+    else if (wave == 1) add(whole, Number<KT < 8 ? 0 : 1>());
+    else if (wave == 2) add(whole, Number<KT < 8 ? 0 : 2>());
+    else add(whole, Number<KT < 8 ? 0 : 3>());
   };
+  if (!TALL || k % KT == 0) by_rows(Number<1>());
+  else by_rows(Number<0>());
+}
+// the row of a tile among those on and under the diagonal, counted row by row
+__device__ __forceinline__ u32 tile_row(u32 tile) {
+  u32 i = 0;
+  while ((i + 1) * (i + 2) / 2 <= tile) ++i;
+  return i;
+}
+// A block's sums of up to four rows of tiles, five tiles at a time: put(row, column, sum) for both halves, zeros past the short side.
+template <int KT>
+constexpr int tiles_at_once() {
+  return pairs_of<KT>() < 5 ? pairs_of<KT>() : KT == 3 ? 3 : 5;
+}
+template <int KT, bool TALL, u32 WAVES, class Put>
+__device__ __forceinline__ void gram_sums(const f64x4 (&acc)[pairs_of<KT>()], u32 wave, u32 k, double (*sum)[tiles_at_once<KT>()][256], const Put& put) {
+  constexpr int kOnce = tiles_at_once<KT>();
+  const u32 lane = lane_id();
+#pragma unroll
+  for (int n0 = 0; n0 < pairs_of<KT>(); n0 += kOnce) {
+    if (n0) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kOnce; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[wave][n][(4 * r + lane / 16) * 16 + lane % 16] = acc[n0 + n][r];
+    __syncthreads();
+    for (u32 at = threadIdx.x; at < kOnce * 256; at += WAVES * kWave) {
+      const u32 n = at / 256, of = at % 256, i = tile_row(n0 + n), j = n0 + n - i * (i + 1) / 2;
+      double v = 0.0;
+#pragma unroll
+      for (u32 w = 0; w < WAVES; ++w) v += sum[w][n][of];
+      const u32 s = short_of<KT, TALL>(i, of / 16), t = short_of<KT, TALL>(j, of % 16);
+      v = s < k && t < k ? v : 0.0;
+      put(s, t, v);
+      if (i != j) put(t, s, v);
+    }
+  }
+}
+
+// One part of K_0, unscaled: a block takes `parts`-th pieces of the long side.
+template <class T, int KT, bool TALL>
+__global__ __launch_bounds__(kThreads) void k_gram(Batch<const T> g, u32 k, u32 length, u32 parts, u32 parties, double* out, u32 first_block) {
+  constexpr u32 N = 16 * KT;
+  constexpr bool kSplit = KT == 8;
+  __shared__ double sum[kSplit ? 1 : kWaves][tiles_at_once<KT>()][256];
+  const auto [party, part] = place_of_block(first_block + blockIdx.x, parts, parties);
+  if (party >= parties) return;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
+  const u32 chunks = (length + kChunk - 1) / kChunk, first = (u32)((u64)chunks * part / parts), end = (u32)((u64)chunks * (part + 1) / parts);
+  f64x4 acc[pairs_of<KT>()];
+  gram<T, KT, TALL>(g.p + party * g.step, g.ld, k, length, kSplit ? first : first + wave, end, kSplit ? 1 : kWaves, wave, acc);
+  double* const to = out + ((size_t)party * parts + part) * N * N;
   if constexpr (kSplit) {
 #pragma unroll
     for (int n = 0; n < 9; ++n) {
       const bool up = (u32)n <= wave;
+      const u32 i = up ? wave : 7 - wave, j = up ? n : n - wave - 1;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) put(up ? wave : 7 - wave, up ? n : n - wave - 1, 4 * r + lane / 16, lane % 16, acc[n][r]);
+      for (int r = 0; r < 4; ++r) {
+        const u32 s = short_of<KT, TALL>(i, 4 * r + lane / 16), t = short_of<KT, TALL>(j, lane % 16);
+        const double v = s < k && t < k ? acc[n][r] : 0.0;
+        to[s * N + t] = v;
+        if (i != j) to[t * N + s] = v;
+      }
     }
   } else {
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < KT; ++i)
-#pragma unroll
-      for (int j = 0; j <= i; ++j, ++n) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sum[wave][(4 * r + lane / 16) * 16 + lane % 16] = acc[n][r];
-        __syncthreads();
-        double s = 0.0;
-#pragma unroll
-        for (u32 w = 0; w < kWaves; ++w) s += sum[w][threadIdx.x];
-        put(i, j, threadIdx.x / 16, threadIdx.x % 16, s);
-        __syncthreads();
-      }
+    gram_sums<KT, TALL, kWaves>(acc, wave, k, sum, [&](u32 s, u32 t, double v) { to[s * N + t] = v; });
   }
 }
 
@@ -199,19 +256,27 @@ __device__ __forceinline__ double block_sum(double v, double* room) {
   for (u32 w = 0; w < THREADS / kWave; ++w) v += room[w];
   return v;
 }
-// element i of the parts' sum, eight loads on their way at a time
-__device__ __forceinline__ double sum_parts(const double* parts, u32 count, size_t each, u32 i) {
-  double s = 0.0;
-  u32 p = 0;
-  for (; p + 8 <= count; p += 8) {
-    double v[8];
+// Elements at, at + apart .. of the parts' sums, many loads on their way at a time.
+template <u32 E>
+__device__ __forceinline__ void sum_parts(const double* parts, u32 count, size_t each, u32 at, u32 apart, double (&s)[E]) {
+  constexpr u32 kAhead = E >= 8 ? 2 : 16 / E;
 #pragma unroll
-    for (u32 j = 0; j < 8; ++j) v[j] = parts[(p + j) * each + i];
-    s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  for (u32 e = 0; e < E; ++e) s[e] = 0.0;
+  u32 p = 0;
+  for (; p + kAhead <= count; p += kAhead) {
+    double v[kAhead][E];
+#pragma unroll
+    for (u32 j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (u32 e = 0; e < E; ++e) v[j][e] = parts[(p + j) * each + at + e * apart];
+#pragma unroll
+    for (u32 e = 0; e < E; ++e)
+#pragma unroll
+      for (u32 j = 0; j < kAhead; ++j) s[e] += v[j][e];
   }
-#pragma unroll 4
-  for (; p < count; ++p) s += parts[p * each + i];
-  return s;
+  for (; p < count; ++p)
+#pragma unroll
+    for (u32 e = 0; e < E; ++e) s[e] += parts[p * each + at + e * apart];
 }
 __device__ __forceinline__ double factor_of(double squares, double eps) { return 1.0 / (sqrt(squares) + eps); }
 
@@ -226,6 +291,7 @@ __device__ __forceinline__ f64x4 tile_product(const double* x, const double* y, 
     __builtin_memcpy(u[t], __builtin_assume_aligned(a + 8 * t, 16), 16);
     __builtin_memcpy(v[t], __builtin_assume_aligned(b + 8 * t, 16), 16);
   }
+  __builtin_amdgcn_sched_barrier(0);  // all are asked for before the first is waited for
   f64x4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
   for (u32 t = 0; t < N / 8; ++t)
@@ -233,41 +299,18 @@ __device__ __forceinline__ f64x4 tile_product(const double* x, const double* y, 
     for (int e = 0; e < 2; ++e) acc = mma4(u[t][e], v[t][e], acc);
   return acc;
 }
-// tile -> its row and column among those on and under the diagonal
-__device__ __forceinline__ u32 tile_row(u32 tile) {
-  u32 i = 0;
-  while ((i + 1) * (i + 2) / 2 <= tile) ++i;
-  return i;
-}
 
-// The polynomial of up to 64 rows, by one block in LDS: to = scale P / (|G|_F + eps). Products are of symmetric matrices that commute: the
-// tiles on and under the diagonal are formed and mirrored, and the second operand's rows are read for its columns. Results
-// stay in registers until all have read the operands, and then take an operand's place. The matrix instructions in turn bound it.
-template <int KT>
-constexpr u32 step_threads() {
-  return KT == 1 ? kWave : KT == 2 ? 4 * kWave : 8 * kWave;
-}
-template <int KT>
-__global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, double* to) {
-  constexpr u32 N = 16 * KT, S = N + 2, THREADS = step_threads<KT>(), WAVES = THREADS / kWave, TILES = KT * (KT + 1) / 2;
-  __shared__ __align__(16) double lds[3][N * S];
-  __shared__ double room[WAVES];
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
-  parts += (size_t)blockIdx.x * count * N * N;
-  to += (size_t)blockIdx.x * N * N;
-  double *const K = lds[0], *const Q = lds[1], *const P = lds[2];
-  double squares = 0.0;
-  for (u32 i = threadIdx.x; i < N * N; i += THREADS) {
-    const double s = sum_parts(parts, count, N * N, i);
-    K[i / N * S + i % N] = s;
-    if (i / N == i % N) squares += s;
-  }
-  const double by = factor_of(block_sum<THREADS>(squares, room), eps);
-  for (u32 i = threadIdx.x; i < N * N; i += THREADS) K[i / N * S + i % N] *= by * by;  // (each thread its own)
-  __syncthreads();
+// The polynomial of K where it lies in LDS with Q and P, rows N + 2 apart, by a block of WAVES wavefronts; it is left in P. Products are of
+// symmetric matrices that commute: the tiles on and under the diagonal are formed and mirrored, and the second operand's rows are
+// read for its columns. Results stay in registers until all have read the operands, and then take an operand's place. The matrix
+// instructions in turn bound it.
+template <int KT, u32 WAVES>
+__device__ __forceinline__ void polynomial(double* K, double* Q, double* P, const Steps& steps, u32 wave) {
+  constexpr u32 N = 16 * KT, S = N + 2, TILES = KT * (KT + 1) / 2;
+  const u32 lane = lane_id();
   // out = one I + self x + both x y, of x0 and, with two jobs, of x1
   const auto products = [&](auto jobs, double* out0, double* out1, const double* x0, const double* x1, const double* y, double one, double self, double both) {
-    constexpr u32 TOTAL = decltype(jobs)::value ? 2 * TILES : TILES, PER = (TOTAL + WAVES - 1) / WAVES;
+    constexpr u32 TOTAL = decltype(jobs)::value * TILES, PER = (TOTAL + WAVES - 1) / WAVES;
     f64x4 acc[PER];
 #pragma unroll
     for (u32 n = 0; n < PER; ++n) {
@@ -296,8 +339,8 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
     }
     __syncthreads();
   };
-  const Flag<false> one_job;
-  const Flag<true> two_jobs;
+  const Number<1> one_job;
+  const Number<2> two_jobs;
   for (int s = 0; s < steps.count; ++s) {
     const bool last = s + 1 == steps.count;
     double* const first = s == 0 ? P : Q;
@@ -312,26 +355,111 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
       products(one_job, K, K, K, K, Q, 0.0, 0.0, 1.0);
     }
   }
-  for (u32 i = threadIdx.x; i < N * N; i += THREADS) to[i] = P[i / N * S + i % N] * (by * scale);
+}
+// The same of one tile by one wavefront, in registers: lane l's results are elements 4 r + l / 16 of row l % 16, as the matrix is symmetric,
+// which is what the lane brings to the next product. 256 cycles each, one after the other.
+__device__ __forceinline__ f64x4 tile_squared(const f64x4& x, const f64x4& y) {
+  f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (int r = 0; r < 4; ++r) acc = mma4(x[r], y[r], acc);
+  return acc;
+}
+__device__ __forceinline__ f64x4 polynomial(f64x4 K, const Steps& steps) {
+  f64x4 P = {};
+  for (int s = 0; s < steps.count; ++s) {
+    const f64x4 square = tile_squared(K, K);
+    f64x4 Q;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      Q[r] = steps.c[s][2] * square[r] + (steps.c[s][1] * K[r] + (4 * r + lane_id() / 16 == lane_id() % 16 ? steps.c[s][0] : 0.0));
+    if (s + 1 < steps.count) K = tile_squared(tile_squared(K, Q), Q);
+    P = s == 0 ? Q : tile_squared(P, Q);
+  }
+  return P;
 }
 
-// More than 64 rows: K_0 and G's factor, from the parts.
-constexpr u32 kLarge = 128;
-__global__ __launch_bounds__(1024) void k_gram_join(const double* parts, u32 count, double eps, double* K, double* factor) {
-  __shared__ double room[16];
-  constexpr u32 kEach = kLarge * kLarge / 1024;
-  parts += (size_t)blockIdx.x * count * kLarge * kLarge;
-  double s[kEach], squares = 0.0;
+// From K's sums, element threadIdx.x + e THREADS of it in `sums`, to scale P / (|G|_F + eps), which put(row, column, value) takes: by a block,
+// of one tile by a wavefront.
+template <int KT>
+struct StepRoom {
+  double m[KT == 1 ? 1 : 3][KT == 1 ? 1 : 16 * KT * (16 * KT + 2)];
+};
+template <int KT>
+constexpr u32 step_threads() {
+  return KT == 1 ? kWave : KT == 2 ? 8 * kWave : KT == 3 ? 12 * kWave : 16 * kWave;
+}
+template <int KT>
+constexpr u32 step_elements() {
+  return 256 * KT * KT / step_threads<KT>();
+}
+template <int KT, class Put>
+__device__ __forceinline__ void steps_of(const Steps& steps, double scale, double eps, StepRoom<KT>& held, double* room, const double (&sums)[step_elements<KT>()],
+                                         const Put& put) {
+  constexpr u32 N = 16 * KT, S = N + 2, THREADS = step_threads<KT>(), E = step_elements<KT>();
+  double squares = 0.0;
 #pragma unroll
-  for (u32 n = 0; n < kEach; ++n) {
-    const u32 i = n * 1024 + threadIdx.x;
-    s[n] = sum_parts(parts, count, kLarge * kLarge, i);
-    if (i / kLarge == i % kLarge) squares += s[n];
+  for (u32 e = 0; e < E; ++e) {
+    const u32 i = threadIdx.x + e * THREADS;
+    if (i / N == i % N) squares += sums[e];
   }
-  const double by = factor_of(block_sum<1024>(squares, room), eps);
+  const double by = factor_of(block_sum<THREADS>(squares, room), eps);
+  if constexpr (KT == 1) {
+    // (element lane + 64 r is of row 4 r + lane / 16 and column lane % 16: as the products have it)
+    f64x4 K;
 #pragma unroll
-  for (u32 n = 0; n < kEach; ++n) K[(size_t)blockIdx.x * kLarge * kLarge + n * 1024 + threadIdx.x] = s[n] * by * by;
-  if (threadIdx.x == 0) factor[blockIdx.x] = by;
+    for (int r = 0; r < 4; ++r) K[r] = sums[r] * by * by;
+    const f64x4 P = polynomial(K, steps);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) put(4 * r + threadIdx.x / 16, threadIdx.x % 16, P[r] * (by * scale));
+  } else {
+    double *const K = held.m[0], *const P = held.m[2];
+#pragma unroll
+    for (u32 e = 0; e < E; ++e) {
+      const u32 i = threadIdx.x + e * THREADS;
+      K[i / N * S + i % N] = sums[e] * by * by;
+    }
+    __syncthreads();
+    polynomial<KT, THREADS / kWave>(K, held.m[1], P, steps, (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)));
+#pragma unroll
+    for (u32 e = 0; e < E; ++e) {
+      const u32 i = threadIdx.x + e * THREADS;
+      put(i / N, i % N, P[i / N * S + i % N] * (by * scale));
+    }
+  }
+}
+
+// The polynomial of up to 64 rows, from the parts' sums, by a block.
+template <int KT>
+__global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, double* to) {
+  constexpr u32 N = 16 * KT;
+  __shared__ __align__(16) StepRoom<KT> held;
+  __shared__ double room[16];
+  parts += (size_t)blockIdx.x * count * N * N;
+  to += (size_t)blockIdx.x * N * N;
+  double sums[step_elements<KT>()];
+  sum_parts(parts, count, N * N, threadIdx.x, step_threads<KT>(), sums);
+  steps_of<KT>(steps, scale, eps, held, room, sums, [&](u32 i, u32 j, double v) { to[i * N + j] = v; });
+}
+
+// More than 64 rows: K_0 and G's factor, from the parts; a block takes an eighth of a matrix, and each the parts' diagonals.
+constexpr u32 kLarge = 128, kJoinThreads = 512, kSlices = 8;
+__global__ __launch_bounds__(kJoinThreads) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, double* K, double* factor) {
+  __shared__ double room[kJoinThreads / kWave];
+  constexpr u32 kEach = kLarge * kLarge / kSlices / kJoinThreads;
+  const auto [party, slice] = place_of_block(blockIdx.x, kSlices, parties);
+  if (party >= parties) return;
+  parts += (size_t)party * count * kLarge * kLarge;
+  double s[kEach], squares = 0.0;
+  sum_parts(parts, count, kLarge * kLarge, slice * kEach * kJoinThreads + threadIdx.x, kJoinThreads, s);
+  if (threadIdx.x < kLarge) {
+    double d[1];
+    sum_parts(parts, count, kLarge * kLarge, threadIdx.x * (kLarge + 1), 0, d);
+    squares = d[0];
+  }
+  const double by = factor_of(block_sum<kJoinThreads>(squares, room), eps);
+#pragma unroll
+  for (u32 n = 0; n < kEach; ++n) K[(size_t)party * kLarge * kLarge + (slice * kEach + n) * kJoinThreads + threadIdx.x] = s[n] * by * by;
+  if (slice == 0 && threadIdx.x == 0) factor[party] = by;
 }
 // out = one I + self x + both x y, times the party's factor where there is one
 struct Product {
@@ -344,10 +472,11 @@ struct Products {
 };
 // A wavefront forms one tile on or under the diagonal.
 constexpr u32 kLargeTiles = 36;
-__global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 first_block) {
-  const u32 block = first_block + blockIdx.x, lane = lane_id(), tile = block % kLargeTiles, of = block / kLargeTiles;
-  const Product q = p.job[of % jobs];
-  const u32 party = of / jobs;
+__global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 parties, u32 first_block) {
+  const auto [party, part] = place_of_block(first_block + blockIdx.x, jobs * kLargeTiles, parties);
+  if (party >= parties) return;
+  const u32 lane = lane_id(), tile = part % kLargeTiles;
+  const Product q = p.job[part / kLargeTiles];
   const u32 i = tile_row(tile), j = tile - i * (i + 1) / 2;
   const size_t at = (size_t)party * kLarge * kLarge;
   const double* const x = q.x + at;
@@ -362,48 +491,51 @@ __global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 fi
   }
 }
 
-// out = keep base + P G. P lies in LDS; a wavefront takes `kPlaces` places of the long side by the whole short side at a time, and asks
-// for the next ones before it multiplies.
+// out = keep base + P G, P in LDS with rows N + 2 apart: a wavefront takes `kPlaces` places of the long side by the whole short side at a
+// time, pieces piece, piece + stride .., and asks for the next ones before it multiplies. Past the short side P is 0 against
+// everything before it, so that any numbers may stand there. WHOLE: no load or store is cut by the short side's end.
 template <int KT, bool TALL>
 struct Apply {
-  static constexpr int kVec = KT == 8 ? 2 : 4;  // along the long side, of rows
+  static constexpr int kVec = KT > 2 ? 2 : 4;  // along the long side, of rows
   static constexpr u32 kPlaces = TALL ? 16 : 16 * kVec;
   static constexpr u32 N = 16 * KT, S = N + 2;
+  static bool whole(size_t k) { return !TALL || (k % 4 == 0 && k % KT == 0); }
 };
-template <class T, int KT, bool TALL>
-__global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<const T> base, Batch<T> out, const double* poly, u32 k, u32 length, double keep,
-                                                    u32 blocks, u32 first_block) {
+template <class T>
+struct Matrices {
+  const T *g, *base;
+  T* out;
+  size_t ldg, ldb, ldo;
+};
+template <class T, int KT, bool TALL, bool WHOLE>
+__device__ __forceinline__ void apply(const Matrices<T>& m, const double* P, u32 k, u32 length, double keep, u32 piece, u32 stride) {
   using A = Apply<KT, TALL>;
   constexpr u32 N = A::N, S = A::S;
-  __shared__ __align__(16) double P[N * S];
-  const u32 block = first_block + blockIdx.x, party = block / blocks;
-  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id(), place = lane % 16, group = lane / 16;
-  poly += (size_t)party * N * N;
-  const T* const m = g.p + party * g.step;
-  const T* const b = base.p ? base.p + party * base.step : nullptr;
-  T* const o = out.p + party * out.step;
-  const u32 pieces = (length + A::kPlaces - 1) / A::kPlaces, stride = blocks * kWaves;
-  u32 piece = block % blocks * kWaves + wave;
+  const u32 place = lane_id() % 16, group = lane_id() / 16, pieces = (length + A::kPlaces - 1) / A::kPlaces;
+  const auto row = [&](u32 i, u32 n) { return (size_t)(i < n ? i : n - 1); };
   if constexpr (TALL) {
     // rows of the result are places of the long side; tile j holds the short side's KT (lane % 16) + j
+    const u32 s = KT * place;
     T next[KT][4], x[KT][4];
     const auto ask = [&](u32 at) {  // sixteen of the reduction, four to a lane, KT times
-      const u32 l = at + place;
+      const T* const from = m.g + row(at + place, length) * m.ldg;
 #pragma unroll
-      for (u32 t = 0; t < KT; ++t) load_few<T, 4>(m + (size_t)(l < length ? l : length - 1) * g.ld, 16 * t + 4 * group, k, next[t]);
+      for (u32 t = 0; t < KT; ++t) {
+        if (WHOLE) load_whole<T, 4>(from, 16 * t + 4 * group, k, next[t]);
+        else load_few<T, 4>(from, 16 * t + 4 * group, k, next[t]);
+      }
     };
     if (piece < pieces) ask(piece * A::kPlaces);
-    for (u32 i = threadIdx.x; i < N * N; i += kThreads) P[i / N * S + i % N] = poly[i];
-    __syncthreads();
     for (; piece < pieces; piece += stride) {
-      const u32 at = piece * A::kPlaces, s = KT * place;
+      const u32 at = piece * A::kPlaces;
       __builtin_memcpy(x, next, sizeof(x));
       T was[4][KT] = {};
-      if (b) {
+      if (m.base) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const u32 l = at + 4 * r + group;
-          load_few<T, KT>(b + (size_t)(l < length ? l : length - 1) * base.ld, s, k, was[r]);
+          const T* const from = m.base + row(at + 4 * r + group, length) * m.ldb;
+          if (WHOLE) load_whole<T, KT>(from, s, k, was[r]);
+          else load_few<T, KT>(from, s, k, was[r]);
         }
       }
       if (piece + stride < pieces) ask((piece + stride) * A::kPlaces);
@@ -419,30 +551,22 @@ __global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<cons
           const double v = (double)(float)x[t][e];
 #pragma unroll
           for (int j = 0; j < KT; ++j) acc[j] = mma4(v, d[j], acc[j]);
-          if (KT == 8) __builtin_amdgcn_sched_barrier(0);  // (P's elements not all at once: there are registers for two steps')
+          if (KT >= 3) __builtin_amdgcn_sched_barrier(0);  // (P's elements not all at once: there are registers for two steps')
         }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const u32 l = at + 4 * r + group;
-        if (l >= length) continue;
         T now[KT];
 #pragma unroll
-        for (int j = 0; j < KT; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[r][j] + acc[j][r] : acc[j][r]);
-        T* const to = o + (size_t)l * out.ld + s;
-        if (s + KT <= k) {
-          __builtin_memcpy(to, now, sizeof(now));
-        } else {
-#pragma unroll
-          for (int j = 0; j < KT; ++j)
-            if (s + j < k) to[j] = now[j];
-        }
+        for (int j = 0; j < KT; ++j) now[j] = (T)(float)(m.base ? keep * (double)(float)was[r][j] + acc[j][r] : acc[j][r]);
+        if (l < length) store_few<T, KT>(m.out + (size_t)l * m.ldo, s, k, now);
       }
     }
   } else {
     // tile j of the result's columns holds places at + kVec (lane % 16) + j
     constexpr int V = A::kVec;
-    for (u32 i = threadIdx.x; i < N * N; i += kThreads) P[i / N * S + i % N] = poly[i];
-    __syncthreads();
+    constexpr u32 kAhead = KT == 1 ? 4 : KT == 3 ? 6 : 8;  // loads on their way together, of one row of each lane group
+    static_assert(N % (4 * kAhead) == 0, "");
     for (; piece < pieces; piece += stride) {
       f64x4 acc[KT][V];
 #pragma unroll
@@ -450,50 +574,95 @@ __global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<cons
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[i][j] = f64x4{0.0, 0.0, 0.0, 0.0};
       const u32 l = piece * A::kPlaces + V * place;
-      const auto ask = [&](u32 s, T (&x)[V]) { load_few<T, V>(m + (size_t)(s < k ? s : k - 1) * g.ld, l < length ? l : length, length, x); };
-      constexpr u32 kAhead = N / 4 < 8 ? N / 4 : 8;  // loads on their way together, of one row of each lane group
+      const bool full = (piece + 1) * A::kPlaces <= length;
+      const auto load = [&](const T* from, T (&x)[V]) {
+        if (full) load_whole<T, V>(from, l, length, x);
+        else load_few<T, V>(from, l, length, x);
+      };
       T x[kAhead][V];
 #pragma unroll
-      for (u32 n = 0; n < kAhead; ++n) ask(4 * n + group, x[n]);
+      for (u32 n = 0; n < kAhead; ++n) load(m.g + row(4 * n + group, k) * m.ldg, x[n]);
       for (u32 t0 = 0; t0 < N; t0 += 4 * kAhead) {
         T now[kAhead][V];
         __builtin_memcpy(now, x, sizeof(x));
         if (t0 + 4 * kAhead < N) {
 #pragma unroll
-          for (u32 n = 0; n < kAhead; ++n) ask(t0 + 4 * (kAhead + n) + group, x[n]);
+          for (u32 n = 0; n < kAhead; ++n) load(m.g + row(t0 + 4 * (kAhead + n) + group, k) * m.ldg, x[n]);
         }
 #pragma unroll
         for (u32 n = 0; n < kAhead; ++n) {
-          const u32 s = t0 + 4 * n + group;
 #pragma unroll
           for (int i = 0; i < KT; ++i) {
-            const double d = P[(16 * i + place) * S + s];
+            const double d = P[(16 * i + place) * S + t0 + 4 * n + group];
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[i][j] = mma4(d, s < k ? (double)(float)now[n][j] : 0.0, acc[i][j]);
+            for (int j = 0; j < V; ++j) acc[i][j] = mma4(d, (double)(float)now[n][j], acc[i][j]);
           }
+          if (KT >= 3) __builtin_amdgcn_sched_barrier(0);
         }
       }
 #pragma unroll
-      for (int i = 0; i < KT; ++i)
+      for (int i = 0; i < KT; ++i) {
+        T was[4][V] = {};
+        if (m.base) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) load(m.base + row(16 * i + 4 * r + group, k) * m.ldb, was[r]);
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const u32 s = 16 * i + 4 * r + group;
-          if (s >= k) continue;
-          T was[V] = {}, now[V];
-          if (b) load_few<T, V>(b + (size_t)s * base.ld, l < length ? l : length, length, was);
+          T now[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) now[j] = (T)(float)(b ? keep * (double)(float)was[j] + acc[i][j][r] : acc[i][j][r]);
-          T* const to = o + (size_t)s * out.ld + l;
-          if (l + V <= length) {
-            __builtin_memcpy(to, now, sizeof(now));
-          } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-              if (l + j < length) to[j] = now[j];
-          }
+          for (int j = 0; j < V; ++j) now[j] = (T)(float)(m.base ? keep * (double)(float)was[r][j] + acc[i][j][r] : acc[i][j][r]);
+          if (s < k) store_few<T, V>(m.out + (size_t)s * m.ldo, l, length, now);
         }
+      }
     }
   }
+}
+template <class T>
+__device__ __forceinline__ Matrices<T> matrices_of(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, u32 party) {
+  return {g.p + party * g.step, base.p ? base.p + party * base.step : nullptr, out.p + party * out.step, g.ld, base.ld, out.ld};
+}
+template <class T, int KT, bool TALL, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<const T> base, Batch<T> out, const double* poly, u32 k, u32 length, double keep,
+                                                    u32 blocks, u32 parties, u32 first_block) {
+  using A = Apply<KT, TALL>;
+  __shared__ __align__(16) double P[A::N * A::S];
+  const auto [party, part] = place_of_block(first_block + blockIdx.x, blocks, parties);
+  if (party >= parties) return;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  poly += (size_t)party * A::N * A::N;
+#pragma unroll 8
+  for (u32 i = threadIdx.x; i < A::N * A::N; i += kThreads) P[i / A::N * A::S + i % A::N] = poly[i];
+  __syncthreads();
+  apply<T, KT, TALL, WHOLE>(matrices_of(g, base, out, party), P, k, length, keep, part * kWaves + wave, blocks * kWaves);
+}
+
+// All of it for small matrices of one tile, by a block each and without a workspace. us a call by one launch and by three: 8 matrices of 4 x 256 float32
+// 8 and 12, of 16 x 1024 16 and 13 (where the host waits for neither; its own part is 7 us less for one).
+constexpr u32 kOneThreads = 512, kOneWaves = kOneThreads / kWave;
+template <class T, bool TALL, bool WHOLE>
+__global__ __launch_bounds__(kOneThreads) void k_update(Batch<const T> g, Batch<const T> base, Batch<T> out, u32 k, u32 length, Steps steps, double keep,
+                                                        double scale, double eps) {
+  constexpr int KT = 1;
+  constexpr u32 N = 16 * KT, S = N + 2;
+  __shared__ __align__(16) StepRoom<KT> held;
+  __shared__ __align__(16) double sums[N * S];  // K's, and then P
+  __shared__ double part[kOneWaves][1][256], room[16];
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const Matrices<T> m = matrices_of(g, base, out, blockIdx.x);
+  f64x4 acc[pairs_of<KT>()];
+  gram<T, KT, TALL>(m.g, m.ldg, k, length, wave, (length + kChunk - 1) / kChunk, kOneWaves, wave, acc);
+  gram_sums<KT, TALL, kOneWaves>(acc, wave, k, part, [&](u32 s, u32 t, double v) { sums[s * S + t] = v; });
+  __syncthreads();
+  if (wave == 0) {
+    double own[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) own[e] = sums[(4 * e + threadIdx.x / 16) * S + threadIdx.x % 16];
+    steps_of<KT>(steps, scale, eps, held, room, own, [&](u32 i, u32 j, double v) { sums[i * S + j] = v; });
+  }
+  __syncthreads();
+  apply<T, KT, TALL, WHOLE>(m, sums, k, length, keep, wave, kOneWaves);
 }
 
 struct Shape {
@@ -502,7 +671,8 @@ struct Shape {
   u32 tiles() const { return k <= 16 ? 1 : k <= 32 ? 2 : k <= 48 ? 3 : k <= 64 ? 4 : 8; }
   size_t side() const { return 16 * tiles(); }
 };
-struct Plan {
+constexpr size_t kOneLength = 768;
+struct Plan {  // parts 0: a block a matrix, and no workspace
   size_t parts, gram, poly, factor, extra, total;
 };
 bool update_sizes(int type, size_t parties, size_t rows, size_t cols, Shape& s) {
@@ -511,8 +681,9 @@ bool update_sizes(int type, size_t parties, size_t rows, size_t cols, Shape& s) 
   return s.k <= kMostShort && parties * s.length <= kMostLength;
 }
 Plan update_plan(const Shape& s) {
-  Plan p;
-  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div((size_t)512, s.parties ? s.parties : 1), most = ceil_div(chunks, 8);
+  Plan p = {};
+  if (s.k <= 16 && s.length <= kOneLength) return p;
+  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div((size_t)256, s.parties ? s.parties : 1), most = ceil_div(chunks, 8);
   p.parts = want < most ? want : most;
   const size_t each = s.side() * s.side() * 8;
   p.gram = 0;
@@ -529,9 +700,11 @@ void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double sc
   const auto place = [&](int i) { return (double*)(ws + plan.extra + i * each); };
   double *const K = place(0), *const Q = place(1), *P = place(2), *const M = place(3), *spare = place(4);
   double *const factor = (double*)(ws + plan.factor), *const to = (double*)(ws + plan.poly);
-  hipLaunchKernelGGL(k_gram_join, dim3((unsigned)s.parties), dim3(1024), 0, st, (const double*)(ws + plan.gram), (u32)plan.parts, eps, K, factor);
+  hipLaunchKernelGGL(k_gram_join, dim3((unsigned)blocks_of(kSlices, s.parties)), dim3(kJoinThreads), 0, st, (const double*)(ws + plan.gram), (u32)plan.parts,
+                     (u32)s.parties, eps, K, factor);
   const auto run = [&](Products p, u32 jobs) {
-    in_turns(s.parties * jobs * kLargeTiles, kWave, [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL(k_products, grid, block, 0, st, p, jobs, first); });
+    in_turns(blocks_of(jobs * kLargeTiles, s.parties), kWave,
+             [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL(k_products, grid, block, 0, st, p, jobs, (u32)s.parties, first); });
   };
   for (int i = 0; i < steps.count; ++i) {
     const double a = steps.c[i][0], b = steps.c[i][1], c = steps.c[i][2];
@@ -557,38 +730,47 @@ void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double sc
 
 // Blocks of one matrix in k_apply: each brings P to LDS once, and there are enough for all compute units.
 u32 apply_blocks(const Shape& s, u32 places) {
-  const size_t need = ceil_div(s.length, places), want = ceil_div((size_t)1024, s.parties);
+  const size_t need = ceil_div(s.length, places), want = ceil_div((size_t)512, s.parties);
   return (u32)(need < want ? need : want);
 }
 
+template <class T, int KT, bool TALL>
+void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, const Shape& s, const Plan& plan, const Steps& steps, double keep,
+            double scale, double eps, char* ws, hipStream_t st) {
+  const u32 k = (u32)s.k, length = (u32)s.length;
+  const bool whole = Apply<KT, TALL>::whole(k);
+  if constexpr (KT == 1) {
+    if (plan.parts == 0) {
+      const dim3 grid((unsigned)s.parties), block(kOneThreads);
+      if (whole) hipLaunchKernelGGL((k_update<T, TALL, true>), grid, block, 0, st, g, base, out, k, length, steps, keep, scale, eps);
+      else hipLaunchKernelGGL((k_update<T, TALL, !TALL>), grid, block, 0, st, g, base, out, k, length, steps, keep, scale, eps);
+      return;
+    }
+  }
+  double *const sums = (double*)(ws + plan.gram), *const poly = (double*)(ws + plan.poly);
+  in_turns(blocks_of(plan.parts, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
+    hipLaunchKernelGGL((k_gram<T, KT, TALL>), grid, block, 0, st, g, k, length, (u32)plan.parts, (u32)s.parties, sums, first);
+  });
+  if constexpr (KT <= 4)
+    hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)sums, (u32)plan.parts, steps, scale, eps, poly);
+  else
+    large_steps(s, plan, steps, scale, eps, ws, st);
+  const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);
+  in_turns(blocks_of(blocks, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
+    if (whole) hipLaunchKernelGGL((k_apply<T, KT, TALL, true>), grid, block, 0, st, g, base, out, (const double*)poly, k, length, keep, blocks, (u32)s.parties, first);
+    else hipLaunchKernelGGL((k_apply<T, KT, TALL, !TALL>), grid, block, 0, st, g, base, out, (const double*)poly, k, length, keep, blocks, (u32)s.parties, first);
+  });
+}
 template <class T, bool TALL>
 void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, const Shape& s, const Plan& plan, const Steps& steps, double keep,
             double scale, double eps, char* ws, hipStream_t st) {
-  double* const poly = (double*)(ws + plan.poly);
-#define HAFLO_LOCAL_RUN(KT)                                                                                                                     \
-  do {                                                                                                                                          \
-    in_turns(s.parties * plan.parts, kThreads, [&](u32 first, dim3 grid, dim3 block) {                                                          \
-      hipLaunchKernelGGL((k_gram<T, KT, TALL>), grid, block, 0, st, g, (u32)s.k, (u32)s.length, (u32)plan.parts, (double*)(ws + plan.gram), first); \
-    });                                                                                                                                         \
-    if constexpr (KT <= 4)                                                                                                                      \
-      hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)(ws + plan.gram),             \
-                         (u32)plan.parts, steps, scale, eps, poly);                                                                             \
-    else                                                                                                                                        \
-      large_steps(s, plan, steps, scale, eps, ws, st);                                                                                          \
-    const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);                                                                      \
-    in_turns(s.parties * blocks, kThreads, [&](u32 first, dim3 grid, dim3 block) {                                                              \
-      hipLaunchKernelGGL((k_apply<T, KT, TALL>), grid, block, 0, st, g, base, out, (const double*)poly, (u32)s.k, (u32)s.length, keep, blocks,  \
-                         first);                                                                                                                \
-    });                                                                                                                                         \
-  } while (0)
   switch (s.tiles()) {
-    case 1: HAFLO_LOCAL_RUN(1); break;
-    case 2: HAFLO_LOCAL_RUN(2); break;
-    case 3: HAFLO_LOCAL_RUN(3); break;
-    case 4: HAFLO_LOCAL_RUN(4); break;
-    default: HAFLO_LOCAL_RUN(8); break;
+    case 1: return update<T, 1, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
+    case 2: return update<T, 2, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
+    case 3: return update<T, 3, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
+    case 4: return update<T, 4, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
+    default: return update<T, 8, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
   }
-#undef HAFLO_LOCAL_RUN
 }
 
 // Whether an output may lie where an input does: matrix over matrix, row over row.

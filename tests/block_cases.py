@@ -165,6 +165,8 @@ UPDATES = [  # type, parties, rows, cols, base, steps, pad
     ("f32", 2, 16, 33, True, [QUINTIC] * 5, 3), ("bf16", 2, 70, 17, True, [CUBIC] * 4, 0), ("f16", 1, 33, 40, False, [QUINTIC], 1),
     ("f32", 1, 64, 64, False, [QUINTIC] * 2, 0), ("bf16", 1, 65, 70, True, [QUINTIC] * 2, 0), ("f32", 2, 300, 4, False, [QUINTIC] * 5, 0),
     ("f32", 1, 3, 600, True, [CUBIC] * 16, 5), ("f32", 1, 90, 66, False, [QUINTIC], 0),
+    ("f32", 2, 9, 800, True, [QUINTIC] * 2, 0), ("f16", 1, 780, 16, False, [QUINTIC] * 5, 1), ("bf16", 1, 45, 300, True, [QUINTIC] * 2, 0),
+    ("f32", 1, 290, 48, True, [CUBIC], 0), ("f16", 1, 100, 30, True, [QUINTIC] * 2, 0), ("f32", 1, 60, 52, False, [QUINTIC], 2),
 ]
 UPDATES_LARGE = [
     ("f32", 8, 16, 4096, True, [QUINTIC] * 5, 0), ("bf16", 7, 1001, 37, False, [QUINTIC] * 5, 0), ("f32", 64, 512, 64, True, [QUINTIC] * 5, 0),
