@@ -122,17 +122,16 @@ __device__ __forceinline__ void store_four(const Out<T>& to, u32 t, u32 o, const
   }
 }
 
-// A block takes TM rows by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS: one
-// is filled while the other is read.
+// A block takes TM rows by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS, and one
+// is filled while the other is read; of tiles of 64 x 64 four steps'.
 template <class T, int TM, int TN, int WM, int WN, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const int8_t* w, u32 width, Out<T> to, u32 x_bytes, u32 w_bytes, u32 first_block) {
   constexpr int KE = step_elems<int8_t>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
   constexpr int LX = TM / 8 / WAVES, LW = TN / 8 / WAVES;
-  __shared__ __align__(16) int8_t lds[2 * (TM + TN) * KE];
-  int8_t* const lx0 = lds;
-  int8_t* const lw0 = lx0 + TM * KE;
-  int8_t* const lx1 = lw0 + TN * KE;
-  int8_t* const lw1 = lx1 + TM * KE;
+  constexpr bool kDeep = TM == 64;
+  __shared__ __align__(16) int8_t lds[(kDeep ? 4 : 2) * (TM + TN) * KE];
+  const auto x_tile = [&](int n) { return lds + n * (TM + TN) * KE; };
+  const auto w_tile = [&](int n) { return x_tile(n) + TM * KE; };
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
   // Blocks are dealt to the eight dies in turn: each gets neighbouring tiles, four tiles of rows by all outputs at a time,
   // whose operands its cache holds.
@@ -161,7 +160,11 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const
   for (int j = 0; j < RT; ++j)
 #pragma unroll
     for (int i = 0; i < OT; ++i) acc[i][j] = i32x4{0, 0, 0, 0};
-  reduce<int8_t, TM, TN, WAVES>(from_x, at_x, from_w, at_w, width / KE, wave, row0, out0, lx0, lw0, lx1, lw1, acc);
+  if constexpr (kDeep)
+    reduce_deep<int8_t, TM, TN, WAVES>(from_x, at_x, from_w, at_w, width / KE, wave, row0, out0, x_tile(0), w_tile(0), x_tile(1), w_tile(1), x_tile(2),
+                                       w_tile(2), x_tile(3), w_tile(3), acc);
+  else
+    reduce<int8_t, TM, TN, WAVES>(from_x, at_x, from_w, at_w, width / KE, wave, row0, out0, x_tile(0), w_tile(0), x_tile(1), w_tile(1), acc);
 #pragma unroll
   for (int j = 0; j < RT; ++j) {
     const u32 t = t0 + row0 + j * 16 + lane % 16;
@@ -173,12 +176,14 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const
 }
 
 // Few rows: a block takes 16 outputs by 16 R rows, its wavefronts a part of the reduction each, so that W is on its way from all
-// of them at once; their sums are joined in LDS. With OWN the block brings the rows, at most four, to eight bits itself.
+// of them at once, x and the next pieces with it; their sums are joined in LDS. With OWN the block brings the rows, at most four, to
+// eight bits itself.
 constexpr u32 kFewWaves = 8, kFewThreads = kFewWaves * kWave, kOwnBytes = 32768;
 template <class T, int R, bool OWN>
 __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ldx, u32 cols, const int8_t* xq, const int8_t* w, u32 width, Out<T> to,
                                                           u32 first_block) {
-  constexpr u32 kAhead = R == 1 ? 4 : R == 2 ? 4 : 2;  // pieces of 128 bytes of each row that are on their way together
+  constexpr u32 kAhead = R == 1 ? 4 : 2;  // pieces of 128 bytes of each row that are on their way together
+  constexpr u32 kResults = (256 * R + kFewThreads - 1) / kFewThreads;
   __shared__ __align__(16) int8_t own[OWN ? kOwnBytes : 16];
   __shared__ float own_scale[4];
   __shared__ u32 room[kFewWaves];
@@ -188,14 +193,37 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
   const auto last = [](u32 i, u32 n) { return i < n ? i : n - 1; };
   const u32 pieces = width / 128, first = pieces * wave / kFewWaves, end = pieces * (wave + 1) / kFewWaves;
   const int8_t* const wr = w + (size_t)last(o0 + lane % 16, to.outer) * width + lane / 16 * 16;
-  i32x4 wv[kAhead][2];
+  const int8_t* xr[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) xr[j] = (OWN ? own : xq) + (size_t)last(t0 + 16 * j + lane % 16, to.rows) * width + lane / 16 * 16;
+  struct Pieces {
+    i32x4 w[kAhead][2], x[OWN ? 1 : kAhead][2][R];
+  };
+  Pieces next;
   const auto ask = [&](u32 p) {
 #pragma unroll
     for (u32 u = 0; u < kAhead; ++u)
 #pragma unroll
-      for (u32 h = 0; h < 2; ++h) wv[u][h] = *(const i32x4*)(wr + (size_t)last(p + u, end) * 128 + h * 64);
+      for (u32 h = 0; h < 2; ++h) {
+        const size_t at = (size_t)last(p + u, end) * 128 + h * 64;
+        next.w[u][h] = *(const i32x4*)(wr + at);
+        if (!OWN) {
+#pragma unroll
+          for (int j = 0; j < R; ++j) next.x[OWN ? 0 : u][h][j] = *(const i32x4*)(xr[j] + at);
+        }
+      }
   };
   if (first < end) ask(first);
+  // what the results take besides their sums: result i is of row t0 + i / 16 and output o0 + i % 16
+  float by[kResults], bias[kResults], was[kResults], x_scale[kResults];
+#pragma unroll
+  for (u32 n = 0; n < kResults; ++n) {
+    const u32 i = threadIdx.x + n * kFewThreads, t = last(t0 + i / 16, to.rows), o = last(o0 + i % 16, to.outer);
+    by[n] = to.w_scale[o];
+    x_scale[n] = OWN ? 0.0f : to.x_scale[t];
+    bias[n] = to.bias ? to.bias[o] : 0.0f;
+    was[n] = to.residual ? (float)to.residual[t * to.ldr + o] : 0.0f;
+  }
   if (OWN) {
     const u32 groups = to.rows == 1 ? 1 : to.rows == 2 ? 2 : 4, lanes = kFewThreads / groups, group = threadIdx.x / lanes, row = last(group, to.rows);
     const float s = quantize_row(xf + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
@@ -204,29 +232,21 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
     if (threadIdx.x % lanes == 0) own_scale[group] = s;
     __syncthreads();
   }
-  const int8_t* xr[R];
   i32x4 acc[R];
 #pragma unroll
-  for (int j = 0; j < R; ++j) {
-    xr[j] = (OWN ? own : xq) + (size_t)last(t0 + 16 * j + lane % 16, to.rows) * width + lane / 16 * 16;
-    acc[j] = i32x4{0, 0, 0, 0};
-  }
+  for (int j = 0; j < R; ++j) acc[j] = i32x4{0, 0, 0, 0};
   for (u32 p = first; p < end; p += kAhead) {
-    i32x4 wn[kAhead][2];
-#pragma unroll
-    for (u32 u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (u32 h = 0; h < 2; ++h) wn[u][h] = wv[u][h];
+    const Pieces now = next;
     if (p + kAhead < end) ask(p + kAhead);
 #pragma unroll
     for (u32 u = 0; u < kAhead; ++u)
 #pragma unroll
       for (u32 h = 0; h < 2; ++h) {
-        if (p + u >= end) wn[u][h] = i32x4{0, 0, 0, 0};
+        const i32x4 wv = p + u < end ? now.w[u][h] : i32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-          const i32x4 xv = *(const i32x4*)(xr[j] + (size_t)last(p + u, end) * 128 + h * 64);
-          acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wn[u][h], xv, acc[j], 0, 0, 0);
+          const i32x4 xv = OWN ? *(const i32x4*)(xr[j] + (size_t)last(p + u, end) * 128 + h * 64) : now.x[OWN ? 0 : u][h][j];
+          acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc[j], 0, 0, 0);
         }
       }
   }
@@ -234,21 +254,23 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
 #pragma unroll
   for (int j = 0; j < R; ++j) *(i32x4*)&sums[wave][j][lane % 16 * 16 + lane / 16 * 4] = acc[j];
   __syncthreads();
-  for (u32 i = threadIdx.x; i < 256 * R; i += kFewThreads) {
-    const u32 t = t0 + i / 16, o = o0 + i % 16;
-    if (t >= to.rows || o >= to.outer) continue;
+#pragma unroll
+  for (u32 n = 0; n < kResults; ++n) {
+    const u32 i = threadIdx.x + n * kFewThreads, t = t0 + i / 16, o = o0 + i % 16;
+    if (i >= 256 * R || t >= to.rows || o >= to.outer) continue;
     int s = 0;
 #pragma unroll
     for (u32 v = 0; v < kFewWaves; ++v) s += sums[v][i / 256][i % 256];
-    float y = (float)s * ((OWN ? own_scale[t] : to.x_scale[t]) * to.w_scale[o]);
-    if (to.bias) y += to.bias[o];
-    if (to.residual) y += (float)to.residual[t * to.ldr + o];
-    to.y[t * to.ldy + o] = (T)y;
+    to.y[t * to.ldy + o] = (T)((float)s * ((OWN ? own_scale[t] : x_scale[n]) * by[n]) + bias[n] + was[n]);
   }
 }
 
-constexpr size_t kFewRows = 64, kOwnRows = 4;
+constexpr size_t kFewRows = 32, kFewOuter = 4096, kFewBytes = 2048, kOwnRows = 4;
 bool own_rows(size_t rows, size_t cols) { return rows <= kOwnRows && rows * row_bytes(cols) <= kOwnBytes; }
+// One block for each compute unit at most, and rows long enough to split: then k_int8_few, else tiles of 64 x 64. Calls of few / of tiles, us, 5, 16
+// and 32 rows: 1024 to 1024 7.4 / 6.7, 8.4 / 6.9, 7.8 / 7.5; 2048 to 2048 7.5 / 8.0, 8.6 / 8.4, 7.8 / 9.0; 4096 to 1024 7.6 / 10.6, 8.6 / 10.9,
+// 10.3 / 11.5; 4096 to 4096 7.9 / 10.8, 8.8 / 11.0, 10.8 / 11.5, 48 rows 13.5 / 11.8; 4096 to 8192 11.5 / 11.9, 13.5 / 11.8, 16.2 / 12.5.
+bool few_rows(size_t rows, size_t width, size_t outer) { return rows <= kFewRows && outer <= kFewOuter && width >= kFewBytes; }
 template <class T>
 void few(const T* x, size_t ldx, size_t cols, const int8_t* xq, const int8_t* w, const Out<T>& to, hipStream_t st) {
 #define HAFLO_LOCAL_RUN(R, OWN)                                                                                                            \
@@ -257,8 +279,7 @@ void few(const T* x, size_t ldx, size_t cols, const int8_t* xq, const int8_t* w,
   })
   if (!xq) HAFLO_LOCAL_RUN(1, true);
   else if (to.rows <= 16) HAFLO_LOCAL_RUN(1, false);
-  else if (to.rows <= 32) HAFLO_LOCAL_RUN(2, false);
-  else HAFLO_LOCAL_RUN(4, false);
+  else HAFLO_LOCAL_RUN(2, false);
 #undef HAFLO_LOCAL_RUN
 }
 template <class T>
@@ -273,8 +294,9 @@ void quantize(const void* x, size_t ldx, size_t rows, size_t cols, int8_t* q, fl
 }
 template <class T>
 void product(const int8_t* x, const int8_t* w, size_t cols, const Out<T>& to, hipStream_t st) {
-  if (to.rows <= kFewRows) return few<T>(nullptr, 0, cols, x, w, to, st);
-  const size_t width = row_bytes(cols), x_bytes = to.rows * width, w_bytes = to.outer * width;
+  const size_t width = row_bytes(cols);
+  if (few_rows(to.rows, width, to.outer)) return few<T>(nullptr, 0, cols, x, w, to, st);
+  const size_t x_bytes = to.rows * width, w_bytes = to.outer * width;
   const bool far = x_bytes > 0xFFFFFFFFu || w_bytes > 0xFFFFFFFFu;
 #define HAFLO_LOCAL_RUN(TM, TN, WM, WN, FAR)                                                                                        \
   in_turns(ceil_div(to.rows, TM) * ceil_div(to.outer, TN), WM * WN * kWave, [&](u32 first, dim3 grid, dim3 block) {                 \

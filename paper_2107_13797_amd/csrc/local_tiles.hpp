@@ -187,5 +187,66 @@ __device__ __forceinline__ void reduce(const From& x, const typename From::At (&
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): none of them arrives after the block's end
 }
 
+// One step of a reduction whose tiles lie in LDS four steps deep: this one's tiles are waited for, the ones three steps on asked for
+// in place of the last step's.
+template <class T, int TM, int TN, int WAVES, class From, int RT, int OT>
+__device__ __forceinline__ void deep_step(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
+                                          const typename From::At (&at_w)[TN / 8 / WAVES], u32 k_later, u32 wave, u32 row0, u32 out0, T* cx, T* cw, T* lx,
+                                          T* lw, typename Multiplied<T>::Sum (&acc)[OT][RT]) {
+  constexpr int kSub = step_elems<T>() / 4 / Multiplied<T>::kLane;
+  wait_for_tiles<2 * (TM + TN) / 8 / WAVES>();
+  ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k_later, wave, lx, lw);
+  ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k_later, wave, lx, lw);
+  Frags<T, OT, RT> f[kSub];
+#pragma unroll
+  for (int s = 0; s < kSub; ++s) {
+    load_x(f[s], cx, row0, s, 0);
+    load_w(f[s], cw, out0, s);
+  }
+#pragma unroll
+  for (int s = 0; s < kSub; ++s)
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int i = 0; i < OT; ++i) acc[i][j] = mma32(f[s].w[i], f[s].x[j], acc[i][j]);
+}
+// The whole reduction of a small tile, of which few are on a compute unit: what bounds it is how long a load takes, so that three
+// steps' are on their way. The eight tiles in LDS are told apart here, as in `reduce`.
+template <class T, int TM, int TN, int WAVES, class From, int RT, int OT>
+__device__ __forceinline__ void reduce_deep(const From& x, const typename From::At (&at_x)[TM / 8 / WAVES], const From& w,
+                                            const typename From::At (&at_w)[TN / 8 / WAVES], u32 steps, u32 wave, u32 row0, u32 out0, T* __restrict__ x0,
+                                            T* __restrict__ w0, T* __restrict__ x1, T* __restrict__ w1, T* __restrict__ x2, T* __restrict__ w2,
+                                            T* __restrict__ x3, T* __restrict__ w3, typename Multiplied<T>::Sum (&acc)[OT][RT]) {
+  constexpr u32 KE = step_elems<T>();
+  const u32 inner = steps * KE;
+  const auto after = [&](u32 at) { return at + KE < inner ? at + KE : 0; };
+  const auto ask = [&](u32 k, T* lx, T* lw) {
+    ask_tiles<T, TM, TN, WAVES>(0, x, at_x, w, at_w, k, wave, lx, lw);
+    ask_tiles<T, TM, TN, WAVES>(1, x, at_x, w, at_w, k, wave, lx, lw);
+  };
+  u32 k = 0;
+  ask(k, x0, w0);
+  k = after(k);
+  ask(k, x1, w1);
+  k = after(k);
+  ask(k, x2, w2);
+  // the loads go round past the last step, rather than that the loop has other forms for its end
+  for (u32 i = 0;; i += 4) {
+    k = after(k);
+    deep_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, wave, row0, out0, x0, w0, x3, w3, acc);
+    if (i + 1 >= steps) break;
+    k = after(k);
+    deep_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, wave, row0, out0, x1, w1, x0, w0, acc);
+    if (i + 2 >= steps) break;
+    k = after(k);
+    deep_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, wave, row0, out0, x2, w2, x1, w1, acc);
+    if (i + 3 >= steps) break;
+    k = after(k);
+    deep_step<T, TM, TN, WAVES>(x, at_x, w, at_w, k, wave, row0, out0, x3, w3, x2, w2, acc);
+    if (i + 4 >= steps) break;
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): none of them arrives after the block's end
+}
+
 }  // namespace local
 }  // namespace haflo

@@ -623,17 +623,35 @@ template <class T>
 __device__ __forceinline__ Matrices<T> matrices_of(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, u32 party) {
   return {g.p + party * g.step, base.p ? base.p + party * base.step : nullptr, out.p + party * out.step, g.ld, base.ld, out.ld};
 }
+// `from`: P; of one tile the parts' sums, from which each block's first wavefront forms the polynomial itself, which takes it no longer
+// than a launch (8 matrices of 16 x 4096 float32 13.5 us by three launches and 12.3 by two).
+struct Polynomial {
+  const double* from;
+  u32 count;
+  Steps steps;
+  double scale, eps;
+};
 template <class T, int KT, bool TALL, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<const T> base, Batch<T> out, const double* poly, u32 k, u32 length, double keep,
+__global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<const T> base, Batch<T> out, Polynomial poly, u32 k, u32 length, double keep,
                                                     u32 blocks, u32 parties, u32 first_block) {
   using A = Apply<KT, TALL>;
   __shared__ __align__(16) double P[A::N * A::S];
   const auto [party, part] = place_of_block(first_block + blockIdx.x, blocks, parties);
   if (party >= parties) return;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-  poly += (size_t)party * A::N * A::N;
+  const double* const from = poly.from + (size_t)party * poly.count * A::N * A::N;
+  if constexpr (KT == 1) {
+    __shared__ StepRoom<1> held;
+    __shared__ double room[1];
+    if (wave == 0) {
+      double sums[4];
+      sum_parts(from, poly.count, 256, threadIdx.x, kWave, sums);
+      steps_of<1>(poly.steps, poly.scale, poly.eps, held, room, sums, [&](u32 i, u32 j, double v) { P[i * A::S + j] = v; });
+    }
+  } else {
 #pragma unroll 8
-  for (u32 i = threadIdx.x; i < A::N * A::N; i += kThreads) P[i / A::N * A::S + i % A::N] = poly[i];
+    for (u32 i = threadIdx.x; i < A::N * A::N; i += kThreads) P[i / A::N * A::S + i % A::N] = from[i];
+  }
   __syncthreads();
   apply<T, KT, TALL, WHOLE>(matrices_of(g, base, out, party), P, k, length, keep, part * kWaves + wave, blocks * kWaves);
 }
@@ -683,12 +701,12 @@ bool update_sizes(int type, size_t parties, size_t rows, size_t cols, Shape& s) 
 Plan update_plan(const Shape& s) {
   Plan p = {};
   if (s.k <= 16 && s.length <= kOneLength) return p;
-  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div((size_t)256, s.parties ? s.parties : 1), most = ceil_div(chunks, 8);
+  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div(s.tiles() <= 2 ? (size_t)512 : (size_t)256, s.parties ? s.parties : 1), most = ceil_div(chunks, 8);
   p.parts = want < most ? want : most;
   const size_t each = s.side() * s.side() * 8;
   p.gram = 0;
   p.poly = p.gram + s.parties * p.parts * each;
-  p.factor = p.poly + s.parties * each;
+  p.factor = p.poly + (s.k <= 16 ? 0 : s.parties * each);
   p.extra = p.factor + align256(s.parties * 8);
   p.total = s.k > 64 ? p.extra + 5 * s.parties * each : p.factor;
   return p;
@@ -730,7 +748,7 @@ void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double sc
 
 // Blocks of one matrix in k_apply: each brings P to LDS once, and there are enough for all compute units.
 u32 apply_blocks(const Shape& s, u32 places) {
-  const size_t need = ceil_div(s.length, places), want = ceil_div((size_t)512, s.parties);
+  const size_t need = ceil_div(s.length, places), want = ceil_div(s.tiles() <= 2 ? (size_t)768 : (size_t)512, s.parties);
   return (u32)(need < want ? need : want);
 }
 
@@ -751,14 +769,17 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
   in_turns(blocks_of(plan.parts, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
     hipLaunchKernelGGL((k_gram<T, KT, TALL>), grid, block, 0, st, g, k, length, (u32)plan.parts, (u32)s.parties, sums, first);
   });
-  if constexpr (KT <= 4)
+  Polynomial from = {poly, 1, steps, scale, eps};
+  if constexpr (KT == 1)
+    from = {sums, (u32)plan.parts, steps, scale, eps};
+  else if constexpr (KT <= 4)
     hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)sums, (u32)plan.parts, steps, scale, eps, poly);
   else
     large_steps(s, plan, steps, scale, eps, ws, st);
   const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);
   in_turns(blocks_of(blocks, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
-    if (whole) hipLaunchKernelGGL((k_apply<T, KT, TALL, true>), grid, block, 0, st, g, base, out, (const double*)poly, k, length, keep, blocks, (u32)s.parties, first);
-    else hipLaunchKernelGGL((k_apply<T, KT, TALL, !TALL>), grid, block, 0, st, g, base, out, (const double*)poly, k, length, keep, blocks, (u32)s.parties, first);
+    if (whole) hipLaunchKernelGGL((k_apply<T, KT, TALL, true>), grid, block, 0, st, g, base, out, from, k, length, keep, blocks, (u32)s.parties, first);
+    else hipLaunchKernelGGL((k_apply<T, KT, TALL, !TALL>), grid, block, 0, st, g, base, out, from, k, length, keep, blocks, (u32)s.parties, first);
   });
 }
 template <class T, bool TALL>

@@ -240,6 +240,7 @@ INT8 = [  # type, rows, inner, outer, pad, bias, residual
     ("f32", 1, 1, 1, 0, False, False), ("bf16", 1, 130, 20, 0, True, False), ("f16", 3, 127, 33, 1, False, True), ("f32", 17, 128, 16, 0, True, True),
     ("bf16", 40, 33, 70, 0, False, False), ("f16", 65, 257, 65, 3, True, True), ("f32", 2, 1025, 130, 0, False, True), ("bf16", 130, 64, 40, 8, True, False),
     ("f16", 1, 2049, 7, 0, True, True), ("f32", 70, 300, 5, 1, False, False), ("bf16", 20, 700, 90, 0, True, True), ("bf16", 1, 9000, 3, 0, False, False),
+    ("f16", 6, 2050, 20, 1, True, True), ("f32", 19, 2300, 18, 0, False, True), ("bf16", 33, 2048, 70, 0, True, False), ("f32", 2, 20000, 5, 0, True, False),
 ]
 INT8_LARGE = [
     ("bf16", 1, 4096, 4096, 0, False, False), ("f16", 16, 4096, 515, 0, True, True), ("f32", 64, 1000, 1001, 1, True, False), ("f16", 3001, 1001, 515, 0, True, True),
