@@ -26,29 +26,10 @@ __device__ __forceinline__ int party_of(const int* index, u32 t, u32 parties) {
 // a place below `count`, the last one for those behind it
 __device__ __forceinline__ u32 lowest(u32 i, u32 count) { return i < count ? i : count - 1; }
 
-// Eight elements at column k of a row of `cols`, in two steps: a load without a branch, as the compiler waits for a load at the
-// next branch around one, and where the elements pass the row's end, so the row's last eight were loaded, their moving to
-// their places, with zeros behind them. Rows of less than eight are loaded element by element.
-template <class T>
-__device__ __forceinline__ Vec8<T> load_row(const T* row, u32 k, u32 cols) {
-  return load_wide(row + (k + 8 <= cols ? k : cols - 8));
-}
+// Eight elements at column k of a row of less than eight; longer ones are loaded by load_clamped and settled.
 template <class T>
 __device__ __forceinline__ Vec8<T> load_short(const T* row, u32 k, u32 cols) {
   return load_some(row, k == 0 ? (int)cols : 0);
-}
-template <class T>
-__device__ __forceinline__ void settle(Vec8<T>& v, u32 k, u32 cols) {
-  if (k + 8 <= cols || cols < 8) return;
-  const u32 by = k + 8 - cols;
-  const Vec8<T> was = v;
-  v = Vec8<T>{};
-#pragma unroll
-  for (u32 n = 1; n < 8; ++n)
-    if (by == n) {
-#pragma unroll
-      for (u32 j = 0; j + n < 8; ++j) v.set(j, was.get(j + n));
-    }
 }
 template <class T>
 __device__ __forceinline__ void apply_drop(Vec8<T>& v, const Drop& d, u32 row, u32 k) {
@@ -127,9 +108,9 @@ __global__ __launch_bounds__(kShrinkWaves * kWave) void k_shrink(const T* x, siz
       if (inner >= 8) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-          xv[u] = load_row(x_row, k[u], inner);
+          xv[u] = load_clamped(x_row, k[u], inner);
 #pragma unroll
-          for (int i = 0; i < RT; ++i) fv[u][i] = load_row(fa + f_at[i], k[u], inner);
+          for (int i = 0; i < RT; ++i) fv[u][i] = load_clamped(fa + f_at[i], k[u], inner);
         }
       } else {
 #pragma unroll
@@ -395,7 +376,7 @@ __device__ __forceinline__ void few_product(const T* x, size_t ldx, const T* w, 
   for (u32 n = first; n < end; ++n) {
     Vec8<T> wv[kSteps], xv[kLoads];
     const u32 kx = n * kElems + lane % kLanes * 8, kw = n * kElems + wave / 4 * kSteps * 32 + lane / 16 * 8;
-    const auto load = [&](const T* row, u32 k) { return SHORT ? load_short(row, k, inner) : load_row(row, k, inner); };
+    const auto load = [&](const T* row, u32 k) { return SHORT ? load_short(row, k, inner) : load_clamped(row, k, inner); };
 #pragma unroll
     for (u32 i = 0; i < kLoads; ++i) xv[i] = load(x + x_at[i], kx);
 #pragma unroll
@@ -479,9 +460,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(const T* x, size_t ld
     if (inner >= 8) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        xv[u] = load_row(x + (size_t)t * ldx, k[u], inner);
+        xv[u] = load_clamped(x + (size_t)t * ldx, k[u], inner);
 #pragma unroll
-        for (int i = 0; i < ZT; ++i) fv[u][i] = load_row(fa + f_at[i], k[u], inner);
+        for (int i = 0; i < ZT; ++i) fv[u][i] = load_clamped(fa + f_at[i], k[u], inner);
       }
     } else {
 #pragma unroll
@@ -707,7 +688,7 @@ __global__ __launch_bounds__(kPrepareThreads) void k_prepare(Prepare<T> p, u32 f
     if (at >= (u64)job.rows * groups) return;
     const u32 r = (u32)(at / groups), c = (u32)(at - (u64)r * groups) * 8;
     const T* const row = job.in + (size_t)r * job.ld;
-    Vec8<T> v = job.cols < 8 ? load_short(row, c, job.cols) : load_row(row, c, job.cols);
+    Vec8<T> v = job.cols < 8 ? load_short(row, c, job.cols) : load_clamped(row, c, job.cols);
     settle(v, c, job.cols);
     store_wide(job.out + (size_t)r * job.out_ld + c, v);
     return;
@@ -797,7 +778,7 @@ __global__ __launch_bounds__(kThreads) void k_grad(GradOf<T> a, GradOf<T> b, u32
     look(n + kAhead);
     if (cols >= 8) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) ahead[u].v = load_row(m + (size_t)ahead[u].t * ld, col, cols);
+      for (int u = 0; u < kAhead; ++u) ahead[u].v = load_clamped(m + (size_t)ahead[u].t * ld, col, cols);
     } else {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) ahead[u].v = load_short(m + (size_t)ahead[u].t * ld, col, cols);

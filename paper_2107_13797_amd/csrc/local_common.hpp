@@ -79,15 +79,38 @@ __device__ __forceinline__ void store_some(T* p, const Vec8<T>& v, int n) {
     if (j < n) p[j] = v.get(j);
 }
 
-// Eight elements of a row from column `col` on, zeros behind its end; no element of another vector is read.
+// Eight elements of a row from column `col` on, zeros behind its end; no element of another vector is read. Lanes past the end, as
+// groups of a power of two have them, take no part in what the one across it does.
 template <class T>
 __device__ __forceinline__ Vec8<T> load_cols(const T* row, u32 col, u32 cols) {
-  return col + 8 <= cols ? load_wide(row + col) : load_some(row + col, col < cols ? (int)(cols - col) : 0);
+  if (col + 8 <= cols) return load_wide(row + col);
+  if (col >= cols) return Vec8<T>{};
+  return load_some(row + col, (int)(cols - col));
+}
+// The same in two steps where nothing is written over the row, and it has eight elements: a load without a branch, as the compiler waits for
+// a load at the next branch around one, of the row's last eight where the elements pass its end; and their moving to their places,
+// with zeros behind them.
+template <class T>
+__device__ __forceinline__ Vec8<T> load_clamped(const T* row, u32 col, u32 cols) {
+  return load_wide(row + (col + 8 <= cols ? col : cols - 8));
+}
+template <class T>
+__device__ __forceinline__ void settle(Vec8<T>& v, u32 col, u32 cols) {
+  if (col + 8 <= cols || cols < 8) return;
+  const u32 by = col + 8 - cols;
+  const Vec8<T> was = v;
+  v = Vec8<T>{};
+#pragma unroll
+  for (u32 n = 1; n < 8; ++n)
+    if (by == n) {
+#pragma unroll
+      for (u32 j = 0; j + n < 8; ++j) v.set(j, was.get(j + n));
+    }
 }
 template <class T>
 __device__ __forceinline__ void store_cols(T* row, u32 col, u32 cols, const Vec8<T>& v) {
   if (col + 8 <= cols) store_wide(row + col, v);
-  else store_some(row + col, v, col < cols ? (int)(cols - col) : 0);
+  else if (col < cols) store_some(row + col, v, (int)(cols - col));
 }
 
 // The dropout of one call: what a kernel needs of (p, seed, offset).

@@ -31,6 +31,13 @@ struct Norm {
   u32 rows, cols;
   float scale;
   double eps, per_col;  // 1 / cols
+  bool apart;           // no result lies over an operand, and rows have eight elements
+
+  // a vector of a row, on its way and as it is
+  __device__ __forceinline__ Vec8<T> ask(const T* row, u32 col) const { return apart ? load_clamped(row, col, cols) : load_cols(row, col, cols); }
+  __device__ __forceinline__ void have(Vec8<T>& v, u32 col) const {
+    if (apart) settle(v, col, cols);
+  }
 };
 
 struct Eight {
@@ -107,16 +114,19 @@ __global__ __launch_bounds__(MOST) void k_norm(Norm<T> n, u32 lanes, T* r_out, s
   Vec8<T> xn, fn, gn;
   const auto ask = [&](u64 row) {
     row = row < n.rows ? row : n.rows - 1;
-    xn = load_cols(n.x + row * n.ldx, col, n.cols);
-    if (MODE != kStream) fn = load_cols(n.f + row * n.ldf, col, n.cols);
-    if (MODE == kFullGate) gn = load_cols(n.gate + row * n.ldg, col, n.cols);
+    xn = n.ask(n.x + row * n.ldx, col);
+    if (MODE != kStream) fn = n.ask(n.f + row * n.ldf, col);
+    if (MODE == kFullGate) gn = n.ask(n.gate + row * n.ldg, col);
   };
   ask(mine);
   for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += step, mine += step) {
     const bool live = mine < n.rows;
     const u64 row = mine;
-    const Vec8<T> xv = xn, fv = fn, gv = gn;
+    Vec8<T> xv = xn, fv = fn, gv = gn;
     if (base + step < n.rows) ask(mine + step);
+    n.have(xv, col);
+    if (MODE != kStream) n.have(fv, col);
+    if (MODE == kFullGate) n.have(gv, col);
     Eight f = floats(fv), p, r;
     float q = 1.0f, t = 1.0f;
     if (MODE != kStream && n.post) q = root(sum(squares(f)), n.per_col, n.eps);
@@ -194,12 +204,12 @@ struct BackIn {
   float q, t;
   __device__ __forceinline__ void load(const Norm<T>& n, const Back<T>& b, u64 row, u32 col) {
     row = row < n.rows ? row : n.rows - 1;
-    x = load_cols(n.x + row * n.ldx, col, n.cols);
-    if (MODE != kStream) f = load_cols(n.f + row * n.ldf, col, n.cols);
-    if (MODE == kFullGate) gate = load_cols(n.gate + row * n.ldg, col, n.cols);
+    x = n.ask(n.x + row * n.ldx, col);
+    if (MODE != kStream) f = n.ask(n.f + row * n.ldf, col);
+    if (MODE == kFullGate) gate = n.ask(n.gate + row * n.ldg, col);
     dh = dr = Vec8<T>{};
-    if (n.pre) dh = load_cols(b.dh + row * b.lddh, col, n.cols);
-    if (b.dr) dr = load_cols(b.dr + row * b.lddr, col, n.cols);
+    if (n.pre) dh = n.ask(b.dh + row * b.lddh, col);
+    if (b.dr) dr = n.ask(b.dr + row * b.lddr, col);
     q = b.rstd[row];
     t = b.rstd[n.rows + row];
   }
@@ -209,14 +219,19 @@ struct BackRow {
   float q, t;
 };
 template <int MODE, class T>
-__device__ __forceinline__ BackRow back_row(const BackIn<T, MODE>& in, const Eight& post, const Eight& by_cols, float scale) {
+__device__ __forceinline__ BackRow back_row(BackIn<T, MODE> in, const Norm<T>& n, u32 col, const Eight& post, const Eight& by_cols) {
   BackRow v;
+  n.have(in.x, col);
+  if (MODE != kStream) n.have(in.f, col);
+  if (MODE == kFullGate) n.have(in.gate, col);
+  n.have(in.dh, col);
+  n.have(in.dr, col);
   v.f = MODE == kStream ? Eight{} : floats(in.f);
   v.gate = MODE == kFullGate ? floats(in.gate) : by_cols;
   v.q = in.q;
   v.t = in.t;
   Eight p;
-  join_stream<MODE>(floats(in.x), v.f, post, v.gate, v.q, scale, p, v.unit);
+  join_stream<MODE>(floats(in.x), v.f, post, v.gate, v.q, n.scale, p, v.unit);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v.unit.v[j] *= v.t;
   v.dh = floats(in.dh);
@@ -293,7 +308,7 @@ __global__ __launch_bounds__(MOST, 4) void k_norm_back(Norm<T> n, Back<T> b, u32
   __syncthreads();
   for (u64 base = (u64)blockIdx.x * groups; base < n.rows; base += step, mine += step) {
     if (!kEarly) next.load(n, b, mine, col);
-    BackRow v = back_row(next, gain(0), MODE == kFullGate ? Eight{} : gain(2), n.scale);
+    BackRow v = back_row(next, n, col, gain(0), MODE == kFullGate ? Eight{} : gain(2));
     if (kEarly && base + step < n.rows) next.load(n, b, mine + step, col);
     if (n.pre) {
       const float mean = sum(stream_terms(v, gain(1))) * (float)n.per_col;
@@ -335,7 +350,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_means(Norm<T> n, Back<T> b,
       const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols);
       BackIn<T, MODE> in;
       in.load(n, b, row, col);
-      BackRow v = back_row(in, post, gains(n.gate_cols, col, n.cols), n.scale);
+      BackRow v = back_row(in, n, col, post, gains(n.gate_cols, col, n.cols));
       if (step == 0) return stream_terms(v, pre);
       if (n.pre) stream_grad(v, pre, first);
       return block_terms(v, post);
@@ -366,7 +381,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_long(Norm<T> n, Back<T> 
   for (u64 row = part; row < n.rows; row += blocks) {
     BackIn<T, MODE> in;
     in.load(n, b, row, col);
-    BackRow v = back_row(in, post, by_cols, n.scale);
+    BackRow v = back_row(in, n, col, post, by_cols);
     if (n.pre) stream_grad(v, pre, means[row]);
     back_store<T, MODE>(n, b, row, col, v, post, means[n.rows + row], s);
   }
@@ -483,14 +498,17 @@ int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, 
     const void* p;
     size_t ld;
   } in[3] = {{d_x, ldx}, {d_f, ldf}, {d_gate, ldg}}, out[2] = {{d_f ? d_r : nullptr, ldr}, {d_pre ? d_h : nullptr, ldh}};
+  bool apart = cols >= 8;
   for (const auto& o : out)
-    for (const auto& i : in)
+    for (const auto& i : in) {
       if (o.p && !in_place(i.p, i.ld, o.p, o.ld, rows)) return HAFLO_EINVAL;
+      apart = apart && !(o.p && o.p == i.p);
+    }
   if (out[0].p && out[0].p == out[1].p) return HAFLO_EINVAL;
   const hipStream_t st = (hipStream_t)stream;
   HAFLO_LOCAL_TYPES(type, {
     const Norm<T> n = {(const T*)d_x, (const T*)d_f, (const T*)d_gate, ldx, ldf, ldg, d_gate_cols, d_post, d_pre, (u32)rows, (u32)cols, (float)scale,
-                       eps, 1.0 / (double)cols};
+                       eps, 1.0 / (double)cols, apart};
     if (!d_f) norm<T, kStream>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
     else if (d_gate) norm<T, kFullGate>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
     else norm<T, kGated>(n, (T*)d_r, ldr, (T*)d_h, ldh, d_rstd, st);
@@ -518,9 +536,12 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
     const void* p;
     size_t ld;
   } in[5] = {{d_x, ldx}, {d_f, ldf}, {d_gate, ldg}, {d_pre ? d_dh : nullptr, lddh}, {d_dr, lddr}}, out[3] = {{d_dx, lddx}, {d_df, lddf}, {d_dgate, lddg}};
+  bool apart = cols >= 8;
   for (int o = 0; o < 3; ++o) {
-    for (const auto& i : in)
+    for (const auto& i : in) {
       if (out[o].p && !in_place(i.p, i.ld, out[o].p, out[o].ld, rows)) return HAFLO_EINVAL;
+      apart = apart && !(out[o].p && out[o].p == i.p);
+    }
     if (out[o].p && (out[o].p == out[(o + 1) % 3].p)) return HAFLO_EINVAL;
   }
   const Plan plan = back_plan(rows, cols);
@@ -529,7 +550,7 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
   const hipStream_t st = (hipStream_t)stream;
   if (rows) HAFLO_LOCAL_TYPES(type, {
     const Norm<T> n = {(const T*)d_x, (const T*)d_f, (const T*)d_gate, ldx, ldf, ldg, d_gate_cols, d_post, d_pre, (u32)rows, (u32)cols, (float)scale,
-                       0.0, 1.0 / (double)cols};
+                       0.0, 1.0 / (double)cols, apart};
     const Back<T> b = {(const T*)d_dh, (const T*)d_dr, lddh, lddr, d_rstd, (T*)d_dx, (T*)d_df, (T*)d_dgate, lddx, lddf, lddg, (float*)ws, (u32)plan.width};
     if (!d_f) norm_back<T, kStream>(n, b, plan, ws, st);
     else if (d_gate) norm_back<T, kFullGate>(n, b, plan, ws, st);
