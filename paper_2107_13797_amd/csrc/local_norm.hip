@@ -373,8 +373,8 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_means(Norm<T> n, Back<T> b,
 }
 // Long rows with their means: a block takes eight columns a lane of every `blocks`-th row.
 template <class T, int MODE>
-__global__ __launch_bounds__(kThreads) void k_norm_back_long(Norm<T> n, Back<T> b, const float* means, u32 blocks) {
-  const u32 part = blockIdx.x % blocks, col = blockIdx.x / blocks * kTileCols + threadIdx.x * 8;
+__global__ __launch_bounds__(kThreads) void k_norm_back_long(Norm<T> n, Back<T> b, const float* means, u32 blocks, u32 first_block) {
+  const u32 block = first_block + blockIdx.x, part = block % blocks, col = block / blocks * kTileCols + threadIdx.x * 8;
   if (col >= n.cols) return;
   const Eight post = gains(n.post, col, n.cols), pre = gains(n.pre, col, n.cols), by_cols = gains(n.gate_cols, col, n.cols);
   Sums s = {};
@@ -396,10 +396,10 @@ struct Joined {
   float *post, *gate, *pre;
   const float *of_post, *of_gate;  // what the first sum is multiplied by for them, or NULL
 };
-__global__ __launch_bounds__(kJoinWaves * kWave) void k_norm_join(const float* sums, u32 blocks, u32 width, u32 cols, Joined to) {
+__global__ __launch_bounds__(kJoinWaves * kWave) void k_norm_join(const float* sums, u32 blocks, u32 width, u32 cols, Joined to, u32 first_block) {
   __shared__ float parts[kJoinWaves][kWave];
-  const u32 tiles = (cols + kWave - 1) / kWave, which = blockIdx.x / tiles, lane = lane_id(), wave = threadIdx.x / kWave;
-  const u32 col = blockIdx.x % tiles * kWave + lane;
+  const u32 tiles = (cols + kWave - 1) / kWave, block = first_block + blockIdx.x, which = block / tiles, lane = lane_id(), wave = threadIdx.x / kWave;
+  const u32 col = block % tiles * kWave + lane;
   if (which == 0 ? !to.post && !to.gate : !to.pre) return;
   const u32 first = (u32)((u64)blocks * wave / kJoinWaves), end = (u32)((u64)blocks * (wave + 1) / kJoinWaves);
   const float* const from = sums + (size_t)which * blocks * width + (col < cols ? col : cols - 1);
@@ -472,8 +472,9 @@ void norm_back(const Norm<T>& n, const Back<T>& b, const Plan& plan, char* ws, h
   if (n.cols > kRowCols) {
     float* const means = (float*)(ws + plan.means);
     hipLaunchKernelGGL((k_norm_means<T, MODE>), dim3((unsigned)(n.rows < kNormBlocks ? n.rows : kNormBlocks)), dim3(kMostLanes), 0, st, n, b, means);
-    hipLaunchKernelGGL((k_norm_back_long<T, MODE>), dim3((unsigned)(plan.blocks * ceil_div(n.cols, kTileCols))), dim3(kThreads), 0, st, n, b,
-                       (const float*)means, (u32)plan.blocks);
+    in_turns(plan.blocks * ceil_div(n.cols, kTileCols), kThreads, [&](u32 first, dim3 grid, dim3 block) {
+      hipLaunchKernelGGL((k_norm_back_long<T, MODE>), grid, block, 0, st, n, b, (const float*)means, (u32)plan.blocks, first);
+    });
     return;
   }
   const u32 lanes = lanes_of(n.cols), threads = threads_of(lanes, n.rows);
@@ -490,8 +491,8 @@ int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, 
                         const float* d_gate_cols, const float* d_pre, size_t rows, size_t cols, double scale, double eps, void* d_r, size_t ldr,
                         void* d_h, size_t ldh, float* d_rstd, void* stream) {
   if (!norm_sizes(type, rows, cols) || !(eps > 0.0 && eps < HUGE_VAL) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
-  if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
   if (rows == 0) return HAFLO_OK;
+  if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
   if (!d_x || ldx < cols || (d_f && (ldf < cols || !d_r || ldr < cols)) || (d_gate && ldg < cols) || (d_pre && (!d_h || ldh < cols)) || !d_rstd)
     return HAFLO_EINVAL;
   const struct {
@@ -526,9 +527,10 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
                                  void* d_dgate, size_t lddg, float* d_dgate_cols, float* d_dpost, float* d_dpre, void* d_workspace,
                                  size_t workspace_bytes, void* stream) {
   if (!norm_sizes(type, rows, cols) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
-  if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
-  // a gradient of what is not there
-  if ((d_dpost && !d_post) || (d_dpre && !d_pre) || (d_dgate_cols && !d_gate_cols) || (d_dgate && !d_gate) || (d_df && !d_f)) return HAFLO_EINVAL;
+  if ((d_dpost && !d_post) || (d_dpre && !d_pre) || (d_dgate_cols && !d_gate_cols)) return HAFLO_EINVAL;  // gradients of what is not there
+  // (matrices of no rows may have no address)
+  if (rows && ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols) || (d_dgate && !d_gate) || (d_df && !d_f)))
+    return HAFLO_EINVAL;
   if (rows && (!d_x || ldx < cols || (d_f && ldf < cols) || (d_gate && ldg < cols) || (d_pre && (!d_dh || lddh < cols)) || (d_dr && lddr < cols) || !d_rstd ||
                (d_dx && lddx < cols) || (d_df && lddf < cols) || (d_dgate && lddg < cols)))
     return HAFLO_EINVAL;
@@ -557,8 +559,10 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
     else norm_back<T, kGated>(n, b, plan, ws, st);
   });
   if (d_dpost || d_dgate_cols || d_dpre)
-    hipLaunchKernelGGL(k_norm_join, dim3((unsigned)(2 * ceil_div(cols, kWave))), dim3(kJoinWaves * kWave), 0, st, (const float*)ws, (u32)plan.blocks, (u32)plan.width,
-                       (u32)cols, Joined{d_dpost, d_dgate_cols, d_dpre, d_gate_cols, d_post});
+    in_turns(2 * ceil_div(cols, kWave), kJoinWaves * kWave, [&](u32 first, dim3 grid, dim3 block) {
+      hipLaunchKernelGGL(k_norm_join, grid, block, 0, st, (const float*)ws, (u32)(rows ? plan.blocks : 0), (u32)plan.width, (u32)cols,
+                         Joined{d_dpost, d_dgate_cols, d_dpre, rows ? d_gate_cols : nullptr, rows ? d_post : nullptr}, first);
+    });
   return launched();
 }
 

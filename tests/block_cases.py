@@ -322,3 +322,28 @@ def check_int8_limits(run):
     got = run.int8_forward(x, wq, ws, None, None)
     want = torch.tensor([[1.0, 0.0], [-1.0, 0.0]], dtype=torch.float64) * cols
     near(got, want, 5 * ULP * want.abs())
+
+
+# --------------------------------------------------------------------------------------------------- each kernel form
+
+def norm_forms(kind):
+    """Every group size, with and without a vector across the row's end, by mode: rows that fill no block and rows that fill several."""
+    for n, cols in enumerate((3, 8, 30, 64, 130, 512, 777, 1500, 2048, 3001, 4096, 5003, 8192, 8193, 9000)):
+        for block, post, gate, pre in ((True, True, "cols", True), (True, True, "full", True), (False, False, "none", True), (True, n % 2 == 0, "none", n % 3 == 0)):
+            yield (kind, 5 if n % 2 else 19, cols, n % 2, n % 3, block, post, gate, pre, 1.0 if not block else 0.75)
+
+
+def update_forms(kind, tall):
+    """Every number of tiles, filled and not, with loads of whole and of single elements, by one launch and by several."""
+    for k in (1, 5, 16, 17, 24, 32, 33, 36, 48, 50, 64, 65, 100, 128):
+        for length in ((k, 70, 800, 1100) if k <= 16 else (k, 140, 300)):
+            if length >= k:
+                rows, cols = (length, k) if tall else (k, length)
+                yield (kind, 2 if k % 2 else 9, rows, cols, k % 3 == 0, [QUINTIC] * (1 + k % 3), k % 2)
+
+
+def int8_forms(kind):
+    """Rows that a block brings to eight bits itself, few rows, and tiles of three sizes."""
+    for rows, inner, outer in ((1, 2048, 40), (2, 100, 17), (3, 4096, 33), (4, 8192, 20), (4, 8200, 20), (5, 2048, 40), (16, 2049, 4096), (17, 2048, 30), (32, 4100, 9),
+                               (33, 2048, 30), (32, 2048, 4097), (8, 1900, 50), (70, 40, 70), (2050, 130, 2050), (4100, 200, 4100), (4097, 3000, 4097)):
+        yield (kind, rows, inner, outer, 0, rows % 2 == 0, rows % 3 == 0)

@@ -91,3 +91,208 @@ def test_int8(run, case):
 
 def test_int8_limits(run):
     cases.check_int8_limits(run)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_norm_forms(run, kind):
+    for case in cases.norm_forms(kind):
+        print(case, flush=True)
+        cases.check_norm(run, *case)
+
+
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_update_forms(run, kind, tall):
+    for case in cases.update_forms(kind, tall):
+        print(case, flush=True)
+        cases.check_update(run, *case)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_int8_forms(run, kind):
+    for case in cases.int8_forms(kind):
+        print(case, flush=True)
+        cases.check_int8(run, *case)
+
+
+def step(api, t):
+    """A block as a party trains it and the common model answers with it: norm, projection with adapters, norm with gate and residual, head,
+    log-probabilities of the labels, the gradients back to all that is trained, the adapters' updates, and the answer in eight bits."""
+    one = torch.ones_like(t["scale"])
+    _, h0, t0 = api.haflo_residual_norm(t["x"], pre=t["pre0"])
+    f, z = api.haflo_adapter_forward(h0, t["w"], t["a"], t["b"], t["scale"], t["index"], 0.1, 7, 1)
+    r, h1, t1 = api.haflo_residual_norm(t["x"], f, t["post"], t["gate"], t["pre1"], 0.9)
+    logits, z2 = api.haflo_adapter_forward(h1, t["head"], t["a2"], t["b2"], one, t["index"])
+    logp, entropy, lse, _, _ = api.haflo_label_logprobs(logits, t["label"])
+    dlogits = api.haflo_label_logprobs_backward(logits, t["label"], lse, entropy, t["minus"])
+    dh1, da2, db2 = api.haflo_adapter_backward(dlogits, h1, t["head"], t["a2"], t["b2"], one, t["index"], z2)
+    dx1, df, dpost, dgate, dpre1 = api.haflo_residual_norm_backward(dh1, None, t["x"], f, t["post"], t["gate"], t["pre1"], t1, 0.9)
+    dh0, da, db = api.haflo_adapter_backward(df, h0, t["w"], t["a"], t["b"], t["scale"], t["index"], z, 0.1, 7, 1)
+    dx, _, _, _, dpre0 = api.haflo_residual_norm_backward(dh0, dx1, t["x"], None, None, None, t["pre0"], t0)
+    ups = [api.haflo_orthogonal_update(g, v, 0.99, -0.02) for g, v in ((da, t["a32"]), (db, t["b32"]), (da2, t["a32"]), (db2, t["b2_32"]))]
+    q, s = api.haflo_quantize_rows(t["w"])
+    answer = api.haflo_int8_forward(h0, q, s, bias=t["pre0"], residual=t["x"])
+    one_row = api.haflo_int8_forward(h0[:1], q, s)
+    return [r, h1, logp, dx, dpost, dgate, dpre1, dpre0, *ups, answer, one_row]
+
+
+def step_inputs(rows=200, width=136, labels=72, rank=4, parties=3):
+    g = torch.Generator().manual_seed(4)
+    n = lambda *s: torch.randn(*s, generator=g).cuda()  # noqa: E731
+    bf = torch.bfloat16
+    t = dict(x=n(rows, width).to(bf), w=(n(width, width) * width ** -0.5).to(bf), head=(n(labels, width) * width ** -0.5).to(bf), a32=n(parties, rank, width),
+             b32=n(parties, width, rank), b2_32=n(parties, labels, rank), scale=torch.rand(parties, generator=g).cuda() + 0.5,
+             index=(torch.arange(rows) % (parties + 1) - 1).to(torch.int32).cuda(), label=(torch.arange(rows) % labels).to(torch.int32).cuda(),
+             minus=torch.full((rows,), -1.0 / rows, device="cuda"))
+    t.update(a=t["a32"].to(bf), b=t["b32"].to(bf), a2=t["a32"].to(bf), b2=t["b2_32"].to(bf))
+    t.update({k: 1.0 + 0.1 * n(width) for k in ("pre0", "post", "gate", "pre1")})
+    return t
+
+
+def test_same_bits_again(api):
+    """No result depends on timing, nor on what else the card does."""
+    t, other = step_inputs(), torch.cuda.Stream()
+    want = [v.clone() for v in step(api, t)]
+    busy = torch.randn(2048, 2048, device="cuda")
+    for _ in range(3):
+        with torch.cuda.stream(other):
+            for _ in range(4):
+                busy = busy @ busy * 1e-3
+        got = step(api, t)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+
+
+def test_side_stream_and_graph(api):
+    """A step captured on a side stream, twice, and replayed on new contents of the same buffers gives what the eager calls give."""
+    t, side = step_inputs(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(api, t)
+    side.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step(api, t)
+        graphs.append((graph, out))
+    for k in range(3):
+        t["x"].copy_(torch.randn(t["x"].shape, generator=torch.Generator().manual_seed(k)).to(t["x"].dtype))
+        torch.cuda.synchronize()
+        want = [v.clone() for v in step(api, t)]
+        torch.cuda.synchronize()
+        for graph, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_two_streams(api):
+    """Calls on two streams at once."""
+    first, second = step_inputs(), step_inputs(rows=333, width=264, rank=16)
+    want = [[v.clone() for v in step(api, t)] for t in (first, second)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = []
+        for t, s in zip((first, second), streams):
+            with torch.cuda.stream(s):
+                got.append(step(api, t))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+
+
+def test_in_place_and_slices(api):
+    """Results over operands, and into rows of a wider array, whose other elements stay as they are."""
+    for rows, cols in ((70, 1001), (300, 4096), (5, 7), (9, 9001)):
+        g = torch.Generator().manual_seed(cols)
+        wide = lambda: torch.randn(rows, cols + 9, generator=g).to(torch.float16).cuda()  # noqa: E731
+        x, f, gate = wide(), wide(), wide()
+        post, pre = torch.rand(cols, generator=g).cuda() + 0.5, torch.rand(cols, generator=g).cuda() + 0.5
+        at = slice(1, cols + 1)
+        r, h, _ = api.haflo_residual_norm(x[:, at], f[:, at], post, gate[:, at], pre, 0.5)
+        to, to_h = torch.full_like(x, 3.0), torch.full_like(x, 4.0)
+        got = api.haflo_residual_norm(x[:, at], f[:, at], post, gate[:, at], pre, 0.5, out=to[:, at], normed=to_h[:, at])
+        assert torch.equal(got[0], r) and torch.equal(to[:, at], r) and torch.equal(to_h[:, at], h)
+        assert bool((to[:, 0] == 3).all()) and bool((to[:, cols + 1:] == 3).all()) and bool((to_h[:, cols + 1:] == 4).all())
+        last = f[:, cols + 1:].clone()
+        api.haflo_residual_norm(x[:, at], f[:, at], post, gate[:, at], pre, 0.5, out=x[:, at], normed=f[:, at])
+        assert torch.equal(x[:, at], r) and torch.equal(f[:, at], h) and torch.equal(f[:, cols + 1:], last)
+    for shape in ((3, 16, 900), (3, 900, 40), (2, 70, 333), (2, 333, 128)):
+        g, base = torch.randn(shape, device="cuda"), torch.randn(shape, device="cuda")
+        want = api.haflo_orthogonal_update(g, base, 0.9, -0.1)
+        wide = torch.full((shape[0], shape[1] + 2, shape[2] + 5), 7.0, device="cuda")
+        api.haflo_orthogonal_update(g, base, 0.9, -0.1, out=wide[:, 1:-1, 2:-3])
+        assert torch.equal(wide[:, 1:-1, 2:-3], want) and int((wide != 7).sum()) <= want.numel()
+        assert torch.equal(api.haflo_orthogonal_update(g, base.clone(), 0.9, -0.1, out=g.clone()), want)
+        assert torch.equal(api.haflo_orthogonal_update(g, base, 0.9, -0.1, out=base), want)
+        assert torch.equal(api.haflo_orthogonal_update(g[:1].expand(2, -1, -1))[1], api.haflo_orthogonal_update(g[:1])[0])
+    for rows in (1, 20, 300):
+        x, w = torch.randn(rows, 300, device="cuda").bfloat16(), torch.randn(45, 300, device="cuda").bfloat16()
+        q, s = api.haflo_quantize_rows(w)
+        res = torch.randn(rows, 60, device="cuda").bfloat16()
+        want = api.haflo_int8_forward(x, q, s, residual=res[:, 3:48])
+        keep = res.clone()
+        api.haflo_int8_forward(x, q, s, residual=res[:, 3:48], out=res[:, 3:48])
+        assert torch.equal(res[:, 3:48], want) and torch.equal(res[:, :3], keep[:, :3]) and torch.equal(res[:, 48:], keep[:, 48:])
+
+
+def test_far_offsets(api):
+    """Elements past 2^31 and bytes past 2^32 in one array: the last rows are what they are by themselves."""
+    rows, cols = 70001, 32768
+    x = torch.empty((rows, cols), dtype=torch.float16, device="cuda").fill_(0.5)
+    x[-3:] = torch.randn(3, cols, device="cuda").half()
+    pre = torch.ones(cols, device="cuda")
+    _, h, rstd = api.haflo_residual_norm(x, pre=pre)
+    _, own, own_rstd = api.haflo_residual_norm(x[-3:].clone(), pre=pre)
+    assert torch.equal(h[-3:], own) and torch.equal(rstd[:, -3:], own_rstd)
+    dx, _, _, _, _ = api.haflo_residual_norm_backward(x, None, x, None, None, None, pre, rstd)
+    assert torch.equal(dx[-3:], api.haflo_residual_norm_backward(x[-3:].clone(), None, x[-3:].clone(), None, None, None, pre, own_rstd)[0])
+    del h, dx
+    w = torch.randn(40, cols, device="cuda").half()
+    q, s = api.haflo_quantize_rows(w)
+    x = torch.cat([x, x])  # rows of eight bits past 4 GiB
+    y = api.haflo_int8_forward(x, q, s)
+    assert torch.equal(y[-3:], api.haflo_int8_forward(x[-3:].clone(), q, s))
+    del x
+    g = torch.empty((40, 100000, 600), dtype=torch.bfloat16, device="cuda").fill_(1.0)[:, :, :64]
+    g[-1] = torch.randn(100000, 64, device="cuda").bfloat16()
+    assert torch.equal(api.haflo_orthogonal_update(g)[-1], api.haflo_orthogonal_update(g[-1:].clone())[0])
+
+
+def test_refusals(api):
+    f32, i8 = torch.float32, torch.int8
+    z = lambda *s, kind=f32: torch.zeros(*s, dtype=kind, device="cuda")  # noqa: E731
+    x, v, s = z(4, 8), z(8), z(2, 4)
+    norm, back, update, quant, fwd, prod = (api.haflo_residual_norm, api.haflo_residual_norm_backward, api.haflo_orthogonal_update, api.haflo_quantize_rows,
+                                            api.haflo_int8_forward, api.haflo_int8_product)
+    q, ws = quant(z(6, 8))
+    bad = [
+        lambda: norm(x.double(), pre=v), lambda: norm(x), lambda: norm(x, x[:3], pre=v), lambda: norm(x, x.half(), pre=v), lambda: norm(x, x, v[:7]), lambda: norm(x, x, v.half()),
+        lambda: norm(x, x, v, x[:, :7]), lambda: norm(x, x, v, x.half()), lambda: norm(x, x, v, v.half()), lambda: norm(x, pre=v, scale=0.5), lambda: norm(x, None, v, None, v),
+        lambda: norm(x, None, None, v, v), lambda: norm(x, x, v, None, v, eps=0.0), lambda: norm(x, x, v, None, v, float("nan")), lambda: norm(x.cpu(), pre=v),
+        lambda: norm(x.t(), pre=z(4)), lambda: norm(x, x, v, None, v, out=x.half()), lambda: norm(x, x, v, None, v, out=x, normed=x), lambda: norm(x[:, :0], pre=v[:0]),
+        lambda: norm(x[0], pre=v), lambda: norm(x, x, v.expand(2, 8)[0:1], None, v),
+        lambda: back(None, x, x, x, v, None, v, s), lambda: back(x, x, x, x, v, None, None, s), lambda: back(x, x[:3], x, x, v, None, v, s), lambda: back(x, x, x, x, v, None, v, s[:, :3]),
+        lambda: back(x.half(), x, x, x, v, None, v, s), lambda: back(x, x, x, x, v, None, v, s.double()), lambda: back(x, x, x, None, v, None, v, s),
+        lambda: update(z(4, 8)), lambda: update(z(2, 200, 300)), lambda: update(z(2, 4, 8, kind=torch.int32)), lambda: update(z(2, 4, 8), z(2, 4, 7)), lambda: update(z(2, 4, 8), z(2, 4, 8).half()),
+        lambda: update(z(2, 4, 8), coefficients=[]), lambda: update(z(2, 4, 8), coefficients=[(1.0, 2.0)]), lambda: update(z(2, 4, 8), coefficients=[(1.0, 0.0, 0.0)] * 17),
+        lambda: update(z(2, 4, 8), eps=0.0), lambda: update(z(2, 4, 8), scale=float("inf")), lambda: update(z(2, 8, 4).transpose(1, 2)), lambda: update(z(2, 4, 8), out=z(1, 4, 8).expand(2, 4, 8)),
+        lambda: update(z(2, 0, 8)), lambda: update(z(2, 4, 8).cpu()),
+        lambda: quant(z(4, 8, kind=i8)), lambda: quant(z(4, 8).t()), lambda: quant(z(4, 0)), lambda: quant(z(2, 130945)), lambda: quant(v),
+        lambda: fwd(x, q[:, :64], ws), lambda: fwd(x, q, ws[:5]), lambda: fwd(x, q.float(), ws), lambda: fwd(z(4, 129), q, ws), lambda: fwd(x, q, ws, bias=z(5)), lambda: fwd(x, q, ws, residual=z(4, 5)),
+        lambda: fwd(x, q, ws, residual=z(4, 6).half()), lambda: fwd(x, q, ws, out=z(4, 6).half()), lambda: fwd(x, q[0], ws), lambda: fwd(x, z(6, 136, kind=i8)[:, 8:], ws),
+        lambda: fwd(x, z(6 * 128 + 8, kind=i8)[8:].view(6, 128), ws), lambda: fwd(x.double(), q, ws),
+        lambda: prod(q, ws, q, ws, 129), lambda: prod(q, ws[:3], q, ws, 8), lambda: prod(q, ws, q, ws, 8, torch.float64), lambda: prod(q[0], ws, q, ws, 8),
+    ]
+    for n, call in enumerate(bad):
+        with pytest.raises(api.HafloError):
+            call()
+            pytest.fail("call %d was not refused" % n)
+    # nothing to do is no error
+    r, h, t = norm(x[:0], x[:0], v, None, v)
+    assert r.shape == h.shape == (0, 8) and t.shape == (2, 0)
+    dx, df, dpost, dgate, dpre = back(x[:0], None, x[:0], x[:0], v + 1, v + float("inf"), v + 1, t)
+    assert dx.shape == df.shape == (0, 8) and not dpost.any() and not dgate.any() and not dpre.any() and dpost.shape == (8,)
+    assert update(z(0, 4, 8)).shape == (0, 4, 8) and quant(x[:0])[0].shape == (0, 128) and fwd(x[:0], q, ws).shape == (0, 6)
