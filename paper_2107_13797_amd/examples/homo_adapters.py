@@ -69,6 +69,25 @@ def step(api, shared, adapters, x, label, index, weight, rate, p, seed, offset):
     return logp
 
 
+def aggregate(api, pub, own, flat, counts, rng, timed):
+    """The decoded sum over parties of counts[k] flat[k], through ciphertexts: as whole numbers and as float64."""
+    total, lp = None, pub.plain_limbs
+    for k in range(len(flat)):
+        r = rng.integers(0, 2 ** 32, size=(flat[k].numel(), lp), dtype=np.uint32)
+        r[:, -1] &= 0x7FFFFFFF
+        r = torch.from_numpy(r.view(np.int32)).cuda()
+        c = timed("parties: encode + encrypt", lambda: api.haflo_encrypt(own, api.haflo_encode_f32(own, flat[k], SCALE_W), r))
+        scaled = timed("coordinator: scalar_mul by n_k", lambda: api.haflo_scalar_mul_i64_bcast(pub, c, counts[k]))
+        total = scaled if total is None else timed("coordinator: add", lambda: api.haflo_add(pub, total, scaled))
+    return timed("party: decrypt + decode", lambda: api.haflo_decode(own, api.haflo_decrypt(own, total), SCALE_W))
+
+
+def exact_sum(flat, counts):
+    """The same sum in exact integers on the quantised weights."""
+    q = [np.rint(f.cpu().numpy().astype(np.float64) * 2.0 ** SCALE_W).astype(np.int64) for f in flat]
+    return sum(n * qk for n, qk in zip(counts, q)).tolist()
+
+
 def run_round(api, pub, own, parties, rows, width, labels, rank, steps, seed=0, rate=0.1, p=0.05, timings=None):
     """pub: public context (the coordinator), own: private context (the parties). Every party has between half of `rows` and
     `rows` rows."""
@@ -109,16 +128,8 @@ def run_round(api, pub, own, parties, rows, width, labels, rank, steps, seed=0, 
         timed("parties: local steps", lambda: step(api, shared, adapters, x, label, index, weight, rate, p, seed, 3 * n))
     local = loss(adapters, index)
 
-    total, lp = None, pub.plain_limbs
     flat = [adapters.flat(k) for k in range(parties)]
-    for k in range(parties):
-        r = rng.integers(0, 2 ** 32, size=(flat[k].numel(), lp), dtype=np.uint32)
-        r[:, -1] &= 0x7FFFFFFF
-        r = torch.from_numpy(r.view(np.int32)).cuda()
-        c = timed("parties: encode + encrypt", lambda: api.haflo_encrypt(own, api.haflo_encode_f32(own, flat[k], SCALE_W), r))
-        scaled = timed("coordinator: scalar_mul by n_k", lambda: api.haflo_scalar_mul_i64_bcast(pub, c, counts[k]))
-        total = scaled if total is None else timed("coordinator: add", lambda: api.haflo_add(pub, total, scaled))
-    sum_q, summed = timed("party: decrypt + decode", lambda: api.haflo_decode(own, api.haflo_decrypt(own, total), SCALE_W))
+    sum_q, summed = aggregate(api, pub, own, flat, counts, rng, timed)
 
     common = Adapters.of_flat((summed / sum(counts)).to(torch.float32), width, labels, rank)
     after = loss(common, torch.zeros_like(index))
@@ -129,10 +140,9 @@ def run_round(api, pub, own, parties, rows, width, labels, rank, steps, seed=0, 
         return api.haflo_label_logprobs(logits, none, top=5)
 
     _, _, _, top_logp, top_index = timed("party: one row's answer", answer)
-    q = [np.rint(f.cpu().numpy().astype(np.float64) * 2.0 ** SCALE_W).astype(np.int64) for f in flat]
     return {
         "sum_q": sum_q.tolist(),
-        "want_sum_q": sum(n * qk for n, qk in zip(counts, q)).tolist(),
+        "want_sum_q": exact_sum(flat, counts),
         "loss": {"before": before, "local": local, "common": after},
         "answer": list(zip(top_index[0].tolist(), top_logp[0].tolist())),
         "label": int(label[0]),

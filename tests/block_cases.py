@@ -137,10 +137,10 @@ def check_norm_special(run):
 
 
 def check_norm_gradients(run):
-    """Against differences of the forward call along random directions, in float32; the third derivative and the results' roundings
-    bound how far the quotient is off."""
+    """Against differences of the forward call along each gradient, in float32; the third derivative and the results' roundings bound how
+    far the quotient is off."""
     x, f, post, gate, pre, dh, dr = norm_inputs("f32", 5, 48, 0, 0, True, True, "full", True, seed=3)
-    args, gen, step = [x, f, post, gate, pre], torch.Generator().manual_seed(9), 2.0 ** -7
+    args, step = [x, f, post, gate, pre], 2.0 ** -7
     _, _, rstd = run.residual_norm(*args, 0.8, 1e-5)
     dx, df, dpost, dgate, dpre = run.residual_norm_backward(dh, dr, *args, rstd, 0.8)
 
@@ -150,11 +150,12 @@ def check_norm_gradients(run):
 
     weight = float(dr.abs().sum() + dh.abs().sum())
     for i, grad in enumerate((dx, df, dpost, dgate, dpre)):
-        d = torch.randn(args[i].shape, generator=gen)
+        d = grad / grad.norm()
         plus, minus = ([v + s * step * d if j == i else v for j, v in enumerate(args)] for s in (1.0, -1.0))
         got, want = float((grad.double() * d).sum()), (value(plus) - value(minus)) / (2 * step)
         # results are below 16, their third derivatives along d below 64 max|d|^3
-        assert abs(got - want) <= weight * (step ** 2 * 64 * float(d.abs().max()) ** 3 / 6 + 16 * 2.0 ** -22 / step)
+        room = weight * (step ** 2 * 64 * float(d.abs().max()) ** 3 / 6 + 16 * 2.0 ** -22 / step)
+        assert abs(got - want) <= room < 0.1 * got
 
 
 # --------------------------------------------------------------------------------------------------- orthogonalised updates

@@ -296,3 +296,44 @@ def test_refusals(api):
     dx, df, dpost, dgate, dpre = back(x[:0], None, x[:0], x[:0], v + 1, v + float("inf"), v + 1, t)
     assert dx.shape == df.shape == (0, 8) and not dpost.any() and not dgate.any() and not dpre.any() and dpost.shape == (8,)
     assert update(z(0, 4, 8)).shape == (0, 4, 8) and quant(x[:0])[0].shape == (0, 128) and fwd(x[:0], q, ws).shape == (0, 6)
+
+
+def test_homo_blocks_round(api):
+    """A round runs: the decoded sum is the exact integer sum of the quantised weights, results are finite, the answer's labels stand in order."""
+    from paper_2107_13797_amd.examples import homo_blocks
+    p, q = api.haflo_keygen(1024, 11)
+    own, pub = api.haflo_ctx_create_private(p, q, 1024), api.haflo_ctx_create_public(p * q, 1024)
+    res = homo_blocks.run_round(api, pub, own, parties=3, rows=100, width=72, labels=10, rank=4, steps=3, seed=3)
+    own.close()
+    pub.close()
+    assert res["weights"] == 4 * (72 + 72 + 72 + 10) and res["sum_q"] == res["want_sum_q"]
+    assert all(0 < v < 100 for v in res["loss"].values())
+    logps = [v for _, v in res["answer"]]
+    assert len(set(i for i, _ in res["answer"])) == 5 and logps == sorted(logps, reverse=True) and max(logps) < 0
+
+
+def test_homo_blocks_gradients(api):
+    """The example's gradients against differences of its losses, in float32."""
+    from paper_2107_13797_amd.examples import homo_blocks as ex
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    normal = lambda *s, by=1.0: torch.randn(s, generator=gen, device="cuda") * by  # noqa: E731
+    parties, rows, width, labels, rank, step = 2, 12, 24, 7, 3, 2.0 ** -8
+    block = ex.Block(normal, width, labels, torch.float32)
+    values = [normal(parties, rank, width, by=0.2), normal(parties, width, rank, by=0.2), normal(parties, rank, width, by=0.2), normal(parties, labels, rank, by=0.2)]
+    adapters = ex.Adapters(parties, width, labels, rank, values)
+    x, label = normal(rows, width), (torch.arange(rows, device="cuda") % labels).to(torch.int32)
+    index, weight = (torch.arange(rows, device="cuda") % (parties + 1) - 1).to(torch.int32), torch.full((rows,), 1.0 / rows, device="cuda")
+    _, grads = ex.gradients(api, block, adapters, x, label, index, weight)
+
+    def value(v):
+        logits, _ = ex.forward(api, block, ex.Adapters(parties, width, labels, rank, v), x, index)
+        return float(-(api.haflo_label_logprobs(logits, label)[0].double() * weight).sum())
+
+    for i, g in enumerate(grads):
+        d = g / g.norm()
+        plus, minus = ([v + s * step * d if j == i else v for j, v in enumerate(values)] for s in (1.0, -1.0))
+        got, want = float((g.double() * d).sum()), (value(plus) - value(minus)) / (2 * step)
+        # along a direction of length 1 scaled by 2 the logits change by at most 2 * 6 (a norm's length is below 6) a unit, and their loss's third
+        # derivative is below that cubed; the losses' own roundings are below 2^-19
+        room = step ** 2 / 6 * 12.0 ** 3 / 8 + 2.0 ** -19 / step
+        assert abs(got - want) <= room < 0.1 * got
