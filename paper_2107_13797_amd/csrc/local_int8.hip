@@ -100,25 +100,54 @@ struct Out {
   size_t ldy;
   u32 rows, outer;
 };
-// four outputs from `o` on of row t, which there is
-template <class T>
-__device__ __forceinline__ void store_four(const Out<T>& to, u32 t, u32 o, const i32x4& acc, float x_scale) {
-  float v[4];
-  T* const y = to.y + t * to.ldy + o;
-  const T* const res = to.residual ? to.residual + t * to.ldr + o : nullptr;
-  if (o + 4 <= to.outer) {
-    float ws[4], bias[4] = {};
-    T was[4] = {}, now[4];
-    __builtin_memcpy(ws, to.w_scale + o, sizeof(ws));
-    if (to.bias) __builtin_memcpy(bias, to.bias + o, sizeof(bias));
-    if (res) __builtin_memcpy(was, res, sizeof(was));
+// A wavefront's results, RT x OT products of 16 x 16 from row t0 and output o0 on, by way of LDS, 32 rows at a time, so that lanes store, and
+// load the residual, along rows: of a short reduction the results are most of the work (16384 rows of 128 to 4096, float16, 60 us by four
+// outputs of sixteen rows at a time and 44 by rows; 8192 of 4096 to 4096 147 and 124).
+template <int RT, int OT>
+constexpr u32 out_floats() {  // of one wavefront
+  return (RT < 2 ? 16 : 32) * (16 * OT + 4);
+}
+template <class T, int RT, int OT>
+__device__ __forceinline__ void store_results(const Out<T>& to, u32 t0, u32 o0, const i32x4 (&acc)[OT][RT], float* room) {
+  constexpr u32 ROWS = RT < 2 ? 16 : 32, WIDTH = 16 * OT, LD = WIDTH + 4, PER = WIDTH / 8;
+  const u32 lane = lane_id();
+  f32x4 ws[OT], bias[OT];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) now[r] = (T)((float)acc[r] * (x_scale * ws[r]) + bias[r] + (float)was[r]);
-    __builtin_memcpy(y, now, sizeof(now));
-  } else {
+  for (int i = 0; i < OT; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (o + r < to.outer) y[r] = (T)((float)acc[r] * (x_scale * to.w_scale[o + r]) + (to.bias ? to.bias[o + r] : 0.0f) + (res ? (float)res[r] : 0.0f));
+    for (u32 r = 0; r < 4; ++r) {
+      const u32 o = o0 + 16 * i + lane / 16 * 4 + r, at = o < to.outer ? o : to.outer - 1;
+      ws[i][r] = to.w_scale[at];
+      bias[i][r] = to.bias ? to.bias[at] : 0.0f;
+    }
+#pragma unroll
+  for (int j0 = 0; j0 < RT; j0 += ROWS / 16) {
+    if (j0) __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (u32 j = 0; j < ROWS / 16; ++j) {
+      const u32 t = t0 + 16 * (j0 + j) + lane % 16;
+      const float by = to.x_scale[t < to.rows ? t : to.rows - 1];
+#pragma unroll
+      for (int i = 0; i < OT; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j0 + j][r] * (by * ws[i][r]) + bias[i][r];
+        *(f32x4*)(room + (16 * j + lane % 16) * LD + 16 * i + lane / 16 * 4) = v;
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (u32 n = 0; n < ROWS * PER / kWave; ++n) {
+      const u32 at = n * kWave + lane, row = at / PER, col = at % PER * 8, t = t0 + 16 * j0 + row, o = o0 + col;
+      if (t >= to.rows || o >= to.outer) continue;
+      f32x4 v[2];
+      __builtin_memcpy(v, __builtin_assume_aligned(room + row * LD + col, 16), sizeof(v));
+      Vec8<T> y = {};
+      if (to.residual) y = load_cols(to.residual + t * to.ldr, o, to.outer);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y.set(e, (T)(v[e / 4][e % 4] + (to.residual ? (float)y.get(e) : 0.0f)));
+      store_cols(to.y + t * to.ldy, o, to.outer, y);
+    }
   }
 }
 
@@ -165,14 +194,9 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const
                                        w_tile(2), x_tile(3), w_tile(3), acc);
   else
     reduce<int8_t, TM, TN, WAVES>(from_x, at_x, from_w, at_w, width / KE, wave, row0, out0, x_tile(0), w_tile(0), x_tile(1), w_tile(1), acc);
-#pragma unroll
-  for (int j = 0; j < RT; ++j) {
-    const u32 t = t0 + row0 + j * 16 + lane % 16;
-    if (t >= to.rows) continue;
-    const float by = to.x_scale[t];
-#pragma unroll
-    for (int i = 0; i < OT; ++i) store_four(to, t, o0 + out0 + i * 16 + lane / 16 * 4, acc[i][j], by);
-  }
+  __syncthreads();  // the tiles' place is free
+  static_assert(sizeof(lds) >= WAVES * out_floats<RT, OT>() * sizeof(float), "");
+  store_results(to, t0 + row0, o0 + out0, acc, (float*)lds + wave * out_floats<RT, OT>());
 }
 
 // Few rows: a block takes 16 outputs by 16 R rows, its wavefronts a part of the reduction each, so that W is on its way from all
@@ -302,9 +326,13 @@ void product(const int8_t* x, const int8_t* w, size_t cols, const Out<T>& to, hi
   in_turns(ceil_div(to.rows, TM) * ceil_div(to.outer, TN), WM * WN * kWave, [&](u32 first, dim3 grid, dim3 block) {                 \
     hipLaunchKernelGGL((k_int8<T, TM, TN, WM, WN, FAR>), grid, block, 0, st, x, w, (u32)width, to, (u32)x_bytes, (u32)w_bytes, first); \
   })
+  // A tile of 256 x 256 takes a compute unit for itself, of 128 x 128 two share one; two rounds of the latter take 1.2 times one of the
+  // former. us by 256 and by 128: float16 8192 of 4096 to 4096 124 and 155, 4096 of 1024 to 4096 24.5 and 31; 3656 of 94 to 4371, 270 large
+  // tiles, 23.3 and 16.9. Fewer than 256 tiles of 128 x 128 leave compute units idle: 2048 of 2048 to 2048 16.6 by them and 18.2 by 64 x 64.
+  const size_t large = ceil_div(to.rows, 256) * ceil_div(to.outer, 256), middle = ceil_div(to.rows, 128) * ceil_div(to.outer, 128);
   if (far) HAFLO_LOCAL_RUN(256, 256, 2, 4, true);
-  else if (ceil_div(to.rows, 256) * ceil_div(to.outer, 256) >= 256) HAFLO_LOCAL_RUN(256, 256, 2, 4, false);
-  else if (ceil_div(to.rows, 128) * ceil_div(to.outer, 128) >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, false);
+  else if (large >= 256 && 5 * ceil_div(large, 256) <= 3 * ceil_div(middle, 512)) HAFLO_LOCAL_RUN(256, 256, 2, 4, false);
+  else if (middle >= 256) HAFLO_LOCAL_RUN(128, 128, 2, 2, false);
   else HAFLO_LOCAL_RUN(64, 64, 2, 2, false);
 #undef HAFLO_LOCAL_RUN
 }
