@@ -542,17 +542,18 @@ __device__ __forceinline__ void apply(const Matrices<T>& m, const double* P, u32
       f64x4 acc[KT];
 #pragma unroll
       for (int j = 0; j < KT; ++j) acc[j] = f64x4{0.0, 0.0, 0.0, 0.0};
+      // a step's elements of P are read under the products of the step before (and not earlier: there are registers for two steps')
+      double d[2][KT];
+      const auto read = [&](int n) { __builtin_memcpy(d[n & 1], &P[(16 * (n / 4) + 4 * group + n % 4) * S + s], sizeof(d[0])); };
+      read(0);
 #pragma unroll
-      for (u32 t = 0; t < KT; ++t)
+      for (int n = 0; n < 4 * KT; ++n) {
+        if (n + 1 < 4 * KT) read(n + 1);
+        const double v = (double)(float)x[n / 4][n % 4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          double d[KT];
-          __builtin_memcpy(d, &P[(16 * t + 4 * group + e) * S + s], sizeof(d));
-          const double v = (double)(float)x[t][e];
-#pragma unroll
-          for (int j = 0; j < KT; ++j) acc[j] = mma4(v, d[j], acc[j]);
-          if (KT >= 3) __builtin_amdgcn_sched_barrier(0);  // (P's elements not all at once: there are registers for two steps')
-        }
+        for (int j = 0; j < KT; ++j) acc[j] = mma4(v, d[n & 1][j], acc[j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const u32 l = at + 4 * r + group;
@@ -589,15 +590,22 @@ __device__ __forceinline__ void apply(const Matrices<T>& m, const double* P, u32
 #pragma unroll
           for (u32 n = 0; n < kAhead; ++n) load(m.g + row(t0 + 4 * (kAhead + n) + group, k) * m.ldg, x[n]);
         }
+        double d[2][KT];
+        const auto read = [&](u32 n) {
+#pragma unroll
+          for (int i = 0; i < KT; ++i) d[n & 1][i] = P[(16 * i + place) * S + t0 + 4 * n + group];
+        };
+        read(0);
 #pragma unroll
         for (u32 n = 0; n < kAhead; ++n) {
+          if (n + 1 < kAhead) read(n + 1);
 #pragma unroll
-          for (int i = 0; i < KT; ++i) {
-            const double d = P[(16 * i + place) * S + t0 + 4 * n + group];
+          for (int j = 0; j < V; ++j) {
+            const double v = (double)(float)now[n][j];
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[i][j] = mma4(d, (double)(float)now[n][j], acc[i][j]);
+            for (int i = 0; i < KT; ++i) acc[i][j] = mma4(d[n & 1][i], v, acc[i][j]);
           }
-          if (KT >= 3) __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
 #pragma unroll
