@@ -308,13 +308,22 @@ template <int KT, u32 WAVES>
 __device__ __forceinline__ void polynomial(double* K, double* Q, double* P, const Steps& steps, u32 wave) {
   constexpr u32 N = 16 * KT, S = N + 2, TILES = KT * (KT + 1) / 2;
   const u32 lane = lane_id();
+  // this wavefront's tiles, of two jobs at most (the row of a tile is found once: the search takes as long as some matrix instructions)
+  constexpr u32 MOST = (2 * TILES + WAVES - 1) / WAVES;
+  u32 row_of[MOST], col_of[MOST];
+#pragma unroll
+  for (u32 n = 0; n < MOST; ++n) {
+    const u32 tile = (wave + n * WAVES) % TILES;
+    row_of[n] = tile_row(tile);
+    col_of[n] = tile - row_of[n] * (row_of[n] + 1) / 2;
+  }
   // out = one I + self x + both x y, of x0 and, with two jobs, of x1
   const auto products = [&](auto jobs, double* out0, double* out1, const double* x0, const double* x1, const double* y, double one, double self, double both) {
     constexpr u32 TOTAL = decltype(jobs)::value * TILES, PER = (TOTAL + WAVES - 1) / WAVES;
     f64x4 acc[PER];
 #pragma unroll
     for (u32 n = 0; n < PER; ++n) {
-      const u32 id = wave + n * WAVES, tile = id % TILES, i = tile_row(tile), j = tile - i * (i + 1) / 2;
+      const u32 id = wave + n * WAVES, i = row_of[n], j = col_of[n];
       if (id >= TOTAL) continue;
       const double* const from = id < TILES ? x0 : x1;
       acc[n] = tile_product<N>(from, y, i, j, S);
@@ -327,7 +336,7 @@ __device__ __forceinline__ void polynomial(double* K, double* Q, double* P, cons
     __syncthreads();
 #pragma unroll
     for (u32 n = 0; n < PER; ++n) {
-      const u32 id = wave + n * WAVES, tile = id % TILES, i = tile_row(tile), j = tile - i * (i + 1) / 2;
+      const u32 id = wave + n * WAVES, i = row_of[n], j = col_of[n];
       if (id >= TOTAL) continue;
       double* const o = id < TILES ? out0 : out1;
 #pragma unroll
