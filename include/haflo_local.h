@@ -7,7 +7,9 @@
  * parties share. The operators of that step are here: dropout whose mask is
  * never stored, the shared projection with every row's own adapter and its
  * gradients, and the log-probabilities of labels with entropy, top alternatives
- * and gradient (logistic regression's loss for two classes or any number).
+ * and gradient (logistic regression's loss for two classes or any number); the
+ * norms around a block of such a model, and orthogonalised updates of adapters.
+ * The common model's answers may take its projections in eight bits.
  * Gradients of adapters are float32, as haflo_encode_f32 takes them.
  *
  * The conventions of haflo.h hold: 0 or a negative HAFLO_E* code, no exception,

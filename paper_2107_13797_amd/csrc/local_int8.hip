@@ -76,7 +76,7 @@ __device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width
   for (u32 col = at + lanes * 8; col < width; col += lanes * 8) put(col, eight_bits(load_cols(from, col, cols), s));
   return s.scale;
 }
-// Memory bounds it.
+// Memory bounds it (8192 x 4096 bfloat16 24 us, 4.2 TB/s), a launch where rows are few (64 of 4096 3.3 us).
 template <class T>
 __global__ __launch_bounds__(kMostLanes) void k_quantize(const T* x, size_t ldx, u32 rows, u32 cols, u32 width, u32 lanes, int8_t* q, float* scale,
                                                          u32 first_block) {
@@ -152,7 +152,9 @@ __device__ __forceinline__ void store_results(const Out<T>& to, u32 t0, u32 o0, 
 }
 
 // A block takes TM rows by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS, and one
-// is filled while the other is read; of tiles of 64 x 64 four steps'.
+// is filled while the other is read; of tiles of 64 x 64 four steps' (4096 to 4096, 128 rows 19.8 us by two and 12.6 by four). Matrix
+// instructions bound the large tiles: 8192 of 4096 to 4096 112 us, 2450 TOP/s (a library product of these numbers 129 us), busy in two thirds
+// of the cycles; the wait for loads the small ones (64 rows 9.2 us).
 template <class T, int TM, int TN, int WM, int WN, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const int8_t* w, u32 width, Out<T> to, u32 x_bytes, u32 w_bytes, u32 first_block) {
   constexpr int KE = step_elems<int8_t>(), WAVES = WM * WN, RT = TM / WM / 16, OT = TN / WN / 16;
@@ -201,7 +203,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const
 
 // Few rows: a block takes 16 outputs by 16 R rows, its wavefronts a part of the reduction each, so that W is on its way from all
 // of them at once, x and the next pieces with it; their sums are joined in LDS. With OWN the block brings the rows, at most four, to
-// eight bits itself.
+// eight bits itself, which takes less than a launch. One row of 4096 to 4096 6 us, 2.7 TB/s of W: its way from memory, x's and the joining one
+// after the other.
 constexpr u32 kFewWaves = 8, kFewThreads = kFewWaves * kWave, kOwnBytes = 32768;
 template <class T, int R, bool OWN>
 __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ldx, u32 cols, const int8_t* xq, const int8_t* w, u32 width, Out<T> to,
