@@ -15,7 +15,7 @@
  * The conventions of haflo.h hold: 0 or a negative HAFLO_E* code, no exception,
  * device pointers and sizes, a stream, no allocation and no synchronisation,
  * kernels only (a sequence of calls can be captured into a HIP graph). A call
- * works on the current device. Every sum is held in 32 bits; a result is
+ * works on the current device. Every sum is held in 32 bits or more; a result is
  * rounded to its type once. Results do not depend on timing: the same call on the
  * same device gives the same bits.
  *

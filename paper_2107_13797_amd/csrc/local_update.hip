@@ -453,7 +453,8 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
   steps_of<KT>(steps, scale, eps, held, room, sums, [&](u32 i, u32 j, double v) { to[i * N + j] = v; });
 }
 
-// More than 64 rows: K_0 and G's factor, from the parts; a block takes an eighth of a matrix, and each the parts' diagonals.
+// More than 64 rows: K_0 and G's factor, from the parts; a block takes an eighth of a matrix, and each the parts' diagonals (16 parts of 8
+// matrices 7.6 us, by a block each 34).
 constexpr u32 kLarge = 128, kJoinThreads = 512, kSlices = 8;
 __global__ __launch_bounds__(kJoinThreads) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, double* K, double* factor) {
   __shared__ double room[kJoinThreads / kWave];
@@ -723,7 +724,14 @@ bool update_sizes(int type, size_t parties, size_t rows, size_t cols, Shape& s) 
 Plan update_plan(const Shape& s) {
   Plan p = {};
   if (s.k <= 16 && s.length <= kOneLength) return p;
-  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div(s.tiles() <= 2 ? (size_t)512 : (size_t)256, s.parties ? s.parties : 1), most = ceil_div(chunks, 8);
+  // Parts of K_0's sums: enough for all compute units, and no more chunks to one than hide the first loads; but whoever joins the parts reads them
+  // all. Calls, us, with at most an 8th / a 4th / a 16th of the chunks' number: 7 of 1001 x 37 float32 35.3 / 34.5 / 38.5, 8 of 64 x 4096 (parts of
+  // 4 chunks and more: 32) 64.3 / 69.1 / 65.9, 2 of 64 x 10000 76.6 / 93.1 / 72.8 (40, 79 and 20 parts), 3001 x 100 121 / 109 / 153, 8 of
+  // 4096 x 32 22.4 / 23.1 / 23.4. All matrices' parts: of 64 of 16 x 4096 28 with 1024, 23 with 512; 300 of them 67 and 72, with 256 77.
+  const u32 tiles = s.tiles();
+  const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div((size_t)(tiles <= 2 ? 512 : 256), s.parties ? s.parties : 1);
+  size_t most = ceil_div(chunks, tiles <= 2 ? 8 : 4);
+  if (tiles > 2 && tiles <= 4 && most > 20) most = 20;
   p.parts = want < most ? want : most;
   const size_t each = s.side() * s.side() * 8;
   p.gram = 0;
@@ -770,7 +778,9 @@ void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double sc
 
 // Blocks of one matrix in k_apply: each brings P to LDS once, and there are enough for all compute units.
 u32 apply_blocks(const Shape& s, u32 places) {
-  const size_t need = ceil_div(s.length, places), want = ceil_div(s.tiles() <= 2 ? (size_t)768 : (size_t)512, s.parties);
+  // (us a call with 512 / 768 / 1024 for all matrices: 64 of 16 x 4096 float32 22.5 / 23.3 / 27.6, 300 of them 77 / 72 / 71, 300 of 2000 x 32
+  // 98 / 92 / 93, 64 of 64 x 4096 124 / 142 / 124)
+  const size_t need = ceil_div(s.length, places), want = ceil_div((size_t)(s.tiles() <= 2 ? 768 : 512), s.parties);
   return (u32)(need < want ? need : want);
 }
 
