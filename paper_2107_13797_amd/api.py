@@ -504,15 +504,16 @@ def _vector(t, n):
 def _norm_operands(x, f, post, gate, pre):
     dtype = x.dtype
     kind, (rows, cols, ldx) = _type(x), _matrix(x, dtype)
-    ldf = cols if f is None else _matrix(f, dtype, rows, cols)[2]
-    pg = pc = None
-    ldg = cols
+    pf = pg = pc = None
+    ldf = ldg = cols
+    if f is not None:
+        pf, ldf = f.data_ptr(), _matrix(f, dtype, rows, cols)[2]
     if gate is not None:
         if gate.dim() == 1:
-            pc = _vector(gate, cols)
+            pc = _dense(gate, torch.float32, cols)
         else:
-            ldg, pg = _matrix(gate, dtype, rows, cols)[2], gate.data_ptr()
-    return kind, rows, cols, (x.data_ptr(), ldx, None if f is None else f.data_ptr(), ldf, _vector(post, cols), pg, ldg, pc, _vector(pre, cols))
+            pg, ldg = gate.data_ptr(), _matrix(gate, dtype, rows, cols)[2]
+    return kind, rows, cols, (x.data_ptr(), ldx, pf, ldf, _vector(post, cols), pg, ldg, pc, _vector(pre, cols))
 
 
 def _result(like, rows, cols, out):
@@ -548,17 +549,32 @@ def haflo_residual_norm_backward(dh, dr, x, f, post, gate, pre, rstd, scale=1.0,
         raise HafloError("dh: the gradient of h, where there is one")
     lddh = cols if dh is None else _matrix(dh, x.dtype, rows, cols)[2]
     lddr = cols if dr is None else _matrix(dr, x.dtype, rows, cols)[2]
-    pr = _dense(rstd, torch.float32, 2, rows)
-    dx = x.new_empty((rows, cols)) if need_dx else None
-    df = None if f is None else x.new_empty((rows, cols))
-    by_cols = gate is not None and gate.dim() == 1
-    dgate = None if gate is None else gate.new_empty(gate.shape)
-    dpost, dpre = (None if t is None else t.new_empty(cols) for t in (post, pre))
+    ps = _dense(rstd, torch.float32, 2, rows)
+    # (each result's address as it is made: this takes most of a small call's time)
+    dx = df = dpost = dgate = dpre = p_dx = p_df = p_dpost = p_dgate = p_dgate_cols = p_dpre = None
+    if need_dx:
+        dx = x.new_empty((rows, cols))
+        p_dx = dx.data_ptr()
+    if f is not None:
+        df = x.new_empty((rows, cols))
+        p_df = df.data_ptr()
+    if post is not None:
+        dpost = post.new_empty(cols)
+        p_dpost = dpost.data_ptr()
+    if pre is not None:
+        dpre = pre.new_empty(cols)
+        p_dpre = dpre.data_ptr()
+    if gate is not None:
+        if gate.dim() == 1:
+            dgate = gate.new_empty(cols)
+            p_dgate_cols = dgate.data_ptr()
+        else:
+            dgate = x.new_empty((rows, cols))
+            p_dgate = dgate.data_ptr()
     nbytes = lib().haflo_residual_norm_workspace_bytes(kind, rows, cols)
     pw, ws = _scratch(nbytes, x)
-    at = [None if t is None else t.data_ptr() for t in (dh, dr, dx, df, dgate, dpost, dpre)]
-    _check(lib().haflo_residual_norm_backward(kind, at[0], lddh, at[1], lddr, *operands, pr, rows, cols, scale, at[2], cols, at[3], cols,
-                                              None if by_cols else at[4], cols, at[4] if by_cols else None, at[5], at[6], pw, nbytes, stream))
+    _check(lib().haflo_residual_norm_backward(kind, None if dh is None else dh.data_ptr(), lddh, None if dr is None else dr.data_ptr(), lddr, *operands, ps,
+                                              rows, cols, scale, p_dx, cols, p_df, cols, p_dgate, cols, p_dgate_cols, p_dpost, p_dpre, pw, nbytes, stream))
     return dx, df, dpost, dgate, dpre
 
 
@@ -587,8 +603,12 @@ def haflo_orthogonal_update(g, base=None, keep=1.0, scale=1.0, coefficients=NEWT
     kind = _type(g)
     if g.dim() != 3:
         raise HafloError("g: parties x rows x cols")
-    steps = len(coefficients)
-    if not 1 <= steps <= 16 or any(len(c) != 3 for c in coefficients):
+    try:
+        values = [v for a, b, c in coefficients for v in (a, b, c)]
+    except (TypeError, ValueError):
+        raise HafloError("coefficients: three of each of 1 to 16 steps") from None
+    steps = len(values) // 3
+    if not 1 <= steps <= 16:
         raise HafloError("coefficients: three of each of 1 to 16 steps")
     parties, rows, cols = shape
     pg, pb = _batch(g, dtype, shape), (None, cols, 0) if base is None else _batch(base, dtype, shape)
@@ -597,8 +617,7 @@ def haflo_orthogonal_update(g, base=None, keep=1.0, scale=1.0, coefficients=NEWT
     po = _batch(out, dtype, shape)
     nbytes = lib().haflo_update_workspace_bytes(kind, parties, rows, cols)
     pw, ws = _scratch(nbytes, g)
-    values = (C.c_double * (3 * steps))(*(v for c in coefficients for v in c))
-    _check(lib().haflo_orthogonal_update(kind, *pg, *pb, parties, rows, cols, values, steps, keep, scale, eps, *po, pw, nbytes, stream))
+    _check(lib().haflo_orthogonal_update(kind, *pg, *pb, parties, rows, cols, (C.c_double * (3 * steps))(*values), steps, keep, scale, eps, *po, pw, nbytes, stream))
     return out
 
 
