@@ -128,7 +128,7 @@ __device__ __forceinline__ void two_rows(const double (&d)[8], f64x4 (&acc)[9]) 
   for (int j = 0; j <= 7 - W; ++j) acc[W + 1 + j] = mma4(d[7 - W], d[j], acc[W + 1 + j]);
 }
 
-// The products of tiles of chunks first, first + stride .. below end. Up to four tiles a wavefront forms all products, of eight two
+// The products of tiles of chunks first, first + stride .. below end. Up to six tiles a wavefront forms all products, of eight two
 // rows' (`wave` 0 .. 3).
 template <int KT>
 constexpr int pairs_of() {
@@ -179,10 +179,10 @@ __device__ __forceinline__ u32 tile_row(u32 tile) {
   while ((i + 1) * (i + 2) / 2 <= tile) ++i;
   return i;
 }
-// A block's sums of up to four rows of tiles, five tiles at a time: put(row, column, sum) for both halves, zeros past the short side.
+// A block's sums of up to six rows of tiles, some tiles at a time: put(row, column, sum) for both halves, zeros past the short side.
 template <int KT>
 constexpr int tiles_at_once() {
-  return pairs_of<KT>() < 5 ? pairs_of<KT>() : KT == 3 ? 3 : 5;
+  return pairs_of<KT>() < 5 ? pairs_of<KT>() : KT == 3 ? 3 : KT == 6 ? 7 : 5;
 }
 template <int KT, bool TALL, u32 WAVES, class Put>
 __device__ __forceinline__ void gram_sums(const f64x4 (&acc)[pairs_of<KT>()], u32 wave, u32 k, double (*sum)[tiles_at_once<KT>()][256], const Put& put) {
@@ -455,23 +455,28 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
 
 // More than 64 rows: K_0 and G's factor, from the parts; a block takes an eighth of a matrix, and each the parts' diagonals (16 parts of 8
 // matrices 7.6 us, by a block each 34).
-constexpr u32 kLarge = 128, kJoinThreads = 512, kSlices = 8;
-__global__ __launch_bounds__(kJoinThreads) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, double* K, double* factor) {
-  __shared__ double room[kJoinThreads / kWave];
-  constexpr u32 kEach = kLarge * kLarge / kSlices / kJoinThreads;
+constexpr u32 kSlices = 8;
+template <u32 N>
+constexpr u32 join_threads() {
+  return 4 * N;
+}
+template <u32 N>
+__global__ __launch_bounds__(join_threads<N>()) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, double* K, double* factor) {
+  __shared__ double room[join_threads<N>() / kWave];
+  constexpr u32 kEach = N * N / kSlices / join_threads<N>();
   const auto [party, slice] = place_of_block(blockIdx.x, kSlices, parties);
   if (party >= parties) return;
-  parts += (size_t)party * count * kLarge * kLarge;
+  parts += (size_t)party * count * N * N;
   double s[kEach], squares = 0.0;
-  sum_parts(parts, count, kLarge * kLarge, slice * kEach * kJoinThreads + threadIdx.x, kJoinThreads, s);
-  if (threadIdx.x < kLarge) {
+  sum_parts(parts, count, N * N, slice * kEach * join_threads<N>() + threadIdx.x, join_threads<N>(), s);
+  if (threadIdx.x < N) {
     double d[1];
-    sum_parts(parts, count, kLarge * kLarge, threadIdx.x * (kLarge + 1), 0, d);
+    sum_parts(parts, count, N * N, threadIdx.x * (N + 1), 0, d);
     squares = d[0];
   }
-  const double by = factor_of(block_sum<kJoinThreads>(squares, room), eps);
+  const double by = factor_of(block_sum<join_threads<N>()>(squares, room), eps);
 #pragma unroll
-  for (u32 n = 0; n < kEach; ++n) K[(size_t)party * kLarge * kLarge + (slice * kEach + n) * kJoinThreads + threadIdx.x] = s[n] * by * by;
+  for (u32 n = 0; n < kEach; ++n) K[(size_t)party * N * N + (slice * kEach + n) * join_threads<N>() + threadIdx.x] = s[n] * by * by;
   if (slice == 0 && threadIdx.x == 0) factor[party] = by;
 }
 // out = one I + self x + both x y, times the party's factor where there is one
@@ -484,24 +489,29 @@ struct Products {
   Product job[2];
 };
 // A wavefront forms one tile on or under the diagonal. Five steps are fourteen launches: of 8 matrices 4.8 us each, most of it the launch and the
-// operands' way from the last one's results; of 64 12.7, in which operands are read 32 KiB a tile.
-constexpr u32 kLargeTiles = 36;
+// operands' way from the last one's results; of 64 12.7, in which operands are read 32 KiB a tile. Up to 96 rows are taken as 96 (39
+// matrices of 87 x 3927 float32 268 us, 419 as 128).
+template <u32 N>
+constexpr u32 large_tiles() {
+  return (N / 16) * (N / 16 + 1) / 2;
+}
+template <u32 N>
 __global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 parties, u32 first_block) {
-  const auto [party, part] = place_of_block(first_block + blockIdx.x, jobs * kLargeTiles, parties);
+  const auto [party, part] = place_of_block(first_block + blockIdx.x, jobs * large_tiles<N>(), parties);
   if (party >= parties) return;
-  const u32 lane = lane_id(), tile = part % kLargeTiles;
-  const Product q = p.job[part / kLargeTiles];
+  const u32 lane = lane_id(), tile = part % large_tiles<N>();
+  const Product q = p.job[part / large_tiles<N>()];
   const u32 i = tile_row(tile), j = tile - i * (i + 1) / 2;
-  const size_t at = (size_t)party * kLarge * kLarge;
+  const size_t at = (size_t)party * N * N;
   const double* const x = q.x + at;
-  const f64x4 acc = tile_product<kLarge>(x, q.y + at, i, j, kLarge);
+  const f64x4 acc = tile_product<N>(x, q.y + at, i, j, N);
   const double by = q.factor ? q.factor[party] : 1.0;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const u32 row = 16 * i + 4 * r + lane / 16, col = 16 * j + lane % 16;
-    const double v = (q.both * acc[r] + (q.self != 0.0 ? q.self * x[row * kLarge + col] : 0.0) + (row == col ? q.one : 0.0)) * by;
-    q.out[at + row * kLarge + col] = v;
-    if (i != j) q.out[at + col * kLarge + row] = v;
+    const double v = (q.both * acc[r] + (q.self != 0.0 ? q.self * x[row * N + col] : 0.0) + (row == col ? q.one : 0.0)) * by;
+    q.out[at + row * N + col] = v;
+    if (i != j) q.out[at + col * N + row] = v;
   }
 }
 
@@ -709,7 +719,7 @@ __global__ __launch_bounds__(kOneThreads) void k_update(Batch<const T> g, Batch<
 struct Shape {
   size_t parties, k, length;
   bool tall;
-  u32 tiles() const { return k <= 16 ? 1 : k <= 32 ? 2 : k <= 48 ? 3 : k <= 64 ? 4 : 8; }
+  u32 tiles() const { return k <= 16 ? 1 : k <= 32 ? 2 : k <= 48 ? 3 : k <= 64 ? 4 : k <= 96 ? 6 : 8; }
   size_t side() const { return 16 * tiles(); }
 };
 constexpr size_t kOneLength = 768;
@@ -743,16 +753,17 @@ Plan update_plan(const Shape& s) {
 }
 
 // scale P / (|G|_F + eps) of more than 64 rows, product by product
+template <u32 N>
 void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double scale, double eps, char* ws, hipStream_t st) {
-  const size_t each = s.parties * kLarge * kLarge * 8;
+  const size_t each = s.parties * N * N * 8;
   const auto place = [&](int i) { return (double*)(ws + plan.extra + i * each); };
   double *const K = place(0), *const Q = place(1), *P = place(2), *const M = place(3), *spare = place(4);
   double *const factor = (double*)(ws + plan.factor), *const to = (double*)(ws + plan.poly);
-  hipLaunchKernelGGL(k_gram_join, dim3((unsigned)blocks_of(kSlices, s.parties)), dim3(kJoinThreads), 0, st, (const double*)(ws + plan.gram), (u32)plan.parts,
+  hipLaunchKernelGGL((k_gram_join<N>), dim3((unsigned)blocks_of(kSlices, s.parties)), dim3(join_threads<N>()), 0, st, (const double*)(ws + plan.gram), (u32)plan.parts,
                      (u32)s.parties, eps, K, factor);
   const auto run = [&](Products p, u32 jobs) {
-    in_turns(blocks_of(jobs * kLargeTiles, s.parties), kWave,
-             [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL(k_products, grid, block, 0, st, p, jobs, (u32)s.parties, first); });
+    in_turns(blocks_of(jobs * large_tiles<N>(), s.parties), kWave,
+             [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL((k_products<N>), grid, block, 0, st, p, jobs, (u32)s.parties, first); });
   };
   for (int i = 0; i < steps.count; ++i) {
     const double a = steps.c[i][0], b = steps.c[i][1], c = steps.c[i][2];
@@ -807,7 +818,7 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
   else if constexpr (KT <= 4)
     hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)sums, (u32)plan.parts, steps, scale, eps, poly);
   else
-    large_steps(s, plan, steps, scale, eps, ws, st);
+    large_steps<16 * KT>(s, plan, steps, scale, eps, ws, st);
   const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);
   in_turns(blocks_of(blocks, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
     if (whole) hipLaunchKernelGGL((k_apply<T, KT, TALL, true>), grid, block, 0, st, g, base, out, from, k, length, keep, blocks, (u32)s.parties, first);
@@ -822,6 +833,7 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
     case 2: return update<T, 2, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
     case 3: return update<T, 3, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
     case 4: return update<T, 4, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
+    case 6: return update<T, 6, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
     default: return update<T, 8, TALL>(g, base, out, s, plan, steps, keep, scale, eps, ws, st);
   }
 }

@@ -168,6 +168,7 @@ UPDATES = [  # type, parties, rows, cols, base, steps, pad
     ("f32", 1, 3, 600, True, [CUBIC] * 16, 5), ("f32", 1, 90, 66, False, [QUINTIC], 0),
     ("f32", 2, 9, 800, True, [QUINTIC] * 2, 0), ("f16", 1, 780, 16, False, [QUINTIC] * 5, 1), ("bf16", 1, 45, 300, True, [QUINTIC] * 2, 0),
     ("f32", 1, 290, 48, True, [CUBIC], 0), ("f16", 1, 100, 30, True, [QUINTIC] * 2, 0), ("f32", 1, 60, 52, False, [QUINTIC], 2),
+    ("bf16", 1, 97, 99, True, [QUINTIC] * 2, 0), ("f32", 1, 130, 104, False, [QUINTIC], 0), ("f16", 1, 73, 72, True, [CUBIC] * 3, 0),
 ]
 UPDATES_LARGE = [
     ("f32", 8, 16, 4096, True, [QUINTIC] * 5, 0), ("bf16", 7, 1001, 37, False, [QUINTIC] * 5, 0), ("f32", 64, 512, 64, True, [QUINTIC] * 5, 0),
@@ -336,7 +337,7 @@ def norm_forms(kind):
 
 def update_forms(kind, tall):
     """Every number of tiles, filled and not, with loads of whole and of single elements, by one launch and by several."""
-    for k in (1, 5, 16, 17, 24, 32, 33, 36, 48, 50, 64, 65, 100, 128):
+    for k in (1, 5, 16, 17, 24, 32, 33, 36, 48, 50, 64, 65, 72, 90, 96, 97, 100, 128):
         for length in ((k, 70, 800, 1100) if k <= 16 else (k, 140, 300)):
             if length >= k:
                 rows, cols = (length, k) if tall else (k, length)
