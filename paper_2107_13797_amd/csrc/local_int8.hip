@@ -53,16 +53,31 @@ __device__ __forceinline__ u64 eight_bits(const Vec8<T>& v, const Scale& s) {
   return q;
 }
 
-// A row to eight bits by a group of `lanes` lanes, eight columns to a lane, and of a longer row the others again: `put` takes eight bytes at
-// each multiple of eight below `width`. All of a block's groups call it together. Returns the row's scale.
+// A row to eight bits by a group of `lanes` lanes, four times eight columns to a lane, and of a longer row the others again: `put` takes eight
+// bytes at each multiple of eight below `width`. All of a block's groups call it together. Returns the row's scale.
 template <class T, class Put>
 __device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width, u32 lanes, u32* room, const Put& put) {
-  const u32 at = threadIdx.x % lanes * 8;
-  const Vec8<T> own = load_cols(from, at, cols);
-  u32 m = most_of(own);
-  for (u32 col = at + lanes * 8; col < cols; col += lanes * 8) {
-    const u32 b = most_of(load_cols(from, col, cols));
-    m = b > m ? b : m;
+  constexpr u32 kHeld = 4;
+  const u32 at = threadIdx.x % lanes * 8, apart = lanes * 8;
+  u32 m = 0;
+  const auto load = [&](u32 first, Vec8<T> (&v)[kHeld]) {
+#pragma unroll
+    for (u32 i = 0; i < kHeld; ++i) v[i] = load_cols(from, first + i * apart, cols);
+  };
+  const auto look = [&](const Vec8<T> (&v)[kHeld]) {
+#pragma unroll
+    for (u32 i = 0; i < kHeld; ++i) {
+      const u32 b = most_of(v[i]);
+      m = b > m ? b : m;
+    }
+  };
+  Vec8<T> own[kHeld];
+  load(at, own);
+  look(own);
+  for (u32 col = at + kHeld * apart; col < cols; col += kHeld * apart) {
+    Vec8<T> more[kHeld];
+    load(col, more);
+    look(more);
   }
   m = lanes_join(m, lanes, [](u32 a, u32 b) { return a > b ? a : b; });
   if (lanes > kWave) {
@@ -72,8 +87,17 @@ __device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width
     for (u32 w = 0; w < waves; ++w) m = room[first + w] > m ? room[first + w] : m;
   }
   const Scale s = scale_of(m);
-  if (at < width) put(at, eight_bits(own, s));
-  for (u32 col = at + lanes * 8; col < width; col += lanes * 8) put(col, eight_bits(load_cols(from, col, cols), s));
+  const auto give = [&](u32 first, const Vec8<T> (&v)[kHeld]) {
+#pragma unroll
+    for (u32 i = 0; i < kHeld; ++i)
+      if (first + i * apart < width) put(first + i * apart, eight_bits(v[i], s));
+  };
+  give(at, own);
+  for (u32 col = at + kHeld * apart; col < width; col += kHeld * apart) {
+    Vec8<T> more[kHeld];
+    load(col, more);
+    give(col, more);
+  }
   return s.scale;
 }
 // Memory bounds it (8192 x 4096 bfloat16 24 us, 4.2 TB/s), a launch where rows are few (64 of 4096 3.3 us).
@@ -202,17 +226,18 @@ __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const
 }
 
 // Few rows: a block takes 16 outputs by 16 R rows, its wavefronts a part of the reduction each, so that W is on its way from all
-// of them at once, x and the next pieces with it; their sums are joined in LDS. With OWN the block brings the rows, at most four, to
-// eight bits itself, which takes no longer than a launch (4 rows of 4096 to 4096 7.6 us, 5 by way of k_quantize 7.7) and spares the host one. One row of 4096 to 4096 6 us, 2.7 TB/s of W: its way from memory, x's and the joining one
+// of them at once, x and the next pieces with it; their sums are joined in LDS. With OWN the block brings the rows, at most sixteen, to
+// eight bits itself, which takes no longer than a launch (8 rows of 2048 to 4096 6.4 us, by way of k_quantize 7.9; 16 8.5 and 8.6) and spares
+// the host one. One row of 4096 to 4096 6 us, 2.7 TB/s of W: its way from memory, x's and the joining one
 // after the other.
-constexpr u32 kFewWaves = 8, kFewThreads = kFewWaves * kWave, kOwnBytes = 32768;
+constexpr u32 kFewWaves = 8, kFewThreads = kFewWaves * kWave, kOwnBytes = 32768, kOwnPad = 16;  // (rows in LDS begin on different banks)
 template <class T, int R, bool OWN>
 __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ldx, u32 cols, const int8_t* xq, const int8_t* w, u32 width, Out<T> to,
                                                           u32 first_block) {
   constexpr u32 kAhead = R == 1 ? 4 : 2;  // pieces of 128 bytes of each row that are on their way together
   constexpr u32 kResults = (256 * R + kFewThreads - 1) / kFewThreads;
-  __shared__ __align__(16) int8_t own[OWN ? kOwnBytes : 16];
-  __shared__ float own_scale[4];
+  __shared__ __align__(16) int8_t own[OWN ? kOwnBytes + 16 * kOwnPad : 16];
+  __shared__ float own_scale[16];
   __shared__ u32 room[kFewWaves];
   __shared__ int sums[kFewWaves][R][256];
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = lane_id();
@@ -222,7 +247,7 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
   const int8_t* const wr = w + (size_t)last(o0 + lane % 16, to.outer) * width + lane / 16 * 16;
   const int8_t* xr[R];
 #pragma unroll
-  for (int j = 0; j < R; ++j) xr[j] = (OWN ? own : xq) + (size_t)last(t0 + 16 * j + lane % 16, to.rows) * width + lane / 16 * 16;
+  for (int j = 0; j < R; ++j) xr[j] = (OWN ? own : xq) + (size_t)last(t0 + 16 * j + lane % 16, to.rows) * (OWN ? width + kOwnPad : width) + lane / 16 * 16;
   struct Pieces {
     i32x4 w[kAhead][2], x[OWN ? 1 : kAhead][2][R];
   };
@@ -252,9 +277,11 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
     was[n] = to.residual ? (float)to.residual[t * to.ldr + o] : 0.0f;
   }
   if (OWN) {
-    const u32 groups = to.rows == 1 ? 1 : to.rows == 2 ? 2 : 4, lanes = kFewThreads / groups, group = threadIdx.x / lanes, row = last(group, to.rows);
+    u32 groups = 1;
+    while (groups < to.rows) groups *= 2;
+    const u32 lanes = kFewThreads / groups, group = threadIdx.x / lanes, row = last(group, to.rows);
     const float s = quantize_row(xf + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
-      if (group < to.rows) *(u64*)(own + group * width + col) = v;
+      if (group < to.rows) *(u64*)(own + group * (width + kOwnPad) + col) = v;
     });
     if (threadIdx.x % lanes == 0) own_scale[group] = s;
     __syncthreads();
@@ -292,8 +319,8 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
   }
 }
 
-constexpr size_t kFewRows = 32, kFewOuter = 4096, kFewBytes = 2048, kOwnRows = 4;
-bool own_rows(size_t rows, size_t cols) { return rows <= kOwnRows && rows * row_bytes(cols) <= kOwnBytes; }
+constexpr size_t kFewRows = 32, kFewOuter = 4096, kFewBytes = 2048;
+bool own_rows(size_t rows, size_t cols, size_t outer) { return rows <= (outer <= kFewOuter ? 16 : 4) && rows * row_bytes(cols) <= kOwnBytes; }
 // One block for each compute unit at most, and rows long enough to split: then k_int8_few, else tiles of 64 x 64. Calls of few / of tiles, us, 5, 16
 // and 32 rows: 1024 to 1024 7.4 / 6.7, 8.4 / 6.9, 7.8 / 7.5; 2048 to 2048 7.5 / 8.0, 8.6 / 8.4, 7.8 / 9.0; 4096 to 1024 7.6 / 10.6, 8.6 / 10.9,
 // 10.3 / 11.5; 4096 to 4096 7.9 / 10.8, 8.8 / 11.0, 10.8 / 11.5, 48 rows 13.5 / 11.8; 4096 to 8192 11.5 / 11.9, 13.5 / 11.8, 16.2 / 12.5.
@@ -347,9 +374,9 @@ bool aligned(const void* p) { return p && (uintptr_t)p % 16 == 0; }
 struct Plan {
   size_t scale, total;
 };
-Plan int8_plan(size_t rows, size_t inner) {
+Plan int8_plan(size_t rows, size_t inner, size_t outer) {
   Plan p = {0, 0};
-  if (own_rows(rows, inner)) return p;
+  if (own_rows(rows, inner, outer)) return p;
   p.scale = align256(rows * row_bytes(inner));
   p.total = p.scale + align256(rows * 4);
   return p;
@@ -381,7 +408,7 @@ int haflo_int8_product(int type, const int8_t* d_xq, const float* d_x_scale, con
 }
 
 size_t haflo_int8_workspace_bytes(int type, size_t rows, size_t inner, size_t outer) {
-  return int8_sizes(type, rows, inner, outer) ? int8_plan(rows, inner).total : (size_t)-1;
+  return int8_sizes(type, rows, inner, outer) ? int8_plan(rows, inner, outer).total : (size_t)-1;
 }
 
 int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq, const float* d_w_scale, const float* d_bias, const void* d_residual,
@@ -391,7 +418,7 @@ int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq
   if (rows == 0) return HAFLO_OK;
   if (!d_x || ldx < inner || !aligned(d_wq) || !d_w_scale || (d_residual && ldr < outer) || !d_y || ldy < outer) return HAFLO_EINVAL;
   if (!in_place(d_residual, ldr, d_y, ldy, rows)) return HAFLO_EINVAL;
-  const Plan plan = int8_plan(rows, inner);
+  const Plan plan = int8_plan(rows, inner, outer);
   if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;
   int8_t* const xq = (int8_t*)d_workspace;
   float* const x_scale = (float*)((char*)d_workspace + plan.scale);

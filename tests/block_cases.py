@@ -346,6 +346,6 @@ def update_forms(kind, tall):
 
 def int8_forms(kind):
     """Rows that a block brings to eight bits itself, few rows, and tiles of three sizes."""
-    for rows, inner, outer in ((1, 2048, 40), (2, 100, 17), (3, 4096, 33), (4, 8192, 20), (4, 8200, 20), (5, 2048, 40), (16, 2049, 4096), (17, 2048, 30), (32, 4100, 9),
+    for rows, inner, outer in ((1, 2048, 40), (2, 100, 17), (3, 4096, 33), (4, 8192, 20), (4, 8200, 20), (5, 2048, 40), (5, 8200, 20), (8, 4096, 40), (9, 3500, 40), (11, 300, 4097), (13, 70, 4096), (16, 2049, 4096), (17, 2048, 30), (32, 4100, 9),
                                (33, 2048, 30), (32, 2048, 4097), (8, 1900, 50), (70, 40, 70), (2050, 130, 2050), (4090, 200, 4093), (4097, 3000, 4097)):
         yield (kind, rows, inner, outer, 0, rows % 2 == 0, rows % 3 == 0)
