@@ -53,29 +53,28 @@ __device__ __forceinline__ u64 eight_bits(const Vec8<T>& v, const Scale& s) {
   return q;
 }
 
-// A row to eight bits by a group of `lanes` lanes, four times eight columns to a lane, and of a longer row the others again: `put` takes eight
+// A row to eight bits by a group of `lanes` lanes, HELD times eight columns to a lane, and of a longer row the others again: `put` takes eight
 // bytes at each multiple of eight below `width`. All of a block's groups call it together. Returns the row's scale.
-template <class T, class Put>
+template <u32 HELD, class T, class Put>
 __device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width, u32 lanes, u32* room, const Put& put) {
-  constexpr u32 kHeld = 4;
   const u32 at = threadIdx.x % lanes * 8, apart = lanes * 8;
   u32 m = 0;
-  const auto load = [&](u32 first, Vec8<T> (&v)[kHeld]) {
+  const auto load = [&](u32 first, Vec8<T> (&v)[HELD]) {
 #pragma unroll
-    for (u32 i = 0; i < kHeld; ++i) v[i] = load_cols(from, first + i * apart, cols);
+    for (u32 i = 0; i < HELD; ++i) v[i] = load_cols(from, first + i * apart, cols);
   };
-  const auto look = [&](const Vec8<T> (&v)[kHeld]) {
+  const auto look = [&](const Vec8<T> (&v)[HELD]) {
 #pragma unroll
-    for (u32 i = 0; i < kHeld; ++i) {
+    for (u32 i = 0; i < HELD; ++i) {
       const u32 b = most_of(v[i]);
       m = b > m ? b : m;
     }
   };
-  Vec8<T> own[kHeld];
+  Vec8<T> own[HELD];
   load(at, own);
   look(own);
-  for (u32 col = at + kHeld * apart; col < cols; col += kHeld * apart) {
-    Vec8<T> more[kHeld];
+  for (u32 col = at + HELD * apart; col < cols; col += HELD * apart) {
+    Vec8<T> more[HELD];
     load(col, more);
     look(more);
   }
@@ -87,14 +86,14 @@ __device__ __forceinline__ float quantize_row(const T* from, u32 cols, u32 width
     for (u32 w = 0; w < waves; ++w) m = room[first + w] > m ? room[first + w] : m;
   }
   const Scale s = scale_of(m);
-  const auto give = [&](u32 first, const Vec8<T> (&v)[kHeld]) {
+  const auto give = [&](u32 first, const Vec8<T> (&v)[HELD]) {
 #pragma unroll
-    for (u32 i = 0; i < kHeld; ++i)
+    for (u32 i = 0; i < HELD; ++i)
       if (first + i * apart < width) put(first + i * apart, eight_bits(v[i], s));
   };
   give(at, own);
-  for (u32 col = at + kHeld * apart; col < width; col += kHeld * apart) {
-    Vec8<T> more[kHeld];
+  for (u32 col = at + HELD * apart; col < width; col += HELD * apart) {
+    Vec8<T> more[HELD];
     load(col, more);
     give(col, more);
   }
@@ -109,7 +108,7 @@ __global__ __launch_bounds__(kMostLanes) void k_quantize(const T* x, size_t ldx,
   const bool live = mine < rows;
   const u64 row = live ? mine : rows - 1;
   u64* const to = (u64*)(q + row * width);
-  const float s = quantize_row(x + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
+  const float s = quantize_row<1>(x + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
     if (live) to[col / 8] = v;
   });
   if (live && threadIdx.x % lanes == 0) scale[row] = s;
@@ -280,9 +279,11 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
     u32 groups = 1;
     while (groups < to.rows) groups *= 2;
     const u32 lanes = kFewThreads / groups, group = threadIdx.x / lanes, row = last(group, to.rows);
-    const float s = quantize_row(xf + row * ldx, cols, width, lanes, room, [&](u32 col, u64 v) {
+    const auto put = [&](u32 col, u64 v) {
       if (group < to.rows) *(u64*)(own + group * (width + kOwnPad) + col) = v;
-    });
+    };
+    // (four vectors on their way where a lane has several; where it has one, the other three's branches cost 0.3 us)
+    const float s = cols <= lanes * 8 ? quantize_row<1>(xf + row * ldx, cols, width, lanes, room, put) : quantize_row<4>(xf + row * ldx, cols, width, lanes, room, put);
     if (threadIdx.x % lanes == 0) own_scale[group] = s;
     __syncthreads();
   }
