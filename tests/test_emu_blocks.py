@@ -301,7 +301,7 @@ def test_sizes_and_refusals(run):
                 dict(res=q, ldr=5), dict(inner=0), dict(outer=0)):
         assert product(**bad) == -1, bad
 
-    def forward(x=p, ldx=8, rows=5, wq=p, y=q, ldy=4, w=q + 1024, n=2048):
+    def forward(x=p, ldx=8, rows=17, wq=p, y=q, ldy=4, w=q + 1024, n=4096):
         return lib.haflo_int8_forward(0, x, ldx, wq, p, None, None, 0, rows, 8, 4, y, ldy, w, n, None)
 
     assert forward() == 0
