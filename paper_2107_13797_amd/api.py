@@ -597,7 +597,8 @@ def _batch(t, dtype, shape):
 def haflo_orthogonal_update(g, base=None, keep=1.0, scale=1.0, coefficients=NEWTON_SCHULZ, eps=1e-7, out=None):
     """keep base + scale X, X from Newton-Schulz steps on each matrix of g [parties, rows, cols], the shorter side at most 128: X = g /
     (|g| + eps), then for each (a, b, c) of `coefficients` X <- a X + (b K + c K^2) X, K = X X^T. base, and out, which may be g or base: of
-    g's type and shape; without base scale X alone. Products are held in 64 bits; autograd records nothing."""
+    g's type and shape; without base scale X alone. Products are held in 64 bits; lists whose steps raise directions by more than 512 together take
+    readings of g in between. Autograd records nothing."""
     stream = _stream_of(g, base, out)
     dtype, shape = g.dtype, g.shape
     kind = _type(g)

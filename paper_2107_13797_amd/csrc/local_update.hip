@@ -3,11 +3,16 @@
 //   X_0 = G / (|G|_F + eps),   X_j+1 = (a_j + b_j K_j + c_j K_j^2) X_j,   K_j = X_j X_j^T,   out = keep base + scale X_n
 //
 // X_j is P_j X_0 with a polynomial P_j of K_0, which is k x k for a short side of k, and K_j, P_j and all factors commute. So G
-// is read twice however many steps there are: k_gram forms K_0, k_steps the polynomial from it (of more than 64 rows
+// is read twice by most lists of steps: k_gram forms K_0, k_steps the polynomial from it (of more than 64 rows
 // k_products does, product by product), and k_apply multiplies.
 // All of it is in 64 bits. A quintic of slope a at zero raises weak directions by a in each step, to 485 in five of 3.4445, and takes
 // that back where they have grown; an error d of K_0 then changes a weak direction by some 28000 d of itself, which 32 bits
 // do not bear. The matrix instructions of 64 bits take 64 cycles for 16 x 16 x 4, half the rate of those of 32.
+// What is rounded on the way from K_0 does not commute, and grows with the cube of what the steps raise, where X's own roundings
+// grow with that itself. So a list that raises by more is cut (cuts_of): behind each part K is formed again from X = P G (k_gram_again), and
+// the parts' polynomials are multiplied (k_chain). Against products one by one in 80 bits, as parts of what is greatest, 64 x 256 of equal rows: 5 steps
+// of 3.4445 in one part 8e-10, 8 uncut 1e-5, 16 uncut 4e6; 8 in three parts 3.4e-11, 16 in six 3.2e-7 (one by one in 64 bits an error is
+// some 2^-53 of what the steps raise by, of the greatest singular value: 4.4e-8, which is 50 times as much of what is greatest here).
 #include "local_common.hpp"
 
 using namespace haflo::local;
@@ -245,6 +250,12 @@ __global__ __launch_bounds__(kThreads) void k_gram(Batch<const T> g, u32 k, u32 
 struct Steps {
   double c[HAFLO_UPDATE_MAX_STEPS][3];
   int count;
+  u32 cuts;  // bit i: behind step i K is formed again
+  // the end of the part that begins with step `first`
+  __host__ __device__ __forceinline__ int end(int first) const {
+    while (first + 1 < count && !(cuts >> first & 1)) ++first;
+    return first + 1;
+  }
 };
 // The sum over a block's threads.
 template <u32 THREADS>
@@ -376,22 +387,22 @@ __device__ __forceinline__ f64x4 tile_squared(const f64x4& x, const f64x4& y) {
   for (int r = 0; r < 4; ++r) acc = mma4(x[r], y[r], acc);
   return acc;
 }
-__device__ __forceinline__ f64x4 polynomial(f64x4 K, const Steps& steps) {
+__device__ __forceinline__ f64x4 polynomial(f64x4 K, const Steps& steps, int first, int end) {
   f64x4 P = {};
-  for (int s = 0; s < steps.count; ++s) {
+  for (int s = first; s < end; ++s) {
     const f64x4 square = tile_squared(K, K);
     f64x4 Q;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       Q[r] = steps.c[s][2] * square[r] + (steps.c[s][1] * K[r] + (4 * r + lane_id() / 16 == lane_id() % 16 ? steps.c[s][0] : 0.0));
-    if (s + 1 < steps.count) K = tile_squared(tile_squared(K, Q), Q);
-    P = s == 0 ? Q : tile_squared(P, Q);
+    if (s + 1 < end) K = tile_squared(tile_squared(K, Q), Q);
+    P = s == first ? Q : tile_squared(P, Q);
   }
   return P;
 }
 
 // From K's sums, element threadIdx.x + e THREADS of it in `sums`, to scale P / (|G|_F + eps), which put(row, column, value) takes: by a block,
-// of one tile by a wavefront.
+// of one tile by a wavefront. `again`: they are sums of X, and the factor of G is in it. Of one tile steps first .. end - 1.
 template <int KT>
 struct StepRoom {
   double m[KT == 1 ? 1 : 3][KT == 1 ? 1 : 16 * KT * (16 * KT + 2)];
@@ -405,8 +416,8 @@ constexpr u32 step_elements() {
   return 256 * KT * KT / step_threads<KT>();
 }
 template <int KT, class Put>
-__device__ __forceinline__ void steps_of(const Steps& steps, double scale, double eps, StepRoom<KT>& held, double* room, const double (&sums)[step_elements<KT>()],
-                                         const Put& put) {
+__device__ __forceinline__ void steps_of(const Steps& steps, int first, int end, double scale, double eps, bool again, StepRoom<KT>& held, double* room,
+                                         const double (&sums)[step_elements<KT>()], const Put& put) {
   constexpr u32 N = 16 * KT, S = N + 2, THREADS = step_threads<KT>(), E = step_elements<KT>();
   double squares = 0.0;
 #pragma unroll
@@ -414,13 +425,13 @@ __device__ __forceinline__ void steps_of(const Steps& steps, double scale, doubl
     const u32 i = threadIdx.x + e * THREADS;
     if (i / N == i % N) squares += sums[e];
   }
-  const double by = factor_of(block_sum<THREADS>(squares, room), eps);
+  const double by = again ? 1.0 : factor_of(block_sum<THREADS>(squares, room), eps);
   if constexpr (KT == 1) {
     // (element lane + 64 r is of row 4 r + lane / 16 and column lane % 16: as the products have it)
     f64x4 K;
 #pragma unroll
     for (int r = 0; r < 4; ++r) K[r] = sums[r] * by * by;
-    const f64x4 P = polynomial(K, steps);
+    const f64x4 P = polynomial(K, steps, first, end);
 #pragma unroll
     for (int r = 0; r < 4; ++r) put(4 * r + threadIdx.x / 16, threadIdx.x % 16, P[r] * (by * scale));
   } else {
@@ -440,9 +451,10 @@ __device__ __forceinline__ void steps_of(const Steps& steps, double scale, doubl
   }
 }
 
-// The polynomial of 17 to 64 rows, from the parts' sums, by a block (five steps of 32 rows 13 us, of 48 21, of 64 36).
+// The polynomial of 17 to 64 rows, and of up to 16 where the list is cut, from the parts' sums, by a block (five steps of 32 rows 13 us, of
+// 48 21, of 64 36).
 template <int KT>
-__global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, double* to) {
+__global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* parts, u32 count, Steps steps, double scale, double eps, u32 again, double* to) {
   constexpr u32 N = 16 * KT;
   __shared__ __align__(16) StepRoom<KT> held;
   __shared__ double room[16];
@@ -450,7 +462,107 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
   to += (size_t)blockIdx.x * N * N;
   double sums[step_elements<KT>()];
   sum_parts(parts, count, N * N, threadIdx.x, step_threads<KT>(), sums);
-  steps_of<KT>(steps, scale, eps, held, room, sums, [&](u32 i, u32 j, double v) { to[i * N + j] = v; });
+  steps_of<KT>(steps, 0, steps.count, scale, eps, again, held, room, sums, [&](u32 i, u32 j, double v) { to[i * N + j] = v; });
+}
+
+// K of X = P G: a wavefront forms X on sixteen places of the long side, as the transpose, whose results lie in registers as the products by
+// themselves take them, and rows FROM .. TO - 1 of tiles of X X^T from it. R is P transposed, rows N + 2 apart in LDS. Pieces piece, piece + stride ..
+// below end. It is a part of lists that most calls do not have, and is kept simple: loads are waited for.
+constexpr int tiles_below(int rows) { return rows * (rows + 1) / 2; }
+template <class T, int KT, bool TALL, int FROM, int TO, int COUNT>
+__device__ __forceinline__ void gram_again(const T* m, size_t ld, const double* R, u32 k, u32 length, u32 piece, u32 end, u32 stride, f64x4 (&acc)[COUNT]) {
+  static_assert(tiles_below(TO) - tiles_below(FROM) <= COUNT, "");
+  constexpr u32 S = 16 * KT + 2;
+  const u32 place = lane_id() % 16, group = lane_id() / 16;
+#pragma unroll
+  for (int n = 0; n < COUNT; ++n) acc[n] = f64x4{0.0, 0.0, 0.0, 0.0};
+  for (; piece < end; piece += stride) {
+    const u32 l = piece * 16 + place, at = l < length ? l : length - 1;
+    f64x4 x[TO];
+#pragma unroll
+    for (int i = 0; i < TO; ++i) x[i] = f64x4{0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
+    for (u32 t = 0; t < 4 * KT; ++t) {
+      const u32 s = 4 * t + group, row = s < k ? s : k - 1;
+      const T v = TALL ? m[at * ld + row] : m[row * ld + at];
+      const double d = s < k && l < length ? (double)(float)v : 0.0;
+#pragma unroll
+      for (int i = 0; i < TO; ++i) x[i] = mma4(d, R[s * S + 16 * i + place], x[i]);
+    }
+    // x[i][r]: place 4 r + group of row 16 i + place
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      int n = 0;
+#pragma unroll
+      for (int i = FROM; i < TO; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j, ++n) acc[n] = mma4(x[i][r], x[j][r], acc[n]);
+    }
+  }
+}
+// A block's sums of them in `room`: wavefronts in turn put, and from the one behind `from` on add, `count` tiles from the `first` on.
+template <u32 WAVES, int COUNT>
+__device__ __forceinline__ void join_waves(const f64x4 (&acc)[COUNT], u32 wave, u32 from, u32 first, int count, double* room) {
+  const u32 lane = lane_id();
+  for (u32 w = 0; w < WAVES; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int n = 0; n < COUNT; ++n) {
+        if (n >= count) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          double& sum = room[256 * (first + n) + 64 * r + lane];
+          sum = w > from ? sum + acc[n][r] : acc[n][r];
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+template <class T, int KT, bool TALL>
+__global__ __launch_bounds__(kThreads) void k_gram_again(Batch<const T> g, const double* R, u32 k, u32 length, u32 parts, u32 parties, double* out) {
+  constexpr u32 N = 16 * KT, S = N + 2, TILES = KT * (KT + 1) / 2;
+  __shared__ __align__(16) double held[N * S];
+  static_assert(N * S >= 256 * TILES, "");
+  const auto [party, part] = place_of_block(blockIdx.x, parts, parties);
+  if (party >= parties) return;
+  const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const u32 pieces = (length + 15) / 16, first = (u32)((u64)pieces * part / parts), end = (u32)((u64)pieces * (part + 1) / parts);
+  R += (size_t)party * N * N;
+  for (u32 i = threadIdx.x; i < N * N; i += kThreads) held[i / N * S + i % N] = R[i];
+  __syncthreads();
+  // (the sums of eight rows of tiles are too many for one wavefront's registers: a pair of them shares its pieces)
+  constexpr bool kPairs = KT == 8;
+  constexpr int kRows = kPairs ? 6 : KT, kCount = tiles_below(kRows);
+  const T* const m = g.p + party * g.step;
+  f64x4 acc[kCount];
+  const bool second = kPairs && wave % 2;
+  if (second) gram_again<T, KT, TALL, kPairs ? kRows : 0, KT>(m, g.ld, held, k, length, first + wave / 2, end, kWaves / 2, acc);
+  else gram_again<T, KT, TALL, 0, kRows>(m, g.ld, held, k, length, kPairs ? first + wave / 2 : first + wave, end, kPairs ? kWaves / 2 : kWaves, acc);
+  __syncthreads();  // R's place is free
+  join_waves<kWaves>(acc, wave, second, second ? kCount : 0, second ? (int)TILES - kCount : kCount, held);
+  double* const to = out + ((size_t)party * parts + part) * N * N;
+  for (u32 at = threadIdx.x; at < 256 * TILES; at += kThreads) {
+    const u32 n = at / 256, i = tile_row(n), j = n - i * (i + 1) / 2, s = 16 * i + at % 256 / 16, t = 16 * j + at % 16;
+    to[s * N + t] = held[at];
+    if (i != j) to[t * N + s] = held[at];
+  }
+}
+// R P, of the polynomial so far, transposed, and the next part's, which is symmetric: the transpose of their product in its order. All of its
+// tiles: what is rounded on the way is not symmetric. `turned`: the product itself.
+template <u32 N>
+__global__ __launch_bounds__(kWave) void k_chain(const double* R, const double* P, u32 parties, u32 turned, double* out) {
+  constexpr u32 KT = N / 16;
+  const auto [party, tile] = place_of_block(blockIdx.x, KT * KT, parties);
+  if (party >= parties) return;
+  const u32 lane = lane_id(), i = tile / KT, j = tile % KT;
+  const size_t at = (size_t)party * N * N;
+  const f64x4 acc = tile_product<N>(R + at, P + at, i, j, N);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const u32 row = 16 * i + 4 * r + lane / 16, col = 16 * j + lane % 16;
+    out[at + (turned ? col * N + row : row * N + col)] = acc[r];
+  }
 }
 
 // More than 64 rows: K_0 and G's factor, from the parts; a block takes an eighth of a matrix, and each the parts' diagonals (16 parts of 8
@@ -461,7 +573,7 @@ constexpr u32 join_threads() {
   return 4 * N;
 }
 template <u32 N>
-__global__ __launch_bounds__(join_threads<N>()) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, double* K, double* factor) {
+__global__ __launch_bounds__(join_threads<N>()) void k_gram_join(const double* parts, u32 count, u32 parties, double eps, u32 again, double* K, double* factor) {
   __shared__ double room[join_threads<N>() / kWave];
   constexpr u32 kEach = N * N / kSlices / join_threads<N>();
   const auto [party, slice] = place_of_block(blockIdx.x, kSlices, parties);
@@ -474,7 +586,7 @@ __global__ __launch_bounds__(join_threads<N>()) void k_gram_join(const double* p
     sum_parts(parts, count, N * N, threadIdx.x * (N + 1), 0, d);
     squares = d[0];
   }
-  const double by = factor_of(block_sum<join_threads<N>()>(squares, room), eps);
+  const double by = again ? 1.0 : factor_of(block_sum<join_threads<N>()>(squares, room), eps);
 #pragma unroll
   for (u32 n = 0; n < kEach; ++n) K[(size_t)party * N * N + (slice * kEach + n) * join_threads<N>() + threadIdx.x] = s[n] * by * by;
   if (slice == 0 && threadIdx.x == 0) factor[party] = by;
@@ -656,8 +768,8 @@ template <class T>
 __device__ __forceinline__ Matrices<T> matrices_of(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>& out, u32 party) {
   return {g.p + party * g.step, base.p ? base.p + party * base.step : nullptr, out.p + party * out.step, g.ld, base.ld, out.ld};
 }
-// `from`: P; of one tile the parts' sums, from which each block's first wavefront forms the polynomial itself, which takes it no longer
-// than a launch (8 matrices of 16 x 4096 float32 13.5 us by three launches and 12.3 by two).
+// `from`: P; of one tile and with steps the parts' sums, from which each block's first wavefront forms the polynomial itself, which takes it no
+// longer than a launch (8 matrices of 16 x 4096 float32 13.5 us by three launches and 12.3 by two).
 struct Polynomial {
   const double* from;
   u32 count;
@@ -673,13 +785,13 @@ __global__ __launch_bounds__(kThreads) void k_apply(Batch<const T> g, Batch<cons
   if (party >= parties) return;
   const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const double* const from = poly.from + (size_t)party * poly.count * A::N * A::N;
-  if constexpr (KT == 1) {
+  if (KT == 1 && poly.steps.count) {
     __shared__ StepRoom<1> held;
     __shared__ double room[1];
     if (wave == 0) {
       double sums[4];
       sum_parts(from, poly.count, 256, threadIdx.x, kWave, sums);
-      steps_of<1>(poly.steps, poly.scale, poly.eps, held, room, sums, [&](u32 i, u32 j, double v) { P[i * A::S + j] = v; });
+      steps_of<1>(poly.steps, 0, poly.steps.count, poly.scale, poly.eps, false, held, room, sums, [&](u32 i, u32 j, double v) { P[i * A::S + j] = v; });
     }
   } else {
 #pragma unroll 8
@@ -706,13 +818,40 @@ __global__ __launch_bounds__(kOneThreads) void k_update(Batch<const T> g, Batch<
   gram<T, KT, TALL>(m.g, m.ldg, k, length, wave, (length + kChunk - 1) / kChunk, kOneWaves, wave, acc);
   gram_sums<KT, TALL, kOneWaves>(acc, wave, k, part, [&](u32 s, u32 t, double v) { sums[s * S + t] = v; });
   __syncthreads();
+  int end = steps.end(0);
   if (wave == 0) {
     double own[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) own[e] = sums[(4 * e + threadIdx.x / 16) * S + threadIdx.x % 16];
-    steps_of<KT>(steps, scale, eps, held, room, own, [&](u32 i, u32 j, double v) { sums[i * S + j] = v; });
+    steps_of<KT>(steps, 0, end, end == steps.count ? scale : 1.0, eps, false, held, room, own, [&](u32 i, u32 j, double v) { sums[i * S + j] = v; });
   }
   __syncthreads();
+  while (end < steps.count) {  // k_gram_again, k_steps and k_chain of the next part
+    const int first = end;
+    end = steps.end(first);
+    gram_again<T, KT, TALL, 0, KT>(m.g, m.ldg, sums, k, length, wave, (length + 15) / 16, kOneWaves, acc);
+    join_waves<kOneWaves>(acc, wave, 0, 0, 1, part[0][0]);
+    if (wave == 0) {
+      const u32 place = threadIdx.x % 16, group = threadIdx.x / 16;
+      double own[4], R[4], next[4];
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        own[e] = part[0][0][64 * e + threadIdx.x];
+        R[e] = sums[place * S + 4 * e + group];
+      }
+      steps_of<KT>(steps, first, end, end == steps.count ? scale : 1.0, eps, true, held, room, own, [&](u32, u32, double v) { next[n++] = v; });
+      f64x4 chain = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) chain = mma4(R[e], next[e], chain);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const u32 row = 4 * r + group;
+        sums[end == steps.count && !TALL ? place * S + row : row * S + place] = chain[r];
+      }
+    }
+    __syncthreads();
+  }
   apply<T, KT, TALL, WHOLE>(m, sums, k, length, keep, wave, kOneWaves);
 }
 
@@ -724,7 +863,7 @@ struct Shape {
 };
 constexpr size_t kOneLength = 768;
 struct Plan {  // parts 0: a block a matrix, and no workspace
-  size_t parts, gram, poly, factor, extra, total;
+  size_t parts, gram, poly, factor, chain, extra, total;
 };
 bool update_sizes(int type, size_t parties, size_t rows, size_t cols, Shape& s) {
   if (!valid_type(type) || parties > HAFLO_ADAPTER_MAX_PARTIES || rows < 1 || cols < 1 || rows > kMostCount || cols > kMostCount) return false;
@@ -746,21 +885,65 @@ Plan update_plan(const Shape& s) {
   const size_t each = s.side() * s.side() * 8;
   p.gram = 0;
   p.poly = p.gram + s.parties * p.parts * each;
-  p.factor = p.poly + (s.k <= 16 ? 0 : s.parties * each);
+  p.chain = p.poly + s.parties * each;  // two, of lists that are cut
+  p.factor = p.chain + 2 * s.parties * each;
   p.extra = p.factor + align256(s.parties * 8);
   p.total = s.k > 64 ? p.extra + 5 * s.parties * each : p.factor;
   return p;
 }
 
+// Where a list is cut: it may raise a direction by kMostWhole in one part (five steps of 3.4445 are 485, whose roundings are then below 2e-9 of what
+// is greatest, a thirtieth of a rounding to float32), and each part of a longer one by kMostEach (three are 41). Steps' factors a + b x + c x^2 are taken at their
+// greatest over what K's eigenvalues x can be: 0 .. `most`, and x (a + b x + c x^2)^2 after the step, whose slope is 0 where the factor
+// or a + 3 b x + 5 c x^2 is.
+constexpr double kMostWhole = 512.0, kMostEach = 48.0;
+u32 cuts_of(const Steps& steps) {
+  double grow[HAFLO_UPDATE_MAX_STEPS], most = 1.0;
+  for (int i = 0; i < steps.count; ++i) {
+    const double a = steps.c[i][0], b = steps.c[i][1], c = steps.c[i][2], last = most;
+    const auto factor = [&](double x) { return a + x * (b + c * x); };
+    double after = 0.0;
+    grow[i] = 1.0;
+    const auto look = [&](double x) {
+      if (!(x >= 0.0 && x <= last)) return;
+      const double f = fabs(factor(x));
+      if (!(f <= grow[i])) grow[i] = f;
+      if (!(x * f * f <= after)) after = x * f * f;
+    };
+    look(0.0);
+    look(last);
+    if (c != 0.0) {
+      const double root = sqrt(9.0 * b * b - 20.0 * a * c);
+      look(-b / (2.0 * c));
+      look((-3.0 * b + root) / (10.0 * c));
+      look((-3.0 * b - root) / (10.0 * c));
+    } else if (b != 0.0) {
+      look(-a / (3.0 * b));
+    }
+    most = after;
+    if (!(grow[i] < HUGE_VAL && most < HUGE_VAL)) grow[i] = most = HUGE_VAL;
+  }
+  double whole = 1.0, part = 1.0;
+  for (int i = 0; i < steps.count; ++i) whole *= grow[i];
+  u32 cuts = 0;
+  for (int i = 0; i < steps.count && !(whole <= kMostWhole); ++i) {
+    part *= grow[i];
+    if (i == 0 || part <= kMostEach) continue;
+    cuts |= 1u << (i - 1);
+    part = grow[i];
+  }
+  return cuts;
+}
+
 // scale P / (|G|_F + eps) of more than 64 rows, product by product
 template <u32 N>
-void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double scale, double eps, char* ws, hipStream_t st) {
+void large_steps(const Shape& s, const Plan& plan, const Steps& steps, double scale, double eps, bool again, double* to, char* ws, hipStream_t st) {
   const size_t each = s.parties * N * N * 8;
   const auto place = [&](int i) { return (double*)(ws + plan.extra + i * each); };
   double *const K = place(0), *const Q = place(1), *P = place(2), *const M = place(3), *spare = place(4);
-  double *const factor = (double*)(ws + plan.factor), *const to = (double*)(ws + plan.poly);
+  double* const factor = (double*)(ws + plan.factor);
   hipLaunchKernelGGL((k_gram_join<N>), dim3((unsigned)blocks_of(kSlices, s.parties)), dim3(join_threads<N>()), 0, st, (const double*)(ws + plan.gram), (u32)plan.parts,
-                     (u32)s.parties, eps, K, factor);
+                     (u32)s.parties, eps, (u32)again, K, factor);
   const auto run = [&](Products p, u32 jobs) {
     in_turns(blocks_of(jobs * large_tiles<N>(), s.parties), kWave,
              [&](u32 first, dim3 grid, dim3 block) { hipLaunchKernelGGL((k_products<N>), grid, block, 0, st, p, jobs, (u32)s.parties, first); });
@@ -812,13 +995,42 @@ void update(const Batch<const T>& g, const Batch<const T>& base, const Batch<T>&
   in_turns(blocks_of(plan.parts, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
     hipLaunchKernelGGL((k_gram<T, KT, TALL>), grid, block, 0, st, g, k, length, (u32)plan.parts, (u32)s.parties, sums, first);
   });
-  Polynomial from = {poly, 1, steps, scale, eps};
-  if constexpr (KT == 1)
+  const auto form = [&](const Steps& part, double by, bool again, double* to) {
+    if constexpr (KT <= 4)
+      hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)sums, (u32)plan.parts, part, by, eps, (u32)again, to);
+    else
+      large_steps<16 * KT>(s, plan, part, by, eps, again, to, ws, st);
+  };
+  Polynomial from = {poly, 1, {}, scale, eps};
+  if (steps.cuts) {
+    constexpr u32 N = 16 * KT;
+    double *R = (double*)(ws + plan.chain), *next = R + s.parties * N * N;
+    for (int first = 0, end; first < steps.count; first = end) {
+      end = steps.end(first);
+      const bool last = end == steps.count;
+      Steps part = {};
+      for (; part.count < end - first; ++part.count)
+        for (int j = 0; j < 3; ++j) part.c[part.count][j] = steps.c[first + part.count][j];
+      if (first == 0) {
+        form(part, 1.0, false, R);
+        continue;
+      }
+      // (few enough lanes for one launch each, as in k_gram_join)
+      hipLaunchKernelGGL((k_gram_again<T, KT, TALL>), dim3((unsigned)blocks_of(plan.parts, s.parties)), dim3(kThreads), 0, st, g, (const double*)R, k, length,
+                         (u32)plan.parts, (u32)s.parties, sums);
+      form(part, last ? scale : 1.0, true, poly);
+      hipLaunchKernelGGL((k_chain<N>), dim3((unsigned)blocks_of(KT * KT, s.parties)), dim3(kWave), 0, st, (const double*)R, (const double*)poly, (u32)s.parties,
+                         (u32)(last && !TALL), next);
+      double* const was = R;
+      R = next;
+      next = was;
+    }
+    from.from = R;
+  } else if constexpr (KT == 1) {
     from = {sums, (u32)plan.parts, steps, scale, eps};
-  else if constexpr (KT <= 4)
-    hipLaunchKernelGGL((k_steps<KT>), dim3((unsigned)s.parties), dim3(step_threads<KT>()), 0, st, (const double*)sums, (u32)plan.parts, steps, scale, eps, poly);
-  else
-    large_steps<16 * KT>(s, plan, steps, scale, eps, ws, st);
+  } else {
+    form(steps, scale, false, poly);
+  }
   const u32 blocks = apply_blocks(s, kWaves * Apply<KT, TALL>::kPlaces);
   in_turns(blocks_of(blocks, s.parties), kThreads, [&](u32 first, dim3 grid, dim3 block) {
     if (whole) hipLaunchKernelGGL((k_apply<T, KT, TALL, true>), grid, block, 0, st, g, base, out, from, k, length, keep, blocks, (u32)s.parties, first);
@@ -865,6 +1077,7 @@ int haflo_orthogonal_update(int type, const void* d_g, size_t ldg, size_t step_g
     if (!(fabs(coefficients[i]) < HUGE_VAL)) return HAFLO_EINVAL;
     list.c[i / 3][i % 3] = coefficients[i];
   }
+  list.cuts = cuts_of(list);
   if (parties == 0) return HAFLO_OK;
   if (!d_g || ldg < cols || !d_out || ldo < cols || (d_base && ldb < cols) || ldo > kMostDistance) return HAFLO_EINVAL;
   if (parties > 1 && step_o < (rows - 1) * ldo + cols) return HAFLO_EINVAL;  // matrices of the result over each other

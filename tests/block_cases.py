@@ -236,6 +236,84 @@ def check_update_orthogonal(run):
     assert float((x @ x.mT - torch.eye(12, dtype=torch.float64)).abs().max()) < 50 * 2.0 ** -23
 
 
+# Lists that raise directions by more than an adapter's gradient of a low rank bears at once: their steps are taken in parts
+POLAR = (1.875, -1.25, 0.375)
+LISTS = {"6": [QUINTIC] * 6, "8": [QUINTIC] * 8, "12": [QUINTIC] * 12, "16": [QUINTIC] * 16, "steep": [(6.0, -21.0, 16.0)] + [POLAR] * 9,
+         "first": [(3000.0, 0.0, 0.0), (1e-3, 0.0, 0.0)] + [POLAR] * 2, "polar": [POLAR] * 16, "both": [QUINTIC] * 3 + [POLAR] * 13, "cubic": [CUBIC] * 16}
+STEPS = [  # type, rows, cols, list, base
+    ("f32", 16, 256, "16", False), ("f32", 900, 16, "12", True), ("f32", 3, 1, "16", False), ("f32", 1000, 7, "16", False), ("f32", 16, 800, "steep", True),
+    ("f32", 20, 256, "16", False), ("f32", 256, 32, "12", False), ("f32", 48, 100, "8", True), ("f32", 90, 45, "16", False), ("f32", 64, 256, "8", False),
+    ("f32", 200, 64, "16", True), ("f32", 70, 100, "12", False), ("f32", 128, 140, "8", False), ("f32", 140, 128, "16", False), ("bf16", 20, 70, "16", True),
+    ("f16", 100, 66, "12", False), ("f32", 32, 256, "polar", False), ("f32", 60, 64, "both", False), ("f32", 64, 50, "steep", False),
+    ("f32", 33, 40, "first", True), ("f32", 300, 4, "first", False), ("f32", 33, 40, "6", False), ("f32", 33, 100, "cubic", True), ("bf16", 97, 128, "6", False),
+]
+
+
+def low_ranks(kind, rows, cols, seed=0):
+    """Matrices of rank 1 in whole numbers, of rank 3, of equal rows, and one whose directions go down to a thousandth of the strongest."""
+    gen = torch.Generator().manual_seed(seed + rows * 23 + cols)
+    n = lambda *s: torch.randn(*s, generator=gen)  # noqa: E731
+    whole = torch.randint(-8, 9, (rows, 1), generator=gen) * torch.randint(-8, 9, (1, cols), generator=gen)
+    whole[0, 0] = 1
+    short = min(rows, cols)
+    weak = torch.logspace(0, -3, short)
+    full = n(rows, cols) * (weak if cols == short else weak[:, None])
+    return torch.stack([whole.float(), n(rows, 3) @ n(3, cols), n(1, cols).expand(rows, cols), full]).to(TYPES[kind])
+
+
+def update_longer(g, steps, eps):
+    """X product by product in 80 bits, and for each matrix what the steps raise a direction by: the product of their greatest factors on the
+    singular values, with zero, that there are."""
+    import numpy as np
+    out, raised = [], []
+    for m in g:
+        x = m.double().numpy().astype(np.longdouble)
+        x = x / (np.sqrt((x * x).sum()) + np.longdouble(eps))
+        tall = x.shape[0] > x.shape[1]
+        x = x.T if tall else x
+        values, most = np.append(np.linalg.svd(x.astype(np.float64), compute_uv=False), 0.0), 1.0
+        for a, b, c in steps:
+            factor = a + b * values ** 2 + c * values ** 4
+            values, most = values * factor, most * max(1.0, float(abs(factor).max()))
+            k = x @ x.T
+            x = np.longdouble(a) * x + (np.longdouble(b) * k + np.longdouble(c) * (k @ k)) @ x
+        out.append(torch.from_numpy((x.T if tall else x).astype(np.float64)))
+        raised.append(most)
+    return torch.stack(out), torch.tensor(raised, dtype=torch.float64)[:, None, None]
+
+
+def check_update_steps(run, kind, rows, cols, name, base, eps=1e-7):
+    g, steps, keep, scale = low_ranks(kind, rows, cols), LISTS[name], 0.9, -0.3
+    held = torch.randn(g.shape, generator=torch.Generator().manual_seed(rows)).to(g.dtype) if base else None
+    x, raised = update_longer(g, steps, eps)
+    want = scale * x + (0.0 if held is None else keep * held.double())
+    got = run.orthogonal_update(g, held, keep, scale, steps, eps)
+    # As in check_update, and a rounding of 2^-53 in each of three products a step, of sums of min(rows, cols), which the steps raise; of what they
+    # multiply, X's greatest column (or row)
+    norm = torch.linalg.vector_norm(g.double(), dim=(1, 2), keepdim=True)
+    wide = torch.linalg.vector_norm(g.double(), dim=1 if rows <= cols else 2).amax(1)[:, None, None] / norm
+    room = 3 * len(steps) * min(rows, cols) * 2.0 ** -53 * raised * wide
+    near(got, want, (UNIT[g.dtype] + ULP) * want.abs() + abs(scale) * (2.0 ** -31 * x.abs().amax((1, 2), keepdim=True) + room) + TINY[g.dtype])
+
+
+def check_update_steps_special(run):
+    """check_update_special's matrices, each by itself, with steps that are taken in parts, and rows that lie further apart."""
+    for rows, cols in ((5, 40), (900, 6), (50, 24), (70, 80)):
+        gen = torch.Generator().manual_seed(rows)
+        wide = torch.randn(6, rows, cols + 3, generator=gen)
+        g = wide[:, :, :cols]
+        g[1], g[2, 3, 4], g[3, 0, 0] = 0.0, math.nan, math.inf
+        g[4] *= 2.0 ** 100
+        g[5] *= 2.0 ** -100
+        steps, eps = LISTS["12"], 2.0 ** -140
+        got = run.orthogonal_update(g, None, 1.0, 1.0, steps, eps)
+        assert not got[1].any() and bool(got[2].isnan().all()) and bool(got[3].isnan().all())
+        fine = [0, 4, 5]
+        want, raised = update_longer(g[fine], steps, eps)
+        # (what is not of a low rank has no directions that only roundings raise)
+        near(got[fine], want, 2 * ULP * want.abs() + 2.0 ** -31)
+
+
 # --------------------------------------------------------------------------------------------------- eight bits
 
 INT8 = [  # type, rows, inner, outer, pad, bias, residual

@@ -130,6 +130,15 @@ def test_update(run, case):
     cases.check_update(run, *case)
 
 
+@pytest.mark.parametrize("case", cases.STEPS, ids=str)
+def test_update_steps(run, case):
+    cases.check_update_steps(run, *case)
+
+
+def test_update_steps_special(run):
+    cases.check_update_steps_special(run)
+
+
 def test_update_special(run):
     cases.check_update_special(run)
 
@@ -324,6 +333,21 @@ def test_launches_in_turns(run):
     cases.check_update(narrow, "f32", 150, 2, 800, True, [cases.QUINTIC], 0)
     cases.check_update(narrow, "bf16", 3, 70, 66, True, [cases.QUINTIC] * 2, 0)
     cases.check_norm(narrow, "bf16", 2, 70000, 0, 0, True, True, "cols", True, 1.0)
+
+
+def test_update_steps_in_place(run):
+    """Steps that are taken in parts read G again before any result is written: over G and over the base the results are the same."""
+    lib, steps = run.lib, cases.LISTS["8"]
+    values = (C.c_double * 24)(*(v for s in steps for v in s))
+    for rows, cols in ((6, 50), (50, 6), (16, 900), (20, 90), (90, 20), (70, 75)):
+        g, held = cases.update_inputs("f32", 2, rows, cols, True, 0)
+        want = run.orthogonal_update(g, held, 0.9, -0.3, steps, 1e-7)
+        ws, nbytes = run.workspace(lib.haflo_update_workspace_bytes(0, 2, rows, cols))
+        for over in (0, 1):
+            b = [run.buf(g), run.buf(held)]
+            assert lib.haflo_orthogonal_update(0, b[0].p, cols, rows * cols, b[1].p, cols, rows * cols, 2, rows, cols, values, 8, 0.9, -0.3, 1e-7, b[over].p, cols,
+                                               rows * cols, ws.p, nbytes, None) == 0
+            assert torch.equal(b[over].get(), want)
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])

@@ -67,6 +67,15 @@ def test_update(run, case):
     cases.check_update(run, *case)
 
 
+@pytest.mark.parametrize("case", cases.STEPS, ids=str)
+def test_update_steps(run, case):
+    cases.check_update_steps(run, *case)
+
+
+def test_update_steps_special(run):
+    cases.check_update_steps_special(run)
+
+
 def test_update_special(run):
     cases.check_update_special(run)
 
@@ -236,6 +245,40 @@ def test_in_place_and_slices(api):
         keep = res.clone()
         api.haflo_int8_forward(x, q, s, residual=res[:, 3:48], out=res[:, 3:48])
         assert torch.equal(res[:, 3:48], want) and torch.equal(res[:, :3], keep[:, :3]) and torch.equal(res[:, 48:], keep[:, 48:])
+
+
+def test_update_steps_again_and_in_a_graph(api):
+    """Steps that are taken in parts: the same bits on a busy card, over the operands, and from two captured graphs on new contents."""
+    steps = cases.LISTS["16"]
+    for shape in ((3, 16, 600), (3, 900, 12), (2, 40, 300), (2, 333, 64), (2, 80, 500), (2, 500, 128)):
+        print(shape, flush=True)
+        g, base = torch.randn(shape, device="cuda"), torch.randn(shape, device="cuda")
+        run = lambda out=None: api.haflo_orthogonal_update(g, base, 0.9, -0.1, steps, out=out)  # noqa: E731
+        want, side = run(), torch.cuda.Stream()
+        assert torch.equal(api.haflo_orthogonal_update(g, base, 0.9, -0.1, steps, out=g.clone()), want)
+        assert torch.equal(api.haflo_orthogonal_update(g.clone(), base, 0.9, -0.1, steps, out=base.clone()), want)
+        wide = torch.zeros((shape[0], shape[1] + 1, shape[2] + 5), device="cuda")
+        wide[:, 1:, 2:-3] = g
+        assert torch.equal(api.haflo_orthogonal_update(wide[:, 1:, 2:-3], base, 0.9, -0.1, steps), want)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            run()
+        side.synchronize()
+        graphs = []
+        for _ in range(2):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                out = run()
+            graphs.append((graph, out))
+        for k in range(3):
+            g.copy_(torch.randn(shape, generator=torch.Generator().manual_seed(k)))
+            torch.cuda.synchronize()
+            want = run()
+            torch.cuda.synchronize()
+            for graph, _ in graphs:
+                graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(out, want) for _, out in graphs)
 
 
 def test_far_offsets(api):
