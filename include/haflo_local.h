@@ -21,7 +21,7 @@
  *
  * Matrices are row-major; `ld*` is the distance between rows in elements, at
  * least the row's length. Elements need no more alignment than their type's, a workspace that of 16 bytes (else HAFLO_EINVAL). Outputs
- * may not overlap inputs except where it says so. Counts are below 2^31.
+ * may not overlap inputs except where it says so, and there from the same address on; that they do not overlap otherwise is not looked for. Counts are below 2^31.
  */
 #ifndef HAFLO_LOCAL_H
 #define HAFLO_LOCAL_H
@@ -183,7 +183,10 @@ int haflo_quantize_rows(int type, const void* d_x, size_t ldx, size_t rows, size
 int haflo_int8_product(int type, const int8_t* d_xq, const float* d_x_scale, const int8_t* d_wq, const float* d_w_scale,
                        const float* d_bias, const void* d_residual, size_t ldr, size_t rows, size_t inner, size_t outer,
                        void* d_y, size_t ldy, void* stream);
-/* The same of x (type, rows x inner), which is brought to eight bits first, in the workspace. */
+/*
+ * The same of x (type, rows x inner), which is brought to eight bits first, in the workspace. d_y may be d_x too, however far apart the rows of
+ * either; the workspace is then at least that of 17 rows (else HAFLO_EINVAL), as calls of up to 16 rows may need none otherwise.
+ */
 size_t haflo_int8_workspace_bytes(int type, size_t rows, size_t inner, size_t outer);
 int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq, const float* d_w_scale,
                        const float* d_bias, const void* d_residual, size_t ldr, size_t rows, size_t inner, size_t outer,

@@ -661,14 +661,16 @@ def haflo_int8_product(xq, x_scale, wq, w_scale, cols, dtype=torch.float32, bias
 
 def haflo_int8_forward(x, wq, w_scale, bias=None, residual=None, out=None):
     """haflo_int8_product of x, whose rows are brought to eight bits within the call: the projection with weights of eight bits that the
-    common model answers with. It is not trained through. The result is of x's type."""
+    common model answers with. It is not trained through. The result is of x's type; `out` may be the residual, x, or both."""
     stream = _stream_of(x, wq, w_scale, bias, residual, out)
     dtype = x.dtype
     kind, (rows, inner, ldx) = _type(x), _matrix(x, dtype)
     outer, pw, pws, pb = _int8_weights(wq, w_scale, inner, bias)
     ldr = outer if residual is None else _matrix(residual, dtype, rows, outer)[2]
     y, ldy = _result(x, rows, outer, out)
-    nbytes = lib().haflo_int8_workspace_bytes(kind, rows, inner, outer)
+    # (over x, calls of up to 16 rows need a workspace too)
+    over = out is not None and rows < 17 and y.data_ptr() == x.data_ptr()
+    nbytes = lib().haflo_int8_workspace_bytes(kind, 17 if over else rows, inner, outer)
     pws2, ws = _scratch(nbytes, x)
     _check(lib().haflo_int8_forward(kind, x.data_ptr(), ldx, pw, pws, pb, None if residual is None else residual.data_ptr(), ldr, rows, inner, outer,
                                     y.data_ptr(), ldy, pws2, nbytes, stream))

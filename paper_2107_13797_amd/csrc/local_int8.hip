@@ -375,9 +375,10 @@ bool aligned(const void* p) { return p && (uintptr_t)p % 16 == 0; }
 struct Plan {
   size_t scale, total;
 };
-Plan int8_plan(size_t rows, size_t inner, size_t outer) {
+// `over`: the result lies over x, whose rows then have to be in eight bits before any block writes
+Plan int8_plan(size_t rows, size_t inner, size_t outer, bool over) {
   Plan p = {0, 0};
-  if (own_rows(rows, inner, outer)) return p;
+  if (!over && own_rows(rows, inner, outer)) return p;
   p.scale = align256(rows * row_bytes(inner));
   p.total = p.scale + align256(rows * 4);
   return p;
@@ -409,7 +410,7 @@ int haflo_int8_product(int type, const int8_t* d_xq, const float* d_x_scale, con
 }
 
 size_t haflo_int8_workspace_bytes(int type, size_t rows, size_t inner, size_t outer) {
-  return int8_sizes(type, rows, inner, outer) ? int8_plan(rows, inner, outer).total : (size_t)-1;
+  return int8_sizes(type, rows, inner, outer) ? int8_plan(rows, inner, outer, false).total : (size_t)-1;
 }
 
 int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq, const float* d_w_scale, const float* d_bias, const void* d_residual,
@@ -419,7 +420,7 @@ int haflo_int8_forward(int type, const void* d_x, size_t ldx, const int8_t* d_wq
   if (rows == 0) return HAFLO_OK;
   if (!d_x || ldx < inner || !aligned(d_wq) || !d_w_scale || (d_residual && ldr < outer) || !d_y || ldy < outer) return HAFLO_EINVAL;
   if (!in_place(d_residual, ldr, d_y, ldy, rows)) return HAFLO_EINVAL;
-  const Plan plan = int8_plan(rows, inner, outer);
+  const Plan plan = int8_plan(rows, inner, outer, d_y == d_x);
   if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;
   int8_t* const xq = (int8_t*)d_workspace;
   float* const x_scale = (float*)((char*)d_workspace + plan.scale);

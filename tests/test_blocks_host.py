@@ -82,3 +82,13 @@ def test_distances(api):
     x = OnDevice(torch.zeros(4, 30)[:, 3:11], 0)
     q, s = api.haflo_quantize_rows(x)
     assert api.reached[-1][1][1:5] == (x.data_ptr(), 30, 4, 8) and q.shape == (4, 128) and s.shape == (4,)
+
+
+def test_int8_workspace_over_its_rows(api):
+    """Where the result lies over x, the binding asks for the workspace of 17 rows or more."""
+    q, s = (OnDevice(torch.zeros(*n, dtype=t), 0) for n, t in (((8, 128), torch.int8), ((8,), torch.float32)))
+    for rows, over, want in ((3, False, 3), (3, True, 17), (40, True, 40), (40, False, 40)):
+        x = OnDevice(torch.zeros(rows, 8), 0)
+        api.haflo_int8_forward(x, q, s, out=x if over else OnDevice(torch.zeros(rows, 8), 0))
+        name, args = api.reached[-2]
+        assert name == "haflo_int8_workspace_bytes" and args == (0, want, 8, 8)

@@ -207,6 +207,31 @@ def test_in_place(run):
         assert torch.equal(b[4].get(), want)
 
 
+OVER_X = [(kind, rows, width, outer) for kind in ("f32", "bf16") for rows in (1, 2, 8, 16, 17, 40) for width, outer in ((256, 256), (300, 45), (2048, 64))]
+
+
+@pytest.mark.parametrize("case", OVER_X, ids=str)
+def test_int8_over_its_rows(run, case):
+    """A result over x, with x for a residual and without, is what it is elsewhere, whatever the number of rows; the workspace is then that of
+    17 rows or more, and a call without it is refused."""
+    kind, rows, width, outer = case
+    lib = run.lib
+    x, w, bias, _ = cases.int8_inputs(kind, rows, width, outer, 0, True, False)
+    q, s = run.quantize_rows(w)
+    number = NAMES[x.dtype]
+    ws, nbytes = run.workspace(lib.haflo_int8_workspace_bytes(number, max(rows, 17), width, outer))
+    for with_x in (False, True):
+        want = run.int8_forward(x, q, s, bias, x[:, :outer] if with_x else None)
+        b = [run.buf(t) for t in (x, q, s, bias)]
+        px, pq, ps, pb = (v.p for v in b)
+        call = lambda w, n: lib.haflo_int8_forward(number, px, width, pq, ps, pb, px if with_x else None, width, rows, width, outer, px, width, w, n, None)  # noqa: E731
+        assert call(None, 0) == -1 and call(ws.p, nbytes // 32) == -1
+        assert torch.equal(b[0].get(), x)
+        assert call(ws.p, nbytes) == 0
+        got = b[0].get()
+        assert torch.equal(got[:, :outer], want) and torch.equal(got[:, outer:], x[:, outer:])
+
+
 def test_some_gradients(run):
     """Gradients that are not asked for change nothing about the others; what r has from elsewhere may be nothing."""
     lib = run.lib

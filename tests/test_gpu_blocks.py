@@ -281,6 +281,20 @@ def test_update_steps_again_and_in_a_graph(api):
             assert all(torch.equal(out, want) for _, out in graphs)
 
 
+def test_int8_over_its_rows(api):
+    """A result over x, with x for a residual and without, and over a part of its columns."""
+    for rows in (1, 2, 8, 16, 17, 40, 300):
+        for width, outer in ((256, 256), (2048, 2048), (2048, 64), (300, 45)):
+            x, w = torch.randn(rows, width, device="cuda").bfloat16(), torch.randn(outer, width, device="cuda").bfloat16()
+            q, s = api.haflo_quantize_rows(w)
+            for residual in (False, True):
+                want = api.haflo_int8_forward(x, q, s, residual=x[:, :outer] if residual else None)
+                y = x.clone()
+                part = y[:, :outer]
+                assert api.haflo_int8_forward(y, q, s, residual=part if residual else None, out=part) is part
+                assert torch.equal(part, want) and torch.equal(y[:, outer:], x[:, outer:])
+
+
 def test_far_offsets(api):
     """Elements past 2^31 and bytes past 2^32 in one array: the last rows are what they are by themselves."""
     rows, cols = 70001, 32768
