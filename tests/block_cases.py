@@ -404,6 +404,36 @@ def check_int8_limits(run):
     near(got, want, 5 * ULP * want.abs())
 
 
+INT8_SCALES = [(2, 300, 40), (16, 2048, 20), (20, 2100, 18), (40, 300, 70)]
+INT8_SCALES_LARGE = [(300, 600, 2050), (2050, 200, 2050), (4097, 300, 4097)]
+
+
+def check_int8_scales(run, rows, inner, outer):
+    """Scales whose product alone is below the least normal number, or above the greatest, where the results are ordinary: each sum is a whole
+    number times both."""
+    gen = torch.Generator().manual_seed(rows)
+    for kind in (torch.float32, torch.bfloat16):
+        x, w = torch.randn(rows, inner, generator=gen), torch.randn(outer, inner, generator=gen)
+        x[0], w[0] = 1.0, 1.0
+        x[1], w[1] = 0.0, 0.0
+        x[1, :2], w[1, 0], w[1, 1] = 1.0, 1.0, -1.0  # (against each other a sum of zero)
+        for by_x, by_w in ((2.0 ** -60, 2.0 ** -60), (2.0 ** -20, 2.0 ** -98), (2.0 ** 90, 2.0 ** -95), (2.0 ** 60, 2.0 ** 100)):
+            wq, ws = run.quantize_rows((w * by_w).to(kind))
+            xq, xs = eight_bits((x * by_x).to(kind))
+            ww, _ = eight_bits((w * by_w).to(kind))
+            got = run.int8_forward((x * by_x).to(kind), wq, ws, None, None)
+            want = xs.double()[:, None] * ws.double() * (xq.double() @ ww.double().T)
+            assert float(want[1, 1]) == 0.0 and float(got[1, 1]) == 0.0
+            most, greatest = want.abs(), torch.finfo(kind).max
+            want = torch.where(most > greatest, want.sign() * math.inf, want)
+            clear = (most / greatest - 1.0).abs() > 2.0 ** -6  # (not within a rounding of the greatest number)
+            room = torch.where(most > greatest, 0.0, UNIT[kind] * most + 5 * ULP * most + TINY[kind])
+            near(torch.where(clear, got.double(), 0.0), torch.where(clear, want, 0.0), room)
+    # a row whose scale is below the least number is zero whatever the weights are
+    wq, ws = run.quantize_rows(torch.full((outer, inner), 2.0 ** 127))
+    assert not run.int8_forward(torch.full((rows, inner), 2.0 ** -149), wq, ws, None, None).any()
+
+
 # --------------------------------------------------------------------------------------------------- each kernel form
 
 def norm_forms(kind):

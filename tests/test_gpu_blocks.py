@@ -98,6 +98,11 @@ def test_int8(run, case):
     cases.check_int8(run, *case)
 
 
+@pytest.mark.parametrize("case", cases.INT8_SCALES + cases.INT8_SCALES_LARGE, ids=str)
+def test_int8_scales(run, case):
+    cases.check_int8_scales(run, *case)
+
+
 def test_int8_limits(run):
     cases.check_int8_limits(run)
 
