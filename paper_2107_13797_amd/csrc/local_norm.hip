@@ -138,7 +138,7 @@ __global__ __launch_bounds__(MOST) void k_norm(Norm<T> n, u32 lanes, T* r_out, s
     if (MODE != kStream) store_cols(r_out + row * ldr, col, n.cols, rounded<T>(r));
     if (n.pre) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r.v[j] *= t * pre.v[j];
+      for (int j = 0; j < 8; ++j) r.v[j] = r.v[j] * t * pre.v[j];  // (t pre may be below the normal numbers)
       store_cols(h_out + row * ldh, col, n.cols, rounded<T>(r));
     }
     if (col == 0) {
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kMostLanes) void k_norm_long(Norm<T> n, T* r_out, s
       if (n.pre) {
         const Eight pre = gains(n.pre, col, n.cols);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.v[j] *= t * pre.v[j];
+        for (int j = 0; j < 8; ++j) r.v[j] = r.v[j] * t * pre.v[j];
         store_cols(h_out + row * ldh, col, n.cols, rounded<T>(r));
       }
     }

@@ -136,6 +136,21 @@ def check_norm_special(run):
         assert bool(dpre.isnan().all()) and bool(dpost.isnan().any())
 
 
+def check_norm_far(run):
+    """Rows near the greatest numbers with small gains, and the least with large ones: no factor of h alone leaves the normal numbers by far."""
+    for cols in (5, 64, 1001, 9001):
+        gen = torch.Generator().manual_seed(cols)
+        unit = torch.randn(4, cols, generator=gen).clamp(-3.0, 3.0)
+        for kind in (torch.float32, torch.bfloat16):
+            for size, gain in ((2.0 ** 125, 1e-3), (2.0 ** 120, 1e-4), (2.0 ** 126, 1e-12), (2.0 ** -100, 1e5)):
+                x, pre = (unit * size).to(kind), torch.full((cols,), gain) * (1.0 + torch.rand(cols, generator=gen))
+                for f in (None, torch.zeros(4, cols, dtype=kind)):
+                    want, most, _ = norm_exact(x, f, None, None, pre, None, None, 1.0, 2.0 ** -240)
+                    _, h, _ = run.residual_norm(x, f, None, None, pre, 1.0, 2.0 ** -240)
+                    # as in check_norm: the root, which below the normal numbers has 21 bits, is within two of its twelve
+                    near(h, want["h"], UNIT[kind] * want["h"].abs() + 12 * ULP * most["h"] + TINY[kind])
+
+
 def check_norm_gradients(run):
     """Against differences of the forward call along each gradient, in float32; the third derivative and the results' roundings bound how
     far the quotient is off."""

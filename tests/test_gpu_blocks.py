@@ -58,6 +58,10 @@ def test_norm_special(run):
     cases.check_norm_special(run)
 
 
+def test_norm_far(run):
+    cases.check_norm_far(run)
+
+
 def test_norm_gradients(run):
     cases.check_norm_gradients(run)
 
