@@ -122,7 +122,7 @@ int haflo_label_logprobs_backward(int type, const void* d_logits, size_t ld, con
  * NULL: only h, of r = x, and scale has to be 1; not both NULL.
  * d_post, d_pre: float32[cols]. d_rstd: float32, 2 x rows, both roots' reciprocals (1 where there is no norm), which the
  * backward pass takes. h is formed from r before its rounding; means of squares are held in 64 bits. d_r and d_h may each be one of the
- * inputs where the distances between rows are the same (else HAFLO_EINVAL). cols >= 1, eps > 0, finite.
+ * inputs where the distances between rows are the same (else HAFLO_EINVAL). cols >= 1; 2^-254 <= eps, finite; scale finite in float32.
  */
 int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, size_t ldf, const float* d_post,
                         const void* d_gate, size_t ldg, const float* d_gate_cols, const float* d_pre, size_t rows,

@@ -528,7 +528,7 @@ def haflo_residual_norm(x, f=None, post=None, gate=None, pre=None, scale=1.0, ep
     (f itself without `post`), and h = r / sqrt(mean r^2 + eps) pre. x: the stream before the block, f: what the block gave (None: r
     is x), gate: float32 [cols] for all rows, or a matrix of x's type, or None; post, pre: float32 [cols] or None. Returns r (None without f), h
     (None without pre) and, for haflo_residual_norm_backward, both roots' reciprocals (float32 [2, rows]); autograd records nothing.
-    `out` and `normed`, what r and h are written to, may each be one of the inputs."""
+    `out` and `normed`, what r and h are written to, may each be one of the inputs; eps is 2^-254 at least."""
     stream = _stream_of(x, f, post, gate, pre, out, normed)
     kind, rows, cols, operands = _norm_operands(x, f, post, gate, pre)
     r, ldr = (None, cols) if f is None else _result(x, rows, cols, out)

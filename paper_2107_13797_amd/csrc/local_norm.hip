@@ -460,6 +460,8 @@ Plan back_plan(size_t rows, size_t cols) {
   p.total = p.means + (cols <= kRowCols ? 0 : align256(2 * rows * 4));
   return p;
 }
+constexpr double kLeastEps = 0x1p-254;  // a row of zeros has the root's reciprocal 2^127
+bool finite_scale(double scale) { return fabs((float)scale) < HUGE_VAL; }
 bool norm_sizes(int type, size_t rows, size_t cols) { return valid_type(type) && rows <= kMostCount && cols >= 1 && cols <= kMostCount; }
 
 template <class T, int MODE>
@@ -497,7 +499,7 @@ extern "C" {
 int haflo_residual_norm(int type, const void* d_x, size_t ldx, const void* d_f, size_t ldf, const float* d_post, const void* d_gate, size_t ldg,
                         const float* d_gate_cols, const float* d_pre, size_t rows, size_t cols, double scale, double eps, void* d_r, size_t ldr,
                         void* d_h, size_t ldh, float* d_rstd, void* stream) {
-  if (!norm_sizes(type, rows, cols) || !(eps > 0.0 && eps < HUGE_VAL) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
+  if (!norm_sizes(type, rows, cols) || !(eps >= kLeastEps && eps < HUGE_VAL) || !finite_scale(scale)) return HAFLO_EINVAL;
   if (rows == 0) return HAFLO_OK;
   if ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols)) return HAFLO_EINVAL;
   if (!d_x || ldx < cols || (d_f && (ldf < cols || !d_r || ldr < cols)) || (d_gate && ldg < cols) || (d_pre && (!d_h || ldh < cols)) || !d_rstd)
@@ -533,7 +535,7 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
                                  const float* d_rstd, size_t rows, size_t cols, double scale, void* d_dx, size_t lddx, void* d_df, size_t lddf,
                                  void* d_dgate, size_t lddg, float* d_dgate_cols, float* d_dpost, float* d_dpre, void* d_workspace,
                                  size_t workspace_bytes, void* stream) {
-  if (!norm_sizes(type, rows, cols) || !(fabs(scale) < HUGE_VAL)) return HAFLO_EINVAL;
+  if (!norm_sizes(type, rows, cols) || !finite_scale(scale)) return HAFLO_EINVAL;
   if ((d_dpost && !d_post) || (d_dpre && !d_pre) || (d_dgate_cols && !d_gate_cols)) return HAFLO_EINVAL;  // gradients of what is not there
   // (matrices of no rows may have no address)
   if (rows && ((!d_f && (!d_pre || d_post || d_gate || d_gate_cols || scale != 1.0)) || (d_gate && d_gate_cols) || (d_dgate && !d_gate) || (d_df && !d_f)))

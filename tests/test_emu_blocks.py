@@ -260,6 +260,24 @@ def test_some_gradients(run):
                 assert torch.equal(o.get(), w) if a else bool((o.get() == 9).all())
 
 
+def test_norm_least_eps_and_greatest_scale(run):
+    """Roots' reciprocals and the scale are float32: what leaves them infinite is refused, and with the least eps a row of zeros gives zeros."""
+    lib = run.lib
+    b = run.buf(torch.zeros(256))
+    p, q = b.p, b.p + 512
+    for scale, eps, code in ((1.0, 2.0 ** -254, 0), (1.0, 2.0 ** -255, -1), (1.0, 5e-324, -1), (3.4028234663852886e38, 1e-6, 0), (-3.5e38, 1e-6, -1), (1e200, 1e-6, -1)):
+        assert lib.haflo_residual_norm(0, p, 8, p, 8, p, None, 8, None, p, 2, 8, scale, eps, q, 8, q + 128, 8, q + 256, None) == code, (scale, eps)
+        if eps == 1e-6:
+            assert lib.haflo_residual_norm_backward(0, p, 8, None, 8, p, 8, p, 8, p, None, 8, None, p, p, 2, 8, scale, q, 8, None, 8, None, 8, None, None, None,
+                                                    q + 128, 256, None) == code, scale
+    for cols in (40, 9000):
+        zero, ones = torch.zeros(2, cols), torch.ones(cols)
+        r, h, rstd = run.residual_norm(zero, zero, ones, ones, ones, 1.0, 2.0 ** -254)
+        assert not r.any() and not h.any() and bool((rstd == 2.0 ** 127).all())
+        grads = run.residual_norm_backward(torch.full((2, cols), 2.0 ** -100), None, zero, zero, ones, 0.0 * ones, ones, rstd, 1.0)
+        assert not any(bool(g.isnan().any()) for g in grads)
+
+
 def test_nothing_to_do(run):
     """No rows, no matrices: gradients summed over rows are zeros, nothing else is touched."""
     lib = run.lib
