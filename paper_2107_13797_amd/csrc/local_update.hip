@@ -627,6 +627,18 @@ __global__ __launch_bounds__(kWave) void k_products(Products p, u32 jobs, u32 pa
   }
 }
 
+// A result rounded once. On the way to 16 bits float32 takes it towards zero, and its last bit says whether anything was cut off: with more than two
+// bits behind those of the type the second rounding is then as one of the whole number.
+template <class T>
+__device__ __forceinline__ T once(double v) {
+  const float near = (float)v;
+  if (sizeof(T) == 4) return (T)near;
+  const double back = (double)near;
+  u32 bits = __builtin_bit_cast(u32, near);
+  if (back != v) bits = (bits - (fabs(back) > fabs(v) ? 1u : 0u)) | 1u;
+  return (T)__builtin_bit_cast(float, bits);
+}
+
 // out = keep base + P G, P in LDS with rows N + 2 apart: a wavefront takes `kPlaces` places of the long side by the whole short side at a
 // time, pieces piece, piece + stride .., and asks for the next ones before it multiplies. Past the short side P is 0 against
 // everything before it, so that any numbers may stand there. WHOLE: no load or store is cut by the short side's end. 64 matrices of
@@ -696,7 +708,7 @@ __device__ __forceinline__ void apply(const Matrices<T>& m, const double* P, u32
         const u32 l = at + 4 * r + group;
         T now[KT];
 #pragma unroll
-        for (int j = 0; j < KT; ++j) now[j] = (T)(float)(m.base ? keep * (double)(float)was[r][j] + acc[j][r] : acc[j][r]);
+        for (int j = 0; j < KT; ++j) now[j] = once<T>(m.base ? keep * (double)(float)was[r][j] + acc[j][r] : acc[j][r]);
         if (l < length) store_few<T, KT>(m.out + (size_t)l * m.ldo, s, k, now);
       }
     }
@@ -757,7 +769,7 @@ __device__ __forceinline__ void apply(const Matrices<T>& m, const double* P, u32
           const u32 s = 16 * i + 4 * r + group;
           T now[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) now[j] = (T)(float)(m.base ? keep * (double)(float)was[r][j] + acc[i][j][r] : acc[i][j][r]);
+          for (int j = 0; j < V; ++j) now[j] = once<T>(m.base ? keep * (double)(float)was[r][j] + acc[i][j][r] : acc[i][j][r]);
           if (s < k) store_few<T, V>(m.out + (size_t)s * m.ldo, l, length, now);
         }
       }

@@ -329,6 +329,24 @@ def check_update_steps_special(run):
         near(got[fine], want, 2 * ULP * want.abs() + 2.0 ** -31)
 
 
+def check_update_rounds_once(run):
+    """Results next to a border between two numbers of 16 bits, which a rounding to 32 bits on the way would put on it; of every form of the products."""
+    for kind in (torch.float16, torch.bfloat16):
+        u = UNIT[kind]
+        for rows, cols in ((5, 40), (40, 5), (5, 900), (900, 5), (20, 41), (41, 20), (39, 40), (60, 64), (64, 50), (70, 81), (81, 70), (100, 101), (101, 100)):
+            g, base = torch.zeros(1, rows, cols, dtype=kind), torch.ones(1, rows, cols, dtype=kind)
+            for keep, want in ((1 + u + 2.0 ** -40, 1 + 2 * u), (1 + u - 2.0 ** -40, 1), (1 + 3 * u - 2.0 ** -40, 1 + 2 * u), (-1 - 3 * u + 2.0 ** -40, -1 - 2 * u),
+                               (-1 - u - 2.0 ** -40, -1 - 2 * u), (1 + u, 1), (1 + 3 * u, 1 + 4 * u)):
+                got = run.orthogonal_update(g, base, keep, 1.0, [QUINTIC], 1e-7)
+                assert bool((got.double() == want).all()), (kind, rows, cols, keep)
+        # the greatest, the least, and what has no value
+        base[0, 0, :6] = torch.tensor([torch.finfo(kind).max, torch.finfo(kind).smallest_normal * 2 * u, math.inf, -math.inf, math.nan, -0.0]).to(kind)
+        got = run.orthogonal_update(g, base, 1.0, 1.0, [QUINTIC], 1e-7)
+        assert torch.equal(got.nan_to_num(7.0), base.nan_to_num(7.0))
+        got = run.orthogonal_update(g, base, 1.0 + 2.0 * u, 1.0, [QUINTIC], 1e-7)[0, 0, :5]
+        assert float(got[0]) == math.inf and torch.equal(got[1:4], base[0, 0, 1:4]) and bool(got[4].isnan())
+
+
 # --------------------------------------------------------------------------------------------------- eight bits
 
 INT8 = [  # type, rows, inner, outer, pad, bias, residual

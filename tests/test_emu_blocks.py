@@ -147,6 +147,10 @@ def test_update_special(run):
     cases.check_update_special(run)
 
 
+def test_update_rounds_once(run):
+    cases.check_update_rounds_once(run)
+
+
 def test_update_orthogonal(run):
     cases.check_update_orthogonal(run)
 
