@@ -291,7 +291,8 @@ __device__ __forceinline__ void sum_parts(const double* parts, u32 count, size_t
 #pragma unroll
     for (u32 e = 0; e < E; ++e) s[e] += parts[p * each + at + e * apart];
 }
-__device__ __forceinline__ double factor_of(double squares, double eps) { return 1.0 / (sqrt(squares) + eps); }
+// (of a matrix of zeros 0: 1 / eps may be infinite)
+__device__ __forceinline__ double factor_of(double squares, double eps) { return squares == 0.0 ? 0.0 : 1.0 / (sqrt(squares) + eps); }
 
 // One tile of x y, N elements each of rows i of x and j of y: lane l takes elements 8 t + 2 (l / 16) and the next of row l % 16 of both.
 template <u32 N>

@@ -347,6 +347,19 @@ def check_update_rounds_once(run):
         assert float(got[0]) == math.inf and torch.equal(got[1:4], base[0, 0, 1:4]) and bool(got[4].isnan())
 
 
+def check_update_zeros(run):
+    """A matrix of zeros gives zeros with the least eps there is and whatever the steps raise, and leaves the others alone."""
+    for rows, cols in ((5, 40), (900, 6), (20, 41), (70, 80)):
+        g = torch.randn(3, rows, cols, generator=torch.Generator().manual_seed(rows))
+        g[1] = 0.0
+        for steps in ([QUINTIC] * 2, LISTS["8"], [(1e200, 0.0, 0.0), (1e-200, 0.0, 0.0)], [(1e200, 1e100, 0.0)] * 3):
+            got = run.orthogonal_update(g, None, 1.0, 1.0, steps, 5e-324)
+            assert not got[1].any()
+            if steps[0] == QUINTIC:
+                want, _ = update_longer(g[[0, 2]], steps, 0.0)
+                near(got[[0, 2]], want, 2 * ULP * want.abs() + 2.0 ** -31)
+
+
 # --------------------------------------------------------------------------------------------------- eight bits
 
 INT8 = [  # type, rows, inner, outer, pad, bias, residual

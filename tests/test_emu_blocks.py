@@ -151,6 +151,10 @@ def test_update_rounds_once(run):
     cases.check_update_rounds_once(run)
 
 
+def test_update_zeros(run):
+    cases.check_update_zeros(run)
+
+
 def test_update_orthogonal(run):
     cases.check_update_orthogonal(run)
 
