@@ -150,7 +150,7 @@ int haflo_residual_norm_backward(int type, const void* d_dh, size_t lddh, const 
  *   X = G / (|G|_F + eps);  for each step (a, b, c): K = X X^T, X <- a X + (b K + c K^2) X;   out = keep base + scale X
  * (of a matrix with more rows than columns K = X^T X, from the right). d_coefficients: host memory, steps x 3; five times
  * (3.4445, -4.7750, 2.0315) brings singular values between about 0.7 and 1.2, (1.5, -0.5, 0) towards 1. d_base NULL: none.
- * Matrices lie step_* elements apart. All products are held in 64 bits: X is off by some
+ * Matrices lie step_* elements apart; those of the result behind one another or with all their rows between each other's (else HAFLO_EINVAL). All products are held in 64 bits: X is off by some
  * 2^-53 of what the steps raise a direction by together (2^-29 of its greatest element for 512 and less). A list that raises by more
  * than 512 (five steps of 3.4445 do not) has K formed again from X on the way, by readings of G. A NaN or an infinity in a matrix makes its X NaN; one of
  * zeros gives X = 0. d_out may be d_g or d_base where all distances are the same (else HAFLO_EINVAL).

@@ -1093,7 +1093,8 @@ int haflo_orthogonal_update(int type, const void* d_g, size_t ldg, size_t step_g
   list.cuts = cuts_of(list);
   if (parties == 0) return HAFLO_OK;
   if (!d_g || ldg < cols || !d_out || ldo < cols || (d_base && ldb < cols) || ldo > kMostDistance) return HAFLO_EINVAL;
-  if (parties > 1 && step_o < (rows - 1) * ldo + cols) return HAFLO_EINVAL;  // matrices of the result over each other
+  // matrices of the result over each other: neither behind one another nor with rows between each other's
+  if (parties > 1 && step_o < (rows - 1) * ldo + cols && !(step_o >= cols && step_o <= ldo && (parties - 1) * step_o + cols <= ldo)) return HAFLO_EINVAL;
   if (!over(d_g, ldg, step_g, d_out, ldo, step_o, parties, rows) || !over(d_base, ldb, step_b, d_out, ldo, step_o, parties, rows)) return HAFLO_EINVAL;
   const Plan plan = update_plan(s);
   if (!enough(d_workspace, workspace_bytes, plan.total)) return HAFLO_EINVAL;

@@ -249,6 +249,26 @@ def test_int8_over_its_rows(run, case):
         assert torch.equal(got[:, :outer], want) and torch.equal(got[:, outer:], x[:, outer:])
 
 
+def test_update_interleaved(run):
+    """Matrices whose rows lie between each other's, as in rows x parties x cols, also over the operands; rows that overlap are refused."""
+    lib = run.lib
+    values = (C.c_double * 3)(*cases.QUINTIC)
+    for rows, cols in ((5, 40), (40, 5), (900, 16), (20, 30), (70, 66)):
+        g, held = cases.update_inputs("f32", 3, rows, cols, True, 0)
+        want = run.orthogonal_update(g, held, 0.9, -0.3, [cases.QUINTIC], 1e-7)
+        ws, nbytes = run.workspace(lib.haflo_update_workspace_bytes(0, 3, rows, cols))
+        between = lambda t: run.buf(t.transpose(0, 1).contiguous())  # noqa: E731
+        for over in (None, 0, 1):
+            b = [between(g), between(held)]
+            out = run.new(rows, 3, cols) if over is None else b[over]
+            call = lambda ldo, so: lib.haflo_orthogonal_update(0, b[0].p, 3 * cols, cols, b[1].p, 3 * cols, cols, 3, rows, cols, values, 1, 0.9, -0.3, 1e-7,  # noqa: E731
+                                                               out.p, ldo, so, ws.p, nbytes, None)
+            if over is None:
+                assert call(3 * cols - 1, cols) == -1 and call(3 * cols, cols - 1) == -1 and call(3 * cols, 2 * cols) == -1
+            assert call(3 * cols, cols) == 0
+            assert torch.equal(out.get().transpose(0, 1), want)
+
+
 def test_some_gradients(run):
     """Gradients that are not asked for change nothing about the others; what r has from elsewhere may be nothing."""
     lib = run.lib

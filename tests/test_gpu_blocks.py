@@ -298,6 +298,16 @@ def test_update_steps_again_and_in_a_graph(api):
             assert all(torch.equal(out, want) for _, out in graphs)
 
 
+def test_update_interleaved(api):
+    """Matrices whose rows lie between each other's, also over the gradient."""
+    for rows, cols in ((4, 256), (900, 16), (20, 300), (333, 100)):
+        g = torch.randn(rows, 5, cols, device="cuda").transpose(0, 1)
+        want = api.haflo_orthogonal_update(g.contiguous())
+        out = torch.zeros(rows, 5, cols, device="cuda").transpose(0, 1)
+        assert torch.equal(api.haflo_orthogonal_update(g, out=out), want)
+        assert torch.equal(api.haflo_orthogonal_update(g, out=g), want)
+
+
 def test_int8_over_its_rows(api):
     """A result over x, with x for a residual and without, and over a part of its columns."""
     for rows in (1, 2, 8, 16, 17, 40, 300):
