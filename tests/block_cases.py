@@ -173,6 +173,33 @@ def check_norm_gradients(run):
         assert abs(got - want) <= room < 0.1 * got
 
 
+SUMS = [(1, 3), (70, 40), (200, 260), (530, 2050), (100, 9001)]  # rows, cols
+SUMS_LARGE = [(3001, 1001), (5000, 520), (2100, 4096), (700, 8000), (1500, 9001), (263000, 5), (300001, 8)]  # blocks that take several sets of rows
+
+
+def check_norm_sums(run, rows, cols):
+    """Gradients summed over rows of whole numbers, where both norms are of rows of ones: every sum is exact, so no row may be missing or counted
+    twice."""
+    gen = torch.Generator().manual_seed(rows + cols)
+    whole = lambda lo, hi, *shape: torch.randint(lo, hi + 1, shape, generator=gen).float()  # noqa: E731
+    ones, eps = 2.0 * whole(0, 1, rows, cols) - 1.0, 2.0 ** -254
+    dh, dr, full = whole(-8, 8, rows, cols), whole(-8, 8, rows, cols), whole(-2, 2, rows, cols)
+    post, gate, kind = 2.0 ** whole(-2, 2, cols), whole(1, 5, cols), torch.bfloat16 if cols % 2 else torch.float32
+    to = lambda *t: tuple(v.to(kind) for v in t)  # noqa: E731
+    x, f, dr, full, dh = to(whole(-3, 3, rows, cols), ones, dr, full, dh)
+    _, _, rstd = run.residual_norm(x, f, post, gate, None, 1.0, eps)
+    assert bool((rstd == 1.0).all())
+    _, _, dpost, dgate, _ = run.residual_norm_backward(None, dr, x, f, post, gate, None, rstd, 1.0)
+    part = (dr.double() * f.double()).sum(0)
+    assert torch.equal(dpost.double(), part * gate) and torch.equal(dgate.double(), part * post)
+    _, _, dpost, dgate, _ = run.residual_norm_backward(None, dr, x, f, post, full, None, rstd, 1.0)
+    assert torch.equal(dpost.double(), (dr.double() * full.double() * f.double()).sum(0))
+    assert torch.equal(dgate.double(), dr.double() * f.double() * post)
+    _, _, rstd = run.residual_norm(f, None, None, None, post, 1.0, eps)
+    dpre = run.residual_norm_backward(dh, dr, f, None, None, None, post, rstd, 1.0)[4]
+    assert torch.equal(dpre.double(), (dh.double() * f.double()).sum(0))
+
+
 # --------------------------------------------------------------------------------------------------- orthogonalised updates
 
 QUINTIC, CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
@@ -479,6 +506,12 @@ def check_int8_scales(run, rows, inner, outer):
     wq, ws = run.quantize_rows(torch.full((outer, inner), 2.0 ** 127))
     assert not run.int8_forward(torch.full((rows, inner), 2.0 ** -149), wq, ws, None, None).any()
 
+
+INT8_WIDE = [  # more outputs than a common model's width: rows that the multiplying blocks bring to eight bits themselves, and one more
+    ("bf16", 1, 130, 4100, 0, True, True), ("f32", 3, 2050, 4113, 1, False, False), ("f16", 4, 1001, 5000, 0, True, False), ("bf16", 5, 520, 4097, 0, False, True),
+    ("f32", 16, 100, 4096, 0, True, False), ("f32", 4, 300, 8192, 0, False, True), ("bf16", 4, 140, 8193, 0, True, False), ("f16", 1, 300, 8193, 0, False, False),
+]
+INT8_WIDE_LARGE = [("bf16", 1, 4096, 32000, 0, False, False), ("f16", 2, 8192, 20001, 0, True, True), ("bf16", 4, 2048, 128000, 0, False, False)]
 
 # --------------------------------------------------------------------------------------------------- each kernel form
 

@@ -125,6 +125,11 @@ def test_norm_far(run):
     cases.check_norm_far(run)
 
 
+@pytest.mark.parametrize("case", cases.SUMS, ids=str)
+def test_norm_sums(run, case):
+    cases.check_norm_sums(run, *case)
+
+
 def test_norm_gradients(run):
     cases.check_norm_gradients(run)
 
@@ -176,6 +181,11 @@ def test_int8(run, case):
 @pytest.mark.parametrize("case", cases.INT8_SCALES, ids=str)
 def test_int8_scales(run, case):
     cases.check_int8_scales(run, *case)
+
+
+@pytest.mark.parametrize("case", cases.INT8_WIDE, ids=str)
+def test_int8_wide(run, case):
+    cases.check_int8(run, *case)
 
 
 def test_int8_limits(run):
@@ -435,3 +445,18 @@ def test_norm_forms(run, kind):
     for case in cases.norm_forms(kind):
         if case[2] <= 1500 or (kind == "bf16" and case[2] % 4 != 1):
             cases.check_norm(run, *case)
+
+
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_update_forms(run, kind, tall):
+    for n, case in enumerate(cases.update_forms(kind, tall)):
+        if n % 3 == ("f32", "f16", "bf16").index(kind) and case[1] * case[2] * case[3] < 2 ** 16:  # (each size once over the types, but the largest)
+            cases.check_update(run, *case)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_int8_forms(run, kind):
+    for case in cases.int8_forms(kind):
+        if case[1] * case[2] * case[3] < 2 ** 23:
+            cases.check_int8(run, *case)

@@ -62,6 +62,11 @@ def test_norm_far(run):
     cases.check_norm_far(run)
 
 
+@pytest.mark.parametrize("case", cases.SUMS + cases.SUMS_LARGE, ids=str)
+def test_norm_sums(run, case):
+    cases.check_norm_sums(run, *case)
+
+
 def test_norm_gradients(run):
     cases.check_norm_gradients(run)
 
@@ -113,6 +118,11 @@ def test_int8(run, case):
 @pytest.mark.parametrize("case", cases.INT8_SCALES + cases.INT8_SCALES_LARGE, ids=str)
 def test_int8_scales(run, case):
     cases.check_int8_scales(run, *case)
+
+
+@pytest.mark.parametrize("case", cases.INT8_WIDE + cases.INT8_WIDE_LARGE, ids=str)
+def test_int8_wide(run, case):
+    cases.check_int8(run, *case)
 
 
 def test_int8_limits(run):
