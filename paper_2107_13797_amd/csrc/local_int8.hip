@@ -338,11 +338,19 @@ __global__ __launch_bounds__(kFewThreads) void k_int8_few(const T* xf, size_t ld
   }
 }
 
-constexpr size_t kFewRows = 32, kFewOuter = 4096, kFewBytes = 2048;
-bool own_rows(size_t rows, size_t cols, size_t outer) { return rows <= (outer <= kFewOuter ? 16 : 4) && rows * row_bytes(cols) <= kOwnBytes; }
-// One block for each compute unit at most, and rows long enough to split: then k_int8_few, else tiles of 64 x 64. Calls of few / of tiles, us, 5, 16
-// and 32 rows: 1024 to 1024 7.4 / 6.7, 8.4 / 6.9, 7.8 / 7.5; 2048 to 2048 7.5 / 8.0, 8.6 / 8.4, 7.8 / 9.0; 4096 to 1024 7.6 / 10.6, 8.6 / 10.9,
-// 10.3 / 11.5; 4096 to 4096 7.9 / 10.8, 8.8 / 11.0, 10.8 / 11.5, 48 rows 13.5 / 11.8; 4096 to 8192 11.5 / 11.9, 13.5 / 11.8, 16.2 / 12.5.
+constexpr size_t kFewRows = 32, kFewOuter = 4096, kFewBytes = 2048, kOwnOuter = 8192;
+// Rows that the blocks which multiply them bring to eight bits too: each block does so again, so that few rows for few blocks gain by the launch and the
+// workspace they are spared, and more lose. Graphs of the operator, us, this way / k_quantize before it, bfloat16, 1, 4, 5, 8 and 16 rows:
+// 2048 to 2048 5.2 / 6.8, 5.9 / 7.4, 6.3 / 7.4, 6.4 / 7.8, 8.2 / 8.6; 4096 to 4096 5.4 / 6.9, 6.5 / 7.5, 8.3 / 7.4, 8.7 / 7.9, 8.6 / 8.6 (where calls from
+// the host take 8.5 to 13 and the other way 13 or 17); 1 and 4 rows of 4096 to 8192 7.6 / 11.6, 9.3 / 11.6, to 16384 15.0 / 14.6, 17.5 / 15.2, to 32000
+// 24.3 / 23.5, 28.0 / 23.2, of 2048 to 128000 76 / 50, 82 / 50.
+bool own_rows(size_t rows, size_t cols, size_t outer) {
+  return rows <= (outer <= kFewOuter ? 16 : outer <= kOwnOuter ? 4 : 0) && rows * row_bytes(cols) <= kOwnBytes;
+}
+// Products of rows in eight bits: k_int8_few where there is one block for each compute unit at most, and rows are long enough to split, else tiles of
+// 64 x 64. Graphs of them, us, few / tiles, of 1, 16, 17, 32 and 48 rows: 1024 to 1024 4.4 / 4.4, 5.8 / 4.5, 4.3 / 4.8, 5.0 / 4.7, 5.0 / 4.7;
+// 2048 to 2048 4.4 / 5.7, 5.8 / 5.8, 4.4 / 6.0, 5.0 / 6.0, 5.1 / 6.0; 4096 to 4096 4.7 / 8.4, 6.1 / 8.4, 6.8 / 8.7, 8.1 / 8.6, 12.2 / 8.7; 4096 to 8192
+// 7.7 / 9.0, 10.4 / 9.0, 10.7 / 9.3, 13.2 / 9.4, 21.3 / 9.4.
 bool few_rows(size_t rows, size_t width, size_t outer) { return rows <= kFewRows && outer <= kFewOuter && width >= kFewBytes; }
 template <class T>
 void few(const T* x, size_t ldx, size_t cols, const int8_t* xq, const int8_t* w, const Out<T>& to, hipStream_t st) {
