@@ -194,7 +194,7 @@ __device__ __forceinline__ void store_results(const Out<T>& to, u32 t0, u32 o0, 
 
 // A block takes TM rows by TN outputs, its WM x WN wavefronts a part of that each in products of 16 x 16. Two steps' tiles lie in LDS, and one
 // is filled while the other is read; of tiles of 64 x 64 four steps' (4096 to 4096, 128 rows 19.8 us by two and 12.6 by four). Matrix
-// instructions bound the large tiles: 8192 of 4096 to 4096 112 us, 2450 TOP/s (a library product of these numbers 129 us), busy in two thirds
+// instructions bound the large tiles: 8192 of 4096 to 4096 113 to 117 us, 2350 to 2430 TOP/s (a library product of these numbers 129 us), busy in two thirds
 // of the cycles; the wait for loads the small ones (64 rows 9.2 us).
 template <class T, int TM, int TN, int WM, int WN, bool FAR>
 __global__ __launch_bounds__(WM * WN * kWave) void k_int8(const int8_t* x, const int8_t* w, u32 width, Out<T> to, u32 x_bytes, u32 w_bytes, u32 first_block) {

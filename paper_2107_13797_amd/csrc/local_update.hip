@@ -468,7 +468,8 @@ __global__ __launch_bounds__(step_threads<KT>()) void k_steps(const double* part
 
 // K of X = P G: a wavefront forms X on sixteen places of the long side, as the transpose, whose results lie in registers as the products by
 // themselves take them, and rows FROM .. TO - 1 of tiles of X X^T from it. R is P transposed, rows N + 2 apart in LDS. Pieces piece, piece + stride ..
-// below end. It is a part of lists that most calls do not have, and is kept simple: loads are waited for.
+// below end. It is a part of lists that most calls do not have, and is kept simple: its loads are waited for (64 matrices of 4096 x 64 float32
+// 90 us a part, of 128 x 4096 615, of which matrix instructions are 44 and 250).
 constexpr int tiles_below(int rows) { return rows * (rows + 1) / 2; }
 template <class T, int KT, bool TALL, int FROM, int TO, int COUNT>
 __device__ __forceinline__ void gram_again(const T* m, size_t ld, const double* R, u32 k, u32 length, u32 piece, u32 end, u32 stride, f64x4 (&acc)[COUNT]) {
@@ -889,7 +890,9 @@ Plan update_plan(const Shape& s) {
   // Parts of K_0's sums: enough for all compute units, and no more chunks to one than hide the first loads; but whoever joins the parts reads them
   // all. Calls, us, with at most an 8th / a 4th / a 16th of the chunks' number: 7 of 1001 x 37 float32 35.3 / 34.5 / 38.5, 8 of 64 x 4096 (parts of
   // 4 chunks and more: 32) 64.3 / 69.1 / 65.9, 2 of 64 x 10000 76.6 / 93.1 / 72.8 (40, 79 and 20 parts), 3001 x 100 121 / 109 / 153, 8 of
-  // 4096 x 32 22.4 / 23.1 / 23.4. All matrices' parts: of 64 of 16 x 4096 28 with 1024, 23 with 512; 300 of them 67 and 72, with 256 77.
+  // 4096 x 32 22.4 / 23.1 / 23.4. All matrices' parts: of 64 of 16 x 4096 28 with 1024, 23 with 512; 300 of them 67 and 72, with 256 77. Of more than 32 rows with 256 / 512 /
+  // 1024: 16 of 64 x 4096 74 / 81 / 81, 64 of them 118 / 120 / 132, of 128 x 4096 506 / 525 / 553, of 48 x 2000 54 / 56 / 62; but 300 of 64 x 4096
+  // 510 / 495 / 491, of 128 x 4096 2690 / 2500 / 2420.
   const u32 tiles = s.tiles();
   const size_t chunks = ceil_div(s.length, kChunk), want = ceil_div((size_t)(tiles <= 2 ? 512 : 256), s.parties ? s.parties : 1);
   size_t most = ceil_div(chunks, tiles <= 2 ? 8 : 4);
